@@ -76,7 +76,7 @@ def draw(rng):
                     kv_heads=kv_heads, dim=dim, causal=rng.random() < 0.7, ragged=rng.random() < 0.4)
     vocab = _log(rng, 100, 200000)
     act = rng.choice(("f32", "bf16"))
-    rows = _log(rng, 1, min(16384, (1 << 28) // vocab))
+    rows = _log(rng, 1, min(16384, 800_000_000 // (vocab * SIZE[act])))
     return dict(op=op, way=rng.choice(("forward", "backward", "step", "step")), rows=rows, vocab=vocab,
                 top=min(vocab // 2, _log(rng, 1, 256)), act=act, index=index, temperature=rng.choice((1.0, 2.0, 4.0)))
 
