@@ -69,11 +69,12 @@ def draw(rng):
         heads = kv_heads * rng.choice((1, 2, 3, 4))
         dim = rng.choice((64, 128, 8 * rng.randint(2, 16)))
         batch = rng.choice((1, 2, 3, 5, 8))
-        most = min(8192, int(math.sqrt((1 << 30) / (batch * heads))))
+        causal = rng.random() < 0.7
+        most = min(8192, int(math.sqrt((1 << (30 if causal else 29)) / (batch * heads))))
         q_len = _log(rng, 1, most)
         kv_len = q_len if rng.random() < 0.7 else _log(rng, 1, most)
         return dict(op=op, way=rng.choice(("forward", "backward")), batch=batch, q_len=q_len, kv_len=kv_len, heads=heads,
-                    kv_heads=kv_heads, dim=dim, causal=rng.random() < 0.7, ragged=rng.random() < 0.4)
+                    kv_heads=kv_heads, dim=dim, causal=causal, ragged=rng.random() < 0.4)
     vocab = _log(rng, 100, 200000)
     act = rng.choice(("f32", "bf16"))
     rows = _log(rng, 1, min(16384, 800_000_000 // (vocab * SIZE[act])))
