@@ -387,6 +387,79 @@ int omni_last_cuda_error(const omni_ctx *ctx);
 int omni_query_launch(omni_ctx *ctx, int32_t K, int32_t grad_dtype, int32_t *grid, int32_t *block);
 uint64_t omni_kernel_launches(const omni_ctx *ctx);
 
+/* ==================================================================================================
+ * Operators of a language model's training pass: what a worker computes its gradients with.  The
+ * embedding at the bottom (its dense gradient is a slice of a gradient bucket), attention in the
+ * blocks, the distillation loss on top.  They take the context of the step for their launches,
+ * their errors and the status word of bounded waits; scratch memory is the caller's (a query
+ * function gives its size), so calls on different streams are independent as long as their
+ * buffers are.  Kernels are enqueued on `stream`; nothing synchronises.  Sums, norms and softmax
+ * statistics are float; a result is rounded once where it is stored.  No result depends on the
+ * order of atomics: the same call gives the same bits.
+ * Strides are in elements; the last dimension is contiguous.  "dtype" is an omni_dtype.
+ * ================================================================================================== */
+typedef enum { OMNI_I32 = 0, OMNI_I64 = 1 } omni_index;   /* type of token and vocabulary indices */
+
+/* Embedding lookup: out_i = scale * table_{tokens[i]}, i = 0..n-1, computed in float and rounded to
+ * out_dtype.  A token outside 0..vocab-1 gives a row of zeros.  tokens: device, n contiguous
+ * indices; table: device, vocab rows of dim elements, table_stride apart; out: device, n rows.
+ * Any dim and any stride >= dim; pointers need the alignment of their elements (rows on 16-byte
+ * boundaries with dim a multiple of 8 run with wide accesses).
+ * Errors: NULL, BAD_CONFIG (dtype, dim or vocab < 1, stride < dim), ALIGN, TOO_LARGE (n >= 2^31), CUDA. */
+int omni_embed_forward(omni_ctx *ctx, const void *tokens, int32_t index_type, uint64_t n, const void *table,
+                       int32_t table_dtype, uint64_t table_stride, int32_t vocab, int32_t dim, float scale, void *out,
+                       int32_t out_dtype, uint64_t out_stride, void *stream);
+
+/* Gradient of the lookup, dense, as a gradient bucket wants it:
+ *   grad_v = (accumulate ? grad_v : 0) + scale * sum over i with tokens[i] = v of grad_out_i
+ * for every v = 0..vocab-1.  The tokens are sorted on the device (stable, so that a row's terms are
+ * added in ascending i within blocks of 32 sorted tokens, and the blocks in order) and each row is written once; rows no token names become zero (untouched with
+ * accumulate).  `padding` is a token without gradient (-1: none); tokens outside 0..vocab-1 have none
+ * either.  grad_out: device, n rows of dim; grad: device, vocab rows of dim, not overlapping.
+ * workspace: device, 16-byte aligned, at least omni_embed_workspace() bytes; its contents are free
+ * again when the stream has executed the call.
+ * Errors: as omni_embed_forward; TOO_LARGE also for a workspace below the size asked for. */
+int omni_embed_workspace(uint64_t n, int32_t vocab, int32_t dim, uint64_t *bytes);
+int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, uint64_t n, const void *grad_out,
+                        int32_t grad_out_dtype, uint64_t grad_out_stride, int32_t vocab, int32_t dim, float scale,
+                        int64_t padding, void *grad, int32_t grad_dtype, uint64_t grad_stride, int32_t accumulate,
+                        void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* Distillation from a teacher's top logits.  Per row, with temperature T, the student's logits z over
+ * the vocabulary and the teacher's logits t_j at the indices i_j, j = 0..top-1:
+ *   p = softmax(t / T) over the row's entries;  lse = log sum_v exp(z_v / T)
+ *   loss = T^2 * sum_j p_j * (log p_j - z_{i_j} / T + lse)               (KL divergence, times T^2)
+ *   grad_v = grad_loss * T * (exp(z_v / T - lse) - sum over j with i_j = v of p_j)
+ * An entry whose index is outside 0..vocab-1 (-1 by convention) is not there, one whose logit is -inf
+ * has p = 0; a row without any p > 0 has no target: its loss is 0 and its gradient row is zeros (lse
+ * is still written).  A student logit of -inf has probability 0 (and an infinite loss if the teacher
+ * gives it p > 0).  top = 1 with T = 1 is the ordinary cross-entropy of the index.
+ * top_logits: device float; top_index: device, both rows of `top` elements, top_stride apart. */
+typedef struct {
+    const void *logits;     /* device, rows x vocab of dtype */
+    uint64_t rows, row_stride;
+    int32_t vocab, dtype;
+    const float *top_logits;
+    const void *top_index;  /* of index_type */
+    uint64_t top_stride;
+    int32_t top, index_type;
+    float temperature;      /* > 0 */
+} omni_distill;
+#define OMNI_DISTILL_MAX_TOP 256
+/* omni_distill_forward: loss[rows] and lse[rows] (device float).
+ * omni_distill_backward: grad (rows x vocab of the logits' dtype, grad_stride apart) from the kept lse
+ * and grad_loss[rows] (device float; 0 for rows that do not count).  grad may be the logits' own
+ * storage (same pointer and stride): each value is read before it is overwritten.
+ * omni_distill_step: both in one pass over the logits (one read, one write), for a caller that knows
+ * grad_loss beforehand, as with a mean over rows.
+ * Errors: NULL, BAD_CONFIG (dtype, vocab or top < 1, temperature not finite or <= 0, a stride below the
+ * row), ALIGN, TOO_LARGE (top > OMNI_DISTILL_MAX_TOP, rows >= 2^31), CUDA. */
+int omni_distill_forward(omni_ctx *ctx, const omni_distill *d, float *loss, float *lse, void *stream);
+int omni_distill_backward(omni_ctx *ctx, const omni_distill *d, const float *lse, const float *grad_loss, void *grad,
+                          uint64_t grad_stride, void *stream);
+int omni_distill_step(omni_ctx *ctx, const omni_distill *d, const float *grad_loss, float *loss, float *lse, void *grad,
+                      uint64_t grad_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,7 @@ MAX_K = 32
 TAU_BINS = 33
 BSP, ASP = 0, 1
 F32, BF16 = 0, 1
+I32, I64 = 0, 1
 UNSCALED_MEAN, ASP_NO_LR_SCALE, INPUT_IS_TIME, BULK_COPY, NO_BULK_COPY = 1, 2, 4, 8, 16
 CONSERVE_MULTIPLICATIVE = 32
 DEFAULT_FLAGS = 0  # OR-ed into every new context's flags (the tests use it to force a kernel family)
@@ -33,6 +34,8 @@ EXPORTS = (
     "omni_ctl_to_device", "omni_ctl_from_device", "omni_rebatch_device", "omni_aggregate_bsp_device_batches",
     "omni_shard_range", "omni_asp_push_pull", "omni_ctl_export", "omni_ctl_import", "omni_step_bsp",
     "omni_asp_report_device",
+    "omni_embed_forward", "omni_embed_workspace", "omni_embed_backward",
+    "omni_distill_forward", "omni_distill_backward", "omni_distill_step",
 )
 MAX_ASP_BATCH = 16
 NOALLOC_MAX_BUCKETS = 8
@@ -53,6 +56,12 @@ class omni_stats(C.Structure):
     _fields_ = [("grad_sqnorm", C.c_double), ("weight_sum", C.c_double), ("steps", C.c_uint64),
                 ("arrivals", C.c_uint64), ("tau_hist", C.c_uint64 * TAU_BINS), ("tau_max", C.c_int32),
                 ("tau_sum", C.c_uint64)]
+
+
+class omni_distill(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("rows", C.c_uint64), ("row_stride", C.c_uint64), ("vocab", C.c_int32),
+                ("dtype", C.c_int32), ("top_logits", C.c_void_p), ("top_index", C.c_void_p), ("top_stride", C.c_uint64),
+                ("top", C.c_int32), ("index_type", C.c_int32), ("temperature", C.c_float)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -102,6 +111,13 @@ def lib() -> C.CDLL:
     L.omni_kernel_launches.restype = C.c_uint64
     L.omni_aggregate_bsp_noalloc.argtypes = [i32, C.POINTER(omni_bucket), i32, i32, C.POINTER(i32), C.c_uint32,
                                              f32, f32, f32, vp, vp]
+    u64, i64 = C.c_uint64, C.c_int64
+    L.omni_embed_forward.argtypes = [vp, vp, i32, u64, vp, i32, u64, i32, i32, f32, vp, i32, u64, vp]
+    L.omni_embed_workspace.argtypes = [u64, i32, i32, C.POINTER(u64)]
+    L.omni_embed_backward.argtypes = [vp, vp, i32, u64, vp, i32, u64, i32, i32, f32, i64, vp, i32, u64, i32, vp, u64, vp]
+    L.omni_distill_forward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp]
+    L.omni_distill_backward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp, u64, vp]
+    L.omni_distill_step.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp, vp, u64, vp]
     _lib = L
     return L
 

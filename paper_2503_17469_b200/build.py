@@ -12,9 +12,9 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libomni.so"
 SOURCES = [CSRC / "omni.cu", CSRC / "register_dispatch.cu", CSRC / "bulk_dispatch.cu", CSRC / "device_controller.cu", CSRC / "noalloc.cu",
-           CSRC / "controller.cpp", CSRC / "shard.cpp"]
+           CSRC / "controller.cpp", CSRC / "shard.cpp", CSRC / "embed.cu", CSRC / "distill.cu"]
 HEADERS = [CSRC / "kernels.cuh", CSRC / "tma_kernels.cuh", CSRC / "dispatch.h", CSRC / "controller.h",
-           CSRC / "device_controller.h", PKG.parent / "include" / "omni.h"]
+           CSRC / "device_controller.h", CSRC / "context.h", CSRC / "vector.cuh", PKG.parent / "include" / "omni.h"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

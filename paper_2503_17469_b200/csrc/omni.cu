@@ -5,6 +5,7 @@
 #include <cstring>
 #include <new>
 
+#include "context.h"
 #include "controller.h"
 #include "device_controller.h"
 #include "dispatch.h"
@@ -287,6 +288,26 @@ int enqueue_bsp(omni_ctx *ctx, const omni_bucket *buckets, int32_t n_buckets, in
 }
 
 }  // namespace
+
+int context_bind(omni_ctx *ctx, ContextDevice *out)
+{
+    const int rc = ensure_device(ctx);
+    if (rc != OMNI_OK) return rc;
+    out->sm_count = ctx->sm_count;
+    out->status = &ctx->ws->status;
+    return OMNI_OK;
+}
+
+int context_launched(omni_ctx *ctx, int cuda_error)
+{
+    if (cuda_error != 0) {
+        ctx->last_cuda = cuda_error;
+        return OMNI_ERR_CUDA;
+    }
+    ctx->launches += 1;
+    return OMNI_OK;
+}
+
 }  // namespace omni
 
 using namespace omni;
