@@ -425,6 +425,45 @@ int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, u
                         int64_t padding, void *grad, int32_t grad_dtype, uint64_t grad_stride, int32_t accumulate,
                         void *workspace, uint64_t workspace_bytes, void *stream);
 
+/* Attention over [batch, length, head, dim] bfloat16 tensors, softmax in float:
+ *   S = scale * Q K^T;  a query i of a sequence sees the keys j < kv length, with `causal` only those
+ *   j <= i + (kv length - q length): the two sequences are aligned at their ends.
+ *   lse_i = log sum_j exp(S_ij) over the keys seen;  O_i = sum_j exp(S_ij - lse_i) V_j
+ * A query that sees no key has O = 0 and lse = -inf, and takes part in no gradient.  heads may be a
+ * multiple of kv_heads: query head h uses key head h / (heads / kv_heads), whose gradients are summed.
+ * q_lengths, kv_lengths: device int32[batch] or NULL, the lengths of a padded batch (clamped to
+ * 0..q_len, 0..kv_len); what stands behind them in the inputs (NaN included) is not used, outputs there are 0 (lse: -inf).
+ * dim: a multiple of 8 up to OMNI_ATTN_MAX_DIM; scale > 0. */
+typedef struct {
+    int32_t batch, q_len, kv_len, heads, kv_heads, dim;
+    int32_t causal;
+    float scale;
+    const int32_t *q_lengths, *kv_lengths;
+} omni_attn;
+/* One operand: element (b, i, h, c) at data[b * batch + i * row + h * head + c].  data 16-byte aligned,
+ * strides multiples of 8 elements (those of an extent of one do not matter). */
+typedef struct {
+    void *data;
+    uint64_t batch, row, head;
+} omni_attn_view;
+#define OMNI_ATTN_MAX_DIM 128
+/* omni_attn_forward writes out and lse (device float [batch, heads, q_len], contiguous).
+ * omni_attn_backward recomputes the probabilities from lse:
+ *   P = exp(S - lse), D_i = sum_c dO_ic O_ic, dS = P (dO V^T - D)
+ *   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+ * with P and dS rounded to bfloat16 for the products and every sum in float, in a fixed order.
+ * workspace: device, 16-byte aligned, omni_attn_workspace() bytes.  Inputs and outputs do not overlap.
+ * Errors: NULL, BAD_CONFIG (negative sizes, heads not a multiple of kv_heads, dim, scale, a stride below dim), ALIGN,
+ * TOO_LARGE (dim, batch or heads > 65535, lengths > 2^30, a workspace below the size asked for), CUDA;
+ * a bounded wait of the kernels that runs out surfaces as TIMEOUT from omni_get_stats. */
+int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
+                      const omni_attn_view *v, const omni_attn_view *out, float *lse, void *stream);
+int omni_attn_workspace(const omni_attn *a, uint64_t *bytes);
+int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
+                       const omni_attn_view *v, const omni_attn_view *out, const float *lse, const omni_attn_view *dout,
+                       const omni_attn_view *dq, const omni_attn_view *dk, const omni_attn_view *dv, void *workspace,
+                       uint64_t workspace_bytes, void *stream);
+
 /* Distillation from a teacher's top logits.  Per row, with temperature T, the student's logits z over
  * the vocabulary and the teacher's logits t_j at the indices i_j, j = 0..top-1:
  *   p = softmax(t / T) over the row's entries;  lse = log sum_v exp(z_v / T)

@@ -35,6 +35,7 @@ EXPORTS = (
     "omni_shard_range", "omni_asp_push_pull", "omni_ctl_export", "omni_ctl_import", "omni_step_bsp",
     "omni_asp_report_device",
     "omni_embed_forward", "omni_embed_workspace", "omni_embed_backward",
+    "omni_attn_forward", "omni_attn_workspace", "omni_attn_backward",
     "omni_distill_forward", "omni_distill_backward", "omni_distill_step",
 )
 MAX_ASP_BATCH = 16
@@ -56,6 +57,16 @@ class omni_stats(C.Structure):
     _fields_ = [("grad_sqnorm", C.c_double), ("weight_sum", C.c_double), ("steps", C.c_uint64),
                 ("arrivals", C.c_uint64), ("tau_hist", C.c_uint64 * TAU_BINS), ("tau_max", C.c_int32),
                 ("tau_sum", C.c_uint64)]
+
+
+class omni_attn(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_len", C.c_int32), ("kv_len", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("dim", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float),
+                ("q_lengths", C.c_void_p), ("kv_lengths", C.c_void_p)]
+
+
+class omni_attn_view(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_uint64), ("row", C.c_uint64), ("head", C.c_uint64)]
 
 
 class omni_distill(C.Structure):
@@ -115,6 +126,10 @@ def lib() -> C.CDLL:
     L.omni_embed_forward.argtypes = [vp, vp, i32, u64, vp, i32, u64, i32, i32, f32, vp, i32, u64, vp]
     L.omni_embed_workspace.argtypes = [u64, i32, i32, C.POINTER(u64)]
     L.omni_embed_backward.argtypes = [vp, vp, i32, u64, vp, i32, u64, i32, i32, f32, i64, vp, i32, u64, i32, vp, u64, vp]
+    at, view = C.POINTER(omni_attn), C.POINTER(omni_attn_view)
+    L.omni_attn_forward.argtypes = [vp, at, view, view, view, view, vp, vp]
+    L.omni_attn_workspace.argtypes = [at, C.POINTER(u64)]
+    L.omni_attn_backward.argtypes = [vp, at, view, view, view, view, vp, view, view, view, view, vp, u64, vp]
     L.omni_distill_forward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp]
     L.omni_distill_backward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp, u64, vp]
     L.omni_distill_step.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp, vp, u64, vp]

@@ -1,0 +1,219 @@
+// C ABI of attention: argument checks, tensor maps, launches.
+#include <cmath>
+#include <cstring>
+
+#include "attention_backward.cuh"
+#include "attention_forward.cuh"
+#include "context.h"
+#include "vector.cuh"
+
+namespace omni {
+namespace {
+
+bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+uint64_t round_up(uint64_t x, uint64_t m) { return (x + m - 1) / m * m; }
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder, through the runtime (the library does not link libcuda).
+int encoder(omni_ctx *ctx, EncodeTiled *out)
+{
+    static EncodeTiled found = nullptr;     // the same address whoever looks it up first
+    if (!found) {
+        void *fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+        if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn)
+            return context_launched(ctx, e != cudaSuccess ? int(e) : int(cudaErrorSymbolNotFound));
+        found = reinterpret_cast<EncodeTiled>(fn);
+    }
+    *out = found;
+    return OMNI_OK;
+}
+
+// View as (column, head, row, batch) with boxes of 64 columns x `rows` rows of one head.
+int make_map(omni_ctx *ctx, EncodeTiled encode, CUtensorMap *map, const omni_attn_view &v, int dim, int heads, int len,
+             int batch, int rows)
+{
+    const cuuint64_t extent[4] = {cuuint64_t(dim), cuuint64_t(heads), cuuint64_t(len), cuuint64_t(batch)};
+    // the stride of an extent of one is never used, but has to be a legal one
+    const cuuint64_t strides[3] = {heads > 1 ? v.head * 2 : 16, len > 1 ? v.row * 2 : 16, batch > 1 ? v.batch * 2 : 16};
+    const cuuint32_t box[4] = {64, 1, cuuint32_t(rows), 1}, step[4] = {1, 1, 1, 1};
+    const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.data, extent, strides, box, step,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? OMNI_OK : context_launched(ctx, int(cudaErrorInvalidValue));
+}
+
+int check_shape(const omni_attn *a)
+{
+    if (!a) return OMNI_ERR_NULL;
+    if (a->batch < 0 || a->q_len < 0 || a->kv_len < 0 || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads != 0)
+        return OMNI_ERR_BAD_CONFIG;
+    if (a->dim < 8 || a->dim % 8 != 0 || !(a->scale > 0.0f) || !std::isfinite(a->scale)) return OMNI_ERR_BAD_CONFIG;
+    if (a->dim > OMNI_ATTN_MAX_DIM || a->batch > 65535 || a->heads > 65535 || a->q_len > (1 << 30) || a->kv_len > (1 << 30))
+        return OMNI_ERR_TOO_LARGE;
+    if (!aligned(a->q_lengths, 4) || !aligned(a->kv_lengths, 4)) return OMNI_ERR_ALIGN;
+    return OMNI_OK;
+}
+
+// A tensor of `len` rows per sequence: present, 16-byte aligned, strides of whole 16 bytes within what a tensor map takes.
+int check_view(const omni_attn_view *v, int dim, int heads, int len, int batch)
+{
+    if (!v) return OMNI_ERR_NULL;
+    if (len == 0 || batch == 0) return OMNI_OK;
+    if (!v->data) return OMNI_ERR_NULL;
+    if (!aligned(v->data, 16)) return OMNI_ERR_ALIGN;
+    const uint64_t strides[3] = {v->head, v->row, v->batch};
+    const int extents[3] = {heads, len, batch};
+    for (int i = 0; i < 3; ++i) {
+        if (extents[i] == 1) continue;
+        if (strides[i] % 8 != 0) return OMNI_ERR_ALIGN;
+        if (strides[i] < uint64_t(dim)) return OMNI_ERR_BAD_CONFIG;
+        if (strides[i] >= (1ull << 38)) return OMNI_ERR_TOO_LARGE;
+    }
+    return OMNI_OK;
+}
+
+AttnShape shape_of(const omni_attn *a)
+{
+    return {a->batch, a->heads, a->kv_heads, a->dim, a->q_len, a->kv_len, a->causal != 0, a->scale, a->q_lengths, a->kv_lengths};
+}
+OutView out_of(const omni_attn_view *v)
+{
+    return {static_cast<__nv_bfloat16 *>(v->data), (long long)v->batch, (long long)v->row, (long long)v->head};
+}
+
+// One launch of a kernel that takes its parameter block by value, with its shared memory opted in.
+template <typename P> int launch(omni_ctx *ctx, void (*kernel)(P), dim3 grid, int threads, int smem, cudaStream_t s, const P &p)
+{
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return context_launched(ctx, int(e));
+    void *args[] = {const_cast<P *>(&p)};
+    e = cudaLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), args, smem, s);
+    return context_launched(ctx, int(e));
+}
+
+int q_pad_of(const omni_attn *a) { return int(round_up(uint64_t(a->q_len), kRows)); }
+
+}  // namespace
+}  // namespace omni
+
+using namespace omni;
+
+extern "C" {
+
+int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
+                      const omni_attn_view *v, const omni_attn_view *out, float *lse, void *stream)
+{
+    if (!ctx) return OMNI_ERR_NULL;
+    int rc = check_shape(a);
+    if (rc != OMNI_OK) return rc;
+    const omni_attn_view *qs[2] = {q, out}, *ks[2] = {k, v};
+    for (const omni_attn_view *x : qs)
+        if ((rc = check_view(x, a->dim, a->heads, a->q_len, a->batch)) != OMNI_OK) return rc;
+    for (const omni_attn_view *x : ks)
+        if ((rc = check_view(x, a->dim, a->kv_heads, a->kv_len, a->batch)) != OMNI_OK) return rc;
+    if (a->q_len > 0 && a->batch > 0 && !lse) return OMNI_ERR_NULL;
+    if (!aligned(lse, 4)) return OMNI_ERR_ALIGN;
+    ContextDevice dev;
+    rc = context_bind(ctx, &dev);
+    if (rc != OMNI_OK || a->q_len == 0 || a->batch == 0) return rc;
+    EncodeTiled encode;
+    if ((rc = encoder(ctx, &encode)) != OMNI_OK) return rc;
+    AttnForwardParams p;
+    std::memset(&p, 0, sizeof p);
+    if ((rc = make_map(ctx, encode, &p.q, *q, a->dim, a->heads, a->q_len, a->batch, kRows)) != OMNI_OK) return rc;
+    if (a->kv_len > 0) {      // without keys no kernel touches their maps
+        if ((rc = make_map(ctx, encode, &p.k, *k, a->dim, a->kv_heads, a->kv_len, a->batch, kRows)) != OMNI_OK) return rc;
+        if ((rc = make_map(ctx, encode, &p.v, *v, a->dim, a->kv_heads, a->kv_len, a->batch, kRows)) != OMNI_OK) return rc;
+    }
+    p.s = shape_of(a);
+    p.out = out_of(out);
+    p.lse = lse;
+    p.status = dev.status;
+    const dim3 grid((a->q_len + 2 * kRows - 1) / (2 * kRows), a->heads, a->batch);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (a->dim <= 64) return launch(ctx, attention_forward_kernel<64>, grid, kForwardThreads, ForwardShared<64>::kBytes, s, p);
+    return launch(ctx, attention_forward_kernel<128>, grid, kForwardThreads, ForwardShared<128>::kBytes, s, p);
+}
+
+int omni_attn_workspace(const omni_attn *a, uint64_t *bytes)
+{
+    if (!bytes) return OMNI_ERR_NULL;
+    const int rc = check_shape(a);
+    if (rc != OMNI_OK) return rc;
+    *bytes = 2ull * a->batch * a->heads * q_pad_of(a) * sizeof(float);
+    return OMNI_OK;
+}
+
+int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
+                       const omni_attn_view *v, const omni_attn_view *out, const float *lse, const omni_attn_view *dout,
+                       const omni_attn_view *dq, const omni_attn_view *dk, const omni_attn_view *dv, void *workspace,
+                       uint64_t workspace_bytes, void *stream)
+{
+    if (!ctx) return OMNI_ERR_NULL;
+    int rc = check_shape(a);
+    if (rc != OMNI_OK) return rc;
+    const omni_attn_view *qs[4] = {q, out, dout, dq}, *ks[4] = {k, v, dk, dv};
+    for (const omni_attn_view *x : qs)
+        if ((rc = check_view(x, a->dim, a->heads, a->q_len, a->batch)) != OMNI_OK) return rc;
+    for (const omni_attn_view *x : ks)
+        if ((rc = check_view(x, a->dim, a->kv_heads, a->kv_len, a->batch)) != OMNI_OK) return rc;
+    uint64_t need = 0;
+    rc = omni_attn_workspace(a, &need);
+    if (rc != OMNI_OK) return rc;
+    if (need > 0 && (!lse || !workspace)) return OMNI_ERR_NULL;
+    if (!aligned(lse, 4) || !aligned(workspace, 16)) return OMNI_ERR_ALIGN;
+    if (workspace_bytes < need) return OMNI_ERR_TOO_LARGE;
+    ContextDevice dev;
+    rc = context_bind(ctx, &dev);
+    if (rc != OMNI_OK || a->batch == 0 || (a->q_len == 0 && a->kv_len == 0)) return rc;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int q_pad = q_pad_of(a);
+
+    AttnBackwardParams p;
+    std::memset(&p, 0, sizeof p);
+    p.s = shape_of(a);
+    p.row_lse = static_cast<float *>(workspace);
+    p.row_delta = p.row_lse + uint64_t(a->batch) * a->heads * q_pad;
+    p.q_pad = q_pad;
+    p.dq = out_of(dq);
+    p.dk = out_of(dk);
+    p.dv = out_of(dv);
+    p.status = dev.status;
+    if (a->q_len > 0) {
+        const AttnRowsParams r = {p.s, out_of(out), out_of(dout), lse, const_cast<float *>(p.row_lse),
+                                  const_cast<float *>(p.row_delta), q_pad};
+        rc = launch(ctx, attention_rows_kernel, dim3(q_pad / 16, a->heads, a->batch), 256, 0, s, r);
+        if (rc != OMNI_OK) return rc;
+    }
+    EncodeTiled encode;
+    if ((rc = encoder(ctx, &encode)) != OMNI_OK) return rc;
+    auto maps = [&](int q_rows, int kv_rows) {
+        int e = OMNI_OK;
+        if (a->q_len == 0 || a->kv_len == 0) return e;       // no pair of a query and a key: the maps are not touched
+        if ((e = make_map(ctx, encode, &p.q, *q, a->dim, a->heads, a->q_len, a->batch, q_rows)) != OMNI_OK) return e;
+        if ((e = make_map(ctx, encode, &p.dout, *dout, a->dim, a->heads, a->q_len, a->batch, q_rows)) != OMNI_OK) return e;
+        if ((e = make_map(ctx, encode, &p.k, *k, a->dim, a->kv_heads, a->kv_len, a->batch, kv_rows)) != OMNI_OK) return e;
+        return make_map(ctx, encode, &p.v, *v, a->dim, a->kv_heads, a->kv_len, a->batch, kv_rows);
+    };
+    if (a->kv_len > 0) {
+        if ((rc = maps(kPiece, kRows)) != OMNI_OK) return rc;
+        const dim3 grid((a->kv_len + kRows - 1) / kRows, a->kv_heads, a->batch);
+        rc = a->dim <= 64 ? launch(ctx, attention_keys_kernel<64>, grid, kBackwardThreads, KeysShared<64>::kBytes, s, p)
+                          : launch(ctx, attention_keys_kernel<128>, grid, kBackwardThreads, KeysShared<128>::kBytes, s, p);
+        if (rc != OMNI_OK) return rc;
+    }
+    if (a->q_len > 0) {
+        if ((rc = maps(kRows, kPiece)) != OMNI_OK) return rc;
+        const dim3 grid((a->q_len + kRows - 1) / kRows, a->heads, a->batch);
+        rc = a->dim <= 64 ? launch(ctx, attention_queries_kernel<64>, grid, kBackwardThreads, QueriesShared<64>::kBytes, s, p)
+                          : launch(ctx, attention_queries_kernel<128>, grid, kBackwardThreads, QueriesShared<128>::kBytes, s, p);
+    }
+    return rc;
+}
+
+}  // extern "C"

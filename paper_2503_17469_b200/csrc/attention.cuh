@@ -1,0 +1,113 @@
+// What the attention kernels share: shapes, lengths, loading of operand tiles.
+#pragma once
+#include <climits>
+
+#include "tensor_core.cuh"
+#include "vector.cuh"
+
+namespace omni {
+
+constexpr int kRows = 128;                    // rows of an MMA tile
+constexpr float kAttnLog2e = 1.4426950408889634f;
+constexpr float kAttnLn2 = 0.6931471805599453f;
+
+struct AttnShape {
+    int batch, heads, kv_heads, dim, q_len, kv_len, causal;
+    float scale;
+    const int *q_lengths, *kv_lengths;        // device, per sequence, or null
+};
+
+struct Lengths { int q, kv, shift; };         // query i sees keys j <= i + shift (causal)
+
+__device__ __forceinline__ Lengths lengths_of(const AttnShape &s, int b)
+{
+    Lengths l;
+    l.q = s.q_lengths ? min(max(s.q_lengths[b], 0), s.q_len) : s.q_len;
+    l.kv = s.kv_lengths ? min(max(s.kv_lengths[b], 0), s.kv_len) : s.kv_len;
+    l.shift = l.kv - l.q;
+    return l;
+}
+
+struct OutView { __nv_bfloat16 *data; long long batch, row, head; };
+
+// Rows x DP tile as blocks of 64 columns, each ROWS x 128 bytes.
+template <int DP, int ROWS>
+__device__ __forceinline__ void load_tile(unsigned char *dst, const CUtensorMap *map, int head, int row, int batch,
+                                          unsigned long long *bar)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) tensor_load(dst + c * ROWS * 128, map, c * 64, head, row, batch, bar);
+}
+
+// Zeroes rows [from, ROWS) of a tile, by one warp; the MMA that reads it next sees the zeros.  Rows
+// behind a sequence's length hold whatever the caller left there, and 0 x NaN would reach the sums.
+template <int DP, int ROWS> __device__ __forceinline__ void zero_rows(unsigned char *tile, int from)
+{
+    const int lane = threadIdx.x % 32;
+    for (int c = 0; c < DP / 64; ++c)
+        for (int i = from * 8 + lane; i < ROWS * 8; i += 32)
+            *reinterpret_cast<uint4 *>(tile + c * ROWS * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+    fence_async_proxy();
+    __syncwarp();
+}
+
+// d[128 x N] (+)= A B^T, both tiles with the contraction along their rows' DP columns; RA, RB rows per block.
+template <int DP, int RA, int RB, int N>
+__device__ __forceinline__ void mma_along(unsigned d, unsigned a, unsigned b, bool add)
+{
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const unsigned ka = a + (k / 4) * RA * 128 + (k % 4) * 32, kb = b + (k / 4) * RB * 128 + (k % 4) * 32;
+        mma_ss(d, tile_desc(ka, 1024, 16), tile_desc(kb, 1024, 16), mma_kind(N, false, false), add || k > 0);
+    }
+}
+// d[128 x DP] (+)= P B, P [128 x K] bfloat16 in tensor memory, B a tile of RB rows, of which K are contracted over.
+template <int DP, int RB, int K>
+__device__ __forceinline__ void mma_tmem_across(unsigned d, unsigned p, unsigned b, bool add)
+{
+#pragma unroll
+    for (int k = 0; k < K / 16; ++k)
+        mma_ts(d, p + k * 8, tile_desc(b + k * 2048, 1024, RB * 128), mma_kind(DP, false, true), add || k > 0);
+}
+
+__device__ __forceinline__ float attn_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Two floats to bfloat16, the first in the low half, in one instruction.
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// One row of `cols` float accumulators in tensor memory, times `gain`, to bfloat16 in global memory.
+template <int DP>
+__device__ __forceinline__ void store_row(unsigned tmem, float gain, __nv_bfloat16 *dst, int dim, bool write)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) {
+        uint32_t r[32];
+        tmem_load(r, tmem + c * 32);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int col = c * 32 + g * 8;
+            if (!write || col >= dim) continue;
+            uint4 o;
+            o.x = pack2(gain * __uint_as_float(r[g * 8 + 0]), gain * __uint_as_float(r[g * 8 + 1]));
+            o.y = pack2(gain * __uint_as_float(r[g * 8 + 2]), gain * __uint_as_float(r[g * 8 + 3]));
+            o.z = pack2(gain * __uint_as_float(r[g * 8 + 4]), gain * __uint_as_float(r[g * 8 + 5]));
+            o.w = pack2(gain * __uint_as_float(r[g * 8 + 6]), gain * __uint_as_float(r[g * 8 + 7]));
+            *reinterpret_cast<uint4 *>(dst + col) = o;
+        }
+    }
+}
+__device__ __forceinline__ void store_zeros(__nv_bfloat16 *dst, int dim)
+{
+    for (int c = 0; c < dim; c += 8) *reinterpret_cast<uint4 *>(dst + c) = make_uint4(0, 0, 0, 0);
+}
+
+}  // namespace omni

@@ -1,0 +1,231 @@
+// Attention, forward: O = softmax(scale Q K^T + mask) V in one pass over the keys, and the row's log-sum-exp.
+//
+// A CTA owns 256 query rows of one head as two tiles of 128, and streams key and value tiles of 128.
+// Per tile pair: S = Q K^T (tensor memory, float), a thread per row takes the row's running maximum m
+// and sum l, writes P = 2^(S - m) as bfloat16 over S, and O += P V with P straight from tensor memory.
+// The two tiles take turns: while the threads of one are at their exponentials, the tensor
+// core works for the other.  O stays in tensor memory; it is rescaled only when a row's maximum has grown by more than
+// 2^8 since its reference (the sum and O carry the same reference, so the result does not change, and
+// 2^8 times a tile's sum is far from float's range).  m, l and O are float; P is rounded to bfloat16, as the
+// tensor core multiplies that type.
+//
+// Warps 0-3: rows of tile 0, 4-7: rows of tile 1, 8: loads, 9: MMA.
+#pragma once
+#include "attention.cuh"
+
+namespace omni {
+
+struct AttnForwardParams {
+    CUtensorMap q, k, v;
+    AttnShape s;
+    OutView out;
+    float *lse;
+    unsigned *status;
+};
+
+constexpr int kForwardThreads = 320;
+constexpr float kRescaleAbove = 8.0f;
+
+template <int DP> struct ForwardShared {
+    static constexpr int kStages = DP == 128 ? 2 : 4;
+    static constexpr int kTile = kRows * DP * 2;
+    static constexpr int kQ = 0, kK = 2 * kTile, kV = kK + kStages * kTile, kBars = kV + kStages * kTile;
+    static constexpr int kBytes = kBars + 256 + 1024;      // barriers, and the base rounded up to 1024
+};
+
+template <int DP>
+__global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(const __grid_constant__ AttnForwardParams p)
+{
+    using L = ForwardShared<DP>;
+    constexpr int ST = L::kStages;
+    extern __shared__ unsigned char raw[];
+    unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
+    unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST;
+    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 2, *drained = o_full + 2;
+    volatile int *give_up = reinterpret_cast<int *>(drained + 1);
+    unsigned *tmem_cell = reinterpret_cast<unsigned *>(drained + 2);
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int head = blockIdx.y, b = blockIdx.z, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const int q0 = int(gridDim.x - 1 - blockIdx.x) * 2 * kRows;     // the longest rows of a causal mask first
+    const Lengths len = lengths_of(p.s, b);
+
+    // key tiles that some row of each query tile sees
+    int tiles[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int first = q0 + t * kRows, last = min(first + kRows, len.q) - 1;
+        const int seen = last < first ? 0 : p.s.causal ? min(len.kv, last + len.shift + 1) : len.kv;
+        tiles[t] = seen > 0 ? (seen + kRows - 1) / kRows : 0;
+    }
+    const int n = max(tiles[0], tiles[1]);
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(k_full + i, 1); mbar_init(k_empty + i, 1);
+            mbar_init(v_full + i, 1); mbar_init(v_empty + i, 1);
+        }
+        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(p_ready + t, kRows); mbar_init(o_full + t, 1); }
+        mbar_init(drained, 1);
+        *give_up = 0;
+        fence_barrier_init();
+    }
+    if (warp == 9) tmem_alloc(tmem_cell, 512);
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const unsigned tmem = *tmem_cell;
+    const unsigned s_at = tmem, o_at = tmem + 2 * kRows;             // S0 S1 | O0 O1
+
+    if (warp == 8) {
+        if (lane == 0 && n > 0) {
+            prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v);
+            const int q_tiles = tiles[1] > 0 ? 2 : 1;
+            mbar_expect_tx(q_full, q_tiles * L::kTile);
+            for (int t = 0; t < q_tiles; ++t) load_tile<DP, kRows>(smem + L::kQ + t * L::kTile, &p.q, head, q0 + t * kRows, b, q_full);
+            int kj = 0, vj = 0;                                       // copies armed
+            for (int j = 0; j < n; ++j) {
+                const int st = j % ST;
+                const unsigned free_parity = ((j / ST) & 1) ^ 1;
+                if (!bounded_wait(k_empty + st, free_parity, give_up, p.status)) break;
+                mbar_expect_tx(k_full + st, L::kTile);
+                load_tile<DP, kRows>(smem + L::kK + st * L::kTile, &p.k, kv_head, j * kRows, b, k_full + st);
+                ++kj;
+                if (!bounded_wait(v_empty + st, free_parity, give_up, p.status)) break;
+                mbar_expect_tx(v_full + st, L::kTile);
+                load_tile<DP, kRows>(smem + L::kV + st * L::kTile, &p.v, kv_head, j * kRows, b, v_full + st);
+                ++vj;
+            }
+            // the block may not end with a copy in flight, not even when it gave up
+            mbar_wait(q_full, 0);
+            for (int j = max(0, kj - ST); j < kj; ++j) mbar_wait(k_full + j % ST, (j / ST) & 1);
+            for (int j = max(0, vj - ST); j < vj; ++j) mbar_wait(v_full + j % ST, (j / ST) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        bool ok = n == 0 || warp_wait(q_full, 0, give_up, p.status);
+        if (n > 0 && ok) ok = warp_wait(k_full, 0, give_up, p.status);
+        const unsigned q = smem_addr(smem + L::kQ), k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
+        fence_after_sync();
+        if (ok && lane == 0) {
+            for (int t = 0; t < 2; ++t)
+                if (tiles[t] > 0) {
+                    mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k, false);
+                    mma_commit(s_full + t);
+                }
+            if (n > 0) mma_commit(k_empty);
+        }
+        __syncwarp();
+        for (int j = 0; j < n && ok; ++j) {
+            const int st = j % ST, next = (j + 1) % ST;
+            ok = warp_wait(v_full + st, (j / ST) & 1, give_up, p.status);
+            if (ok && p.s.kv_lengths && len.kv - j * kRows < kRows) zero_rows<DP, kRows>(smem + L::kV + st * L::kTile, len.kv - j * kRows);
+            if (ok && j + 1 < n) ok = warp_wait(k_full + next, ((j + 1) / ST) & 1, give_up, p.status);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (!ok || j >= tiles[t]) continue;
+                ok = warp_wait(p_ready + t, j & 1, give_up, p.status);
+                fence_after_sync();
+                if (ok && lane == 0) {
+                    mma_tmem_across<DP, kRows, kRows>(o_at + t * DP, s_at + t * kRows, v + st * L::kTile, j > 0);
+                    // the next scores go over P: the tensor core takes MMAs in order
+                    if (j + 1 < tiles[t]) {
+                        mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
+                        mma_commit(s_full + t);
+                    } else {
+                        mma_commit(o_full + t);
+                    }
+                }
+                __syncwarp();
+            }
+            if (ok && lane == 0) {
+                if (j + 1 < n) mma_commit(k_empty + next);
+                mma_commit(v_empty + st);
+            }
+            __syncwarp();
+        }
+        if (lane == 0) {
+            mma_commit(drained);
+            mbar_wait(drained, 0);
+        }
+        __syncwarp();
+    } else {
+        const int t = warp / 4, row = threadIdx.x % kRows, i = q0 + t * kRows + row;
+        const unsigned lanes = unsigned(warp % 4) * 32u << 16;
+        const unsigned s_row = s_at + t * kRows + lanes, o_row = o_at + t * DP + lanes;
+        // keys this row sees: [0, limit)
+        const int limit = i >= len.q ? 0 : p.s.causal ? min(len.kv, i + len.shift + 1) : len.kv;
+        const float unit = p.s.scale * kAttnLog2e;
+        float m = -INFINITY, l = 0.0f;                                // in powers of two
+        bool ok = true;
+        for (int j = 0; j < tiles[t]; ++j) {
+            ok = warp_wait(s_full + t, j & 1, give_up, p.status);
+            if (!ok) break;
+            fence_after_sync();
+            uint32_t x[2][64];
+            tmem_load(x[0], s_row);
+            tmem_load(x[1], s_row + 64);
+            const int open = limit - j * kRows;                       // columns of this tile that the row sees
+            if (__any_sync(~0u, open < kRows)) {
+#pragma unroll
+                for (int c = 0; c < kRows; ++c)
+                    if (c >= open) x[c / 64][c % 64] = __float_as_uint(-INFINITY);
+            }
+            float top[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(x[0][c]);
+#pragma unroll
+            for (int c = 4; c < kRows; ++c) top[c % 4] = fmaxf(top[c % 4], __uint_as_float(x[c / 64][c % 64]));
+            const float tile_max = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * unit;
+            const bool grow = tile_max > m + kRescaleAbove;           // also the first finite one
+            if (__any_sync(~0u, grow)) {
+                const float factor = grow ? attn_exp2(m - tile_max) : 1.0f;
+                if (grow) { m = tile_max; l *= factor; }
+                if (j > 0) {
+#pragma unroll
+                    for (int c = 0; c < DP / 32; ++c) {
+                        uint32_t o[32];
+                        tmem_load(o, o_row + c * 32);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+                        tmem_store(o_row + c * 32, o);
+                    }
+                }
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t packed[32];
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) {
+                    const float a = attn_exp2(fmaf(__uint_as_float(x[h][c]), unit, -ref));
+                    const float d = attn_exp2(fmaf(__uint_as_float(x[h][c + 1]), unit, -ref));
+                    sum[c % 4] += a;
+                    sum[c % 4 + 1] += d;
+                    packed[c / 2] = pack2(a, d);
+                }
+                tmem_store(s_row + h * 32, packed);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_wait_store();
+            fence_before_sync();
+            mbar_arrive(p_ready + t);
+        }
+        if (ok && tiles[t] > 0) ok = warp_wait(o_full + t, 0, give_up, p.status);
+        fence_after_sync();
+        const bool mine = i < p.s.q_len && ok;
+        __nv_bfloat16 *dst = p.out.data + b * p.out.batch + (long long)i * p.out.row + head * p.out.head;
+        const bool empty = l == 0.0f;                                 // the row sees no key
+        if (tiles[t] > 0 && ok) store_row<DP>(o_row, 1.0f / l, dst, p.s.dim, mine && !empty);
+        if (mine && empty) store_zeros(dst, p.s.dim);
+        if (mine) p.lse[((long long)b * p.s.heads + head) * p.s.q_len + i] = (m + log2f(l)) * kAttnLn2;
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (warp == 9) tmem_free(tmem, 512);
+}
+
+}  // namespace omni

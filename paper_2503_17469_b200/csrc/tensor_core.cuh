@@ -1,0 +1,127 @@
+// sm_100a building blocks of the attention kernels: tensor-map copies, tensor memory, tcgen05.mma.
+//
+// Operand tiles in shared memory are rows of 128 bytes (64 bfloat16 values), 1024-byte aligned, with the
+// 128-byte swizzle; a tile wider than 64 columns is several such blocks side by side.  The same tile
+// serves as an operand whose contraction runs along the row (K-major) or across the rows (MN-major).
+#pragma once
+#include <cuda.h>
+
+#include "tma_kernels.cuh"
+
+namespace omni {
+
+// ---- tensor-map copies --------------------------------------------------------------------------
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *m)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+}
+// Box at (column, head, row, batch); elements outside the tensor arrive as zeros.
+__device__ __forceinline__ void tensor_load(void *dst, const CUtensorMap *map, int col, int head, int row, int batch,
+                                            unsigned long long *bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(smem_addr(dst)), "l"(map), "r"(col), "r"(head), "r"(row), "r"(batch), "r"(smem_addr(bar)) : "memory");
+}
+// Plain stores to shared memory before an asynchronous unit reads them.
+__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_barrier_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+
+// ---- tensor memory: 128 lanes x 512 columns of 32 bits -----------------------------------------
+
+// Both are executed by one whole warp.
+__device__ __forceinline__ void tmem_alloc(unsigned *cell, unsigned columns)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(cell)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(unsigned addr, unsigned columns)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A warp's 32 lanes x N columns into N registers per thread (lane = row), complete on return.
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[16], unsigned addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[32], unsigned addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[64], unsigned addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+                 : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_store(unsigned addr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_store(unsigned addr, const uint32_t (&r)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+
+// ---- tcgen05.mma --------------------------------------------------------------------------------
+
+// Shared-memory descriptor of a swizzled tile.  K-major: `step` = bytes between groups of 8 rows
+// (1024), `across` unused.  MN-major: `step` = bytes between groups of 8 contraction rows (1024),
+// `across` = bytes between blocks of 64 columns.
+__device__ __forceinline__ uint64_t tile_desc(unsigned addr, unsigned step, unsigned across)
+{
+    return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(across >> 4) << 16 | uint64_t(step >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// bfloat16 x bfloat16 -> float, M = 128.
+__host__ __device__ constexpr uint32_t mma_kind(int n, bool a_mn_major, bool b_mn_major)
+{
+    return 1u << 4 | 1u << 7 | 1u << 10 | uint32_t(a_mn_major) << 15 | uint32_t(b_mn_major) << 16 | uint32_t(n / 8) << 17 | 8u << 24;
+}
+__device__ __forceinline__ void mma_ss(unsigned d, uint64_t a, uint64_t b, uint32_t kind, bool add)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"(uint32_t(add)) : "memory");
+}
+// A from tensor memory: lane = row, two bfloat16 values per column.
+__device__ __forceinline__ void mma_ts(unsigned d, unsigned a, uint64_t b, uint32_t kind, bool add)
+{
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"(uint32_t(add)) : "memory");
+}
+// Arrives on `bar` when every MMA this thread has issued so far is complete.
+__device__ __forceinline__ void mma_commit(unsigned long long *bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+// ---- bounded waits ------------------------------------------------------------------------------
+
+// A wait that runs out raises the block's flag and the context's status word; every other wait of the
+// block then gives up too, so that the block drains and frees its tensor memory.
+__device__ __forceinline__ bool bounded_wait(unsigned long long *bar, unsigned parity, volatile int *give_up, unsigned *status)
+{
+    for (unsigned i = 0; i < kTmaWaitLimit; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 255u) == 255u && *give_up) return false;
+    }
+    *give_up = 1;
+    *status = kStatusTimeout;
+    return false;
+}
+// The same for a whole warp: all lanes go on, or none.
+__device__ __forceinline__ bool warp_wait(unsigned long long *bar, unsigned parity, volatile int *give_up, unsigned *status)
+{
+    return __all_sync(~0u, bounded_wait(bar, parity, give_up, status));
+}
+
+}  // namespace omni

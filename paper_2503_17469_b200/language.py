@@ -118,6 +118,74 @@ class Embedding(_Operator):
         return grad
 
 
+class Attention(_Operator):
+    """Softmax attention on bfloat16 ``[batch, length, head, dim]`` tensors, forward and backward.
+
+    ``heads`` query heads share ``kv_heads`` key/value heads in groups; ``causal`` aligns queries and
+    keys at their ends; ``scale`` defaults to dim ** -0.5.  Any strides with a contiguous last dimension, multiples of 8
+    elements (slices of one projection's output, for example)."""
+
+    def __init__(self, ctx: "B.Omni", heads: int, kv_heads: int, dim: int, causal: bool = True, scale: Optional[float] = None):
+        super().__init__(ctx)
+        _need(heads >= 1 and kv_heads >= 1 and heads % kv_heads == 0, "heads is a multiple of kv_heads")
+        self.heads, self.kv_heads, self.dim, self.causal = heads, kv_heads, dim, causal
+        self.scale = dim ** -0.5 if scale is None else scale
+
+    def _shape(self, q, k, q_lengths, kv_lengths):
+        batch = q.shape[0]
+        for name, t in (("q_lengths", q_lengths), ("kv_lengths", kv_lengths)):
+            if t is not None:
+                _need(t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (batch,) and t.device == q.device,
+                      f"{name}: contiguous int32 [batch] on the tensors' device is wanted")
+        return B.omni_attn(batch, q.shape[1], k.shape[1], self.heads, self.kv_heads, self.dim, self.causal, self.scale,
+                           None if q_lengths is None else q_lengths.data_ptr(),
+                           None if kv_lengths is None else kv_lengths.data_ptr())
+
+    def _view(self, t, what: str, like, length: int, heads: int):
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{what}: dtype {t.dtype} is not bfloat16")
+        _need(tuple(t.shape) == (like.shape[0], length, heads, self.dim) and (self.dim == 1 or t.stride(3) == 1),
+              f"{what}: shape {(like.shape[0], length, heads, self.dim)} with a contiguous last dimension is wanted")
+        _on(like.device, **{what: t})
+        return B.omni_attn_view(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+
+    def forward(self, q, k, v, q_lengths=None, kv_lengths=None, out=None, stream=None):
+        """Returns (out like q, lse float32 [batch, heads, q_len])."""
+        _need(q.dim() == 4 and k.dim() == 4, "q and k: [batch, length, head, dim] is wanted")
+        a = self._shape(q, k, q_lengths, kv_lengths)
+        with self._allocating(stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            lse = torch.empty(a.batch, self.heads, a.q_len, device=q.device)
+        self._check(self._lib.omni_attn_forward(
+            self.ctx._h, C.byref(a), C.byref(self._view(q, "q", q, a.q_len, self.heads)),
+            C.byref(self._view(k, "k", q, a.kv_len, self.kv_heads)), C.byref(self._view(v, "v", q, a.kv_len, self.kv_heads)),
+            C.byref(self._view(out, "out", q, a.q_len, self.heads)), lse.data_ptr(), self._stream(stream)))
+        return out, lse
+
+    def backward(self, q, k, v, out, lse, grad_out, q_lengths=None, kv_lengths=None, grads=None, stream=None):
+        """Returns the gradients of (q, k, v); into ``grads``, a tuple of three, if given.  ``out`` and ``lse`` are the
+        forward call's."""
+        _need(q.dim() == 4 and k.dim() == 4, "q and k: [batch, length, head, dim] is wanted")
+        a = self._shape(q, k, q_lengths, kv_lengths)
+        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (a.batch, self.heads, a.q_len)
+              and lse.device == q.device, "lse: contiguous float32 [batch, heads, q_len] is wanted")
+        with self._allocating(stream):
+            dq, dk, dv = grads or (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+            # the library's own query: rows of whole tiles, two floats each
+            size = C.c_uint64()
+            self._check(self._lib.omni_attn_workspace(C.byref(a), C.byref(size)))
+            scratch = torch.empty(max(16, size.value), dtype=torch.uint8, device=q.device)
+        rows = [C.byref(self._view(t, name, q, a.q_len, self.heads))
+                for t, name in ((q, "q"), (out, "out"), (grad_out, "grad_out"), (dq, "grads[0]"))]
+        keys = [C.byref(self._view(t, name, q, a.kv_len, self.kv_heads))
+                for t, name in ((k, "k"), (v, "v"), (dk, "grads[1]"), (dv, "grads[2]"))]
+        self._check(self._lib.omni_attn_backward(
+            self.ctx._h, C.byref(a), rows[0], keys[0], keys[1], rows[1], lse.data_ptr(), rows[2], rows[3], keys[2], keys[3],
+            scratch.data_ptr(), scratch.numel(), self._stream(stream)))
+        return dq, dk, dv
+
+
 class Distillation(_Operator):
     """KL divergence (times temperature squared) of the student's softmax from a teacher's top logits, per row.
     An index of -1 marks an entry that is not there; a row without entries has loss 0 and no gradient."""
