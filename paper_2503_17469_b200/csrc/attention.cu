@@ -89,11 +89,10 @@ OutView out_of(const omni_attn_view *v)
 // One launch of a kernel that takes its parameter block by value, with its shared memory opted in.
 template <typename P> int launch(omni_ctx *ctx, void (*kernel)(P), dim3 grid, int threads, int smem, cudaStream_t s, const P &p)
 {
-    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return context_launched(ctx, int(e));
+    int rc = context_shared(ctx, reinterpret_cast<const void *>(kernel), smem);
+    if (rc != OMNI_OK) return rc;
     void *args[] = {const_cast<P *>(&p)};
-    e = cudaLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), args, smem, s);
-    return context_launched(ctx, int(e));
+    return context_launched(ctx, int(cudaLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), args, smem, s)));
 }
 
 int q_pad_of(const omni_attn *a) { return int(round_up(uint64_t(a->q_len), kRows)); }

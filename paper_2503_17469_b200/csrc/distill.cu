@@ -1,9 +1,12 @@
 // Distillation loss from a teacher's top logits: forward, backward, both in one pass.
 //
 // Per row: lse = log sum_v exp(z_v / T) needs all of z before the first gradient value can be
-// written, so the gradient is a second walk over the row.  One CTA owns a row; the first walk keeps a
-// running maximum and sum per thread (a sum is rescaled only when its maximum moves), the
-// second finds the row, which the same CTA read a moment ago, in L2.  HBM sees one read and one write.
+// written, so the gradient is a second walk over the row.  The floor is one read of the logits and
+// one write of the gradient.
+//
+// A CTA owns a row.  The first walk keeps a running maximum and sum per thread (the sum is rescaled only
+// when the maximum moves), the second finds the row, which the same CTA read a moment ago, in L2.  One more warp
+// has the teacher: it fetches and weighs the entries beside the first walk.
 #include "context.h"
 #include "vector.cuh"
 
@@ -12,7 +15,6 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kMaxThreads = 1024;
 enum Mode { kForward = 0, kBackward = 1, kStep = 2 };
 
 struct DistillParams {
@@ -34,19 +36,139 @@ __device__ __forceinline__ float exp2_fast(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two floats per instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+        " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
 
-// Maximum and sum of 2^(x - maximum), joined.  Products and sums are spelled out where the compiler could
-// contract them one way in one variant and another way in the next: forward and step give the same bits.
-struct Running {
-    float m, s;
-    __device__ __forceinline__ void join(float om, float os)
+// Eight logits as loaded, their largest, and as four pairs of floats.
+template <typename T> struct Group;
+template <> struct Group<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p)
     {
-        const float nm = fmaxf(m, om);
-        if (nm == -INFINITY) { s += os; return; }    // both empty (a NaN sum stays one)
-        s = fmaf(s, exp2_fast(m - nm), __fmul_rn(os, exp2_fast(om - nm)));
-        m = nm;
+        a = *reinterpret_cast<const float4 *>(p);
+        b = *reinterpret_cast<const float4 *>(p + 4);
+    }
+    __device__ __forceinline__ float largest() const
+    {
+        return fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)), fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w)));
+    }
+    __device__ __forceinline__ float2 pair(int i) const
+    {
+        return i == 0 ? make_float2(a.x, a.y) : i == 1 ? make_float2(a.z, a.w) : i == 2 ? make_float2(b.x, b.y) : make_float2(b.z, b.w);
     }
 };
+template <> struct Group<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ static uint32_t larger(uint32_t x, uint32_t y)
+    {
+        uint32_t z;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(x), "r"(y));
+        return z;
+    }
+    __device__ __forceinline__ float largest() const
+    {
+        const uint32_t m = larger(larger(u.x, u.y), larger(u.z, u.w));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+    __device__ __forceinline__ float2 pair(int i) const
+    {
+        const uint32_t w = i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+};
+
+// A thread's running maximum m and sum of 2^(x - m), x = logit * unit.  Products and sums are spelled out
+// where the compiler could contract them one way in one variant and another way in the next: forward
+// and step give the same bits.
+struct Running {
+    float m = -INFINITY;
+    float2 a = {0.0f, 0.0f}, b = {0.0f, 0.0f};
+    template <typename T, int K> __device__ __forceinline__ void take(const Group<T> (&g)[K], float unit)
+    {
+        float top = g[0].largest();
+#pragma unroll
+        for (int k = 1; k < K; ++k) top = fmaxf(top, g[k].largest());
+        raise(__fmul_rn(top, unit));
+        const float ref = m == -INFINITY ? 0.0f : -m;
+        const float2 u = {unit, unit}, r = {ref, ref};
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 x = fma2(g[k].pair(i), u, r);
+                const float2 e = {exp2_fast(x.x), exp2_fast(x.y)};
+                if (i % 2 == 0) a = add2(a, e);
+                else b = add2(b, e);
+            }
+    }
+    __device__ __forceinline__ void take_one(float z, float unit)
+    {
+        const float x = __fmul_rn(z, unit);
+        raise(x);
+        a.x += exp2_fast(x - (m == -INFINITY ? 0.0f : m));
+    }
+    __device__ __forceinline__ void raise(float to)
+    {
+        if (to > m) {                                // rare after the first few groups
+            const float f = exp2_fast(m - to);
+            a = mul2(a, {f, f});
+            b = mul2(b, {f, f});
+            m = to;
+        }
+    }
+    __device__ __forceinline__ float sum() const { return __fadd_rn(__fadd_rn(a.x, a.y), __fadd_rn(b.x, b.y)); }
+};
+
+struct Joined { float m, s; };
+__device__ __forceinline__ float warp_max(float x)
+{
+    for (int o = 16; o > 0; o /= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
+    return x;
+}
+__device__ __forceinline__ float warp_sum(float x)
+{
+    for (int o = 16; o > 0; o /= 2) x = __fadd_rn(x, __shfl_xor_sync(~0u, x, o));
+    return x;
+}
+// A warp's maximum and sum into its cell.
+__device__ __forceinline__ void put_warp(const Running &run, Joined *cell)
+{
+    const float m = warp_max(run.m);
+    const float s = run.sum();
+    const float t = warp_sum(m == -INFINITY || run.m == m ? s : __fmul_rn(s, exp2_fast(run.m - m)));
+    if (threadIdx.x % 32 == 0) *cell = {m, t};
+}
+
+// The walkers' cells joined, by every warp for itself: the sum for the largest maximum.
+template <int N> __device__ __forceinline__ Joined join_cells(const Joined (&cell)[N], int n = N)
+{
+    const int lane = threadIdx.x % 32;
+    const Joined x = lane < n ? cell[lane] : Joined{-INFINITY, 0.0f};
+    const float m = warp_max(x.m);
+    return {m, warp_sum(m == -INFINITY || x.m == m ? x.s : __fmul_rn(x.s, exp2_fast(x.m - m)))};
+}
 
 // Element range of a row in three parts: up to the first 16-byte boundary, whole groups, the rest.
 template <typename T> struct Parts {
@@ -57,126 +179,189 @@ template <typename T> struct Parts {
         head = lead < vocab ? lead : vocab;
         groups = (vocab - head) / kGroup;
     }
+    // the i-th of the elements outside the groups (fewer than 16)
+    __device__ __forceinline__ int edge(int i) const { return i < head ? i : groups * kGroup + i; }
 };
 
-template <typename F> __device__ __forceinline__ float block_reduce(float x, float *cell, F f, float neutral)
+// The teacher's side of a row: where its entries stand, the student's logit there, their probability.
+struct Teacher {
+    float prob[OMNI_DISTILL_MAX_TOP], hit[OMNI_DISTILL_MAX_TOP];
+    int place[OMNI_DISTILL_MAX_TOP];
+    float term;                                     // sum of p (log p - z / T)
+    int target;                                     // some entry has a probability
+    int repeated;                                   // some place is named twice
+};
+
+// One warp's work, beside the walk over the row.  `seen`: a table of 2 OMNI_DISTILL_MAX_TOP places.
+template <typename T, typename I>
+__device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned long long r, const T *row, Teacher &te, int *seen)
 {
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
-    for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(~0u, x, o));
-    __syncthreads();
-    if (lane == 0) cell[warp] = x;
-    __syncthreads();
-    x = lane < warps ? cell[lane] : neutral;
-    for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(~0u, x, o));
-    return x;
+    const int lane = threadIdx.x % 32;
+    const float *logit = p.top_logits + r * p.top_stride;
+    float top = -INFINITY;
+    int table = 32;                                 // at least twice the entries
+    while (table < 2 * p.top) table *= 2;
+    for (int j = lane; j < table; j += 32) seen[j] = -1;
+    __syncwarp();
+    bool repeated = false;
+    for (int j = lane; j < p.top; j += 32) {
+        const long long i = load_index<I>(p.top_index, r * p.top_stride + j);
+        const bool there = i >= 0 && i < p.vocab;
+        const float t = there ? logit[j] / p.temperature : -INFINITY;
+        te.place[j] = there ? int(i) : -1;
+        te.hit[j] = there ? to_float(row[i]) : 0.0f;
+        te.prob[j] = t;
+        top = fmaxf(top, t);
+        for (int h = int(unsigned(i) * 2654435769u >> 16) & (table - 1); there; h = (h + 1) & (table - 1)) {
+            const int old = atomicCAS(&seen[h], -1, int(i));
+            repeated |= old == int(i);
+            if (old == -1 || old == int(i)) break;
+        }
+    }
+    repeated = __any_sync(~0u, repeated);
+    top = warp_max(top);
+    float total = 0.0f;
+    for (int j = lane; j < p.top; j += 32) {
+        const float e = top == -INFINITY && !isnan(te.prob[j]) ? 0.0f : expf(te.prob[j] - top);
+        te.prob[j] = e;
+        total += e;
+    }
+    total = warp_sum(total);
+    const bool target = !(total == 0.0f);           // NaN counts as a target and shows
+    float term = 0.0f;
+    for (int j = lane; j < p.top; j += 32) {
+        const float q = target ? te.prob[j] / total : 0.0f;
+        te.prob[j] = q;
+        if (!(q == 0.0f)) term = __fadd_rn(term, __fmul_rn(q, logf(q) - te.hit[j] / p.temperature));
+    }
+    term = warp_sum(term);
+    if (lane == 0) {
+        te.term = term;
+        te.target = target;
+        te.repeated = repeated;
+    }
+    __syncwarp();
 }
 
-template <typename T, typename I, int MODE>
-__global__ void __launch_bounds__(kMaxThreads) distill_kernel(DistillParams p)
+// The gradient at the teacher's entries, over what the walk wrote there; an entry that names a token again is
+// left to the first.  `ref`: minus the lse in powers of two.
+template <typename T>
+__device__ __forceinline__ void put_entries(const DistillParams &p, const Teacher &te, T *out, float gain, float unit, float ref, int from, int step)
 {
-    __shared__ float cell[32], cell2[32];
-    __shared__ float prob[OMNI_DISTILL_MAX_TOP], hit[OMNI_DISTILL_MAX_TOP];
-    __shared__ int place[OMNI_DISTILL_MAX_TOP];
+    for (int j = from; j < p.top; j += step) {
+        const int at = te.place[j];
+        if (at < 0) continue;
+        float total = te.prob[j];
+        bool first = true;
+        if (te.repeated) {
+            total = 0.0f;
+            for (int i = 0; i < p.top; ++i)
+                if (te.place[i] == at) {
+                    first = first && i >= j;
+                    total += te.prob[i];
+                }
+        }
+        if (first) out[at] = from_float<T>(gain * (exp2_fast(fmaf(te.hit[j], unit, ref)) - total));
+    }
+}
+
+// gain * 2^(logit * unit + ref) of a group, stored.
+template <typename T>
+__device__ __forceinline__ void put_group(T *dst, const Group<T> &g, float unit, float ref, float gain)
+{
+    float f[kGroup];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 x = fma2(g.pair(i), {unit, unit}, {ref, ref});
+        const float2 y = mul2({exp2_fast(x.x), exp2_fast(x.y)}, {gain, gain});
+        f[2 * i] = y.x;
+        f[2 * i + 1] = y.y;
+    }
+    store_streaming(dst, f);
+}
+template <typename T> __device__ __forceinline__ T put_value(T z, float unit, float ref, float gain)
+{
+    return from_float<T>(__fmul_rn(exp2_fast(fmaf(to_float(z), unit, ref)), gain));
+}
+__device__ __forceinline__ bool same_phase(const void *a, const void *b)
+{
+    return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15) == 0;
+}
+
+// ---- a CTA per row, from global memory ----------------------------------------------------------
+
+constexpr int kRowWalkers = 256;
+
+template <typename T, typename I, int MODE>
+__global__ void __launch_bounds__(kRowWalkers + 32, 4) row_kernel(DistillParams p)
+{
+    __shared__ Joined cell[kRowWalkers / 32];
+    __shared__ Teacher te;
+    __shared__ int seen[2 * OMNI_DISTILL_MAX_TOP];
+    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;  // groups a thread has in flight
+    const int walkers = blockDim.x - 32, tid = threadIdx.x, warp = tid / 32;
     const unsigned long long r = blockIdx.x;
     const T *row = static_cast<const T *>(p.logits) + r * p.row_stride;
-    const int tid = threadIdx.x, threads = blockDim.x, lane = tid % 32, warp = tid / 32;
-    const float unit = kLog2e / p.temperature;      // logits to powers of two
+    const float unit = kLog2e / p.temperature;
     const Parts<T> parts(row, p.vocab);
-
-    // the teacher's entries: place, student's logit there, probability
-    float t = -INFINITY;
-    if (tid < p.top) {
-        const long long i = load_index<I>(p.top_index, r * p.top_stride + tid);
-        const bool there = i >= 0 && i < p.vocab;
-        place[tid] = there ? int(i) : -1;
-        hit[tid] = there ? to_float(row[i]) : 0.0f;
-        if (there) t = p.top_logits[r * p.top_stride + tid] / p.temperature;
+    const int rest = p.vocab - parts.groups * kGroup;
+    // f(first group, groups): kAhead at a time, then one by one
+    auto walk = [&](auto f) {
+        int g = tid;
+        for (; g + (kAhead - 1) * walkers < parts.groups; g += walkers * kAhead) {
+            Group<T> x[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) x[a].load(row + parts.head + (long long)(g + a * walkers) * kGroup);
+            f(g, x);
+        }
+        for (; g < parts.groups; g += walkers) {
+            Group<T> x[1];
+            x[0].load(row + parts.head + (long long)g * kGroup);
+            f(g, x);
+        }
+    };
+    const float weight = MODE == kForward ? 0.0f : p.grad_loss[r];
+    float lse2 = MODE == kBackward ? __fmul_rn(p.lse_in[r], kLog2e) : 0.0f;
+    if (tid >= walkers) {
+        teacher_warp<T, I>(p, r, row, te, seen);
+    } else if constexpr (MODE != kBackward) {
+        Running run;
+        walk([&](int, const auto &x) { run.take(x, unit); });
+        if (tid < rest) run.take_one(to_float(row[parts.edge(tid)]), unit);
+        __syncwarp();
+        put_warp(run, cell + warp);
     }
-    auto larger = [](float a, float b) { return fmaxf(a, b); };
-    auto plus = [](float a, float b) { return a + b; };
-    const float tm = block_reduce(t, cell, larger, -INFINITY);
-    const float te = tid < p.top && tm != -INFINITY ? expf(t - tm) : 0.0f;
-    const float ts = block_reduce(te, cell, plus, 0.0f);
-    const bool target = !(ts == 0.0f);              // NaN counts as a target and shows
-    const float my_p = target ? te / ts : 0.0f;
-    if (tid < p.top) prob[tid] = my_p;
-
-    float lse2;                                     // lse in powers of two
+    __syncthreads();
+    const bool target = te.target;
     if constexpr (MODE != kBackward) {
-        Running run{-INFINITY, 0.0f};
-        for (int g = tid; g < parts.groups; g += threads) {
-            float f[kGroup];
-            load_group(row + parts.head + (long long)g * kGroup, f);
-            float m = f[0];
-#pragma unroll
-            for (int e = 1; e < kGroup; ++e) m = fmaxf(m, f[e]);
-            m = __fmul_rn(m, unit);
-            if (m > run.m) { run.s = __fmul_rn(run.s, exp2_fast(run.m - m)); run.m = m; }
-            const float ref = run.m == -INFINITY ? 0.0f : run.m;
-#pragma unroll
-            for (int e = 0; e < kGroup; ++e) run.s += exp2_fast(fmaf(f[e], unit, -ref));
-        }
-        const int rest = p.vocab - parts.groups * kGroup;   // head and tail together, < 16 elements
-        if (tid < rest) {
-            const int v = tid < parts.head ? tid : parts.groups * kGroup + tid;
-            const float x = __fmul_rn(to_float(row[v]), unit);
-            run.join(x, x == -INFINITY ? 0.0f : exp2_fast(x - x));
-        }
-        for (int o = 16; o > 0; o /= 2) run.join(__shfl_xor_sync(~0u, run.m, o), __shfl_xor_sync(~0u, run.s, o));
-        __syncthreads();
-        if (lane == 0) { cell[warp] = run.m; cell2[warp] = run.s; }
-        __syncthreads();
-        run.m = lane < threads / 32 ? cell[lane] : -INFINITY;
-        run.s = lane < threads / 32 ? cell2[lane] : 0.0f;
-        for (int o = 16; o > 0; o /= 2) run.join(__shfl_xor_sync(~0u, run.m, o), __shfl_xor_sync(~0u, run.s, o));
-        lse2 = run.m + log2f(run.s);
-        const float lse = __fmul_rn(lse2, kLn2);
-        float term = 0.0f;
-        if (tid < p.top && !(my_p == 0.0f)) term = __fmul_rn(my_p, logf(my_p) - hit[tid] / p.temperature + lse);
-        const float sum = block_reduce(term, cell, plus, 0.0f);
+        const Joined all = join_cells(cell, walkers / 32);
+        lse2 = all.m + log2f(all.s);
         if (tid == 0) {
-            p.loss[r] = p.temperature * p.temperature * sum;
+            const float lse = __fmul_rn(lse2, kLn2);
             p.lse_out[r] = lse;
+            p.loss[r] = target ? __fmul_rn(__fmul_rn(p.temperature, p.temperature), __fadd_rn(te.term, lse)) : 0.0f;
         }
-    } else {
-        lse2 = __fmul_rn(p.lse_in[r], kLog2e);
     }
-
     if constexpr (MODE != kForward) {
         T *out = static_cast<T *>(p.grad) + r * p.grad_stride;
-        const float gain = target ? p.grad_loss[r] * p.temperature : 0.0f;
-        const float ref = lse2 == -INFINITY ? 0.0f : lse2;
-        const bool together = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row)) & 15) == 0;
-        auto value = [&](float z) { return target ? gain * exp2_fast(fmaf(z, unit, -ref)) : 0.0f; };
-        if (together) {
-            for (int g = tid; g < parts.groups; g += threads) {
-                float f[kGroup];
-                const long long v = parts.head + (long long)g * kGroup;
-                load_group(row + v, f);
+        const float gain = __fmul_rn(weight, p.temperature);
+        const float ref = lse2 == -INFINITY ? 0.0f : -lse2;
+        if (tid < walkers) {
+            if (!target) {
+                for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(0.0f);
+            } else if (same_phase(out, row)) {
+                walk([&](int g, const auto &x) {
 #pragma unroll
-                for (int e = 0; e < kGroup; ++e) f[e] = value(f[e]);
-                store_group(out + v, f);
+                    for (int a = 0; a < int(sizeof x / sizeof x[0]); ++a)
+                        put_group(out + parts.head + (long long)(g + a * walkers) * kGroup, x[a], unit, ref, gain);
+                });
+                if (tid < rest) out[parts.edge(tid)] = put_value(row[parts.edge(tid)], unit, ref, gain);
+            } else {
+                for (int v = tid; v < p.vocab; v += walkers) out[v] = put_value(row[v], unit, ref, gain);
             }
-            const int rest = p.vocab - parts.groups * kGroup;
-            if (tid < rest) {
-                const int v = tid < parts.head ? tid : parts.groups * kGroup + tid;
-                out[v] = from_float<T>(value(to_float(row[v])));
-            }
-        } else {
-            for (int v = tid; v < p.vocab; v += threads) out[v] = from_float<T>(value(to_float(row[v])));
         }
         __syncthreads();
-        // the teacher's entries over it; one that names a token again is left to the first
-        if (tid < p.top && place[tid] >= 0 && target) {
-            float total = 0.0f;
-            bool first = true;
-            for (int j = 0; j < p.top; ++j)
-                if (place[j] == place[tid]) {
-                    first = first && j >= tid;
-                    total += prob[j];
-                }
-            if (first) out[place[tid]] = from_float<T>(gain * (exp2_fast(fmaf(hit[tid], unit, -ref)) - total));
-        }
+        if (target) put_entries(p, te, out, gain, unit, ref, tid, blockDim.x);
     }
 }
 
@@ -198,15 +383,14 @@ int check_distill(const omni_distill *d)
     return OMNI_OK;
 }
 
-template <typename T, typename I> int enqueue(omni_ctx *ctx, int mode, const DistillParams &p, unsigned rows, cudaStream_t s)
+template <typename T, typename I>
+int enqueue(omni_ctx *ctx, int mode, const DistillParams &p, unsigned rows, cudaStream_t s)
 {
-    // a thread per two groups of eight, a warp per 32 entries of the teacher at least
-    int threads = 128;
-    while (threads < kMaxThreads && threads * 2 * kGroup < p.vocab) threads *= 2;
-    while (threads < p.top) threads *= 2;
-    if (mode == kForward) distill_kernel<T, I, kForward><<<rows, threads, 0, s>>>(p);
-    else if (mode == kBackward) distill_kernel<T, I, kBackward><<<rows, threads, 0, s>>>(p);
-    else distill_kernel<T, I, kStep><<<rows, threads, 0, s>>>(p);
+    int walkers = 64;
+    while (walkers < kRowWalkers && walkers * 8 * kGroup < p.vocab) walkers *= 2;
+    if (mode == kForward) row_kernel<T, I, kForward><<<rows, walkers + 32, 0, s>>>(p);
+    else if (mode == kBackward) row_kernel<T, I, kBackward><<<rows, walkers + 32, 0, s>>>(p);
+    else row_kernel<T, I, kStep><<<rows, walkers + 32, 0, s>>>(p);
     return context_launched(ctx, int(cudaGetLastError()));
 }
 

@@ -419,8 +419,8 @@ int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, u
     const int smem = kSortWarps * kIdsPerCta * int(sizeof(int));
     rc = with_index(index_type, [&](auto *ip) {
         using I = std::remove_pointer_t<decltype(ip)>;
-        const cudaError_t e = cudaFuncSetAttribute(sort_tokens_kernel<I>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return context_launched(ctx, int(e));
+        const int r = context_shared(ctx, reinterpret_cast<const void *>(sort_tokens_kernel<I>), smem);
+        if (r != OMNI_OK) return r;
         sort_tokens_kernel<I><<<(vocab + kIdsPerCta - 1) / kIdsPerCta, kSortThreads, smem, s>>>(tokens, (long long)n, vocab,
                                                                                                padding, sorted, start);
         return context_launched(ctx, int(cudaGetLastError()));

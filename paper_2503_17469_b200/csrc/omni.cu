@@ -41,6 +41,8 @@ struct omni_ctx {
     omni::LaunchShape overwrite_shape[2][2];            // [dtype][wide]
     omni::LaunchShape bulk_overwrite_shape[2];          // [dtype], ring kernel as push with overwrite
     omni::LaunchShape seq_shape[2][2][OMNI_MAX_ASP_BATCH + 1];  // [dtype][wide][M]
+    const void *opted[32] = {};                         // kernels opted into their dynamic shared memory (context_shared)
+    int n_opted = 0;
 };
 
 namespace omni {
@@ -305,6 +307,15 @@ int context_launched(omni_ctx *ctx, int cuda_error)
         return OMNI_ERR_CUDA;
     }
     ctx->launches += 1;
+    return OMNI_OK;
+}
+
+int context_shared(omni_ctx *ctx, const void *kernel, int bytes)
+{
+    for (int i = 0; i < ctx->n_opted; ++i)
+        if (ctx->opted[i] == kernel) return OMNI_OK;
+    OMNI_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    if (ctx->n_opted < int(sizeof ctx->opted / sizeof *ctx->opted)) ctx->opted[ctx->n_opted++] = kernel;
     return OMNI_OK;
 }
 

@@ -49,6 +49,14 @@ __device__ __forceinline__ void store_group(float *p, const float *f)
 }
 __device__ __forceinline__ void store_group(__nv_bfloat16 *p, const float *f) { *reinterpret_cast<uint4 *>(p) = narrow(f); }
 
+// The same for values that nothing reads soon: first to leave L2.
+__device__ __forceinline__ void store_streaming(float *p, const float *f)
+{
+    __stcs(reinterpret_cast<float4 *>(p), make_float4(f[0], f[1], f[2], f[3]));
+    __stcs(reinterpret_cast<float4 *>(p + 4), make_float4(f[4], f[5], f[6], f[7]));
+}
+__device__ __forceinline__ void store_streaming(__nv_bfloat16 *p, const float *f) { __stcs(reinterpret_cast<uint4 *>(p), narrow(f)); }
+
 template <typename I> __device__ __forceinline__ long long load_index(const void *p, unsigned long long i)
 {
     return (long long)static_cast<const I *>(p)[i];

@@ -11,7 +11,6 @@ enqueued; what the library refuses raises ``OmniError``.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 from typing import Optional
 
@@ -21,6 +20,17 @@ from . import binding as B
 
 _DTYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16}
 _INDEX = {torch.int32: B.I32, torch.int64: B.I64}
+_empty, _float, _bf16, _byte = torch.empty, torch.float32, torch.bfloat16, torch.uint8
+_ref = C.byref
+
+
+def _current_stream() -> int:
+    """The raw handle of torch's current stream (what ``Omni._stream`` wraps), without an object around it."""
+    return _raw_stream(_device())
+
+
+_device = torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
 
 def _code(t, codes, what: str) -> int:
@@ -30,37 +40,32 @@ def _code(t, codes, what: str) -> int:
     return c
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
-
-
-def _on(device, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+def _elsewhere(**tensors):
+    """For the messages of tensors that are not where the others are."""
+    return ValueError(", ".join(f"{k} on {t.device}" for k, t in tensors.items() if t is not None) + ": one CUDA device is wanted")
 
 
 def _rows(t, what: str) -> int:
     """Stride between the rows of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: a matrix with contiguous rows is wanted, got shape {tuple(t.shape)}, strides {t.stride()}")
-    stride = t.stride(0)
-    return stride if stride >= t.shape[1] else t.shape[1] if t.shape[0] <= 1 else stride
+    n, m = t.shape
+    stride, one = t.stride()
+    if one != 1 and m > 1:
+        raise ValueError(f"{what}: contiguous rows are wanted, got strides {t.stride()}")
+    return stride if stride >= m or n > 1 else m
 
 
+# The checks below stand in the calls themselves, without helpers and keyword arguments, and a
+# message is only put together where it is raised: a call's host time is most of a short operator's.
 class _Operator:
     def __init__(self, ctx: "B.Omni"):
         self.ctx = ctx
         self._lib = B.lib()
-
-    def _stream(self, stream):
-        return B.Omni._stream(stream)
+        self._sizes = {}       # scratch bytes by problem size
 
     @staticmethod
-    def _allocating(stream):
+    def _on_stream(stream):
         """Outputs and scratch belong to the stream that uses them."""
-        return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+        return torch.cuda.stream(stream)
 
     def _check(self, rc: int) -> None:
         if rc != B.OK:
@@ -72,49 +77,67 @@ class Embedding(_Operator):
 
     def __init__(self, ctx: "B.Omni", vocab: int, dim: int, scale: float = 1.0, padding: int = -1):
         super().__init__(ctx)
-        _need(vocab >= 1 and dim >= 1, "vocab and dim are at least 1")
+        if vocab < 1 or dim < 1:
+            raise ValueError("vocab and dim are at least 1")
         self.vocab, self.dim, self.scale, self.padding = vocab, dim, scale, padding
+        self._table = torch.Size((vocab, dim))
 
     def forward(self, tokens, weight, dtype=None, out=None, stream=None):
         """``tokens``: int32 or int64, any shape, contiguous; ``weight``: [vocab, dim] float32 or bfloat16.
         Returns ``tokens.shape + (dim,)`` of ``dtype`` (default the table's)."""
-        _need(tokens.is_contiguous(), "tokens: a contiguous tensor is wanted")
-        _need(tuple(weight.shape) == (self.vocab, self.dim), f"weight: shape {(self.vocab, self.dim)} is wanted")
-        n = tokens.numel()
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.forward(tokens, weight, dtype, out)
+        shape = (*tokens.shape, self.dim)
         if out is None:
-            with self._allocating(stream):
-                out = torch.empty(*tokens.shape, self.dim, dtype=dtype or weight.dtype, device=tokens.device)
-        _need(tuple(out.shape) == (*tokens.shape, self.dim) and out.is_contiguous(),
-              "out: a contiguous tensor of the tokens' shape and dim is wanted")
-        _on(tokens.device, weight=weight, out=out)
+            out = _empty(shape, dtype=dtype or weight.dtype, device=tokens.device)
+        elif out.shape != shape or not out.is_contiguous():
+            raise ValueError(f"out: a contiguous tensor of shape {shape} is wanted")
+        if weight.shape != self._table:
+            raise ValueError(f"weight: shape {tuple(self._table)} is wanted")
+        if not tokens.is_contiguous():
+            raise ValueError("tokens: a contiguous tensor is wanted")
+        if not tokens.is_cuda or not weight.get_device() == out.get_device() == tokens.get_device():
+            raise _elsewhere(tokens=tokens, weight=weight, out=out)
         self._check(self._lib.omni_embed_forward(
-            self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), n, weight.data_ptr(),
+            self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), tokens.numel(), weight.data_ptr(),
             _code(weight, _DTYPES, "weight"), _rows(weight, "weight"), self.vocab, self.dim, self.scale, out.data_ptr(),
-            _code(out, _DTYPES, "out"), self.dim, self._stream(stream)))
+            _code(out, _DTYPES, "out"), self.dim, _current_stream()))
         return out
 
     def backward(self, tokens, grad_out, dtype=torch.float32, grad=None, accumulate: bool = False, stream=None):
         """Gradient of the table, [vocab, dim] of ``dtype``; into ``grad`` if given (for example a view of a
         gradient bucket), added to it with ``accumulate``.  ``grad_out``: ``tokens.shape + (dim,)``,
         or a matrix of as many rows, rows contiguous."""
-        _need(tokens.is_contiguous(), "tokens: a contiguous tensor is wanted")
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.backward(tokens, grad_out, dtype, grad, accumulate)
         n = tokens.numel()
         g = grad_out if grad_out.dim() == 2 else grad_out.view(n, self.dim)
-        _need(tuple(g.shape) == (n, self.dim), f"grad_out: {n} rows of {self.dim} are wanted")
-        _need(grad is not None or not accumulate, "accumulate needs a gradient to add to")
-        size = C.c_uint64()
-        self._check(self._lib.omni_embed_workspace(n, self.vocab, self.dim, C.byref(size)))
-        with self._allocating(stream):
-            if grad is None:
-                grad = torch.empty(self.vocab, self.dim, dtype=dtype, device=tokens.device)
-            scratch = torch.empty(max(16, size.value), dtype=torch.uint8, device=tokens.device)
-        _need(tuple(grad.shape) == (self.vocab, self.dim), f"grad: shape {(self.vocab, self.dim)} is wanted")
-        _on(tokens.device, grad_out=g, grad=grad)
+        if g.shape != (n, self.dim):
+            raise ValueError(f"grad_out: {n} rows of {self.dim} are wanted")
+        if not tokens.is_contiguous():
+            raise ValueError("tokens: a contiguous tensor is wanted")
+        device = tokens.device
+        if grad is None:
+            if accumulate:
+                raise ValueError("accumulate needs a gradient to add to")
+            grad = _empty(self._table, dtype=dtype, device=device)
+        elif grad.shape != self._table:
+            raise ValueError(f"grad: shape {tuple(self._table)} is wanted")
+        if not tokens.is_cuda or not g.get_device() == grad.get_device() == tokens.get_device():
+            raise _elsewhere(tokens=tokens, grad_out=g, grad=grad)
+        size = self._sizes.get(n)
+        if size is None:
+            need = C.c_uint64()
+            self._check(self._lib.omni_embed_workspace(n, self.vocab, self.dim, _ref(need)))
+            size = self._sizes[n] = max(16, need.value)
+        scratch = _empty(size, dtype=_byte, device=device)
         self._check(self._lib.omni_embed_backward(
             self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), n, g.data_ptr(),
             _code(g, _DTYPES, "grad_out"), _rows(g, "grad_out"), self.vocab, self.dim, self.scale, self.padding,
             grad.data_ptr(), _code(grad, _DTYPES, "grad"), _rows(grad, "grad"), accumulate, scratch.data_ptr(),
-            scratch.numel(), self._stream(stream)))
+            size, _current_stream()))
         return grad
 
 
@@ -122,67 +145,84 @@ class Attention(_Operator):
     """Softmax attention on bfloat16 ``[batch, length, head, dim]`` tensors, forward and backward.
 
     ``heads`` query heads share ``kv_heads`` key/value heads in groups; ``causal`` aligns queries and
-    keys at their ends; ``scale`` defaults to dim ** -0.5.  Any strides with a contiguous last dimension, multiples of 8
-    elements (slices of one projection's output, for example)."""
+    keys at their ends; ``scale`` defaults to dim ** -0.5.  Any strides with a contiguous last
+    dimension, multiples of 8 elements (slices of one projection's output, for example)."""
 
     def __init__(self, ctx: "B.Omni", heads: int, kv_heads: int, dim: int, causal: bool = True, scale: Optional[float] = None):
         super().__init__(ctx)
-        _need(heads >= 1 and kv_heads >= 1 and heads % kv_heads == 0, "heads is a multiple of kv_heads")
+        if heads < 1 or kv_heads < 1 or heads % kv_heads:
+            raise ValueError("heads is a multiple of kv_heads")
         self.heads, self.kv_heads, self.dim, self.causal = heads, kv_heads, dim, causal
         self.scale = dim ** -0.5 if scale is None else scale
 
-    def _shape(self, q, k, q_lengths, kv_lengths):
-        batch = q.shape[0]
-        for name, t in (("q_lengths", q_lengths), ("kv_lengths", kv_lengths)):
+    def _describe(self, q, k, q_lengths, kv_lengths):
+        """(sizes, shape of the query side, shape of the key side) of a call."""
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("q and k: [batch, length, head, dim] is wanted")
+        batch, q_len = q.shape[:2]
+        kv_len = k.shape[1]
+        if not q.is_cuda:
+            raise _elsewhere(q=q)
+        at = [None, None]
+        for i, t in enumerate((q_lengths, kv_lengths)):
             if t is not None:
-                _need(t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == (batch,) and t.device == q.device,
-                      f"{name}: contiguous int32 [batch] on the tensors' device is wanted")
-        return B.omni_attn(batch, q.shape[1], k.shape[1], self.heads, self.kv_heads, self.dim, self.causal, self.scale,
-                           None if q_lengths is None else q_lengths.data_ptr(),
-                           None if kv_lengths is None else kv_lengths.data_ptr())
+                if t.dtype != torch.int32 or not t.is_contiguous() or t.shape != (batch,) or t.get_device() != q.get_device():
+                    raise ValueError("q_lengths and kv_lengths: contiguous int32 [batch] on the tensors' device is wanted")
+                at[i] = t.data_ptr()
+        return (B.omni_attn(batch, q_len, kv_len, self.heads, self.kv_heads, self.dim, self.causal, self.scale, *at),
+                (batch, q_len, self.heads, self.dim), (batch, kv_len, self.kv_heads, self.dim))
 
-    def _view(self, t, what: str, like, length: int, heads: int):
-        if t.dtype != torch.bfloat16:
+    @staticmethod
+    def _view(t, what: str, shape, device: int):
+        if t.dtype != _bf16:
             raise TypeError(f"{what}: dtype {t.dtype} is not bfloat16")
-        _need(tuple(t.shape) == (like.shape[0], length, heads, self.dim) and (self.dim == 1 or t.stride(3) == 1),
-              f"{what}: shape {(like.shape[0], length, heads, self.dim)} with a contiguous last dimension is wanted")
-        _on(like.device, **{what: t})
-        return B.omni_attn_view(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+        batch, row, head, one = t.stride()
+        if t.shape != shape or one != 1 or t.get_device() != device:
+            raise ValueError(f"{what}: shape {shape} with a contiguous last dimension on one device is wanted, "
+                             f"got {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+        return B.omni_attn_view(t.data_ptr(), batch, row, head)
 
     def forward(self, q, k, v, q_lengths=None, kv_lengths=None, out=None, stream=None):
         """Returns (out like q, lse float32 [batch, heads, q_len])."""
-        _need(q.dim() == 4 and k.dim() == 4, "q and k: [batch, length, head, dim] is wanted")
-        a = self._shape(q, k, q_lengths, kv_lengths)
-        with self._allocating(stream):
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            lse = torch.empty(a.batch, self.heads, a.q_len, device=q.device)
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.forward(q, k, v, q_lengths, kv_lengths, out)
+        a, rows, keys = self._describe(q, k, q_lengths, kv_lengths)
+        device, view = q.get_device(), self._view
+        if out is None:
+            out = _empty(rows, dtype=_bf16, device=q.device)
+        lse = _empty((rows[0], self.heads, rows[1]), dtype=_float, device=q.device)
         self._check(self._lib.omni_attn_forward(
-            self.ctx._h, C.byref(a), C.byref(self._view(q, "q", q, a.q_len, self.heads)),
-            C.byref(self._view(k, "k", q, a.kv_len, self.kv_heads)), C.byref(self._view(v, "v", q, a.kv_len, self.kv_heads)),
-            C.byref(self._view(out, "out", q, a.q_len, self.heads)), lse.data_ptr(), self._stream(stream)))
+            self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),
+            _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(), _current_stream()))
         return out, lse
 
     def backward(self, q, k, v, out, lse, grad_out, q_lengths=None, kv_lengths=None, grads=None, stream=None):
-        """Returns the gradients of (q, k, v); into ``grads``, a tuple of three, if given.  ``out`` and ``lse`` are the
-        forward call's."""
-        _need(q.dim() == 4 and k.dim() == 4, "q and k: [batch, length, head, dim] is wanted")
-        a = self._shape(q, k, q_lengths, kv_lengths)
-        _need(lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (a.batch, self.heads, a.q_len)
-              and lse.device == q.device, "lse: contiguous float32 [batch, heads, q_len] is wanted")
-        with self._allocating(stream):
-            dq, dk, dv = grads or (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-            # the library's own query: rows of whole tiles, two floats each
-            size = C.c_uint64()
-            self._check(self._lib.omni_attn_workspace(C.byref(a), C.byref(size)))
-            scratch = torch.empty(max(16, size.value), dtype=torch.uint8, device=q.device)
-        rows = [C.byref(self._view(t, name, q, a.q_len, self.heads))
-                for t, name in ((q, "q"), (out, "out"), (grad_out, "grad_out"), (dq, "grads[0]"))]
-        keys = [C.byref(self._view(t, name, q, a.kv_len, self.kv_heads))
-                for t, name in ((k, "k"), (v, "v"), (dk, "grads[1]"), (dv, "grads[2]"))]
+        """Returns the gradients of (q, k, v); into ``grads``, a tuple of three, if given.  ``out`` and
+        ``lse`` are the forward call's."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.backward(q, k, v, out, lse, grad_out, q_lengths, kv_lengths, grads)
+        a, rows, keys = self._describe(q, k, q_lengths, kv_lengths)
+        device, view, where = q.get_device(), self._view, q.device
+        if lse.dtype != _float or not lse.is_contiguous() or lse.shape != (rows[0], self.heads, rows[1]) or lse.get_device() != device:
+            raise ValueError("lse: contiguous float32 [batch, heads, q_len] is wanted")
+        if grads is None:
+            grads = (_empty(rows, dtype=_bf16, device=where), _empty(keys, dtype=_bf16, device=where),
+                     _empty(keys, dtype=_bf16, device=where))
+        size = self._sizes.get(rows)
+        if size is None:
+            need = C.c_uint64()
+            self._check(self._lib.omni_attn_workspace(_ref(a), _ref(need)))
+            size = self._sizes[rows] = max(16, need.value)
+        scratch = _empty(size, dtype=_byte, device=where)
+        dq, dk, dv = grads
         self._check(self._lib.omni_attn_backward(
-            self.ctx._h, C.byref(a), rows[0], keys[0], keys[1], rows[1], lse.data_ptr(), rows[2], rows[3], keys[2], keys[3],
-            scratch.data_ptr(), scratch.numel(), self._stream(stream)))
+            self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),
+            _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(),
+            _ref(view(grad_out, "grad_out", rows, device)), _ref(view(dq, "grads[0]", rows, device)),
+            _ref(view(dk, "grads[1]", keys, device)), _ref(view(dv, "grads[2]", keys, device)), scratch.data_ptr(), size,
+            _current_stream()))
         return dq, dk, dv
 
 
@@ -192,61 +232,73 @@ class Distillation(_Operator):
 
     def __init__(self, ctx: "B.Omni", temperature: float = 1.0):
         super().__init__(ctx)
-        _need(temperature > 0, "temperature is positive")
+        if not temperature > 0:
+            raise ValueError("temperature is positive")
         self.temperature = temperature
 
     def _describe(self, logits, top_logits, top_index):
-        _need(logits.dim() == 2 and top_logits.dim() == 2 and top_logits.shape == top_index.shape
-              and top_logits.shape[0] == logits.shape[0],
-              "logits [rows, vocab], top_logits and top_index [rows, top] are wanted")
-        if top_logits.dtype != torch.float32:
+        if top_logits.dtype != _float:
             raise TypeError("top_logits: float32 is wanted")
+        rows, vocab = logits.shape
+        n, top = top_logits.shape
+        if n != rows or top_index.shape != (n, top):
+            raise ValueError("logits [rows, vocab], top_logits and top_index [rows, top] are wanted")
         stride = _rows(top_logits, "top_logits")
-        _need(_rows(top_index, "top_index") == stride, "top_logits and top_index: the same stride is wanted")
-        _on(logits.device, top_logits=top_logits, top_index=top_index)
-        return B.omni_distill(logits.data_ptr(), logits.shape[0], _rows(logits, "logits"), logits.shape[1],
-                              _code(logits, _DTYPES, "logits"), top_logits.data_ptr(), top_index.data_ptr(), stride,
-                              top_logits.shape[1], _code(top_index, _INDEX, "top_index"), self.temperature)
+        if _rows(top_index, "top_index") != stride:
+            raise ValueError("top_logits and top_index: the same stride is wanted")
+        if not logits.is_cuda or not logits.get_device() == top_logits.get_device() == top_index.get_device():
+            raise _elsewhere(logits=logits, top_logits=top_logits, top_index=top_index)
+        return B.omni_distill(logits.data_ptr(), rows, _rows(logits, "logits"), vocab, _code(logits, _DTYPES, "logits"),
+                              top_logits.data_ptr(), top_index.data_ptr(), stride, top, _code(top_index, _INDEX, "top_index"),
+                              self.temperature)
 
     @staticmethod
-    def _row_values(t, logits, what: str):
-        _need(t.dtype == torch.float32 and t.is_contiguous() and tuple(t.shape) == (logits.shape[0],),
-              f"{what}: contiguous float32 [rows] is wanted")
-        _on(logits.device, **{what: t})
+    def _row_values(t, logits, what: str) -> int:
+        if t.dtype != _float or not t.is_contiguous() or t.shape != logits.shape[:1] or t.get_device() != logits.get_device():
+            raise ValueError(f"{what}: contiguous float32 [rows] on the logits' device is wanted")
         return t.data_ptr()
 
-    def _grad_like(self, logits, grad):
+    @staticmethod
+    def _grad_like(logits, grad):
         if grad is None:
-            grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        _need(grad.shape == logits.shape and grad.dtype == logits.dtype, "grad: the logits' shape and dtype are wanted")
-        _on(logits.device, grad=grad)
+            return _empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.get_device() != logits.get_device():
+            raise ValueError("grad: the logits' shape, dtype and device are wanted")
         return grad
 
     def forward(self, logits, top_logits, top_index, stream=None):
         """Returns (loss, lse), float32 [rows] each."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.forward(logits, top_logits, top_index)
         d = self._describe(logits, top_logits, top_index)
-        with self._allocating(stream):
-            loss, lse = torch.empty(2, logits.shape[0], device=logits.device)
-        self._check(self._lib.omni_distill_forward(self.ctx._h, C.byref(d), loss.data_ptr(), lse.data_ptr(), self._stream(stream)))
+        loss = _empty(d.rows, dtype=_float, device=logits.device)
+        lse = _empty(d.rows, dtype=_float, device=logits.device)
+        self._check(self._lib.omni_distill_forward(self.ctx._h, _ref(d), loss.data_ptr(), lse.data_ptr(), _current_stream()))
         return loss, lse
 
     def backward(self, logits, top_logits, top_index, lse, grad_loss, grad=None, stream=None):
         """Gradient of the logits from ``lse`` of the forward call and ``grad_loss`` [rows]; ``grad`` may be ``logits``."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.backward(logits, top_logits, top_index, lse, grad_loss, grad)
         d = self._describe(logits, top_logits, top_index)
-        with self._allocating(stream):
-            grad = self._grad_like(logits, grad)
+        grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_distill_backward(
-            self.ctx._h, C.byref(d), self._row_values(lse, logits, "lse"), self._row_values(grad_loss, logits, "grad_loss"),
-            grad.data_ptr(), _rows(grad, "grad"), self._stream(stream)))
+            self.ctx._h, _ref(d), self._row_values(lse, logits, "lse"), self._row_values(grad_loss, logits, "grad_loss"),
+            grad.data_ptr(), _rows(grad, "grad"), _current_stream()))
         return grad
 
     def step(self, logits, top_logits, top_index, grad_loss, grad=None, stream=None):
         """Forward and backward in one pass; returns (loss, lse, gradient of the logits)."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.step(logits, top_logits, top_index, grad_loss, grad)
         d = self._describe(logits, top_logits, top_index)
-        with self._allocating(stream):
-            loss, lse = torch.empty(2, logits.shape[0], device=logits.device)
-            grad = self._grad_like(logits, grad)
-        self._check(self._lib.omni_distill_step(
-            self.ctx._h, C.byref(d), self._row_values(grad_loss, logits, "grad_loss"), loss.data_ptr(), lse.data_ptr(),
-            grad.data_ptr(), _rows(grad, "grad"), self._stream(stream)))
+        weights = self._row_values(grad_loss, logits, "grad_loss")
+        loss = _empty(d.rows, dtype=_float, device=logits.device)
+        lse = _empty(d.rows, dtype=_float, device=logits.device)
+        grad = self._grad_like(logits, grad)
+        self._check(self._lib.omni_distill_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), lse.data_ptr(),
+                                                grad.data_ptr(), _rows(grad, "grad"), _current_stream()))
         return loss, lse, grad

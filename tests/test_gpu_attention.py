@@ -9,6 +9,7 @@ sum over dim <= 128 in float, the hardware's 2^x).  P and dS are rounded to bflo
   |dQ error| <= scale E |K|                   + 2^-8 |dQ|      (dK the same with E^T |Q|)
 The backward pass is compared from the out and lse that it is given.
 """
+import gc
 import math
 
 import pytest
@@ -223,6 +224,7 @@ def test_in_a_captured_graph(ctx):
     out, lse = a.forward(q, k, v)
     want = a.backward(q, k, v, out, lse, do)
     torch.cuda.synchronize()
+    gc.collect()                 # a context of another module that is freed during the capture would end it
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
         o2, l2 = a.forward(q, k, v)

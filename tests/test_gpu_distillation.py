@@ -75,7 +75,7 @@ def inputs(rows, vocab, top, dtype, index, seed, temp=1.0):
 @pytest.mark.parametrize("rows,vocab,top,index,temp", [
     (1, 1, 1, torch.int64, 1.0), (3, 7, 2, torch.int32, 2.0), (5, 16, 16, torch.int64, 1.0), (4, 100, 5, torch.int32, 4.0),
     (33, 1000, 64, torch.int64, 1.0), (9, 5003, 256, torch.int32, 2.0), (7, 50257, 33, torch.int64, 0.5),
-    (2, 131075, 100, torch.int32, 1.0), (1, 300007, 8, torch.int64, 1.0), (600, 2049, 3, torch.int32, 1.0),
+    (2, 131075, 100, torch.int32, 1.0), (1, 300007, 8, torch.int64, 1.0), (2, 1000003, 8, torch.int64, 1.0), (200, 131072, 4, torch.int32, 1.0), (600, 2049, 3, torch.int32, 1.0),
 ])
 def test_against_64_bits(ctx, dtype, rows, vocab, top, index, temp):
     check(ctx, *inputs(rows, vocab, top, dtype, index, rows + vocab)[:3], temp,
