@@ -66,8 +66,10 @@ template <> struct Group<float> {
     float4 a, b;
     __device__ __forceinline__ void load(const float *p)
     {
-        a = *reinterpret_cast<const float4 *>(p);
-        b = *reinterpret_cast<const float4 *>(p + 4);
+        float f[kGroup];
+        load_group(p, f);
+        a = make_float4(f[0], f[1], f[2], f[3]);
+        b = make_float4(f[4], f[5], f[6], f[7]);
     }
     __device__ __forceinline__ float largest() const
     {

@@ -6,29 +6,30 @@
 // Gradient: dW_v = s * sum_{t_i = v} dy_i.  Scattered adds with atomics would leave the order of
 // the sum to chance, so the tokens are sorted first and every row of the table is then written
 // once, by an owner that adds its terms in order:
-//   1. sort_tokens: CTA c owns the ids [512 c, 512 c + 512).  It walks all n tokens, counts its own
-//      (per warp and id, in shared memory) and those of smaller ids, which gives its place in the sorted
-//      order without a word between CTAs, then walks them again and writes (position, id) at its place.
-//      Stable: warps take consecutive stretches of the tokens, lanes of a match rank by lane.
+//   1. sort_tokens: a stable radix sort of (position, id) by nine bits a pass, by one cluster of up to eight CTAs.  A
+//      CTA takes a consecutive stretch of the list, a warp a consecutive part of that; counts per (warp,
+//      digit) in shared memory, joined over the cluster through distributed shared memory, give every token its place;
+//      lanes of one digit rank by lane.  The other CTAs of the launch set the whole table to zero meanwhile: a row
+//      with tokens is written twice, but the sort, which waits more than it moves, is hidden.
 //   2. sum_runs: the sorted list is cut into blocks of 32, whatever the ids, so that a token that
 //      fills a tenth of the batch is spread over as many owners as it needs.  A group of lanes adds a
-//      block's rows in registers, and where the id changes writes the row -- or, for the run
-//      that crosses the block's edge, a float partial to the workspace.  Rows without a token are set to zero by
-//      further groups of the same launch.
-//   3. join_runs: for each run that crosses an edge, the owner of its first block adds the partials
-//      in block order and writes the row.
+//      block's rows in registers and writes a row where the id changes; runs that cross blocks are joined
+//      in block order in shared memory, those that cross CTAs leave a float partial in the workspace.
+//   3. join_runs: the CTA in which such a run starts adds its partials in order and writes the row.
 #include "context.h"
 #include "vector.cuh"
 
 namespace omni {
 namespace {
 
-constexpr int kIdsPerCta = 512;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortPerCta = 1024;   // tokens that make another CTA worth its barriers
 constexpr int kBlock = 32;          // sorted tokens per block
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;           // rows in flight per group of lanes
+constexpr int kBatch = 4;           // accesses in flight per lane
+constexpr int kJoinAhead = 8;       // partials in flight of a run that is joined
 
 struct Entry { int pos, id; };      // a token's place in the batch, and its id
 
@@ -81,85 +82,178 @@ __global__ void __launch_bounds__(kThreads) embed_lookup_kernel(const void *toke
 
 // ---- sort ---------------------------------------------------------------------------------------
 
-template <typename I>
-__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const void *tokens, long long n, int vocab,
-                                                                   long long padding, Entry *sorted, int *start)
+struct SortParams {
+    const void *tokens;
+    long long n, padding;
+    int vocab, passes;
+    Entry *sorted, *other;       // the last pass ends in `sorted`
+    int *total;                  // tokens that count
+    int ranks;                   // CTAs that sort: the first cluster
+    char *table;                 // what the others set to zero: vocab rows of row_bytes, table_stride bytes apart; or null
+    unsigned long long row_bytes, table_stride;
+};
+
+// The table set to zero by the CTAs rank = 0..ranks-1.  16-byte stores where rows allow them.
+__device__ __forceinline__ void zero_table(const SortParams &p, long long rank, long long ranks)
 {
-    extern __shared__ int hist[];   // [kSortWarps][kIdsPerCta]
-    __shared__ int below_total, warp_sum[kIdsPerCta / 32];
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int lo = blockIdx.x * kIdsPerCta;
-    for (int i = threadIdx.x; i < kSortWarps * kIdsPerCta; i += kSortThreads) hist[i] = 0;
-    if (threadIdx.x == 0) below_total = 0;
-    __syncthreads();
-    const long long stretch = ((n + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
-    const long long first = warp * stretch, last = first + stretch < n ? first + stretch : n;
-    int *mine = hist + warp * kIdsPerCta;
-    int below = 0;
-    for (long long base = first; base < last; base += 32 * 4) {
-        int id[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const long long i = base + b * 32 + lane;
-            id[b] = i < last ? token_id<I>(tokens, i, vocab, padding) : -1;
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            below += id[b] >= 0 && id[b] < lo;
-            if (id[b] >= lo && id[b] < lo + kIdsPerCta) atomicAdd(&mine[id[b] - lo], 1);
-        }
+    const bool packed = p.row_bytes == p.table_stride;
+    const unsigned long long rows = packed ? 1 : p.vocab, bytes = packed ? p.row_bytes * p.vocab : p.row_bytes;
+    const bool wide = (reinterpret_cast<uintptr_t>(p.table) | (packed ? 0 : p.table_stride)) % 16 == 0;
+    const unsigned long long at = (unsigned long long)rank * blockDim.x + threadIdx.x, step = (unsigned long long)ranks * blockDim.x;
+    if (packed) {
+        char *t = p.table;
+        const unsigned long long whole = wide ? bytes / 16 : 0;
+        for (unsigned long long i = at; i < whole; i += step) __stcs(reinterpret_cast<uint4 *>(t) + i, make_uint4(0, 0, 0, 0));
+        for (unsigned long long i = whole * 16 + 2 * at; i < bytes; i += 2 * step) *reinterpret_cast<unsigned short *>(t + i) = 0;
+        return;
     }
-    for (int o = 16; o > 0; o /= 2) below += __shfl_down_sync(~0u, below, o);
-    if (lane == 0 && below) atomicAdd(&below_total, below);
-    __syncthreads();
-    // exclusive sums: over the warps of an id, then over the ids
-    int total = 0, inc = 0;
-    if (threadIdx.x < kIdsPerCta) {
-        for (int w = 0; w < kSortWarps; ++w) {
-            const int c = hist[w * kIdsPerCta + threadIdx.x];
-            hist[w * kIdsPerCta + threadIdx.x] = total;
-            total += c;
+    const unsigned long long warps = step / 32;
+    for (unsigned long long r = at / 32; r < rows; r += warps) {
+        char *t = p.table + r * p.table_stride;
+        const unsigned long long whole = wide ? bytes / 16 : 0;
+        for (unsigned long long i = threadIdx.x % 32; i < whole; i += 32) __stcs(reinterpret_cast<uint4 *>(t) + i, make_uint4(0, 0, 0, 0));
+        for (unsigned long long i = whole * 16 + 2 * (threadIdx.x % 32); i < bytes; i += 64) *reinterpret_cast<unsigned short *>(t + i) = 0;
+    }
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int load_remote(const int *cell, unsigned rank)
+{
+    unsigned at;
+    int x;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(unsigned(__cvta_generic_to_shared(cell))), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    return x;
+}
+
+// The lanes of a warp that have this lane's digit (-1: none).
+__device__ __forceinline__ unsigned lanes_of(int digit)
+{
+    unsigned peers = __ballot_sync(~0u, digit >= 0);
+#pragma unroll
+    for (int bit = 0; bit < kDigitBits; ++bit) {
+        const bool set = digit >> bit & 1;
+        const unsigned b = __ballot_sync(~0u, set);
+        peers &= set ? b : ~b;
+    }
+    return peers;
+}
+
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads) sort_tokens_kernel(const SortParams p)
+{
+    extern __shared__ int hist[];                   // [kSortWarps][kDigits]: a warp's tokens, then its first place in the CTA's
+    __shared__ int mine[kDigits], place_of[kDigits], warp_sum[kDigits / 32];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, ranks = p.ranks, rank = blockIdx.x;
+    if (rank >= ranks) {
+        zero_table(p, rank - ranks, gridDim.x - ranks);
+        return;
+    }
+    int *own = hist + warp * kDigits;
+    long long m = p.n;
+    const Entry *from = nullptr;
+    for (int pass = 0; pass < p.passes; ++pass) {
+        Entry *to = (p.passes - pass) % 2 == 1 ? p.sorted : p.other;
+        const int shift = pass * kDigitBits;
+        // this warp's part [first, last) of the list
+        const long long part = ((m + ranks * kSortWarps - 1) / (ranks * kSortWarps) + 31) / 32 * 32;
+        const long long first = ((long long)rank * kSortWarps + warp) * part, last = first + part < m ? first + part : m;
+        auto fetch = [&](long long base, Entry (&e)[kBatch], int (&digit)[kBatch]) {
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                const long long i = base + b * 32 + lane;
+                e[b] = {-1, -1};
+                if (i < last) {
+                    if (!from) {
+                        e[b] = {int(i), token_id<I>(p.tokens, i, p.vocab, p.padding)};
+                    } else {
+                        const int2 x = __ldcg(reinterpret_cast<const int2 *>(from + i));
+                        e[b] = {x.x, x.y};
+                    }
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) digit[b] = e[b].id >= 0 ? e[b].id >> shift & (kDigits - 1) : -1;
+        };
+        Entry e[kBatch];
+        int digit[kBatch];
+        unsigned peers[kBatch];
+        fetch(first, e, digit);
+        for (int i = tid; i < kSortWarps * kDigits / 4; i += kSortThreads) reinterpret_cast<int4 *>(hist)[i] = make_int4(0, 0, 0, 0);
+        __syncthreads();
+        for (long long base = first; base < last; base += 32 * kBatch) {
+            if (base > first) fetch(base, e, digit);
+#pragma unroll
+            for (int b = 0; b < kBatch; ++b) {
+                peers[b] = lanes_of(digit[b]);      // one add per digit: half of a batch may have the same
+                if (digit[b] >= 0 && (peers[b] & ((1u << lane) - 1u)) == 0) own[digit[b]] += __popc(peers[b]);
+                __syncwarp();
+            }
         }
-        inc = total;
+        __syncthreads();
+        // over the warps of a digit, over the CTAs, over the digits
+        int before = 0, all = 0;
+        if (tid < kDigits) {
+            int c[kSortWarps], sum = 0;
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) c[w] = hist[w * kDigits + tid];
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) {
+                hist[w * kDigits + tid] = sum;
+                sum += c[w];
+            }
+            mine[tid] = sum;
+            all = sum;
+        }
+        if (ranks > 1) {
+            cluster_sync();
+            if (tid < kDigits) {
+                all = 0;
+                for (int k = 0; k < ranks; ++k) {
+                    const int c = load_remote(mine + tid, k);
+                    if (k < rank) before += c;
+                    all += c;
+                }
+            }
+        }
+        int inc = all;
         for (int o = 1; o < 32; o *= 2) {
             const int y = __shfl_up_sync(~0u, inc, o);
             if (lane >= o) inc += y;
         }
-        if (lane == 31) warp_sum[warp] = inc;
-    }
-    __syncthreads();
-    if (threadIdx.x < kIdsPerCta) {
-        int at = below_total + inc - total;
-        for (int w = 0; w < warp; ++w) at += warp_sum[w];
-        const int id = lo + threadIdx.x;
-        if (id < vocab) start[id] = at;
-        if (id == vocab - 1) start[vocab] = at + total;
-        for (int w = 0; w < kSortWarps; ++w) hist[w * kIdsPerCta + threadIdx.x] += at;
-    }
-    __syncthreads();
-    for (long long base = first; base < last; base += 32 * 4) {
-        int id[4];
+        if (tid < kDigits && lane == 31) warp_sum[warp] = inc;
+        __syncthreads();
+        int total = 0;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const long long i = base + b * 32 + lane;
-            id[b] = i < last ? token_id<I>(tokens, i, vocab, padding) : -1;
+        for (int w = 0; w < kDigits / 32; ++w) {
+            if (w < warp) before += warp_sum[w];
+            total += warp_sum[w];
         }
+        if (tid < kDigits) place_of[tid] = before + inc - all;
+        __syncthreads();
+        const bool once = part <= 32 * kBatch;      // the batch of the first walk is still there
+        for (long long base = first; base < last; base += 32 * kBatch) {
+            if (!once) fetch(base, e, digit);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const bool in = id[b] >= lo && id[b] < lo + kIdsPerCta;
-            const unsigned takers = __ballot_sync(~0u, in);
-            if (!takers) continue;
-            if (in) {
-                const unsigned peers = __match_any_sync(takers, id[b]);
-                const int rank = __popc(peers & ((1u << lane) - 1u));
-                const int at = mine[id[b] - lo] + rank;
-                sorted[at] = {int(base + b * 32 + lane), id[b]};
-                __syncwarp(takers);
-                if (rank == 0) mine[id[b] - lo] += __popc(peers);
-                __syncwarp(takers);
+            for (int b = 0; b < kBatch; ++b) {
+                if (!once) peers[b] = lanes_of(digit[b]);
+                const int rank_in = __popc(peers[b] & ((1u << lane) - 1u));
+                if (digit[b] >= 0) to[place_of[digit[b]] + own[digit[b]] + rank_in] = e[b];
+                __syncwarp();
+                if (digit[b] >= 0 && rank_in == 0) own[digit[b]] += __popc(peers[b]);
+                __syncwarp();
             }
         }
+        m = total;
+        from = to;
+        // the next pass reads what the others wrote, and nobody leaves while `mine` may be read
+        if (ranks > 1) cluster_sync();
+        else __syncthreads();
     }
+    if (rank == 0 && tid == 0) *p.total = int(m);
 }
 
 // ---- sums ---------------------------------------------------------------------------------------
@@ -181,106 +275,181 @@ __device__ __forceinline__ void put_row(G *dst, int col, float *acc, float scale
 
 struct RunParams {
     const Entry *sorted;
-    const int *start;
-    float *partial;             // [2 * blocks][padded dim]
-    long long blocks;           // upper bound: of n tokens
-    int vocab, dim, padded;     // padded: dim rounded up to 8
+    const int *total;
+    float *partial;             // [2 * CTAs along the list][padded dim]: the run that enters, the run that leaves
+    int dim, padded;            // padded: dim rounded up to 8
     int lanes, slices;          // lanes per group, column slices of lanes * E elements
     float scale;
     int accumulate;
     unsigned long long src_stride, dst_stride;
 };
 
+// Rows of a block of sorted tokens: raw, so that more of them are in flight per register.
+template <typename T, bool WIDE> struct RawRow;
+template <> struct RawRow<__nv_bfloat16, true> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = __ldcs(reinterpret_cast<const uint4 *>(p)); }
+    __device__ __forceinline__ void add(float *acc) const
+    {
+        float f[kGroup];
+        widen(u, f);
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) acc[e] += f[e];
+    }
+};
+template <> struct RawRow<float, true> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float *p)
+    {
+        float f[kGroup];
+        load_group(p, f);
+        a = make_float4(f[0], f[1], f[2], f[3]);
+        b = make_float4(f[4], f[5], f[6], f[7]);
+    }
+    __device__ __forceinline__ void add(float *acc) const
+    {
+        acc[0] += a.x; acc[1] += a.y; acc[2] += a.z; acc[3] += a.w;
+        acc[4] += b.x; acc[5] += b.y; acc[6] += b.z; acc[7] += b.w;
+    }
+};
+template <typename T> struct RawRow<T, false> {
+    T x;
+    __device__ __forceinline__ void load(const T *p) { x = *p; }
+    __device__ __forceinline__ void add(float *acc) const { acc[0] += to_float(x); }
+};
+
+// A CTA takes kThreads / lanes consecutive blocks of the sorted list and one slice of the columns.
 template <typename T, typename G, bool WIDE>
-__global__ void __launch_bounds__(kThreads) sum_runs_kernel(RunParams p, const T *src, G *dst, long long run_groups)
+__global__ void __launch_bounds__(kThreads, 4) sum_runs_kernel(const RunParams p, const T *src, G *dst)
 {
     constexpr int E = WIDE ? kGroup : 1;
-    const int per = kThreads / p.lanes, lane = threadIdx.x % p.lanes;
-    const long long g = (long long)blockIdx.x * per + threadIdx.x / p.lanes;
-    if (g >= run_groups) {
-        // rows without a token: zeros
-        const long long v = g - run_groups;
-        if (p.accumulate || v >= p.vocab || p.start[v] != p.start[v + 1]) return;
-        G *row = dst + (unsigned long long)v * p.dst_stride;
-        float zero[E] = {};
-        for (int col = lane * E; col < p.dim; col += p.lanes * E) {
-            if constexpr (WIDE) store_group(row + col, zero);
-            else row[col] = from_float<G>(0.0f);
-        }
-        return;
-    }
-    const long long block = g / p.slices;
-    const int col = (int(g % p.slices) * p.lanes + lane) * E;
-    const int total = p.start[p.vocab];
-    const long long begin = block * kBlock;
-    if (begin >= total || col >= p.dim) return;
-    const int end = begin + kBlock < total ? int(begin) + kBlock : total;
-    int cur = p.sorted[begin].id;
-    bool open = begin > 0 && p.sorted[begin - 1].id == cur;     // the run began before this block
-    const int next = end < total ? p.sorted[end].id : -1;
-    float acc[E] = {};
-    for (int i = int(begin); i < end; i += kBatch) {
-        Entry en[kBatch];
-        float f[kBatch][E];
+    constexpr int kRowsAhead = sizeof(T) == 2 ? 8 : 4;
+    __shared__ float enters[kThreads * E], leaves[kThreads * E];    // [block of the CTA][column of the slice]
+    __shared__ int4 runs[kThreads];                                 // per block: first id, last id, see below
+    const int per = kThreads / p.lanes, lane = threadIdx.x % p.lanes, mine = threadIdx.x / p.lanes, cols = p.lanes * E;
+    const int slice = blockIdx.x % p.slices;
+    const long long cta = blockIdx.x / p.slices;
+    const int col = slice * cols + lane * E;
+    const int total = *p.total;
+    const long long begin = (cta * per + mine) * kBlock;
+    if (cta * per * kBlock >= total) return;
+    constexpr int kEnters = 1, kLeaves = 2, kWhole = 4;             // the run crosses the block's start, its end, fills it
+    int how = 0, cur = -1, first_id = -1;
+    if (begin < total) {
+        const int end = begin + kBlock < total ? int(begin) + kBlock : total;
+        first_id = cur = p.sorted[begin].id;
+        bool open = begin > 0 && p.sorted[begin - 1].id == cur;
+        const int next = end < total ? p.sorted[end].id : -1;
+        if (open) how |= kEnters;
+        float acc[E] = {};
+        const bool inside = col < p.dim;
+        for (int i = int(begin); i < end; i += kRowsAhead) {
+            Entry en[kRowsAhead];
+            RawRow<T, WIDE> x[kRowsAhead];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) en[b] = i + b < end ? p.sorted[i + b] : Entry{-1, -1};
+            for (int b = 0; b < kRowsAhead; ++b) en[b] = i + b < end ? p.sorted[i + b] : Entry{-1, -1};
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b)
-            if (en[b].id >= 0) {
-                const T *row = src + (unsigned long long)en[b].pos * p.src_stride;
-                if constexpr (WIDE) load_group(row + col, f[b]);
-                else f[b][0] = to_float(row[col]);
-            }
+            for (int b = 0; b < kRowsAhead; ++b)
+                if (en[b].id >= 0 && inside) x[b].load(src + (unsigned long long)en[b].pos * p.src_stride + col);
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            if (en[b].id < 0) continue;
-            if (en[b].id != cur) {
-                if (open) {
+            for (int b = 0; b < kRowsAhead; ++b) {
+                if (en[b].id < 0) continue;
+                if (en[b].id != cur) {
+                    if (open) {
 #pragma unroll
-                    for (int e = 0; e < E; ++e) p.partial[(2 * block) * p.padded + col + e] = acc[e];
-                } else {
-                    put_row<G, WIDE>(dst + (unsigned long long)cur * p.dst_stride, col, acc, p.scale, p.accumulate);
+                        for (int e = 0; e < E; ++e) enters[mine * cols + lane * E + e] = acc[e];
+                    } else if (inside) {
+                        put_row<G, WIDE>(dst + (unsigned long long)cur * p.dst_stride, col, acc, p.scale, p.accumulate);
+                    }
+                    open = false;
+                    cur = en[b].id;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
                 }
-                open = false;
-                cur = en[b].id;
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+                if (inside) x[b].add(acc);
             }
+        }
+        if (next == cur) how |= kLeaves;
+        if (open) how |= kWhole;                                    // one run from start to end: its sum is in `enters`
+        if (open || next == cur) {
+            float *to = (open ? enters : leaves) + mine * cols + lane * E;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += f[b][e];
+            for (int e = 0; e < E; ++e) to[e] = acc[e];
+        } else if (inside) {
+            put_row<G, WIDE>(dst + (unsigned long long)cur * p.dst_stride, col, acc, p.scale, p.accumulate);
         }
     }
-    if (!open && next != cur) {
-        put_row<G, WIDE>(dst + (unsigned long long)cur * p.dst_stride, col, acc, p.scale, p.accumulate);
-    } else {
+    if (lane == 0) runs[mine] = make_int4(first_id, cur, how, 0);
+    __syncthreads();
+    // the runs that cross blocks, in block order, a thread per group of E columns
+    if (threadIdx.x >= p.lanes || col >= p.dim) return;             // the first group's lanes: their columns are the CTA's
+    float acc[E] = {};
+    bool before = (runs[0].z & kEnters) != 0;                       // the run at hand began before the CTA
+    for (int k = 0; k < per && (cta * per + k) * kBlock < total; ++k) {
+        const int4 r = runs[k];
+        if (r.z & kEnters) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) p.partial[(2 * block + (open ? 0 : 1)) * p.padded + col + e] = acc[e];
+            for (int e = 0; e < E; ++e) acc[e] += enters[k * cols + lane * E + e];
+            if ((r.z & kWhole) && (r.z & kLeaves)) continue;
+            if (before) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) p.partial[2 * cta * p.padded + col + e] = acc[e];
+            } else {
+                put_row<G, WIDE>(dst + (unsigned long long)r.x * p.dst_stride, col, acc, p.scale, p.accumulate);
+            }
+            before = false;
+        }
+        if (r.z & kLeaves) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = leaves[k * cols + lane * E + e];
+        }
+    }
+    const long long after = (cta + 1) * per * kBlock;
+    if (after < total && (runs[per - 1].z & kLeaves)) {             // into the next CTA, as one that entered or one that leaves
+#pragma unroll
+        for (int e = 0; e < E; ++e) p.partial[(2 * cta + (before ? 0 : 1)) * p.padded + col + e] = acc[e];
     }
 }
 
-// One group per (block, slice): if a run starts in the block and goes on in the next, add its partials.
+// A group per (CTA of sum_runs, slice): if a run starts there and goes on in the next, its partials are added.
 template <typename G, bool WIDE>
-__global__ void __launch_bounds__(kThreads) join_runs_kernel(RunParams p, G *dst, long long run_groups)
+__global__ void __launch_bounds__(kThreads) join_runs_kernel(const RunParams p, G *dst, long long ctas)
 {
     constexpr int E = WIDE ? kGroup : 1;
-    const int per = kThreads / p.lanes, lane = threadIdx.x % p.lanes;
-    const long long g = (long long)blockIdx.x * per + threadIdx.x / p.lanes;
-    if (g >= run_groups) return;
-    const long long block = g / p.slices;
+    const int per = kThreads / p.lanes, lane = threadIdx.x % p.lanes, span = per * kBlock;
+    const long long g = (long long)blockIdx.x * per + threadIdx.x / p.lanes, cta = g / p.slices;
     const int col = (int(g % p.slices) * p.lanes + lane) * E;
-    const int total = p.start[p.vocab];
-    const long long edge = (block + 1) * kBlock;
-    if (edge >= total || col >= p.dim) return;
+    const int total = *p.total;
+    const long long edge = (cta + 1) * span;
+    if (cta >= ctas || edge >= total || col >= p.dim) return;
     const int id = p.sorted[edge].id;
-    if (p.sorted[edge - 1].id != id || p.start[id] / kBlock != block) return;
-    const long long last = (p.start[id + 1] - 1) / kBlock;
+    if (p.sorted[edge - 1].id != id || (cta > 0 && p.sorted[cta * span - 1].id == id)) return;   // not crossed, or begun earlier
     float acc[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = p.partial[(2 * block + 1) * p.padded + col + e];
-#pragma unroll 4
-    for (long long b = block + 1; b <= last; ++b) {
+    for (int e = 0; e < E; ++e) acc[e] = p.partial[(2 * cta + 1) * p.padded + col + e];
+    for (long long b = cta + 1;; b += kJoinAhead) {
+        bool goes_on[kJoinAhead];
+        float x[kJoinAhead][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += p.partial[(2 * b) * p.padded + col + e];
+        for (int k = 0; k < kJoinAhead; ++k) {
+            const long long at = (b + k) * span;                 // the run reaches CTA b + k if it has its first token
+            goes_on[k] = at < total;
+            if (goes_on[k]) {                                    // fetched before it is known to belong: one wait instead of two
+                goes_on[k] = p.sorted[at].id == id;
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[k][e] = p.partial[2 * (b + k) * p.padded + col + e];
+            }
+        }
+        bool more = true;
+#pragma unroll
+        for (int k = 0; k < kJoinAhead; ++k) {
+            more = more && goes_on[k];
+            if (more) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] += x[k][e];
+            }
+        }
+        if (!more) break;
     }
     put_row<G, WIDE>(dst + (unsigned long long)id * p.dst_stride, col, acc, p.scale, p.accumulate);
 }
@@ -307,16 +476,16 @@ int lanes_for(int dim, bool wide)
     return lanes;
 }
 
-struct EmbedWorkspace { unsigned long long sorted, start, partial, bytes; };
+struct EmbedWorkspace { unsigned long long other, total, partial, bytes; };
 
-EmbedWorkspace plan_workspace(uint64_t n, int32_t vocab, int32_t dim)
+EmbedWorkspace plan_workspace(uint64_t n, int32_t dim)
 {
-    EmbedWorkspace w;
-    w.sorted = 0;
-    w.start = round_up(n * sizeof(Entry), 256);
-    w.partial = w.start + round_up((uint64_t(vocab) + 1) * sizeof(int), 256);
-    const uint64_t blocks = (n + kBlock - 1) / kBlock;
-    w.bytes = w.partial + 2 * blocks * round_up(dim, kGroup) * sizeof(float);
+    EmbedWorkspace w;                 // the sorted list comes first
+    w.other = round_up(n * sizeof(Entry), 256);
+    w.total = 2 * w.other;
+    w.partial = w.total + 256;
+    const uint64_t ctas = (n + 8 * kBlock - 1) / (8 * kBlock);      // of sum_runs along the list: eight blocks each at least
+    w.bytes = w.partial + 2 * ctas * round_up(dim, kGroup) * sizeof(float);
     return w;
 }
 
@@ -392,7 +561,7 @@ int omni_embed_workspace(uint64_t n, int32_t vocab, int32_t dim, uint64_t *bytes
     if (!bytes) return OMNI_ERR_NULL;
     if (vocab < 1 || dim < 1) return OMNI_ERR_BAD_CONFIG;
     if (n >= (1ull << 31)) return OMNI_ERR_TOO_LARGE;
-    *bytes = plan_workspace(n, vocab, dim).bytes;
+    *bytes = plan_workspace(n, dim).bytes;
     return OMNI_OK;
 }
 
@@ -407,33 +576,61 @@ int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, u
     if (rc != OMNI_OK) return rc;
     if (!workspace) return OMNI_ERR_NULL;
     if (!aligned(workspace, 16)) return OMNI_ERR_ALIGN;
-    const EmbedWorkspace w = plan_workspace(n, vocab, dim);
+    const EmbedWorkspace w = plan_workspace(n, dim);
     if (workspace_bytes < w.bytes) return OMNI_ERR_TOO_LARGE;
     ContextDevice dev;
     rc = context_bind(ctx, &dev);
     if (rc != OMNI_OK) return rc;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     char *ws = static_cast<char *>(workspace);
-    Entry *sorted = reinterpret_cast<Entry *>(ws + w.sorted);
-    int *start = reinterpret_cast<int *>(ws + w.start);
-    const int smem = kSortWarps * kIdsPerCta * int(sizeof(int));
+    SortParams o;
+    o.tokens = tokens;
+    o.n = (long long)n;
+    o.padding = padding;
+    o.vocab = vocab;
+    o.passes = 1;
+    while (o.passes < 4 && (uint64_t(vocab) - 1) >> (o.passes * kDigitBits) != 0) ++o.passes;
+    o.sorted = reinterpret_cast<Entry *>(ws);
+    o.other = reinterpret_cast<Entry *>(ws + w.other);
+    o.total = reinterpret_cast<int *>(ws + w.total);
+    o.ranks = 1;
+    while (o.ranks < 8 && n > uint64_t(o.ranks) * kSortPerCta) o.ranks *= 2;
+    o.table = static_cast<char *>(grad);
+    o.row_bytes = uint64_t(dim) * element_size(grad_dtype);
+    o.table_stride = vocab == 1 ? o.row_bytes : grad_stride * element_size(grad_dtype);
+    // beside the sort: CTAs for the zeros, as many as find 64 KB each to write, two per SM at most
+    int zero_ctas = 0;
+    if (!accumulate) {
+        const uint64_t want = o.row_bytes * vocab / 65536 + 1, most = 2ull * dev.sm_count;
+        zero_ctas = int(round_up(want < most ? want : most, o.ranks));
+    }
     rc = with_index(index_type, [&](auto *ip) {
         using I = std::remove_pointer_t<decltype(ip)>;
-        const int r = context_shared(ctx, reinterpret_cast<const void *>(sort_tokens_kernel<I>), smem);
+        const void *kernel = reinterpret_cast<const void *>(sort_tokens_kernel<I>);
+        const int smem = kSortWarps * kDigits * int(sizeof(int));
+        const int r = context_shared(ctx, kernel, smem);
         if (r != OMNI_OK) return r;
-        sort_tokens_kernel<I><<<(vocab + kIdsPerCta - 1) / kIdsPerCta, kSortThreads, smem, s>>>(tokens, (long long)n, vocab,
-                                                                                               padding, sorted, start);
-        return context_launched(ctx, int(cudaGetLastError()));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(o.ranks + zero_ctas);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = o.ranks;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        void *args[] = {&o};
+        return context_launched(ctx, int(cudaLaunchKernelExC(&cfg, kernel, args)));
     });
     if (rc != OMNI_OK) return rc;
     const bool wide = dim % kGroup == 0 && wide_rows(grad_out, grad_out_dtype, grad_out_stride) &&
                       wide_rows(grad, grad_dtype, grad_stride);
     RunParams p;
-    p.sorted = sorted;
-    p.start = start;
+    p.sorted = o.sorted;
+    p.total = o.total;
     p.partial = reinterpret_cast<float *>(ws + w.partial);
-    p.blocks = (n + kBlock - 1) / kBlock;
-    p.vocab = vocab;
     p.dim = dim;
     p.padded = int(round_up(dim, kGroup));
     p.lanes = lanes_for(dim, wide);
@@ -444,21 +641,19 @@ int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, u
     p.src_stride = grad_out_stride;
     p.dst_stride = grad_stride;
     const int per = kThreads / p.lanes;
-    const long long run_groups = p.blocks * p.slices;
-    const long long groups = run_groups + (accumulate ? 0 : vocab);
+    const long long ctas = ((long long)n + per * kBlock - 1) / (per * kBlock);
+    if (ctas == 0) return OMNI_OK;
     return with_type(grad_out_dtype, [&](auto *tp) {
         return with_type(grad_dtype, [&](auto *gp) {
             return with_flag(wide, [&](auto wd) {
                 using T = std::remove_pointer_t<decltype(tp)>;
                 using G = std::remove_pointer_t<decltype(gp)>;
                 constexpr bool W = decltype(wd)::value;
-                if (groups == 0) return int(OMNI_OK);
-                sum_runs_kernel<T, G, W><<<unsigned((groups + per - 1) / per), kThreads, 0, s>>>(
-                    p, static_cast<const T *>(grad_out), static_cast<G *>(grad), run_groups);
+                sum_runs_kernel<T, G, W><<<unsigned(ctas * p.slices), kThreads, 0, s>>>(p, static_cast<const T *>(grad_out),
+                                                                                        static_cast<G *>(grad));
                 const int r = context_launched(ctx, int(cudaGetLastError()));
-                if (r != OMNI_OK || p.blocks < 2) return r;
-                join_runs_kernel<G, W><<<unsigned((run_groups + per - 1) / per), kThreads, 0, s>>>(p, static_cast<G *>(grad),
-                                                                                                  run_groups);
+                if (r != OMNI_OK || ctas == 1) return r;
+                join_runs_kernel<G, W><<<unsigned((ctas * p.slices + per - 1) / per), kThreads, 0, s>>>(p, static_cast<G *>(grad), ctas);
                 return context_launched(ctx, int(cudaGetLastError()));
             });
         });

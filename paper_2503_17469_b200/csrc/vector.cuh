@@ -34,9 +34,16 @@ __device__ __forceinline__ uint4 narrow(const float *f)
     }
     return {w[0], w[1], w[2], w[3]};
 }
-// Eight elements at a 16-byte aligned address.
+// Eight elements at a 16-byte aligned address.  Floats take one 256-bit access where the address allows it: two of 128
+// bits would each touch half of every 32-byte sector of a warp's stretch.
+__device__ __forceinline__ bool aligned32(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 __device__ __forceinline__ void load_group(const float *p, float *f)
 {
+    if (aligned32(p)) {
+        asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]), "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7]) : "l"(p) : "memory");
+        return;
+    }
     const float4 a = *reinterpret_cast<const float4 *>(p), b = *reinterpret_cast<const float4 *>(p + 4);
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
     f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
@@ -44,14 +51,23 @@ __device__ __forceinline__ void load_group(const float *p, float *f)
 __device__ __forceinline__ void load_group(const __nv_bfloat16 *p, float *f) { widen(*reinterpret_cast<const uint4 *>(p), f); }
 __device__ __forceinline__ void store_group(float *p, const float *f)
 {
+    if (aligned32(p)) {
+        asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+        return;
+    }
     *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
     *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
 }
 __device__ __forceinline__ void store_group(__nv_bfloat16 *p, const float *f) { *reinterpret_cast<uint4 *>(p) = narrow(f); }
-
 // The same for values that nothing reads soon: first to leave L2.
 __device__ __forceinline__ void store_streaming(float *p, const float *f)
 {
+    if (aligned32(p)) {
+        asm volatile("st.global.cs.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]) : "memory");
+        return;
+    }
     __stcs(reinterpret_cast<float4 *>(p), make_float4(f[0], f[1], f[2], f[3]));
     __stcs(reinterpret_cast<float4 *>(p + 4), make_float4(f[4], f[5], f[6], f[7]));
 }
