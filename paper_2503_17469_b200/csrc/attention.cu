@@ -55,6 +55,8 @@ int check_shape(const omni_attn *a)
     if (a->dim < 8 || a->dim % 8 != 0 || !(a->scale > 0.0f) || !std::isfinite(a->scale)) return OMNI_ERR_BAD_CONFIG;
     if (a->dim > OMNI_ATTN_MAX_DIM || a->batch > 65535 || a->heads > 65535 || a->q_len > (1 << 30) || a->kv_len > (1 << 30))
         return OMNI_ERR_TOO_LARGE;
+    const int64_t rows = a->q_len > a->kv_len ? a->q_len : a->kv_len;
+    if ((rows / kRows + 1) * a->heads * a->batch >= (1ll << 31)) return OMNI_ERR_TOO_LARGE;      // CTAs of a launch
     if (!aligned(a->q_lengths, 4) || !aligned(a->kv_lengths, 4)) return OMNI_ERR_ALIGN;
     return OMNI_OK;
 }
@@ -133,7 +135,8 @@ int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q
     p.out = out_of(out);
     p.lse = lse;
     p.status = dev.status;
-    const dim3 grid((a->q_len + 2 * kRows - 1) / (2 * kRows), a->heads, a->batch);
+    p.q_tiles = (a->q_len + 2 * kRows - 1) / (2 * kRows);
+    const dim3 grid(unsigned(p.q_tiles) * a->heads * a->batch);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (a->dim <= 64) return launch(ctx, attention_forward_kernel<64>, grid, kForwardThreads, ForwardShared<64>::kBytes, s, p);
     return launch(ctx, attention_forward_kernel<128>, grid, kForwardThreads, ForwardShared<128>::kBytes, s, p);
@@ -179,6 +182,7 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
     p.row_lse = static_cast<float *>(workspace);
     p.row_delta = p.row_lse + uint64_t(a->batch) * a->heads * q_pad;
     p.q_pad = q_pad;
+    p.q_tiles = q_pad / kRows;
     p.dq = out_of(dq);
     p.dk = out_of(dk);
     p.dv = out_of(dv);
@@ -201,14 +205,14 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
     };
     if (a->kv_len > 0) {
         if ((rc = maps(kPiece, kRows)) != OMNI_OK) return rc;
-        const dim3 grid((a->kv_len + kRows - 1) / kRows, a->kv_heads, a->batch);
+        const dim3 grid(unsigned((a->kv_len + kRows - 1) / kRows) * a->kv_heads * a->batch);
         rc = a->dim <= 64 ? launch(ctx, attention_keys_kernel<64>, grid, kBackwardThreads, KeysShared<64>::kBytes, s, p)
                           : launch(ctx, attention_keys_kernel<128>, grid, kBackwardThreads, KeysShared<128>::kBytes, s, p);
         if (rc != OMNI_OK) return rc;
     }
     if (a->q_len > 0) {
         if ((rc = maps(kRows, kPiece)) != OMNI_OK) return rc;
-        const dim3 grid((a->q_len + kRows - 1) / kRows, a->heads, a->batch);
+        const dim3 grid(unsigned(p.q_tiles) * a->heads * a->batch);
         rc = a->dim <= 64 ? launch(ctx, attention_queries_kernel<64>, grid, kBackwardThreads, QueriesShared<64>::kBytes, s, p)
                           : launch(ctx, attention_queries_kernel<128>, grid, kBackwardThreads, QueriesShared<128>::kBytes, s, p);
     }

@@ -28,6 +28,15 @@ __device__ __forceinline__ Lengths lengths_of(const AttnShape &s, int b)
     return l;
 }
 
+// Which tile of rows of which head and sequence a CTA has.  Tiles are the slowest index, so that the
+// longest ones of a causal mask (tile 0 here) of all heads come first and the short ones fill the end.
+struct Place { int tile, head, batch; };
+__device__ __forceinline__ Place place_of(int heads, int batch)
+{
+    const int per = heads * batch, rest = int(blockIdx.x) % per;
+    return {int(blockIdx.x) / per, rest % heads, rest / heads};
+}
+
 struct OutView { __nv_bfloat16 *data; long long batch, row, head; };
 
 // Rows x DP tile as blocks of 64 columns, each ROWS x 128 bytes.
@@ -62,20 +71,15 @@ __device__ __forceinline__ void mma_along(unsigned d, unsigned a, unsigned b, bo
     }
 }
 // d[128 x DP] (+)= P B, P [128 x K] bfloat16 in tensor memory, B a tile of RB rows, of which K are contracted over.
-template <int DP, int RB, int K>
+// P stands in stretches of RUN values, each at the start of the RUN columns whose scores it came from.
+template <int DP, int RB, int K, int RUN>
 __device__ __forceinline__ void mma_tmem_across(unsigned d, unsigned p, unsigned b, bool add)
 {
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        mma_ts(d, p + k * 8, tile_desc(b + k * 2048, 1024, RB * 128), mma_kind(DP, false, true), add || k > 0);
+        mma_ts(d, p + k * 16 / RUN * RUN + k * 16 % RUN / 2, tile_desc(b + k * 2048, 1024, RB * 128), mma_kind(DP, false, true), add || k > 0);
 }
 
-__device__ __forceinline__ float attn_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // Two floats to bfloat16, the first in the low half, in one instruction.
 __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 {
@@ -88,13 +92,14 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi)
 template <int DP>
 __device__ __forceinline__ void store_row(unsigned tmem, float gain, __nv_bfloat16 *dst, int dim, bool write)
 {
+    constexpr int kAt = DP < 32 ? DP : 32;     // columns at a time
 #pragma unroll
-    for (int c = 0; c < DP / 32; ++c) {
-        uint32_t r[32];
-        tmem_load(r, tmem + c * 32);
+    for (int c = 0; c < DP / kAt; ++c) {
+        uint32_t r[kAt];
+        tmem_load(r, tmem + c * kAt);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int col = c * 32 + g * 8;
+        for (int g = 0; g < kAt / 8; ++g) {
+            const int col = c * kAt + g * 8;
             if (!write || col >= dim) continue;
             uint4 o;
             o.x = pack2(gain * __uint_as_float(r[g * 8 + 0]), gain * __uint_as_float(r[g * 8 + 1]));

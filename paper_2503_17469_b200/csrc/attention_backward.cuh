@@ -6,27 +6,31 @@
 // tile, which adds up dQ over the keys.  Seven products instead of five, but every sum has one owner and one order:
 // no float atomics, no zeroed and re-read dQ in float, the same bits from the same call.
 //
-// Both kernels work on 128 x 64 pieces.  Two warpgroups take the pieces in turn, a thread per row of 64 columns, while the
-// tensor core works on the pieces before and after.
+// Both kernels work on 128 x 64 pieces.  Two pairs of warpgroups take the pieces in turn, a thread per 32
+// columns of a row, while the tensor core works on the pieces before and after.
 //   dK, dV: S^T = K Q^T and dP^T = V dO^T (128 keys x 64 queries).  P^T goes back to tensor memory over
 //     S^T as the A operand of dV += P^T dO; dS^T goes to shared memory as that of dK += dS^T Q.
 //   dQ:     S = Q K^T and dP = dO V^T (128 queries x 64 keys); dS over S as the A operand of dQ += dS K.
 // P and dS are rounded to bfloat16 for the products; all sums are float.
 //
-// Warps 0-3 and 4-7: pieces in turn, 8: loads, 9: MMA.
+// Warps 0-7 and 8-15: pieces in turn (the first four of each the first 32 columns), 16: loads, 17: MMA.
 #pragma once
+#include <type_traits>
+
 #include "attention.cuh"
 
 namespace omni {
 
-constexpr int kBackwardThreads = 320;
+constexpr int kBackwardThreads = 576;
+constexpr int kLoadWarp = 16, kMmaWarp = 17;
+constexpr int kHalf = 32;           // columns of a thread
 constexpr int kPiece = 64;
 
 struct AttnBackwardParams {
     CUtensorMap q, k, v, dout;      // boxes of 128 rows for the operands a block keeps, of 64 for those it streams
     AttnShape s;
-    const float *row_lse, *row_delta;   // [batch * heads][q_pad]: L in powers of two (+inf: no row), D
-    int q_pad;
+    const float *row_lse, *row_delta;   // [batch * heads][q_pad]: -L in powers of two (-inf: no row), -D
+    int q_pad, q_tiles;
     OutView dq, dk, dv;
     unsigned *status;
 };
@@ -39,7 +43,7 @@ struct AttnRowsParams {
     int q_pad;
 };
 
-// D and the log-sum-exp in powers of two, for every query row and the padding up to whole tiles.
+// -D and minus the log-sum-exp in powers of two, for every query row and the padding up to whole tiles.
 // 16 lanes a row.  Reads O and dO once.
 __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnRowsParams p)
 {
@@ -61,8 +65,8 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnRowsParam
     const long long at = ((long long)b * p.s.heads + head) * p.q_pad + i;
     const float lse = i < q_length ? p.lse[((long long)b * p.s.heads + head) * p.s.q_len + i] : -INFINITY;
     const bool there = lse != -INFINITY;
-    p.row_lse[at] = there ? lse * kAttnLog2e : INFINITY;
-    p.row_delta[at] = there ? sum : 0.0f;
+    p.row_lse[at] = there ? -lse * kAttnLog2e : -INFINITY;
+    p.row_delta[at] = there ? -sum : 0.0f;
 }
 
 // ---- dK, dV -------------------------------------------------------------------------------------
@@ -93,8 +97,9 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     const float *stats = reinterpret_cast<const float *>(smem + L::kStats);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int kv_head = blockIdx.y, b = blockIdx.z, group = p.s.heads / p.s.kv_heads;
-    const int k0 = int(blockIdx.x) * kRows;
+    const Place at_tile = place_of(p.s.kv_heads, p.s.batch);
+    const int kv_head = at_tile.head, b = at_tile.batch, group = p.s.heads / p.s.kv_heads;
+    const int k0 = at_tile.tile * kRows;
     const Lengths len = lengths_of(p.s, b);
 
     // query pieces that see some key of this tile: from the one with the first row i >= k0 - shift
@@ -106,19 +111,19 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     if (threadIdx.x == 0) {
         mbar_init(kv_full, 1);
         for (int i = 0; i < ST; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(ds_ready + t, kRows); }
+        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(ds_ready + t, 2 * kRows); }
         mbar_init(done, 1);
         *give_up = 0;
         fence_barrier_init();
     }
-    if (warp == 9) tmem_alloc(tmem_cell, 512);
+    if (warp == kMmaWarp) tmem_alloc(tmem_cell, 512);
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
     const unsigned tmem = *tmem_cell;
     const unsigned dv_at = tmem, dk_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + 2 * kPiece;
 
-    if (warp == 8) {
+    if (warp == kLoadWarp) {
         if (lane == 0 && n > 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
             mbar_expect_tx(kv_full, 2 * L::kTile);
@@ -142,7 +147,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
             for (int h = max(0, armed - ST); h < armed; ++h) mbar_wait(full + h % ST, (h / ST) & 1);
         }
         __syncwarp();
-    } else if (warp == 9) {
+    } else if (warp == kMmaWarp) {
         const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV), ds = smem_addr(smem + L::kS);
         bool ok = n == 0 || warp_wait(kv_full, 0, give_up, p.status);
         // scores of piece h into its half of tensor memory
@@ -172,7 +177,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
             fence_after_sync();
             if (lane == 0) {
                 const unsigned q = smem_addr(smem + L::kQ + st * L::kPieceTile), d = smem_addr(smem + L::kDo + st * L::kPieceTile);
-                mma_tmem_across<DP, kPiece, kPiece>(dv_at, s_at + t * kPiece, d, h > 0);
+                mma_tmem_across<DP, kPiece, kPiece, kHalf>(dv_at, s_at + t * kPiece, d, h > 0);
 #pragma unroll
                 for (int s = 0; s < kPiece / 16; ++s)
                     mma_ss(dk_at, tile_desc(ds + t * L::kDs + s * 32, 1024, 16), tile_desc(q + s * 2048, 1024, kPiece * 128),
@@ -188,69 +193,72 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
         }
         __syncwarp();
     } else {
-        const int t = warp / 4, row = threadIdx.x % kRows, j = k0 + row;
+        const int t = warp / 8, half = warp / 4 % 2, row = threadIdx.x % kRows, j = k0 + row;
         const unsigned lanes = unsigned(warp % 4) * 32u << 16;
-        const unsigned s_row = s_at + t * kPiece + lanes, dp_row = dp_at + t * kPiece + lanes;
-        const float unit = p.s.scale * kAttnLog2e;
+        const unsigned s_row = s_at + t * kPiece + half * kHalf + lanes, dp_row = dp_at + t * kPiece + half * kHalf + lanes;
+        const float2 unit = {p.s.scale * kAttnLog2e, p.s.scale * kAttnLog2e};
         // queries that see this key: i >= from
         const int from = j >= len.kv ? INT_MAX : p.s.causal ? j - len.shift : 0;
         unsigned char *ds_row = smem + L::kS + t * L::kDs + row * 128;
         bool ok = true;
         for (int h = t; h < n; h += 2) {
-            const int st = h % ST, i0 = (piece0 + h % pieces) * kPiece;
+            const int st = h % ST, i0 = (piece0 + h % pieces) * kPiece + half * kHalf;
             ok = warp_wait(s_full + t, (h / 2) & 1, give_up, p.status);
             if (!ok) break;
             fence_after_sync();
-            const float *lse = stats + st * 2 * kPiece, *delta = lse + kPiece;
-            const bool edge = __any_sync(~0u, from > i0);
+            const float4 *lse = reinterpret_cast<const float4 *>(stats + st * 2 * kPiece + half * kHalf);
+            const float4 *delta = lse + kPiece / 4;
+            uint32_t s[kHalf], dp[kHalf], pk[kHalf / 2], dk[kHalf / 2];
+            tmem_load2(s, s_row, dp, dp_row);
+            auto piece = [&](auto edge) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t s[32], dp[32];
-                tmem_load(s, s_row + half * 32);
-                tmem_load(dp, dp_row + half * 32);
-                uint32_t pk[16], dk[16];
-#pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const float4 ls = *reinterpret_cast<const float4 *>(lse + half * 32 + c);
-                    const float4 dl = *reinterpret_cast<const float4 *>(delta + half * 32 + c);
-                    const float lv[4] = {ls.x, ls.y, ls.z, ls.w}, dv[4] = {dl.x, dl.y, dl.z, dl.w};
-                    float pr[4], dr[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        pr[e] = attn_exp2(fmaf(__uint_as_float(s[c + e]), unit, -lv[e]));
-                        dr[e] = pr[e] * (__uint_as_float(dp[c + e]) - dv[e]);
-                        if (edge && i0 + half * 32 + c + e < from) pr[e] = dr[e] = 0.0f;
+                for (int c = 0; c < kHalf; c += 4) {
+                    const float4 l = lse[c / 4], d = delta[c / 4];
+                    const float2 x0 = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, unit, {l.x, l.y});
+                    const float2 x1 = fma2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])}, unit, {l.z, l.w});
+                    float2 p0 = {exp2_fast(x0.x), exp2_fast(x0.y)}, p1 = {exp2_fast(x1.x), exp2_fast(x1.y)};
+                    float2 d0 = mul2(p0, add2({__uint_as_float(dp[c]), __uint_as_float(dp[c + 1])}, {d.x, d.y}));
+                    float2 d1 = mul2(p1, add2({__uint_as_float(dp[c + 2]), __uint_as_float(dp[c + 3])}, {d.z, d.w}));
+                    if constexpr (decltype(edge)::value) {
+                        if (i0 + c < from) p0.x = d0.x = 0.0f;
+                        if (i0 + c + 1 < from) p0.y = d0.y = 0.0f;
+                        if (i0 + c + 2 < from) p1.x = d1.x = 0.0f;
+                        if (i0 + c + 3 < from) p1.y = d1.y = 0.0f;
                     }
-                    pk[c / 2] = pack2(pr[0], pr[1]);
-                    pk[c / 2 + 1] = pack2(pr[2], pr[3]);
-                    dk[c / 2] = pack2(dr[0], dr[1]);
-                    dk[c / 2 + 1] = pack2(dr[2], dr[3]);
+                    pk[c / 2] = pack2(p0.x, p0.y);
+                    pk[c / 2 + 1] = pack2(p1.x, p1.y);
+                    dk[c / 2] = pack2(d0.x, d0.y);
+                    dk[c / 2 + 1] = pack2(d1.x, d1.y);
                 }
-                tmem_store(s_row + half * 16, pk);
+            };
+            if (__any_sync(~0u, from > i0)) piece(std::true_type{});
+            else piece(std::false_type{});
+            tmem_store(s_row, pk);
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<uint4 *>(ds_row + (((half * 4 + g) ^ (row & 7)) * 16)) =
-                        make_uint4(dk[g * 4], dk[g * 4 + 1], dk[g * 4 + 2], dk[g * 4 + 3]);
-            }
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<uint4 *>(ds_row + (((half * 4 + g) ^ (row & 7)) * 16)) =
+                    make_uint4(dk[g * 4], dk[g * 4 + 1], dk[g * 4 + 2], dk[g * 4 + 3]);
             tmem_wait_store();
             fence_async_proxy();
             fence_before_sync();
             mbar_arrive(ds_ready + t);
         }
-        // warps 0-3 write dV, warps 4-7 dK
+        // warps 0-7 write dV, warps 8-15 dK, half of the columns each four
         if (n > 0 && ok) ok = warp_wait(done, 0, give_up, p.status);
-        ok = ok && *give_up == 0;
-        ok = __all_sync(~0u, ok);
+        ok = __all_sync(~0u, ok && *give_up == 0);
         fence_after_sync();
         const OutView &o = t == 0 ? p.dv : p.dk;
+        const int c0 = half * (DP / 2);
         __nv_bfloat16 *dst = o.data + b * o.batch + (long long)j * o.row + kv_head * o.head;
         const bool mine = ok && j < p.s.kv_len;
-        if (n > 0 && ok) store_row<DP>((t == 0 ? dv_at : dk_at) + lanes, t == 0 ? 1.0f : p.s.scale, dst, p.s.dim, mine);
-        else if (mine) store_zeros(dst, p.s.dim);
+        if (n > 0 && ok)
+            store_row<DP / 2>((t == 0 ? dv_at : dk_at) + lanes + c0, t == 0 ? 1.0f : p.s.scale, dst + c0, p.s.dim - c0, mine);
+        else if (mine && half == 0)
+            store_zeros(dst, p.s.dim);
     }
     fence_before_sync();
     __syncthreads();
-    if (warp == 9) tmem_free(tmem, 512);
+    if (warp == kMmaWarp) tmem_free(tmem, 512);
 }
 
 // ---- dQ -----------------------------------------------------------------------------------------
@@ -277,8 +285,9 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(done + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int head = blockIdx.y, b = blockIdx.z, kv_head = head / (p.s.heads / p.s.kv_heads);
-    const int q0 = int(gridDim.x - 1 - blockIdx.x) * kRows;
+    const Place at_tile = place_of(p.s.heads, p.s.batch);
+    const int head = at_tile.head, b = at_tile.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const int q0 = (p.q_tiles - 1 - at_tile.tile) * kRows;
     const Lengths len = lengths_of(p.s, b);
     const int last = min(q0 + kRows, len.q) - 1;
     const int seen = last < q0 ? 0 : p.s.causal ? min(len.kv, last + len.shift + 1) : len.kv;
@@ -287,19 +296,19 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
         for (int i = 0; i < ST; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(ds_ready + t, kRows); }
+        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(ds_ready + t, 2 * kRows); }
         mbar_init(done, 1);
         *give_up = 0;
         fence_barrier_init();
     }
-    if (warp == 9) tmem_alloc(tmem_cell, 512);
+    if (warp == kMmaWarp) tmem_alloc(tmem_cell, 512);
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
     const unsigned tmem = *tmem_cell;
     const unsigned dq_at = tmem, s_at = tmem + DP, dp_at = s_at + 2 * kPiece;
 
-    if (warp == 8) {
+    if (warp == kLoadWarp) {
         if (lane == 0 && n > 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
             mbar_expect_tx(q_full, 2 * L::kTile);
@@ -318,7 +327,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
             for (int h = max(0, armed - ST); h < armed; ++h) mbar_wait(full + h % ST, (h / ST) & 1);
         }
         __syncwarp();
-    } else if (warp == 9) {
+    } else if (warp == kMmaWarp) {
         const unsigned q = smem_addr(smem + L::kQ), d = smem_addr(smem + L::kDo);
         bool ok = n == 0 || warp_wait(q_full, 0, give_up, p.status);
         auto scores = [&](int h) {
@@ -344,7 +353,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
             if (!ok) break;
             fence_after_sync();
             if (lane == 0) {
-                mma_tmem_across<DP, kPiece, kPiece>(dq_at, s_at + t * kPiece, smem_addr(smem + L::kK + st * L::kPieceTile), h > 0);
+                mma_tmem_across<DP, kPiece, kPiece, kHalf>(dq_at, s_at + t * kPiece, smem_addr(smem + L::kK + st * L::kPieceTile), h > 0);
                 mma_commit(empty + st);
             }
             __syncwarp();
@@ -356,10 +365,10 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
         }
         __syncwarp();
     } else {
-        const int t = warp / 4, row = threadIdx.x % kRows, i = q0 + row;
+        const int t = warp / 8, half = warp / 4 % 2, row = threadIdx.x % kRows, i = q0 + row;
         const unsigned lanes = unsigned(warp % 4) * 32u << 16;
-        const unsigned s_row = s_at + t * kPiece + lanes, dp_row = dp_at + t * kPiece + lanes;
-        const float unit = p.s.scale * kAttnLog2e;
+        const unsigned s_row = s_at + t * kPiece + half * kHalf + lanes, dp_row = dp_at + t * kPiece + half * kHalf + lanes;
+        const float2 unit = {p.s.scale * kAttnLog2e, p.s.scale * kAttnLog2e};
         const int limit = i >= len.q ? 0 : p.s.causal ? min(len.kv, i + len.shift + 1) : len.kv;
         const long long at = ((long long)b * p.s.heads + head) * p.q_pad + i;
         const float lse = p.row_lse[at], delta = p.row_delta[at];
@@ -368,22 +377,24 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
             ok = warp_wait(s_full + t, (h / 2) & 1, give_up, p.status);
             if (!ok) break;
             fence_after_sync();
-            const int open = limit - h * kPiece;
-            const bool edge = __any_sync(~0u, open < kPiece);
-            uint32_t s[64], dp[64], pk[32];
-            tmem_load(s, s_row);
-            tmem_load(dp, dp_row);
+            const int open = limit - h * kPiece - half * kHalf;
+            uint32_t s[kHalf], dp[kHalf], pk[kHalf / 2];
+            tmem_load2(s, s_row, dp, dp_row);
+            auto piece = [&](auto edge) {
 #pragma unroll
-            for (int c = 0; c < kPiece; c += 2) {
-                float dr[2];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float pr = attn_exp2(fmaf(__uint_as_float(s[c + e]), unit, -lse));
-                    dr[e] = pr * (__uint_as_float(dp[c + e]) - delta);
-                    if (edge && c + e >= open) dr[e] = 0.0f;
+                for (int c = 0; c < kHalf; c += 2) {
+                    const float2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, unit, {lse, lse});
+                    const float2 pr = {exp2_fast(x.x), exp2_fast(x.y)};
+                    float2 dr = mul2(pr, add2({__uint_as_float(dp[c]), __uint_as_float(dp[c + 1])}, {delta, delta}));
+                    if constexpr (decltype(edge)::value) {
+                        if (c >= open) dr.x = 0.0f;
+                        if (c + 1 >= open) dr.y = 0.0f;
+                    }
+                    pk[c / 2] = pack2(dr.x, dr.y);
                 }
-                pk[c / 2] = pack2(dr[0], dr[1]);
-            }
+            };
+            if (__any_sync(~0u, open < kHalf)) piece(std::true_type{});
+            else piece(std::false_type{});
             tmem_store(s_row, pk);
             tmem_wait_store();
             fence_before_sync();
@@ -392,16 +403,16 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
         if (n > 0 && ok) ok = warp_wait(done, 0, give_up, p.status);
         ok = __all_sync(~0u, ok && *give_up == 0);
         fence_after_sync();
-        // the two warpgroups share the columns
+        // every warpgroup a quarter of the columns
+        const int c0 = (2 * t + half) * (DP / 4);
         __nv_bfloat16 *dst = p.dq.data + b * p.dq.batch + (long long)i * p.dq.row + head * p.dq.head;
-        const bool mine = ok && i < p.s.q_len;
-        const bool empty = limit <= 0;
-        if (n > 0 && ok) store_row<DP / 2>(dq_at + lanes + t * (DP / 2), p.s.scale, dst + t * (DP / 2), p.s.dim - t * (DP / 2), mine && !empty);
-        if (t == 0 && mine && empty) store_zeros(dst, p.s.dim);
+        const bool mine = ok && i < p.s.q_len, empty = limit <= 0;
+        if (n > 0 && ok) store_row<DP / 4>(dq_at + lanes + c0, p.s.scale, dst + c0, p.s.dim - c0, mine && !empty);
+        if (c0 == 0 && mine && empty) store_zeros(dst, p.s.dim);
     }
     fence_before_sync();
     __syncthreads();
-    if (warp == 9) tmem_free(tmem, 512);
+    if (warp == kMmaWarp) tmem_free(tmem, 512);
 }
 
 }  // namespace omni

@@ -18,6 +18,7 @@ namespace omni {
 struct AttnForwardParams {
     CUtensorMap q, k, v;
     AttnShape s;
+    int q_tiles;                    // pairs of tiles
     OutView out;
     float *lse;
     unsigned *status;
@@ -47,8 +48,9 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(drained + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int head = blockIdx.y, b = blockIdx.z, kv_head = head / (p.s.heads / p.s.kv_heads);
-    const int q0 = int(gridDim.x - 1 - blockIdx.x) * 2 * kRows;     // the longest rows of a causal mask first
+    const Place at = place_of(p.s.heads, p.s.batch);
+    const int head = at.head, b = at.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const int q0 = (p.q_tiles - 1 - at.tile) * 2 * kRows;
     const Lengths len = lengths_of(p.s, b);
 
     // key tiles that some row of each query tile sees
@@ -129,7 +131,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 ok = warp_wait(p_ready + t, j & 1, give_up, p.status);
                 fence_after_sync();
                 if (ok && lane == 0) {
-                    mma_tmem_across<DP, kRows, kRows>(o_at + t * DP, s_at + t * kRows, v + st * L::kTile, j > 0);
+                    mma_tmem_across<DP, kRows, kRows, kRows>(o_at + t * DP, s_at + t * kRows, v + st * L::kTile, j > 0);
                     // the next scores go over P: the tensor core takes MMAs in order
                     if (j + 1 < tiles[t]) {
                         mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
@@ -165,8 +167,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
             if (!ok) break;
             fence_after_sync();
             uint32_t x[2][64];
-            tmem_load(x[0], s_row);
-            tmem_load(x[1], s_row + 64);
+            tmem_load2(x[0], s_row, x[1], s_row + 64);
             const int open = limit - j * kRows;                       // columns of this tile that the row sees
             if (__any_sync(~0u, open < kRows)) {
 #pragma unroll
@@ -177,11 +178,15 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
 #pragma unroll
             for (int c = 0; c < 4; ++c) top[c] = __uint_as_float(x[0][c]);
 #pragma unroll
-            for (int c = 4; c < kRows; ++c) top[c % 4] = fmaxf(top[c % 4], __uint_as_float(x[c / 64][c % 64]));
+            for (int c = 4; c < kRows; c += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    top[e] = c + 4 + e < kRows ? max3(top[e], __uint_as_float(x[c / 64][c % 64 + e]), __uint_as_float(x[(c + 4) / 64][(c + 4) % 64 + e]))
+                                               : fmaxf(top[e], __uint_as_float(x[c / 64][c % 64 + e]));
             const float tile_max = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * unit;
             const bool grow = tile_max > m + kRescaleAbove;           // also the first finite one
             if (__any_sync(~0u, grow)) {
-                const float factor = grow ? attn_exp2(m - tile_max) : 1.0f;
+                const float factor = grow ? exp2_fast(m - tile_max) : 1.0f;
                 if (grow) { m = tile_max; l *= factor; }
                 if (j > 0) {
 #pragma unroll
@@ -195,21 +200,21 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 }
             }
             const float ref = m == -INFINITY ? 0.0f : m;
-            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const float2 unit2 = {unit, unit}, ref2 = {-ref, -ref};
+            float2 sum[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t packed[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) {
-                    const float a = attn_exp2(fmaf(__uint_as_float(x[h][c]), unit, -ref));
-                    const float d = attn_exp2(fmaf(__uint_as_float(x[h][c + 1]), unit, -ref));
-                    sum[c % 4] += a;
-                    sum[c % 4 + 1] += d;
-                    packed[c / 2] = pack2(a, d);
+                    const float2 y = fma2({__uint_as_float(x[h][c]), __uint_as_float(x[h][c + 1])}, unit2, ref2);
+                    const float2 e = {exp2_fast(y.x), exp2_fast(y.y)};
+                    sum[c / 2 % 2] = add2(sum[c / 2 % 2], e);
+                    packed[c / 2] = pack2(e.x, e.y);
                 }
                 tmem_store(s_row + h * 32, packed);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             tmem_wait_store();
             fence_before_sync();
             mbar_arrive(p_ready + t);
