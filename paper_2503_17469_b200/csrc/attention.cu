@@ -33,14 +33,14 @@ int encoder(omni_ctx *ctx, EncodeTiled *out)
     return OMNI_OK;
 }
 
-// View as (column, head, row, batch) with boxes of 64 columns x `rows` rows of one head.
+// View as (column, head, row, batch) with boxes of 64 columns x 128 rows of one head.
 int make_map(omni_ctx *ctx, EncodeTiled encode, CUtensorMap *map, const omni_attn_view &v, int dim, int heads, int len,
-             int batch, int rows)
+             int batch)
 {
     const cuuint64_t extent[4] = {cuuint64_t(dim), cuuint64_t(heads), cuuint64_t(len), cuuint64_t(batch)};
     // the stride of an extent of one is never used, but has to be a legal one
     const cuuint64_t strides[3] = {heads > 1 ? v.head * 2 : 16, len > 1 ? v.row * 2 : 16, batch > 1 ? v.batch * 2 : 16};
-    const cuuint32_t box[4] = {64, 1, cuuint32_t(rows), 1}, step[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, 1, kRows, 1}, step[4] = {1, 1, 1, 1};
     const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, v.data, extent, strides, box, step,
                               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
@@ -126,10 +126,10 @@ int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q
     if ((rc = encoder(ctx, &encode)) != OMNI_OK) return rc;
     AttnForwardParams p;
     std::memset(&p, 0, sizeof p);
-    if ((rc = make_map(ctx, encode, &p.q, *q, a->dim, a->heads, a->q_len, a->batch, kRows)) != OMNI_OK) return rc;
+    if ((rc = make_map(ctx, encode, &p.q, *q, a->dim, a->heads, a->q_len, a->batch)) != OMNI_OK) return rc;
     if (a->kv_len > 0) {      // without keys no kernel touches their maps
-        if ((rc = make_map(ctx, encode, &p.k, *k, a->dim, a->kv_heads, a->kv_len, a->batch, kRows)) != OMNI_OK) return rc;
-        if ((rc = make_map(ctx, encode, &p.v, *v, a->dim, a->kv_heads, a->kv_len, a->batch, kRows)) != OMNI_OK) return rc;
+        if ((rc = make_map(ctx, encode, &p.k, *k, a->dim, a->kv_heads, a->kv_len, a->batch)) != OMNI_OK) return rc;
+        if ((rc = make_map(ctx, encode, &p.v, *v, a->dim, a->kv_heads, a->kv_len, a->batch)) != OMNI_OK) return rc;
     }
     p.s = shape_of(a);
     p.out = out_of(out);
@@ -195,23 +195,20 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
     }
     EncodeTiled encode;
     if ((rc = encoder(ctx, &encode)) != OMNI_OK) return rc;
-    auto maps = [&](int q_rows, int kv_rows) {
-        int e = OMNI_OK;
-        if (a->q_len == 0 || a->kv_len == 0) return e;       // no pair of a query and a key: the maps are not touched
-        if ((e = make_map(ctx, encode, &p.q, *q, a->dim, a->heads, a->q_len, a->batch, q_rows)) != OMNI_OK) return e;
-        if ((e = make_map(ctx, encode, &p.dout, *dout, a->dim, a->heads, a->q_len, a->batch, q_rows)) != OMNI_OK) return e;
-        if ((e = make_map(ctx, encode, &p.k, *k, a->dim, a->kv_heads, a->kv_len, a->batch, kv_rows)) != OMNI_OK) return e;
-        return make_map(ctx, encode, &p.v, *v, a->dim, a->kv_heads, a->kv_len, a->batch, kv_rows);
-    };
+    if (a->q_len > 0 && a->kv_len > 0) {         // without a pair of a query and a key no kernel touches the maps
+        const struct { CUtensorMap *map; const omni_attn_view *view; int heads, len; } maps[4] = {
+            {&p.q, q, a->heads, a->q_len}, {&p.dout, dout, a->heads, a->q_len},
+            {&p.k, k, a->kv_heads, a->kv_len}, {&p.v, v, a->kv_heads, a->kv_len}};
+        for (const auto &m : maps)
+            if ((rc = make_map(ctx, encode, m.map, *m.view, a->dim, m.heads, m.len, a->batch)) != OMNI_OK) return rc;
+    }
     if (a->kv_len > 0) {
-        if ((rc = maps(kPiece, kRows)) != OMNI_OK) return rc;
         const dim3 grid(unsigned((a->kv_len + kRows - 1) / kRows) * a->kv_heads * a->batch);
         rc = a->dim <= 64 ? launch(ctx, attention_keys_kernel<64>, grid, kBackwardThreads, KeysShared<64>::kBytes, s, p)
                           : launch(ctx, attention_keys_kernel<128>, grid, kBackwardThreads, KeysShared<128>::kBytes, s, p);
         if (rc != OMNI_OK) return rc;
     }
     if (a->q_len > 0) {
-        if ((rc = maps(kRows, kPiece)) != OMNI_OK) return rc;
         const dim3 grid(unsigned(p.q_tiles) * a->heads * a->batch);
         rc = a->dim <= 64 ? launch(ctx, attention_queries_kernel<64>, grid, kBackwardThreads, QueriesShared<64>::kBytes, s, p)
                           : launch(ctx, attention_queries_kernel<128>, grid, kBackwardThreads, QueriesShared<128>::kBytes, s, p);

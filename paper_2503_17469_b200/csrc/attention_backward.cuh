@@ -6,28 +6,31 @@
 // tile, which adds up dQ over the keys.  Seven products instead of five, but every sum has one owner and one order:
 // no float atomics, no zeroed and re-read dQ in float, the same bits from the same call.
 //
-// Both kernels work on 128 x 64 pieces.  Two pairs of warpgroups take the pieces in turn, a thread per 32
-// columns of a row, while the tensor core works on the pieces before and after.
-//   dK, dV: S^T = K Q^T and dP^T = V dO^T (128 keys x 64 queries).  P^T goes back to tensor memory over
-//     S^T as the A operand of dV += P^T dO; dS^T goes to shared memory as that of dK += dS^T Q.
-//   dQ:     S = Q K^T and dP = dO V^T (128 queries x 64 keys); dS over S as the A operand of dQ += dS K.
+// Both kernels walk 128 x 128 tiles of S and dP in tensor memory.  (64 columns a tile would leave room for two of each,
+// but an MMA of M = 128 with both operands in shared memory takes about 75 cycles, N = 64 or 128.)  The
+// elementwise work comes in two phases, P from S and dS from P and dP, sixteen warps at 32 columns of a row per thread,
+// and each phase runs beside products of the same or the next tile:
+//   dK, dV: S^T = K Q^T and dP^T = V dO^T (128 keys x 128 queries).  P^T goes back to tensor memory over S^T as the A
+//     operand of dV += P^T dO; dS^T goes to shared memory as that of dK += dS^T Q.
+//     Order of the products: S0 dP0 | dV0 S1 dK0 dP1 | dV1 S2 dK1 dP2 | ...
+//   dQ:     S = Q K^T and dP = dO V^T (128 queries x 128 keys), two tiles of S; dS over S as the A operand of dQ += dS K.
+//     Order: S0 dP0 S1 | dQ0 dP1 S2 | dQ1 dP2 S3 | ...
+// An operand in tensor memory is overwritten by a product that is issued after the one that reads it; one thread
+// issues all of a block's, and the tensor core takes them in that order.
 // P and dS are rounded to bfloat16 for the products; all sums are float.
 //
-// Warps 0-7 and 8-15: pieces in turn (the first four of each the first 32 columns), 16: loads, 17: MMA.
+// Warps 0-15: elementwise (four warps cover the 128 rows, each four another 32 columns), 16: loads, 17: MMA.
 #pragma once
-#include <type_traits>
-
 #include "attention.cuh"
 
 namespace omni {
 
-constexpr int kBackwardThreads = 576;
-constexpr int kLoadWarp = 16, kMmaWarp = 17;
-constexpr int kHalf = 32;           // columns of a thread
-constexpr int kPiece = 64;
+constexpr int kLoadWarp = 16, kMmaWarp = 17, kBackwardThreads = 18 * 32;
+constexpr int kElementWarps = 16;
+constexpr int kCols = 32;           // columns of a thread
 
 struct AttnBackwardParams {
-    CUtensorMap q, k, v, dout;      // boxes of 128 rows for the operands a block keeps, of 64 for those it streams
+    CUtensorMap q, k, v, dout;
     AttnShape s;
     const float *row_lse, *row_delta;   // [batch * heads][q_pad]: -L in powers of two (-inf: no row), -D
     int q_pad, q_tiles;
@@ -72,11 +75,11 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnRowsParam
 // ---- dK, dV -------------------------------------------------------------------------------------
 
 template <int DP> struct KeysShared {
-    static constexpr int kStages = 4;
-    static constexpr int kTile = kRows * DP * 2, kPieceTile = kPiece * DP * 2, kDs = kRows * kPiece * 2;
-    static constexpr int kK = 0, kV = kTile, kQ = 2 * kTile, kDo = kQ + kStages * kPieceTile, kS = kDo + kStages * kPieceTile;
-    static constexpr int kStats = kS + 2 * kDs;                    // [stages][2][64] float
-    static constexpr int kBars = kStats + kStages * 2 * kPiece * 4;
+    static constexpr int kStages = DP == 128 ? 2 : 3;
+    static constexpr int kTile = kRows * DP * 2;
+    static constexpr int kK = 0, kV = kTile, kQ = 2 * kTile, kDo = kQ + kStages * kTile, kDs = kDo + kStages * kTile;
+    static constexpr int kStats = kDs + kRows * kRows * 2;         // [stages][2][128] float
+    static constexpr int kBars = kStats + kStages * 2 * kRows * 4;
     // barriers, and what is left of the block's 227 KB for rounding the base up to 1024
     static constexpr int kBytes = kBars + 256 + (DP == 128 ? 768 : 1024);
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
@@ -90,8 +93,8 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     extern __shared__ unsigned char raw[];
     unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
-    unsigned long long *kv_full = bars, *full = bars + 1, *empty = full + ST, *s_full = empty + ST, *ds_ready = s_full + 2;
-    unsigned long long *done = ds_ready + 2;
+    unsigned long long *kv_full = bars, *q_full = bars + 1, *q_empty = q_full + ST, *do_full = q_empty + ST, *do_empty = do_full + ST;
+    unsigned long long *s_full = do_empty + ST, *p_ready = s_full + 1, *dp_full = p_ready + 1, *ds_ready = dp_full + 1, *done = ds_ready + 1;
     volatile int *give_up = reinterpret_cast<int *>(done + 1);
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(done + 2);
     const float *stats = reinterpret_cast<const float *>(smem + L::kStats);
@@ -102,16 +105,20 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     const int k0 = at_tile.tile * kRows;
     const Lengths len = lengths_of(p.s, b);
 
-    // query pieces that see some key of this tile: from the one with the first row i >= k0 - shift
+    // query tiles that see some key of this tile: from the one with the first row i >= k0 - shift
     const int first_row = p.s.causal ? max(0, k0 - len.shift) : 0;
-    const int piece0 = first_row / kPiece;
-    const int pieces = k0 < len.kv && first_row < len.q ? (len.q + kPiece - 1) / kPiece - piece0 : 0;
-    const int n = pieces * group;
+    const int tile0 = first_row / kRows;
+    const int tiles = k0 < len.kv && first_row < len.q ? (len.q + kRows - 1) / kRows - tile0 : 0;
+    const int n = tiles * group;                                    // (query head, tile) one after the other
 
     if (threadIdx.x == 0) {
         mbar_init(kv_full, 1);
-        for (int i = 0; i < ST; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(ds_ready + t, 2 * kRows); }
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(q_full + i, 1); mbar_init(q_empty + i, 1);
+            mbar_init(do_full + i, 1); mbar_init(do_empty + i, 1);
+        }
+        mbar_init(s_full, 1); mbar_init(p_ready, kElementWarps);
+        mbar_init(dp_full, 1); mbar_init(ds_ready, kElementWarps);
         mbar_init(done, 1);
         *give_up = 0;
         fence_barrier_init();
@@ -121,138 +128,182 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     __syncthreads();
     fence_after_sync();
     const unsigned tmem = *tmem_cell;
-    const unsigned dv_at = tmem, dk_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + 2 * kPiece;
+    const unsigned dv_at = tmem, dk_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kRows;
 
     if (warp == kLoadWarp) {
         if (lane == 0 && n > 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
             mbar_expect_tx(kv_full, 2 * L::kTile);
             load_tile<DP, kRows>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
-            load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
-            int armed = 0;
+            int q_armed = 0, do_armed = 0;
             const unsigned long long policy = policy_evict_last();
             for (int h = 0; h < n; ++h) {
-                const int st = h % ST, head = kv_head * group + h / pieces, row = (piece0 + h % pieces) * kPiece;
-                if (!bounded_wait(empty + st, ((h / ST) & 1) ^ 1, give_up, p.status)) break;
-                mbar_expect_tx(full + st, 2 * L::kPieceTile + 2 * kPiece * 4);
-                load_tile<DP, kPiece>(smem + L::kQ + st * L::kPieceTile, &p.q, head, row, b, full + st);
-                load_tile<DP, kPiece>(smem + L::kDo + st * L::kPieceTile, &p.dout, head, row, b, full + st);
+                const int st = h % ST, head = kv_head * group + h / tiles, row = (tile0 + h % tiles) * kRows;
+                const unsigned free_parity = ((h / ST) & 1) ^ 1;
+                if (!bounded_wait(q_empty + st, free_parity, give_up, p.status)) break;
+                mbar_expect_tx(q_full + st, L::kTile + 2 * kRows * 4);
+                load_tile<DP, kRows>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st);
                 const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
-                float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kPiece;
-                bulk_load(to, p.row_lse + at, kPiece * 4, full + st, policy);
-                bulk_load(to + kPiece, p.row_delta + at, kPiece * 4, full + st, policy);
-                ++armed;
+                float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kRows;
+                bulk_load(to, p.row_lse + at, kRows * 4, q_full + st, policy);
+                bulk_load(to + kRows, p.row_delta + at, kRows * 4, q_full + st, policy);
+                ++q_armed;
+                if (h == 0) load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
+                if (!bounded_wait(do_empty + st, free_parity, give_up, p.status)) break;
+                mbar_expect_tx(do_full + st, L::kTile);
+                load_tile<DP, kRows>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st);
+                ++do_armed;
             }
+            // the block may not end with a copy in flight, not even when it gave up
             mbar_wait(kv_full, 0);
-            for (int h = max(0, armed - ST); h < armed; ++h) mbar_wait(full + h % ST, (h / ST) & 1);
+            for (int h = max(0, q_armed - ST); h < q_armed; ++h) mbar_wait(q_full + h % ST, (h / ST) & 1);
+            for (int h = max(0, do_armed - ST); h < do_armed; ++h) mbar_wait(do_full + h % ST, (h / ST) & 1);
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV), ds = smem_addr(smem + L::kS);
+        const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV), ds = smem_addr(smem + L::kDs);
+        const unsigned q0 = smem_addr(smem + L::kQ), do0 = smem_addr(smem + L::kDo);
         bool ok = n == 0 || warp_wait(kv_full, 0, give_up, p.status);
-        // scores of piece h into its half of tensor memory
+        // rows of tile h that are queries of this sequence; those behind it may hold anything
+        auto rows_of = [&](int h) { return p.s.q_lengths ? len.q - (tile0 + h % tiles) * kRows : kRows; };
         auto scores = [&](int h) {
-            const int st = h % ST, row = (piece0 + h % pieces) * kPiece;
-            const bool w = warp_wait(full + st, (h / ST) & 1, give_up, p.status);
-            if (!w) return false;
-            if (p.s.q_lengths && len.q - row < kPiece) {
-                zero_rows<DP, kPiece>(smem + L::kQ + st * L::kPieceTile, len.q - row);
-                zero_rows<DP, kPiece>(smem + L::kDo + st * L::kPieceTile, len.q - row);
-            }
+            const int st = h % ST;
+            if (!warp_wait(q_full + st, (h / ST) & 1, give_up, p.status)) return false;
+            if (rows_of(h) < kRows) zero_rows<DP, kRows>(smem + L::kQ + st * L::kTile, rows_of(h));
             fence_after_sync();
-            if (lane == 0) {
-                const unsigned q = smem_addr(smem + L::kQ + st * L::kPieceTile), d = smem_addr(smem + L::kDo + st * L::kPieceTile);
-                mma_along<DP, kRows, kPiece, kPiece>(s_at + (h & 1) * kPiece, k, q, false);
-                mma_along<DP, kRows, kPiece, kPiece>(dp_at + (h & 1) * kPiece, v, d, false);
-                mma_commit(s_full + (h & 1));
+            if (elect_one()) {
+                mma_along<DP, kRows, kRows, kRows>(s_at, k, q0 + st * L::kTile, false);
+                mma_commit(s_full);
             }
             __syncwarp();
             return true;
         };
-        for (int h = 0; h < 2 && h < n && ok; ++h) ok = scores(h);
-        for (int h = 0; h < n && ok; ++h) {
-            const int st = h % ST, t = h & 1;
-            ok = warp_wait(ds_ready + t, (h / 2) & 1, give_up, p.status);
-            if (!ok) break;
+        auto slopes = [&](int h) {
+            const int st = h % ST;
+            if (!warp_wait(do_full + st, (h / ST) & 1, give_up, p.status)) return false;
+            if (rows_of(h) < kRows) zero_rows<DP, kRows>(smem + L::kDo + st * L::kTile, rows_of(h));
             fence_after_sync();
-            if (lane == 0) {
-                const unsigned q = smem_addr(smem + L::kQ + st * L::kPieceTile), d = smem_addr(smem + L::kDo + st * L::kPieceTile);
-                mma_tmem_across<DP, kPiece, kPiece, kHalf>(dv_at, s_at + t * kPiece, d, h > 0);
-#pragma unroll
-                for (int s = 0; s < kPiece / 16; ++s)
-                    mma_ss(dk_at, tile_desc(ds + t * L::kDs + s * 32, 1024, 16), tile_desc(q + s * 2048, 1024, kPiece * 128),
-                           mma_kind(DP, false, true), h > 0 || s > 0);
-                mma_commit(empty + st);
+            if (elect_one()) {
+                mma_along<DP, kRows, kRows, kRows>(dp_at, v, do0 + st * L::kTile, false);
+                mma_commit(dp_full);
             }
             __syncwarp();
-            if (h + 2 < n) ok = scores(h + 2);     // over P of piece h: MMAs run in the order of issue
+            return true;
+        };
+        if (n > 0) ok = ok && scores(0) && slopes(0);
+        for (int h = 0; h < n && ok; ++h) {
+            const int st = h % ST;
+            ok = warp_wait(p_ready, h & 1, give_up, p.status);
+            if (!ok) break;
+            fence_after_sync();
+            if (elect_one()) {
+                mma_tmem_across<DP, kRows, kRows, kCols>(dv_at, s_at, do0 + st * L::kTile, h > 0);
+                mma_commit(do_empty + st);
+            }
+            __syncwarp();
+            if (h + 1 < n && !(ok = scores(h + 1))) break;
+            ok = warp_wait(ds_ready, h & 1, give_up, p.status);
+            if (!ok) break;
+            fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+                for (int i = 0; i < kRows / 16; ++i)
+                    mma_ss(dk_at, tile_desc(ds + (i / 4) * kRows * 128 + (i % 4) * 32, 1024, 16),
+                           tile_desc(q0 + st * L::kTile + i * 2048, 1024, kRows * 128), mma_kind(DP, false, true), h > 0 || i > 0);
+                mma_commit(q_empty + st);
+            }
+            __syncwarp();
+            if (h + 1 < n) ok = slopes(h + 1);
         }
-        if (lane == 0) {
+        if (elect_one()) {
             mma_commit(done);
             mbar_wait(done, 0);
         }
         __syncwarp();
     } else {
-        const int t = warp / 8, half = warp / 4 % 2, row = threadIdx.x % kRows, j = k0 + row;
+        const int c0 = warp / 4 * kCols, row = threadIdx.x % kRows, j = k0 + row;
         const unsigned lanes = unsigned(warp % 4) * 32u << 16;
-        const unsigned s_row = s_at + t * kPiece + half * kHalf + lanes, dp_row = dp_at + t * kPiece + half * kHalf + lanes;
+        const unsigned s_row = s_at + c0 + lanes, dp_row = dp_at + c0 + lanes;
         const float2 unit = {p.s.scale * kAttnLog2e, p.s.scale * kAttnLog2e};
         // queries that see this key: i >= from
         const int from = j >= len.kv ? INT_MAX : p.s.causal ? j - len.shift : 0;
-        unsigned char *ds_row = smem + L::kS + t * L::kDs + row * 128;
+        unsigned char *ds_row = smem + L::kDs + (c0 / 64) * kRows * 128 + row * 128;
         bool ok = true;
-        for (int h = t; h < n; h += 2) {
-            const int st = h % ST, i0 = (piece0 + h % pieces) * kPiece + half * kHalf;
-            ok = warp_wait(s_full + t, (h / 2) & 1, give_up, p.status);
+        for (int h = 0; h < n; ++h) {
+            const int i0 = (tile0 + h % tiles) * kRows + c0;
+            const float4 *lse = reinterpret_cast<const float4 *>(stats + h % ST * 2 * kRows + c0), *delta = lse + kRows / 4;
+            // the row values came with Q: their copy is waited for here too
+            ok = warp_wait(q_full + h % ST, (h / ST) & 1, give_up, p.status) && warp_wait(s_full, h & 1, give_up, p.status);
             if (!ok) break;
             fence_after_sync();
-            const float4 *lse = reinterpret_cast<const float4 *>(stats + st * 2 * kPiece + half * kHalf);
-            const float4 *delta = lse + kPiece / 4;
-            uint32_t s[kHalf], dp[kHalf], pk[kHalf / 2], dk[kHalf / 2];
-            tmem_load2(s, s_row, dp, dp_row);
-            auto piece = [&](auto edge) {
+            const bool edge = __any_sync(~0u, from > i0);
+            uint32_t x[kCols], out[kCols / 2];
+            float2 pr[kCols / 2];
+            tmem_load(x, s_row);
 #pragma unroll
-                for (int c = 0; c < kHalf; c += 4) {
-                    const float4 l = lse[c / 4], d = delta[c / 4];
-                    const float2 x0 = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, unit, {l.x, l.y});
-                    const float2 x1 = fma2({__uint_as_float(s[c + 2]), __uint_as_float(s[c + 3])}, unit, {l.z, l.w});
-                    float2 p0 = {exp2_fast(x0.x), exp2_fast(x0.y)}, p1 = {exp2_fast(x1.x), exp2_fast(x1.y)};
-                    float2 d0 = mul2(p0, add2({__uint_as_float(dp[c]), __uint_as_float(dp[c + 1])}, {d.x, d.y}));
-                    float2 d1 = mul2(p1, add2({__uint_as_float(dp[c + 2]), __uint_as_float(dp[c + 3])}, {d.z, d.w}));
-                    if constexpr (decltype(edge)::value) {
-                        if (i0 + c < from) p0.x = d0.x = 0.0f;
-                        if (i0 + c + 1 < from) p0.y = d0.y = 0.0f;
-                        if (i0 + c + 2 < from) p1.x = d1.x = 0.0f;
-                        if (i0 + c + 3 < from) p1.y = d1.y = 0.0f;
-                    }
-                    pk[c / 2] = pack2(p0.x, p0.y);
-                    pk[c / 2 + 1] = pack2(p1.x, p1.y);
-                    dk[c / 2] = pack2(d0.x, d0.y);
-                    dk[c / 2 + 1] = pack2(d1.x, d1.y);
+            for (int c = 0; c < kCols; c += 4) {
+                const float4 l = lse[c / 4];
+                const float2 a = fma2({__uint_as_float(x[c]), __uint_as_float(x[c + 1])}, unit, {l.x, l.y});
+                const float2 d = fma2({__uint_as_float(x[c + 2]), __uint_as_float(x[c + 3])}, unit, {l.z, l.w});
+                pr[c / 2] = {exp2_fast(a.x), exp2_fast(a.y)};
+                pr[c / 2 + 1] = {exp2_fast(d.x), exp2_fast(d.y)};
+            }
+            if (edge) {
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    if (i0 + c < from) pr[c / 2].x = 0.0f;
+                    if (i0 + c + 1 < from) pr[c / 2].y = 0.0f;
                 }
-            };
-            if (__any_sync(~0u, from > i0)) piece(std::true_type{});
-            else piece(std::false_type{});
-            tmem_store(s_row, pk);
+            }
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<uint4 *>(ds_row + (((half * 4 + g) ^ (row & 7)) * 16)) =
-                    make_uint4(dk[g * 4], dk[g * 4 + 1], dk[g * 4 + 2], dk[g * 4 + 3]);
+            for (int c = 0; c < kCols / 2; ++c) out[c] = pack2(pr[c].x, pr[c].y);
+            tmem_store(s_row, out);
             tmem_wait_store();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_ready);
+
+            ok = warp_wait(dp_full, h & 1, give_up, p.status);
+            if (!ok) break;
+            fence_after_sync();
+            tmem_load(x, dp_row);
+#pragma unroll
+            for (int c = 0; c < kCols; c += 4) {
+                const float4 d = delta[c / 4];
+                const float2 a = mul2(pr[c / 2], add2({__uint_as_float(x[c]), __uint_as_float(x[c + 1])}, {d.x, d.y}));
+                const float2 e = mul2(pr[c / 2 + 1], add2({__uint_as_float(x[c + 2]), __uint_as_float(x[c + 3])}, {d.z, d.w}));
+                pr[c / 2] = a;
+                pr[c / 2 + 1] = e;
+            }
+            if (edge) {                                             // 0 x NaN would not be 0
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    if (i0 + c < from) pr[c / 2].x = 0.0f;
+                    if (i0 + c + 1 < from) pr[c / 2].y = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kCols / 2; ++c) out[c] = pack2(pr[c].x, pr[c].y);
+#pragma unroll
+            for (int g = 0; g < kCols / 8; ++g)
+                *reinterpret_cast<uint4 *>(ds_row + (((c0 % 64 / 8 + g) ^ (row & 7)) * 16)) =
+                    make_uint4(out[g * 4], out[g * 4 + 1], out[g * 4 + 2], out[g * 4 + 3]);
             fence_async_proxy();
             fence_before_sync();
-            mbar_arrive(ds_ready + t);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_ready);
         }
         // warps 0-7 write dV, warps 8-15 dK, half of the columns each four
         if (n > 0 && ok) ok = warp_wait(done, 0, give_up, p.status);
         ok = __all_sync(~0u, ok && *give_up == 0);
         fence_after_sync();
-        const OutView &o = t == 0 ? p.dv : p.dk;
-        const int c0 = half * (DP / 2);
+        const bool values = warp < 8;
+        const OutView &o = values ? p.dv : p.dk;
+        const int half = warp / 4 % 2, d0 = half * (DP / 2);
         __nv_bfloat16 *dst = o.data + b * o.batch + (long long)j * o.row + kv_head * o.head;
         const bool mine = ok && j < p.s.kv_len;
         if (n > 0 && ok)
-            store_row<DP / 2>((t == 0 ? dv_at : dk_at) + lanes + c0, t == 0 ? 1.0f : p.s.scale, dst + c0, p.s.dim - c0, mine);
+            store_row<DP / 2>((values ? dv_at : dk_at) + lanes + d0, values ? 1.0f : p.s.scale, dst + d0, p.s.dim - d0, mine);
         else if (mine && half == 0)
             store_zeros(dst, p.s.dim);
     }
@@ -264,23 +315,24 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
 // ---- dQ -----------------------------------------------------------------------------------------
 
 template <int DP> struct QueriesShared {
-    static constexpr int kStages = 4;
-    static constexpr int kTile = kRows * DP * 2, kPieceTile = kPiece * DP * 2;
-    static constexpr int kQ = 0, kDo = kTile, kK = 2 * kTile, kV = kK + kStages * kPieceTile;
-    static constexpr int kBars = kV + kStages * kPieceTile;
-    static constexpr int kBytes = kBars + 256 + 1024;
+    static constexpr int kKStages = 3, kVStages = 2;
+    static constexpr int kTile = kRows * DP * 2;
+    static constexpr int kQ = 0, kDo = kTile, kK = 2 * kTile, kV = kK + kKStages * kTile;
+    static constexpr int kBars = kV + kVStages * kTile;
+    static constexpr int kBytes = kBars + 256 + 1024;      // barriers, and the base rounded up to 1024
+    static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
 template <int DP>
 __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(const __grid_constant__ AttnBackwardParams p)
 {
     using L = QueriesShared<DP>;
-    constexpr int ST = L::kStages;
+    constexpr int KS = L::kKStages, VS = L::kVStages;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
-    unsigned long long *q_full = bars, *full = bars + 1, *empty = full + ST, *s_full = empty + ST, *ds_ready = s_full + 2;
-    unsigned long long *done = ds_ready + 2;
+    unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + KS, *v_full = k_empty + KS, *v_empty = v_full + VS;
+    unsigned long long *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_ready = dp_full + 1, *done = ds_ready + 1;
     volatile int *give_up = reinterpret_cast<int *>(done + 1);
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(done + 2);
 
@@ -291,12 +343,14 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     const Lengths len = lengths_of(p.s, b);
     const int last = min(q0 + kRows, len.q) - 1;
     const int seen = last < q0 ? 0 : p.s.causal ? min(len.kv, last + len.shift + 1) : len.kv;
-    const int n = seen > 0 ? (seen + kPiece - 1) / kPiece : 0;
+    const int n = seen > 0 ? (seen + kRows - 1) / kRows : 0;
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
-        for (int i = 0; i < ST; ++i) { mbar_init(full + i, 1); mbar_init(empty + i, 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(ds_ready + t, 2 * kRows); }
+        for (int i = 0; i < KS; ++i) { mbar_init(k_full + i, 1); mbar_init(k_empty + i, 1); }
+        for (int i = 0; i < VS; ++i) { mbar_init(v_full + i, 1); mbar_init(v_empty + i, 1); }
+        mbar_init(s_full, 1); mbar_init(s_full + 1, 1);
+        mbar_init(dp_full, 1); mbar_init(ds_ready, kElementWarps);
         mbar_init(done, 1);
         *give_up = 0;
         fence_barrier_init();
@@ -306,109 +360,133 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     __syncthreads();
     fence_after_sync();
     const unsigned tmem = *tmem_cell;
-    const unsigned dq_at = tmem, s_at = tmem + DP, dp_at = s_at + 2 * kPiece;
+    const unsigned dq_at = tmem, s_at = tmem + DP, dp_at = s_at + 2 * kRows;
 
     if (warp == kLoadWarp) {
         if (lane == 0 && n > 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
             mbar_expect_tx(q_full, 2 * L::kTile);
             load_tile<DP, kRows>(smem + L::kQ, &p.q, head, q0, b, q_full);
-            load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
-            int armed = 0;
+            int k_armed = 0, v_armed = 0;
             for (int h = 0; h < n; ++h) {
-                const int st = h % ST;
-                if (!bounded_wait(empty + st, ((h / ST) & 1) ^ 1, give_up, p.status)) break;
-                mbar_expect_tx(full + st, 2 * L::kPieceTile);
-                load_tile<DP, kPiece>(smem + L::kK + st * L::kPieceTile, &p.k, kv_head, h * kPiece, b, full + st);
-                load_tile<DP, kPiece>(smem + L::kV + st * L::kPieceTile, &p.v, kv_head, h * kPiece, b, full + st);
-                ++armed;
+                const int ks = h % KS, vs = h % VS;
+                if (!bounded_wait(k_empty + ks, ((h / KS) & 1) ^ 1, give_up, p.status)) break;
+                mbar_expect_tx(k_full + ks, L::kTile);
+                load_tile<DP, kRows>(smem + L::kK + ks * L::kTile, &p.k, kv_head, h * kRows, b, k_full + ks);
+                ++k_armed;
+                if (h == 0) load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
+                if (!bounded_wait(v_empty + vs, ((h / VS) & 1) ^ 1, give_up, p.status)) break;
+                mbar_expect_tx(v_full + vs, L::kTile);
+                load_tile<DP, kRows>(smem + L::kV + vs * L::kTile, &p.v, kv_head, h * kRows, b, v_full + vs);
+                ++v_armed;
             }
             mbar_wait(q_full, 0);
-            for (int h = max(0, armed - ST); h < armed; ++h) mbar_wait(full + h % ST, (h / ST) & 1);
+            for (int h = max(0, k_armed - KS); h < k_armed; ++h) mbar_wait(k_full + h % KS, (h / KS) & 1);
+            for (int h = max(0, v_armed - VS); h < v_armed; ++h) mbar_wait(v_full + h % VS, (h / VS) & 1);
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
         const unsigned q = smem_addr(smem + L::kQ), d = smem_addr(smem + L::kDo);
+        const unsigned k0 = smem_addr(smem + L::kK), v0 = smem_addr(smem + L::kV);
         bool ok = n == 0 || warp_wait(q_full, 0, give_up, p.status);
         auto scores = [&](int h) {
-            const int st = h % ST;
-            const bool w = warp_wait(full + st, (h / ST) & 1, give_up, p.status);
-            if (!w) return false;
-            if (p.s.kv_lengths && len.kv - h * kPiece < kPiece)
-                zero_rows<DP, kPiece>(smem + L::kK + st * L::kPieceTile, len.kv - h * kPiece);
+            const int st = h % KS;
+            if (!warp_wait(k_full + st, (h / KS) & 1, give_up, p.status)) return false;
+            if (p.s.kv_lengths && len.kv - h * kRows < kRows) zero_rows<DP, kRows>(smem + L::kK + st * L::kTile, len.kv - h * kRows);
             fence_after_sync();
-            if (lane == 0) {
-                const unsigned k = smem_addr(smem + L::kK + st * L::kPieceTile), v = smem_addr(smem + L::kV + st * L::kPieceTile);
-                mma_along<DP, kRows, kPiece, kPiece>(s_at + (h & 1) * kPiece, q, k, false);
-                mma_along<DP, kRows, kPiece, kPiece>(dp_at + (h & 1) * kPiece, d, v, false);
+            if (elect_one()) {
+                mma_along<DP, kRows, kRows, kRows>(s_at + (h & 1) * kRows, q, k0 + st * L::kTile, false);
                 mma_commit(s_full + (h & 1));
             }
             __syncwarp();
             return true;
         };
-        for (int h = 0; h < 2 && h < n && ok; ++h) ok = scores(h);
-        for (int h = 0; h < n && ok; ++h) {
-            const int st = h % ST, t = h & 1;
-            ok = warp_wait(ds_ready + t, (h / 2) & 1, give_up, p.status);
-            if (!ok) break;
+        auto slopes = [&](int h) {
+            const int st = h % VS;
+            if (!warp_wait(v_full + st, (h / VS) & 1, give_up, p.status)) return false;
             fence_after_sync();
-            if (lane == 0) {
-                mma_tmem_across<DP, kPiece, kPiece, kHalf>(dq_at, s_at + t * kPiece, smem_addr(smem + L::kK + st * L::kPieceTile), h > 0);
-                mma_commit(empty + st);
+            if (elect_one()) {
+                mma_along<DP, kRows, kRows, kRows>(dp_at, d, v0 + st * L::kTile, false);
+                mma_commit(dp_full);
+                mma_commit(v_empty + st);
             }
             __syncwarp();
-            if (h + 2 < n) ok = scores(h + 2);     // over dS of piece h: MMAs run in the order of issue
+            return true;
+        };
+        if (n > 0) ok = ok && scores(0) && slopes(0);
+        if (n > 1) ok = ok && scores(1);
+        for (int h = 0; h < n && ok; ++h) {
+            const int st = h % KS;
+            ok = warp_wait(ds_ready, h & 1, give_up, p.status);
+            if (!ok) break;
+            fence_after_sync();
+            if (elect_one()) {
+                mma_tmem_across<DP, kRows, kRows, kCols>(dq_at, s_at + (h & 1) * kRows, k0 + st * L::kTile, h > 0);
+                mma_commit(k_empty + st);
+            }
+            __syncwarp();
+            if (h + 1 < n) ok = slopes(h + 1);
+            if (ok && h + 2 < n) ok = scores(h + 2);
         }
-        if (lane == 0) {
+        if (elect_one()) {
             mma_commit(done);
             mbar_wait(done, 0);
         }
         __syncwarp();
     } else {
-        const int t = warp / 8, half = warp / 4 % 2, row = threadIdx.x % kRows, i = q0 + row;
+        const int c0 = warp / 4 * kCols, row = threadIdx.x % kRows, i = q0 + row;
         const unsigned lanes = unsigned(warp % 4) * 32u << 16;
-        const unsigned s_row = s_at + t * kPiece + half * kHalf + lanes, dp_row = dp_at + t * kPiece + half * kHalf + lanes;
+        const unsigned s_row = s_at + c0 + lanes, dp_row = dp_at + c0 + lanes;
         const float2 unit = {p.s.scale * kAttnLog2e, p.s.scale * kAttnLog2e};
         const int limit = i >= len.q ? 0 : p.s.causal ? min(len.kv, i + len.shift + 1) : len.kv;
         const long long at = ((long long)b * p.s.heads + head) * p.q_pad + i;
-        const float lse = p.row_lse[at], delta = p.row_delta[at];
+        const float2 lse = {p.row_lse[at], p.row_lse[at]}, delta = {p.row_delta[at], p.row_delta[at]};
         bool ok = true;
-        for (int h = t; h < n; h += 2) {
-            ok = warp_wait(s_full + t, (h / 2) & 1, give_up, p.status);
+        for (int h = 0; h < n; ++h) {
+            const unsigned s_here = s_row + (h & 1) * kRows;
+            ok = warp_wait(s_full + (h & 1), (h / 2) & 1, give_up, p.status);
             if (!ok) break;
             fence_after_sync();
-            const int open = limit - h * kPiece - half * kHalf;
-            uint32_t s[kHalf], dp[kHalf], pk[kHalf / 2];
-            tmem_load2(s, s_row, dp, dp_row);
-            auto piece = [&](auto edge) {
+            const int open = limit - h * kRows - c0;
+            uint32_t x[kCols], out[kCols / 2];
+            float2 pr[kCols / 2];
+            tmem_load(x, s_here);
 #pragma unroll
-                for (int c = 0; c < kHalf; c += 2) {
-                    const float2 x = fma2({__uint_as_float(s[c]), __uint_as_float(s[c + 1])}, unit, {lse, lse});
-                    const float2 pr = {exp2_fast(x.x), exp2_fast(x.y)};
-                    float2 dr = mul2(pr, add2({__uint_as_float(dp[c]), __uint_as_float(dp[c + 1])}, {delta, delta}));
-                    if constexpr (decltype(edge)::value) {
-                        if (c >= open) dr.x = 0.0f;
-                        if (c + 1 >= open) dr.y = 0.0f;
-                    }
-                    pk[c / 2] = pack2(dr.x, dr.y);
+            for (int c = 0; c < kCols; c += 2) {
+                const float2 a = fma2({__uint_as_float(x[c]), __uint_as_float(x[c + 1])}, unit, lse);
+                pr[c / 2] = {exp2_fast(a.x), exp2_fast(a.y)};
+            }
+            ok = warp_wait(dp_full, h & 1, give_up, p.status);
+            if (!ok) break;
+            fence_after_sync();
+            tmem_load(x, dp_row);
+#pragma unroll
+            for (int c = 0; c < kCols; c += 2)
+                pr[c / 2] = mul2(pr[c / 2], add2({__uint_as_float(x[c]), __uint_as_float(x[c + 1])}, delta));
+            if (__any_sync(~0u, open < kCols)) {
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    if (c >= open) pr[c / 2].x = 0.0f;
+                    if (c + 1 >= open) pr[c / 2].y = 0.0f;
                 }
-            };
-            if (__any_sync(~0u, open < kHalf)) piece(std::true_type{});
-            else piece(std::false_type{});
-            tmem_store(s_row, pk);
+            }
+#pragma unroll
+            for (int c = 0; c < kCols / 2; ++c) out[c] = pack2(pr[c].x, pr[c].y);
+            tmem_store(s_here, out);
             tmem_wait_store();
             fence_before_sync();
-            mbar_arrive(ds_ready + t);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ds_ready);
         }
         if (n > 0 && ok) ok = warp_wait(done, 0, give_up, p.status);
         ok = __all_sync(~0u, ok && *give_up == 0);
         fence_after_sync();
-        // every warpgroup a quarter of the columns
-        const int c0 = (2 * t + half) * (DP / 4);
+        // every four warps a quarter of the columns
+        const int d0 = warp / 4 * (DP / 4);
         __nv_bfloat16 *dst = p.dq.data + b * p.dq.batch + (long long)i * p.dq.row + head * p.dq.head;
         const bool mine = ok && i < p.s.q_len, empty = limit <= 0;
-        if (n > 0 && ok) store_row<DP / 4>(dq_at + lanes + c0, p.s.scale, dst + c0, p.s.dim - c0, mine && !empty);
-        if (c0 == 0 && mine && empty) store_zeros(dst, p.s.dim);
+        if (n > 0 && ok) store_row<DP / 4>(dq_at + lanes + d0, p.s.scale, dst + d0, p.s.dim - d0, mine && !empty);
+        if (d0 == 0 && mine && empty) store_zeros(dst, p.s.dim);
     }
     fence_before_sync();
     __syncthreads();

@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
         if (n > 0 && ok) ok = warp_wait(k_full, 0, give_up, p.status);
         const unsigned q = smem_addr(smem + L::kQ), k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
         fence_after_sync();
-        if (ok && lane == 0) {
+        if (ok && elect_one()) {
             for (int t = 0; t < 2; ++t)
                 if (tiles[t] > 0) {
                     mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k, false);
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 if (!ok || j >= tiles[t]) continue;
                 ok = warp_wait(p_ready + t, j & 1, give_up, p.status);
                 fence_after_sync();
-                if (ok && lane == 0) {
+                if (ok && elect_one()) {
                     mma_tmem_across<DP, kRows, kRows, kRows>(o_at + t * DP, s_at + t * kRows, v + st * L::kTile, j > 0);
                     // the next scores go over P: the tensor core takes MMAs in order
                     if (j + 1 < tiles[t]) {
@@ -142,13 +142,13 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 }
                 __syncwarp();
             }
-            if (ok && lane == 0) {
+            if (ok && elect_one()) {
                 if (j + 1 < n) mma_commit(k_empty + next);
                 mma_commit(v_empty + st);
             }
             __syncwarp();
         }
-        if (lane == 0) {
+        if (elect_one()) {
             mma_commit(drained);
             mbar_wait(drained, 0);
         }

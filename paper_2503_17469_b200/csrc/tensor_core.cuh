@@ -91,6 +91,16 @@ __device__ __forceinline__ void tmem_store(unsigned addr, const uint32_t (&r)[32
 
 // ---- tcgen05.mma --------------------------------------------------------------------------------
 
+// True in one lane of a converged warp, the same one every time.  The MMAs of a block are issued under it: the
+// compiler knows that one thread runs and keeps descriptors in uniform registers (under `lane == 0` every MMA
+// first moved its operands there, and issuing took 75-90 cycles each, more than the tensor core needs for it).
+__device__ __forceinline__ bool elect_one()
+{
+    unsigned one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one)::"memory");
+    return one != 0;
+}
+
 // Shared-memory descriptor of a swizzled tile.  K-major: `step` = bytes between groups of 8 rows
 // (1024), `across` unused.  MN-major: `step` = bytes between groups of 8 contraction rows (1024),
 // `across` = bytes between blocks of 64 columns.
