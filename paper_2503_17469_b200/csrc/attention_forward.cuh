@@ -24,7 +24,9 @@ struct AttnForwardParams {
     unsigned *status;
 };
 
-constexpr int kForwardThreads = 320;
+// Three warpgroups at 168 registers; the third, of which two warps have work, hands most of its share to the other two.
+constexpr int kForwardThreads = 384;
+constexpr int kForwardFew = 80, kForwardMany = 208;    // 128 x 40 + 256 x 232 = 384 x 168
 constexpr float kRescaleAbove = 8.0f;
 
 template <int DP> struct ForwardShared {
@@ -43,7 +45,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
     unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST;
-    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 2, *drained = o_full + 2;
+    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 4, *drained = o_full + 2;
     volatile int *give_up = reinterpret_cast<int *>(drained + 1);
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(drained + 2);
 
@@ -69,7 +71,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
             mbar_init(k_full + i, 1); mbar_init(k_empty + i, 1);
             mbar_init(v_full + i, 1); mbar_init(v_empty + i, 1);
         }
-        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(p_ready + t, kRows); mbar_init(o_full + t, 1); }
+        for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(o_full + t, 1); }
+        for (int i = 0; i < 4; ++i) mbar_init(p_ready + i, 4);        // [tile][half]
         mbar_init(drained, 1);
         *give_up = 0;
         fence_barrier_init();
@@ -81,6 +84,8 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     const unsigned tmem = *tmem_cell;
     const unsigned s_at = tmem, o_at = tmem + 2 * kRows;             // S0 S1 | O0 O1
 
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kForwardFew));
     if (warp == 8) {
         if (lane == 0 && n > 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v);
@@ -128,19 +133,25 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 if (!ok || j >= tiles[t]) continue;
-                ok = warp_wait(p_ready + t, j & 1, give_up, p.status);
-                fence_after_sync();
-                if (ok && elect_one()) {
-                    mma_tmem_across<DP, kRows, kRows, kRows>(o_at + t * DP, s_at + t * kRows, v + st * L::kTile, j > 0);
-                    // the next scores go over P: the tensor core takes MMAs in order
-                    if (j + 1 < tiles[t]) {
-                        mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
-                        mma_commit(s_full + t);
-                    } else {
-                        mma_commit(o_full + t);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ok = ok && warp_wait(p_ready + 2 * t + half, j & 1, give_up, p.status);
+                    fence_after_sync();
+                    if (ok && elect_one()) {
+                        mma_tmem_across<DP, kRows, 64, 64>(o_at + t * DP, s_at + t * kRows + half * 32, v + st * L::kTile + half * 64 * 128,
+                                                           j > 0 || half > 0);
+                        if (half == 1) {
+                            // the next scores go over P: the tensor core takes MMAs in order
+                            if (j + 1 < tiles[t]) {
+                                mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
+                                mma_commit(s_full + t);
+                            } else {
+                                mma_commit(o_full + t);
+                            }
+                        }
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
             if (ok && elect_one()) {
                 if (j + 1 < n) mma_commit(k_empty + next);
@@ -153,7 +164,9 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
             mbar_wait(drained, 0);
         }
         __syncwarp();
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kForwardMany));
         const int t = warp / 4, row = threadIdx.x % kRows, i = q0 + t * kRows + row;
         const unsigned lanes = unsigned(warp % 4) * 32u << 16;
         const unsigned s_row = s_at + t * kRows + lanes, o_row = o_at + t * DP + lanes;
@@ -207,17 +220,18 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 uint32_t packed[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) {
-                    const float2 y = fma2({__uint_as_float(x[h][c]), __uint_as_float(x[h][c + 1])}, unit2, ref2);
-                    const float2 e = {exp2_fast(y.x), exp2_fast(y.y)};
+                    const float2 z = fma2({__uint_as_float(x[h][c]), __uint_as_float(x[h][c + 1])}, unit2, ref2);
+                    const float2 e = {exp2_fast(z.x), exp2_fast(z.y)};
                     sum[c / 2 % 2] = add2(sum[c / 2 % 2], e);
                     packed[c / 2] = pack2(e.x, e.y);
                 }
                 tmem_store(s_row + h * 32, packed);
+                tmem_wait_store();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_ready + 2 * t + h);
             }
             l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-            tmem_wait_store();
-            fence_before_sync();
-            mbar_arrive(p_ready + t);
         }
         if (ok && tiles[t] > 0) ok = warp_wait(o_full + t, 0, give_up, p.status);
         fence_after_sync();
