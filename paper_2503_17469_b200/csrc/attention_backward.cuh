@@ -11,7 +11,7 @@
 // elementwise work comes in two phases, P from S and dS from P and dP, sixteen warps at 32 columns of a row per thread,
 // and each phase runs beside products of the same or the next tile:
 //   dK, dV: S^T = K Q^T and dP^T = V dO^T (128 keys x 128 queries).  P^T goes back to tensor memory over S^T as the A
-//     operand of dV += P^T dO; dS^T goes to shared memory as that of dK += dS^T Q.
+//     operand of dV += P^T dO, dS^T over dP^T as that of dK += dS^T Q.
 //     Order of the products: S0 dP0 | dV0 S1 dK0 dP1 | dV1 S2 dK1 dP2 | ...
 //   dQ:     S = Q K^T and dP = dO V^T (128 queries x 128 keys), two tiles of S; dS over S as the A operand of dQ += dS K.
 //     Order: S0 dP0 S1 | dQ0 dP1 S2 | dQ1 dP2 S3 | ...
@@ -77,11 +77,10 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnRowsParam
 template <int DP> struct KeysShared {
     static constexpr int kStages = DP == 128 ? 2 : 3;
     static constexpr int kTile = kRows * DP * 2;
-    static constexpr int kK = 0, kV = kTile, kQ = 2 * kTile, kDo = kQ + kStages * kTile, kDs = kDo + kStages * kTile;
-    static constexpr int kStats = kDs + kRows * kRows * 2;         // [stages][2][128] float
+    static constexpr int kK = 0, kV = kTile, kQ = 2 * kTile, kDo = kQ + kStages * kTile;
+    static constexpr int kStats = kDo + kStages * kTile;           // [stages][2][128] float
     static constexpr int kBars = kStats + kStages * 2 * kRows * 4;
-    // barriers, and what is left of the block's 227 KB for rounding the base up to 1024
-    static constexpr int kBytes = kBars + 256 + (DP == 128 ? 768 : 1024);
+    static constexpr int kBytes = kBars + 256 + 1024;              // barriers, and the base rounded up to 1024
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
@@ -161,7 +160,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV), ds = smem_addr(smem + L::kDs);
+        const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
         const unsigned q0 = smem_addr(smem + L::kQ), do0 = smem_addr(smem + L::kDo);
         bool ok = n == 0 || warp_wait(kv_full, 0, give_up, p.status);
         // rows of tile h that are queries of this sequence; those behind it may hold anything
@@ -206,10 +205,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
             if (!ok) break;
             fence_after_sync();
             if (elect_one()) {
-#pragma unroll
-                for (int i = 0; i < kRows / 16; ++i)
-                    mma_ss(dk_at, tile_desc(ds + (i / 4) * kRows * 128 + (i % 4) * 32, 1024, 16),
-                           tile_desc(q0 + st * L::kTile + i * 2048, 1024, kRows * 128), mma_kind(DP, false, true), h > 0 || i > 0);
+                mma_tmem_across<DP, kRows, kRows, kCols>(dk_at, dp_at, q0 + st * L::kTile, h > 0);
                 mma_commit(q_empty + st);
             }
             __syncwarp();
@@ -227,7 +223,6 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
         const float2 unit = {p.s.scale * kAttnLog2e, p.s.scale * kAttnLog2e};
         // queries that see this key: i >= from
         const int from = j >= len.kv ? INT_MAX : p.s.causal ? j - len.shift : 0;
-        unsigned char *ds_row = smem + L::kDs + (c0 / 64) * kRows * 128 + row * 128;
         bool ok = true;
         for (int h = 0; h < n; ++h) {
             const int i0 = (tile0 + h % tiles) * kRows + c0;
@@ -284,11 +279,8 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
             }
 #pragma unroll
             for (int c = 0; c < kCols / 2; ++c) out[c] = pack2(pr[c].x, pr[c].y);
-#pragma unroll
-            for (int g = 0; g < kCols / 8; ++g)
-                *reinterpret_cast<uint4 *>(ds_row + (((c0 % 64 / 8 + g) ^ (row & 7)) * 16)) =
-                    make_uint4(out[g * 4], out[g * 4 + 1], out[g * 4 + 2], out[g * 4 + 3]);
-            fence_async_proxy();
+            tmem_store(dp_row, out);
+            tmem_wait_store();
             fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(ds_ready);

@@ -71,34 +71,6 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
     return d;
 }
 
-// The same for two finite or NaN values of at least -2^22, on the multiply-add units, for kernels that the special-function
-// unit bounds: x = n + f with n = round(x), 2^f by a polynomial of degree 4 or 5 fitted to least relative error on
-// [-1/2, 1/2] (2.6e-6 and 7.5e-8, then float rounding), times 2^n built from its exponent.  Below 2^-126: 2^-126.
-template <int DEGREE> __device__ __forceinline__ float2 exp2_fma(float2 x)
-{
-    static_assert(DEGREE == 4 || DEGREE == 5, "fitted degrees");
-    constexpr float kRound = 12582912.0f;                           // 1.5 * 2^23: adding it rounds to an integer
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.0f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.0f));
-    const float2 t = add2(x, {kRound, kRound});
-    const float2 n = add2(t, {-kRound, -kRound});
-    const float2 f = fma2(n, {-1.0f, -1.0f}, x);
-    float2 p;
-    if constexpr (DEGREE == 5) {
-        p = fma2({1.327647129e-3f, 1.327647129e-3f}, f, {9.675540961e-3f, 9.675540961e-3f});
-        p = fma2(p, f, {5.550713092e-2f, 5.550713092e-2f});
-        p = fma2(p, f, {2.402212024e-1f, 2.402212024e-1f});
-        p = fma2(p, f, {6.931469440e-1f, 6.931469440e-1f});
-        p = fma2(p, f, {1.000000119f, 1.000000119f});
-    } else {
-        p = fma2({9.570101276e-3f, 9.570101276e-3f}, f, {5.591785908e-2f, 5.591785908e-2f});
-        p = fma2(p, f, {2.402474433e-1f, 2.402474433e-1f});
-        p = fma2(p, f, {6.931217909e-1f, 6.931217909e-1f});
-        p = fma2(p, f, {9.999992847e-1f, 9.999992847e-1f});
-    }
-    const float2 e = {__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u)};
-    return mul2(p, e);
-}
 // Eight elements at a 16-byte aligned address.  Floats take one 256-bit access where the address allows it: two of 128
 // bits would each touch half of every 32-byte sector of a warp's stretch.
 __device__ __forceinline__ bool aligned32(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
