@@ -48,17 +48,61 @@ __device__ __forceinline__ void load_tile(unsigned char *dst, const CUtensorMap 
     for (int c = 0; c < DP / 64; ++c) tensor_load(dst + c * ROWS * 128, map, c * 64, head, row, batch, bar);
 }
 
-// Zeroes rows [from, ROWS) of a tile, by one warp; the MMA that reads it next sees the zeros.  Rows
-// behind a sequence's length hold whatever the caller left there, and 0 x NaN would reach the sums.
-template <int DP, int ROWS> __device__ __forceinline__ void zero_rows(unsigned char *tile, int from)
+// Zeroes rows [from, 128) of a tile, by one warp; the MMA that reads it next sees the zeros.
+template <int DP> __device__ __forceinline__ void zero_rows(unsigned char *tile, int from)
 {
     const int lane = threadIdx.x % 32;
     for (int c = 0; c < DP / 64; ++c)
-        for (int i = from * 8 + lane; i < ROWS * 8; i += 32)
-            *reinterpret_cast<uint4 *>(tile + c * ROWS * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        for (int i = from * 8 + lane; i < kRows * 8; i += 32)
+            *reinterpret_cast<uint4 *>(tile + c * kRows * 128 + i * 16) = make_uint4(0, 0, 0, 0);
     fence_async_proxy();
     __syncwarp();
 }
+
+// What the loading warp of a block keeps: where waits are recorded, and a barrier of its own.
+struct Loader {
+    unsigned long long *own;
+    unsigned parity;
+    volatile int *give_up;
+    unsigned *status;
+
+    __device__ __forceinline__ bool wait(unsigned long long *bar, unsigned p) { return warp_wait(bar, p, give_up, status); }
+
+    // A 128 x DP tile into `dst`; `bar` gets this phase's one arrival and the bytes, `more` further bytes are on their way to
+    // it.  Rows from `valid` on lie behind the sequence's length, where the caller may have left anything, and
+    // 0 x NaN would reach the sums: such a tile is waited for here, zeroed from there on, and handed over then.
+    template <int DP>
+    __device__ __forceinline__ bool tile(unsigned char *dst, const CUtensorMap *map, int head, int row, int batch,
+                                         unsigned long long *bar, int valid, unsigned more = 0)
+    {
+        const bool first = threadIdx.x % 32 == 0;
+        constexpr unsigned bytes = kRows * DP * 2;
+        if (valid >= kRows) {
+            if (first) {
+                mbar_expect_tx(bar, bytes + more);
+                load_tile<DP, kRows>(dst, map, head, row, batch, bar);
+            }
+            return true;
+        }
+        if (first) {
+            mbar_expect_tx(own, bytes);
+            load_tile<DP, kRows>(dst, map, head, row, batch, own);
+        }
+        __syncwarp();
+        if (!wait(own, parity)) {
+            mbar_wait(own, parity);          // the block may not end with the copy in flight
+            return false;
+        }
+        parity ^= 1;
+        zero_rows<DP>(dst, valid);
+        if (first) {
+            if (more) mbar_expect_tx(bar, more);
+            else mbar_arrive(bar);
+        }
+        __syncwarp();
+        return true;
+    }
+};
 
 // d[128 x N] (+)= A B^T, both tiles with the contraction along their rows' DP columns; RA, RB rows per block.
 template <int DP, int RA, int RB, int N>

@@ -94,8 +94,9 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
     unsigned long long *kv_full = bars, *q_full = bars + 1, *q_empty = q_full + ST, *do_full = q_empty + ST, *do_empty = do_full + ST;
     unsigned long long *s_full = do_empty + ST, *p_ready = s_full + 1, *dp_full = p_ready + 1, *ds_ready = dp_full + 1, *done = ds_ready + 1;
-    volatile int *give_up = reinterpret_cast<int *>(done + 1);
-    unsigned *tmem_cell = reinterpret_cast<unsigned *>(done + 2);
+    unsigned long long *own = done + 1;
+    volatile int *give_up = reinterpret_cast<int *>(own + 1);
+    unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
     const float *stats = reinterpret_cast<const float *>(smem + L::kStats);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
         }
         mbar_init(s_full, 1); mbar_init(p_ready, kElementWarps);
         mbar_init(dp_full, 1); mbar_init(ds_ready, kElementWarps);
-        mbar_init(done, 1);
+        mbar_init(done, 1); mbar_init(own, 1);
         *give_up = 0;
         fence_barrier_init();
     }
@@ -130,27 +131,31 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     const unsigned dv_at = tmem, dk_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kRows;
 
     if (warp == kLoadWarp) {
-        if (lane == 0 && n > 0) {
-            prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
-            mbar_expect_tx(kv_full, 2 * L::kTile);
-            load_tile<DP, kRows>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
+        if (n > 0) {
+            Loader load = {own, 0, give_up, p.status};
+            if (lane == 0) {
+                prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
+                mbar_expect_tx(kv_full, 2 * L::kTile);
+                load_tile<DP, kRows>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
+                load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
+            }
             int q_armed = 0, do_armed = 0;
             const unsigned long long policy = policy_evict_last();
             for (int h = 0; h < n; ++h) {
                 const int st = h % ST, head = kv_head * group + h / tiles, row = (tile0 + h % tiles) * kRows;
+                const int valid = p.s.q_lengths ? len.q - row : kRows;
                 const unsigned free_parity = ((h / ST) & 1) ^ 1;
-                if (!bounded_wait(q_empty + st, free_parity, give_up, p.status)) break;
-                mbar_expect_tx(q_full + st, L::kTile + 2 * kRows * 4);
-                load_tile<DP, kRows>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st);
-                const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
-                float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kRows;
-                bulk_load(to, p.row_lse + at, kRows * 4, q_full + st, policy);
-                bulk_load(to + kRows, p.row_delta + at, kRows * 4, q_full + st, policy);
+                if (!load.wait(q_empty + st, free_parity)) break;
+                if (!load.tile<DP>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st, valid, 2 * kRows * 4)) break;
+                if (lane == 0) {
+                    const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
+                    float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kRows;
+                    bulk_load(to, p.row_lse + at, kRows * 4, q_full + st, policy);
+                    bulk_load(to + kRows, p.row_delta + at, kRows * 4, q_full + st, policy);
+                }
                 ++q_armed;
-                if (h == 0) load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
-                if (!bounded_wait(do_empty + st, free_parity, give_up, p.status)) break;
-                mbar_expect_tx(do_full + st, L::kTile);
-                load_tile<DP, kRows>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st);
+                if (!load.wait(do_empty + st, free_parity)) break;
+                if (!load.tile<DP>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st, valid)) break;
                 ++do_armed;
             }
             // the block may not end with a copy in flight, not even when it gave up
@@ -160,58 +165,40 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
-        const unsigned q0 = smem_addr(smem + L::kQ), do0 = smem_addr(smem + L::kDo);
-        bool ok = n == 0 || warp_wait(kv_full, 0, give_up, p.status);
-        // rows of tile h that are queries of this sequence; those behind it may hold anything
-        auto rows_of = [&](int h) { return p.s.q_lengths ? len.q - (tile0 + h % tiles) * kRows : kRows; };
-        auto scores = [&](int h) {
-            const int st = h % ST;
-            if (!warp_wait(q_full + st, (h / ST) & 1, give_up, p.status)) return false;
-            if (rows_of(h) < kRows) zero_rows<DP, kRows>(smem + L::kQ + st * L::kTile, rows_of(h));
-            fence_after_sync();
-            if (elect_one()) {
+        if (elect_one()) {
+            const unsigned k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
+            const unsigned q0 = smem_addr(smem + L::kQ), do0 = smem_addr(smem + L::kDo);
+            auto wait = [&](unsigned long long *bar, unsigned parity) { return bounded_wait(bar, parity, give_up, p.status); };
+            auto scores = [&](int h) {
+                const int st = h % ST;
+                if (!wait(q_full + st, (h / ST) & 1)) return false;
+                fence_after_sync();
                 mma_along<DP, kRows, kRows, kRows>(s_at, k, q0 + st * L::kTile, false);
                 mma_commit(s_full);
-            }
-            __syncwarp();
-            return true;
-        };
-        auto slopes = [&](int h) {
-            const int st = h % ST;
-            if (!warp_wait(do_full + st, (h / ST) & 1, give_up, p.status)) return false;
-            if (rows_of(h) < kRows) zero_rows<DP, kRows>(smem + L::kDo + st * L::kTile, rows_of(h));
-            fence_after_sync();
-            if (elect_one()) {
+                return true;
+            };
+            auto slopes = [&](int h) {
+                const int st = h % ST;
+                if (!wait(do_full + st, (h / ST) & 1)) return false;
+                fence_after_sync();
                 mma_along<DP, kRows, kRows, kRows>(dp_at, v, do0 + st * L::kTile, false);
                 mma_commit(dp_full);
-            }
-            __syncwarp();
-            return true;
-        };
-        if (n > 0) ok = ok && scores(0) && slopes(0);
-        for (int h = 0; h < n && ok; ++h) {
-            const int st = h % ST;
-            ok = warp_wait(p_ready, h & 1, give_up, p.status);
-            if (!ok) break;
-            fence_after_sync();
-            if (elect_one()) {
+                return true;
+            };
+            bool ok = n > 0 && wait(kv_full, 0) && scores(0) && slopes(0);
+            for (int h = 0; h < n && ok; ++h) {
+                const int st = h % ST;
+                if (!(ok = wait(p_ready, h & 1))) break;
+                fence_after_sync();
                 mma_tmem_across<DP, kRows, kRows, kCols>(dv_at, s_at, do0 + st * L::kTile, h > 0);
                 mma_commit(do_empty + st);
-            }
-            __syncwarp();
-            if (h + 1 < n && !(ok = scores(h + 1))) break;
-            ok = warp_wait(ds_ready, h & 1, give_up, p.status);
-            if (!ok) break;
-            fence_after_sync();
-            if (elect_one()) {
+                if (h + 1 < n && !(ok = scores(h + 1))) break;
+                if (!(ok = wait(ds_ready, h & 1))) break;
+                fence_after_sync();
                 mma_tmem_across<DP, kRows, kRows, kCols>(dk_at, dp_at, q0 + st * L::kTile, h > 0);
                 mma_commit(q_empty + st);
+                if (h + 1 < n) ok = slopes(h + 1);
             }
-            __syncwarp();
-            if (h + 1 < n) ok = slopes(h + 1);
-        }
-        if (elect_one()) {
             mma_commit(done);
             mbar_wait(done, 0);
         }
@@ -325,8 +312,9 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
     unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + KS, *v_full = k_empty + KS, *v_empty = v_full + VS;
     unsigned long long *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_ready = dp_full + 1, *done = ds_ready + 1;
-    volatile int *give_up = reinterpret_cast<int *>(done + 1);
-    unsigned *tmem_cell = reinterpret_cast<unsigned *>(done + 2);
+    unsigned long long *own = done + 1;
+    volatile int *give_up = reinterpret_cast<int *>(own + 1);
+    unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Place at_tile = place_of(p.s.heads, p.s.batch);
@@ -343,7 +331,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
         for (int i = 0; i < VS; ++i) { mbar_init(v_full + i, 1); mbar_init(v_empty + i, 1); }
         mbar_init(s_full, 1); mbar_init(s_full + 1, 1);
         mbar_init(dp_full, 1); mbar_init(ds_ready, kElementWarps);
-        mbar_init(done, 1);
+        mbar_init(done, 1); mbar_init(own, 1);
         *give_up = 0;
         fence_barrier_init();
     }
@@ -355,21 +343,24 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     const unsigned dq_at = tmem, s_at = tmem + DP, dp_at = s_at + 2 * kRows;
 
     if (warp == kLoadWarp) {
-        if (lane == 0 && n > 0) {
-            prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
-            mbar_expect_tx(q_full, 2 * L::kTile);
-            load_tile<DP, kRows>(smem + L::kQ, &p.q, head, q0, b, q_full);
+        if (n > 0) {
+            Loader load = {own, 0, give_up, p.status};
+            if (lane == 0) {
+                prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
+                mbar_expect_tx(q_full, 2 * L::kTile);
+                load_tile<DP, kRows>(smem + L::kQ, &p.q, head, q0, b, q_full);
+                load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
+            }
             int k_armed = 0, v_armed = 0;
             for (int h = 0; h < n; ++h) {
                 const int ks = h % KS, vs = h % VS;
-                if (!bounded_wait(k_empty + ks, ((h / KS) & 1) ^ 1, give_up, p.status)) break;
-                mbar_expect_tx(k_full + ks, L::kTile);
-                load_tile<DP, kRows>(smem + L::kK + ks * L::kTile, &p.k, kv_head, h * kRows, b, k_full + ks);
+                if (!load.wait(k_empty + ks, ((h / KS) & 1) ^ 1)) break;
+                if (!load.tile<DP>(smem + L::kK + ks * L::kTile, &p.k, kv_head, h * kRows, b, k_full + ks,
+                                   p.s.kv_lengths ? len.kv - h * kRows : kRows))
+                    break;
                 ++k_armed;
-                if (h == 0) load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
-                if (!bounded_wait(v_empty + vs, ((h / VS) & 1) ^ 1, give_up, p.status)) break;
-                mbar_expect_tx(v_full + vs, L::kTile);
-                load_tile<DP, kRows>(smem + L::kV + vs * L::kTile, &p.v, kv_head, h * kRows, b, v_full + vs);
+                if (!load.wait(v_empty + vs, ((h / VS) & 1) ^ 1)) break;
+                load.tile<DP>(smem + L::kV + vs * L::kTile, &p.v, kv_head, h * kRows, b, v_full + vs, kRows);
                 ++v_armed;
             }
             mbar_wait(q_full, 0);
@@ -378,49 +369,37 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
         }
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        const unsigned q = smem_addr(smem + L::kQ), d = smem_addr(smem + L::kDo);
-        const unsigned k0 = smem_addr(smem + L::kK), v0 = smem_addr(smem + L::kV);
-        bool ok = n == 0 || warp_wait(q_full, 0, give_up, p.status);
-        auto scores = [&](int h) {
-            const int st = h % KS;
-            if (!warp_wait(k_full + st, (h / KS) & 1, give_up, p.status)) return false;
-            if (p.s.kv_lengths && len.kv - h * kRows < kRows) zero_rows<DP, kRows>(smem + L::kK + st * L::kTile, len.kv - h * kRows);
-            fence_after_sync();
-            if (elect_one()) {
+        if (elect_one()) {
+            const unsigned q = smem_addr(smem + L::kQ), d = smem_addr(smem + L::kDo);
+            const unsigned k0 = smem_addr(smem + L::kK), v0 = smem_addr(smem + L::kV);
+            auto wait = [&](unsigned long long *bar, unsigned parity) { return bounded_wait(bar, parity, give_up, p.status); };
+            auto scores = [&](int h) {
+                const int st = h % KS;
+                if (!wait(k_full + st, (h / KS) & 1)) return false;
+                fence_after_sync();
                 mma_along<DP, kRows, kRows, kRows>(s_at + (h & 1) * kRows, q, k0 + st * L::kTile, false);
                 mma_commit(s_full + (h & 1));
-            }
-            __syncwarp();
-            return true;
-        };
-        auto slopes = [&](int h) {
-            const int st = h % VS;
-            if (!warp_wait(v_full + st, (h / VS) & 1, give_up, p.status)) return false;
-            fence_after_sync();
-            if (elect_one()) {
+                return true;
+            };
+            auto slopes = [&](int h) {
+                const int st = h % VS;
+                if (!wait(v_full + st, (h / VS) & 1)) return false;
+                fence_after_sync();
                 mma_along<DP, kRows, kRows, kRows>(dp_at, d, v0 + st * L::kTile, false);
                 mma_commit(dp_full);
                 mma_commit(v_empty + st);
-            }
-            __syncwarp();
-            return true;
-        };
-        if (n > 0) ok = ok && scores(0) && slopes(0);
-        if (n > 1) ok = ok && scores(1);
-        for (int h = 0; h < n && ok; ++h) {
-            const int st = h % KS;
-            ok = warp_wait(ds_ready, h & 1, give_up, p.status);
-            if (!ok) break;
-            fence_after_sync();
-            if (elect_one()) {
+                return true;
+            };
+            bool ok = n > 0 && wait(q_full, 0) && scores(0) && slopes(0) && (n < 2 || scores(1));
+            for (int h = 0; h < n && ok; ++h) {
+                const int st = h % KS;
+                if (!(ok = wait(ds_ready, h & 1))) break;
+                fence_after_sync();
                 mma_tmem_across<DP, kRows, kRows, kCols>(dq_at, s_at + (h & 1) * kRows, k0 + st * L::kTile, h > 0);
                 mma_commit(k_empty + st);
+                if (h + 1 < n) ok = slopes(h + 1);
+                if (ok && h + 2 < n) ok = scores(h + 2);
             }
-            __syncwarp();
-            if (h + 1 < n) ok = slopes(h + 1);
-            if (ok && h + 2 < n) ok = scores(h + 2);
-        }
-        if (elect_one()) {
             mma_commit(done);
             mbar_wait(done, 0);
         }

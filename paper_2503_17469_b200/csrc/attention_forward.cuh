@@ -45,9 +45,9 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
     unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST;
-    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 4, *drained = o_full + 2;
-    volatile int *give_up = reinterpret_cast<int *>(drained + 1);
-    unsigned *tmem_cell = reinterpret_cast<unsigned *>(drained + 2);
+    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 4, *drained = o_full + 2, *own = drained + 1;
+    volatile int *give_up = reinterpret_cast<int *>(own + 1);
+    unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const Place at = place_of(p.s.heads, p.s.batch);
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
         }
         for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(o_full + t, 1); }
         for (int i = 0; i < 4; ++i) mbar_init(p_ready + i, 4);        // [tile][half]
-        mbar_init(drained, 1);
+        mbar_init(drained, 1); mbar_init(own, 1);
         *give_up = 0;
         fence_barrier_init();
     }
@@ -85,86 +85,77 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     const unsigned s_at = tmem, o_at = tmem + 2 * kRows;             // S0 S1 | O0 O1
 
     if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kForwardFew));
-    if (warp == 8) {
-        if (lane == 0 && n > 0) {
-            prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v);
-            const int q_tiles = tiles[1] > 0 ? 2 : 1;
-            mbar_expect_tx(q_full, q_tiles * L::kTile);
-            for (int t = 0; t < q_tiles; ++t) load_tile<DP, kRows>(smem + L::kQ + t * L::kTile, &p.q, head, q0 + t * kRows, b, q_full);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kForwardFew));
+        if (warp == 8 && n > 0) {
+            Loader load = {own, 0, give_up, p.status};
+            if (lane == 0) {
+                prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v);
+                const int q_tiles = tiles[1] > 0 ? 2 : 1;
+                mbar_expect_tx(q_full, q_tiles * L::kTile);
+                for (int t = 0; t < q_tiles; ++t) load_tile<DP, kRows>(smem + L::kQ + t * L::kTile, &p.q, head, q0 + t * kRows, b, q_full);
+            }
             int kj = 0, vj = 0;                                       // copies armed
             for (int j = 0; j < n; ++j) {
                 const int st = j % ST;
                 const unsigned free_parity = ((j / ST) & 1) ^ 1;
-                if (!bounded_wait(k_empty + st, free_parity, give_up, p.status)) break;
-                mbar_expect_tx(k_full + st, L::kTile);
-                load_tile<DP, kRows>(smem + L::kK + st * L::kTile, &p.k, kv_head, j * kRows, b, k_full + st);
+                if (!load.wait(k_empty + st, free_parity)) break;
+                load.tile<DP>(smem + L::kK + st * L::kTile, &p.k, kv_head, j * kRows, b, k_full + st, kRows);
                 ++kj;
-                if (!bounded_wait(v_empty + st, free_parity, give_up, p.status)) break;
-                mbar_expect_tx(v_full + st, L::kTile);
-                load_tile<DP, kRows>(smem + L::kV + st * L::kTile, &p.v, kv_head, j * kRows, b, v_full + st);
+                if (!load.wait(v_empty + st, free_parity)) break;
+                if (!load.tile<DP>(smem + L::kV + st * L::kTile, &p.v, kv_head, j * kRows, b, v_full + st,
+                                   p.s.kv_lengths ? len.kv - j * kRows : kRows))
+                    break;
                 ++vj;
             }
             // the block may not end with a copy in flight, not even when it gave up
             mbar_wait(q_full, 0);
             for (int j = max(0, kj - ST); j < kj; ++j) mbar_wait(k_full + j % ST, (j / ST) & 1);
             for (int j = max(0, vj - ST); j < vj; ++j) mbar_wait(v_full + j % ST, (j / ST) & 1);
-        }
-        __syncwarp();
-    } else if (warp == 9) {
-        bool ok = n == 0 || warp_wait(q_full, 0, give_up, p.status);
-        if (n > 0 && ok) ok = warp_wait(k_full, 0, give_up, p.status);
-        const unsigned q = smem_addr(smem + L::kQ), k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
-        fence_after_sync();
-        if (ok && elect_one()) {
-            for (int t = 0; t < 2; ++t)
-                if (tiles[t] > 0) {
-                    mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k, false);
-                    mma_commit(s_full + t);
-                }
-            if (n > 0) mma_commit(k_empty);
-        }
-        __syncwarp();
-        for (int j = 0; j < n && ok; ++j) {
-            const int st = j % ST, next = (j + 1) % ST;
-            ok = warp_wait(v_full + st, (j / ST) & 1, give_up, p.status);
-            if (ok && p.s.kv_lengths && len.kv - j * kRows < kRows) zero_rows<DP, kRows>(smem + L::kV + st * L::kTile, len.kv - j * kRows);
-            if (ok && j + 1 < n) ok = warp_wait(k_full + next, ((j + 1) / ST) & 1, give_up, p.status);
+        } else if (warp == 9 && elect_one()) {
+            const unsigned q = smem_addr(smem + L::kQ), k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
+            auto wait = [&](unsigned long long *bar, unsigned parity) { return bounded_wait(bar, parity, give_up, p.status); };
+            bool ok = n == 0 || (wait(q_full, 0) && wait(k_full, 0));
+            fence_after_sync();
+            if (ok && n > 0) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                if (!ok || j >= tiles[t]) continue;
+                for (int t = 0; t < 2; ++t)
+                    if (tiles[t] > 0) {
+                        mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k, false);
+                        mma_commit(s_full + t);
+                    }
+                mma_commit(k_empty);
+            }
+            for (int j = 0; j < n && ok; ++j) {
+                const int st = j % ST, next = (j + 1) % ST;
+                ok = wait(v_full + st, (j / ST) & 1) && (j + 1 >= n || wait(k_full + next, ((j + 1) / ST) & 1));
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    ok = ok && warp_wait(p_ready + 2 * t + half, j & 1, give_up, p.status);
-                    fence_after_sync();
-                    if (ok && elect_one()) {
+                for (int t = 0; t < 2; ++t) {
+                    if (j >= tiles[t]) continue;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        ok = ok && wait(p_ready + 2 * t + half, j & 1);
+                        if (!ok) break;
+                        fence_after_sync();
                         mma_tmem_across<DP, kRows, 64, 64>(o_at + t * DP, s_at + t * kRows + half * 32, v + st * L::kTile + half * 64 * 128,
                                                            j > 0 || half > 0);
-                        if (half == 1) {
-                            // the next scores go over P: the tensor core takes MMAs in order
-                            if (j + 1 < tiles[t]) {
-                                mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
-                                mma_commit(s_full + t);
-                            } else {
-                                mma_commit(o_full + t);
-                            }
-                        }
                     }
-                    __syncwarp();
+                    if (!ok) break;
+                    // the next scores go over P: the tensor core takes MMAs in order
+                    if (j + 1 < tiles[t]) {
+                        mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
+                        mma_commit(s_full + t);
+                    } else {
+                        mma_commit(o_full + t);
+                    }
                 }
-            }
-            if (ok && elect_one()) {
+                if (!ok) break;
                 if (j + 1 < n) mma_commit(k_empty + next);
                 mma_commit(v_empty + st);
             }
-            __syncwarp();
-        }
-        if (elect_one()) {
             mma_commit(drained);
             mbar_wait(drained, 0);
         }
         __syncwarp();
-    }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kForwardMany));
         const int t = warp / 4, row = threadIdx.x % kRows, i = q0 + t * kRows + row;
