@@ -56,7 +56,7 @@ int check_shape(const omni_attn *a)
     if (a->dim > OMNI_ATTN_MAX_DIM || a->batch > 65535 || a->heads > 65535 || a->q_len > (1 << 30) || a->kv_len > (1 << 30))
         return OMNI_ERR_TOO_LARGE;
     const int64_t rows = a->q_len > a->kv_len ? a->q_len : a->kv_len;
-    if ((rows / kRows + 1) * a->heads * a->batch >= (1ll << 31)) return OMNI_ERR_TOO_LARGE;      // CTAs of a launch
+    if ((rows / kRows + 1) * a->heads * a->batch >= (1ll << 30)) return OMNI_ERR_TOO_LARGE;      // blocks of a launch
     if (!aligned(a->q_lengths, 4) || !aligned(a->kv_lengths, 4)) return OMNI_ERR_ALIGN;
     return OMNI_OK;
 }
@@ -202,17 +202,10 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
         for (const auto &m : maps)
             if ((rc = make_map(ctx, encode, m.map, *m.view, a->dim, m.heads, m.len, a->batch)) != OMNI_OK) return rc;
     }
-    if (a->kv_len > 0) {
-        const dim3 grid(unsigned((a->kv_len + kRows - 1) / kRows) * a->kv_heads * a->batch);
-        rc = a->dim <= 64 ? launch(ctx, attention_keys_kernel<64>, grid, kBackwardThreads, KeysShared<64>::kBytes, s, p)
-                          : launch(ctx, attention_keys_kernel<128>, grid, kBackwardThreads, KeysShared<128>::kBytes, s, p);
-        if (rc != OMNI_OK) return rc;
-    }
-    if (a->q_len > 0) {
-        const dim3 grid(unsigned(p.q_tiles) * a->heads * a->batch);
-        rc = a->dim <= 64 ? launch(ctx, attention_queries_kernel<64>, grid, kBackwardThreads, QueriesShared<64>::kBytes, s, p)
-                          : launch(ctx, attention_queries_kernel<128>, grid, kBackwardThreads, QueriesShared<128>::kBytes, s, p);
-    }
+    p.key_blocks = (a->kv_len + kRows - 1) / kRows * a->kv_heads * a->batch;
+    const dim3 grid(unsigned(p.key_blocks) + unsigned(p.q_tiles) * a->heads * a->batch);
+    rc = a->dim <= 64 ? launch(ctx, attention_backward_kernel<64>, grid, kBackwardThreads, BackwardShared<64>::kBytes, s, p)
+                      : launch(ctx, attention_backward_kernel<128>, grid, kBackwardThreads, BackwardShared<128>::kBytes, s, p);
     return rc;
 }
 

@@ -28,13 +28,13 @@ __device__ __forceinline__ Lengths lengths_of(const AttnShape &s, int b)
     return l;
 }
 
-// Which tile of rows of which head and sequence a CTA has.  Tiles are the slowest index, so that the
+// Which tile of rows of which head and sequence a block has.  Tiles are the slowest index, so that the
 // longest ones of a causal mask (tile 0 here) of all heads come first and the short ones fill the end.
 struct Place { int tile, head, batch; };
-__device__ __forceinline__ Place place_of(int heads, int batch)
+__device__ __forceinline__ Place place_of(int block, int heads, int batch)
 {
-    const int per = heads * batch, rest = int(blockIdx.x) % per;
-    return {int(blockIdx.x) / per, rest % heads, rest / heads};
+    const int per = heads * batch, rest = block % per;
+    return {block / per, rest % heads, rest / heads};
 }
 
 struct OutView { __nv_bfloat16 *data; long long batch, row, head; };

@@ -6,7 +6,7 @@
 // tile, which adds up dQ over the keys.  Seven products instead of five, but every sum has one owner and one order:
 // no float atomics, no zeroed and re-read dQ in float, the same bits from the same call.
 //
-// Both kernels walk 128 x 128 tiles of S and dP in tensor memory.  (64 columns a tile would leave room for two of each,
+// Both walk 128 x 128 tiles of S and dP in tensor memory.  (64 columns a tile would leave room for two of each,
 // but an MMA of M = 128 with both operands in shared memory takes about 75 cycles, N = 64 or 128.)  The
 // elementwise work comes in two phases, P from S and dS from P and dP, sixteen warps at 32 columns of a row per thread,
 // and each phase runs beside products of the same or the next tile:
@@ -34,6 +34,7 @@ struct AttnBackwardParams {
     AttnShape s;
     const float *row_lse, *row_delta;   // [batch * heads][q_pad]: -L in powers of two (-inf: no row), -D
     int q_pad, q_tiles;
+    int key_blocks;                 // blocks that own keys; the others own queries
     OutView dq, dk, dv;
     unsigned *status;
 };
@@ -84,8 +85,7 @@ template <int DP> struct KeysShared {
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
-template <int DP>
-__global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(const __grid_constant__ AttnBackwardParams p)
+template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackwardParams &p, int block)
 {
     using L = KeysShared<DP>;
     constexpr int ST = L::kStages;
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_keys_kernel(con
     const float *stats = reinterpret_cast<const float *>(smem + L::kStats);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Place at_tile = place_of(p.s.kv_heads, p.s.batch);
+    const Place at_tile = place_of(block, p.s.kv_heads, p.s.batch);
     const int kv_head = at_tile.head, b = at_tile.batch, group = p.s.heads / p.s.kv_heads;
     const int k0 = at_tile.tile * kRows;
     const Lengths len = lengths_of(p.s, b);
@@ -302,8 +302,7 @@ template <int DP> struct QueriesShared {
     static_assert(kBytes <= 227 * 1024, "shared memory of a block");
 };
 
-template <int DP>
-__global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(const __grid_constant__ AttnBackwardParams p)
+template <int DP> __device__ __forceinline__ void attention_queries(const AttnBackwardParams &p, int block)
 {
     using L = QueriesShared<DP>;
     constexpr int KS = L::kKStages, VS = L::kVStages;
@@ -317,7 +316,7 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Place at_tile = place_of(p.s.heads, p.s.batch);
+    const Place at_tile = place_of(block, p.s.heads, p.s.batch);
     const int head = at_tile.head, b = at_tile.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
     const int q0 = (p.q_tiles - 1 - at_tile.tile) * kRows;
     const Lengths len = lengths_of(p.s, b);
@@ -463,5 +462,16 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_queries_kernel(
     __syncthreads();
     if (warp == kMmaWarp) tmem_free(tmem, 512);
 }
+
+// Both in one launch: neither waits for the other, and the shorter blocks of dQ fill the SMs that the last of dK, dV leave.
+template <int DP>
+__global__ void __launch_bounds__(kBackwardThreads, 1) attention_backward_kernel(const __grid_constant__ AttnBackwardParams p)
+{
+    if (int(blockIdx.x) < p.key_blocks) attention_keys<DP>(p, int(blockIdx.x));
+    else attention_queries<DP>(p, int(blockIdx.x) - p.key_blocks);
+}
+template <int DP> struct BackwardShared {
+    static constexpr int kBytes = KeysShared<DP>::kBytes > QueriesShared<DP>::kBytes ? KeysShared<DP>::kBytes : QueriesShared<DP>::kBytes;
+};
 
 }  // namespace omni

@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Place at = place_of(p.s.heads, p.s.batch);
+    const Place at = place_of(int(blockIdx.x), p.s.heads, p.s.batch);
     const int head = at.head, b = at.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
     const int q0 = (p.q_tiles - 1 - at.tile) * 2 * kRows;
     const Lengths len = lengths_of(p.s, b);
