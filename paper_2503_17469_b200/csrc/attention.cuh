@@ -159,4 +159,13 @@ __device__ __forceinline__ void store_zeros(__nv_bfloat16 *dst, int dim)
     for (int c = 0; c < dim; c += 8) *reinterpret_cast<uint4 *>(dst + c) = make_uint4(0, 0, 0, 0);
 }
 
+// `rows` rows from `row` on set to zero by the whole block.
+__device__ __forceinline__ void zero_tile(const OutView &o, int batch, int head, int row, int rows, int dim)
+{
+    const int groups = dim / 8;
+    for (int i = threadIdx.x; i < rows * groups; i += blockDim.x)
+        *reinterpret_cast<uint4 *>(o.data + batch * o.batch + (long long)(row + i / groups) * o.row + head * o.head + i % groups * 8) =
+            make_uint4(0, 0, 0, 0);
+}
+
 }  // namespace omni

@@ -110,6 +110,11 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
     const int tile0 = first_row / kRows;
     const int tiles = k0 < len.kv && first_row < len.q ? (len.q + kRows - 1) / kRows - tile0 : 0;
     const int n = tiles * group;                                    // (query head, tile) one after the other
+    if (n == 0) {                                                   // no query sees these keys
+        zero_tile(p.dk, b, kv_head, k0, min(kRows, p.s.kv_len - k0), p.s.dim);
+        zero_tile(p.dv, b, kv_head, k0, min(kRows, p.s.kv_len - k0), p.s.dim);
+        return;
+    }
 
     if (threadIdx.x == 0) {
         mbar_init(kv_full, 1);
@@ -131,38 +136,36 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
     const unsigned dv_at = tmem, dk_at = tmem + DP, s_at = tmem + 2 * DP, dp_at = s_at + kRows;
 
     if (warp == kLoadWarp) {
-        if (n > 0) {
-            Loader load = {own, 0, give_up, p.status};
-            if (lane == 0) {
-                prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
-                mbar_expect_tx(kv_full, 2 * L::kTile);
-                load_tile<DP, kRows>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
-                load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
-            }
-            int q_armed = 0, do_armed = 0;
-            const unsigned long long policy = policy_evict_last();
-            for (int h = 0; h < n; ++h) {
-                const int st = h % ST, head = kv_head * group + h / tiles, row = (tile0 + h % tiles) * kRows;
-                const int valid = p.s.q_lengths ? len.q - row : kRows;
-                const unsigned free_parity = ((h / ST) & 1) ^ 1;
-                if (!load.wait(q_empty + st, free_parity)) break;
-                if (!load.tile<DP>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st, valid, 2 * kRows * 4)) break;
-                if (lane == 0) {
-                    const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
-                    float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kRows;
-                    bulk_load(to, p.row_lse + at, kRows * 4, q_full + st, policy);
-                    bulk_load(to + kRows, p.row_delta + at, kRows * 4, q_full + st, policy);
-                }
-                ++q_armed;
-                if (!load.wait(do_empty + st, free_parity)) break;
-                if (!load.tile<DP>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st, valid)) break;
-                ++do_armed;
-            }
-            // the block may not end with a copy in flight, not even when it gave up
-            mbar_wait(kv_full, 0);
-            for (int h = max(0, q_armed - ST); h < q_armed; ++h) mbar_wait(q_full + h % ST, (h / ST) & 1);
-            for (int h = max(0, do_armed - ST); h < do_armed; ++h) mbar_wait(do_full + h % ST, (h / ST) & 1);
+        Loader load = {own, 0, give_up, p.status};
+        if (lane == 0) {
+            prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
+            mbar_expect_tx(kv_full, 2 * L::kTile);
+            load_tile<DP, kRows>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
+            load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
         }
+        int q_armed = 0, do_armed = 0;
+        const unsigned long long policy = policy_evict_last();
+        for (int h = 0; h < n; ++h) {
+            const int st = h % ST, head = kv_head * group + h / tiles, row = (tile0 + h % tiles) * kRows;
+            const int valid = p.s.q_lengths ? len.q - row : kRows;
+            const unsigned free_parity = ((h / ST) & 1) ^ 1;
+            if (!load.wait(q_empty + st, free_parity)) break;
+            if (!load.tile<DP>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st, valid, 2 * kRows * 4)) break;
+            if (lane == 0) {
+                const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
+                float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kRows;
+                bulk_load(to, p.row_lse + at, kRows * 4, q_full + st, policy);
+                bulk_load(to + kRows, p.row_delta + at, kRows * 4, q_full + st, policy);
+            }
+            ++q_armed;
+            if (!load.wait(do_empty + st, free_parity)) break;
+            if (!load.tile<DP>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st, valid)) break;
+            ++do_armed;
+        }
+        // the block may not end with a copy in flight, not even when it gave up
+        mbar_wait(kv_full, 0);
+        for (int h = max(0, q_armed - ST); h < q_armed; ++h) mbar_wait(q_full + h % ST, (h / ST) & 1);
+        for (int h = max(0, do_armed - ST); h < do_armed; ++h) mbar_wait(do_full + h % ST, (h / ST) & 1);
         __syncwarp();
     } else if (warp == kMmaWarp) {
         if (elect_one()) {
@@ -185,7 +188,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
                 mma_commit(dp_full);
                 return true;
             };
-            bool ok = n > 0 && wait(kv_full, 0) && scores(0) && slopes(0);
+            bool ok = wait(kv_full, 0) && scores(0) && slopes(0);
             for (int h = 0; h < n && ok; ++h) {
                 const int st = h % ST;
                 if (!(ok = wait(p_ready, h & 1))) break;
@@ -273,7 +276,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
             if (lane == 0) mbar_arrive(ds_ready);
         }
         // warps 0-7 write dV, warps 8-15 dK, half of the columns each four
-        if (n > 0 && ok) ok = warp_wait(done, 0, give_up, p.status);
+        if (ok) ok = warp_wait(done, 0, give_up, p.status);
         ok = __all_sync(~0u, ok && *give_up == 0);
         fence_after_sync();
         const bool values = warp < 8;
@@ -281,10 +284,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         const int half = warp / 4 % 2, d0 = half * (DP / 2);
         __nv_bfloat16 *dst = o.data + b * o.batch + (long long)j * o.row + kv_head * o.head;
         const bool mine = ok && j < p.s.kv_len;
-        if (n > 0 && ok)
-            store_row<DP / 2>((values ? dv_at : dk_at) + lanes + d0, values ? 1.0f : p.s.scale, dst + d0, p.s.dim - d0, mine);
-        else if (mine && half == 0)
-            store_zeros(dst, p.s.dim);
+        if (ok) store_row<DP / 2>((values ? dv_at : dk_at) + lanes + d0, values ? 1.0f : p.s.scale, dst + d0, p.s.dim - d0, mine);
     }
     fence_before_sync();
     __syncthreads();
@@ -323,6 +323,10 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
     const int last = min(q0 + kRows, len.q) - 1;
     const int seen = last < q0 ? 0 : p.s.causal ? min(len.kv, last + len.shift + 1) : len.kv;
     const int n = seen > 0 ? (seen + kRows - 1) / kRows : 0;
+    if (n == 0) {                                                   // no query of the tile sees a key
+        zero_tile(p.dq, b, head, q0, min(kRows, p.s.q_len - q0), p.s.dim);
+        return;
+    }
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
@@ -342,30 +346,28 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
     const unsigned dq_at = tmem, s_at = tmem + DP, dp_at = s_at + 2 * kRows;
 
     if (warp == kLoadWarp) {
-        if (n > 0) {
-            Loader load = {own, 0, give_up, p.status};
-            if (lane == 0) {
-                prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
-                mbar_expect_tx(q_full, 2 * L::kTile);
-                load_tile<DP, kRows>(smem + L::kQ, &p.q, head, q0, b, q_full);
-                load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
-            }
-            int k_armed = 0, v_armed = 0;
-            for (int h = 0; h < n; ++h) {
-                const int ks = h % KS, vs = h % VS;
-                if (!load.wait(k_empty + ks, ((h / KS) & 1) ^ 1)) break;
-                if (!load.tile<DP>(smem + L::kK + ks * L::kTile, &p.k, kv_head, h * kRows, b, k_full + ks,
-                                   p.s.kv_lengths ? len.kv - h * kRows : kRows))
-                    break;
-                ++k_armed;
-                if (!load.wait(v_empty + vs, ((h / VS) & 1) ^ 1)) break;
-                load.tile<DP>(smem + L::kV + vs * L::kTile, &p.v, kv_head, h * kRows, b, v_full + vs, kRows);
-                ++v_armed;
-            }
-            mbar_wait(q_full, 0);
-            for (int h = max(0, k_armed - KS); h < k_armed; ++h) mbar_wait(k_full + h % KS, (h / KS) & 1);
-            for (int h = max(0, v_armed - VS); h < v_armed; ++h) mbar_wait(v_full + h % VS, (h / VS) & 1);
+        Loader load = {own, 0, give_up, p.status};
+        if (lane == 0) {
+            prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
+            mbar_expect_tx(q_full, 2 * L::kTile);
+            load_tile<DP, kRows>(smem + L::kQ, &p.q, head, q0, b, q_full);
+            load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
         }
+        int k_armed = 0, v_armed = 0;
+        for (int h = 0; h < n; ++h) {
+            const int ks = h % KS, vs = h % VS;
+            if (!load.wait(k_empty + ks, ((h / KS) & 1) ^ 1)) break;
+            if (!load.tile<DP>(smem + L::kK + ks * L::kTile, &p.k, kv_head, h * kRows, b, k_full + ks,
+                               p.s.kv_lengths ? len.kv - h * kRows : kRows))
+                break;
+            ++k_armed;
+            if (!load.wait(v_empty + vs, ((h / VS) & 1) ^ 1)) break;
+            load.tile<DP>(smem + L::kV + vs * L::kTile, &p.v, kv_head, h * kRows, b, v_full + vs, kRows);
+            ++v_armed;
+        }
+        mbar_wait(q_full, 0);
+        for (int h = max(0, k_armed - KS); h < k_armed; ++h) mbar_wait(k_full + h % KS, (h / KS) & 1);
+        for (int h = max(0, v_armed - VS); h < v_armed; ++h) mbar_wait(v_full + h % VS, (h / VS) & 1);
         __syncwarp();
     } else if (warp == kMmaWarp) {
         if (elect_one()) {
@@ -389,7 +391,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
                 mma_commit(v_empty + st);
                 return true;
             };
-            bool ok = n > 0 && wait(q_full, 0) && scores(0) && slopes(0) && (n < 2 || scores(1));
+            bool ok = wait(q_full, 0) && scores(0) && slopes(0) && (n < 2 || scores(1));
             for (int h = 0; h < n && ok; ++h) {
                 const int st = h % KS;
                 if (!(ok = wait(ds_ready, h & 1))) break;
@@ -448,14 +450,14 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
             __syncwarp();
             if (lane == 0) mbar_arrive(ds_ready);
         }
-        if (n > 0 && ok) ok = warp_wait(done, 0, give_up, p.status);
+        if (ok) ok = warp_wait(done, 0, give_up, p.status);
         ok = __all_sync(~0u, ok && *give_up == 0);
         fence_after_sync();
         // every four warps a quarter of the columns
         const int d0 = warp / 4 * (DP / 4);
         __nv_bfloat16 *dst = p.dq.data + b * p.dq.batch + (long long)i * p.dq.row + head * p.dq.head;
         const bool mine = ok && i < p.s.q_len, empty = limit <= 0;
-        if (n > 0 && ok) store_row<DP / 4>(dq_at + lanes + d0, p.s.scale, dst + d0, p.s.dim - d0, mine && !empty);
+        if (ok) store_row<DP / 4>(dq_at + lanes + d0, p.s.scale, dst + d0, p.s.dim - d0, mine && !empty);
         if (d0 == 0 && mine && empty) store_zeros(dst, p.s.dim);
     }
     fence_before_sync();

@@ -64,6 +64,12 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
         tiles[t] = seen > 0 ? (seen + kRows - 1) / kRows : 0;
     }
     const int n = max(tiles[0], tiles[1]);
+    if (n == 0) {                                                     // no row sees a key
+        const int rows = min(2 * kRows, p.s.q_len - q0);
+        zero_tile(p.out, b, head, q0, rows, p.s.dim);
+        for (int i = threadIdx.x; i < rows; i += blockDim.x) p.lse[((long long)b * p.s.heads + head) * p.s.q_len + q0 + i] = -INFINITY;
+        return;
+    }
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
@@ -86,7 +92,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kForwardFew));
-        if (warp == 8 && n > 0) {
+        if (warp == 8) {
             Loader load = {own, 0, give_up, p.status};
             if (lane == 0) {
                 prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v);
@@ -114,9 +120,9 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
         } else if (warp == 9 && elect_one()) {
             const unsigned q = smem_addr(smem + L::kQ), k = smem_addr(smem + L::kK), v = smem_addr(smem + L::kV);
             auto wait = [&](unsigned long long *bar, unsigned parity) { return bounded_wait(bar, parity, give_up, p.status); };
-            bool ok = n == 0 || (wait(q_full, 0) && wait(k_full, 0));
+            bool ok = wait(q_full, 0) && wait(k_full, 0);
             fence_after_sync();
-            if (ok && n > 0) {
+            if (ok) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (tiles[t] > 0) {
