@@ -89,12 +89,17 @@ OutView out_of(const omni_attn_view *v)
 }
 
 // One launch of a kernel that takes its parameter block by value, with its shared memory opted in.
-template <typename P> int launch(omni_ctx *ctx, void (*kernel)(P), dim3 grid, int threads, int smem, cudaStream_t s, const P &p)
+// `after`: it begins while the call's previous kernel ends.
+template <typename P>
+int launch(omni_ctx *ctx, void (*kernel)(P), dim3 grid, int threads, int smem, cudaStream_t s, const P &p, const ContextDevice *after = nullptr)
 {
-    int rc = context_shared(ctx, reinterpret_cast<const void *>(kernel), smem);
+    const void *fn = reinterpret_cast<const void *>(kernel);
+    int rc = context_shared(ctx, fn, smem);
     if (rc != OMNI_OK) return rc;
     void *args[] = {const_cast<P *>(&p)};
-    return context_launched(ctx, int(cudaLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(threads), args, smem, s)));
+    if (!after) return context_launched(ctx, int(cudaLaunchKernel(fn, grid, dim3(threads), args, smem, s)));
+    const Dependent d(*after, grid, threads, smem, s);
+    return context_launched(ctx, int(cudaLaunchKernelExC(&d.cfg, fn, args)));
 }
 
 int q_pad_of(const omni_attn *a) { return int(round_up(uint64_t(a->q_len), kRows)); }
@@ -189,7 +194,7 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
     p.status = dev.status;
     if (a->q_len > 0) {
         const AttnRowsParams r = {p.s, out_of(out), out_of(dout), lse, const_cast<float *>(p.row_lse),
-                                  const_cast<float *>(p.row_delta), q_pad};
+                                  const_cast<float *>(p.row_delta), q_pad, dev.overlap};
         rc = launch(ctx, attention_rows_kernel, dim3(q_pad / 16, a->heads, a->batch), 256, 0, s, r);
         if (rc != OMNI_OK) return rc;
     }
@@ -204,8 +209,8 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
     }
     p.key_blocks = (a->kv_len + kRows - 1) / kRows * a->kv_heads * a->batch;
     const dim3 grid(unsigned(p.key_blocks) + unsigned(p.q_tiles) * a->heads * a->batch);
-    rc = a->dim <= 64 ? launch(ctx, attention_backward_kernel<64>, grid, kBackwardThreads, BackwardShared<64>::kBytes, s, p)
-                      : launch(ctx, attention_backward_kernel<128>, grid, kBackwardThreads, BackwardShared<128>::kBytes, s, p);
+    rc = a->dim <= 64 ? launch(ctx, attention_backward_kernel<64>, grid, kBackwardThreads, BackwardShared<64>::kBytes, s, p, a->q_len > 0 ? &dev : nullptr)
+                      : launch(ctx, attention_backward_kernel<128>, grid, kBackwardThreads, BackwardShared<128>::kBytes, s, p, a->q_len > 0 ? &dev : nullptr);
     return rc;
 }
 

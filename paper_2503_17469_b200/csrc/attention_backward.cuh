@@ -45,12 +45,14 @@ struct AttnRowsParams {
     const float *lse;
     float *row_lse, *row_delta;
     int q_pad;
+    bool overlap;                   // the next kernel may begin early
 };
 
 // -D and minus the log-sum-exp in powers of two, for every query row and the padding up to whole tiles.
 // 16 lanes a row.  Reads O and dO once.
 __global__ void __launch_bounds__(256) attention_rows_kernel(const AttnRowsParams p)
 {
+    let_next_begin(p.overlap);
     const int lane = threadIdx.x % 16, i = blockIdx.x * 16 + threadIdx.x / 16, head = blockIdx.y, b = blockIdx.z;
     const int q_length = p.s.q_lengths ? min(max(p.s.q_lengths[b], 0), p.s.q_len) : p.s.q_len;
     float sum = 0.0f;
@@ -152,6 +154,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
             if (!load.wait(q_empty + st, free_parity)) break;
             if (!load.tile<DP>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st, valid, 2 * kRows * 4)) break;
             if (lane == 0) {
+                if (h == 0) wait_for_previous();                   // the row values are the previous kernel's
                 const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
                 float *to = reinterpret_cast<float *>(smem + L::kStats) + st * 2 * kRows;
                 bulk_load(to, p.row_lse + at, kRows * 4, q_full + st, policy);
@@ -412,6 +415,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
         const float2 unit = {p.s.scale * kAttnLog2e, p.s.scale * kAttnLog2e};
         const int limit = i >= len.q ? 0 : p.s.causal ? min(len.kv, i + len.shift + 1) : len.kv;
         const long long at = ((long long)b * p.s.heads + head) * p.q_pad + i;
+        wait_for_previous();                                        // the row values are the previous kernel's
         const float2 lse = {p.row_lse[at], p.row_lse[at]}, delta = {p.row_delta[at], p.row_delta[at]};
         bool ok = true;
         for (int h = 0; h < n; ++h) {

@@ -296,6 +296,7 @@ int context_bind(omni_ctx *ctx, ContextDevice *out)
     const int rc = ensure_device(ctx);
     if (rc != OMNI_OK) return rc;
     out->sm_count = ctx->sm_count;
+    out->overlap = !(ctx->ctl.config().flags & OMNI_NO_BULK_COPY);
     out->status = &ctx->ws->status;
     return OMNI_OK;
 }

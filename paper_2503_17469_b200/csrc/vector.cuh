@@ -7,6 +7,14 @@
 
 namespace omni {
 
+// For kernels of one call that follow one another (see Dependent in context.h): the next may begin its set-up; what the one
+// before wrote is there.
+__device__ __forceinline__ void let_next_begin(bool allowed)
+{
+    if (allowed) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 constexpr int kGroup = 8;  // elements of a wide access: 16 bytes of bfloat16, 32 of float
 
 __device__ __forceinline__ float to_float(float x) { return x; }

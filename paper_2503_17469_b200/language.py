@@ -20,7 +20,7 @@ from . import binding as B
 
 _DTYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16}
 _INDEX = {torch.int32: B.I32, torch.int64: B.I64}
-_empty, _float, _bf16, _byte = torch.empty, torch.float32, torch.bfloat16, torch.uint8
+_like, _float, _bf16, _byte = torch.empty_like, torch.float32, torch.bfloat16, torch.uint8
 _ref = C.byref
 
 
@@ -90,7 +90,7 @@ class Embedding(_Operator):
                 return self.forward(tokens, weight, dtype, out)
         shape = (*tokens.shape, self.dim)
         if out is None:
-            out = _empty(shape, dtype=dtype or weight.dtype, device=tokens.device)
+            out = weight.new_empty(shape, dtype=dtype or weight.dtype)
         elif out.shape != shape or not out.is_contiguous():
             raise ValueError(f"out: a contiguous tensor of shape {shape} is wanted")
         if weight.shape != self._table:
@@ -118,11 +118,10 @@ class Embedding(_Operator):
             raise ValueError(f"grad_out: {n} rows of {self.dim} are wanted")
         if not tokens.is_contiguous():
             raise ValueError("tokens: a contiguous tensor is wanted")
-        device = tokens.device
         if grad is None:
             if accumulate:
                 raise ValueError("accumulate needs a gradient to add to")
-            grad = _empty(self._table, dtype=dtype, device=device)
+            grad = g.new_empty(self._table, dtype=dtype)
         elif grad.shape != self._table:
             raise ValueError(f"grad: shape {tuple(self._table)} is wanted")
         if not tokens.is_cuda or not g.get_device() == grad.get_device() == tokens.get_device():
@@ -132,7 +131,7 @@ class Embedding(_Operator):
             need = C.c_uint64()
             self._check(self._lib.omni_embed_workspace(n, self.vocab, self.dim, _ref(need)))
             size = self._sizes[n] = max(16, need.value)
-        scratch = _empty(size, dtype=_byte, device=device)
+        scratch = g.new_empty(size, dtype=_byte)
         self._check(self._lib.omni_embed_backward(
             self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), n, g.data_ptr(),
             _code(g, _DTYPES, "grad_out"), _rows(g, "grad_out"), self.vocab, self.dim, self.scale, self.padding,
@@ -190,8 +189,8 @@ class Attention(_Operator):
         a, rows, keys = self._describe(q, k, q_lengths, kv_lengths)
         device, view = q.get_device(), self._view
         if out is None:
-            out = _empty(rows, dtype=_bf16, device=q.device)
-        lse = _empty((rows[0], self.heads, rows[1]), dtype=_float, device=q.device)
+            out = _like(q)
+        lse = q.new_empty((rows[0], self.heads, rows[1]), dtype=_float)
         self._check(self._lib.omni_attn_forward(
             self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),
             _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(), _current_stream()))
@@ -204,18 +203,17 @@ class Attention(_Operator):
             with self._on_stream(stream):
                 return self.backward(q, k, v, out, lse, grad_out, q_lengths, kv_lengths, grads)
         a, rows, keys = self._describe(q, k, q_lengths, kv_lengths)
-        device, view, where = q.get_device(), self._view, q.device
+        device, view = q.get_device(), self._view
         if lse.dtype != _float or not lse.is_contiguous() or lse.shape != (rows[0], self.heads, rows[1]) or lse.get_device() != device:
             raise ValueError("lse: contiguous float32 [batch, heads, q_len] is wanted")
         if grads is None:
-            grads = (_empty(rows, dtype=_bf16, device=where), _empty(keys, dtype=_bf16, device=where),
-                     _empty(keys, dtype=_bf16, device=where))
+            grads = (_like(q), _like(k), _like(v))
         size = self._sizes.get(rows)
         if size is None:
             need = C.c_uint64()
             self._check(self._lib.omni_attn_workspace(_ref(a), _ref(need)))
             size = self._sizes[rows] = max(16, need.value)
-        scratch = _empty(size, dtype=_byte, device=where)
+        scratch = q.new_empty(size, dtype=_byte)
         dq, dk, dv = grads
         self._check(self._lib.omni_attn_backward(
             self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),
@@ -261,7 +259,7 @@ class Distillation(_Operator):
     @staticmethod
     def _grad_like(logits, grad):
         if grad is None:
-            return _empty(logits.shape, dtype=logits.dtype, device=logits.device)
+            return _like(logits)
         if grad.shape != logits.shape or grad.dtype != logits.dtype or grad.get_device() != logits.get_device():
             raise ValueError("grad: the logits' shape, dtype and device are wanted")
         return grad
@@ -272,8 +270,8 @@ class Distillation(_Operator):
             with self._on_stream(stream):
                 return self.forward(logits, top_logits, top_index)
         d = self._describe(logits, top_logits, top_index)
-        loss = _empty(d.rows, dtype=_float, device=logits.device)
-        lse = _empty(d.rows, dtype=_float, device=logits.device)
+        loss = logits.new_empty(d.rows, dtype=_float)
+        lse = _like(loss)
         self._check(self._lib.omni_distill_forward(self.ctx._h, _ref(d), loss.data_ptr(), lse.data_ptr(), _current_stream()))
         return loss, lse
 
@@ -296,8 +294,7 @@ class Distillation(_Operator):
                 return self.step(logits, top_logits, top_index, grad_loss, grad)
         d = self._describe(logits, top_logits, top_index)
         weights = self._row_values(grad_loss, logits, "grad_loss")
-        loss = _empty(d.rows, dtype=_float, device=logits.device)
-        lse = _empty(d.rows, dtype=_float, device=logits.device)
+        loss, lse = _like(grad_loss), _like(grad_loss)
         grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_distill_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), lse.data_ptr(),
                                                 grad.data_ptr(), _rows(grad, "grad"), _current_stream()))
