@@ -14,7 +14,7 @@
 //     operand of dV += P^T dO, dS^T over dP^T as that of dK += dS^T Q.
 //     Order of the products: S0 dP0 | dV0 S1 dK0 dP1 | dV1 S2 dK1 dP2 | ...
 //   dQ:     S = Q K^T and dP = dO V^T (128 queries x 128 keys), two tiles of S; dS over S as the A operand of dQ += dS K.
-//     Order: S0 dP0 S1 | dQ0 dP1 S2 | dQ1 dP2 S3 | ...
+//     Order: S0 dP0 S1 | dP1 dQ0 S2 | dP2 dQ1 S3 | ...
 // An operand in tensor memory is overwritten by a product that is issued after the one that reads it; one thread
 // issues all of a block's, and the tensor core takes them in that order.
 // P and dS are rounded to bfloat16 for the products; all sums are float.
@@ -313,7 +313,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
     unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
     unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + KS, *v_full = k_empty + KS, *v_empty = v_full + VS;
-    unsigned long long *s_full = v_empty + VS, *dp_full = s_full + 2, *ds_ready = dp_full + 1, *done = ds_ready + 1;
+    unsigned long long *s_full = v_empty + VS, *dp_full = s_full + 2, *dp_read = dp_full + 1, *ds_ready = dp_read + 1, *done = ds_ready + 1;
     unsigned long long *own = done + 1;
     volatile int *give_up = reinterpret_cast<int *>(own + 1);
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
@@ -336,7 +336,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
         for (int i = 0; i < KS; ++i) { mbar_init(k_full + i, 1); mbar_init(k_empty + i, 1); }
         for (int i = 0; i < VS; ++i) { mbar_init(v_full + i, 1); mbar_init(v_empty + i, 1); }
         mbar_init(s_full, 1); mbar_init(s_full + 1, 1);
-        mbar_init(dp_full, 1); mbar_init(ds_ready, kElementWarps);
+        mbar_init(dp_full, 1); mbar_init(dp_read, kElementWarps); mbar_init(ds_ready, kElementWarps);
         mbar_init(done, 1); mbar_init(own, 1);
         *give_up = 0;
         fence_barrier_init();
@@ -397,12 +397,12 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
             bool ok = wait(q_full, 0) && scores(0) && slopes(0) && (n < 2 || scores(1));
             for (int h = 0; h < n && ok; ++h) {
                 const int st = h % KS;
+                if (h + 1 < n && !(ok = wait(dp_read, h & 1) && slopes(h + 1))) break;
                 if (!(ok = wait(ds_ready, h & 1))) break;
                 fence_after_sync();
                 mma_tmem_across<DP, kRows, kRows, kCols>(dq_at, s_at + (h & 1) * kRows, k0 + st * L::kTile, h > 0);
                 mma_commit(k_empty + st);
-                if (h + 1 < n) ok = slopes(h + 1);
-                if (ok && h + 2 < n) ok = scores(h + 2);
+                if (h + 2 < n) ok = scores(h + 2);
             }
             mma_commit(done);
             mbar_wait(done, 0);
@@ -436,6 +436,9 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
             if (!ok) break;
             fence_after_sync();
             tmem_load(x, dp_row);
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(dp_read);
 #pragma unroll
             for (int c = 0; c < kCols; c += 2)
                 pr[c / 2] = mul2(pr[c / 2], add2({__uint_as_float(x[c]), __uint_as_float(x[c + 1])}, delta));

@@ -28,12 +28,13 @@ struct AttnForwardParams {
 constexpr int kForwardThreads = 384;
 constexpr int kForwardFew = 80, kForwardMany = 208;    // 128 x 40 + 256 x 232 = 384 x 168
 constexpr float kRescaleAbove = 8.0f;
+constexpr int kParts = 4, kPart = kRows / kParts;      // of P: its product starts when the first is there
 
 template <int DP> struct ForwardShared {
     static constexpr int kStages = DP == 128 ? 2 : 4;
     static constexpr int kTile = kRows * DP * 2;
     static constexpr int kQ = 0, kK = 2 * kTile, kV = kK + kStages * kTile, kBars = kV + kStages * kTile;
-    static constexpr int kBytes = kBars + 256 + 1024;      // barriers, and the base rounded up to 1024
+    static constexpr int kBytes = kBars + 512 + 1024;      // barriers, and the base rounded up to 1024
 };
 
 template <int DP>
@@ -45,7 +46,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     unsigned char *smem = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(smem + L::kBars);
     unsigned long long *q_full = bars, *k_full = bars + 1, *k_empty = k_full + ST, *v_full = k_empty + ST, *v_empty = v_full + ST;
-    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 4, *drained = o_full + 2, *own = drained + 1;
+    unsigned long long *s_full = v_empty + ST, *p_ready = s_full + 2, *o_full = p_ready + 2 * kParts, *drained = o_full + 2, *own = drained + 1;
     volatile int *give_up = reinterpret_cast<int *>(own + 1);
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
             mbar_init(v_full + i, 1); mbar_init(v_empty + i, 1);
         }
         for (int t = 0; t < 2; ++t) { mbar_init(s_full + t, 1); mbar_init(o_full + t, 1); }
-        for (int i = 0; i < 4; ++i) mbar_init(p_ready + i, 4);        // [tile][half]
+        for (int i = 0; i < 2 * kParts; ++i) mbar_init(p_ready + i, 4);   // [tile][part]
         mbar_init(drained, 1); mbar_init(own, 1);
         *give_up = 0;
         fence_barrier_init();
@@ -138,12 +139,12 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 for (int t = 0; t < 2; ++t) {
                     if (j >= tiles[t]) continue;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        ok = ok && wait(p_ready + 2 * t + half, j & 1);
+                    for (int part = 0; part < kParts; ++part) {
+                        ok = ok && wait(p_ready + kParts * t + part, j & 1);
                         if (!ok) break;
                         fence_after_sync();
-                        mma_tmem_across<DP, kRows, 64, 64>(o_at + t * DP, s_at + t * kRows + half * 32, v + st * L::kTile + half * 64 * 128,
-                                                           j > 0 || half > 0);
+                        mma_tmem_across<DP, kRows, kPart, kPart>(o_at + t * DP, s_at + t * kRows + part * kPart / 2,
+                                                                 v + st * L::kTile + part * kPart * 128, j > 0 || part > 0);
                     }
                     if (!ok) break;
                     // the next scores go over P: the tensor core takes MMAs in order
@@ -213,20 +214,20 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
             const float2 unit2 = {unit, unit}, ref2 = {-ref, -ref};
             float2 sum[2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t packed[32];
+            for (int h = 0; h < kParts; ++h) {
+                uint32_t packed[kPart / 2];
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    const float2 z = fma2({__uint_as_float(x[h][c]), __uint_as_float(x[h][c + 1])}, unit2, ref2);
+                for (int c = 0; c < kPart; c += 2) {
+                    const float2 z = fma2({__uint_as_float(x[(h * kPart + c) / 64][(h * kPart + c) % 64]), __uint_as_float(x[(h * kPart + c) / 64][(h * kPart + c) % 64 + 1])}, unit2, ref2);
                     const float2 e = {exp2_fast(z.x), exp2_fast(z.y)};
                     sum[c / 2 % 2] = add2(sum[c / 2 % 2], e);
                     packed[c / 2] = pack2(e.x, e.y);
                 }
-                tmem_store(s_row + h * 32, packed);
+                tmem_store(s_row + h * kPart / 2, packed);
                 tmem_wait_store();
                 fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_ready + 2 * t + h);
+                if (lane == 0) mbar_arrive(p_ready + kParts * t + h);
             }
             l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         }
