@@ -452,12 +452,16 @@ typedef struct {
  *   P = exp(S - lse), D_i = sum_c dO_ic O_ic, dS = P (dO V^T - D)
  *   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
  * with P and dS rounded to bfloat16 for the products and every sum in float, in a fixed order.
- * workspace: device, 16-byte aligned, omni_attn_workspace() bytes.  Inputs and outputs do not overlap.
+ * workspace: device, 16-byte aligned, omni_attn_forward_workspace() bytes for the forward call (0 unless there are few
+ * query rows for the GPU, whose walk along the keys is then split; NULL will do for 0) and omni_attn_workspace() for the
+ * backward call.  Inputs, outputs and workspace do not overlap.
  * Errors: NULL, BAD_CONFIG (negative sizes, heads not a multiple of kv_heads, dim, scale, a stride below dim), ALIGN,
  * TOO_LARGE (dim, batch or heads > 65535, lengths > 2^30, a workspace below the size asked for), CUDA;
  * a bounded wait of the kernels that runs out surfaces as TIMEOUT from omni_get_stats. */
 int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
-                      const omni_attn_view *v, const omni_attn_view *out, float *lse, void *stream);
+                      const omni_attn_view *v, const omni_attn_view *out, float *lse, void *workspace, uint64_t workspace_bytes,
+                      void *stream);
+int omni_attn_forward_workspace(const omni_attn *a, uint64_t *bytes);
 int omni_attn_workspace(const omni_attn *a, uint64_t *bytes);
 int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
                        const omni_attn_view *v, const omni_attn_view *out, const float *lse, const omni_attn_view *dout,

@@ -35,7 +35,7 @@ EXPORTS = (
     "omni_shard_range", "omni_asp_push_pull", "omni_ctl_export", "omni_ctl_import", "omni_step_bsp",
     "omni_asp_report_device",
     "omni_embed_forward", "omni_embed_workspace", "omni_embed_backward",
-    "omni_attn_forward", "omni_attn_workspace", "omni_attn_backward",
+    "omni_attn_forward", "omni_attn_forward_workspace", "omni_attn_workspace", "omni_attn_backward",
     "omni_distill_forward", "omni_distill_backward", "omni_distill_step",
 )
 MAX_ASP_BATCH = 16
@@ -127,7 +127,8 @@ def lib() -> C.CDLL:
     L.omni_embed_workspace.argtypes = [u64, i32, i32, C.POINTER(u64)]
     L.omni_embed_backward.argtypes = [vp, vp, i32, u64, vp, i32, u64, i32, i32, f32, i64, vp, i32, u64, i32, vp, u64, vp]
     at, view = C.POINTER(omni_attn), C.POINTER(omni_attn_view)
-    L.omni_attn_forward.argtypes = [vp, at, view, view, view, view, vp, vp]
+    L.omni_attn_forward.argtypes = [vp, at, view, view, view, view, vp, vp, u64, vp]
+    L.omni_attn_forward_workspace.argtypes = [at, C.POINTER(u64)]
     L.omni_attn_workspace.argtypes = [at, C.POINTER(u64)]
     L.omni_attn_backward.argtypes = [vp, at, view, view, view, view, vp, view, view, view, view, vp, u64, vp]
     L.omni_distill_forward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp]

@@ -10,6 +10,8 @@
 namespace omni {
 namespace {
 
+constexpr int64_t kSms = 148;
+
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 uint64_t round_up(uint64_t x, uint64_t m) { return (x + m - 1) / m * m; }
 
@@ -102,6 +104,39 @@ int launch(omni_ctx *ctx, void (*kernel)(P), dim3 grid, int threads, int smem, c
     return context_launched(ctx, int(cudaLaunchKernelExC(&d.cfg, fn, args)));
 }
 
+// Blocks per tile: where the tiles do not fill half of the SMs (148), the walks along the other axis, `steps` tiles long at
+// most, are dealt out until they fill them all once, two steps a block at least.  Whole walks against dealt out, us a call:
+// one query on 8192 keys, 8 heads on 1, forward 113.7 / 26.8, backward 84.2 / 36.0; 4096 x 4096, 2 heads on 1, causal 63.3 / 30.8
+// and 116.2 / 45.1; 1025 queries on 11 keys, 8 heads on 2, three sequences, backward 68.0 / 28.8.  Below eight steps the
+// joining kernel costs more than it gives (512 x 512, 8 heads: forward 15.3 / 19.5), and so does dealing out from a tile
+// per SM on or filling the SMs twice (777 x 777, 12 heads on 4, two sequences: forward 18.5 / 33.1; 256 x 8192: 30.8 / 45.1).
+int splits_of(int64_t tiles, int64_t steps)
+{
+    if (tiles < 1 || 2 * tiles > kSms || steps < 8) return 1;
+    const int64_t fill = kSms / tiles, most = steps / 2;
+    return int(fill < most ? fill : most);
+}
+int64_t row_tiles(int64_t rows, int tile = kRows) { return (rows + tile - 1) / tile; }
+int forward_splits(const omni_attn *a)
+{
+    return splits_of(row_tiles(a->q_len, 2 * kRows) * a->heads * a->batch, row_tiles(a->kv_len));
+}
+int query_splits(const omni_attn *a) { return splits_of(row_tiles(a->q_len) * a->heads * a->batch, row_tiles(a->kv_len)); }
+int key_splits(const omni_attn *a)
+{
+    return splits_of(row_tiles(a->kv_len) * a->kv_heads * a->batch, row_tiles(a->q_len) * (a->heads / a->kv_heads));
+}
+// Floats of the parts, and what describes them; `at` moves on behind them.
+uint64_t part_floats(int splits, const omni_attn *a, int len, int heads)
+{
+    return splits > 1 ? uint64_t(splits) * a->batch * len * heads * a->dim : 0;
+}
+Parts take_parts(float *&at, int splits, const omni_attn *a, int len, int heads)
+{
+    const Parts p = {splits, at, (long long)a->batch * len * heads, len, heads};
+    at += part_floats(splits, a, len, heads);
+    return p;
+}
 int q_pad_of(const omni_attn *a) { return int(round_up(uint64_t(a->q_len), kRows)); }
 
 }  // namespace
@@ -112,7 +147,8 @@ using namespace omni;
 extern "C" {
 
 int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q, const omni_attn_view *k,
-                      const omni_attn_view *v, const omni_attn_view *out, float *lse, void *stream)
+                      const omni_attn_view *v, const omni_attn_view *out, float *lse, void *workspace, uint64_t workspace_bytes,
+                      void *stream)
 {
     if (!ctx) return OMNI_ERR_NULL;
     int rc = check_shape(a);
@@ -123,7 +159,11 @@ int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q
     for (const omni_attn_view *x : ks)
         if ((rc = check_view(x, a->dim, a->kv_heads, a->kv_len, a->batch)) != OMNI_OK) return rc;
     if (a->q_len > 0 && a->batch > 0 && !lse) return OMNI_ERR_NULL;
-    if (!aligned(lse, 4)) return OMNI_ERR_ALIGN;
+    uint64_t need = 0;
+    if ((rc = omni_attn_forward_workspace(a, &need)) != OMNI_OK) return rc;
+    if (need > 0 && !workspace) return OMNI_ERR_NULL;
+    if (!aligned(lse, 4) || !aligned(workspace, 16)) return OMNI_ERR_ALIGN;
+    if (workspace_bytes < need) return OMNI_ERR_TOO_LARGE;
     ContextDevice dev;
     rc = context_bind(ctx, &dev);
     if (rc != OMNI_OK || a->q_len == 0 || a->batch == 0) return rc;
@@ -141,10 +181,25 @@ int omni_attn_forward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *q
     p.lse = lse;
     p.status = dev.status;
     p.q_tiles = (a->q_len + 2 * kRows - 1) / (2 * kRows);
-    const dim3 grid(unsigned(p.q_tiles) * a->heads * a->batch);
+    float *at = static_cast<float *>(workspace);
+    p.parts = take_parts(at, forward_splits(a), a, a->q_len, a->heads);
+    p.part_lse = at;
+    const dim3 grid(unsigned(p.q_tiles) * a->heads * a->batch * p.parts.splits);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a->dim <= 64) return launch(ctx, attention_forward_kernel<64>, grid, kForwardThreads, ForwardShared<64>::kBytes, s, p);
-    return launch(ctx, attention_forward_kernel<128>, grid, kForwardThreads, ForwardShared<128>::kBytes, s, p);
+    rc = a->dim <= 64 ? launch(ctx, attention_forward_kernel<64>, grid, kForwardThreads, ForwardShared<64>::kBytes, s, p)
+                      : launch(ctx, attention_forward_kernel<128>, grid, kForwardThreads, ForwardShared<128>::kBytes, s, p);
+    if (rc != OMNI_OK || p.parts.splits == 1) return rc;
+    return launch(ctx, attention_forward_join_kernel, dim3(unsigned((p.parts.rows * (a->dim / 8) + 255) / 256)), 256, 0, s, p, &dev);
+}
+
+int omni_attn_forward_workspace(const omni_attn *a, uint64_t *bytes)
+{
+    if (!bytes) return OMNI_ERR_NULL;
+    const int rc = check_shape(a);
+    if (rc != OMNI_OK) return rc;
+    const int splits = forward_splits(a);
+    *bytes = splits > 1 ? (part_floats(splits, a, a->q_len, a->heads) + uint64_t(splits) * a->batch * a->heads * a->q_len) * sizeof(float) : 0;
+    return OMNI_OK;
 }
 
 int omni_attn_workspace(const omni_attn *a, uint64_t *bytes)
@@ -152,7 +207,8 @@ int omni_attn_workspace(const omni_attn *a, uint64_t *bytes)
     if (!bytes) return OMNI_ERR_NULL;
     const int rc = check_shape(a);
     if (rc != OMNI_OK) return rc;
-    *bytes = 2ull * a->batch * a->heads * q_pad_of(a) * sizeof(float);
+    *bytes = (2ull * a->batch * a->heads * q_pad_of(a) + part_floats(query_splits(a), a, a->q_len, a->heads) +
+              2 * part_floats(key_splits(a), a, a->kv_len, a->kv_heads)) * sizeof(float);
     return OMNI_OK;
 }
 
@@ -207,11 +263,17 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
         for (const auto &m : maps)
             if ((rc = make_map(ctx, encode, m.map, *m.view, a->dim, m.heads, m.len, a->batch)) != OMNI_OK) return rc;
     }
-    p.key_blocks = (a->kv_len + kRows - 1) / kRows * a->kv_heads * a->batch;
-    const dim3 grid(unsigned(p.key_blocks) + unsigned(p.q_tiles) * a->heads * a->batch);
+    float *at = static_cast<float *>(workspace) + 2ull * a->batch * a->heads * q_pad;
+    p.parts_dq = take_parts(at, query_splits(a), a, a->q_len, a->heads);
+    p.parts_dk = take_parts(at, key_splits(a), a, a->kv_len, a->kv_heads);
+    p.parts_dv = take_parts(at, key_splits(a), a, a->kv_len, a->kv_heads);
+    p.key_blocks = int(row_tiles(a->kv_len)) * a->kv_heads * a->batch * p.parts_dk.splits;
+    const dim3 grid(unsigned(p.key_blocks) + unsigned(p.q_tiles) * a->heads * a->batch * p.parts_dq.splits);
     rc = a->dim <= 64 ? launch(ctx, attention_backward_kernel<64>, grid, kBackwardThreads, BackwardShared<64>::kBytes, s, p, a->q_len > 0 ? &dev : nullptr)
                       : launch(ctx, attention_backward_kernel<128>, grid, kBackwardThreads, BackwardShared<128>::kBytes, s, p, a->q_len > 0 ? &dev : nullptr);
-    return rc;
+    const int64_t rows = (p.parts_dq.splits > 1 ? p.parts_dq.rows : 0) + (p.parts_dk.splits > 1 ? 2 * p.parts_dk.rows : 0);
+    if (rc != OMNI_OK || rows == 0) return rc;
+    return launch(ctx, attention_backward_join_kernel, dim3(unsigned((rows * (a->dim / 8) + 255) / 256)), 256, 0, s, p, &dev);
 }
 
 }  // extern "C"

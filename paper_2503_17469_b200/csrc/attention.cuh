@@ -154,6 +154,24 @@ __device__ __forceinline__ void store_row(unsigned tmem, float gain, __nv_bfloat
         }
     }
 }
+// The same as floats, for a part of a sum.
+template <int DP> __device__ __forceinline__ void store_row(unsigned tmem, float gain, float *dst, int dim, bool write)
+{
+    constexpr int kAt = DP < 32 ? DP : 32;
+#pragma unroll
+    for (int c = 0; c < DP / kAt; ++c) {
+        uint32_t r[kAt];
+        tmem_load(r, tmem + c * kAt);
+#pragma unroll
+        for (int g = 0; g < kAt / 8; ++g) {
+            if (!write || c * kAt + g * 8 >= dim) continue;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = gain * __uint_as_float(r[g * 8 + e]);
+            store_group(dst + c * kAt + g * 8, f);
+        }
+    }
+}
 __device__ __forceinline__ void store_zeros(__nv_bfloat16 *dst, int dim)
 {
     for (int c = 0; c < dim; c += 8) *reinterpret_cast<uint4 *>(dst + c) = make_uint4(0, 0, 0, 0);
@@ -166,6 +184,42 @@ __device__ __forceinline__ void zero_tile(const OutView &o, int batch, int head,
     for (int i = threadIdx.x; i < rows * groups; i += blockDim.x)
         *reinterpret_cast<uint4 *>(o.data + batch * o.batch + (long long)(row + i / groups) * o.row + head * o.head + i % groups * 8) =
             make_uint4(0, 0, 0, 0);
+}
+
+// Few blocks with long walks leave most SMs without work, so the walk is dealt out to `splits` blocks; each leaves its float
+// sums as part k of [splits][batch][len][heads][dim], and the call's last kernel joins them in order.
+struct Parts {
+    int splits;
+    float *data;
+    long long rows;     // batch * len * heads
+    int len, heads;
+    __device__ __forceinline__ float *at(int part, int batch, int row, int head, int dim) const
+    {
+        return data + (((long long)part * rows + ((long long)batch * len + row) * heads + head) * dim);
+    }
+};
+// The stretch [from, to) of n steps that part k of `splits` takes.
+__device__ __forceinline__ void stretch_of(int n, int k, int splits, int *from, int *to)
+{
+    *from = int((long long)n * k / splits);
+    *to = int((long long)n * (k + 1) / splits);
+}
+__device__ __forceinline__ void zero_parts(const Parts &o, int part, int batch, int head, int row, int rows, int dim)
+{
+    for (int i = threadIdx.x; i < rows * dim; i += blockDim.x) o.at(part, batch, row + i / dim, head, dim)[i % dim] = 0.0f;
+}
+// Sum of the parts at 8 columns of a row, weighted by w(part).
+template <typename W> __device__ __forceinline__ void join_parts(const Parts &o, int batch, int row, int head, int dim, int c, float *sum, W w)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+    for (int k = 0; k < o.splits; ++k) {
+        float f[8];
+        load_group(o.at(k, batch, row, head, dim) + c, f);
+        const float g = w(k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] = fmaf(g, f[e], sum[e]);
+    }
 }
 
 }  // namespace omni

@@ -36,6 +36,7 @@ struct AttnBackwardParams {
     int q_pad, q_tiles;
     int key_blocks;                 // blocks that own keys; the others own queries
     OutView dq, dk, dv;
+    Parts parts_dq, parts_dk, parts_dv;
     unsigned *status;
 };
 
@@ -102,8 +103,9 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
     const float *stats = reinterpret_cast<const float *>(smem + L::kStats);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Place at_tile = place_of(block, p.s.kv_heads, p.s.batch);
-    const int kv_head = at_tile.head, b = at_tile.batch, group = p.s.heads / p.s.kv_heads;
+    const int splits = p.parts_dk.splits;
+    const Place at_tile = place_of(block, p.s.kv_heads * splits, p.s.batch);
+    const int kv_head = at_tile.head / splits, part = at_tile.head % splits, b = at_tile.batch, group = p.s.heads / p.s.kv_heads;
     const int k0 = at_tile.tile * kRows;
     const Lengths len = lengths_of(p.s, b);
 
@@ -111,10 +113,18 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
     const int first_row = p.s.causal ? max(0, k0 - len.shift) : 0;
     const int tile0 = first_row / kRows;
     const int tiles = k0 < len.kv && first_row < len.q ? (len.q + kRows - 1) / kRows - tile0 : 0;
-    const int n = tiles * group;                                    // (query head, tile) one after the other
+    int h0, h1;                                                     // this block's steps, (query head, tile) one after the other
+    stretch_of(tiles * group, part, splits, &h0, &h1);
+    const int n = h1 - h0;
     if (n == 0) {                                                   // no query sees these keys
-        zero_tile(p.dk, b, kv_head, k0, min(kRows, p.s.kv_len - k0), p.s.dim);
-        zero_tile(p.dv, b, kv_head, k0, min(kRows, p.s.kv_len - k0), p.s.dim);
+        const int rows = min(kRows, p.s.kv_len - k0);
+        if (splits > 1) {
+            zero_parts(p.parts_dk, part, b, kv_head, k0, rows, p.s.dim);
+            zero_parts(p.parts_dv, part, b, kv_head, k0, rows, p.s.dim);
+        } else {
+            zero_tile(p.dk, b, kv_head, k0, rows, p.s.dim);
+            zero_tile(p.dv, b, kv_head, k0, rows, p.s.dim);
+        }
         return;
     }
 
@@ -148,7 +158,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         int q_armed = 0, do_armed = 0;
         const unsigned long long policy = policy_evict_last();
         for (int h = 0; h < n; ++h) {
-            const int st = h % ST, head = kv_head * group + h / tiles, row = (tile0 + h % tiles) * kRows;
+            const int st = h % ST, head = kv_head * group + (h0 + h) / tiles, row = (tile0 + (h0 + h) % tiles) * kRows;
             const int valid = p.s.q_lengths ? len.q - row : kRows;
             const unsigned free_parity = ((h / ST) & 1) ^ 1;
             if (!load.wait(q_empty + st, free_parity)) break;
@@ -218,7 +228,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         const int from = j >= len.kv ? INT_MAX : p.s.causal ? j - len.shift : 0;
         bool ok = true;
         for (int h = 0; h < n; ++h) {
-            const int i0 = (tile0 + h % tiles) * kRows + c0;
+            const int i0 = (tile0 + (h0 + h) % tiles) * kRows + c0;
             const float4 *lse = reinterpret_cast<const float4 *>(stats + h % ST * 2 * kRows + c0), *delta = lse + kRows / 4;
             // the row values came with Q: their copy is waited for here too
             ok = warp_wait(q_full + h % ST, (h / ST) & 1, give_up, p.status) && warp_wait(s_full, h & 1, give_up, p.status);
@@ -285,9 +295,16 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         const bool values = warp < 8;
         const OutView &o = values ? p.dv : p.dk;
         const int half = warp / 4 % 2, d0 = half * (DP / 2);
-        __nv_bfloat16 *dst = o.data + b * o.batch + (long long)j * o.row + kv_head * o.head;
+        const unsigned from_tmem = (values ? dv_at : dk_at) + lanes + d0;
+        const float gain = values ? 1.0f : p.s.scale;
         const bool mine = ok && j < p.s.kv_len;
-        if (ok) store_row<DP / 2>((values ? dv_at : dk_at) + lanes + d0, values ? 1.0f : p.s.scale, dst + d0, p.s.dim - d0, mine);
+        if (splits > 1) {
+            float *dst = (values ? p.parts_dv : p.parts_dk).at(part, b, j, kv_head, p.s.dim) + d0;
+            if (ok) store_row<DP / 2>(from_tmem, gain, dst, p.s.dim - d0, mine);
+        } else {
+            __nv_bfloat16 *dst = o.data + b * o.batch + (long long)j * o.row + kv_head * o.head + d0;
+            if (ok) store_row<DP / 2>(from_tmem, gain, dst, p.s.dim - d0, mine);
+        }
     }
     fence_before_sync();
     __syncthreads();
@@ -319,15 +336,19 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Place at_tile = place_of(block, p.s.heads, p.s.batch);
-    const int head = at_tile.head, b = at_tile.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const int splits = p.parts_dq.splits;
+    const Place at_tile = place_of(block, p.s.heads * splits, p.s.batch);
+    const int head = at_tile.head / splits, part = at_tile.head % splits, b = at_tile.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
     const int q0 = (p.q_tiles - 1 - at_tile.tile) * kRows;
     const Lengths len = lengths_of(p.s, b);
     const int last = min(q0 + kRows, len.q) - 1;
     const int seen = last < q0 ? 0 : p.s.causal ? min(len.kv, last + len.shift + 1) : len.kv;
-    const int n = seen > 0 ? (seen + kRows - 1) / kRows : 0;
+    int h0, h1;                                                     // this block's key tiles
+    stretch_of(seen > 0 ? (seen + kRows - 1) / kRows : 0, part, splits, &h0, &h1);
+    const int n = h1 - h0;
     if (n == 0) {                                                   // no query of the tile sees a key
-        zero_tile(p.dq, b, head, q0, min(kRows, p.s.q_len - q0), p.s.dim);
+        if (splits > 1) zero_parts(p.parts_dq, part, b, head, q0, min(kRows, p.s.q_len - q0), p.s.dim);
+        else zero_tile(p.dq, b, head, q0, min(kRows, p.s.q_len - q0), p.s.dim);
         return;
     }
 
@@ -360,12 +381,12 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
         for (int h = 0; h < n; ++h) {
             const int ks = h % KS, vs = h % VS;
             if (!load.wait(k_empty + ks, ((h / KS) & 1) ^ 1)) break;
-            if (!load.tile<DP>(smem + L::kK + ks * L::kTile, &p.k, kv_head, h * kRows, b, k_full + ks,
-                               p.s.kv_lengths ? len.kv - h * kRows : kRows))
+            if (!load.tile<DP>(smem + L::kK + ks * L::kTile, &p.k, kv_head, (h0 + h) * kRows, b, k_full + ks,
+                               p.s.kv_lengths ? len.kv - (h0 + h) * kRows : kRows))
                 break;
             ++k_armed;
             if (!load.wait(v_empty + vs, ((h / VS) & 1) ^ 1)) break;
-            load.tile<DP>(smem + L::kV + vs * L::kTile, &p.v, kv_head, h * kRows, b, v_full + vs, kRows);
+            load.tile<DP>(smem + L::kV + vs * L::kTile, &p.v, kv_head, (h0 + h) * kRows, b, v_full + vs, kRows);
             ++v_armed;
         }
         mbar_wait(q_full, 0);
@@ -423,7 +444,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
             ok = warp_wait(s_full + (h & 1), (h / 2) & 1, give_up, p.status);
             if (!ok) break;
             fence_after_sync();
-            const int open = limit - h * kRows - c0;
+            const int open = limit - (h0 + h) * kRows - c0;
             uint32_t x[kCols], out[kCols / 2];
             float2 pr[kCols / 2];
             tmem_load(x, s_here);
@@ -462,10 +483,18 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
         fence_after_sync();
         // every four warps a quarter of the columns
         const int d0 = warp / 4 * (DP / 4);
-        __nv_bfloat16 *dst = p.dq.data + b * p.dq.batch + (long long)i * p.dq.row + head * p.dq.head;
         const bool mine = ok && i < p.s.q_len, empty = limit <= 0;
-        if (ok) store_row<DP / 4>(dq_at + lanes + d0, p.s.scale, dst + d0, p.s.dim - d0, mine && !empty);
-        if (d0 == 0 && mine && empty) store_zeros(dst, p.s.dim);
+        if (splits > 1) {
+            // a row that sees no key has P = 0 throughout, but a row of Q may hold NaN
+            float *dst = p.parts_dq.at(part, b, i, head, p.s.dim) + d0;
+            if (ok) store_row<DP / 4>(dq_at + lanes + d0, p.s.scale, dst, p.s.dim - d0, mine && !empty);
+            if (mine && empty)
+                for (int c = 0; c < DP / 4 && d0 + c < p.s.dim; ++c) dst[c] = 0.0f;
+        } else {
+            __nv_bfloat16 *dst = p.dq.data + b * p.dq.batch + (long long)i * p.dq.row + head * p.dq.head;
+            if (ok) store_row<DP / 4>(dq_at + lanes + d0, p.s.scale, dst + d0, p.s.dim - d0, mine && !empty);
+            if (d0 == 0 && mine && empty) store_zeros(dst, p.s.dim);
+        }
     }
     fence_before_sync();
     __syncthreads();
@@ -482,5 +511,26 @@ __global__ void __launch_bounds__(kBackwardThreads, 1) attention_backward_kernel
 template <int DP> struct BackwardShared {
     static constexpr int kBytes = KeysShared<DP>::kBytes > QueriesShared<DP>::kBytes ? KeysShared<DP>::kBytes : QueriesShared<DP>::kBytes;
 };
+
+// The gradients whose walks were dealt out, from their parts: a thread per 8 columns of a row.
+__global__ void __launch_bounds__(256) attention_backward_join_kernel(const __grid_constant__ AttnBackwardParams p)
+{
+    wait_for_previous();
+    const int groups = p.s.dim / 8;
+    long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+#pragma unroll
+    for (int side = 0; side < 3; ++side) {
+        const Parts &o = side == 0 ? p.parts_dq : side == 1 ? p.parts_dk : p.parts_dv;
+        const OutView &v = side == 0 ? p.dq : side == 1 ? p.dk : p.dv;
+        const long long mine = o.splits > 1 ? o.rows * groups : 0;
+        if (at >= mine) { at -= mine; continue; }
+        const long long row = at / groups;
+        const int c = int(at % groups) * 8, head = int(row % o.heads), i = int(row / o.heads % o.len), b = int(row / o.heads / o.len);
+        float sum[8];
+        join_parts(o, b, i, head, p.s.dim, c, sum, [](int) { return 1.0f; });
+        store_group(v.data + b * v.batch + (long long)i * v.row + head * v.head + c, sum);
+        return;
+    }
+}
 
 }  // namespace omni

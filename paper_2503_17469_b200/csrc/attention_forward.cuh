@@ -21,6 +21,8 @@ struct AttnForwardParams {
     int q_tiles;                    // pairs of tiles
     OutView out;
     float *lse;
+    Parts parts;                    // of out, each divided by its own sum
+    float *part_lse;                // [splits][batch][heads][q_len]
     unsigned *status;
 };
 
@@ -51,8 +53,9 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
     unsigned *tmem_cell = reinterpret_cast<unsigned *>(own + 2);
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const Place at = place_of(int(blockIdx.x), p.s.heads, p.s.batch);
-    const int head = at.head, b = at.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
+    const int splits = p.parts.splits;
+    const Place at = place_of(int(blockIdx.x), p.s.heads * splits, p.s.batch);
+    const int head = at.head / splits, part = at.head % splits, b = at.batch, kv_head = head / (p.s.heads / p.s.kv_heads);
     const int q0 = (p.q_tiles - 1 - at.tile) * 2 * kRows;
     const Lengths len = lengths_of(p.s, b);
 
@@ -64,11 +67,18 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
         const int seen = last < first ? 0 : p.s.causal ? min(len.kv, last + len.shift + 1) : len.kv;
         tiles[t] = seen > 0 ? (seen + kRows - 1) / kRows : 0;
     }
-    const int n = max(tiles[0], tiles[1]);
+    int j0, j1;                                                       // this block's key tiles
+    stretch_of(max(tiles[0], tiles[1]), part, splits, &j0, &j1);
+    const int n = j1 - j0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) tiles[t] = min(max(tiles[t] - j0, 0), n);
+    float *lse = splits > 1 ? p.part_lse + (long long)part * p.s.batch * p.s.heads * p.s.q_len : p.lse;
+    lse += ((long long)b * p.s.heads + head) * p.s.q_len;
     if (n == 0) {                                                     // no row sees a key
         const int rows = min(2 * kRows, p.s.q_len - q0);
-        zero_tile(p.out, b, head, q0, rows, p.s.dim);
-        for (int i = threadIdx.x; i < rows; i += blockDim.x) p.lse[((long long)b * p.s.heads + head) * p.s.q_len + q0 + i] = -INFINITY;
+        if (splits > 1) zero_parts(p.parts, part, b, head, q0, rows, p.s.dim);
+        else zero_tile(p.out, b, head, q0, rows, p.s.dim);
+        for (int i = threadIdx.x; i < rows; i += blockDim.x) lse[q0 + i] = -INFINITY;
         return;
     }
 
@@ -106,11 +116,11 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 const int st = j % ST;
                 const unsigned free_parity = ((j / ST) & 1) ^ 1;
                 if (!load.wait(k_empty + st, free_parity)) break;
-                load.tile<DP>(smem + L::kK + st * L::kTile, &p.k, kv_head, j * kRows, b, k_full + st, kRows);
+                load.tile<DP>(smem + L::kK + st * L::kTile, &p.k, kv_head, (j0 + j) * kRows, b, k_full + st, kRows);
                 ++kj;
                 if (!load.wait(v_empty + st, free_parity)) break;
-                if (!load.tile<DP>(smem + L::kV + st * L::kTile, &p.v, kv_head, j * kRows, b, v_full + st,
-                                   p.s.kv_lengths ? len.kv - j * kRows : kRows))
+                if (!load.tile<DP>(smem + L::kV + st * L::kTile, &p.v, kv_head, (j0 + j) * kRows, b, v_full + st,
+                                   p.s.kv_lengths ? len.kv - (j0 + j) * kRows : kRows))
                     break;
                 ++vj;
             }
@@ -179,7 +189,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
             fence_after_sync();
             uint32_t x[2][64];
             tmem_load2(x[0], s_row, x[1], s_row + 64);
-            const int open = limit - j * kRows;                       // columns of this tile that the row sees
+            const int open = limit - (j0 + j) * kRows;                       // columns of this tile that the row sees
             if (__any_sync(~0u, open < kRows)) {
 #pragma unroll
                 for (int c = 0; c < kRows; ++c)
@@ -234,15 +244,48 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
         if (ok && tiles[t] > 0) ok = warp_wait(o_full + t, 0, give_up, p.status);
         fence_after_sync();
         const bool mine = i < p.s.q_len && ok;
-        __nv_bfloat16 *dst = p.out.data + b * p.out.batch + (long long)i * p.out.row + head * p.out.head;
-        const bool empty = l == 0.0f;                                 // the row sees no key
-        if (tiles[t] > 0 && ok) store_row<DP>(o_row, 1.0f / l, dst, p.s.dim, mine && !empty);
-        if (mine && empty) store_zeros(dst, p.s.dim);
-        if (mine) p.lse[((long long)b * p.s.heads + head) * p.s.q_len + i] = (m + log2f(l)) * kAttnLn2;
+        const bool empty = l == 0.0f, write = mine && !empty;         // empty: the row sees no key
+        if (splits > 1) {
+            float *dst = p.parts.at(part, b, i, head, p.s.dim);
+            if (tiles[t] > 0 && ok) store_row<DP>(o_row, 1.0f / l, dst, p.s.dim, write);
+            if (mine && empty)
+                for (int c = 0; c < p.s.dim; ++c) dst[c] = 0.0f;
+        } else {
+            __nv_bfloat16 *dst = p.out.data + b * p.out.batch + (long long)i * p.out.row + head * p.out.head;
+            if (tiles[t] > 0 && ok) store_row<DP>(o_row, 1.0f / l, dst, p.s.dim, write);
+            if (mine && empty) store_zeros(dst, p.s.dim);
+        }
+        if (mine) lse[i] = (m + log2f(l)) * kAttnLn2;
     }
     fence_before_sync();
     __syncthreads();
     if (warp == 9) tmem_free(tmem, 512);
+}
+
+// out and lse from the parts, a thread per 8 columns: out = sum of exp(lse_k - lse) out_k.
+__global__ void __launch_bounds__(256) attention_forward_join_kernel(const __grid_constant__ AttnForwardParams p)
+{
+    wait_for_previous();
+    const int groups = p.s.dim / 8;
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (at >= p.parts.rows * groups) return;
+    const long long row = at / groups;
+    const int c = int(at % groups) * 8, head = int(row % p.s.heads);
+    const int i = int(row / p.s.heads % p.s.q_len), b = int(row / p.s.heads / p.s.q_len);
+    const long long cell = ((long long)b * p.s.heads + head) * p.s.q_len + i, step = (long long)p.s.batch * p.s.heads * p.s.q_len;
+    float top = -INFINITY, total = 0.0f;
+    bool nan = false;
+    for (int k = 0; k < p.parts.splits; ++k) {
+        const float x = p.part_lse[k * step + cell];
+        nan = nan || x != x;
+        top = fmaxf(top, x);
+    }
+    for (int k = 0; k < p.parts.splits; ++k) total += top == -INFINITY ? 0.0f : expf(p.part_lse[k * step + cell] - top);
+    const float lse = nan ? NAN : top + logf(total);
+    float sum[8];
+    join_parts(p.parts, b, i, head, p.s.dim, c, sum, [&](int k) { return top == -INFINITY ? 0.0f : expf(p.part_lse[k * step + cell] - lse); });
+    store_group(p.out.data + b * p.out.batch + (long long)i * p.out.row + head * p.out.head + c, sum);
+    if (c == 0) p.lse[cell] = lse;
 }
 
 }  // namespace omni

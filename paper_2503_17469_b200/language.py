@@ -181,6 +181,15 @@ class Attention(_Operator):
                              f"got {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         return B.omni_attn_view(t.data_ptr(), batch, row, head)
 
+    def _scratch_bytes(self, query, a, rows, kv_len, forward: bool) -> int:
+        key = (forward, rows[0], rows[1], kv_len)
+        size = self._sizes.get(key)
+        if size is None:
+            need = C.c_uint64()
+            self._check(query(_ref(a), _ref(need)))
+            size = self._sizes[key] = need.value
+        return size
+
     def forward(self, q, k, v, q_lengths=None, kv_lengths=None, out=None, stream=None):
         """Returns (out like q, lse float32 [batch, heads, q_len])."""
         if stream is not None:
@@ -191,9 +200,12 @@ class Attention(_Operator):
         if out is None:
             out = _like(q)
         lse = q.new_empty((rows[0], self.heads, rows[1]), dtype=_float)
+        size = self._scratch_bytes(self._lib.omni_attn_forward_workspace, a, rows, keys[1], True)
+        scratch = q.new_empty(size, dtype=_byte) if size else None
         self._check(self._lib.omni_attn_forward(
             self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),
-            _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(), _current_stream()))
+            _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(),
+            scratch.data_ptr() if size else None, size, _current_stream()))
         return out, lse
 
     def backward(self, q, k, v, out, lse, grad_out, q_lengths=None, kv_lengths=None, grads=None, stream=None):
@@ -208,12 +220,8 @@ class Attention(_Operator):
             raise ValueError("lse: contiguous float32 [batch, heads, q_len] is wanted")
         if grads is None:
             grads = (_like(q), _like(k), _like(v))
-        size = self._sizes.get(rows)
-        if size is None:
-            need = C.c_uint64()
-            self._check(self._lib.omni_attn_workspace(_ref(a), _ref(need)))
-            size = self._sizes[rows] = max(16, need.value)
-        scratch = q.new_empty(size, dtype=_byte)
+        size = self._scratch_bytes(self._lib.omni_attn_workspace, a, rows, keys[1], False)
+        scratch = q.new_empty(max(16, size), dtype=_byte)
         dq, dk, dv = grads
         self._check(self._lib.omni_attn_backward(
             self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),

@@ -122,6 +122,8 @@ def tensors(batch, q_len, kv_len, heads, kv_heads, dim, seed=0):
     (1, 1, 1, 1, 1, 64), (2, 1, 700, 4, 2, 128), (1, 64, 64, 2, 1, 64), (1, 127, 129, 2, 2, 128), (1, 128, 128, 1, 1, 8),
     (2, 129, 127, 3, 1, 72), (1, 255, 257, 2, 2, 64), (3, 300, 300, 4, 1, 80), (1, 513, 400, 2, 1, 128), (1, 1100, 1100, 2, 2, 96),
     (1, 400, 1300, 4, 4, 16), (1, 1000, 65, 1, 1, 128), (70, 33, 33, 1, 1, 64),
+    # few tiles on one side: the walk along the other is split
+    (1, 5, 3000, 2, 1, 128), (2, 1, 1500, 3, 1, 64), (1, 3000, 11, 4, 1, 64), (1, 2500, 100, 2, 2, 80), (1, 300, 2600, 1, 1, 72),
 ])
 def test_against_64_bits(ctx, batch, q_len, kv_len, heads, kv_heads, dim, causal):
     run(ctx, *tensors(batch, q_len, kv_len, heads, kv_heads, dim), causal)

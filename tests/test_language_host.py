@@ -68,12 +68,12 @@ def attn(**kw):
     return B.omni_attn(*a.values())
 
 
-def attn_forward(ctx, a, lse=PTR, change=None):
+def attn_forward(ctx, a, lse=PTR, change=None, workspace=PTR, size=1 << 30):
     v = [B.omni_attn_view(PTR, 5 * 256, 256, 64), B.omni_attn_view(PTR, 7 * 128, 128, 64), B.omni_attn_view(PTR, 7 * 128, 128, 64),
          B.omni_attn_view(PTR, 5 * 256, 256, 64)]
     for i, view in (change or {}).items():
         v[i] = view
-    return B.lib().omni_attn_forward(ctx, C.byref(a), *(None if x is None else C.byref(x) for x in v), lse, None)
+    return B.lib().omni_attn_forward(ctx, C.byref(a), *(None if x is None else C.byref(x) for x in v), lse, workspace, size, None)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -99,11 +99,18 @@ def test_attention_refuses_operands(omni, view, status):
         assert attn_forward(omni._h, attn(), change={i: view}) == status
     assert attn_forward(omni._h, attn(), lse=None) == B.ERR_NULL and attn_forward(omni._h, attn(), lse=PTR + 2) == B.ERR_ALIGN
     assert attn_forward(None, attn()) == B.ERR_NULL
+    few = attn(batch=1, kv_len=5000)           # one pair of query tiles per head: the keys are split
+    keys = B.omni_attn_view(PTR, 5000 * 128, 128, 64)
+    size = C.c_uint64()
+    assert B.lib().omni_attn_forward_workspace(C.byref(few), C.byref(size)) == B.OK and size.value > 5 * 4 * 64 * 4
+    for workspace, n, status in ((None, size.value, B.ERR_NULL), (PTR + 8, size.value, B.ERR_ALIGN), (PTR, size.value - 1, B.ERR_TOO_LARGE)):
+        assert attn_forward(omni._h, few, change={1: keys, 2: keys}, workspace=workspace, size=n) == status
+    assert B.lib().omni_attn_forward_workspace(C.byref(attn(batch=100)), C.byref(size)) == B.OK and size.value == 0
 
 
 def test_attention_backward_workspace(omni):
     size = C.c_uint64()
-    assert B.lib().omni_attn_workspace(C.byref(attn()), C.byref(size)) == B.OK and size.value == 2 * 2 * 4 * 128 * 4
+    assert B.lib().omni_attn_workspace(C.byref(attn()), C.byref(size)) == B.OK and size.value >= 2 * 2 * 4 * 128 * 4
     rows, keys = C.byref(B.omni_attn_view(PTR, 5 * 256, 256, 64)), C.byref(B.omni_attn_view(PTR, 7 * 128, 128, 64))
 
     def call(workspace, n, lse=PTR):
