@@ -6,9 +6,8 @@
 // tile, which adds up dQ over the keys.  Seven products instead of five, but every sum has one owner and one order:
 // no float atomics, no zeroed and re-read dQ in float, the same bits from the same call.
 //
-// Both walk 128 x 128 tiles of S and dP in tensor memory.  (64 columns a tile would leave room for two of each,
-// but an MMA of M = 128 with both operands in shared memory takes about 75 cycles, N = 64 or 128.)  The
-// elementwise work comes in two phases, P from S and dS from P and dP, sixteen warps at 32 columns of a row per thread,
+// Both walk 128 x 128 tiles of S and dP in tensor memory.  (64 columns a tile would leave room for two of each, but an MMA
+// m128 n64 k16 with both operands in shared memory takes 48 cycles, n128 64: measured.)  The elementwise work comes in two phases, P from S and dS from P and dP, sixteen warps at 32 columns of a row per thread,
 // and each phase runs beside products of the same or the next tile:
 //   dK, dV: S^T = K Q^T and dP^T = V dO^T (128 keys x 128 queries).  P^T goes back to tensor memory over S^T as the A
 //     operand of dV += P^T dO, dS^T over dP^T as that of dK += dS^T Q.
@@ -17,6 +16,11 @@
 //     Order: S0 dP0 S1 | dP1 dQ0 S2 | dP2 dQ1 S3 | ...
 // An operand in tensor memory is overwritten by a product that is issued after the one that reads it; one thread
 // issues all of a block's, and the tensor core takes them in that order.
+// What bounds it: the chain of one tile, S, P, dV and the next S over P, about 3100 cycles a step with dK and dV where
+// the four products take 2048; then the power cap.  Measured: 8192 rows, 16 heads on 8 of 128, causal, 752 us at
+// 1965 MHz (914 TFLOP/s at five products), 870 us sustained at 1.63 GHz and 1000 W.  Tried: P and dS through shared
+// memory 1018 against 940 us then; P over dP, so that S is free earlier (Q's copies then come late) 541 against 455 us of dK, dV; a third
+// place for Q 744 against 747; exponentials by a polynomial 451-472 against 455.
 // P and dS are rounded to bfloat16 for the products; all sums are float.
 //
 // Warps 0-15: elementwise (four warps cover the 128 rows, each four another 32 columns), 16: loads, 17: MMA.

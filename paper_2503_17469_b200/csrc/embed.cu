@@ -1,7 +1,8 @@
 // Embedding lookup with scaling, and its dense gradient by sorted tokens.
 //
 // Lookup: out_i = s * W[t_i].  Pure gather: the floor is the n rows written plus the distinct rows
-// read.  A group of lanes owns a row, 8 elements (16 or 32 bytes) per lane and access.
+// read.  A group of lanes owns a row, 8 elements (16 or 32 bytes) per lane and access, two rows in flight.
+// 65536 rows of 1024 bfloat16 from a table of 50257, Zipf: 31 us, 5.3 TB/s.
 //
 // Gradient: dW_v = s * sum_{t_i = v} dy_i.  Scattered adds with atomics would leave the order of
 // the sum to chance, so the tokens are sorted first and every row of the table is then written
@@ -16,6 +17,11 @@
 //      block's rows in registers and writes a row where the id changes; runs that cross blocks are joined
 //      in block order in shared memory, those that cross CTAs leave a float partial in the workspace.
 //   3. join_runs: the CTA in which such a run starts adds its partials in order and writes the row.
+// 32768 bfloat16 rows of 768 into 50257 float rows: 29.5 us sort and zeros (154 MB), 28 us sums, 5 us joins, 62-65 us a call
+// against a floor of 31 (each input read, each output written once): the sort, 23 us by itself, waits on its barriers and
+// the zeros leave L2 while the sums run.  Small calls are bound by their three launches.
+// Tried: every CTA counting its own ids among all tokens 30 us and as much skew as the tokens have; matches by
+// __match_any_sync 31.6 against 28.5 us with nine ballots; one launch of one cluster for small batches 30.7 against 20.5 us.
 #include "context.h"
 #include "vector.cuh"
 
