@@ -1,6 +1,6 @@
 """Operators of a language model's training pass: embedding, attention, distillation loss.
 
-What a worker computes its gradients with, on torch tensors of one CUDA device.  Each class keeps an
+What a worker computes its gradients with, on torch tensors of the current CUDA device.  Each class keeps an
 operator's constants and an ``Omni`` context (launch counts, errors, the status word of bounded
 waits); its calls allocate their outputs with torch unless they are given, take scratch memory from torch's
 caching allocator, enqueue on ``stream`` (a torch stream, default the current one) and do not
@@ -41,8 +41,8 @@ def _code(t, codes, what: str) -> int:
 
 
 def _elsewhere(**tensors):
-    """For the messages of tensors that are not where the others are."""
-    return ValueError(", ".join(f"{k} on {t.device}" for k, t in tensors.items() if t is not None) + ": one CUDA device is wanted")
+    """For the messages of tensors that are not on the current device, whose stream takes the call."""
+    return ValueError(", ".join(f"{k} on {t.device}" for k, t in tensors.items() if t is not None) + ": the current CUDA device is wanted")
 
 
 def _rows(t, what: str) -> int:
@@ -97,7 +97,7 @@ class Embedding(_Operator):
             raise ValueError(f"weight: shape {tuple(self._table)} is wanted")
         if not tokens.is_contiguous():
             raise ValueError("tokens: a contiguous tensor is wanted")
-        if not tokens.is_cuda or not weight.get_device() == out.get_device() == tokens.get_device():
+        if not tokens.is_cuda or not weight.get_device() == out.get_device() == tokens.get_device() == _device():
             raise _elsewhere(tokens=tokens, weight=weight, out=out)
         self._check(self._lib.omni_embed_forward(
             self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), tokens.numel(), weight.data_ptr(),
@@ -124,7 +124,7 @@ class Embedding(_Operator):
             grad = g.new_empty(self._table, dtype=dtype)
         elif grad.shape != self._table:
             raise ValueError(f"grad: shape {tuple(self._table)} is wanted")
-        if not tokens.is_cuda or not g.get_device() == grad.get_device() == tokens.get_device():
+        if not tokens.is_cuda or not g.get_device() == grad.get_device() == tokens.get_device() == _device():
             raise _elsewhere(tokens=tokens, grad_out=g, grad=grad)
         size = self._sizes.get(n)
         if size is None:
@@ -160,7 +160,7 @@ class Attention(_Operator):
             raise ValueError("q and k: [batch, length, head, dim] is wanted")
         batch, q_len = q.shape[:2]
         kv_len = k.shape[1]
-        if not q.is_cuda:
+        if not q.is_cuda or q.get_device() != _device():
             raise _elsewhere(q=q)
         at = [None, None]
         for i, t in enumerate((q_lengths, kv_lengths)):
@@ -177,7 +177,7 @@ class Attention(_Operator):
             raise TypeError(f"{what}: dtype {t.dtype} is not bfloat16")
         batch, row, head, one = t.stride()
         if t.shape != shape or one != 1 or t.get_device() != device:
-            raise ValueError(f"{what}: shape {shape} with a contiguous last dimension on one device is wanted, "
+            raise ValueError(f"{what}: shape {shape} with a contiguous last dimension on the current device is wanted, "
                              f"got {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         return B.omni_attn_view(t.data_ptr(), batch, row, head)
 
@@ -252,7 +252,7 @@ class Distillation(_Operator):
         stride = _rows(top_logits, "top_logits")
         if _rows(top_index, "top_index") != stride:
             raise ValueError("top_logits and top_index: the same stride is wanted")
-        if not logits.is_cuda or not logits.get_device() == top_logits.get_device() == top_index.get_device():
+        if not logits.is_cuda or not logits.get_device() == top_logits.get_device() == top_index.get_device() == _device():
             raise _elsewhere(logits=logits, top_logits=top_logits, top_index=top_index)
         return B.omni_distill(logits.data_ptr(), rows, _rows(logits, "logits"), vocab, _code(logits, _DTYPES, "logits"),
                               top_logits.data_ptr(), top_index.data_ptr(), stride, top, _code(top_index, _INDEX, "top_index"),
