@@ -121,6 +121,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
     stretch_of(tiles * group, part, splits, &h0, &h1);
     const int n = h1 - h0;
     if (n == 0) {                                                   // no query sees these keys
+        wait_for_previous();                                        // a grid that is complete has to mean that both kernels are
         const int rows = min(kRows, p.s.kv_len - k0);
         if (splits > 1) {
             zero_parts(p.parts_dk, part, b, kv_head, k0, rows, p.s.dim);
@@ -179,6 +180,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
             if (!load.tile<DP>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st, valid)) break;
             ++do_armed;
         }
+        wait_for_previous();                                       // also when it gave up before the first row values
         // the block may not end with a copy in flight, not even when it gave up
         mbar_wait(kv_full, 0);
         for (int h = max(0, q_armed - ST); h < q_armed; ++h) mbar_wait(q_full + h % ST, (h / ST) & 1);
@@ -351,6 +353,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
     stretch_of(seen > 0 ? (seen + kRows - 1) / kRows : 0, part, splits, &h0, &h1);
     const int n = h1 - h0;
     if (n == 0) {                                                   // no query of the tile sees a key
+        wait_for_previous();                                        // as in attention_keys
         if (splits > 1) zero_parts(p.parts_dq, part, b, head, q0, min(kRows, p.s.q_len - q0), p.s.dim);
         else zero_tile(p.dq, b, head, q0, min(kRows, p.s.q_len - q0), p.s.dim);
         return;
