@@ -48,12 +48,12 @@ __device__ __forceinline__ void load_tile(unsigned char *dst, const CUtensorMap 
     for (int c = 0; c < DP / 64; ++c) tensor_load(dst + c * ROWS * 128, map, c * 64, head, row, batch, bar);
 }
 
-// Zeroes rows [from, 128) of a tile, by one warp; the MMA that reads it next sees the zeros.
-template <int DP> __device__ __forceinline__ void zero_rows(unsigned char *tile, int from)
+// Zeroes rows [from, to) of a tile, by one warp; the MMA that reads it next sees the zeros.
+template <int DP> __device__ __forceinline__ void zero_rows(unsigned char *tile, int from, int to)
 {
     const int lane = threadIdx.x % 32;
     for (int c = 0; c < DP / 64; ++c)
-        for (int i = from * 8 + lane; i < kRows * 8; i += 32)
+        for (int i = from * 8 + lane; i < to * 8; i += 32)
             *reinterpret_cast<uint4 *>(tile + c * kRows * 128 + i * 16) = make_uint4(0, 0, 0, 0);
     fence_async_proxy();
     __syncwarp();
@@ -69,15 +69,16 @@ struct Loader {
     __device__ __forceinline__ bool wait(unsigned long long *bar, unsigned p) { return warp_wait(bar, p, give_up, status); }
 
     // A 128 x DP tile into `dst`; `bar` gets this phase's one arrival and the bytes, `more` further bytes are on their way to
-    // it.  Rows from `valid` on lie behind the sequence's length, where the caller may have left anything, and
-    // 0 x NaN would reach the sums: such a tile is waited for here, zeroed from there on, and handed over then.
+    // it.  Rows from `valid` on lie behind the sequence's length and rows before `from` are queries that see no key; the caller
+    // may have left anything in both, and 0 x NaN would reach the sums: such a tile is waited for here, its rows outside
+    // [from, valid) are zeroed, and it is handed over then.
     template <int DP>
     __device__ __forceinline__ bool tile(unsigned char *dst, const CUtensorMap *map, int head, int row, int batch,
-                                         unsigned long long *bar, int valid, unsigned more = 0)
+                                         unsigned long long *bar, int valid, unsigned more = 0, int from = 0)
     {
         const bool first = threadIdx.x % 32 == 0;
         constexpr unsigned bytes = kRows * DP * 2;
-        if (valid >= kRows) {
+        if (valid >= kRows && from <= 0) {
             if (first) {
                 mbar_expect_tx(bar, bytes + more);
                 load_tile<DP, kRows>(dst, map, head, row, batch, bar);
@@ -94,7 +95,8 @@ struct Loader {
             return false;
         }
         parity ^= 1;
-        zero_rows<DP>(dst, valid);
+        zero_rows<DP>(dst, 0, from);
+        zero_rows<DP>(dst, valid, kRows);
         if (first) {
             if (more) mbar_expect_tx(bar, more);
             else mbar_arrive(bar);

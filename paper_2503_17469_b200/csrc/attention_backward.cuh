@@ -164,10 +164,10 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         const unsigned long long policy = policy_evict_last();
         for (int h = 0; h < n; ++h) {
             const int st = h % ST, head = kv_head * group + (h0 + h) / tiles, row = (tile0 + (h0 + h) % tiles) * kRows;
-            const int valid = p.s.q_lengths ? len.q - row : kRows;
+            const int valid = p.s.q_lengths ? len.q - row : kRows, unseeing = p.s.causal ? -len.shift - row : 0;
             const unsigned free_parity = ((h / ST) & 1) ^ 1;
             if (!load.wait(q_empty + st, free_parity)) break;
-            if (!load.tile<DP>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st, valid, 2 * kRows * 4)) break;
+            if (!load.tile<DP>(smem + L::kQ + st * L::kTile, &p.q, head, row, b, q_full + st, valid, 2 * kRows * 4, unseeing)) break;
             if (lane == 0) {
                 if (h == 0) wait_for_previous();                   // the row values are the previous kernel's
                 const long long at = ((long long)b * p.s.heads + head) * p.q_pad + row;
@@ -177,7 +177,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
             }
             ++q_armed;
             if (!load.wait(do_empty + st, free_parity)) break;
-            if (!load.tile<DP>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st, valid)) break;
+            if (!load.tile<DP>(smem + L::kDo + st * L::kTile, &p.dout, head, row, b, do_full + st, valid, 0, unseeing)) break;
             ++do_armed;
         }
         wait_for_previous();                                       // also when it gave up before the first row values
