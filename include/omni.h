@@ -476,7 +476,9 @@ int omni_attn_backward(omni_ctx *ctx, const omni_attn *a, const omni_attn_view *
  * An entry whose index is outside 0..vocab-1 (-1 by convention) is not there, one whose logit is -inf
  * has p = 0; a row without any p > 0 has no target: its loss is 0 and its gradient row is zeros (lse
  * is still written).  A student logit of -inf has probability 0 (and an infinite loss if the teacher
- * gives it p > 0).  top = 1 with T = 1 is the ordinary cross-entropy of the index.
+ * gives it p > 0; in a row of -inf throughout every token has).  Logits far from zero are taken by their distances:
+ * a row masked throughout by the type's lowest value is uniform (its lse is that value / T, -inf below float's range).
+ * top = 1 with T = 1 is the ordinary cross-entropy of the index.
  * top_logits: device float; top_index: device, both rows of `top` elements, top_stride apart. */
 typedef struct {
     const void *logits;     /* device, rows x vocab of dtype */
@@ -490,7 +492,7 @@ typedef struct {
 } omni_distill;
 #define OMNI_DISTILL_MAX_TOP 256
 /* omni_distill_forward: loss[rows] and lse[rows] (device float).
- * omni_distill_backward: grad (rows x vocab of the logits' dtype, grad_stride apart) from the kept lse
+ * omni_distill_backward: grad (rows x vocab of the logits' dtype, grad_stride apart) from the kept lse, as the float it is,
  * and grad_loss[rows] (device float; 0 for rows that do not count).  grad may be the logits' own
  * storage (same pointer and stride): each value is read before it is overwritten.
  * omni_distill_step: both in one pass over the logits (one read, one write), for a caller that knows

@@ -13,6 +13,8 @@
 // the read and the write).  Tried for the step: the row kept in shared memory by a cluster 392-448 us; a persistent ring of bulk
 // copies, the row held in it, 407-470 us: many warps from several rows hide the exponentials better than a held row saves.
 // 256 walkers and four CTAs an SM; 128 and seven 390 us, 512 and three 326 (and 137 against 133 for the loss alone).
+#include <type_traits>
+
 #include "context.h"
 #include "vector.cuh"
 
@@ -77,10 +79,16 @@ template <> struct Group<__nv_bfloat16> {
     }
 };
 
-// A thread's running maximum m and sum of 2^(x - m), x = logit * unit.  Products and sums are spelled out
-// where the compiler could contract them one way in one variant and another way in the next: forward
-// and step give the same bits.
-struct Running {
+// A thread's running maximum m and sum of exponentials over it, unit = log2(e) / T.  Near zero m = z unit, and an exponential
+// 2^(z unit - m) is one fused multiply-add: whatever the rounding of m was, the sum carries it too.  Far from zero (a row masked by
+// the type's lowest value or -1e30, say) that rounding, or an overflow, would leave nothing of the row, so such rows are
+// walked again with m = z and 2^((z - m) unit).  Differences first for every row would cost 8192 x 50257 bfloat16 338.9 instead of
+// 334.8 us a step and 3000 x 131072 142.5 instead of 139.5 us a loss.
+// Products and sums are spelled out where the compiler could contract them one way in one variant and another way in the next:
+// forward and step give the same bits.
+constexpr float kFar = 16777216.0f;                  // of a row's m: from here on its rounding is a factor of two and more
+
+template <bool FAR> struct Running {
     float m = -INFINITY;
     float2 a = {0.0f, 0.0f}, b = {0.0f, 0.0f};
     template <typename T, int K> __device__ __forceinline__ void take(const Group<T> (&g)[K], float unit)
@@ -88,14 +96,14 @@ struct Running {
         float top = g[0].largest();
 #pragma unroll
         for (int k = 1; k < K; ++k) top = fmaxf(top, g[k].largest());
-        raise(__fmul_rn(top, unit));
-        const float ref = m == -INFINITY ? 0.0f : -m;
+        raise(FAR ? top : __fmul_rn(top, unit), unit);
+        const float ref = reference(m);
         const float2 u = {unit, unit}, r = {ref, ref};
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 x = fma2(g[k].pair(i), u, r);
+                const float2 z = g[k].pair(i), x = FAR ? mul2(add2(z, r), u) : fma2(z, u, r);
                 const float2 e = {exp2_fast(x.x), exp2_fast(x.y)};
                 if (i % 2 == 0) a = add2(a, e);
                 else b = add2(b, e);
@@ -103,20 +111,23 @@ struct Running {
     }
     __device__ __forceinline__ void take_one(float z, float unit)
     {
-        const float x = __fmul_rn(z, unit);
-        raise(x);
-        a.x += exp2_fast(x - (m == -INFINITY ? 0.0f : m));
+        raise(FAR ? z : __fmul_rn(z, unit), unit);
+        a.x += exp2_fast(FAR ? __fmul_rn(__fadd_rn(z, reference(m)), unit) : __fmaf_rn(z, unit, reference(m)));
     }
-    __device__ __forceinline__ void raise(float to)
+    __device__ __forceinline__ void raise(float to, float unit)
     {
         if (to > m) {                                // rare after the first few groups
-            const float f = exp2_fast(m - to);
+            const float f = ratio(m, to, unit);
             a = mul2(a, {f, f});
             b = mul2(b, {f, f});
             m = to;
         }
     }
     __device__ __forceinline__ float sum() const { return __fadd_rn(__fadd_rn(a.x, a.y), __fadd_rn(b.x, b.y)); }
+    // what is added to an exponent; -inf - -inf would be no number
+    __device__ __forceinline__ static float reference(float m) { return m == -INFINITY ? 0.0f : -m; }
+    // of a sum over `from` to one over `to`
+    __device__ __forceinline__ static float ratio(float from, float to, float unit) { return exp2_fast(FAR ? __fmul_rn(from - to, unit) : from - to); }
 };
 
 struct Joined { float m, s; };
@@ -130,22 +141,24 @@ __device__ __forceinline__ float warp_sum(float x)
     for (int o = 16; o > 0; o /= 2) x = __fadd_rn(x, __shfl_xor_sync(~0u, x, o));
     return x;
 }
-// A warp's maximum and sum into its cell.
-__device__ __forceinline__ void put_warp(const Running &run, Joined *cell)
+// The warp's pairs of maximum and sum as one: the sum for the largest maximum.
+template <bool FAR> __device__ __forceinline__ Joined join_warp(float own, float s, float unit)
 {
-    const float m = warp_max(run.m);
-    const float s = run.sum();
-    const float t = warp_sum(m == -INFINITY || run.m == m ? s : __fmul_rn(s, exp2_fast(run.m - m)));
-    if (threadIdx.x % 32 == 0) *cell = {m, t};
+    const float m = warp_max(own);
+    return {m, warp_sum(m == -INFINITY || own == m ? s : __fmul_rn(s, Running<FAR>::ratio(own, m, unit)))};
 }
-
-// The walkers' cells joined, by every warp for itself: the sum for the largest maximum.
-template <int N> __device__ __forceinline__ Joined join_cells(const Joined (&cell)[N], int n = N)
+// A warp's maximum and sum into its cell.
+template <bool FAR> __device__ __forceinline__ void put_warp(const Running<FAR> &run, float unit, Joined *cell)
+{
+    const Joined w = join_warp<FAR>(run.m, run.sum(), unit);
+    if (threadIdx.x % 32 == 0) *cell = w;
+}
+// The walkers' cells joined, by every warp for itself.
+template <bool FAR> __device__ __forceinline__ Joined join_cells(const Joined *cell, int n, float unit)
 {
     const int lane = threadIdx.x % 32;
     const Joined x = lane < n ? cell[lane] : Joined{-INFINITY, 0.0f};
-    const float m = warp_max(x.m);
-    return {m, warp_sum(m == -INFINITY || x.m == m ? x.s : __fmul_rn(x.s, exp2_fast(x.m - m)))};
+    return join_warp<FAR>(x.m, x.s, unit);
 }
 
 // Element range of a row in three parts: up to the first 16-byte boundary, whole groups, the rest.
@@ -165,7 +178,8 @@ template <typename T> struct Parts {
 struct Teacher {
     float prob[OMNI_DISTILL_MAX_TOP], hit[OMNI_DISTILL_MAX_TOP];
     int place[OMNI_DISTILL_MAX_TOP];
-    float term;                                     // sum of p (log p - z / T)
+    float best;                                     // the largest of the student's logits there, if it is finite, else 0
+    float term;                                     // sum of p (log p - (z - best) / T)
     int target;                                     // some entry has a probability
     int repeated;                                   // some place is named twice
 };
@@ -176,7 +190,7 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
 {
     const int lane = threadIdx.x % 32;
     const float *logit = p.top_logits + r * p.top_stride;
-    float top = -INFINITY;
+    float top = -INFINITY, best = -INFINITY;
     int table = 32;                                 // at least twice the entries
     while (table < 2 * p.top) table *= 2;
     for (int j = lane; j < table; j += 32) seen[j] = -1;
@@ -190,6 +204,7 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
         te.hit[j] = there ? to_float(row[i]) : 0.0f;
         te.prob[j] = t;
         top = fmaxf(top, t);
+        if (there) best = fmaxf(best, te.hit[j]);
         for (int h = int(unsigned(i) * 2654435769u >> 16) & (table - 1); there; h = (h + 1) & (table - 1)) {
             const int old = atomicCAS(&seen[h], -1, int(i));
             repeated |= old == int(i);
@@ -198,6 +213,8 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
     }
     repeated = __any_sync(~0u, repeated);
     top = warp_max(top);
+    best = warp_max(best);
+    if (!isfinite(best)) best = 0.0f;
     float total = 0.0f;
     for (int j = lane; j < p.top; j += 32) {
         const float e = top == -INFINITY && !isnan(te.prob[j]) ? 0.0f : expf(te.prob[j] - top);
@@ -210,10 +227,11 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
     for (int j = lane; j < p.top; j += 32) {
         const float q = target ? te.prob[j] / total : 0.0f;
         te.prob[j] = q;
-        if (!(q == 0.0f)) term = __fadd_rn(term, __fmul_rn(q, logf(q) - te.hit[j] / p.temperature));
+        if (!(q == 0.0f)) term = __fadd_rn(term, __fmul_rn(q, logf(q) - __fsub_rn(te.hit[j], best) / p.temperature));
     }
     term = warp_sum(term);
     if (lane == 0) {
+        te.best = best;
         te.term = term;
         te.target = target;
         te.repeated = repeated;
@@ -221,10 +239,29 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
     __syncwarp();
 }
 
+// share * 2^((z times + add) unit) of a logit z: gain (the row's weight times T) times the student's probability of the token.  From
+// the row's own maximum and sum near zero (u, -m, 1, gain / s) and far from it (1, -m, u, gain / s), with u = log2(e) / T; from a kept
+// lse (1 / T, -lse, log2(e), gain), where the difference comes first too, and a product with 1 / T that is rounded once
+// with it is exact if T is a power of two.  NEAR: unit is 1.
+template <bool NEAR> struct Softmax {
+    float times, add, unit, share;
+    __device__ __forceinline__ float operator()(float z) const
+    {
+        const float x = __fmaf_rn(z, times, add);
+        return __fmul_rn(exp2_fast(NEAR ? x : __fmul_rn(x, unit)), share);
+    }
+    __device__ __forceinline__ float2 operator()(float2 z) const
+    {
+        float2 x = fma2(z, {times, times}, {add, add});
+        if (!NEAR) x = mul2(x, {unit, unit});
+        return mul2({exp2_fast(x.x), exp2_fast(x.y)}, {share, share});
+    }
+};
+
 // The gradient at the teacher's entries, over what the walk wrote there; an entry that names a token again is
-// left to the first.  `ref`: minus the lse in powers of two.
-template <typename T>
-__device__ __forceinline__ void put_entries(const DistillParams &p, const Teacher &te, T *out, float gain, float unit, float ref, int from, int step)
+// left to the first.
+template <typename T, bool NEAR>
+__device__ __forceinline__ void put_entries(const DistillParams &p, const Teacher &te, T *out, float gain, const Softmax<NEAR> &q, int from, int step)
 {
     for (int j = from; j < p.top; j += step) {
         const int at = te.place[j];
@@ -239,27 +276,21 @@ __device__ __forceinline__ void put_entries(const DistillParams &p, const Teache
                     total += te.prob[i];
                 }
         }
-        if (first) out[at] = from_float<T>(gain * (exp2_fast(fmaf(te.hit[j], unit, ref)) - total));
+        if (first) out[at] = from_float<T>(__fmaf_rn(-gain, total, q(te.hit[j])));
     }
 }
 
-// gain * 2^(logit * unit + ref) of a group, stored.
-template <typename T>
-__device__ __forceinline__ void put_group(T *dst, const Group<T> &g, float unit, float ref, float gain)
+template <typename T, bool NEAR>
+__device__ __forceinline__ void put_group(T *dst, const Group<T> &g, const Softmax<NEAR> &q)
 {
     float f[kGroup];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 x = fma2(g.pair(i), {unit, unit}, {ref, ref});
-        const float2 y = mul2({exp2_fast(x.x), exp2_fast(x.y)}, {gain, gain});
+        const float2 y = q(g.pair(i));
         f[2 * i] = y.x;
         f[2 * i + 1] = y.y;
     }
     store_streaming(dst, f);
-}
-template <typename T> __device__ __forceinline__ T put_value(T z, float unit, float ref, float gain)
-{
-    return from_float<T>(__fmul_rn(exp2_fast(fmaf(to_float(z), unit, ref)), gain));
 }
 __device__ __forceinline__ bool same_phase(const void *a, const void *b)
 {
@@ -270,76 +301,126 @@ __device__ __forceinline__ bool same_phase(const void *a, const void *b)
 
 constexpr int kRowWalkers = 256;
 
+// What every thread of a row's CTA knows.
+template <typename T> struct Row {
+    const T *row;
+    Parts<T> parts;
+    int walkers, vocab;
+    __device__ __forceinline__ Row(const DistillParams &p)
+        : row(static_cast<const T *>(p.logits) + blockIdx.x * p.row_stride), parts(row, p.vocab), walkers(blockDim.x - 32), vocab(p.vocab) {}
+    // the thread's element outside the groups, or -1
+    __device__ __forceinline__ int edge() const { return int(threadIdx.x) < vocab - parts.groups * kGroup ? parts.edge(threadIdx.x) : -1; }
+};
+
+// f(first group, groups) over the groups of a thread: AHEAD at a time, then one by one.
+template <int AHEAD, typename T, typename F> __device__ __forceinline__ void walk(const Row<T> &w, F f)
+{
+    int g = threadIdx.x;
+    if constexpr (AHEAD > 1) {
+        for (; g + (AHEAD - 1) * w.walkers < w.parts.groups; g += w.walkers * AHEAD) {
+            Group<T> x[AHEAD];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) x[a].load(w.row + w.parts.head + (long long)(g + a * w.walkers) * kGroup);
+            f(g, x);
+        }
+    }
+    for (; g < w.parts.groups; g += w.walkers) {
+        Group<T> x[1];
+        x[0].load(w.row + w.parts.head + (long long)g * kGroup);
+        f(g, x);
+    }
+}
+
+// The walkers' maxima and sums into their warps' cells.
+template <bool FAR, int AHEAD, typename T>
+__device__ __forceinline__ void reduce_row(const Row<T> &w, float unit, Joined *cell)
+{
+    Running<FAR> run;
+    walk<AHEAD>(w, [&](int, const auto &x) { run.take(x, unit); });
+    if (w.edge() >= 0) run.take_one(to_float(w.row[w.edge()]), unit);
+    __syncwarp();
+    put_warp(run, unit, cell + threadIdx.x / 32);
+}
+
+// The gradient of the row, by the whole CTA.
+template <int AHEAD, typename T, bool NEAR>
+__device__ __forceinline__ void put_row(const DistillParams &p, const Row<T> &w, const Teacher &te, const Softmax<NEAR> &q, float gain)
+{
+    T *out = static_cast<T *>(p.grad) + blockIdx.x * p.grad_stride;
+    const int tid = threadIdx.x, walkers = w.walkers;
+    const bool target = te.target;
+    if (tid < walkers) {
+        if (!target) {
+            for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(0.0f);
+        } else if (same_phase(out, w.row)) {
+            walk<AHEAD>(w, [&](int g, const auto &x) {
+#pragma unroll
+                for (int a = 0; a < int(sizeof x / sizeof x[0]); ++a)
+                    put_group(out + w.parts.head + (long long)(g + a * walkers) * kGroup, x[a], q);
+            });
+            if (w.edge() >= 0) out[w.edge()] = from_float<T>(q(to_float(w.row[w.edge()])));
+        } else {
+            for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(q(to_float(w.row[v])));
+        }
+    }
+    __syncthreads();
+    if (target) put_entries(p, te, out, gain, q, tid, blockDim.x);
+}
+
+// A row far from zero from its start, by the whole CTA.
+template <typename T, int MODE> __device__ __forceinline__ void far_row(const DistillParams &p, const Teacher &te, Joined *cell)
+{
+    const Row<T> w(p);
+    const float unit = kLog2e / p.temperature;
+    __syncthreads();                                // the cells have been read
+    if (int(threadIdx.x) < w.walkers) reduce_row<true, 1>(w, unit, cell);
+    __syncthreads();
+    const Joined all = join_cells<true>(cell, w.walkers / 32, unit);
+    const bool nothing = all.m == -INFINITY && all.s == 0.0f;         // a row of -inf: no token has a probability
+    if (threadIdx.x == 0) {
+        const float log_sum = __fmul_rn(log2f(all.s), kLn2), t = p.temperature;
+        p.lse_out[blockIdx.x] = __fadd_rn(all.m / t, log_sum);
+        const float ahead = nothing ? 0.0f : __fadd_rn(__fsub_rn(all.m, te.best) / t, log_sum);
+        p.loss[blockIdx.x] = te.target ? __fmul_rn(__fmul_rn(t, t), __fadd_rn(te.term, ahead)) : 0.0f;
+    }
+    if constexpr (MODE == kStep) {
+        const float gain = __fmul_rn(p.grad_loss[blockIdx.x], p.temperature);
+        put_row<1>(p, w, te, Softmax<false>{1.0f, Running<true>::reference(all.m), unit, nothing ? 0.0f : gain / all.s}, gain);
+    }
+}
+
 template <typename T, typename I, int MODE>
-__global__ void __launch_bounds__(kRowWalkers + 32, 4) row_kernel(DistillParams p)
+__global__ void __launch_bounds__(kRowWalkers + 32, 4) row_kernel(const __grid_constant__ DistillParams p)
 {
     __shared__ Joined cell[kRowWalkers / 32];
     __shared__ Teacher te;
     __shared__ int seen[2 * OMNI_DISTILL_MAX_TOP];
     constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;  // groups a thread has in flight
-    const int walkers = blockDim.x - 32, tid = threadIdx.x, warp = tid / 32;
+    const Row<T> w(p);
     const unsigned long long r = blockIdx.x;
-    const T *row = static_cast<const T *>(p.logits) + r * p.row_stride;
     const float unit = kLog2e / p.temperature;
-    const Parts<T> parts(row, p.vocab);
-    const int rest = p.vocab - parts.groups * kGroup;
-    // f(first group, groups): kAhead at a time, then one by one
-    auto walk = [&](auto f) {
-        int g = tid;
-        for (; g + (kAhead - 1) * walkers < parts.groups; g += walkers * kAhead) {
-            Group<T> x[kAhead];
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) x[a].load(row + parts.head + (long long)(g + a * walkers) * kGroup);
-            f(g, x);
-        }
-        for (; g < parts.groups; g += walkers) {
-            Group<T> x[1];
-            x[0].load(row + parts.head + (long long)g * kGroup);
-            f(g, x);
-        }
-    };
     const float weight = MODE == kForward ? 0.0f : p.grad_loss[r];
-    float lse2 = MODE == kBackward ? __fmul_rn(p.lse_in[r], kLog2e) : 0.0f;
-    if (tid >= walkers) {
-        teacher_warp<T, I>(p, r, row, te, seen);
-    } else if constexpr (MODE != kBackward) {
-        Running run;
-        walk([&](int, const auto &x) { run.take(x, unit); });
-        if (tid < rest) run.take_one(to_float(row[parts.edge(tid)]), unit);
-        __syncwarp();
-        put_warp(run, cell + warp);
-    }
+    const float lse = MODE == kBackward ? p.lse_in[r] : 0.0f;
+    if (int(threadIdx.x) >= w.walkers) teacher_warp<T, I>(p, r, w.row, te, seen);
+    else if constexpr (MODE != kBackward) reduce_row<false, kAhead>(w, unit, cell);
     __syncthreads();
-    const bool target = te.target;
-    if constexpr (MODE != kBackward) {
-        const Joined all = join_cells(cell, walkers / 32);
-        lse2 = all.m + log2f(all.s);
-        if (tid == 0) {
-            const float lse = __fmul_rn(lse2, kLn2);
-            p.lse_out[r] = lse;
-            p.loss[r] = target ? __fmul_rn(__fmul_rn(p.temperature, p.temperature), __fadd_rn(te.term, lse)) : 0.0f;
+    const float gain = __fmul_rn(weight, p.temperature);
+    if constexpr (MODE == kBackward) {
+        put_row<kAhead>(p, w, te, Softmax<false>{1.0f / p.temperature, lse == -INFINITY ? 0.0f : -lse, kLog2e, gain}, gain);
+    } else {
+        const Joined all = join_cells<false>(cell, w.walkers / 32, unit);     // every warp finds the same
+        if (!(fabsf(all.m) < kFar)) {
+            far_row<T, MODE>(p, te, cell);
+            return;
         }
-    }
-    if constexpr (MODE != kForward) {
-        T *out = static_cast<T *>(p.grad) + r * p.grad_stride;
-        const float gain = __fmul_rn(weight, p.temperature);
-        const float ref = lse2 == -INFINITY ? 0.0f : -lse2;
-        if (tid < walkers) {
-            if (!target) {
-                for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(0.0f);
-            } else if (same_phase(out, row)) {
-                walk([&](int g, const auto &x) {
-#pragma unroll
-                    for (int a = 0; a < int(sizeof x / sizeof x[0]); ++a)
-                        put_group(out + parts.head + (long long)(g + a * walkers) * kGroup, x[a], unit, ref, gain);
-                });
-                if (tid < rest) out[parts.edge(tid)] = put_value(row[parts.edge(tid)], unit, ref, gain);
-            } else {
-                for (int v = tid; v < p.vocab; v += walkers) out[v] = put_value(row[v], unit, ref, gain);
-            }
+        if (threadIdx.x == 0) {
+            const float log_sum = log2f(all.s);
+            p.lse_out[r] = __fmul_rn(__fadd_rn(all.m, log_sum), kLn2);
+            // the lse less the logit that the teacher's term is measured from: what is added up is all distances
+            const float ahead = __fmul_rn(__fadd_rn(__fmaf_rn(-te.best, unit, all.m), log_sum), kLn2);
+            p.loss[r] = te.target ? __fmul_rn(__fmul_rn(p.temperature, p.temperature), __fadd_rn(te.term, ahead)) : 0.0f;
         }
-        __syncthreads();
-        if (target) put_entries(p, te, out, gain, unit, ref, tid, blockDim.x);
+        if constexpr (MODE == kStep) put_row<kAhead>(p, w, te, Softmax<true>{unit, -all.m, 1.0f, gain / all.s}, gain);
     }
 }
 
