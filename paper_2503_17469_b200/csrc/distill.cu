@@ -199,7 +199,7 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
     for (int j = lane; j < p.top; j += 32) {
         const long long i = load_index<I>(p.top_index, r * p.top_stride + j);
         const bool there = i >= 0 && i < p.vocab;
-        const float t = there ? logit[j] / p.temperature : -INFINITY;
+        const float t = there ? logit[j] : -INFINITY;
         te.place[j] = there ? int(i) : -1;
         te.hit[j] = there ? to_float(row[i]) : 0.0f;
         te.prob[j] = t;
@@ -217,7 +217,8 @@ __device__ __forceinline__ void teacher_warp(const DistillParams &p, unsigned lo
     if (!isfinite(best)) best = 0.0f;
     float total = 0.0f;
     for (int j = lane; j < p.top; j += 32) {
-        const float e = top == -INFINITY && !isnan(te.prob[j]) ? 0.0f : expf(te.prob[j] - top);
+        // the difference first: entries at the type's lowest value throughout would overflow at T < 1 and not be there
+        const float e = top == -INFINITY && !isnan(te.prob[j]) ? 0.0f : expf(__fsub_rn(te.prob[j], top) / p.temperature);
         te.prob[j] = e;
         total += e;
     }

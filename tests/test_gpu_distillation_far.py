@@ -101,3 +101,17 @@ def test_a_row_of_minus_infinity(ctx, dtype):
     want = torch.zeros(VOCAB, dtype=torch.float64, device="cuda").scatter_add_(0, i[3], torch.softmax(t[3].double() / 2, 0)) * gl[3].double() * -2
     for g in (grad, d.backward(z, t, i, lse, gl)):
         assert bool(((g[3].double() - want).abs() <= (2.0 ** -19 + ROUND[dtype]) * want.abs()).all())
+
+@pytest.mark.parametrize("temp", [1.0, 0.5])
+def test_a_teacher_of_lowest_values_is_uniform(ctx, temp):
+    z, t, i, gl = inputs(F32, 2)
+    z, i = z.nan_to_num().clamp(-10, 10), i.clone()
+    t[0] = torch.finfo(F32).min
+    t[1] = torch.finfo(F32).min
+    t[1, 2] = -math.inf
+    d = L.Distillation(ctx, temp)
+    even = t.clone()
+    even[0], even[1] = 0.0, 0.0
+    even[1, 2] = -math.inf
+    for a, b in zip(d.step(z, t, i, gl), d.step(z, even, i, gl)):
+        assert torch.equal(a, b)                                   # distances from the largest entry are what counts
