@@ -46,12 +46,12 @@ def _elsewhere(**tensors):
 
 
 def _rows(t, what: str) -> int:
-    """Stride between the rows of a matrix whose rows are contiguous."""
+    """Stride between the rows of a matrix whose rows are contiguous; that of a single row is its length, whatever it was cut from."""
     n, m = t.shape
     stride, one = t.stride()
     if one != 1 and m > 1:
         raise ValueError(f"{what}: contiguous rows are wanted, got strides {t.stride()}")
-    return stride if stride >= m or n > 1 else m
+    return stride if n > 1 else m
 
 
 # The checks below stand in the calls themselves, without helpers and keyword arguments, and a
