@@ -113,8 +113,11 @@ class Embedding(_Operator):
             with self._on_stream(stream):
                 return self.backward(tokens, grad_out, dtype, grad, accumulate)
         n = tokens.numel()
-        g = grad_out if grad_out.dim() == 2 else grad_out.view(n, self.dim)
-        if g.shape != (n, self.dim):
+        try:
+            g = grad_out if grad_out.dim() == 2 else grad_out.view(n, self.dim)
+        except RuntimeError:           # other sizes, or strides that are no matrix's
+            g = None
+        if g is None or g.shape != (n, self.dim):
             raise ValueError(f"grad_out: {n} rows of {self.dim} are wanted")
         if not tokens.is_contiguous():
             raise ValueError("tokens: a contiguous tensor is wanted")
