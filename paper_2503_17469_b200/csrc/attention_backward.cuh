@@ -303,13 +303,18 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         const int half = warp / 4 % 2, d0 = half * (DP / 2);
         const unsigned from_tmem = (values ? dv_at : dk_at) + lanes + d0;
         const float gain = values ? 1.0f : p.s.scale;
-        const bool mine = ok && j < p.s.kv_len;
+        // a key behind the length has P = 0 throughout, but a row of dO may hold NaN
+        const bool mine = ok && j < p.s.kv_len, seen = j < len.kv;
+        const int cols = min(DP / 2, p.s.dim - d0);
         if (splits > 1) {
             float *dst = (values ? p.parts_dv : p.parts_dk).at(part, b, j, kv_head, p.s.dim) + d0;
-            if (ok) store_row<DP / 2>(from_tmem, gain, dst, p.s.dim - d0, mine);
+            if (ok) store_row<DP / 2>(from_tmem, gain, dst, cols, mine && seen);
+            if (mine && !seen)
+                for (int c = 0; c < cols; ++c) dst[c] = 0.0f;
         } else {
             __nv_bfloat16 *dst = o.data + b * o.batch + (long long)j * o.row + kv_head * o.head + d0;
-            if (ok) store_row<DP / 2>(from_tmem, gain, dst, p.s.dim - d0, mine);
+            if (ok) store_row<DP / 2>(from_tmem, gain, dst, cols, mine && seen);
+            if (mine && !seen) store_zeros(dst, cols);
         }
     }
     fence_before_sync();

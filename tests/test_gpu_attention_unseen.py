@@ -35,3 +35,21 @@ def test_queries_without_keys_may_hold_anything(dim, q_len, kv_len, q_lengths, k
     assert torch.equal(out, out2) and torch.equal(lse, lse2)
     assert all(torch.equal(x, y) for x, y in zip(want, got))
     ctx.stats()
+
+
+@pytest.mark.parametrize("dim", [16, 64, 80, 128])
+@pytest.mark.parametrize("batch,q_len,kv_len", [(3, 200, 200), (2, 3000, 70)])
+def test_what_stands_behind_the_lengths_stays_zero_beside_a_nan(dim, batch, q_len, kv_len):
+    """A NaN in the output's gradient belongs to the keys that its query sees, not to the padding behind them."""
+    ctx = B.Omni(1, 1, 1, 1)
+    q, k, v, do = tensors(batch, q_len, kv_len, 4, 2, dim, 95)
+    n = torch.tensor([60, 9, 33][:batch], dtype=torch.int32, device="cuda")
+    a = L.Attention(ctx, 4, 2, dim, causal=False)
+    out, lse = a.forward(q, k, v, n, n)
+    want = a.backward(q, k, v, out, lse, do, n, n)
+    do[0, 3] = math.nan
+    got = a.backward(q, k, v, out, lse, do, n, n)
+    for x, y in zip(want, got):
+        assert torch.equal(x[1:], y[1:]) and not bool(y[0, 60:].any())
+        assert bool(y[0, :60].isnan().any())
+    ctx.stats()
