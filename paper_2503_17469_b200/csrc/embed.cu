@@ -634,9 +634,11 @@ int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, u
     if (!accumulate) {
         const uint64_t want = o.row_bytes * vocab / 65536 + 1, most = 2ull * dev.sm_count;
         zero_ctas = int(round_up(want < most ? want : most, o.ranks));
-        // blocks of the next kernel that wait beside a long run of zeros take its place on the SMs: 1500 x 99 into 331 rows
-        // 26.6 us without an early start, 20.5 with it; 32768 x 768 into 50257 rows 63.2 and 70.7
-        o.overlap = o.overlap && o.row_bytes * vocab < (16u << 20);
+        // Blocks of the sums that wait beside the sort and the zeros are there at once when those end, but take their place on the
+        // SMs meanwhile: worth it while both are short.  Without / with an early start, us a call: 8192 tokens into 331 x 99 floats
+        // 19.7 / 18.4, into 8192 x 128 29.2 / 28.6; 32768 tokens into 2048 x 128 36.7 / 38.4, into 8192 x 512 44.3 / 48.4; into 50257 x 768
+        // 1500 tokens 44.8 / 51.6, 32768 62.9 / 70.3.  (Adding to the table, with nothing to set to zero: even at every size.)
+        o.overlap = o.overlap && n <= 8 * kSortPerCta && o.row_bytes * vocab < (16u << 20);
     }
     rc = with_index(index_type, [&](auto *ip) {
         using I = std::remove_pointer_t<decltype(ip)>;
