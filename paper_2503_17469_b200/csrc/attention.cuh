@@ -39,13 +39,13 @@ __device__ __forceinline__ Place place_of(int block, int heads, int batch)
 
 struct OutView { __nv_bfloat16 *data; long long batch, row, head; };
 
-// Rows x DP tile as blocks of 64 columns, each ROWS x 128 bytes.
-template <int DP, int ROWS>
+// 128 x DP tile as blocks of 64 columns, each 128 rows of 128 bytes.
+template <int DP>
 __device__ __forceinline__ void load_tile(unsigned char *dst, const CUtensorMap *map, int head, int row, int batch,
                                           unsigned long long *bar)
 {
 #pragma unroll
-    for (int c = 0; c < DP / 64; ++c) tensor_load(dst + c * ROWS * 128, map, c * 64, head, row, batch, bar);
+    for (int c = 0; c < DP / 64; ++c) tensor_load(dst + c * kRows * 128, map, c * 64, head, row, batch, bar);
 }
 
 // Zeroes rows [from, to) of a tile, by one warp; the MMA that reads it next sees the zeros.
@@ -81,13 +81,13 @@ struct Loader {
         if (valid >= kRows && from <= 0) {
             if (first) {
                 mbar_expect_tx(bar, bytes + more);
-                load_tile<DP, kRows>(dst, map, head, row, batch, bar);
+                load_tile<DP>(dst, map, head, row, batch, bar);
             }
             return true;
         }
         if (first) {
             mbar_expect_tx(own, bytes);
-            load_tile<DP, kRows>(dst, map, head, row, batch, own);
+            load_tile<DP>(dst, map, head, row, batch, own);
         }
         __syncwarp();
         if (!wait(own, parity)) {
@@ -106,24 +106,24 @@ struct Loader {
     }
 };
 
-// d[128 x N] (+)= A B^T, both tiles with the contraction along their rows' DP columns; RA, RB rows per block.
-template <int DP, int RA, int RB, int N>
-__device__ __forceinline__ void mma_along(unsigned d, unsigned a, unsigned b, bool add)
+// d[128 x 128] = A B^T, both tiles with the contraction along their rows' DP columns.
+template <int DP>
+__device__ __forceinline__ void mma_along(unsigned d, unsigned a, unsigned b)
 {
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
-        const unsigned ka = a + (k / 4) * RA * 128 + (k % 4) * 32, kb = b + (k / 4) * RB * 128 + (k % 4) * 32;
-        mma_ss(d, tile_desc(ka, 1024, 16), tile_desc(kb, 1024, 16), mma_kind(N, false, false), add || k > 0);
+        const unsigned at = (k / 4) * kRows * 128 + (k % 4) * 32;
+        mma_ss(d, tile_desc(a + at, 1024, 16), tile_desc(b + at, 1024, 16), mma_kind(kRows, false), k > 0);
     }
 }
-// d[128 x DP] (+)= P B, P [128 x K] bfloat16 in tensor memory, B a tile of RB rows, of which K are contracted over.
+// d[128 x DP] (+)= P B, P [128 x K] bfloat16 in tensor memory, B a tile of whose rows K are contracted over.
 // P stands in stretches of RUN values, each at the start of the RUN columns whose scores it came from.
-template <int DP, int RB, int K, int RUN>
+template <int DP, int K, int RUN>
 __device__ __forceinline__ void mma_tmem_across(unsigned d, unsigned p, unsigned b, bool add)
 {
 #pragma unroll
     for (int k = 0; k < K / 16; ++k)
-        mma_ts(d, p + k * 16 / RUN * RUN + k * 16 % RUN / 2, tile_desc(b + k * 2048, 1024, RB * 128), mma_kind(DP, false, true), add || k > 0);
+        mma_ts(d, p + k * 16 / RUN * RUN + k * 16 % RUN / 2, tile_desc(b + k * 2048, 1024, kRows * 128), mma_kind(DP, true), add || k > 0);
 }
 
 // Two floats to bfloat16, the first in the low half, in one instruction.

@@ -157,8 +157,8 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
         if (lane == 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
             mbar_expect_tx(kv_full, 2 * L::kTile);
-            load_tile<DP, kRows>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
-            load_tile<DP, kRows>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
+            load_tile<DP>(smem + L::kK, &p.k, kv_head, k0, b, kv_full);
+            load_tile<DP>(smem + L::kV, &p.v, kv_head, k0, b, kv_full);
         }
         int q_armed = 0, do_armed = 0;
         const unsigned long long policy = policy_evict_last();
@@ -195,7 +195,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
                 const int st = h % ST;
                 if (!wait(q_full + st, (h / ST) & 1)) return false;
                 fence_after_sync();
-                mma_along<DP, kRows, kRows, kRows>(s_at, k, q0 + st * L::kTile, false);
+                mma_along<DP>(s_at, k, q0 + st * L::kTile);
                 mma_commit(s_full);
                 return true;
             };
@@ -203,7 +203,7 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
                 const int st = h % ST;
                 if (!wait(do_full + st, (h / ST) & 1)) return false;
                 fence_after_sync();
-                mma_along<DP, kRows, kRows, kRows>(dp_at, v, do0 + st * L::kTile, false);
+                mma_along<DP>(dp_at, v, do0 + st * L::kTile);
                 mma_commit(dp_full);
                 return true;
             };
@@ -212,12 +212,12 @@ template <int DP> __device__ __forceinline__ void attention_keys(const AttnBackw
                 const int st = h % ST;
                 if (!(ok = wait(p_ready, h & 1))) break;
                 fence_after_sync();
-                mma_tmem_across<DP, kRows, kRows, kCols>(dv_at, s_at, do0 + st * L::kTile, h > 0);
+                mma_tmem_across<DP, kRows, kCols>(dv_at, s_at, do0 + st * L::kTile, h > 0);
                 mma_commit(do_empty + st);
                 if (h + 1 < n && !(ok = scores(h + 1))) break;
                 if (!(ok = wait(ds_ready, h & 1))) break;
                 fence_after_sync();
-                mma_tmem_across<DP, kRows, kRows, kCols>(dk_at, dp_at, q0 + st * L::kTile, h > 0);
+                mma_tmem_across<DP, kRows, kCols>(dk_at, dp_at, q0 + st * L::kTile, h > 0);
                 mma_commit(q_empty + st);
                 if (h + 1 < n) ok = slopes(h + 1);
             }
@@ -386,8 +386,8 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
         if (lane == 0) {
             prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v); prefetch_map(&p.dout);
             mbar_expect_tx(q_full, 2 * L::kTile);
-            load_tile<DP, kRows>(smem + L::kQ, &p.q, head, q0, b, q_full);
-            load_tile<DP, kRows>(smem + L::kDo, &p.dout, head, q0, b, q_full);
+            load_tile<DP>(smem + L::kQ, &p.q, head, q0, b, q_full);
+            load_tile<DP>(smem + L::kDo, &p.dout, head, q0, b, q_full);
         }
         int k_armed = 0, v_armed = 0;
         for (int h = 0; h < n; ++h) {
@@ -414,7 +414,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
                 const int st = h % KS;
                 if (!wait(k_full + st, (h / KS) & 1)) return false;
                 fence_after_sync();
-                mma_along<DP, kRows, kRows, kRows>(s_at + (h & 1) * kRows, q, k0 + st * L::kTile, false);
+                mma_along<DP>(s_at + (h & 1) * kRows, q, k0 + st * L::kTile);
                 mma_commit(s_full + (h & 1));
                 return true;
             };
@@ -422,7 +422,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
                 const int st = h % VS;
                 if (!wait(v_full + st, (h / VS) & 1)) return false;
                 fence_after_sync();
-                mma_along<DP, kRows, kRows, kRows>(dp_at, d, v0 + st * L::kTile, false);
+                mma_along<DP>(dp_at, d, v0 + st * L::kTile);
                 mma_commit(dp_full);
                 mma_commit(v_empty + st);
                 return true;
@@ -433,7 +433,7 @@ template <int DP> __device__ __forceinline__ void attention_queries(const AttnBa
                 if (h + 1 < n && !(ok = wait(dp_read, h & 1) && slopes(h + 1))) break;
                 if (!(ok = wait(ds_ready, h & 1))) break;
                 fence_after_sync();
-                mma_tmem_across<DP, kRows, kRows, kCols>(dq_at, s_at + (h & 1) * kRows, k0 + st * L::kTile, h > 0);
+                mma_tmem_across<DP, kRows, kCols>(dq_at, s_at + (h & 1) * kRows, k0 + st * L::kTile, h > 0);
                 mma_commit(k_empty + st);
                 if (h + 2 < n) ok = scores(h + 2);
             }

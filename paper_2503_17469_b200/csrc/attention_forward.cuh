@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                 prefetch_map(&p.q); prefetch_map(&p.k); prefetch_map(&p.v);
                 const int q_tiles = tiles[1] > 0 ? 2 : 1;
                 mbar_expect_tx(q_full, q_tiles * L::kTile);
-                for (int t = 0; t < q_tiles; ++t) load_tile<DP, kRows>(smem + L::kQ + t * L::kTile, &p.q, head, q0 + t * kRows, b, q_full);
+                for (int t = 0; t < q_tiles; ++t) load_tile<DP>(smem + L::kQ + t * L::kTile, &p.q, head, q0 + t * kRows, b, q_full);
             }
             int kj = 0, vj = 0;                                       // copies armed
             for (int j = 0; j < n; ++j) {
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (tiles[t] > 0) {
-                        mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k, false);
+                        mma_along<DP>(s_at + t * kRows, q + t * L::kTile, k);
                         mma_commit(s_full + t);
                     }
                 mma_commit(k_empty);
@@ -159,13 +159,13 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attention_forward_kernel(c
                         ok = ok && wait(p_ready + kParts * t + part, j & 1);
                         if (!ok) break;
                         fence_after_sync();
-                        mma_tmem_across<DP, kRows, kPart, kPart>(o_at + t * DP, s_at + t * kRows + part * kPart / 2,
+                        mma_tmem_across<DP, kPart, kPart>(o_at + t * DP, s_at + t * kRows + part * kPart / 2,
                                                                  v + st * L::kTile + part * kPart * 128, j > 0 || part > 0);
                     }
                     if (!ok) break;
                     // the next scores go over P: the tensor core takes MMAs in order
                     if (j + 1 < tiles[t]) {
-                        mma_along<DP, kRows, kRows, kRows>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile, false);
+                        mma_along<DP>(s_at + t * kRows, q + t * L::kTile, k + next * L::kTile);
                         mma_commit(s_full + t);
                     } else {
                         mma_commit(o_full + t);

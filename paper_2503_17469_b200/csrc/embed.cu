@@ -34,6 +34,8 @@ constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortPerCta = 1024;   // tokens that make another CTA worth its barriers
 constexpr int kBlock = 32;          // sorted tokens per block
 constexpr int kThreads = 256;
+constexpr int kRunLanes = 32;       // of a block of sorted tokens, however narrow the rows: 32768 rows of 8 floats took 126 us with a lane a block
+constexpr int kRunsPer = kThreads / kRunLanes;      // blocks per CTA
 constexpr int kBatch = 4;           // accesses in flight per lane
 constexpr int kJoinAhead = 8;       // partials in flight of a run that is joined
 
@@ -335,7 +337,7 @@ struct RunParams {
     const int *total;
     float *partial;             // [2 * CTAs along the list][padded dim]: the run that enters, the run that leaves
     int dim, padded;            // padded: dim rounded up to 8
-    int lanes, slices;          // lanes per group, column slices of lanes * E elements
+    int slices;                 // of the columns, kRunLanes * E elements each
     float scale;
     int accumulate;
     bool overlap;               // the next kernel may begin early
@@ -351,8 +353,9 @@ __global__ void __launch_bounds__(kThreads, 4) sum_runs_kernel(const RunParams p
     let_next_begin(p.overlap);
     wait_for_previous();
     __shared__ float enters[kThreads * E], leaves[kThreads * E];    // [block of the CTA][column of the slice]
-    __shared__ int4 runs[kThreads];                                 // per block: first id, last id, see below
-    const int per = kThreads / p.lanes, lane = threadIdx.x % p.lanes, mine = threadIdx.x / p.lanes, cols = p.lanes * E;
+    __shared__ int4 runs[kRunsPer];                                 // per block: first id, last id, see below
+    constexpr int per = kRunsPer, cols = kRunLanes * E;
+    const int lane = threadIdx.x % kRunLanes, mine = threadIdx.x / kRunLanes;
     const int slice = blockIdx.x % p.slices;
     const long long cta = blockIdx.x / p.slices;
     const int col = slice * cols + lane * E;
@@ -408,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 4) sum_runs_kernel(const RunParams p
     if (lane == 0) runs[mine] = make_int4(first_id, cur, how, 0);
     __syncthreads();
     // the runs that cross blocks, in block order, a thread per group of E columns
-    if (threadIdx.x >= p.lanes || col >= p.dim) return;             // the first group's lanes: their columns are the CTA's
+    if (threadIdx.x >= kRunLanes || col >= p.dim) return;             // the first group's lanes: their columns are the CTA's
     float acc[E] = {};
     bool before = (runs[0].z & kEnters) != 0;                       // the run at hand began before the CTA
     for (int k = 0; k < per && (cta * per + k) * kBlock < total; ++k) {
@@ -442,9 +445,10 @@ template <typename G, bool WIDE>
 __global__ void __launch_bounds__(kThreads) join_runs_kernel(const RunParams p, G *dst, long long ctas)
 {
     constexpr int E = WIDE ? kGroup : 1;
-    const int per = kThreads / p.lanes, lane = threadIdx.x % p.lanes, span = per * kBlock;
-    const long long g = (long long)blockIdx.x * per + threadIdx.x / p.lanes, cta = g / p.slices;
-    const int col = (int(g % p.slices) * p.lanes + lane) * E;
+    constexpr int per = kRunsPer, span = per * kBlock;
+    const int lane = threadIdx.x % kRunLanes;
+    const long long g = (long long)blockIdx.x * per + threadIdx.x / kRunLanes, cta = g / p.slices;
+    const int col = (int(g % p.slices) * kRunLanes + lane) * E;
     wait_for_previous();
     const int total = *p.total;
     const long long edge = (cta + 1) * span;
@@ -511,7 +515,7 @@ EmbedWorkspace plan_workspace(uint64_t n, int32_t dim)
     w.other = round_up(n * sizeof(Entry), 256);
     w.total = 2 * w.other;
     w.partial = w.total + 256;
-    const uint64_t ctas = (n + 8 * kBlock - 1) / (8 * kBlock);      // of sum_runs along the list: eight blocks each at least
+    const uint64_t ctas = (n + kRunsPer * kBlock - 1) / (kRunsPer * kBlock);      // of sum_runs along the list
     w.bytes = w.partial + 2 * ctas * round_up(dim, kGroup) * sizeof(float);
     return w;
 }
@@ -669,14 +673,13 @@ int omni_embed_backward(omni_ctx *ctx, const void *tokens, int32_t index_type, u
     p.partial = reinterpret_cast<float *>(ws + w.partial);
     p.dim = dim;
     p.padded = int(round_up(dim, kGroup));
-    p.lanes = 32;                // a warp a block, however narrow the rows: 32768 rows of 8 floats took 126 us with a lane a block
-    const int cols = p.lanes * (wide ? kGroup : 1);
+    const int cols = kRunLanes * (wide ? kGroup : 1);
     p.slices = (dim + cols - 1) / cols;
     p.scale = scale;
     p.accumulate = accumulate != 0;
     p.src_stride = grad_out_stride;
     p.dst_stride = grad_stride;
-    const int per = kThreads / p.lanes;
+    constexpr int per = kRunsPer;
     const long long ctas = ((long long)n + per * kBlock - 1) / (per * kBlock);
     if (ctas == 0) return OMNI_OK;
     p.overlap = dev.overlap && ctas > 1;
