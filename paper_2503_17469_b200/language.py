@@ -24,11 +24,7 @@ _like, _float, _bf16, _byte = torch.empty_like, torch.float32, torch.bfloat16, t
 _ref = C.byref
 
 
-def _current_stream() -> int:
-    """The raw handle of torch's current stream (what ``Omni._stream`` wraps), without an object around it."""
-    return _raw_stream(_device())
-
-
+# The current device, and the raw handle of its current stream (what ``Omni._stream`` wraps) without an object around it.
 _device = torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
 
@@ -97,12 +93,13 @@ class Embedding(_Operator):
             raise ValueError(f"weight: shape {tuple(self._table)} is wanted")
         if not tokens.is_contiguous():
             raise ValueError("tokens: a contiguous tensor is wanted")
-        if not tokens.is_cuda or not weight.get_device() == out.get_device() == tokens.get_device() == _device():
+        device = tokens.get_device()
+        if not tokens.is_cuda or not weight.get_device() == out.get_device() == device == _device():
             raise _elsewhere(tokens=tokens, weight=weight, out=out)
         self._check(self._lib.omni_embed_forward(
             self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), tokens.numel(), weight.data_ptr(),
             _code(weight, _DTYPES, "weight"), _rows(weight, "weight"), self.vocab, self.dim, self.scale, out.data_ptr(),
-            _code(out, _DTYPES, "out"), self.dim, _current_stream()))
+            _code(out, _DTYPES, "out"), self.dim, _raw_stream(device)))
         return out
 
     def backward(self, tokens, grad_out, dtype=torch.float32, grad=None, accumulate: bool = False, stream=None):
@@ -127,7 +124,8 @@ class Embedding(_Operator):
             grad = g.new_empty(self._table, dtype=dtype)
         elif grad.shape != self._table:
             raise ValueError(f"grad: shape {tuple(self._table)} is wanted")
-        if not tokens.is_cuda or not g.get_device() == grad.get_device() == tokens.get_device() == _device():
+        device = tokens.get_device()
+        if not tokens.is_cuda or not g.get_device() == grad.get_device() == device == _device():
             raise _elsewhere(tokens=tokens, grad_out=g, grad=grad)
         size = self._sizes.get(n)
         if size is None:
@@ -139,7 +137,7 @@ class Embedding(_Operator):
             self.ctx._h, tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), n, g.data_ptr(),
             _code(g, _DTYPES, "grad_out"), _rows(g, "grad_out"), self.vocab, self.dim, self.scale, self.padding,
             grad.data_ptr(), _code(grad, _DTYPES, "grad"), _rows(grad, "grad"), accumulate, scratch.data_ptr(),
-            size, _current_stream()))
+            size, _raw_stream(device)))
         return grad
 
 
@@ -208,7 +206,7 @@ class Attention(_Operator):
         self._check(self._lib.omni_attn_forward(
             self.ctx._h, _ref(a), _ref(view(q, "q", rows, device)), _ref(view(k, "k", keys, device)),
             _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(),
-            scratch.data_ptr() if size else None, size, _current_stream()))
+            scratch.data_ptr() if size else None, size, _raw_stream(device)))
         return out, lse
 
     def backward(self, q, k, v, out, lse, grad_out, q_lengths=None, kv_lengths=None, grads=None, stream=None):
@@ -231,7 +229,7 @@ class Attention(_Operator):
             _ref(view(v, "v", keys, device)), _ref(view(out, "out", rows, device)), lse.data_ptr(),
             _ref(view(grad_out, "grad_out", rows, device)), _ref(view(dq, "grads[0]", rows, device)),
             _ref(view(dk, "grads[1]", keys, device)), _ref(view(dv, "grads[2]", keys, device)), scratch.data_ptr(), size,
-            _current_stream()))
+            _raw_stream(device)))
         return dq, dk, dv
 
 
@@ -283,7 +281,7 @@ class Distillation(_Operator):
         d = self._describe(logits, top_logits, top_index)
         loss = logits.new_empty(d.rows, dtype=_float)
         lse = _like(loss)
-        self._check(self._lib.omni_distill_forward(self.ctx._h, _ref(d), loss.data_ptr(), lse.data_ptr(), _current_stream()))
+        self._check(self._lib.omni_distill_forward(self.ctx._h, _ref(d), loss.data_ptr(), lse.data_ptr(), _raw_stream(logits.get_device())))
         return loss, lse
 
     def backward(self, logits, top_logits, top_index, lse, grad_loss, grad=None, stream=None):
@@ -295,7 +293,7 @@ class Distillation(_Operator):
         grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_distill_backward(
             self.ctx._h, _ref(d), self._row_values(lse, logits, "lse"), self._row_values(grad_loss, logits, "grad_loss"),
-            grad.data_ptr(), _rows(grad, "grad"), _current_stream()))
+            grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
         return grad
 
     def step(self, logits, top_logits, top_index, grad_loss, grad=None, stream=None):
@@ -308,5 +306,5 @@ class Distillation(_Operator):
         loss, lse = _like(grad_loss), _like(grad_loss)
         grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_distill_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), lse.data_ptr(),
-                                                grad.data_ptr(), _rows(grad, "grad"), _current_stream()))
+                                                grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
         return loss, lse, grad
