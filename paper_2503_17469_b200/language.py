@@ -41,6 +41,11 @@ def _elsewhere(**tensors):
     return ValueError(", ".join(f"{k} on {t.device}" for k, t in tensors.items() if t is not None) + ": the current CUDA device is wanted")
 
 
+def _too_large():
+    """For sizes that the library takes as 32 bits: ctypes would cut them."""
+    return ValueError("a size of 2**31 or more")
+
+
 def _rows(t, what: str) -> int:
     """Stride between the rows of a matrix whose rows are contiguous; that of a single row is its length, whatever it was cut from."""
     n, m = t.shape
@@ -75,6 +80,8 @@ class Embedding(_Operator):
         super().__init__(ctx)
         if vocab < 1 or dim < 1:
             raise ValueError("vocab and dim are at least 1")
+        if (vocab | dim) >> 31:
+            raise _too_large()
         self.vocab, self.dim, self.scale, self.padding = vocab, dim, scale, padding
         self._table = torch.Size((vocab, dim))
 
@@ -152,6 +159,8 @@ class Attention(_Operator):
         super().__init__(ctx)
         if heads < 1 or kv_heads < 1 or heads % kv_heads:
             raise ValueError("heads is a multiple of kv_heads")
+        if (heads | dim) >> 31:
+            raise _too_large()
         self.heads, self.kv_heads, self.dim, self.causal = heads, kv_heads, dim, causal
         self.scale = dim ** -0.5 if scale is None else scale
 
@@ -161,6 +170,8 @@ class Attention(_Operator):
             raise ValueError("q and k: [batch, length, head, dim] is wanted")
         batch, q_len = q.shape[:2]
         kv_len = k.shape[1]
+        if (batch | q_len | kv_len) >> 31:
+            raise _too_large()
         if not q.is_cuda or q.get_device() != _device():
             raise _elsewhere(q=q)
         at = [None, None]
@@ -250,6 +261,8 @@ class Distillation(_Operator):
         n, top = top_logits.shape
         if n != rows or top_index.shape != (n, top):
             raise ValueError("logits [rows, vocab], top_logits and top_index [rows, top] are wanted")
+        if (vocab | top) >> 31:
+            raise _too_large()
         stride = _rows(top_logits, "top_logits")
         if _rows(top_index, "top_index") != stride:
             raise ValueError("top_logits and top_index: the same stride is wanted")
