@@ -396,7 +396,8 @@ uint64_t omni_kernel_launches(const omni_ctx *ctx);
  * buffers are.  Kernels are enqueued on `stream`; nothing synchronises.  Sums, norms and softmax
  * statistics are float; a result is rounded once where it is stored.  No result depends on the
  * order of atomics: the same call gives the same bits.
- * Strides are in elements; the last dimension is contiguous.  "dtype" is an omni_dtype.
+ * Strides are in elements; the last dimension is contiguous.  "dtype" is an omni_dtype.  Pointers belong to the
+ * current device.  The calls can be captured in a graph once the context has been used: its first call on a device allocates.
  * ================================================================================================== */
 typedef enum { OMNI_I32 = 0, OMNI_I64 = 1 } omni_index;   /* type of token and vocabulary indices */
 
@@ -413,8 +414,8 @@ int omni_embed_forward(omni_ctx *ctx, const void *tokens, int32_t index_type, ui
 /* Gradient of the lookup, dense, as a gradient bucket wants it:
  *   grad_v = (accumulate ? grad_v : 0) + scale * sum over i with tokens[i] = v of grad_out_i
  * for every v = 0..vocab-1.  The tokens are sorted on the device (stable, so that a row's terms are
- * added in ascending i within blocks of 32 sorted tokens, and the blocks in order) and each row is written once; rows no token names become zero (untouched with
- * accumulate).  `padding` is a token without gradient (-1: none); tokens outside 0..vocab-1 have none
+ * added in ascending i within blocks of 32 sorted tokens, and the blocks in order).  Without accumulate all rows are set to
+ * zero first, and the sums are stored over that; with it rows that no token names are not touched.  `padding` is a token without gradient (-1: none); tokens outside 0..vocab-1 have none
  * either.  grad_out: device, n rows of dim; grad: device, vocab rows of dim, not overlapping.
  * workspace: device, 16-byte aligned, at least omni_embed_workspace() bytes; its contents are free
  * again when the stream has executed the call.
@@ -497,6 +498,8 @@ typedef struct {
  * storage (same pointer and stride): each value is read before it is overwritten.
  * omni_distill_step: both in one pass over the logits (one read, one write), for a caller that knows
  * grad_loss beforehand, as with a mean over rows.
+ * A gradient whose rows lie to 16-byte boundaries as the logits' do (the same storage, or the same stride and alignment) is
+ * written in groups of eight; any other layout element by element, at a fifth to a half of the rate.
  * Errors: NULL, BAD_CONFIG (dtype, vocab or top < 1, temperature not finite or <= 0, a stride below the
  * row), ALIGN, TOO_LARGE (top > OMNI_DISTILL_MAX_TOP, rows >= 2^31), CUDA. */
 int omni_distill_forward(omni_ctx *ctx, const omni_distill *d, float *loss, float *lse, void *stream);

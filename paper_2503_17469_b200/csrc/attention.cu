@@ -110,6 +110,8 @@ int launch(omni_ctx *ctx, void (*kernel)(P), dim3 grid, int threads, int smem, c
 // and 116.2 / 45.1; 1025 queries on 11 keys, 8 heads on 2, three sequences, backward 68.0 / 28.8.  Below eight steps the
 // joining kernel costs more than it gives (512 x 512, 8 heads: forward 15.3 / 19.5), and so does dealing out from a tile
 // per SM on or filling the SMs twice (777 x 777, 12 heads on 4, two sequences: forward 18.5 / 33.1; 256 x 8192: 30.8 / 45.1).
+// The rule looks at the number of tiles, not at the longest walk: a padded batch whose one long sequence keeps an SM busy after the
+// others are done is not dealt out (6 x 777, 12 heads on 4 of 80, backward, every walk in parts and joined: 68 against 53 us).
 int splits_of(int64_t tiles, int64_t steps)
 {
     if (tiles < 1 || 2 * tiles > kSms || steps < 8) return 1;

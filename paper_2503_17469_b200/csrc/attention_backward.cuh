@@ -16,11 +16,16 @@
 //     Order: S0 dP0 S1 | dP1 dQ0 S2 | dP2 dQ1 S3 | ...
 // An operand in tensor memory is overwritten by a product that is issued after the one that reads it; one thread
 // issues all of a block's, and the tensor core takes them in that order.
-// What bounds it: the chain of one tile, S, P, dV and the next S over P, about 3100 cycles a step with dK and dV where
-// the four products take 2048; then the power cap.  Measured: 8192 rows, 16 heads on 8 of 128, causal, 752 us at
-// 1965 MHz (914 TFLOP/s at five products), 870 us sustained at 1.63 GHz and 1000 W.  Tried: P and dS through shared
-// memory 1018 against 940 us then; P over dP, so that S is free earlier (Q's copies then come late) 541 against 455 us of dK, dV; a third
-// place for Q 744 against 747; exponentials by a polynomial 451-472 against 455.
+// What bounds it: the chain of one tile, S, P, dV and the next S over P, 2900 cycles a step with dK and dV where the four
+// products take 2048, and 2200 a step with dQ where the three take 1536; then the power cap.  Measured: 8192 rows, 16 heads on 8 of
+// 128, causal, 744 us (924 TFLOP/s at five products) in a burst, where the clock is at 1.73 GHz, and 870 us a call in a
+// long run.  By clock stamps, in thousands of cycles an SM: 33280 steps of dK and dV 652 and as many of dQ 494; beside their steps
+// 512 blocks of keys, 16 each, 55 and 1024 blocks of queries, 11 each, 77 (set-up 2.3, first loads and scores 3.0-3.7, last product and
+// stores 4.0-8.4, on to the next 1.7); mean 1277, busiest SM 1286.
+// Where a padded batch leaves few blocks the longest decides: 6 x 777, 12 heads on 4 of 80, causal, lasts the 21 steps that the
+// first key tile has to do (three heads, seven query tiles), 77 thousand cycles, 42 of 52 us a call; the mean SM works 33.
+// Tried: P and dS through shared memory 1018 against 940 us then; P over dP, so that S is free earlier (Q's copies then come late) 541
+// against 455 us of dK, dV; a third place for Q 744 against 747; exponentials by a polynomial 451-472 against 455.
 // P and dS are rounded to bfloat16 for the products; all sums are float.
 //
 // Warps 0-15: elementwise (four warps cover the 128 rows, each four another 32 columns), 16: loads, 17: MMA.

@@ -6,8 +6,10 @@
 // The two tiles take turns: while the threads of one are at their exponentials, the tensor
 // core works for the other; the product with V starts on the first quarter of P.
 // What bounds it: S, its exponentials and its product with V follow one another (all 512 columns are taken, so the next S
-// goes over P), about 1900 + 1100 cycles per tile pair and step where the products alone take 2048.  Measured: 2 x 4096
-// rows, 16 heads on 4 of 128, causal, 130 us at 1965 MHz (1057 TFLOP/s of seen pairs), 146 us under the power cap.
+// goes over P), 1900 + 1150 cycles per tile pair and step where the products alone take 2048.  Measured: 2 x 4096 rows, 16 heads on
+// 4 of 128, causal, 130 us (1057 TFLOP/s of seen pairs) in a burst, where the clock is at 1.75 GHz, and 146 us a call in a
+// long run.  By clock stamps, in thousands of cycles an SM: 8704 steps 179; 512 blocks, 3.5 an SM, 39 more, 11 each (set-up 2.1,
+// first loads and scores 2.9, the end with its stores of 16 bytes a row 4.8, on to the next 1.4); mean 217, busiest SM 228.
 // Tried: P through shared memory (S free earlier, but an MMA with both operands there takes all its bandwidth) 171 against
 // 147 us then; two threads a row 154; exponentials in part by a polynomial on the multiply-add units 137-156 against 135.
 // O stays in tensor memory; it is rescaled only when a row's maximum has grown by more than

@@ -8,9 +8,11 @@
 // when the maximum moves), the second finds the row, which the same CTA read a moment ago, in L2.  One more warp
 // has the teacher: it fetches and weighs the entries beside the first walk.
 // What bounds it: backward and forward alone the memory (4096 x 32000 float 160 us, 6.5 TB/s; 3000 x 131072 bfloat16 loss
-// 128-138 us, 5.7-6.1 TB/s); the step its two exponentials per element, 8 cycles per warp and scheduler each, and its
-// instructions beside three passes of L2 (8192 x 50257 bfloat16, rows on 2-byte boundaries: 313-330 us, 5.0-5.3 TB/s of
-// the read and the write).  Tried for the step: the row kept in shared memory by a cluster 392-448 us; a persistent ring of bulk
+// 128-140 us, 5.6-6.1 TB/s); the step its two exponentials per element, 8 cycles per warp and scheduler each, and its
+// instructions beside three passes of L2 (8192 x 50257 bfloat16, rows on 2-byte boundaries: 319-335 us, 4.9-5.2 TB/s of
+// the read and the write).  Few rows leave SMs idle: 1 to 148 rows of 131072 bfloat16 12-14 us a loss.  A gradient whose rows lie to
+// 16-byte boundaries in another way than the logits' is written element by element: 8192 x 50257 of 50304 into dense rows 873
+// instead of 319 us a step.  Tried for the step: the row kept in shared memory by a cluster 392-448 us; a persistent ring of bulk
 // copies, the row held in it, 407-470 us: many warps from several rows hide the exponentials better than a held row saves.
 // 256 walkers and four CTAs an SM; 128 and seven 390 us, 512 and three 326 (and 137 against 133 for the loss alone).
 #include <type_traits>

@@ -2,11 +2,12 @@
 //
 // Lookup: out_i = s * W[t_i].  Pure gather: the floor is the n rows written plus the distinct rows
 // read.  A group of lanes owns a row, 8 elements (16 or 32 bytes) per lane and access, two rows in flight.
-// 65536 rows of 1024 bfloat16 from a table of 50257, Zipf: 31 us, 5.3 TB/s.
+// 65536 rows of 1024 bfloat16 from a table of 50257, Zipf: 33 us a call, 5.1 TB/s.  Rows that no 16-byte access fits go element
+// by element: of 1023 88 us, of 1025 94 us.
 //
 // Gradient: dW_v = s * sum_{t_i = v} dy_i.  Scattered adds with atomics would leave the order of
-// the sum to chance, so the tokens are sorted first and every row of the table is then written
-// once, by an owner that adds its terms in order:
+// the sum to chance, so the tokens are sorted first and a row's sum is then written by one owner that adds its terms
+// in order:
 //   1. sort_tokens: a stable radix sort of (position, id) by nine bits a pass, by one cluster of up to eight CTAs.  A
 //      CTA takes a consecutive stretch of the list, a warp a consecutive part of that; counts per (warp,
 //      digit) in shared memory, joined over the cluster through distributed shared memory, give every token its place;
@@ -17,9 +18,10 @@
 //      block's rows in registers and writes a row where the id changes; runs that cross blocks are joined
 //      in block order in shared memory, those that cross CTAs leave a float partial in the workspace.
 //   3. join_runs: the CTA in which such a run starts adds its partials in order and writes the row.
-// 32768 bfloat16 rows of 768 into 50257 float rows: 29.5 us sort and zeros (154 MB), 28 us sums, 5 us joins, 62-65 us a call
-// against a floor of 31 (each input read, each output written once): the sort, 23 us by itself, waits on its barriers and
-// the zeros leave L2 while the sums run.  Small calls are bound by their three launches.
+// 32768 bfloat16 rows of 768 into 50257 float rows: 29.6 us sort and zeros (154 MB), 27.5 us sums, 5 us joins, 63.6 us a call
+// against a floor of 31 (each input read, each output written once): the sort, 23 us by itself, waits on its barriers; the sums
+// wait on their loads (22 % of DRAM, and at four CTAs an SM their rows in flight spill 108 bytes a thread) while the zeros leave L2.
+// Added to the table 64 us; rows of 767 or 769, element by element, 118-120 us.  Small calls are bound by their three launches.
 // Tried: every CTA counting its own ids among all tokens 30 us and as much skew as the tokens have; matches by
 // __match_any_sync 31.6 against 28.5 us with nine ballots; one launch of one cluster for small batches 30.7 against 20.5 us.
 #include "context.h"
@@ -570,7 +572,9 @@ int omni_embed_forward(omni_ctx *ctx, const void *tokens, int32_t index_type, ui
     const bool wide = dim % kGroup == 0 && wide_rows(table, table_dtype, table_stride) && wide_rows(out, out_dtype, out_stride);
     const int lanes = lanes_for(dim, wide), per = kThreads / lanes;
     // Several rows per group once every SM has enough, so that blocks come and go less often: 65536 rows of 1024 bfloat16 take
-    // 33.1 us with four (34.8 with two, 34.4 with eight, 39.1 with sixteen; 47 with one row a group and one in flight).
+    // 33.1 us with four (34.8 with two, 34.4 with eight, 39.1 with sixteen; 47 with one row a group and one in flight).  One / two /
+    // four from a cold L2, in the timer's steps of 2 us: 1000 x 1024 8 / 8 / 10, 6000 x 256 10 / 8 / 8, 20000 x 1024 20 / 16 / 18,
+    // 40000 x 256 27 / 18 / 16, 131072 x 1024 94 / 68 / 61.
     const int each = n > uint64_t(dev.sm_count) * 16 * per ? 4 : n > uint64_t(dev.sm_count) * 4 * per ? 2 : 1;
     const unsigned grid = unsigned((n + uint64_t(per) * each - 1) / (uint64_t(per) * each));
     return with_index(index_type, [&](auto *ip) {
