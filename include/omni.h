@@ -508,6 +508,51 @@ int omni_distill_backward(omni_ctx *ctx, const omni_distill *d, const float *lse
 int omni_distill_step(omni_ctx *ctx, const omni_distill *d, const float *grad_loss, float *loss, float *lse, void *grad,
                       uint64_t grad_stride, void *stream);
 
+/* Norms of the query and key heads with the rotation by positions, in one pass.  Per head vector x of dim elements:
+ *   n_c = w_c x_c (mean_c x_c^2 + eps)^(-1/2), with the side's weights; without weights (both NULL) n = x
+ *   a pair (a, b) of n turns by the angle position * frequency:  y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin
+ * Pair i = 0..pairs-1 is elements (i, i + pairs), or (2 i, 2 i + 1) with `interleaved`; the elements from 2 * pairs on are not
+ * turned.  Its position is that of axis[i] (time, height, width of an image or video, say), its frequency frequency[i] in radians
+ * per position.  Angles are taken in 64 bits (off by at most 2^-51 of themselves, so far positions keep their phase), everything
+ * else in float with one rounding where a result is stored.
+ * Backward, dn being the results' gradients turned back and g = w dn:
+ *   dx = r (g - x r^2 mean_c(g_c x_c)),  r = (mean_c x_c^2 + eps)^(-1/2);  dw_c = sum over rows and heads of dn_c x_c r
+ * lengths: device int32[batch] or NULL: rows from there on are not read (NaN included), their results are 0 and they are in no sum. */
+typedef struct {
+    int32_t batch, length, heads, kv_heads;
+    int32_t dim;                  /* even, up to OMNI_ROTARY_MAX_DIM */
+    int32_t pairs;                /* 1..dim / 2 */
+    int32_t axes;                 /* 1..OMNI_ROTARY_MAX_AXES */
+    int32_t interleaved;
+    int32_t dtype, weight_dtype;  /* of q, k and the results; of the weights */
+    int32_t position_type;        /* omni_index */
+    float eps;                    /* >= 0 */
+    const double *frequency;      /* HOST, pairs values */
+    const int32_t *axis;          /* HOST, pairs values in 0..axes-1; or NULL: all 0 */
+    const void *positions;        /* device: that of axis a, sequence b, row i at a * position_axis + b * position_batch + i * position_row */
+    uint64_t position_axis, position_batch, position_row;
+    const void *q_weight, *k_weight;   /* device, dim values each, or both NULL */
+    const int32_t *lengths;
+} omni_rotary;
+#define OMNI_ROTARY_MAX_DIM 256
+#define OMNI_ROTARY_MAX_AXES 4
+/* Operands are omni_attn_views of dtype (element (b, i, h, c) at data[b * batch + i * row + h * head + c]), aligned as their elements;
+ * on 16-byte boundaries throughout, with dim a multiple of 16 and interleaved pairs or a multiple of 8 of them, they run with
+ * wide accesses.  A result may be its operand's own storage (same pointer and strides).
+ * omni_rotary_backward: dq_out, dk_out are the gradients of the forward call's results, dq and dk those of q and k.  With weights it
+ * writes their gradients, dim values each of weight_grad_dtype (zeros if there are no rows), and needs a workspace (device,
+ * 16-byte aligned, omni_rotary_workspace() bytes); without weights q, k, the weight gradients and the workspace are not looked at.
+ * Sums over rows are added in an order that the sizes alone decide.
+ * Errors: NULL, BAD_CONFIG (sizes, dim odd, pairs, axes, dtype, eps, a frequency that is not finite, a result's stride below dim), ALIGN,
+ * TOO_LARGE (dim, batch * length >= 2^31, heads > 65535, strides >= 2^40, a workspace below the size asked for), CUDA. */
+int omni_rotary_forward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_view *q, const omni_attn_view *k,
+                        const omni_attn_view *q_out, const omni_attn_view *k_out, void *stream);
+int omni_rotary_workspace(const omni_rotary *r, uint64_t *bytes);
+int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_view *q, const omni_attn_view *k,
+                         const omni_attn_view *dq_out, const omni_attn_view *dk_out, const omni_attn_view *dq, const omni_attn_view *dk,
+                         void *dq_weight, void *dk_weight, int32_t weight_grad_dtype, void *workspace, uint64_t workspace_bytes,
+                         void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -37,10 +37,12 @@ EXPORTS = (
     "omni_embed_forward", "omni_embed_workspace", "omni_embed_backward",
     "omni_attn_forward", "omni_attn_forward_workspace", "omni_attn_workspace", "omni_attn_backward",
     "omni_distill_forward", "omni_distill_backward", "omni_distill_step",
+    "omni_rotary_forward", "omni_rotary_workspace", "omni_rotary_backward",
 )
 MAX_ASP_BATCH = 16
 NOALLOC_MAX_BUCKETS = 8
 NOALLOC_MAX_ELEMENTS = 1 << 31
+ROTARY_MAX_DIM, ROTARY_MAX_AXES = 256, 4
 
 
 class omni_config(C.Structure):
@@ -73,6 +75,15 @@ class omni_distill(C.Structure):
     _fields_ = [("logits", C.c_void_p), ("rows", C.c_uint64), ("row_stride", C.c_uint64), ("vocab", C.c_int32),
                 ("dtype", C.c_int32), ("top_logits", C.c_void_p), ("top_index", C.c_void_p), ("top_stride", C.c_uint64),
                 ("top", C.c_int32), ("index_type", C.c_int32), ("temperature", C.c_float)]
+
+
+class omni_rotary(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("length", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32),
+                ("pairs", C.c_int32), ("axes", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32),
+                ("weight_dtype", C.c_int32), ("position_type", C.c_int32), ("eps", C.c_float),
+                ("frequency", C.POINTER(C.c_double)), ("axis", C.POINTER(C.c_int32)), ("positions", C.c_void_p),
+                ("position_axis", C.c_uint64), ("position_batch", C.c_uint64), ("position_row", C.c_uint64),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("lengths", C.c_void_p)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -134,6 +145,10 @@ def lib() -> C.CDLL:
     L.omni_distill_forward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp]
     L.omni_distill_backward.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp, u64, vp]
     L.omni_distill_step.argtypes = [vp, C.POINTER(omni_distill), vp, vp, vp, vp, u64, vp]
+    ro = C.POINTER(omni_rotary)
+    L.omni_rotary_forward.argtypes = [vp, ro, view, view, view, view, vp]
+    L.omni_rotary_workspace.argtypes = [ro, C.POINTER(u64)]
+    L.omni_rotary_backward.argtypes = [vp, ro, view, view, view, view, view, view, vp, vp, i32, vp, u64, vp]
     _lib = L
     return L
 

@@ -329,3 +329,128 @@ class Distillation(_Operator):
         self._check(self._lib.omni_distill_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), lse.data_ptr(),
                                                 grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
         return loss, lse, grad
+
+
+class Rotary(_Operator):
+    """Norms of query and key heads with the rotation by positions, on float32 or bfloat16 ``[batch, length, head, dim]`` tensors.
+
+    ``frequencies``: radians per position of each rotated pair (``Rotary.geometric`` gives the usual ones), at most dim / 2;
+    elements behind the pairs are not rotated.  ``axes``: the position axis of each pair, for positions of
+    several axes (time, height, width).  ``interleaved``: pairs are neighbours, otherwise element i and i + pairs.  Any strides with a
+    contiguous last dimension; 16-byte boundaries run faster."""
+
+    def __init__(self, ctx: "B.Omni", heads: int, kv_heads: int, dim: int, frequencies, axes=None, interleaved: bool = False,
+                 eps: float = 1e-6):
+        super().__init__(ctx)
+        frequencies = [float(f) for f in frequencies]
+        axes = [0] * len(frequencies) if axes is None else [int(a) for a in axes]
+        if heads < 1 or kv_heads < 1 or dim < 2 or dim % 2:
+            raise ValueError("heads and kv_heads are at least 1, dim is even")
+        if (heads | kv_heads | dim) >> 31:
+            raise _too_large()
+        if not 1 <= len(frequencies) <= dim // 2 or len(axes) != len(frequencies):
+            raise ValueError("between 1 and dim / 2 frequencies, and an axis for each, are wanted")
+        if min(axes) < 0 or max(axes) >= B.ROTARY_MAX_AXES:
+            raise ValueError(f"axes are 0 to {B.ROTARY_MAX_AXES - 1}")
+        if not 0.0 <= eps < float("inf"):
+            raise ValueError("eps is finite and not negative")
+        self.heads, self.kv_heads, self.dim, self.interleaved, self.eps = heads, kv_heads, dim, interleaved, eps
+        self.frequencies, self.axes = frequencies, max(axes) + 1
+        self._frequency = (C.c_double * len(frequencies))(*frequencies)
+        self._axis = (C.c_int32 * len(axes))(*axes)
+
+    @staticmethod
+    def geometric(pairs: int, base: float = 10000.0):
+        """base ** (-i / pairs), i = 0 .. pairs - 1."""
+        return [base ** (-i / pairs) for i in range(pairs)]
+
+    def _describe(self, q, k, positions, q_weight, k_weight, lengths):
+        """(sizes, shape of the queries, shape of the keys) of a call."""
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("q and k: [batch, length, head, dim] is wanted")
+        batch, length = q.shape[:2]
+        if (batch | length) >> 31:
+            raise _too_large()
+        device = q.get_device()
+        if not q.is_cuda or not device == positions.get_device() == _device():
+            raise _elsewhere(q=q, positions=positions)
+        shape = positions.shape
+        if shape == (batch, length) and self.axes == 1:
+            axis, strides = 0, positions.stride()
+        elif shape == (self.axes, batch, length):
+            axis, *strides = positions.stride()
+        else:
+            raise ValueError(f"positions: shape {(self.axes, batch, length)} is wanted" + ", or without the first" * (self.axes == 1))
+        weight, at = B.F32, (None, None)
+        if q_weight is not None and k_weight is not None:
+            weight, at = _code(q_weight, _DTYPES, "q_weight"), (q_weight.data_ptr(), k_weight.data_ptr())
+            for w in (q_weight, k_weight):
+                if w.shape != (self.dim,) or not w.is_contiguous() or w.dtype != q_weight.dtype or w.get_device() != device:
+                    raise ValueError("q_weight and k_weight: contiguous [dim] of one dtype on the tensors' device is wanted")
+        elif q_weight is not None or k_weight is not None:
+            raise ValueError("q_weight and k_weight: both or neither")
+        if lengths is not None and (lengths.dtype != torch.int32 or not lengths.is_contiguous() or lengths.shape != (batch,)
+                                    or lengths.get_device() != device):
+            raise ValueError("lengths: contiguous int32 [batch] on the tensors' device is wanted")
+        r = B.omni_rotary(batch, length, self.heads, self.kv_heads, self.dim, len(self.frequencies), self.axes, self.interleaved,
+                          _code(q, _DTYPES, "q"), weight, _code(positions, _INDEX, "positions"), self.eps, self._frequency, self._axis,
+                          positions.data_ptr(), axis, *strides, *at, None if lengths is None else lengths.data_ptr())
+        return r, (batch, length, self.heads, self.dim), (batch, length, self.kv_heads, self.dim)
+
+    @staticmethod
+    def _view(t, what: str, shape, q):
+        if t.dtype != q.dtype:
+            raise TypeError(f"{what}: dtype {t.dtype} is not that of q, {q.dtype}")
+        if t.shape != shape or t.stride(3) != 1 or t.get_device() != q.get_device():
+            raise ValueError(f"{what}: shape {shape} with a contiguous last dimension on the current device is wanted, "
+                             f"got {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
+        batch, row, head, _ = t.stride()
+        return _ref(B.omni_attn_view(t.data_ptr(), batch, row, head))
+
+    def forward(self, q, k, positions, q_weight=None, k_weight=None, lengths=None, out=None, stream=None):
+        """Returns normed and rotated (q, k); into ``out``, a tuple of two, if given (q and k themselves, or places in a cache).
+        ``positions``: int32 or int64 [batch, length], or [axes, batch, length], any strides.  Without weights there is no norm.
+        Rows behind ``lengths`` (int32 [batch]) are zeros."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.forward(q, k, positions, q_weight, k_weight, lengths, out)
+        r, rows, keys = self._describe(q, k, positions, q_weight, k_weight, lengths)
+        view = self._view
+        out_q, out_k = (_like(q), _like(k)) if out is None else out
+        self._check(self._lib.omni_rotary_forward(
+            self.ctx._h, _ref(r), view(q, "q", rows, q), view(k, "k", keys, q), view(out_q, "out[0]", rows, q),
+            view(out_k, "out[1]", keys, q), _raw_stream(q.get_device())))
+        return out_q, out_k
+
+    def backward(self, q, k, positions, grad_q, grad_k, q_weight=None, k_weight=None, lengths=None, grads=None, dtype=torch.float32,
+                 weight_grads=None, stream=None):
+        """Gradients of (q, k, q_weight, k_weight) from those of the forward call's results; q and k are the forward call's arguments.
+        Into ``grads`` (a tuple of two; grad_q and grad_k themselves will do) and ``weight_grads`` (a tuple of two [dim]) if given;
+        the weights' are of ``dtype`` otherwise, and None without weights."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.backward(q, k, positions, grad_q, grad_k, q_weight, k_weight, lengths, grads, dtype, weight_grads)
+        r, rows, keys = self._describe(q, k, positions, q_weight, k_weight, lengths)
+        view = self._view
+        dq, dk = (_like(q), _like(k)) if grads is None else grads
+        if q_weight is None:
+            dqw = dkw = scratch = None
+            at, code, size = (None, None, None), B.F32, 0
+        else:
+            dqw, dkw = (q_weight.new_empty(self.dim, dtype=dtype) for _ in range(2)) if weight_grads is None else weight_grads
+            code = _code(dqw, _DTYPES, "weight_grads")
+            for w in (dqw, dkw):
+                if w.shape != (self.dim,) or not w.is_contiguous() or w.dtype != dqw.dtype or w.get_device() != q.get_device():
+                    raise ValueError("weight_grads: contiguous [dim] of one dtype on the current device is wanted")
+            size = self._sizes.get(0)
+            if size is None:
+                need = C.c_uint64()
+                self._check(self._lib.omni_rotary_workspace(_ref(r), _ref(need)))
+                size = self._sizes[0] = need.value
+            scratch = q.new_empty(size, dtype=_byte)
+            at = (dqw.data_ptr(), dkw.data_ptr(), scratch.data_ptr())
+        self._check(self._lib.omni_rotary_backward(
+            self.ctx._h, _ref(r), view(q, "q", rows, q), view(k, "k", keys, q), view(grad_q, "grad_q", rows, q),
+            view(grad_k, "grad_k", keys, q), view(dq, "grads[0]", rows, q), view(dk, "grads[1]", keys, q), at[0], at[1], code, at[2], size,
+            _raw_stream(q.get_device())))
+        return dq, dk, dqw, dkw
