@@ -553,6 +553,42 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
                          void *dq_weight, void *dk_weight, int32_t weight_grad_dtype, void *workspace, uint64_t workspace_bytes,
                          void *stream);
 
+/* Clipped policy loss on sampled tokens, with a divergence from a reference policy.  Per row, with logits z over the vocabulary, the
+ * token t, its log-probability `old` when it was sampled and `reference` under the reference, the advantage A:
+ *   lse = log sum_v exp(z_v / T);  logp = z_t / T - lse;  ratio = exp(logp - old)
+ *   surrogate = min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A);  gap = reference - logp
+ *   loss = -surrogate + kl (exp(gap) - gap - 1)
+ *   grad_v = grad_loss c / T ([v = t] - exp(z_v / T - lse)),
+ *            c = -(ratio A where ratio A is the smaller or equal, else 0) + kl (1 - exp(gap))
+ * A token outside 0..vocab-1 (-1 by convention) is none: the row's loss, logp and gradient are 0, and nothing of it but the logits is
+ * looked at (lse is still written).  A row whose grad_loss c is 0 has a gradient of zeros, and an advantage of 0 has no surrogate, whatever the ratio.
+ * A logit of -inf has probability 0; logits far from zero are taken by their distances, as in omni_distill. */
+typedef struct {
+    const void *logits;           /* device, rows x vocab of dtype */
+    uint64_t rows, row_stride;
+    int32_t vocab, dtype;
+    const void *tokens;           /* device, rows values of index_type */
+    const float *old, *advantage; /* device, rows values each */
+    const float *reference;       /* device, rows values; not looked at if kl is 0 */
+    int32_t index_type;
+    float clip_low, clip_high;    /* >= 0 */
+    float kl;                     /* >= 0 */
+    float temperature;            /* > 0 */
+} omni_policy;
+/* omni_policy_logprob: logp[rows] and lse[rows] (device float) alone; old, advantage, reference, clip and kl are not looked at.
+ * omni_policy_forward: loss, logp, lse.  omni_policy_backward: grad (rows x vocab of the logits' dtype, grad_stride apart) from the
+ * kept lse and grad_loss[rows]; omni_policy_step: both in one pass over the logits, for a caller that knows grad_loss beforehand.
+ * grad may be the logits' own storage (same pointer and stride).  A gradient whose rows lie to 16-byte boundaries as the logits' do
+ * is written in groups of eight, any other element by element.
+ * Errors: NULL, BAD_CONFIG (dtype, vocab < 1, temperature, clip or kl negative or not finite, a stride below the row), ALIGN,
+ * TOO_LARGE (rows >= 2^31), CUDA. */
+int omni_policy_logprob(omni_ctx *ctx, const omni_policy *d, float *logp, float *lse, void *stream);
+int omni_policy_forward(omni_ctx *ctx, const omni_policy *d, float *loss, float *logp, float *lse, void *stream);
+int omni_policy_backward(omni_ctx *ctx, const omni_policy *d, const float *lse, const float *grad_loss, void *grad, uint64_t grad_stride,
+                         void *stream);
+int omni_policy_step(omni_ctx *ctx, const omni_policy *d, const float *grad_loss, float *loss, float *logp, float *lse, void *grad,
+                     uint64_t grad_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,6 +38,7 @@ EXPORTS = (
     "omni_attn_forward", "omni_attn_forward_workspace", "omni_attn_workspace", "omni_attn_backward",
     "omni_distill_forward", "omni_distill_backward", "omni_distill_step",
     "omni_rotary_forward", "omni_rotary_workspace", "omni_rotary_backward",
+    "omni_policy_logprob", "omni_policy_forward", "omni_policy_backward", "omni_policy_step",
 )
 MAX_ASP_BATCH = 16
 NOALLOC_MAX_BUCKETS = 8
@@ -84,6 +85,13 @@ class omni_rotary(C.Structure):
                 ("frequency", C.POINTER(C.c_double)), ("axis", C.POINTER(C.c_int32)), ("positions", C.c_void_p),
                 ("position_axis", C.c_uint64), ("position_batch", C.c_uint64), ("position_row", C.c_uint64),
                 ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class omni_policy(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("rows", C.c_uint64), ("row_stride", C.c_uint64), ("vocab", C.c_int32), ("dtype", C.c_int32),
+                ("tokens", C.c_void_p), ("old", C.c_void_p), ("advantage", C.c_void_p), ("reference", C.c_void_p),
+                ("index_type", C.c_int32), ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl", C.c_float),
+                ("temperature", C.c_float)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -149,6 +157,11 @@ def lib() -> C.CDLL:
     L.omni_rotary_forward.argtypes = [vp, ro, view, view, view, view, vp]
     L.omni_rotary_workspace.argtypes = [ro, C.POINTER(u64)]
     L.omni_rotary_backward.argtypes = [vp, ro, view, view, view, view, view, view, vp, vp, i32, vp, u64, vp]
+    po = C.POINTER(omni_policy)
+    L.omni_policy_logprob.argtypes = [vp, po, vp, vp, vp]
+    L.omni_policy_forward.argtypes = [vp, po, vp, vp, vp, vp]
+    L.omni_policy_backward.argtypes = [vp, po, vp, vp, vp, u64, vp]
+    L.omni_policy_step.argtypes = [vp, po, vp, vp, vp, vp, vp, u64, vp]
     _lib = L
     return L
 

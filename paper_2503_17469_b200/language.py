@@ -454,3 +454,89 @@ class Rotary(_Operator):
             view(grad_k, "grad_k", keys, q), view(dq, "grads[0]", rows, q), view(dk, "grads[1]", keys, q), at[0], at[1], code, at[2], size,
             _raw_stream(q.get_device())))
         return dq, dk, dqw, dkw
+
+
+class Policy(_Operator):
+    """Clipped policy loss on sampled tokens, with ``kl`` times a divergence from a reference policy, per row of logits.
+    The ratio to the sampling policy is clipped to 1 - ``clip`` .. 1 + ``clip_high`` (default ``clip``).  A token of -1 marks a row
+    without one (a prompt's, padding): loss 0, log-probability 0 and no gradient, whatever its other values are."""
+
+    def __init__(self, ctx: "B.Omni", clip: float = 0.2, clip_high: Optional[float] = None, kl: float = 0.0, temperature: float = 1.0):
+        super().__init__(ctx)
+        high = clip if clip_high is None else clip_high
+        if not (0 <= clip < float("inf") and 0 <= high < float("inf") and 0 <= kl < float("inf")):
+            raise ValueError("clip, clip_high and kl are finite and not negative")
+        if not temperature > 0:
+            raise ValueError("temperature is positive")
+        self.clip, self.clip_high, self.kl, self.temperature = clip, high, kl, temperature
+
+    def _describe(self, logits, tokens, old=None, advantage=None, reference=None):
+        rows, vocab = logits.shape
+        if tokens.shape != (rows,) or not tokens.is_contiguous():
+            raise ValueError("logits [rows, vocab] and contiguous tokens [rows] are wanted")
+        if vocab >> 31:
+            raise _too_large()
+        device = tokens.get_device()
+        if not logits.is_cuda or not logits.get_device() == device == _device():
+            raise _elsewhere(logits=logits, tokens=tokens)
+        at = (None, None, None)
+        if old is not None:
+            if self.kl and reference is None:
+                raise ValueError("kl needs the reference's log-probabilities")
+            at = (self._row_values(old, logits, "old"), self._row_values(advantage, logits, "advantage"),
+                  self._row_values(reference, logits, "reference") if self.kl else None)
+        return B.omni_policy(logits.data_ptr(), rows, _rows(logits, "logits"), vocab, _code(logits, _DTYPES, "logits"), tokens.data_ptr(),
+                             *at, _code(tokens, _INDEX, "tokens"), self.clip, self.clip_high, self.kl, self.temperature)
+
+    _row_values = staticmethod(Distillation._row_values)
+    _grad_like = staticmethod(Distillation._grad_like)
+
+    def logprob(self, logits, tokens, stream=None):
+        """Returns (log-probabilities of the tokens, lse), float32 [rows] each: ``old`` and ``reference`` of the calls below come
+        from here, with the logits of the sampling and of the reference policy."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.logprob(logits, tokens)
+        d = self._describe(logits, tokens)
+        logp = logits.new_empty(d.rows, dtype=_float)
+        lse = _like(logp)
+        self._check(self._lib.omni_policy_logprob(self.ctx._h, _ref(d), logp.data_ptr(), lse.data_ptr(), _raw_stream(logits.get_device())))
+        return logp, lse
+
+    def forward(self, logits, tokens, old, advantage, reference=None, stream=None):
+        """Returns (loss, log-probabilities, lse), float32 [rows] each.  ``old``, ``advantage``, ``reference`` (wanted if ``kl`` is
+        not 0): float32 [rows]."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.forward(logits, tokens, old, advantage, reference)
+        d = self._describe(logits, tokens, old, advantage, reference)
+        loss, logp, lse = (_like(old) for _ in range(3))
+        self._check(self._lib.omni_policy_forward(self.ctx._h, _ref(d), loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
+                                                  _raw_stream(logits.get_device())))
+        return loss, logp, lse
+
+    def backward(self, logits, tokens, lse, old, advantage, grad_loss, reference=None, grad=None, stream=None):
+        """Gradient of the logits from ``lse`` of the forward call and ``grad_loss`` [rows]; ``grad`` may be ``logits``."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.backward(logits, tokens, lse, old, advantage, grad_loss, reference, grad)
+        d = self._describe(logits, tokens, old, advantage, reference)
+        grad = self._grad_like(logits, grad)
+        self._check(self._lib.omni_policy_backward(
+            self.ctx._h, _ref(d), self._row_values(lse, logits, "lse"), self._row_values(grad_loss, logits, "grad_loss"), grad.data_ptr(),
+            _rows(grad, "grad"), _raw_stream(logits.get_device())))
+        return grad
+
+    def step(self, logits, tokens, old, advantage, grad_loss, reference=None, grad=None, stream=None):
+        """Forward and backward in one pass; returns (loss, log-probabilities, lse, gradient of the logits).  ``grad`` as in
+        ``backward``."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.step(logits, tokens, old, advantage, grad_loss, reference, grad)
+        d = self._describe(logits, tokens, old, advantage, reference)
+        weights = self._row_values(grad_loss, logits, "grad_loss")
+        loss, logp, lse = (_like(grad_loss) for _ in range(3))
+        grad = self._grad_like(logits, grad)
+        self._check(self._lib.omni_policy_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
+                                               grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
+        return loss, logp, lse, grad
