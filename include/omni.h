@@ -589,6 +589,44 @@ int omni_policy_backward(omni_ctx *ctx, const omni_policy *d, const float *lse, 
 int omni_policy_step(omni_ctx *ctx, const omni_policy *d, const float *grad_loss, float *loss, float *logp, float *lse, void *grad,
                      uint64_t grad_stride, void *stream);
 
+/* AdamW over many tensors in one launch, on the batch-weighted gradients of K workers (the aggregation of omni_aggregate_bsp with
+ * another update).  Per element of a tensor, in float, every operation rounded once, with lambda_k = float(b_k / sum b):
+ *   g = fma(lambda_{K-1}, g_{K-1}, ... fma(lambda_0, g_0, 0));  m = fma(beta1, m, c1 g);  v = fma(c2 g, g, beta2 v)
+ *   theta = fma(-rate, m / fma(sqrt(v), spread, eps), keep theta);  param_lp = bfloat16(theta)
+ * c = float(1 - beta), rate = float(lr / (1 - beta1^t)), spread = float((1 - beta2^t)^(-1/2)), keep = float(1 - lr weight_decay), t = 1,
+ * 2, ... the step's number.  The quotient and the root may be off by 2^-21 of themselves; m and v are exact.
+ * bits = 8: m and v are kept as codes of the float's bits 20 to 30 (exponent and three bits of the fraction), counted from the largest
+ * of their block of OMNI_ADAMW_BLOCK consecutive elements.  With top the block's largest, a code c > 0 is the float of bits (c + top - 127) << 20
+ * for m, bit 7 of the byte its sign, and (c + top - 255) << 20 for v; c = 0 is 0.  theta is computed from m and v before they are
+ * rounded: 16 random bits are added to bits 4 to 19 and what is below bit 20 is dropped; then m below code 1 is 0, v below it is code 1
+ * unless it is 0.  The random bits are x = (x ^ x >> 15) of x = (y ^ y >> 16) * 0x7FEB352D, y = i * 0x9E3779B1 + t * 0x85EBCA77 +
+ * tensor * 0xC2B2AE3D modulo 2^32 for element i of a tensor (numbered from 0 in the list): the low half for m, the high half for v.
+ * So the same state, gradients and step give the same bits.  A gradient that is not finite spoils its element as in float, and the
+ * codes of its block. */
+#define OMNI_ADAMW_BLOCK 256
+typedef struct {
+    float *param;                 /* device, n values, read and written */
+    void *param_lp;               /* device, bfloat16[n], written; or NULL */
+    const void *const *grads;     /* HOST array of K device pointers, n values of grad_dtype each */
+    void *m, *v;                  /* device, float[n], or uint8[n] for 8 bits, read and written; zeros at first */
+    void *tops;                   /* device, 8 bits: int16[2] (m, v) for each block, 4-byte aligned, zeros at first; else not looked at */
+    uint64_t n;                   /* 0 is allowed */
+    double weight_decay;
+} omni_adamw_tensor;
+/* omni_adamw_plan writes a record of the tensors to host memory (8-byte aligned, omni_adamw_plan_bytes() bytes).  The caller copies
+ * it to the device (16-byte aligned) and keeps both while it steps; pointers in it stay as they are.  Pointers need the alignment of
+ * their elements; with all of a tensor's on 16-byte boundaries (8 for codes) it runs with wide accesses.
+ * omni_adamw_step: one step; b: host int32[K], the batches of the gradients.  The step's number is `step`, or, if clock_dev is not
+ * NULL, the int64 that clock_dev (device, 8-byte aligned) holds when the kernel runs, for a step that is captured in a graph; lr is the host's.
+ * omni_adamw_moments: what the codes stand for, into m[i], v[i] (HOST arrays of device float pointers, one for each tensor); 8 bits only.
+ * Errors: NULL, BAD_K, BAD_CONFIG (dtype, bits, tensors written to that overlap, not a record, lr or weight_decay not finite, beta outside [0, 1), eps, step < 1), BAD_BATCH,
+ * ALIGN, TOO_LARGE (a tensor of 2^42 elements, 2^31 pieces of 2048 in all, a record that is too small), NO_MEMORY, CUDA. */
+int omni_adamw_plan_bytes(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, uint64_t *bytes);
+int omni_adamw_plan(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, void *record, uint64_t bytes);
+int omni_adamw_step(omni_ctx *ctx, const void *record, const void *record_dev, const int32_t *b, double lr, double beta1, double beta2,
+                    float eps, int64_t step, const int64_t *clock_dev, void *stream);
+int omni_adamw_moments(omni_ctx *ctx, const void *record, const void *record_dev, float *const *m, float *const *v, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,11 +39,13 @@ EXPORTS = (
     "omni_distill_forward", "omni_distill_backward", "omni_distill_step",
     "omni_rotary_forward", "omni_rotary_workspace", "omni_rotary_backward",
     "omni_policy_logprob", "omni_policy_forward", "omni_policy_backward", "omni_policy_step",
+    "omni_adamw_plan_bytes", "omni_adamw_plan", "omni_adamw_step", "omni_adamw_moments",
 )
 MAX_ASP_BATCH = 16
 NOALLOC_MAX_BUCKETS = 8
 NOALLOC_MAX_ELEMENTS = 1 << 31
 ROTARY_MAX_DIM, ROTARY_MAX_AXES = 256, 4
+ADAMW_BLOCK = 256
 
 
 class omni_config(C.Structure):
@@ -92,6 +94,11 @@ class omni_policy(C.Structure):
                 ("tokens", C.c_void_p), ("old", C.c_void_p), ("advantage", C.c_void_p), ("reference", C.c_void_p),
                 ("index_type", C.c_int32), ("clip_low", C.c_float), ("clip_high", C.c_float), ("kl", C.c_float),
                 ("temperature", C.c_float)]
+
+
+class omni_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("param_lp", C.c_void_p), ("grads", C.POINTER(C.c_void_p)), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("tops", C.c_void_p), ("n", C.c_uint64), ("weight_decay", C.c_double)]
 
 
 _lib: Optional[C.CDLL] = None
@@ -162,6 +169,11 @@ def lib() -> C.CDLL:
     L.omni_policy_forward.argtypes = [vp, po, vp, vp, vp, vp]
     L.omni_policy_backward.argtypes = [vp, po, vp, vp, vp, u64, vp]
     L.omni_policy_step.argtypes = [vp, po, vp, vp, vp, vp, vp, u64, vp]
+    tensors, f64 = C.POINTER(omni_adamw_tensor), C.c_double
+    L.omni_adamw_plan_bytes.argtypes = [tensors, i32, i32, i32, i32, C.POINTER(u64)]
+    L.omni_adamw_plan.argtypes = [tensors, i32, i32, i32, i32, vp, u64]
+    L.omni_adamw_step.argtypes = [vp, vp, vp, C.POINTER(i32), f64, f64, f64, f32, i64, vp, vp]
+    L.omni_adamw_moments.argtypes = [vp, vp, vp, C.POINTER(vp), C.POINTER(vp), vp]
     _lib = L
     return L
 

@@ -13,7 +13,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libomni.so"
 SOURCES = [CSRC / "omni.cu", CSRC / "register_dispatch.cu", CSRC / "bulk_dispatch.cu", CSRC / "device_controller.cu", CSRC / "noalloc.cu",
            CSRC / "controller.cpp", CSRC / "shard.cpp", CSRC / "embed.cu", CSRC / "distill.cu",
-           CSRC / "attention.cu", CSRC / "rotary.cu", CSRC / "policy.cu"]
+           CSRC / "attention.cu", CSRC / "rotary.cu", CSRC / "policy.cu", CSRC / "adamw.cu"]
 HEADERS = [CSRC / "kernels.cuh", CSRC / "tma_kernels.cuh", CSRC / "dispatch.h", CSRC / "controller.h",
            CSRC / "device_controller.h", CSRC / "context.h", CSRC / "vector.cuh", CSRC / "row_softmax.cuh", CSRC / "tensor_core.cuh", CSRC / "attention.cuh",
            CSRC / "attention_forward.cuh", CSRC / "attention_backward.cuh", PKG.parent / "include" / "omni.h"]

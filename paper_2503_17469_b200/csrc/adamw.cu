@@ -1,0 +1,455 @@
+// AdamW over many tensors in one launch, on the weighted gradients of K workers, with moments of 32 bits or of 8.
+//
+// Per element, every operation in float, rounded once, FMA where written so (the states' bits are part of the contract):
+//   g = fma(lambda_{K-1}, g_{K-1}, ... fma(lambda_0, g_0, 0));  m = fma(b1, m, c1 g);  v = fma(c2 g, g, b2 v)
+//   theta = fma(-rate, m / fma(sqrt(v), spread, eps), keep theta)
+// with c = 1 - b, rate = lr / (1 - b1^t), spread = (1 - b2^t)^(-1/2), keep = 1 - lr decay.
+//
+// Moments of 8 bits: a float's top twelve bits (sign, exponent, three of the fraction), counted down from the largest of the
+// 256 elements of its block, which is kept beside the codes: seven bits below a sign for m (16 octaves), eight for v (32 octaves; what is not zero
+// stays at least the lowest code, so that no m is divided by a root that was lost).  Decoding is a shift and an addition,
+// no scale is multiplied.  The bits below are rounded by random ones: a decay of v by a thousandth a step is far below
+// half of a code's step of an eighth, and would never happen with the nearest code.
+#include "context.h"
+#include "vector.cuh"
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+namespace omni {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlock = OMNI_ADAMW_BLOCK;              // elements with one offset: a warp's, eight a lane
+constexpr int kUnit = kThreads * kGroup;              // elements a CTA has at a time
+static_assert(kBlock == 32 * kGroup, "a warp holds a block");
+
+// A tensor in the record, followed by those of all tensors, the K gradient pointers of each, and the owner of each unit.
+struct Entry {
+    float *param;
+    __nv_bfloat16 *copy;
+    void *m, *v;
+    uint32_t *tops;                                   // of a block: that of m in the low half, that of v in the high half
+    unsigned long long n;
+    double decay;
+    unsigned first_unit;
+    int wide;                                         // every pointer allows accesses of eight elements
+};
+struct Header {
+    unsigned long long magic, bytes;
+    int tensors, K, grad_dtype, bits;
+    unsigned units;
+    int pad[7];
+};
+static_assert(sizeof(Entry) == 64 && sizeof(Header) == 64, "the record's layout");
+constexpr unsigned long long kMagic = 0x6f6d6e695f616477ull;
+
+struct Layout {
+    unsigned long long entries, grads, owners, bytes;
+    __host__ __device__ Layout(int tensors, int K, unsigned units)
+    {
+        entries = sizeof(Header);
+        grads = entries + (unsigned long long)tensors * sizeof(Entry);
+        owners = grads + (unsigned long long)tensors * K * sizeof(void *);
+        bytes = (owners + (unsigned long long)units * 4 + 15) / 16 * 16;
+    }
+};
+
+struct AdamParams {
+    const Entry *entries;
+    const void *const *grads;
+    const unsigned *owners;
+    const long long *clock;                           // the step's number on the device, or NULL
+    double lr, beta1, beta2;
+    float b1, b2, c1, c2, eps, rate, spread;
+    unsigned step;
+    int K;
+    float lambda[OMNI_MAX_K];
+};
+
+// Eight elements, or those of them before the end one by one.
+template <typename T> __device__ __forceinline__ void load8(const T *p, bool wide, int count, float *f)
+{
+    if (wide && count == kGroup) {
+        load_group(p, f);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) f[i] = i < count ? to_float(p[i]) : 0.0f;
+}
+template <typename T> __device__ __forceinline__ void store8(T *p, bool wide, int count, const float *f)
+{
+    if (wide && count == kGroup) {
+        store_group(p, f);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+        if (i < count) p[i] = from_float<T>(f[i]);
+}
+__device__ __forceinline__ uint2 load_codes(const unsigned char *p, bool wide, int count)
+{
+    if (wide && count == kGroup) return *reinterpret_cast<const uint2 *>(p);
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+        if (i < count) w[i / 4] |= uint32_t(p[i]) << (8 * (i % 4));
+    return {w[0], w[1]};
+}
+__device__ __forceinline__ void store_codes(unsigned char *p, bool wide, int count, uint2 c)
+{
+    if (wide && count == kGroup) {
+        *reinterpret_cast<uint2 *>(p) = c;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i)
+        if (i < count) p[i] = (unsigned char)((i < 4 ? c.x : c.y) >> (8 * (i % 4)));
+}
+
+// What a code stands for; MOST: 127 for the signed codes of m, 255 for those of v.
+template <int MOST> __device__ __forceinline__ float decode(uint32_t code, int top)
+{
+    const int c = int(code & MOST);
+    const uint32_t bits = c ? uint32_t(c + top - MOST) << 20 : 0u;
+    return __uint_as_float(MOST == 127 ? bits | (code & 128u) << 24 : bits);
+}
+template <int MOST> __device__ __forceinline__ void decode8(uint2 c, int top, float *f)
+{
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) f[i] = decode<MOST>((i < 4 ? c.x : c.y) >> (8 * (i % 4)) & 255u, top);
+}
+// The float's top twelve bits less the sign, rounded by 16 random bits; a NaN stays one.
+__device__ __forceinline__ uint32_t rounded(float x, uint32_t random)
+{
+    return min((__float_as_uint(x) & 0x7fffffffu) + (random << 4) >> 20, 0x7ffu);
+}
+template <int MOST> __device__ __forceinline__ uint32_t encode(uint32_t r, int top, float x)
+{
+    const int c = int(r) - top + MOST;
+    if (MOST == 255) return r ? uint32_t(max(c, 1)) : 0u;
+    return c > 0 ? uint32_t(c) | (__float_as_uint(x) >> 24 & 128u) : 0u;
+}
+
+// 32 bits of an element's own, by multiplications and shifts of its number, its tensor's and the step's.
+constexpr uint32_t kStride = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t scramble(uint32_t x)
+{
+    x = (x ^ x >> 16) * 0x7FEB352Du;
+    return x ^ x >> 15;
+}
+
+template <typename G, int BITS> __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamParams p)
+{
+    __shared__ float scales[2];
+    __shared__ unsigned long long step_now;
+    float rate = p.rate, spread = p.spread;
+    uint32_t step = p.step;
+    if (p.clock) {
+        if (threadIdx.x == 0) {
+            const long long t = *p.clock;
+            scales[0] = float(p.lr / (1.0 - pow(p.beta1, double(t))));
+            scales[1] = float(1.0 / sqrt(1.0 - pow(p.beta2, double(t))));
+            step_now = (unsigned long long)t;
+        }
+        __syncthreads();
+        rate = scales[0];
+        spread = scales[1];
+        step = uint32_t(step_now);
+    }
+    const unsigned unit = blockIdx.x, tensor = p.owners[unit];
+    const Entry &e = p.entries[tensor];
+    const unsigned long long at = (unsigned long long)(unit - e.first_unit) * kUnit + threadIdx.x * kGroup;
+    if (at - threadIdx.x % 32 * kGroup >= e.n) return;                    // the warp's block is behind the end
+    const bool wide = e.wide;
+    const int count = at >= e.n ? 0 : e.n - at < kGroup ? int(e.n - at) : kGroup;
+    float theta[kGroup], m[kGroup], v[kGroup], g[kGroup];
+    load8(e.param + at, wide, count, theta);
+    unsigned char *const cm = static_cast<unsigned char *>(e.m) + at, *const cv = static_cast<unsigned char *>(e.v) + at;
+    float *const fm = static_cast<float *>(e.m) + at, *const fv = static_cast<float *>(e.v) + at;
+    if constexpr (BITS == 32) {
+        load8(fm, wide, count, m);
+        load8(fv, wide, count, v);
+    } else {
+        const uint32_t tops = e.tops[at / kBlock];
+        decode8<127>(load_codes(cm, wide, count), int(tops & 0xffffu), m);
+        decode8<255>(load_codes(cv, wide, count), int(tops >> 16), v);
+    }
+    const void *const *grads = p.grads + (unsigned long long)tensor * p.K;
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) g[i] = 0.0f;
+    for (int k = 0; k < p.K; ++k) {
+        float x[kGroup];
+        load8(static_cast<const G *>(grads[k]) + at, wide, count, x);
+        const float lambda = p.lambda[k];
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) g[i] = __fmaf_rn(lambda, x[i], g[i]);
+    }
+    const float keep = float(1.0 - p.lr * e.decay);
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) {
+        m[i] = __fmaf_rn(p.b1, m[i], __fmul_rn(p.c1, g[i]));
+        v[i] = __fmaf_rn(__fmul_rn(p.c2, g[i]), g[i], __fmul_rn(p.b2, v[i]));
+        const float below = __fmaf_rn(__fsqrt_rn(v[i]), spread, p.eps);
+        theta[i] = __fmaf_rn(-rate, __fdiv_rn(m[i], below), __fmul_rn(keep, theta[i]));
+    }
+    store8(e.param + at, wide, count, theta);
+    if (e.copy) store8(e.copy + at, wide, count, theta);
+    if constexpr (BITS == 32) {
+        store8(fm, wide, count, m);
+        store8(fv, wide, count, v);
+    } else {
+        const uint32_t start = step * 0x85EBCA77u + tensor * 0xC2B2AE3Du + uint32_t(at) * kStride;
+        uint32_t rm[kGroup], rv[kGroup], most_m = 0, most_v = 0;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            const uint32_t random = scramble(start + i * kStride);
+            rm[i] = i < count ? rounded(m[i], random & 0xffffu) : 0u;
+            rv[i] = i < count ? rounded(v[i], random >> 16) : 0u;
+            most_m = max(most_m, rm[i]);
+            most_v = max(most_v, rv[i]);
+        }
+        most_m = __reduce_max_sync(~0u, most_m);
+        most_v = __reduce_max_sync(~0u, most_v);
+        uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) {
+            wm[i / 4] |= encode<127>(rm[i], int(most_m), m[i]) << (8 * (i % 4));
+            wv[i / 4] |= encode<255>(rv[i], int(most_v), v[i]) << (8 * (i % 4));
+        }
+        store_codes(cm, wide, count, {wm[0], wm[1]});
+        store_codes(cv, wide, count, {wv[0], wv[1]});
+        if (threadIdx.x % 32 == 0) e.tops[at / kBlock] = most_m | most_v << 16;
+    }
+}
+
+// What the codes of some tensors stand for.
+constexpr int kPerLaunch = 192;
+struct MomentParams {
+    const Entry *entries;
+    const unsigned *owners;
+    unsigned first_unit;
+    int first;
+    float *m[kPerLaunch], *v[kPerLaunch];
+};
+__global__ void __launch_bounds__(kThreads) adamw_moments_kernel(const __grid_constant__ MomentParams p)
+{
+    const unsigned unit = p.first_unit + blockIdx.x, tensor = p.owners[unit];
+    const Entry &e = p.entries[tensor];
+    const unsigned long long at = (unsigned long long)(unit - e.first_unit) * kUnit + threadIdx.x * kGroup;
+    if (at >= e.n) return;
+    const int count = e.n - at < kGroup ? int(e.n - at) : kGroup;
+    float *const m = p.m[tensor - p.first] + at, *const v = p.v[tensor - p.first] + at;
+    const uint32_t tops = e.tops[at / kBlock];
+    float f[kGroup];
+    decode8<127>(load_codes(static_cast<const unsigned char *>(e.m) + at, e.wide, count), int(tops & 0xffffu), f);
+    store8(m, (reinterpret_cast<uintptr_t>(m) & 15) == 0, count, f);
+    decode8<255>(load_codes(static_cast<const unsigned char *>(e.v) + at, e.wide, count), int(tops >> 16), f);
+    store8(v, (reinterpret_cast<uintptr_t>(v) & 15) == 0, count, f);
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_tensors(const omni_adamw_tensor *t, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, unsigned *units)
+{
+    if (K < 1 || K > OMNI_MAX_K) return OMNI_ERR_BAD_K;
+    if (count < 0 || (grad_dtype != OMNI_F32 && grad_dtype != OMNI_BF16) || (bits != 32 && bits != 8)) return OMNI_ERR_BAD_CONFIG;
+    if (count > 0 && !t) return OMNI_ERR_NULL;
+    const size_t grad = grad_dtype == OMNI_BF16 ? 2 : 4;
+    uint64_t all = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        if (!(t[i].weight_decay - t[i].weight_decay == 0.0)) return OMNI_ERR_BAD_CONFIG;
+        if (t[i].n == 0) continue;
+        if (t[i].n >= (1ull << 42)) return OMNI_ERR_TOO_LARGE;
+        if (!t[i].param || !t[i].grads || !t[i].m || !t[i].v || (bits == 8 && !t[i].tops)) return OMNI_ERR_NULL;
+        if (!aligned(t[i].param, 4) || !aligned(t[i].param_lp, 2) || (bits == 32 && (!aligned(t[i].m, 4) || !aligned(t[i].v, 4))) ||
+            (bits == 8 && !aligned(t[i].tops, 4)))
+            return OMNI_ERR_ALIGN;
+        for (int k = 0; k < K; ++k) {
+            if (!t[i].grads[k]) return OMNI_ERR_NULL;
+            if (!aligned(t[i].grads[k], grad)) return OMNI_ERR_ALIGN;
+        }
+        all += (t[i].n + kUnit - 1) / kUnit;
+        if (all >= (1ull << 31)) return OMNI_ERR_TOO_LARGE;
+    }
+    *units = unsigned(all);
+    return OMNI_OK;
+}
+
+bool all_wide(const omni_adamw_tensor &t, int K, int bits)
+{
+    const size_t state = bits == 8 ? 8 : 16;
+    bool wide = aligned(t.param, 16) && aligned(t.param_lp, 16) && aligned(t.m, state) && aligned(t.v, state);
+    for (int k = 0; k < K; ++k) wide = wide && aligned(t.grads[k], 16);
+    return wide;
+}
+
+// Whether what a step writes lies apart, all of it: a tensor that stands in the list twice would be updated twice at once.
+int check_apart(const omni_adamw_tensor *t, int32_t count, int32_t bits)
+{
+    try {
+        std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
+        ranges.reserve(size_t(count) * 5);
+        const auto add = [&](const void *p, uint64_t bytes) {
+            if (p) ranges.emplace_back(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes);
+        };
+        for (int32_t i = 0; i < count; ++i) {
+            if (t[i].n == 0) continue;
+            const uint64_t n = t[i].n, state = bits == 8 ? n : 4 * n;
+            add(t[i].param, 4 * n);
+            add(t[i].param_lp, 2 * n);
+            add(t[i].m, state);
+            add(t[i].v, state);
+            if (bits == 8) add(t[i].tops, (n + kBlock - 1) / kBlock * 4);
+        }
+        std::sort(ranges.begin(), ranges.end());
+        for (size_t i = 1; i < ranges.size(); ++i)
+            if (ranges[i].first < ranges[i - 1].second) return OMNI_ERR_BAD_CONFIG;
+        return OMNI_OK;
+    } catch (const std::bad_alloc &) {
+        return OMNI_ERR_NO_MEMORY;
+    }
+}
+
+// The header of a record that omni_adamw_plan wrote, or NULL.
+const Header *header_of(const void *record)
+{
+    const Header *h = static_cast<const Header *>(record);
+    return h->magic == kMagic && h->bytes == Layout(h->tensors, h->K, h->units).bytes ? h : nullptr;
+}
+
+template <typename G> void launch(const AdamParams &p, int bits, unsigned units, cudaStream_t s)
+{
+    if (bits == 8) adamw_kernel<G, 8><<<units, kThreads, 0, s>>>(p);
+    else adamw_kernel<G, 32><<<units, kThreads, 0, s>>>(p);
+}
+
+}  // namespace
+}  // namespace omni
+
+using namespace omni;
+
+extern "C" {
+
+int omni_adamw_plan_bytes(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, uint64_t *bytes)
+{
+    if (!bytes) return OMNI_ERR_NULL;
+    unsigned units = 0;
+    const int rc = check_tensors(tensors, count, K, grad_dtype, bits, &units);
+    if (rc == OMNI_OK) *bytes = Layout(count, K, units).bytes;
+    return rc;
+}
+
+int omni_adamw_plan(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, void *record, uint64_t bytes)
+{
+    if (!record) return OMNI_ERR_NULL;
+    if (!aligned(record, 8)) return OMNI_ERR_ALIGN;
+    unsigned units = 0;
+    int rc = check_tensors(tensors, count, K, grad_dtype, bits, &units);
+    if (rc == OMNI_OK) rc = check_apart(tensors, count, bits);
+    if (rc != OMNI_OK) return rc;
+    const Layout at(count, K, units);
+    if (bytes < at.bytes) return OMNI_ERR_TOO_LARGE;
+    char *const base = static_cast<char *>(record);
+    std::memset(base, 0, at.bytes);
+    Header *const h = reinterpret_cast<Header *>(base);
+    *h = {kMagic, at.bytes, count, K, grad_dtype, bits, units, {}};
+    Entry *const entries = reinterpret_cast<Entry *>(base + at.entries);
+    const void **const grads = reinterpret_cast<const void **>(base + at.grads);
+    unsigned *const owners = reinterpret_cast<unsigned *>(base + at.owners);
+    unsigned unit = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const omni_adamw_tensor &t = tensors[i];
+        entries[i] = {t.param, static_cast<__nv_bfloat16 *>(t.param_lp), t.m, t.v, static_cast<uint32_t *>(t.tops), t.n, t.weight_decay, unit,
+                      t.n > 0 && all_wide(t, K, bits)};
+        for (int k = 0; k < K && t.n > 0; ++k) grads[uint64_t(i) * K + k] = t.grads[k];
+        for (uint64_t j = 0; j < t.n; j += kUnit) owners[unit++] = unsigned(i);
+    }
+    return OMNI_OK;
+}
+
+int omni_adamw_step(omni_ctx *ctx, const void *record, const void *record_dev, const int32_t *b, double lr, double beta1, double beta2, float eps,
+                    int64_t step, const int64_t *clock_dev, void *stream)
+{
+    if (!ctx || !record || !record_dev || !b) return OMNI_ERR_NULL;
+    if (!aligned(record, 8) || !aligned(record_dev, 16) || !aligned(clock_dev, 8)) return OMNI_ERR_ALIGN;
+    const Header *const h = header_of(record);
+    if (!h || !(lr - lr == 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0f) || eps - eps != 0.0f ||
+        (!clock_dev && step < 1))
+        return OMNI_ERR_BAD_CONFIG;
+    double sum = 0.0;
+    for (int k = 0; k < h->K; ++k) {
+        if (b[k] < 1) return OMNI_ERR_BAD_BATCH;
+        sum += b[k];
+    }
+    ContextDevice dev;
+    const int rc = context_bind(ctx, &dev);
+    if (rc != OMNI_OK || h->units == 0) return rc;
+    const Layout at(h->tensors, h->K, h->units);
+    const char *const base = static_cast<const char *>(record_dev);
+    AdamParams p;
+    p.entries = reinterpret_cast<const Entry *>(base + at.entries);
+    p.grads = reinterpret_cast<const void *const *>(base + at.grads);
+    p.owners = reinterpret_cast<const unsigned *>(base + at.owners);
+    p.clock = reinterpret_cast<const long long *>(clock_dev);
+    p.lr = lr;
+    p.beta1 = beta1;
+    p.beta2 = beta2;
+    p.b1 = float(beta1);
+    p.b2 = float(beta2);
+    p.c1 = float(1.0 - beta1);
+    p.c2 = float(1.0 - beta2);
+    p.eps = eps;
+    p.rate = clock_dev ? 0.0f : float(lr / (1.0 - std::pow(beta1, double(step))));
+    p.spread = clock_dev ? 0.0f : float(1.0 / std::sqrt(1.0 - std::pow(beta2, double(step))));
+    p.step = unsigned(uint64_t(step));
+    p.K = h->K;
+    for (int k = 0; k < h->K; ++k) p.lambda[k] = float(b[k] / sum);
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (h->grad_dtype == OMNI_BF16) launch<__nv_bfloat16>(p, h->bits, h->units, s);
+    else launch<float>(p, h->bits, h->units, s);
+    return context_launched(ctx, int(cudaGetLastError()));
+}
+
+int omni_adamw_moments(omni_ctx *ctx, const void *record, const void *record_dev, float *const *m, float *const *v, void *stream)
+{
+    if (!ctx || !record || !record_dev) return OMNI_ERR_NULL;
+    if (!aligned(record, 8) || !aligned(record_dev, 16)) return OMNI_ERR_ALIGN;
+    const Header *const h = header_of(record);
+    if (!h || h->bits != 8) return OMNI_ERR_BAD_CONFIG;
+    if (h->tensors > 0 && (!m || !v)) return OMNI_ERR_NULL;
+    const Layout at(h->tensors, h->K, h->units);
+    const Entry *const entries = reinterpret_cast<const Entry *>(static_cast<const char *>(record) + at.entries);
+    for (int i = 0; i < h->tensors; ++i) {
+        if (entries[i].n == 0) continue;
+        if (!m[i] || !v[i]) return OMNI_ERR_NULL;
+        if (!aligned(m[i], 4) || !aligned(v[i], 4)) return OMNI_ERR_ALIGN;
+    }
+    ContextDevice dev;
+    int rc = context_bind(ctx, &dev);
+    const char *const base = static_cast<const char *>(record_dev);
+    MomentParams p;
+    p.entries = reinterpret_cast<const Entry *>(base + at.entries);
+    p.owners = reinterpret_cast<const unsigned *>(base + at.owners);
+    for (int i = 0; rc == OMNI_OK && i < h->tensors; i += kPerLaunch) {
+        const int last = i + kPerLaunch < h->tensors ? i + kPerLaunch : h->tensors;
+        p.first = i;
+        p.first_unit = entries[i].first_unit;
+        const unsigned units = (last < h->tensors ? entries[last].first_unit : h->units) - p.first_unit;
+        if (units == 0) continue;
+        for (int j = i; j < last; ++j) {
+            p.m[j - i] = m[j];
+            p.v[j - i] = v[j];
+        }
+        adamw_moments_kernel<<<units, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
+        rc = context_launched(ctx, int(cudaGetLastError()));
+    }
+    return rc;
+}
+
+}  // extern "C"

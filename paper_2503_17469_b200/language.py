@@ -540,3 +540,126 @@ class Policy(_Operator):
         self._check(self._lib.omni_policy_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
                                                grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
         return loss, logp, lse, grad
+
+
+class AdamW(_Operator):
+    """AdamW on a list of tensors, in one launch, from the batch-weighted gradients of K workers.
+
+    ``params``: float32 tensors; ``grads[i][k]``: worker k's gradient of tensor i, float32 or bfloat16; ``copies``: bfloat16 tensors
+    that receive the rounded parameters, or None.  All contiguous, of the current device, and kept alive by this object, which
+    notes where they lie: they are updated in place and are not to be replaced.  ``weight_decay``: one for all or one for each.
+    ``bits``: 32, or 8 for moments in one byte each with stochastic rounding (formats and formulas in ``include/omni.h``).
+    ``state``: (m, v) float32 tensors, or (m, v, tops) uint8, uint8 and int16 [blocks, 2], for each tensor, to go on from; zeros
+    by default.  ``state`` and ``steps`` (how many have been made) are what a checkpoint holds."""
+
+    def __init__(self, ctx: "B.Omni", params, grads, copies=None, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay=0.01, bits: int = 32,
+                 state=None, steps: int = 0):
+        super().__init__(ctx)
+        params, grads = list(params), [list(g) for g in grads]
+        copies = [None] * len(params) if copies is None else list(copies)
+        decay = [float(weight_decay)] * len(params) if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        if bits not in (8, 32):
+            raise ValueError("bits are 8 or 32")
+        if not len(params) == len(grads) == len(copies) == len(decay):
+            raise ValueError("params, grads, copies and weight_decay: as many of each are wanted")
+        if not (0 <= betas[0] < 1 and 0 <= betas[1] < 1 and 0 <= eps < float("inf")) or steps < 0:
+            raise ValueError("betas are in [0, 1), eps is finite and not negative, steps is not negative")
+        self.K = len(grads[0]) if grads else 1
+        if not 1 <= self.K <= B.MAX_K or any(len(g) != self.K for g in grads):
+            raise ValueError(f"every tensor has the gradients of as many workers, 1 to {B.MAX_K}")
+        self._at = _device()
+        if state is None:
+            state = [self._zeros(p, bits) for p in params]
+        self.state = [tuple(s) for s in state]
+        if len(self.state) != len(params):
+            raise ValueError("state: as many as params are wanted")
+        dtype = grads[0][0].dtype if grads else _float
+        code = B.F32 if not grads else _code(grads[0][0], _DTYPES, "grads")
+        moments = (_float, _float) if bits == 32 else (_byte, _byte, torch.int16)
+        array = (B.omni_adamw_tensor * max(1, len(params)))()
+        self._tables = []
+        for i, (p, gs, c, s) in enumerate(zip(params, grads, copies, self.state)):
+            n, shape = p.numel(), p.shape
+            if len(s) != len(moments):
+                raise ValueError(f"state[{i}]: {len(moments)} tensors are wanted")
+            blocks = torch.Size((-(-n // B.ADAMW_BLOCK), 2))
+            for what, t, kind, size in (("params", p, _float, shape), ("copies", c, _bf16, shape), *(("grads", g, dtype, shape) for g in gs),
+                                        *(("state", t, kind, blocks if kind == torch.int16 else shape) for t, kind in zip(s, moments))):
+                if t is None and what == "copies":
+                    continue
+                if t.dtype != kind:
+                    raise TypeError(f"{what}[{i}]: dtype {t.dtype}, {kind} is wanted")
+                if t.shape != size or not t.is_contiguous():
+                    raise ValueError(f"{what}[{i}]: a contiguous tensor of shape {tuple(size)} is wanted, got {tuple(t.shape)}, strides {t.stride()}")
+                if not t.is_cuda or t.get_device() != self._at:
+                    raise _elsewhere(**{what: t})
+            table = (C.c_void_p * self.K)(*(g.data_ptr() for g in gs))
+            self._tables.append(table)
+            array[i] = B.omni_adamw_tensor(p.data_ptr(), None if c is None else c.data_ptr(), table, s[0].data_ptr(), s[1].data_ptr(),
+                                           s[2].data_ptr() if bits == 8 else None, n, decay[i])
+        self._keep = (params, grads, copies)
+        self.betas, self.eps, self.bits, self.steps = (float(betas[0]), float(betas[1])), float(eps), bits, int(steps)
+        need = C.c_uint64()
+        self._check(self._lib.omni_adamw_plan_bytes(array, len(params), self.K, code, bits, _ref(need)))
+        host = torch.empty(need.value, dtype=_byte)
+        self._check(self._lib.omni_adamw_plan(array, len(params), self.K, code, bits, host.data_ptr(), need.value))
+        self._record = host
+        self._record_dev = host.to(f"cuda:{self._at}")
+        self._batches = C.c_int32 * self.K
+
+    @staticmethod
+    def _zeros(p, bits):
+        if bits == 32:
+            return tuple(torch.zeros(p.shape, dtype=_float, device=p.device) for _ in range(2))
+        return (*(torch.zeros(p.shape, dtype=_byte, device=p.device) for _ in range(2)),
+                torch.zeros((-(-p.numel() // B.ADAMW_BLOCK), 2), dtype=torch.int16, device=p.device))
+
+    def step(self, lr: float, batches=None, clock=None, stream=None) -> None:
+        """One step with the gradients that lie in ``grads`` now.  ``batches``: the K workers' batch sizes (of one worker: not needed).
+        The step's number is ``steps`` + 1, which ``steps`` becomes; with ``clock``, an int64 tensor of one element on the device, it is what
+        that holds when the step runs (1 for the first), and ``steps`` stays: for a captured graph that also adds 1 to the clock."""
+        if batches is None:
+            if self.K > 1:
+                raise ValueError("batches: the workers' batch sizes are wanted")
+            batches = (1,)
+        if len(batches) != self.K:
+            raise ValueError(f"batches: {self.K} of them are wanted")
+        if self._at != _device():
+            raise _elsewhere(params=self._record_dev)
+        at = None
+        if clock is not None:
+            if clock.dtype != torch.int64 or clock.numel() != 1 or clock.get_device() != self._at:
+                raise ValueError("clock: an int64 tensor of one element on the current device is wanted")
+            at = clock.data_ptr()
+        raw = _raw_stream(self._at) if stream is None else stream.cuda_stream
+        self._check(self._lib.omni_adamw_step(self.ctx._h, self._record.data_ptr(), self._record_dev.data_ptr(), self._batches(*batches), lr,
+                                              *self.betas, self.eps, self.steps + 1, at, raw))
+        if clock is None:
+            self.steps += 1
+
+    def moments(self, out=None, stream=None):
+        """[(m, v)] as float32, for each tensor: the state itself at 32 bits, at 8 bits what its codes stand for, into ``out`` if given."""
+        if stream is not None:
+            with self._on_stream(stream):
+                return self.moments(out)
+        if self._at != _device():
+            raise _elsewhere(params=self._record_dev)
+        if self.bits == 32:
+            if out is None:
+                return list(self.state)
+            raise ValueError("out: moments of 32 bits are the state itself")
+        if out is None:
+            out = [tuple(torch.empty(s[0].shape, dtype=_float, device=s[0].device) for _ in range(2)) for s in self.state]
+        if len(out) != len(self.state):
+            raise ValueError("out: a pair for each tensor is wanted")
+        tables = []
+        for j in range(2):
+            table = (C.c_void_p * max(1, len(out)))()
+            for i, pair in enumerate(out):
+                t = pair[j]
+                if t.dtype != _float or t.shape != self.state[i][0].shape or not t.is_contiguous() or t.get_device() != self._at:
+                    raise ValueError(f"out[{i}]: contiguous float32 of shape {tuple(self.state[i][0].shape)} on the current device is wanted")
+                table[i] = t.data_ptr()
+            tables.append(table)
+        self._check(self._lib.omni_adamw_moments(self.ctx._h, self._record.data_ptr(), self._record_dev.data_ptr(), *tables, _raw_stream(self._at)))
+        return out
