@@ -15,7 +15,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxPairs = OMNI_ROTARY_MAX_DIM / 2;
-constexpr int kMaxTile = 32;                          // rows whose angles a block holds
+constexpr int kMaxTile = 16;                          // rows whose angles a block holds
 constexpr int kResident = 2;                          // backward blocks an SM
 constexpr double kInvTwoPi = 0.15915494309189533577;
 
@@ -43,43 +43,12 @@ struct RotaryParams {
     unsigned char axis[kMaxPairs];
 };
 
-// V consecutive elements, kept as loaded.
-template <typename T, int V> struct Chunk;
-template <> struct Chunk<__nv_bfloat16, 8> {
-    uint4 u;
-    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
-    __device__ __forceinline__ void get(float *f) const { widen(u, f); }
-};
-template <> struct Chunk<float, 8> {
-    float v[8];
-    __device__ __forceinline__ void load(const float *p) { load_group(p, v); }
-    __device__ __forceinline__ void get(float *f) const
-    {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = v[i];
-    }
-};
-template <typename T> struct Chunk<T, 1> {
-    T v;
-    __device__ __forceinline__ void load(const T *p) { v = *p; }
-    __device__ __forceinline__ void get(float *f) const { *f = to_float(v); }
-};
-template <typename T, int V> __device__ __forceinline__ void put(T *p, const float *f)
-{
-    if constexpr (V == 8) store_group(p, f);
-    else *p = from_float<T>(*f);
-}
-
-// What a lane has of a head vector: UNITS units of V pairs, that is two chunks of V elements each.  With V = 8 one unit is enough
-// (16 lanes hold 256 elements); element by element it takes up to four.
-template <int V> constexpr int kUnits = V == 8 ? 1 : kMaxPairs / 32;
-
-// Where a unit's two chunks stand.  The elements that are not rotated are pairs of angle zero behind the others.
+// Where the two parts of UNIT pairs stand (UNIT elements each).  The elements that are not rotated are pairs of angle zero behind the others.
 struct Place { int a, b; };
-template <int V> __device__ __forceinline__ Place place(const RotaryParams &p, int unit)
+template <int UNIT> __device__ __forceinline__ Place place(const RotaryParams &p, int unit)
 {
-    const int first = unit * V;
-    if (p.interleaved) return {2 * first, 2 * first + V};
+    const int first = unit * UNIT;
+    if (p.interleaved) return {2 * first, 2 * first + UNIT};
     const int rest = p.dim / 2 - p.pairs;
     return first < p.pairs ? Place{first, first + p.pairs} : Place{first + p.pairs, first + p.pairs + rest};
 }
@@ -90,284 +59,540 @@ __device__ __forceinline__ float group_sum(float x, int lanes)
     return x;
 }
 
-// The first and second elements of pair i of a unit's 2 V elements.
-template <int V, bool ADJACENT> __device__ __forceinline__ constexpr int first_of(int i) { return ADJACENT ? 2 * i : i; }
-template <int V, bool ADJACENT> __device__ __forceinline__ constexpr int second_of(int i) { return ADJACENT ? 2 * i + 1 : i + V; }
+// A row of the batch, and where its heads start in an operand.
+struct RowAt {
+    unsigned batch, i;
+    bool mine, there;                                 // a row of the call; not behind its sequence's length
+    __device__ __forceinline__ RowAt(const RotaryParams &p, unsigned row) : mine(row < p.rows)
+    {
+        batch = row / p.length;
+        i = row - batch * p.length;
+        there = mine && (!p.lengths || int(i) < p.lengths[batch]);
+    }
+    template <typename T> __device__ __forceinline__ T *in(const View &v) const { return static_cast<T *>(v.data) + batch * v.batch + i * v.row; }
+};
 
-// A table row of cosines, then sines: a unit's eight as two pieces of four in two planes, so that neighbouring lanes
-// read neighbouring 16 bytes.
-template <int V> __device__ __forceinline__ int cell(int pair, int half)
+// A table row of cosines, then sines, four floats behind the next so that rows start in different banks.  WIDE: a unit's eight as two
+// pieces of four in two planes, so that neighbouring lanes read neighbouring 16 bytes.
+__host__ __device__ __forceinline__ int table_row(int dim) { return dim + 4; }
+template <bool WIDE> __device__ __forceinline__ int cell(int pair, int half)
 {
-    return V == 8 ? (pair & 4 ? half / 2 : 0) + pair / 8 * 4 + pair % 4 : pair;
+    return WIDE ? (pair & 4 ? half / 2 : 0) + pair / 8 * 4 + pair % 4 : pair;
 }
 
-template <int V> __device__ __forceinline__ void fill_angles(const RotaryParams &p, unsigned first, float *table)
+// The angles of a tile, each lane for one row of it, so that the lanes of a warp ask for few frequencies.
+template <bool WIDE> __device__ __forceinline__ void fill_angles(const RotaryParams &p, unsigned first, float *table)
 {
-    const int half = p.dim / 2;
-    for (int i = threadIdx.x; i < p.tile * half; i += kThreads) {
-        const int k = i / half, pair = i % half;
-        const unsigned row = first + k;
+    const int half = p.dim / 2, k = threadIdx.x & (p.tile - 1);
+    const RowAt row(p, first + k);
+    const unsigned long long at = row.batch * p.position_batch + row.i * p.position_row;
+    float *const out = table + k * table_row(p.dim);
+    double position = 0.0;
+    int axis = -1;
+    for (int pair = threadIdx.x / p.tile; pair < half; pair += kThreads / p.tile) {
         float c = 1.0f, s = 0.0f;
-        if (pair < p.pairs && row < p.rows) {
-            const unsigned long long at = p.axis[pair] * p.position_axis + row / p.length * p.position_batch + row % p.length * p.position_row;
-            const long long position = p.wide_positions ? load_index<long long>(p.positions, at) : load_index<int>(p.positions, at);
+        if (pair < p.pairs && row.mine) {
+            if (p.axis[pair] != axis) {
+                axis = p.axis[pair];
+                const unsigned long long j = at + axis * p.position_axis;
+                position = double(p.wide_positions ? load_index<long long>(p.positions, j) : load_index<int>(p.positions, j));
+            }
             // in turns and in 64 bits: what is left of the angle after its whole turns keeps 2^-51 of the angle
-            const double turns = double(position) * (p.frequency[pair] * kInvTwoPi);
+            const double turns = position * (p.frequency[pair] * kInvTwoPi);
             sincospif(2.0f * float(turns - rint(turns)), &s, &c);
             s *= p.turn;
         }
-        table[k * p.dim + cell<V>(pair, half)] = c;
-        table[k * p.dim + half + cell<V>(pair, half)] = s;
-    }
-}
-template <int V> __device__ __forceinline__ void read_angles(const float *row, int half, int unit, float *c, float *s)
-{
-    if constexpr (V == 8) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float4 x = *reinterpret_cast<const float4 *>(row + h * (half / 2) + unit * 4);
-            const float4 y = *reinterpret_cast<const float4 *>(row + half + h * (half / 2) + unit * 4);
-            c[4 * h] = x.x; c[4 * h + 1] = x.y; c[4 * h + 2] = x.z; c[4 * h + 3] = x.w;
-            s[4 * h] = y.x; s[4 * h + 1] = y.y; s[4 * h + 2] = y.z; s[4 * h + 3] = y.w;
-        }
-    } else {
-        *c = row[unit];
-        *s = row[half + unit];
+        out[cell<WIDE>(pair, half)] = c;
+        out[half + cell<WIDE>(pair, half)] = s;
     }
 }
 
-template <typename T> __device__ __forceinline__ T *vector_at(const View &v, unsigned row, unsigned length, int head)
-{
-    return static_cast<T *>(v.data) + row / length * v.batch + row % length * v.row + head * v.head;
-}
-
-// What a lane keeps for its row: angles and places, and for the block's side its part of the weights.
-template <int V> struct Lane {
-    static constexpr int kN = kUnits<V>;
-    int group, lane, first_head, stride;              // heads of this group: first_head, first_head + stride, ...
-    float w[kN][2 * V];
-    Place at[kN];
-    bool has[kN];
-    __device__ __forceinline__ Lane(const RotaryParams &p, const Side &side, bool norm)
+// How a block's threads share a tile: `lanes` of a head vector, groups of them that go through the heads of one row.
+struct Share {
+    int lane, row, first, stride, turns;              // heads first, first + stride, ...; every group of a block takes `turns` turns, for the shuffles
+    __device__ __forceinline__ Share(const RotaryParams &p, int heads)
     {
-        group = threadIdx.x / p.lanes;
+        const int group = threadIdx.x / p.lanes;
         lane = threadIdx.x % p.lanes;
-        stride = kThreads / p.lanes / p.tile;         // groups of a row
-        first_head = group % stride;
-#pragma unroll
-        for (int n = 0; n < kN; ++n) {
-            const int unit = lane + n * p.lanes;
-            has[n] = unit * V < p.dim / 2;
-            at[n] = place<V>(p, has[n] ? unit : 0);
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) {
-                const int c = e < V ? at[n].a + e : at[n].b + e - V;
-                w[n][e] = !norm ? 1.0f : p.bf16_weight ? to_float(static_cast<const __nv_bfloat16 *>(side.weight)[c])
-                                                       : static_cast<const float *>(side.weight)[c];
-            }
-        }
+        stride = kThreads / p.lanes / p.tile;
+        row = group / stride;
+        first = group % stride;
+        turns = (heads + stride - 1) / stride;
     }
-    __device__ __forceinline__ int row_in_tile() const { return group / stride; }
 };
 
-__device__ __forceinline__ bool row_there(const RotaryParams &p, unsigned row)
+__device__ __forceinline__ float weight_at(const RotaryParams &p, const Side &side, int c)
 {
-    return !p.lengths || int(row % p.length) < p.lengths[row / p.length];
+    return p.bf16_weight ? to_float(static_cast<const __nv_bfloat16 *>(side.weight)[c]) : static_cast<const float *>(side.weight)[c];
 }
 
-// Forward: a block has a tile of rows of one side; a group of lanes goes through heads of one row, AHEAD of them in flight.
-template <typename T, int V, bool ADJACENT, bool NORM>
-__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
+// A block's sums of the weight's gradient: f(channel) of each lane's elements, groups of a warp by shuffles, then the warps in order.
+__device__ __forceinline__ float warp_groups_sum(float v, int lanes)
 {
-    extern __shared__ __align__(16) float table[];
-    constexpr int kN = kUnits<V>, kAhead = sizeof(T) == 2 ? 4 : 2;
+    for (int o = 16; o >= lanes; o /= 2) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+__device__ __forceinline__ void put_partial(const RotaryParams &p, const float *sums, float *partial)
+{
+    for (int ch = threadIdx.x; ch < p.dim; ch += kThreads) {
+        float v = sums[ch];
+        for (int w = 1; w < kWarps; ++w) v += sums[w * p.dim + ch];
+        partial[ch] = v;
+    }
+}
+
+// ---- wide accesses: a lane has a unit of eight pairs, fetched ahead by asynchronous copies into slots of its own ----------------
+
+// Eight elements in shared memory: pieces of 16 bytes, each piece of all threads side by side.
+template <typename T> constexpr int kPieces = int(sizeof(T)) / 2;
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// CHUNKS chunks of eight elements a stage.
+template <typename T, int CHUNKS, int STAGES> struct Ring {
+    static constexpr int kStage = CHUNKS * kPieces<T> * kThreads * 16;
+    static constexpr int kBytes = STAGES * kStage;
+    char *base;
+    uint32_t shared;
+    __device__ __forceinline__ explicit Ring(char *at) : base(at + threadIdx.x * 16), shared(uint32_t(__cvta_generic_to_shared(base))) {}
+    __device__ __forceinline__ void fetch(int stage, int chunk, const T *from) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPieces<T>; ++i)
+            copy_async(shared + stage * kStage + (chunk * kPieces<T> + i) * kThreads * 16, reinterpret_cast<const char *>(from) + 16 * i);
+    }
+    __device__ __forceinline__ void get(int stage, int chunk, float *f) const
+    {
+        const char *const at = base + stage * kStage + chunk * kPieces<T> * kThreads * 16;
+        if constexpr (sizeof(T) == 2) {
+            widen(*reinterpret_cast<const uint4 *>(at), f);
+        } else {
+            const float4 x = *reinterpret_cast<const float4 *>(at), y = *reinterpret_cast<const float4 *>(at + kThreads * 16);
+            f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+            f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+        }
+    }
+};
+
+// A unit's 16 elements, in the order of its two chunks, as two pairs (of first or of second elements) of consecutive rotations.
+template <bool ADJACENT> __device__ __forceinline__ float2 firsts(const float *f, int i)
+{
+    return ADJACENT ? make_float2(f[4 * i], f[4 * i + 2]) : make_float2(f[2 * i], f[2 * i + 1]);
+}
+template <bool ADJACENT> __device__ __forceinline__ float2 seconds(const float *f, int i)
+{
+    return ADJACENT ? make_float2(f[4 * i + 1], f[4 * i + 3]) : make_float2(f[8 + 2 * i], f[8 + 2 * i + 1]);
+}
+template <bool ADJACENT> __device__ __forceinline__ void put_pairs(float *f, int i, float2 a, float2 b)
+{
+    if (ADJACENT) {
+        f[4 * i] = a.x; f[4 * i + 2] = a.y; f[4 * i + 1] = b.x; f[4 * i + 3] = b.y;
+    } else {
+        f[2 * i] = a.x; f[2 * i + 1] = a.y; f[8 + 2 * i] = b.x; f[8 + 2 * i + 1] = b.y;
+    }
+}
+__device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
+
+// A unit's eight cosines (or sines) as four pairs.
+__device__ __forceinline__ void read_plane(const float *at, int half, int unit, float2 *c)
+{
+    const float4 x = *reinterpret_cast<const float4 *>(at + unit * 4), y = *reinterpret_cast<const float4 *>(at + half / 2 + unit * 4);
+    c[0] = make_float2(x.x, x.y);
+    c[1] = make_float2(x.z, x.w);
+    c[2] = make_float2(y.x, y.y);
+    c[3] = make_float2(y.z, y.w);
+}
+template <bool ADJACENT> __device__ __forceinline__ void read_weights(const RotaryParams &p, const Side &side, Place at, float2 *wa, float2 *wb)
+{
+    float f[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) f[e] = weight_at(p, side, e < 8 ? at.a + e : at.b + e - 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        wa[i] = firsts<ADJACENT>(f, i);
+        wb[i] = seconds<ADJACENT>(f, i);
+    }
+}
+
+template <typename T> constexpr int kForwardStages = sizeof(T) == 2 ? 6 : 4;
+template <typename T> using ForwardRing = Ring<T, 2, kForwardStages<T>>;
+
+// Forward: a block has a tile of rows of one side.  With weights they are folded into the angles, and a result is
+// y_a = r ((w_a cos) x_a - (w_b sin) x_b), y_b = r ((w_b cos) x_b + (w_a sin) x_a).
+template <typename T, bool ADJACENT, bool NORM>
+__global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const __grid_constant__ RotaryParams p)
+{
+    extern __shared__ __align__(16) char shared[];
+    constexpr int kStages = kForwardStages<T>;
+    const ForwardRing<T> ring(shared);
+    float *const table = reinterpret_cast<float *>(shared + ForwardRing<T>::kBytes);
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
     const unsigned first = (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * unsigned(p.tile);
-    const Lane<V> me(p, side, NORM);
-    const unsigned row = first + me.row_in_tile();
-    const bool mine = row < p.rows, there = mine && row_there(p, row);
+    const Share me(p, side.heads);
+    const RowAt row(p, first + me.row);
+    const bool has = me.lane * 16 < p.dim;
+    const Place at = place<8>(p, has ? me.lane : 0);
+    const T *const src = row.in<T>(side.x);
+    T *const dst = row.in<T>(side.out);
+    const auto fetch = [&](int turn, int stage) {
+        const int head = me.first + turn * me.stride;
+        if (head < side.heads && row.there && has) {
+            ring.fetch(stage, 0, src + head * side.x.head + at.a);
+            ring.fetch(stage, 1, src + head * side.x.head + at.b);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int j = 0; j < kStages - 1; ++j) fetch(j, j);
+    fill_angles<true>(p, first, table);
+    float2 ca[4], sa[4], cb[4], sb[4];                // cos and sin, with weights those times w_a and w_b
+    if constexpr (NORM) read_weights<ADJACENT>(p, side, at, ca, cb);
+    __syncthreads();
+    {
+        const float *const mine = table + me.row * table_row(p.dim);
+        float2 c[4], s[4];
+        read_plane(mine, p.dim / 2, has ? me.lane : 0, c);
+        read_plane(mine + p.dim / 2, p.dim / 2, has ? me.lane : 0, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sa[i] = NORM ? mul2(s[i], ca[i]) : s[i];
+            sb[i] = NORM ? mul2(s[i], cb[i]) : s[i];
+            ca[i] = NORM ? mul2(c[i], ca[i]) : c[i];
+            cb[i] = NORM ? mul2(c[i], cb[i]) : c[i];
+        }
+    }
     const float inverse_dim = 1.0f / float(p.dim);
-    const int half = p.dim / 2;
-    float c[kN][V], s[kN][V];
-    // every group of a warp takes as many turns, for the shuffles
-    for (int h0 = 0; h0 < side.heads; h0 += me.stride * kAhead) {
-        Chunk<T, V> x[kAhead][kN][2];
+    int stage = 0;
+    for (int j = 0; j < me.turns; ++j) {
+        copies_wait<kStages - 2>();
+        const int head = me.first + j * me.stride;
+        const bool work = head < side.heads && row.mine && has, live = work && row.there;
+        float f[16];
+        if (live) {
+            ring.get(stage, 0, f);
+            ring.get(stage, 1, f + 8);
+        } else {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int head = h0 + i * me.stride + me.first_head;
-            if (there && head < side.heads) {
-                const T *src = vector_at<T>(side.x, row, p.length, head);
-#pragma unroll
-                for (int n = 0; n < kN; ++n)
-                    if (me.has[n]) {
-                        x[i][n][0].load(src + me.at[n].a);
-                        x[i][n][1].load(src + me.at[n].b);
-                    }
-            }
+            for (int e = 0; e < 16; ++e) f[e] = 0.0f;
         }
-        if (h0 == 0) {                                // the first loads are under way
-            fill_angles<V>(p, first, table);
-            __syncthreads();
+        // into the slot that the turn before this one has used up
+        fetch(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        float2 r = {1.0f, 1.0f};
+        if constexpr (NORM) {
+            float2 sum = {0.0f, 0.0f};
 #pragma unroll
-            for (int n = 0; n < kN; ++n)
-                if (me.has[n]) read_angles<V>(table + me.row_in_tile() * p.dim, half, me.lane + n * p.lanes, c[n], s[n]);
+            for (int e = 0; e < 8; ++e) sum = fma2(make_float2(f[2 * e], f[2 * e + 1]), make_float2(f[2 * e], f[2 * e + 1]), sum);
+            r.x = r.y = rsqrtf(fmaf(group_sum(sum.x + sum.y, p.lanes), inverse_dim, p.eps));
         }
+        if (!work) continue;
+        if (live) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int head = h0 + i * me.stride + me.first_head;
-            const bool work = mine && head < side.heads;
-            float f[kN][2 * V], r = 1.0f;
-#pragma unroll
-            for (int n = 0; n < kN; ++n) {
-                if (work && there && me.has[n]) {
-                    x[i][n][0].get(f[n]);
-                    x[i][n][1].get(f[n] + V);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) f[n][e] = 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+                float2 ya = fma2(a, ca[i], minus(mul2(b, sb[i]))), yb = fma2(b, cb[i], mul2(a, sa[i]));
+                if constexpr (NORM) {
+                    ya = mul2(ya, r);
+                    yb = mul2(yb, r);
                 }
-            }
-            if constexpr (NORM) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int n = 0; n < kN; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) sum = fmaf(f[n][e], f[n][e], sum);
-                r = 1.0f / sqrtf(fmaf(group_sum(sum, p.lanes), inverse_dim, p.eps));
-            }
-            if (!work) continue;
-            T *dst = vector_at<T>(side.out, row, p.length, head);
-#pragma unroll
-            for (int n = 0; n < kN; ++n) {
-                if (!me.has[n]) continue;
-                if (there) {
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const int a = first_of<V, ADJACENT>(j), b = second_of<V, ADJACENT>(j);
-                        const float na = NORM ? f[n][a] * r * me.w[n][a] : f[n][a], nb = NORM ? f[n][b] * r * me.w[n][b] : f[n][b];
-                        f[n][a] = fmaf(na, c[n][j], -nb * s[n][j]);
-                        f[n][b] = fmaf(nb, c[n][j], na * s[n][j]);
-                    }
-                }
-                put<T, V>(dst + me.at[n].a, f[n]);
-                put<T, V>(dst + me.at[n].b, f[n] + V);
+                put_pairs<ADJACENT>(f, i, ya, yb);
             }
         }
+        store_group(dst + head * side.out.head + at.a, f);
+        store_group(dst + head * side.out.head + at.b, f + 8);
     }
 }
 
+template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 3;
+template <typename T> using BackwardRing = Ring<T, 4, kBackwardStages<T>>;
+
 // Backward of the norm and the rotation: blocks that stay, each on tiles of one side, with the weight's gradient in registers.
-template <typename T, int V, bool ADJACENT>
-__global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
+template <typename T, bool ADJACENT>
+__global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
-    extern __shared__ __align__(16) float table[];
-    constexpr int kN = kUnits<V>, kAhead = 2;
+    extern __shared__ __align__(16) char shared[];
+    constexpr int kStages = kBackwardStages<T>;
+    const BackwardRing<T> ring(shared);
+    float *const table = reinterpret_cast<float *>(shared + BackwardRing<T>::kBytes);
     let_next_begin(p.overlap);
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
     const unsigned block = blockIdx.x - (keys ? p.side[0].blocks : 0u);
-    const Lane<V> me(p, side, true);
+    const Share me(p, side.heads);
+    const bool has = me.lane * 16 < p.dim;
+    const Place at = place<8>(p, has ? me.lane : 0);
+    float2 wa[4], wb[4], da[4] = {}, db[4] = {};
+    read_weights<ADJACENT>(p, side, at, wa, wb);
     const float inverse_dim = 1.0f / float(p.dim);
-    const int half = p.dim / 2;
-    float dw[kN][2 * V] = {};
     const unsigned tiles = (p.rows + p.tile - 1) / p.tile;
     for (unsigned t = block; t < tiles; t += side.blocks) {
-        const unsigned first = t * unsigned(p.tile), row = first + me.row_in_tile();
-        const bool mine = row < p.rows, there = mine && row_there(p, row);
-        float c[kN][V], s[kN][V];
-        for (int h0 = 0; h0 < side.heads; h0 += me.stride * kAhead) {
-            Chunk<T, V> x[kAhead][kN][2], y[kAhead][kN][2];
+        const unsigned first = t * unsigned(p.tile);
+        const RowAt row(p, first + me.row);
+        const T *const src = row.in<T>(side.x), *const grad = row.in<T>(side.dy);
+        T *const dst = row.in<T>(side.out);
+        const auto fetch = [&](int turn, int stage) {
+            const int head = me.first + turn * me.stride;
+            if (head < side.heads && row.there && has) {
+                ring.fetch(stage, 0, src + head * side.x.head + at.a);
+                ring.fetch(stage, 1, src + head * side.x.head + at.b);
+                ring.fetch(stage, 2, grad + head * side.dy.head + at.a);
+                ring.fetch(stage, 3, grad + head * side.dy.head + at.b);
+            }
+            copies_commit();
+        };
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int head = h0 + i * me.stride + me.first_head;
-                if (there && head < side.heads) {
-                    const T *src = vector_at<T>(side.x, row, p.length, head), *grad = vector_at<T>(side.dy, row, p.length, head);
+        for (int j = 0; j < kStages - 1; ++j) fetch(j, j);
+        __syncthreads();                              // the last tile's angles have been read
+        fill_angles<true>(p, first, table);
+        __syncthreads();
+        float2 c[4], s[4];
+        const float *const mine = table + me.row * table_row(p.dim);
+        read_plane(mine, p.dim / 2, has ? me.lane : 0, c);
+        read_plane(mine + p.dim / 2, p.dim / 2, has ? me.lane : 0, s);
+        int stage = 0;
+        for (int j = 0; j < me.turns; ++j) {
+            copies_wait<kStages - 2>();
+            const int head = me.first + j * me.stride;
+            const bool work = head < side.heads && row.mine && has, live = work && row.there;
+            float f[16], g[16];
+            if (live) {
+                ring.get(stage, 0, f);
+                ring.get(stage, 1, f + 8);
+                ring.get(stage, 2, g);
+                ring.get(stage, 3, g + 8);
+            } else {
 #pragma unroll
-                    for (int n = 0; n < kN; ++n)
-                        if (me.has[n]) {
-                            x[i][n][0].load(src + me.at[n].a);
-                            x[i][n][1].load(src + me.at[n].b);
-                            y[i][n][0].load(grad + me.at[n].a);
-                            y[i][n][1].load(grad + me.at[n].b);
-                        }
+                for (int e = 0; e < 16; ++e) f[e] = g[e] = 0.0f;
+            }
+            fetch(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            float2 square = {0.0f, 0.0f}, dot = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+                const float2 ya = firsts<ADJACENT>(g, i), yb = seconds<ADJACENT>(g, i);
+                const float2 na = fma2(ya, c[i], mul2(yb, s[i])), nb = fma2(yb, c[i], minus(mul2(ya, s[i])));
+                square = fma2(b, b, fma2(a, a, square));
+                dot = fma2(mul2(b, wb[i]), nb, fma2(mul2(a, wa[i]), na, dot));
+                put_pairs<ADJACENT>(g, i, na, nb);
+            }
+            const float squares = group_sum(square.x + square.y, p.lanes), dots = group_sum(dot.x + dot.y, p.lanes);
+            if (!work) continue;
+            if (live) {
+                const float scale = rsqrtf(fmaf(squares, inverse_dim, p.eps)), pull = -dots * inverse_dim * scale * scale;
+                const float2 r = {scale, scale}, q = {pull, pull};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+                    const float2 na = firsts<ADJACENT>(g, i), nb = seconds<ADJACENT>(g, i);
+                    da[i] = fma2(na, mul2(a, r), da[i]);
+                    db[i] = fma2(nb, mul2(b, r), db[i]);
+                    put_pairs<ADJACENT>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
                 }
             }
-            if (h0 == 0) {
+            store_group(dst + head * side.out.head + at.a, f);
+            store_group(dst + head * side.out.head + at.b, f + 8);
+        }
+    }
+    __syncthreads();
+    float dw[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) put_pairs<ADJACENT>(dw, i, da[i], db[i]);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const float v = warp_groups_sum(dw[e], p.lanes);
+        if (int(threadIdx.x % 32) < p.lanes && has) table[threadIdx.x / 32 * p.dim + (e < 8 ? at.a + e : at.b + e - 8)] = v;
+    }
+    __syncthreads();
+    put_partial(p, table, side.partial + (unsigned long long)block * p.dim);
+}
+
+// ---- any alignment: element by element, up to four pairs a lane in registers ------------------------------------------------------
+
+constexpr int kOwn = kMaxPairs / 32;                  // pairs of a lane
+struct Own {
+    Place at[kOwn];
+    bool has[kOwn];
+    float w[kOwn][2];
+    __device__ __forceinline__ Own(const RotaryParams &p, const Side &side, int lane, bool norm)
+    {
+#pragma unroll
+        for (int n = 0; n < kOwn; ++n) {
+            const int unit = lane + n * p.lanes;
+            has[n] = unit < p.dim / 2;
+            at[n] = place<1>(p, has[n] ? unit : 0);
+            w[n][0] = norm ? weight_at(p, side, at[n].a) : 1.0f;
+            w[n][1] = norm ? weight_at(p, side, at[n].b) : 1.0f;
+        }
+    }
+};
+
+template <typename T, bool NORM>
+__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
+{
+    extern __shared__ __align__(16) char shared[];
+    float *const table = reinterpret_cast<float *>(shared);
+    constexpr int kAhead = 4;                         // heads in flight
+    const bool keys = blockIdx.x >= p.side[0].blocks;
+    const Side &side = p.side[keys];
+    const unsigned first = (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * unsigned(p.tile);
+    const Share me(p, side.heads);
+    const RowAt row(p, first + me.row);
+    const Own own(p, side, me.lane, NORM);
+    const T *const src = row.in<T>(side.x);
+    T *const dst = row.in<T>(side.out);
+    const float inverse_dim = 1.0f / float(p.dim);
+    float c[kOwn], s[kOwn];
+    for (int j0 = 0; j0 < me.turns; j0 += kAhead) {
+        T x[kAhead][kOwn][2];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int head = me.first + (j0 + i) * me.stride;
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n)
+                if (row.there && head < side.heads && own.has[n]) {
+                    x[i][n][0] = src[head * side.x.head + own.at[n].a];
+                    x[i][n][1] = src[head * side.x.head + own.at[n].b];
+                }
+        }
+        if (j0 == 0) {                                // the first loads are under way
+            fill_angles<false>(p, first, table);
+            __syncthreads();
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n)
+                if (own.has[n]) {
+                    c[n] = table[me.row * table_row(p.dim) + me.lane + n * p.lanes];
+                    s[n] = table[me.row * table_row(p.dim) + p.dim / 2 + me.lane + n * p.lanes];
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int head = me.first + (j0 + i) * me.stride;
+            const bool work = row.mine && head < side.heads;
+            float f[kOwn][2], sum = 0.0f, r = 1.0f;
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    f[n][e] = work && row.there && own.has[n] ? to_float(x[i][n][e]) : 0.0f;
+                    sum = fmaf(f[n][e], f[n][e], sum);
+                }
+            if constexpr (NORM) r = rsqrtf(fmaf(group_sum(sum, p.lanes), inverse_dim, p.eps));
+            if (!work) continue;
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n) {
+                if (!own.has[n]) continue;
+                const float a = NORM ? f[n][0] * r * own.w[n][0] : f[n][0], b = NORM ? f[n][1] * r * own.w[n][1] : f[n][1];
+                T *const at = dst + head * side.out.head;
+                at[own.at[n].a] = from_float<T>(row.there ? fmaf(a, c[n], -b * s[n]) : 0.0f);
+                at[own.at[n].b] = from_float<T>(row.there ? fmaf(b, c[n], a * s[n]) : 0.0f);
+            }
+        }
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
+{
+    extern __shared__ __align__(16) char shared[];
+    float *const table = reinterpret_cast<float *>(shared);
+    constexpr int kAhead = 2;
+    let_next_begin(p.overlap);
+    const bool keys = blockIdx.x >= p.side[0].blocks;
+    const Side &side = p.side[keys];
+    const unsigned block = blockIdx.x - (keys ? p.side[0].blocks : 0u);
+    const Share me(p, side.heads);
+    const Own own(p, side, me.lane, true);
+    const float inverse_dim = 1.0f / float(p.dim);
+    float dw[kOwn][2] = {};
+    const unsigned tiles = (p.rows + p.tile - 1) / p.tile;
+    for (unsigned t = block; t < tiles; t += side.blocks) {
+        const unsigned first = t * unsigned(p.tile);
+        const RowAt row(p, first + me.row);
+        const T *const src = row.in<T>(side.x), *const grad = row.in<T>(side.dy);
+        T *const dst = row.in<T>(side.out);
+        float c[kOwn], s[kOwn];
+        for (int j0 = 0; j0 < me.turns; j0 += kAhead) {
+            T x[kAhead][kOwn][2], y[kAhead][kOwn][2];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int head = me.first + (j0 + i) * me.stride;
+#pragma unroll
+                for (int n = 0; n < kOwn; ++n)
+                    if (row.there && head < side.heads && own.has[n]) {
+                        x[i][n][0] = src[head * side.x.head + own.at[n].a];
+                        x[i][n][1] = src[head * side.x.head + own.at[n].b];
+                        y[i][n][0] = grad[head * side.dy.head + own.at[n].a];
+                        y[i][n][1] = grad[head * side.dy.head + own.at[n].b];
+                    }
+            }
+            if (j0 == 0) {
                 __syncthreads();                      // the last tile's angles have been read
-                fill_angles<V>(p, first, table);
+                fill_angles<false>(p, first, table);
                 __syncthreads();
 #pragma unroll
-                for (int n = 0; n < kN; ++n)
-                    if (me.has[n]) read_angles<V>(table + me.row_in_tile() * p.dim, half, me.lane + n * p.lanes, c[n], s[n]);
+                for (int n = 0; n < kOwn; ++n)
+                    if (own.has[n]) {
+                        c[n] = table[me.row * table_row(p.dim) + me.lane + n * p.lanes];
+                        s[n] = table[me.row * table_row(p.dim) + p.dim / 2 + me.lane + n * p.lanes];
+                    }
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int head = h0 + i * me.stride + me.first_head;
-                const bool work = mine && head < side.heads, live = work && there;
-                float f[kN][2 * V], g[kN][2 * V], square = 0.0f, dot = 0.0f;
+                const int head = me.first + (j0 + i) * me.stride;
+                const bool work = row.mine && head < side.heads, live = work && row.there;
+                float f[kOwn][2], g[kOwn][2], square = 0.0f, dot = 0.0f;
 #pragma unroll
-                for (int n = 0; n < kN; ++n) {
-                    if (live && me.has[n]) {
-                        x[i][n][0].get(f[n]);
-                        x[i][n][1].get(f[n] + V);
-                        y[i][n][0].get(g[n]);
-                        y[i][n][1].get(g[n] + V);
-#pragma unroll
-                        for (int j = 0; j < V; ++j) {
-                            const int a = first_of<V, ADJACENT>(j), b = second_of<V, ADJACENT>(j);
-                            const float ya = g[n][a], yb = g[n][b];
-                            g[n][a] = fmaf(ya, c[n][j], yb * s[n][j]);
-                            g[n][b] = fmaf(yb, c[n][j], -ya * s[n][j]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) f[n][e] = g[n][e] = 0.0f;
+                for (int n = 0; n < kOwn; ++n) {
+                    f[n][0] = f[n][1] = g[n][0] = g[n][1] = 0.0f;
+                    if (live && own.has[n]) {
+                        const float ya = to_float(y[i][n][0]), yb = to_float(y[i][n][1]);
+                        f[n][0] = to_float(x[i][n][0]);
+                        f[n][1] = to_float(x[i][n][1]);
+                        g[n][0] = fmaf(ya, c[n], yb * s[n]);
+                        g[n][1] = fmaf(yb, c[n], -ya * s[n]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 2 * V; ++e) {
+                    for (int e = 0; e < 2; ++e) {
                         square = fmaf(f[n][e], f[n][e], square);
-                        dot = fmaf(f[n][e] * me.w[n][e], g[n][e], dot);
+                        dot = fmaf(f[n][e] * own.w[n][e], g[n][e], dot);
                     }
                 }
                 square = group_sum(square, p.lanes);
                 dot = group_sum(dot, p.lanes);
                 if (!work) continue;
-                const float r = 1.0f / sqrtf(fmaf(square, inverse_dim, p.eps));
-                const float pull = dot * inverse_dim * r * r;
-                T *dst = vector_at<T>(side.out, row, p.length, head);
+                const float r = rsqrtf(fmaf(square, inverse_dim, p.eps)), pull = dot * inverse_dim * r * r;
+                T *const at = dst + head * side.out.head;
 #pragma unroll
-                for (int n = 0; n < kN; ++n) {
-                    if (!me.has[n]) continue;
-                    if (there) {
+                for (int n = 0; n < kOwn; ++n) {
+                    if (!own.has[n]) continue;
+                    float dx[2] = {0.0f, 0.0f};
 #pragma unroll
-                        for (int e = 0; e < 2 * V; ++e) {
+                    for (int e = 0; e < 2; ++e)
+                        if (row.there) {
                             dw[n][e] = fmaf(g[n][e], f[n][e] * r, dw[n][e]);
-                            f[n][e] = r * fmaf(-f[n][e], pull, g[n][e] * me.w[n][e]);
+                            dx[e] = r * fmaf(-f[n][e], pull, g[n][e] * own.w[n][e]);
                         }
-                    }
-                    put<T, V>(dst + me.at[n].a, f[n]);
-                    put<T, V>(dst + me.at[n].b, f[n] + V);
+                    at[own.at[n].a] = from_float<T>(dx[0]);
+                    at[own.at[n].b] = from_float<T>(dx[1]);
                 }
             }
         }
     }
-    // the block's sums: groups of a warp by shuffles, then the warps in order
     __syncthreads();
 #pragma unroll
-    for (int n = 0; n < kN; ++n)
+    for (int n = 0; n < kOwn; ++n)
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-            float v = dw[n][e];
-            for (int o = 16; o >= p.lanes; o /= 2) v += __shfl_xor_sync(~0u, v, o);
-            if (int(threadIdx.x % 32) < p.lanes && me.has[n]) table[threadIdx.x / 32 * p.dim + (e < V ? me.at[n].a + e : me.at[n].b + e - V)] = v;
+        for (int e = 0; e < 2; ++e) {
+            const float v = warp_groups_sum(dw[n][e], p.lanes);
+            if (int(threadIdx.x % 32) < p.lanes && own.has[n]) table[threadIdx.x / 32 * p.dim + (e ? own.at[n].b : own.at[n].a)] = v;
         }
     __syncthreads();
-    for (int ch = threadIdx.x; ch < p.dim; ch += kThreads) {
-        float v = table[ch];
-        for (int w = 1; w < kWarps; ++w) v += table[w * p.dim + ch];
-        side.partial[(unsigned long long)block * p.dim + ch] = v;
-    }
+    put_partial(p, table, side.partial + (unsigned long long)block * p.dim);
 }
 
 struct WeightParams {
@@ -512,25 +737,35 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
 // Whole units of eight pairs: rotated and unrotated halves of multiples of eight, or any pairs that stand next to one another.
 bool wide_units(const omni_rotary *r) { return r->dim % 16 == 0 && (r->interleaved || r->pairs % 8 == 0); }
 
+constexpr int kMostShared = 113 * 1024;               // dynamic shared memory of a block: two fit an SM
+
+size_t table_bytes(const RotaryParams &p, bool sums)
+{
+    const size_t angles = size_t(p.tile) * table_row(p.dim), partial = sums ? size_t(kWarps) * p.dim : 0;
+    return (angles > partial ? angles : partial) * sizeof(float);
+}
+
+int enqueue(omni_ctx *ctx, void (*kernel)(RotaryParams), const RotaryParams &p, size_t smem, cudaStream_t s)
+{
+    const int rc = smem > 48 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMostShared) : OMNI_OK;
+    if (rc != OMNI_OK) return rc;
+    kernel<<<p.side[0].blocks + p.side[1].blocks, kThreads, smem, s>>>(p);
+    return context_launched(ctx, int(cudaGetLastError()));
+}
+
 template <typename T, bool NORM>
 int enqueue_forward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
-    const unsigned grid = p.side[0].blocks + p.side[1].blocks;
-    const size_t smem = size_t(p.tile) * p.dim * sizeof(float);
-    if (!wide) rotary_forward_kernel<T, 1, false, NORM><<<grid, kThreads, smem, s>>>(p);
-    else if (p.interleaved) rotary_forward_kernel<T, 8, true, NORM><<<grid, kThreads, smem, s>>>(p);
-    else rotary_forward_kernel<T, 8, false, NORM><<<grid, kThreads, smem, s>>>(p);
-    return context_launched(ctx, int(cudaGetLastError()));
+    if (!wide) return enqueue(ctx, rotary_forward_kernel<T, NORM>, p, table_bytes(p, false), s);
+    return enqueue(ctx, p.interleaved ? rotary_forward_wide_kernel<T, true, NORM> : rotary_forward_wide_kernel<T, false, NORM>, p,
+                   ForwardRing<T>::kBytes + table_bytes(p, false), s);
 }
 
 template <typename T> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
-    const unsigned grid = p.side[0].blocks + p.side[1].blocks;
-    const size_t smem = size_t(p.tile > kWarps ? p.tile : kWarps) * p.dim * sizeof(float);
-    if (!wide) rotary_backward_kernel<T, 1, false><<<grid, kThreads, smem, s>>>(p);
-    else if (p.interleaved) rotary_backward_kernel<T, 8, true><<<grid, kThreads, smem, s>>>(p);
-    else rotary_backward_kernel<T, 8, false><<<grid, kThreads, smem, s>>>(p);
-    return context_launched(ctx, int(cudaGetLastError()));
+    if (!wide) return enqueue(ctx, rotary_backward_kernel<T>, p, table_bytes(p, true), s);
+    return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, true> : rotary_backward_wide_kernel<T, false>, p,
+                   BackwardRing<T>::kBytes + table_bytes(p, true), s);
 }
 
 // One pass over both sides without sums: the forward call, and the gradient where there are no weights.
