@@ -513,8 +513,8 @@ int omni_distill_step(omni_ctx *ctx, const omni_distill *d, const float *grad_lo
  *   a pair (a, b) of n turns by the angle position * frequency:  y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin
  * Pair i = 0..pairs-1 is elements (i, i + pairs), or (2 i, 2 i + 1) with `interleaved`; the elements from 2 * pairs on are not
  * turned.  Its position is that of axis[i] (time, height, width of an image or video, say), its frequency frequency[i] in radians
- * per position.  Angles are taken in 64 bits (off by at most 2^-51 of themselves, so far positions keep their phase), everything
- * else in float with one rounding where a result is stored.
+ * per position.  Angles are taken in turns, in 64 bits modulo whole turns (off by 2^-60 turns per position and turn of frequency, so far
+ * positions keep their phase), everything else in float with one rounding where a result is stored.
  * Backward, dn being the results' gradients turned back and g = w dn:
  *   dx = r (g - x r^2 mean_c(g_c x_c)),  r = (mean_c x_c^2 + eps)^(-1/2);  dw_c = sum over rows and heads of dn_c x_c r
  * lengths: device int32[batch] or NULL: rows from there on are not read (NaN included), their results are 0 and they are in no sum. */

@@ -9,15 +9,15 @@
 #include "context.h"
 #include "vector.cuh"
 
+#include <cmath>
+
 namespace omni {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxPairs = OMNI_ROTARY_MAX_DIM / 2;
-constexpr int kMaxTile = 16;                          // rows whose angles a block holds
 constexpr int kResident = 2;                          // backward blocks an SM
-constexpr double kInvTwoPi = 0.15915494309189533577;
 
 struct View {
     void *data;
@@ -36,10 +36,13 @@ struct RotaryParams {
     unsigned long long position_axis, position_batch, position_row;
     const int *lengths;
     unsigned rows, length;                            // batch * length, length
-    int dim, pairs, lanes, tile;                      // lanes of a head vector (a power of two), rows of a tile (a power of two)
+    unsigned magic, shift;                            // row / length = (mulhi(magic, row) + row) >> shift
+    int dim, pairs, axes;
+    int lanes, split;                                 // lanes of a head vector, groups of lanes that share a row's heads: powers of two
     int wide_positions, bf16_weight, interleaved, overlap;
-    float eps, turn;                                  // turn: 1, or -1 for the opposite angle
-    double frequency[kMaxPairs];
+    int backwards;                                    // the opposite angle
+    float eps;
+    unsigned long long frequency[kMaxPairs];          // turns per position, a fraction of 2^64
     unsigned char axis[kMaxPairs];
 };
 
@@ -53,9 +56,24 @@ template <int UNIT> __device__ __forceinline__ Place place(const RotaryParams &p
     return first < p.pairs ? Place{first, first + p.pairs} : Place{first + p.pairs, first + p.pairs + rest};
 }
 
+// Sums over a group of lanes; spelled out, so that the steps are branches of the whole warp.
 __device__ __forceinline__ float group_sum(float x, int lanes)
 {
-    for (int o = lanes / 2; o > 0; o /= 2) x += __shfl_xor_sync(~0u, x, o);
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        if (o >= lanes) break;
+        x += __shfl_xor_sync(~0u, x, o);
+    }
+    return x;
+}
+__device__ __forceinline__ float2 group_sum(float2 x, int lanes)
+{
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        if (o >= lanes) break;
+        const float a = __shfl_xor_sync(~0u, x.x, o), b = __shfl_xor_sync(~0u, x.y, o);
+        x = make_float2(x.x + a, x.y + b);
+    }
     return x;
 }
 
@@ -65,61 +83,77 @@ struct RowAt {
     bool mine, there;                                 // a row of the call; not behind its sequence's length
     __device__ __forceinline__ RowAt(const RotaryParams &p, unsigned row) : mine(row < p.rows)
     {
-        batch = row / p.length;
+        batch = (__umulhi(p.magic, row) + row) >> p.shift;
         i = row - batch * p.length;
         there = mine && (!p.lengths || int(i) < p.lengths[batch]);
     }
     template <typename T> __device__ __forceinline__ T *in(const View &v) const { return static_cast<T *>(v.data) + batch * v.batch + i * v.row; }
 };
 
-// A table row of cosines, then sines, four floats behind the next so that rows start in different banks.  WIDE: a unit's eight as two
-// pieces of four in two planes, so that neighbouring lanes read neighbouring 16 bytes.
-__host__ __device__ __forceinline__ int table_row(int dim) { return dim + 4; }
-template <bool WIDE> __device__ __forceinline__ int cell(int pair, int half)
+// Cosine and sine of an angle in 2^-32 turns: the quadrant nearest to it, and Taylor's series of the rest, which is within pi / 4
+// (next terms below 2^-29).
+__device__ __forceinline__ void cos_sin(uint32_t angle, float *c, float *s)
 {
-    return WIDE ? (pair & 4 ? half / 2 : 0) + pair / 8 * 4 + pair % 4 : pair;
+    const uint32_t quadrant = (angle + (1u << 29)) >> 30;
+    const float x = float(int(angle - (quadrant << 30))) * 1.4629180792671596e-9f, y = x * x;        // 2 pi / 2^32
+    const float odd = fmaf(fmaf(fmaf(fmaf(y, 1.0f / 362880.0f, -1.0f / 5040.0f), y, 1.0f / 120.0f), y, -1.0f / 6.0f) * y, x, x);
+    const float even = fmaf(fmaf(fmaf(fmaf(fmaf(y, -1.0f / 3628800.0f, 1.0f / 40320.0f), y, -1.0f / 720.0f), y, 1.0f / 24.0f), y, -0.5f), y, 1.0f);
+    const float a = quadrant & 1 ? odd : even, b = quadrant & 1 ? even : odd;
+    *c = (quadrant + 1) & 2 ? -a : a;
+    *s = quadrant & 2 ? -b : b;
 }
 
-// The angles of a tile, each lane for one row of it, so that the lanes of a warp ask for few frequencies.
-template <bool WIDE> __device__ __forceinline__ void fill_angles(const RotaryParams &p, unsigned first, float *table)
-{
-    const int half = p.dim / 2, k = threadIdx.x & (p.tile - 1);
-    const RowAt row(p, first + k);
-    const unsigned long long at = row.batch * p.position_batch + row.i * p.position_row;
-    float *const out = table + k * table_row(p.dim);
-    double position = 0.0;
-    int axis = -1;
-    for (int pair = threadIdx.x / p.tile; pair < half; pair += kThreads / p.tile) {
-        float c = 1.0f, s = 0.0f;
-        if (pair < p.pairs && row.mine) {
-            if (p.axis[pair] != axis) {
-                axis = p.axis[pair];
-                const unsigned long long j = at + axis * p.position_axis;
-                position = double(p.wide_positions ? load_index<long long>(p.positions, j) : load_index<int>(p.positions, j));
-            }
-            // in turns and in 64 bits: what is left of the angle after its whole turns keeps 2^-51 of the angle
-            const double turns = position * (p.frequency[pair] * kInvTwoPi);
-            sincospif(2.0f * float(turns - rint(turns)), &s, &c);
-            s *= p.turn;
+// A block's copy of the pairs' frequencies (0, which gives cosine 1 and sine 0, for those that are not rotated) and axes: asked of the
+// parameters, every lane another, they are slow.
+struct Pairs {
+    unsigned long long frequency[kMaxPairs];
+    unsigned char axis[kMaxPairs];
+    __device__ __forceinline__ void fill(const RotaryParams &p)
+    {
+        for (int i = threadIdx.x; i < kMaxPairs; i += kThreads) {
+            frequency[i] = i < p.pairs ? p.frequency[i] : 0;
+            axis[i] = i < p.pairs ? p.axis[i] : 0;
         }
-        out[cell<WIDE>(pair, half)] = c;
-        out[half + cell<WIDE>(pair, half)] = s;
+    }
+};
+
+__device__ __forceinline__ unsigned long long position_at(const RotaryParams &p, const RowAt &row, int axis)
+{
+    if (!row.mine) return 0;
+    const unsigned long long at = row.batch * p.position_batch + row.i * p.position_row + axis * p.position_axis;
+    const unsigned long long x = p.wide_positions ? load_index<long long>(p.positions, at) : load_index<int>(p.positions, at);
+    return p.backwards ? -x : x;
+}
+
+// N of a row's angles, of the pairs from `first` on, STEP apart; `position` is that of the first one's axis, fetched ahead.  A position
+// times the turns per position, in whole numbers modulo 2^64, is what is left of the angle after its whole turns: however far the
+// position, it is off by 2^-65 turns per position, and by the 2^-32 of the part that is used.
+template <int N> __device__ __forceinline__ void angles(const RotaryParams &p, const Pairs &pairs, const RowAt &row, unsigned long long position,
+                                                        int first, int step, float *c, float *s)
+{
+    int axis = pairs.axis[first];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int pair = first + i * step;
+        if (pair >= kMaxPairs) continue;
+        if (p.axes > 1 && pairs.axis[pair] != axis) position = position_at(p, row, axis = pairs.axis[pair]);
+        cos_sin(uint32_t(position * pairs.frequency[pair] >> 32), c + i, s + i);
     }
 }
 
-// How a block's threads share a tile: `lanes` of a head vector, groups of them that go through the heads of one row.
+// How a block's threads share its rows: `lanes` of a head vector; `split` groups of them have the heads of one row in turn.
 struct Share {
-    int lane, row, first, stride, turns;              // heads first, first + stride, ...; every group of a block takes `turns` turns, for the shuffles
+    int lane, row, first, turns;                      // heads first, first + split, ...; every group takes as many turns, for the shuffles
     __device__ __forceinline__ Share(const RotaryParams &p, int heads)
     {
         const int group = threadIdx.x / p.lanes;
         lane = threadIdx.x % p.lanes;
-        stride = kThreads / p.lanes / p.tile;
-        row = group / stride;
-        first = group % stride;
-        turns = (heads + stride - 1) / stride;
+        row = group / p.split;
+        first = group % p.split;
+        turns = (heads + p.split - 1) / p.split;
     }
 };
+__device__ __forceinline__ unsigned rows_of_block(const RotaryParams &p) { return kThreads / (p.lanes * p.split); }
 
 __device__ __forceinline__ float weight_at(const RotaryParams &p, const Side &side, int c)
 {
@@ -165,6 +199,12 @@ template <typename T, int CHUNKS, int STAGES> struct Ring {
         for (int i = 0; i < kPieces<T>; ++i)
             copy_async(shared + stage * kStage + (chunk * kPieces<T> + i) * kThreads * 16, reinterpret_cast<const char *>(from) + 16 * i);
     }
+    // Zeros in place of what is not there: a turn's sums need no cases then.
+    __device__ __forceinline__ void clear(int stage) const
+    {
+#pragma unroll
+        for (int i = 0; i < CHUNKS * kPieces<T>; ++i) *reinterpret_cast<uint4 *>(base + stage * kStage + i * kThreads * 16) = make_uint4(0, 0, 0, 0);
+    }
     __device__ __forceinline__ void get(int stage, int chunk, float *f) const
     {
         const char *const at = base + stage * kStage + chunk * kPieces<T> * kThreads * 16;
@@ -197,15 +237,6 @@ template <bool ADJACENT> __device__ __forceinline__ void put_pairs(float *f, int
 }
 __device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
 
-// A unit's eight cosines (or sines) as four pairs.
-__device__ __forceinline__ void read_plane(const float *at, int half, int unit, float2 *c)
-{
-    const float4 x = *reinterpret_cast<const float4 *>(at + unit * 4), y = *reinterpret_cast<const float4 *>(at + half / 2 + unit * 4);
-    c[0] = make_float2(x.x, x.y);
-    c[1] = make_float2(x.z, x.w);
-    c[2] = make_float2(y.x, y.y);
-    c[3] = make_float2(y.z, y.w);
-}
 template <bool ADJACENT> __device__ __forceinline__ void read_weights(const RotaryParams &p, const Side &side, Place at, float2 *wa, float2 *wb)
 {
     float f[16];
@@ -221,195 +252,214 @@ template <bool ADJACENT> __device__ __forceinline__ void read_weights(const Rota
 template <typename T> constexpr int kForwardStages = sizeof(T) == 2 ? 6 : 4;
 template <typename T> using ForwardRing = Ring<T, 2, kForwardStages<T>>;
 
-// Forward: a block has a tile of rows of one side.  With weights they are folded into the angles, and a result is
+// Forward: a group of lanes has a row of one side.  With weights they are folded into the angles, and a result is
 // y_a = r ((w_a cos) x_a - (w_b sin) x_b), y_b = r ((w_b cos) x_b + (w_a sin) x_a).
 template <typename T, bool ADJACENT, bool NORM>
 __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
     extern __shared__ __align__(16) char shared[];
+    __shared__ Pairs pairs;
     constexpr int kStages = kForwardStages<T>;
     const ForwardRing<T> ring(shared);
-    float *const table = reinterpret_cast<float *>(shared + ForwardRing<T>::kBytes);
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
-    const unsigned first = (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * unsigned(p.tile);
     const Share me(p, side.heads);
-    const RowAt row(p, first + me.row);
+    const RowAt row(p, (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * rows_of_block(p) + me.row);
     const bool has = me.lane * 16 < p.dim;
-    const Place at = place<8>(p, has ? me.lane : 0);
-    const T *const src = row.in<T>(side.x);
-    T *const dst = row.in<T>(side.out);
-    const auto fetch = [&](int turn, int stage) {
-        const int head = me.first + turn * me.stride;
-        if (head < side.heads && row.there && has) {
-            ring.fetch(stage, 0, src + head * side.x.head + at.a);
-            ring.fetch(stage, 1, src + head * side.x.head + at.b);
+    const int unit = has ? me.lane : 0;
+    const Place at = place<8>(p, unit);
+    const int to_b = at.b - at.a;
+    const T *src = row.in<T>(side.x) + me.first * side.x.head + at.a;
+    T *dst = row.in<T>(side.out) + me.first * side.out.head + at.a;
+    const unsigned long long src_step = p.split * side.x.head, dst_step = p.split * side.out.head;
+    int ahead = row.there && has ? me.first : side.heads;               // the next head to be fetched
+    const auto fetch = [&](int stage) {
+        if (ahead < side.heads) {
+            ring.fetch(stage, 0, src);
+            ring.fetch(stage, 1, src + to_b);
+            src += src_step;
+            ahead += p.split;
+        } else {
+            ring.clear(stage);
         }
         copies_commit();
     };
 #pragma unroll
-    for (int j = 0; j < kStages - 1; ++j) fetch(j, j);
-    fill_angles<true>(p, first, table);
-    float2 ca[4], sa[4], cb[4], sb[4];                // cos and sin, with weights those times w_a and w_b
+    for (int j = 0; j < kStages - 1; ++j) fetch(j);
+    pairs.fill(p);
+    float2 ca[4], sa[4], cb[4], sb[4];                // cos and sin, with weights those times w_a and w_b; sb with its sign
     if constexpr (NORM) read_weights<ADJACENT>(p, side, at, ca, cb);
     __syncthreads();
     {
-        const float *const mine = table + me.row * table_row(p.dim);
-        float2 c[4], s[4];
-        read_plane(mine, p.dim / 2, has ? me.lane : 0, c);
-        read_plane(mine + p.dim / 2, p.dim / 2, has ? me.lane : 0, s);
+        float c[8], s[8];
+        angles<8>(p, pairs, row, position_at(p, row, pairs.axis[unit * 8]), unit * 8, 1, c, s);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            sa[i] = NORM ? mul2(s[i], ca[i]) : s[i];
-            sb[i] = NORM ? mul2(s[i], cb[i]) : s[i];
-            ca[i] = NORM ? mul2(c[i], ca[i]) : c[i];
-            cb[i] = NORM ? mul2(c[i], cb[i]) : c[i];
+            const float2 ci = make_float2(c[2 * i], c[2 * i + 1]), si = make_float2(s[2 * i], s[2 * i + 1]);
+            sa[i] = NORM ? mul2(si, ca[i]) : si;
+            sb[i] = minus(NORM ? mul2(si, cb[i]) : si);
+            ca[i] = NORM ? mul2(ci, ca[i]) : ci;
+            cb[i] = NORM ? mul2(ci, cb[i]) : ci;
         }
     }
     const float inverse_dim = 1.0f / float(p.dim);
-    int stage = 0;
-    for (int j = 0; j < me.turns; ++j) {
+    int stage = 0, head = row.mine && has ? me.first : side.heads;
+    for (int j = 0; j < me.turns; ++j, head += p.split, dst += dst_step) {
         copies_wait<kStages - 2>();
-        const int head = me.first + j * me.stride;
-        const bool work = head < side.heads && row.mine && has, live = work && row.there;
         float f[16];
-        if (live) {
-            ring.get(stage, 0, f);
-            ring.get(stage, 1, f + 8);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) f[e] = 0.0f;
-        }
+        ring.get(stage, 0, f);
+        ring.get(stage, 1, f + 8);
         // into the slot that the turn before this one has used up
-        fetch(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        fetch(stage == 0 ? kStages - 1 : stage - 1);
         stage = stage == kStages - 1 ? 0 : stage + 1;
         float2 r = {1.0f, 1.0f};
         if constexpr (NORM) {
             float2 sum = {0.0f, 0.0f};
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fma2(make_float2(f[2 * e], f[2 * e + 1]), make_float2(f[2 * e], f[2 * e + 1]), sum);
-            r.x = r.y = rsqrtf(fmaf(group_sum(sum.x + sum.y, p.lanes), inverse_dim, p.eps));
+            r.x = r.y = row.there ? rsqrtf(fmaf(group_sum(sum.x + sum.y, p.lanes), inverse_dim, p.eps)) : 0.0f;
         }
-        if (!work) continue;
-        if (live) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-                float2 ya = fma2(a, ca[i], minus(mul2(b, sb[i]))), yb = fma2(b, cb[i], mul2(a, sa[i]));
-                if constexpr (NORM) {
-                    ya = mul2(ya, r);
-                    yb = mul2(yb, r);
-                }
-                put_pairs<ADJACENT>(f, i, ya, yb);
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+            float2 ya = fma2(a, ca[i], mul2(b, sb[i])), yb = fma2(b, cb[i], mul2(a, sa[i]));
+            if constexpr (NORM) {
+                ya = mul2(ya, r);
+                yb = mul2(yb, r);
             }
+            put_pairs<ADJACENT>(f, i, ya, yb);
         }
-        store_group(dst + head * side.out.head + at.a, f);
-        store_group(dst + head * side.out.head + at.b, f + 8);
+        if (head < side.heads) {
+            store_group(dst, f);
+            store_group(dst + to_b, f + 8);
+        }
     }
 }
 
 template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 3;
 template <typename T> using BackwardRing = Ring<T, 4, kBackwardStages<T>>;
 
-// Backward of the norm and the rotation: blocks that stay, each on tiles of one side, with the weight's gradient in registers.
+// Backward of the norm and the rotation: blocks that stay, each on rows of one side, with the weight's gradient in registers.
 template <typename T, bool ADJACENT>
 __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
     extern __shared__ __align__(16) char shared[];
+    __shared__ Pairs pairs;
     constexpr int kStages = kBackwardStages<T>;
     const BackwardRing<T> ring(shared);
-    float *const table = reinterpret_cast<float *>(shared + BackwardRing<T>::kBytes);
     let_next_begin(p.overlap);
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
     const unsigned block = blockIdx.x - (keys ? p.side[0].blocks : 0u);
     const Share me(p, side.heads);
     const bool has = me.lane * 16 < p.dim;
-    const Place at = place<8>(p, has ? me.lane : 0);
+    const int unit = has ? me.lane : 0;
+    const Place at = place<8>(p, unit);
+    const int to_b = at.b - at.a;
+    const float inverse_dim = 1.0f / float(p.dim);
+    const unsigned first_row = block * rows_of_block(p), row_step = side.blocks * rows_of_block(p);
+    const unsigned long long x_step = p.split * side.x.head, y_step = p.split * side.dy.head, dst_step = p.split * side.out.head;
+    // what is fetched next: the loads run through all turns of all rows of the group, ahead of the sums
+    unsigned ahead_row = first_row + me.row;
+    int ahead = 0, ahead_heads = 0;                   // turn, heads if the row is there
+    const T *src = nullptr, *grad = nullptr;
+    const auto fetch = [&](int stage) {
+        if (ahead == 0) {
+            const RowAt row(p, ahead_row);
+            ahead_heads = row.there && has ? side.heads - me.first : 0;
+            src = row.in<T>(side.x) + me.first * side.x.head + at.a;
+            grad = row.in<T>(side.dy) + me.first * side.dy.head + at.a;
+        }
+        if (ahead * p.split < ahead_heads) {
+            ring.fetch(stage, 0, src);
+            ring.fetch(stage, 1, src + to_b);
+            ring.fetch(stage, 2, grad);
+            ring.fetch(stage, 3, grad + to_b);
+            src += x_step;
+            grad += y_step;
+        } else {
+            ring.clear(stage);
+        }
+        copies_commit();
+        if (++ahead == me.turns) {
+            ahead = 0;
+            ahead_row = ahead_row < p.rows ? ahead_row + row_step : ahead_row;       // stays behind the last row
+        }
+    };
+#pragma unroll
+    for (int j = 0; j < kStages - 1; ++j) fetch(j);
+    pairs.fill(p);
     float2 wa[4], wb[4], da[4] = {}, db[4] = {};
     read_weights<ADJACENT>(p, side, at, wa, wb);
-    const float inverse_dim = 1.0f / float(p.dim);
-    const unsigned tiles = (p.rows + p.tile - 1) / p.tile;
-    for (unsigned t = block; t < tiles; t += side.blocks) {
-        const unsigned first = t * unsigned(p.tile);
-        const RowAt row(p, first + me.row);
-        const T *const src = row.in<T>(side.x), *const grad = row.in<T>(side.dy);
-        T *const dst = row.in<T>(side.out);
-        const auto fetch = [&](int turn, int stage) {
-            const int head = me.first + turn * me.stride;
-            if (head < side.heads && row.there && has) {
-                ring.fetch(stage, 0, src + head * side.x.head + at.a);
-                ring.fetch(stage, 1, src + head * side.x.head + at.b);
-                ring.fetch(stage, 2, grad + head * side.dy.head + at.a);
-                ring.fetch(stage, 3, grad + head * side.dy.head + at.b);
-            }
-            copies_commit();
-        };
-#pragma unroll
-        for (int j = 0; j < kStages - 1; ++j) fetch(j, j);
-        __syncthreads();                              // the last tile's angles have been read
-        fill_angles<true>(p, first, table);
-        __syncthreads();
+    __syncthreads();
+    unsigned long long position = position_at(p, RowAt(p, first_row + me.row), pairs.axis[unit * 8]);
+    int stage = 0;
+    // a warp's groups have neighbouring rows and go on as long as one of them is there
+    for (unsigned n = first_row + me.row; n - me.row + (threadIdx.x & ~31u) / (p.lanes * p.split) < p.rows; n += row_step) {
+        const RowAt row(p, n);
+        T *dst = row.in<T>(side.out) + me.first * side.out.head + at.a;
         float2 c[4], s[4];
-        const float *const mine = table + me.row * table_row(p.dim);
-        read_plane(mine, p.dim / 2, has ? me.lane : 0, c);
-        read_plane(mine + p.dim / 2, p.dim / 2, has ? me.lane : 0, s);
-        int stage = 0;
-        for (int j = 0; j < me.turns; ++j) {
-            copies_wait<kStages - 2>();
-            const int head = me.first + j * me.stride;
-            const bool work = head < side.heads && row.mine && has, live = work && row.there;
-            float f[16], g[16];
-            if (live) {
-                ring.get(stage, 0, f);
-                ring.get(stage, 1, f + 8);
-                ring.get(stage, 2, g);
-                ring.get(stage, 3, g + 8);
-            } else {
+        {
+            float cs[8], sn[8];
+            angles<8>(p, pairs, row, position, unit * 8, 1, cs, sn);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) f[e] = g[e] = 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                c[i] = make_float2(cs[2 * i], cs[2 * i + 1]);
+                s[i] = make_float2(sn[2 * i], sn[2 * i + 1]);
             }
-            fetch(j + kStages - 1, stage == 0 ? kStages - 1 : stage - 1);
+        }
+        if (n < p.rows && p.rows - n > row_step) position = position_at(p, RowAt(p, n + row_step), pairs.axis[unit * 8]);
+        int head = row.mine && has ? me.first : side.heads;
+        for (int j = 0; j < me.turns; ++j, head += p.split, dst += dst_step) {
+            copies_wait<kStages - 2>();
+            float f[16], g[16];
+            ring.get(stage, 0, f);
+            ring.get(stage, 1, f + 8);
+            ring.get(stage, 2, g);
+            ring.get(stage, 3, g + 8);
+            // into the slot that the turn before this one has used up
+            fetch(stage == 0 ? kStages - 1 : stage - 1);
             stage = stage == kStages - 1 ? 0 : stage + 1;
             float2 square = {0.0f, 0.0f}, dot = {0.0f, 0.0f};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
                 const float2 ya = firsts<ADJACENT>(g, i), yb = seconds<ADJACENT>(g, i);
-                const float2 na = fma2(ya, c[i], mul2(yb, s[i])), nb = fma2(yb, c[i], minus(mul2(ya, s[i])));
+                const float2 na = fma2(ya, c[i], mul2(yb, s[i])), nb = fma2(yb, c[i], mul2(ya, minus(s[i])));
                 square = fma2(b, b, fma2(a, a, square));
                 dot = fma2(mul2(b, wb[i]), nb, fma2(mul2(a, wa[i]), na, dot));
                 put_pairs<ADJACENT>(g, i, na, nb);
             }
-            const float squares = group_sum(square.x + square.y, p.lanes), dots = group_sum(dot.x + dot.y, p.lanes);
-            if (!work) continue;
-            if (live) {
-                const float scale = rsqrtf(fmaf(squares, inverse_dim, p.eps)), pull = -dots * inverse_dim * scale * scale;
-                const float2 r = {scale, scale}, q = {pull, pull};
+            const float2 sums = group_sum(make_float2(square.x + square.y, dot.x + dot.y), p.lanes);
+            const float scale = row.there && head < side.heads ? rsqrtf(fmaf(sums.x, inverse_dim, p.eps)) : 0.0f, pull = -sums.y * inverse_dim * scale * scale;
+            const float2 r = {scale, scale}, q = {pull, pull};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-                    const float2 na = firsts<ADJACENT>(g, i), nb = seconds<ADJACENT>(g, i);
-                    da[i] = fma2(na, mul2(a, r), da[i]);
-                    db[i] = fma2(nb, mul2(b, r), db[i]);
-                    put_pairs<ADJACENT>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
-                }
+            for (int i = 0; i < 4; ++i) {
+                const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+                const float2 na = firsts<ADJACENT>(g, i), nb = seconds<ADJACENT>(g, i);
+                da[i] = fma2(na, mul2(a, r), da[i]);
+                db[i] = fma2(nb, mul2(b, r), db[i]);
+                put_pairs<ADJACENT>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
             }
-            store_group(dst + head * side.out.head + at.a, f);
-            store_group(dst + head * side.out.head + at.b, f + 8);
+            if (head < side.heads) {
+                store_group(dst, f);
+                store_group(dst + to_b, f + 8);
+            }
         }
     }
+    copies_wait<0>();
     __syncthreads();
+    float *const sums = reinterpret_cast<float *>(shared);
     float dw[16];
 #pragma unroll
     for (int i = 0; i < 4; ++i) put_pairs<ADJACENT>(dw, i, da[i], db[i]);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const float v = warp_groups_sum(dw[e], p.lanes);
-        if (int(threadIdx.x % 32) < p.lanes && has) table[threadIdx.x / 32 * p.dim + (e < 8 ? at.a + e : at.b + e - 8)] = v;
+        if (int(threadIdx.x % 32) < p.lanes && has) sums[threadIdx.x / 32 * p.dim + (e < 8 ? at.a + e : at.b + e - 8)] = v;
     }
     __syncthreads();
-    put_partial(p, table, side.partial + (unsigned long long)block * p.dim);
+    put_partial(p, sums, side.partial + (unsigned long long)block * p.dim);
 }
 
 // ---- any alignment: element by element, up to four pairs a lane in registers ------------------------------------------------------
@@ -435,14 +485,12 @@ struct Own {
 template <typename T, bool NORM>
 __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
 {
-    extern __shared__ __align__(16) char shared[];
-    float *const table = reinterpret_cast<float *>(shared);
+    __shared__ Pairs pairs;
     constexpr int kAhead = 4;                         // heads in flight
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
-    const unsigned first = (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * unsigned(p.tile);
     const Share me(p, side.heads);
-    const RowAt row(p, first + me.row);
+    const RowAt row(p, (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * rows_of_block(p) + me.row);
     const Own own(p, side, me.lane, NORM);
     const T *const src = row.in<T>(side.x);
     T *const dst = row.in<T>(side.out);
@@ -452,7 +500,7 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
         T x[kAhead][kOwn][2];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int head = me.first + (j0 + i) * me.stride;
+            const int head = me.first + (j0 + i) * p.split;
 #pragma unroll
             for (int n = 0; n < kOwn; ++n)
                 if (row.there && head < side.heads && own.has[n]) {
@@ -461,18 +509,13 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
                 }
         }
         if (j0 == 0) {                                // the first loads are under way
-            fill_angles<false>(p, first, table);
+            pairs.fill(p);
             __syncthreads();
-#pragma unroll
-            for (int n = 0; n < kOwn; ++n)
-                if (own.has[n]) {
-                    c[n] = table[me.row * table_row(p.dim) + me.lane + n * p.lanes];
-                    s[n] = table[me.row * table_row(p.dim) + p.dim / 2 + me.lane + n * p.lanes];
-                }
+            angles<kOwn>(p, pairs, row, position_at(p, row, pairs.axis[me.lane]), me.lane, p.lanes, c, s);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int head = me.first + (j0 + i) * me.stride;
+            const int head = me.first + (j0 + i) * p.split;
             const bool work = row.mine && head < side.heads;
             float f[kOwn][2], sum = 0.0f, r = 1.0f;
 #pragma unroll
@@ -484,11 +527,11 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
                 }
             if constexpr (NORM) r = rsqrtf(fmaf(group_sum(sum, p.lanes), inverse_dim, p.eps));
             if (!work) continue;
+            T *const at = dst + head * side.out.head;
 #pragma unroll
             for (int n = 0; n < kOwn; ++n) {
                 if (!own.has[n]) continue;
                 const float a = NORM ? f[n][0] * r * own.w[n][0] : f[n][0], b = NORM ? f[n][1] * r * own.w[n][1] : f[n][1];
-                T *const at = dst + head * side.out.head;
                 at[own.at[n].a] = from_float<T>(row.there ? fmaf(a, c[n], -b * s[n]) : 0.0f);
                 at[own.at[n].b] = from_float<T>(row.there ? fmaf(b, c[n], a * s[n]) : 0.0f);
             }
@@ -498,8 +541,8 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
 
 template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
 {
-    extern __shared__ __align__(16) char shared[];
-    float *const table = reinterpret_cast<float *>(shared);
+    __shared__ Pairs pairs;
+    __shared__ float sums[kWarps * OMNI_ROTARY_MAX_DIM];
     constexpr int kAhead = 2;
     let_next_begin(p.overlap);
     const bool keys = blockIdx.x >= p.side[0].blocks;
@@ -508,11 +551,12 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
     const Share me(p, side.heads);
     const Own own(p, side, me.lane, true);
     const float inverse_dim = 1.0f / float(p.dim);
+    const unsigned first_row = block * rows_of_block(p), row_step = side.blocks * rows_of_block(p);
+    pairs.fill(p);
+    __syncthreads();
     float dw[kOwn][2] = {};
-    const unsigned tiles = (p.rows + p.tile - 1) / p.tile;
-    for (unsigned t = block; t < tiles; t += side.blocks) {
-        const unsigned first = t * unsigned(p.tile);
-        const RowAt row(p, first + me.row);
+    for (unsigned n0 = first_row + me.row; n0 - me.row + (threadIdx.x & ~31u) / (p.lanes * p.split) < p.rows; n0 += row_step) {
+        const RowAt row(p, n0);
         const T *const src = row.in<T>(side.x), *const grad = row.in<T>(side.dy);
         T *const dst = row.in<T>(side.out);
         float c[kOwn], s[kOwn];
@@ -520,7 +564,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
             T x[kAhead][kOwn][2], y[kAhead][kOwn][2];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int head = me.first + (j0 + i) * me.stride;
+                const int head = me.first + (j0 + i) * p.split;
 #pragma unroll
                 for (int n = 0; n < kOwn; ++n)
                     if (row.there && head < side.heads && own.has[n]) {
@@ -530,20 +574,10 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
                         y[i][n][1] = grad[head * side.dy.head + own.at[n].b];
                     }
             }
-            if (j0 == 0) {
-                __syncthreads();                      // the last tile's angles have been read
-                fill_angles<false>(p, first, table);
-                __syncthreads();
-#pragma unroll
-                for (int n = 0; n < kOwn; ++n)
-                    if (own.has[n]) {
-                        c[n] = table[me.row * table_row(p.dim) + me.lane + n * p.lanes];
-                        s[n] = table[me.row * table_row(p.dim) + p.dim / 2 + me.lane + n * p.lanes];
-                    }
-            }
+            if (j0 == 0) angles<kOwn>(p, pairs, row, position_at(p, row, pairs.axis[me.lane]), me.lane, p.lanes, c, s);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int head = me.first + (j0 + i) * me.stride;
+                const int head = me.first + (j0 + i) * p.split;
                 const bool work = row.mine && head < side.heads, live = work && row.there;
                 float f[kOwn][2], g[kOwn][2], square = 0.0f, dot = 0.0f;
 #pragma unroll
@@ -562,10 +596,9 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
                         dot = fmaf(f[n][e] * own.w[n][e], g[n][e], dot);
                     }
                 }
-                square = group_sum(square, p.lanes);
-                dot = group_sum(dot, p.lanes);
+                const float2 both = group_sum(make_float2(square, dot), p.lanes);
                 if (!work) continue;
-                const float r = rsqrtf(fmaf(square, inverse_dim, p.eps)), pull = dot * inverse_dim * r * r;
+                const float r = rsqrtf(fmaf(both.x, inverse_dim, p.eps)), pull = both.y * inverse_dim * r * r;
                 T *const at = dst + head * side.out.head;
 #pragma unroll
                 for (int n = 0; n < kOwn; ++n) {
@@ -583,16 +616,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
             }
         }
     }
-    __syncthreads();
 #pragma unroll
     for (int n = 0; n < kOwn; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float v = warp_groups_sum(dw[n][e], p.lanes);
-            if (int(threadIdx.x % 32) < p.lanes && own.has[n]) table[threadIdx.x / 32 * p.dim + (e ? own.at[n].b : own.at[n].a)] = v;
+            if (int(threadIdx.x % 32) < p.lanes && own.has[n]) sums[threadIdx.x / 32 * p.dim + (e ? own.at[n].b : own.at[n].a)] = v;
         }
     __syncthreads();
-    put_partial(p, table, side.partial + (unsigned long long)block * p.dim);
+    put_partial(p, sums, side.partial + (unsigned long long)block * p.dim);
 }
 
 struct WeightParams {
@@ -675,32 +707,31 @@ bool wide_view(const omni_rotary *r, const View &v)
     return aligned(v.data, 16) && v.batch * size % 16 == 0 && v.row * size % 16 == 0 && v.head * size % 16 == 0;
 }
 
-// The launch: rows of a tile, lanes of a head vector, blocks of either side.
+// The launch: lanes of a head vector, groups that share a row's heads, blocks of either side.
 struct Shape {
-    int lanes, tile;
+    int lanes, split;
     unsigned blocks[2];
 };
 
-// A row's heads are dealt to a power of two of lane groups, so that a group has about `deep` heads of one row and its angles stay
-// in registers; a tile is the rows that fill a block then.  Few rows: one a block, its heads on all groups.
-Shape shape_of(const omni_rotary *r, bool wide, int deep, int sms, int resident)
+// A group has all heads of a row, so that every angle is made once; where there are few rows (decoding) groups share a row and make its angles each.
+Shape shape_of(const omni_rotary *r, bool wide, int sms, int resident)
 {
     Shape s;
     const int units = wide ? r->dim / 16 : r->dim / 2;
     s.lanes = 1;
     while (s.lanes < units && s.lanes < 32) s.lanes *= 2;
     const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length);
-    const int groups = kThreads / s.lanes, fewest = r->heads < r->kv_heads ? r->heads : r->kv_heads;
-    s.tile = 1;
-    while (s.tile < groups && s.tile < kMaxTile && groups / s.tile * deep > fewest && rows >= uint64_t(s.tile) * 2 * sms) s.tile *= 2;
-    const uint64_t tiles = (rows + s.tile - 1) / s.tile;
-    s.blocks[0] = s.blocks[1] = unsigned(tiles);
-    if (resident) {                                   // blocks that stay: shares by the work of a row, angles included
+    const int groups = kThreads / s.lanes, most = r->heads > r->kv_heads ? r->heads : r->kv_heads;
+    s.split = 1;
+    while (s.split < groups && s.split < most && rows * s.split < uint64_t(sms) * groups * 2) s.split *= 2;
+    const uint64_t of_block = groups / s.split, blocks = (rows + of_block - 1) / of_block;
+    s.blocks[0] = s.blocks[1] = unsigned(blocks);
+    if (resident) {                                   // blocks that stay: shares by the work of a row, its angles about that of two heads
         const uint64_t all = uint64_t(sms) * resident, q = r->heads + 2, k = r->kv_heads + 2;
         uint64_t share = all * q / (q + k);
         share = share < 1 ? 1 : share > all - 1 ? all - 1 : share;
-        s.blocks[0] = unsigned(tiles < share ? tiles : share);
-        s.blocks[1] = unsigned(tiles < all - share ? tiles : all - share);
+        s.blocks[0] = unsigned(blocks < share ? blocks : share);
+        s.blocks[1] = unsigned(blocks < all - share ? blocks : all - share);
     }
     return s;
 }
@@ -714,17 +745,23 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
     p->lengths = r->lengths;
     p->rows = unsigned(r->batch) * unsigned(r->length);
     p->length = unsigned(r->length);
+    // division of what is below 2^31 by a number of up to 31 bits: ceil(2^(32 + shift) / length) - 2^32
+    for (p->shift = 0; (1ull << p->shift) < p->length; ++p->shift) {}
+    p->magic = unsigned(((1ull << 32) * ((1ull << p->shift) - p->length)) / p->length + 1);
     p->dim = r->dim;
     p->pairs = r->pairs;
+    p->axes = r->axes;
     p->lanes = s.lanes;
-    p->tile = s.tile;
+    p->split = s.split;
     p->wide_positions = r->position_type == OMNI_I64;
     p->bf16_weight = r->weight_dtype == OMNI_BF16;
     p->interleaved = r->interleaved != 0;
     p->eps = r->eps;
-    p->turn = backwards ? -1.0f : 1.0f;
+    p->backwards = backwards;
     for (int i = 0; i < r->pairs; ++i) {
-        p->frequency[i] = r->frequency[i];
+        const long double turns = (long double)r->frequency[i] * 0.159154943091895335768883763372514362L;     // 1 / (2 pi)
+        const long double part = turns - floorl(turns);
+        p->frequency[i] = part < 1.0L ? (unsigned long long)ldexpl(part, 64) : 0;
         p->axis[i] = r->axis ? (unsigned char)r->axis[i] : 0;
     }
     p->side[0].heads = r->heads;
@@ -737,17 +774,11 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
 // Whole units of eight pairs: rotated and unrotated halves of multiples of eight, or any pairs that stand next to one another.
 bool wide_units(const omni_rotary *r) { return r->dim % 16 == 0 && (r->interleaved || r->pairs % 8 == 0); }
 
-constexpr int kMostShared = 113 * 1024;               // dynamic shared memory of a block: two fit an SM
-
-size_t table_bytes(const RotaryParams &p, bool sums)
-{
-    const size_t angles = size_t(p.tile) * table_row(p.dim), partial = sums ? size_t(kWarps) * p.dim : 0;
-    return (angles > partial ? angles : partial) * sizeof(float);
-}
+constexpr int kMostShared = 112 * 1024;               // dynamic shared memory of a block: two fit an SM
 
 int enqueue(omni_ctx *ctx, void (*kernel)(RotaryParams), const RotaryParams &p, size_t smem, cudaStream_t s)
 {
-    const int rc = smem > 48 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMostShared) : OMNI_OK;
+    const int rc = smem > 32 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMostShared) : OMNI_OK;
     if (rc != OMNI_OK) return rc;
     kernel<<<p.side[0].blocks + p.side[1].blocks, kThreads, smem, s>>>(p);
     return context_launched(ctx, int(cudaGetLastError()));
@@ -756,16 +787,16 @@ int enqueue(omni_ctx *ctx, void (*kernel)(RotaryParams), const RotaryParams &p, 
 template <typename T, bool NORM>
 int enqueue_forward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
-    if (!wide) return enqueue(ctx, rotary_forward_kernel<T, NORM>, p, table_bytes(p, false), s);
+    if (!wide) return enqueue(ctx, rotary_forward_kernel<T, NORM>, p, 0, s);
     return enqueue(ctx, p.interleaved ? rotary_forward_wide_kernel<T, true, NORM> : rotary_forward_wide_kernel<T, false, NORM>, p,
-                   ForwardRing<T>::kBytes + table_bytes(p, false), s);
+                   ForwardRing<T>::kBytes, s);
 }
 
 template <typename T> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
-    if (!wide) return enqueue(ctx, rotary_backward_kernel<T>, p, table_bytes(p, true), s);
+    if (!wide) return enqueue(ctx, rotary_backward_kernel<T>, p, 0, s);
     return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, true> : rotary_backward_wide_kernel<T, false>, p,
-                   BackwardRing<T>::kBytes + table_bytes(p, true), s);
+                   BackwardRing<T>::kBytes, s);
 }
 
 // One pass over both sides without sums: the forward call, and the gradient where there are no weights.
@@ -779,7 +810,7 @@ int rotate(omni_ctx *ctx, const omni_rotary *r, const omni_attn_view *const (&in
         p.side[i] = {view_of(r, in[i], heads), {}, view_of(r, out[i], heads), nullptr, nullptr, 0, 0};
         wide = wide && wide_view(r, p.side[i].x) && wide_view(r, p.side[i].out);
     }
-    fill(&p, r, shape_of(r, wide, r->dtype == OMNI_BF16 ? 4 : 2, dev.sm_count, 0), backwards);
+    fill(&p, r, shape_of(r, wide, dev.sm_count, 0), backwards);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool norm = r->q_weight && !backwards;
     if (r->dtype == OMNI_BF16)
@@ -873,7 +904,7 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
             p.side[i] = {view_of(r, x[i], heads), view_of(r, dy[i], heads), view_of(r, dx[i], heads), nullptr, nullptr, 0, 0};
             wide = wide && wide_view(r, p.side[i].x) && wide_view(r, p.side[i].dy) && wide_view(r, p.side[i].out);
         }
-        const Shape shape = shape_of(r, wide, 2, dev.sm_count < kMostSms ? dev.sm_count : kMostSms, kResident);
+        const Shape shape = shape_of(r, wide, dev.sm_count < kMostSms ? dev.sm_count : kMostSms, kResident);
         fill(&p, r, shape, false);
         p.overlap = dev.overlap;
         p.side[0].partial = static_cast<float *>(workspace);
