@@ -10,6 +10,7 @@
 #include "vector.cuh"
 
 #include <cmath>
+#include <numeric>
 
 namespace omni {
 namespace {
@@ -38,7 +39,8 @@ struct RotaryParams {
     unsigned rows, length;                            // batch * length, length
     unsigned magic, shift;                            // row / length = (mulhi(magic, row) + row) >> shift
     int dim, pairs, axes;
-    int lanes, split;                                 // lanes of a head vector, groups of lanes that share a row's heads: powers of two
+    int lanes, split;                                 // lanes of a head vector, groups of lanes that share a row's heads (forward): powers of two
+    unsigned bundles, step;                           // backward: rows in bundles of 32 / lanes; bundle number u of the walk is u * step modulo bundles
     int wide_positions, bf16_weight, interleaved, overlap;
     int backwards;                                    // the opposite angle
     float eps;
@@ -125,23 +127,28 @@ __device__ __forceinline__ unsigned long long position_at(const RotaryParams &p,
     return p.backwards ? -x : x;
 }
 
-// N of a row's angles, of the pairs from `first` on, STEP apart; `position` is that of the first one's axis, fetched ahead.  A position
-// times the turns per position, in whole numbers modulo 2^64, is what is left of the angle after its whole turns: however far the
-// position, it is off by 2^-65 turns per position, and by the 2^-32 of the part that is used.
-template <int N> __device__ __forceinline__ void angles(const RotaryParams &p, const Pairs &pairs, const RowAt &row, unsigned long long position,
-                                                        int first, int step, float *c, float *s)
-{
-    int axis = pairs.axis[first];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int pair = first + i * step;
-        if (pair >= kMaxPairs) continue;
+// A row's angles, pair by pair; `position` is that of `axis`, fetched ahead.  A position times the turns per position, in whole numbers
+// modulo 2^64, is what is left of the angle after its whole turns: however far the position, it is off by
+// 2^-65 turns per position, and by the 2^-32 of the part that is used.
+struct Angles {
+    const RotaryParams &p;
+    const Pairs &pairs;
+    const RowAt &row;
+    unsigned long long position;
+    int axis;
+    __device__ __forceinline__ void at(int pair, float *c, float *s)
+    {
         if (p.axes > 1 && pairs.axis[pair] != axis) position = position_at(p, row, axis = pairs.axis[pair]);
-        cos_sin(uint32_t(position * pairs.frequency[pair] >> 32), c + i, s + i);
+        cos_sin(uint32_t(position * pairs.frequency[pair] >> 32), c, s);
     }
-}
+    __device__ __forceinline__ void two(int pair, float2 *c, float2 *s)
+    {
+        at(pair, &c->x, &s->x);
+        at(pair + 1, &c->y, &s->y);
+    }
+};
 
-// How a block's threads share its rows: `lanes` of a head vector; `split` groups of them have the heads of one row in turn.
+// Forward: how a block's threads share its rows: `lanes` of a head vector; `split` groups of them have the heads of one row in turn.
 struct Share {
     int lane, row, first, turns;                      // heads first, first + split, ...; every group takes as many turns, for the shuffles
     __device__ __forceinline__ Share(const RotaryParams &p, int heads)
@@ -154,6 +161,59 @@ struct Share {
     }
 };
 __device__ __forceinline__ unsigned rows_of_block(const RotaryParams &p) { return kThreads / (p.lanes * p.split); }
+
+// Backward: a warp's share of a side: a group of lanes has a row, the warp's groups a bundle of rows, and a turn is one head of each.  The turns of all
+// bundles are dealt to the side's warps in equal parts, wherever in a bundle they begin; the bundles are walked by large
+// steps, so that sequences of different lengths are spread over all warps.
+struct Walk {
+    unsigned number, bundle;                          // of the walk, of the rows
+    int head, left;                                   // turns that are left
+    __device__ __forceinline__ Walk(const RotaryParams &p, unsigned block, unsigned blocks, int heads)
+    {
+        const unsigned long long all = (unsigned long long)p.bundles * heads, warps = (unsigned long long)blocks * kWarps;
+        const unsigned long long me = (unsigned long long)block * kWarps + threadIdx.x / 32;
+        const unsigned long long first = all * me / warps;
+        left = int(all * (me + 1) / warps - first);
+        number = unsigned(first / heads);
+        head = int(first - (unsigned long long)number * heads);
+        bundle = unsigned((unsigned long long)number * p.step % p.bundles);
+    }
+    __device__ __forceinline__ unsigned following(const RotaryParams &p) const
+    {
+        return bundle >= p.bundles - p.step ? bundle - (p.bundles - p.step) : bundle + p.step;
+    }
+    // the group's row
+    __device__ __forceinline__ unsigned row(const RotaryParams &p) const { return bundle * unsigned(32 / p.lanes) + threadIdx.x % 32 / p.lanes; }
+    __device__ __forceinline__ unsigned next_row(const RotaryParams &p) const
+    {
+        return number + 1 < p.bundles ? following(p) * unsigned(32 / p.lanes) + threadIdx.x % 32 / p.lanes : 0x7fffffffu;    // behind all rows
+    }
+    __device__ __forceinline__ void next(const RotaryParams &p, int heads, int by = 1)
+    {
+        left -= by;
+        head += by;
+        if (head == heads) {
+            head = 0;
+            ++number;
+            bundle = following(p);
+        }
+    }
+};
+
+// Over the bundles that lie behind their sequences' lengths altogether: f(the group's row, turns) for each.  Whether there were any.
+template <typename F> __device__ __forceinline__ bool skip_absent(const RotaryParams &p, int heads, Walk &walk, F f)
+{
+    bool any = false;
+    while (p.lengths && walk.left > 0) {
+        const RowAt row(p, walk.row(p));
+        if (__any_sync(~0u, row.there)) break;
+        const int turns = min(walk.left, heads - walk.head);
+        f(row, turns);
+        walk.next(p, heads, turns);
+        any = true;
+    }
+    return any;
+}
 
 __device__ __forceinline__ float weight_at(const RotaryParams &p, const Side &side, int c)
 {
@@ -237,17 +297,19 @@ template <bool ADJACENT> __device__ __forceinline__ void put_pairs(float *f, int
 }
 __device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
 
-template <bool ADJACENT> __device__ __forceinline__ void read_weights(const RotaryParams &p, const Side &side, Place at, float2 *wa, float2 *wb)
-{
-    float f[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) f[e] = weight_at(p, side, e < 8 ? at.a + e : at.b + e - 8);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        wa[i] = firsts<ADJACENT>(f, i);
-        wb[i] = seconds<ADJACENT>(f, i);
+// The side's weights in shared memory, those of the pairs' first elements, then of the second.
+struct Weights {
+    float first[kMaxPairs], second[kMaxPairs];
+    __device__ __forceinline__ void fill(const RotaryParams &p, const Side &side)
+    {
+        for (int i = threadIdx.x; i < p.dim / 2; i += kThreads) {
+            const Place at = place<1>(p, i);
+            first[i] = weight_at(p, side, at.a);
+            second[i] = weight_at(p, side, at.b);
+        }
     }
-}
+};
+__device__ __forceinline__ float2 two(const float *f, int i) { return *reinterpret_cast<const float2 *>(f + i); }
 
 template <typename T> constexpr int kForwardStages = sizeof(T) == 2 ? 6 : 4;
 template <typename T> using ForwardRing = Ring<T, 2, kForwardStages<T>>;
@@ -259,6 +321,7 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const 
 {
     extern __shared__ __align__(16) char shared[];
     __shared__ Pairs pairs;
+    __shared__ __align__(16) Weights weights;
     constexpr int kStages = kForwardStages<T>;
     const ForwardRing<T> ring(shared);
     const bool keys = blockIdx.x >= p.side[0].blocks;
@@ -287,20 +350,19 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const 
 #pragma unroll
     for (int j = 0; j < kStages - 1; ++j) fetch(j);
     pairs.fill(p);
-    float2 ca[4], sa[4], cb[4], sb[4];                // cos and sin, with weights those times w_a and w_b; sb with its sign
-    if constexpr (NORM) read_weights<ADJACENT>(p, side, at, ca, cb);
+    if constexpr (NORM) weights.fill(p, side);
     __syncthreads();
-    {
-        float c[8], s[8];
-        angles<8>(p, pairs, row, position_at(p, row, pairs.axis[unit * 8]), unit * 8, 1, c, s);
+    float2 ca[4], sa[4], cb[4], sb[4];                // cos and sin, with weights those times w_a and w_b; sb with its sign
+    Angles angles{p, pairs, row, position_at(p, row, pairs.axis[unit * 8]), pairs.axis[unit * 8]};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 ci = make_float2(c[2 * i], c[2 * i + 1]), si = make_float2(s[2 * i], s[2 * i + 1]);
-            sa[i] = NORM ? mul2(si, ca[i]) : si;
-            sb[i] = minus(NORM ? mul2(si, cb[i]) : si);
-            ca[i] = NORM ? mul2(ci, ca[i]) : ci;
-            cb[i] = NORM ? mul2(ci, cb[i]) : ci;
-        }
+    for (int i = 0; i < 4; ++i) {
+        float2 c, s;
+        angles.two(unit * 8 + 2 * i, &c, &s);
+        const float2 wa = NORM ? two(weights.first, unit * 8 + 2 * i) : c, wb = NORM ? two(weights.second, unit * 8 + 2 * i) : c;
+        ca[i] = NORM ? mul2(c, wa) : c;
+        cb[i] = NORM ? mul2(c, wb) : c;
+        sa[i] = NORM ? mul2(s, wa) : s;
+        sb[i] = minus(NORM ? mul2(s, wb) : s);
     }
     const float inverse_dim = 1.0f / float(p.dim);
     int stage = 0, head = row.mine && has ? me.first : side.heads;
@@ -317,7 +379,8 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const 
             float2 sum = {0.0f, 0.0f};
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fma2(make_float2(f[2 * e], f[2 * e + 1]), make_float2(f[2 * e], f[2 * e + 1]), sum);
-            r.x = r.y = row.there ? rsqrtf(fmaf(group_sum(sum.x + sum.y, p.lanes), inverse_dim, p.eps)) : 0.0f;
+            const float squares = group_sum(sum.x + sum.y, p.lanes);
+            r.x = r.y = row.there ? rsqrtf(fmaf(squares, inverse_dim, p.eps)) : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -345,107 +408,122 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
 {
     extern __shared__ __align__(16) char shared[];
     __shared__ Pairs pairs;
+    __shared__ __align__(16) Weights weights;
     constexpr int kStages = kBackwardStages<T>;
     const BackwardRing<T> ring(shared);
     let_next_begin(p.overlap);
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
     const unsigned block = blockIdx.x - (keys ? p.side[0].blocks : 0u);
-    const Share me(p, side.heads);
-    const bool has = me.lane * 16 < p.dim;
-    const int unit = has ? me.lane : 0;
+    const int heads = side.heads, lane = threadIdx.x % p.lanes;
+    const bool has = lane * 16 < p.dim;
+    const int unit = has ? lane : 0;
     const Place at = place<8>(p, unit);
     const int to_b = at.b - at.a;
     const float inverse_dim = 1.0f / float(p.dim);
-    const unsigned first_row = block * rows_of_block(p), row_step = side.blocks * rows_of_block(p);
-    const unsigned long long x_step = p.split * side.x.head, y_step = p.split * side.dy.head, dst_step = p.split * side.out.head;
-    // what is fetched next: the loads run through all turns of all rows of the group, ahead of the sums
-    unsigned ahead_row = first_row + me.row;
-    int ahead = 0, ahead_heads = 0;                   // turn, heads if the row is there
+    // what is fetched next: the loads run ahead of the sums, over the bundles' ends
+    Walk now(p, block, side.blocks, heads), ahead = now;
     const T *src = nullptr, *grad = nullptr;
+    bool ahead_there = false, ahead_new = true;
     const auto fetch = [&](int stage) {
-        if (ahead == 0) {
-            const RowAt row(p, ahead_row);
-            ahead_heads = row.there && has ? side.heads - me.first : 0;
-            src = row.in<T>(side.x) + me.first * side.x.head + at.a;
-            grad = row.in<T>(side.dy) + me.first * side.dy.head + at.a;
-        }
-        if (ahead * p.split < ahead_heads) {
-            ring.fetch(stage, 0, src);
-            ring.fetch(stage, 1, src + to_b);
-            ring.fetch(stage, 2, grad);
-            ring.fetch(stage, 3, grad + to_b);
-            src += x_step;
-            grad += y_step;
-        } else {
-            ring.clear(stage);
+        if (ahead_new) skip_absent(p, heads, ahead, [](const RowAt &, int) {});
+        if (ahead.left > 0) {
+            if (ahead_new) {
+                const RowAt row(p, ahead.row(p));
+                ahead_there = row.there && has;
+                src = row.in<T>(side.x) + ahead.head * side.x.head + at.a;
+                grad = row.in<T>(side.dy) + ahead.head * side.dy.head + at.a;
+            }
+            if (ahead_there) {
+                ring.fetch(stage, 0, src);
+                ring.fetch(stage, 1, src + to_b);
+                ring.fetch(stage, 2, grad);
+                ring.fetch(stage, 3, grad + to_b);
+            } else {
+                ring.clear(stage);
+            }
+            src += side.x.head;
+            grad += side.dy.head;
+            ahead.next(p, heads);
+            ahead_new = ahead.head == 0;
         }
         copies_commit();
-        if (++ahead == me.turns) {
-            ahead = 0;
-            ahead_row = ahead_row < p.rows ? ahead_row + row_step : ahead_row;       // stays behind the last row
-        }
     };
 #pragma unroll
     for (int j = 0; j < kStages - 1; ++j) fetch(j);
     pairs.fill(p);
-    float2 wa[4], wb[4], da[4] = {}, db[4] = {};
-    read_weights<ADJACENT>(p, side, at, wa, wb);
+    weights.fill(p, side);
     __syncthreads();
-    unsigned long long position = position_at(p, RowAt(p, first_row + me.row), pairs.axis[unit * 8]);
+    float2 wa[4], wb[4], da[4] = {}, db[4] = {};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        wa[i] = two(weights.first, unit * 8 + 2 * i);
+        wb[i] = two(weights.second, unit * 8 + 2 * i);
+    }
+    unsigned long long position = position_at(p, RowAt(p, now.row(p)), pairs.axis[unit * 8]);
+    float2 c[4], s[4];
+    T *dst = nullptr;
+    bool mine = false, there = false, fresh = true;
     int stage = 0;
-    // a warp's groups have neighbouring rows and go on as long as one of them is there
-    for (unsigned n = first_row + me.row; n - me.row + (threadIdx.x & ~31u) / (p.lanes * p.split) < p.rows; n += row_step) {
-        const RowAt row(p, n);
-        T *dst = row.in<T>(side.out) + me.first * side.out.head + at.a;
-        float2 c[4], s[4];
-        {
-            float cs[8], sn[8];
-            angles<8>(p, pairs, row, position, unit * 8, 1, cs, sn);
+    while (true) {
+        if (fresh) {
+            const bool skipped = skip_absent(p, heads, now, [&](const RowAt &row, int turns) {
+                T *to = row.in<T>(side.out) + now.head * side.out.head + at.a;
+                const float zeros[8] = {};
+                for (; row.mine && has && turns > 0; --turns, to += side.out.head) {
+                    store_group(to, zeros);
+                    store_group(to + to_b, zeros);
+                }
+            });
+            if (now.left == 0) break;
+            const RowAt row(p, now.row(p));
+            if (skipped) position = position_at(p, row, pairs.axis[unit * 8]);
+            mine = row.mine && has;
+            there = row.there && has;
+            dst = row.in<T>(side.out) + now.head * side.out.head + at.a;
+            Angles angles{p, pairs, row, position, pairs.axis[unit * 8]};
+            position = position_at(p, RowAt(p, now.next_row(p)), pairs.axis[unit * 8]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[i] = make_float2(cs[2 * i], cs[2 * i + 1]);
-                s[i] = make_float2(sn[2 * i], sn[2 * i + 1]);
-            }
+            for (int i = 0; i < 4; ++i) angles.two(unit * 8 + 2 * i, &c[i], &s[i]);
         }
-        if (n < p.rows && p.rows - n > row_step) position = position_at(p, RowAt(p, n + row_step), pairs.axis[unit * 8]);
-        int head = row.mine && has ? me.first : side.heads;
-        for (int j = 0; j < me.turns; ++j, head += p.split, dst += dst_step) {
-            copies_wait<kStages - 2>();
-            float f[16], g[16];
-            ring.get(stage, 0, f);
-            ring.get(stage, 1, f + 8);
-            ring.get(stage, 2, g);
-            ring.get(stage, 3, g + 8);
-            // into the slot that the turn before this one has used up
-            fetch(stage == 0 ? kStages - 1 : stage - 1);
-            stage = stage == kStages - 1 ? 0 : stage + 1;
-            float2 square = {0.0f, 0.0f}, dot = {0.0f, 0.0f};
+        copies_wait<kStages - 2>();
+        float f[16], g[16];
+        ring.get(stage, 0, f);
+        ring.get(stage, 1, f + 8);
+        ring.get(stage, 2, g);
+        ring.get(stage, 3, g + 8);
+        // into the slot that the turn before this one has used up
+        fetch(stage == 0 ? kStages - 1 : stage - 1);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        float2 square = {0.0f, 0.0f}, dot = {0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-                const float2 ya = firsts<ADJACENT>(g, i), yb = seconds<ADJACENT>(g, i);
-                const float2 na = fma2(ya, c[i], mul2(yb, s[i])), nb = fma2(yb, c[i], mul2(ya, minus(s[i])));
-                square = fma2(b, b, fma2(a, a, square));
-                dot = fma2(mul2(b, wb[i]), nb, fma2(mul2(a, wa[i]), na, dot));
-                put_pairs<ADJACENT>(g, i, na, nb);
-            }
-            const float2 sums = group_sum(make_float2(square.x + square.y, dot.x + dot.y), p.lanes);
-            const float scale = row.there && head < side.heads ? rsqrtf(fmaf(sums.x, inverse_dim, p.eps)) : 0.0f, pull = -sums.y * inverse_dim * scale * scale;
-            const float2 r = {scale, scale}, q = {pull, pull};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-                const float2 na = firsts<ADJACENT>(g, i), nb = seconds<ADJACENT>(g, i);
-                da[i] = fma2(na, mul2(a, r), da[i]);
-                db[i] = fma2(nb, mul2(b, r), db[i]);
-                put_pairs<ADJACENT>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
-            }
-            if (head < side.heads) {
-                store_group(dst, f);
-                store_group(dst + to_b, f + 8);
-            }
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+            const float2 ya = firsts<ADJACENT>(g, i), yb = seconds<ADJACENT>(g, i);
+            const float2 na = fma2(ya, c[i], mul2(yb, s[i])), nb = fma2(yb, c[i], mul2(ya, minus(s[i])));
+            square = fma2(b, b, fma2(a, a, square));
+            dot = fma2(mul2(b, wb[i]), nb, fma2(mul2(a, wa[i]), na, dot));
+            put_pairs<ADJACENT>(g, i, na, nb);
         }
+        const float2 sums = group_sum(make_float2(square.x + square.y, dot.x + dot.y), p.lanes);
+        // 0 where nothing is there: infinite without eps, it would make a NaN of the zeros
+        const float scale = there ? rsqrtf(fmaf(sums.x, inverse_dim, p.eps)) : 0.0f, pull = -sums.y * inverse_dim * scale * scale;
+        const float2 r = {scale, scale}, q = {pull, pull};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
+            const float2 na = firsts<ADJACENT>(g, i), nb = seconds<ADJACENT>(g, i);
+            da[i] = fma2(na, mul2(a, r), da[i]);
+            db[i] = fma2(nb, mul2(b, r), db[i]);
+            put_pairs<ADJACENT>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
+        }
+        if (mine) {
+            store_group(dst, f);
+            store_group(dst + to_b, f + 8);
+        }
+        dst += side.out.head;
+        now.next(p, heads);
+        fresh = now.head == 0 || now.left == 0;
     }
     copies_wait<0>();
     __syncthreads();
@@ -511,7 +589,9 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
         if (j0 == 0) {                                // the first loads are under way
             pairs.fill(p);
             __syncthreads();
-            angles<kOwn>(p, pairs, row, position_at(p, row, pairs.axis[me.lane]), me.lane, p.lanes, c, s);
+            Angles angles{p, pairs, row, position_at(p, row, pairs.axis[me.lane]), pairs.axis[me.lane]};
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n) angles.at(min(me.lane + n * p.lanes, kMaxPairs - 1), &c[n], &s[n]);
         }
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
@@ -548,73 +628,74 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
     const bool keys = blockIdx.x >= p.side[0].blocks;
     const Side &side = p.side[keys];
     const unsigned block = blockIdx.x - (keys ? p.side[0].blocks : 0u);
-    const Share me(p, side.heads);
-    const Own own(p, side, me.lane, true);
+    const int heads = side.heads, lane = threadIdx.x % p.lanes;
+    const Own own(p, side, lane, true);
     const float inverse_dim = 1.0f / float(p.dim);
-    const unsigned first_row = block * rows_of_block(p), row_step = side.blocks * rows_of_block(p);
     pairs.fill(p);
     __syncthreads();
-    float dw[kOwn][2] = {};
-    for (unsigned n0 = first_row + me.row; n0 - me.row + (threadIdx.x & ~31u) / (p.lanes * p.split) < p.rows; n0 += row_step) {
-        const RowAt row(p, n0);
-        const T *const src = row.in<T>(side.x), *const grad = row.in<T>(side.dy);
-        T *const dst = row.in<T>(side.out);
-        float c[kOwn], s[kOwn];
-        for (int j0 = 0; j0 < me.turns; j0 += kAhead) {
-            T x[kAhead][kOwn][2], y[kAhead][kOwn][2];
+    float dw[kOwn][2] = {}, c[kOwn], s[kOwn];
+    bool fresh = true;
+    for (Walk now(p, block, side.blocks, heads); now.left > 0;) {
+        const RowAt row(p, now.row(p));
+        const T *const src = row.in<T>(side.x) + now.head * side.x.head, *const grad = row.in<T>(side.dy) + now.head * side.dy.head;
+        T *const dst = row.in<T>(side.out) + now.head * side.out.head;
+        const int turns = min(min(kAhead, now.left), heads - now.head);
+        T x[kAhead][kOwn][2], y[kAhead][kOwn][2];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int head = me.first + (j0 + i) * p.split;
+        for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-                for (int n = 0; n < kOwn; ++n)
-                    if (row.there && head < side.heads && own.has[n]) {
-                        x[i][n][0] = src[head * side.x.head + own.at[n].a];
-                        x[i][n][1] = src[head * side.x.head + own.at[n].b];
-                        y[i][n][0] = grad[head * side.dy.head + own.at[n].a];
-                        y[i][n][1] = grad[head * side.dy.head + own.at[n].b];
-                    }
+            for (int n = 0; n < kOwn; ++n)
+                if (row.there && i < turns && own.has[n]) {
+                    x[i][n][0] = src[i * side.x.head + own.at[n].a];
+                    x[i][n][1] = src[i * side.x.head + own.at[n].b];
+                    y[i][n][0] = grad[i * side.dy.head + own.at[n].a];
+                    y[i][n][1] = grad[i * side.dy.head + own.at[n].b];
+                }
+        if (fresh) {
+            Angles angles{p, pairs, row, position_at(p, row, pairs.axis[lane]), pairs.axis[lane]};
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n) angles.at(min(lane + n * p.lanes, kMaxPairs - 1), &c[n], &s[n]);
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (i >= turns) break;
+            float f[kOwn][2], g[kOwn][2], square = 0.0f, dot = 0.0f;
+#pragma unroll
+            for (int n = 0; n < kOwn; ++n) {
+                f[n][0] = f[n][1] = g[n][0] = g[n][1] = 0.0f;
+                if (row.there && own.has[n]) {
+                    const float ya = to_float(y[i][n][0]), yb = to_float(y[i][n][1]);
+                    f[n][0] = to_float(x[i][n][0]);
+                    f[n][1] = to_float(x[i][n][1]);
+                    g[n][0] = fmaf(ya, c[n], yb * s[n]);
+                    g[n][1] = fmaf(yb, c[n], -ya * s[n]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    square = fmaf(f[n][e], f[n][e], square);
+                    dot = fmaf(f[n][e] * own.w[n][e], g[n][e], dot);
+                }
             }
-            if (j0 == 0) angles<kOwn>(p, pairs, row, position_at(p, row, pairs.axis[me.lane]), me.lane, p.lanes, c, s);
+            const float2 both = group_sum(make_float2(square, dot), p.lanes);
+            if (!row.mine) continue;
+            const float r = rsqrtf(fmaf(both.x, inverse_dim, p.eps)), pull = both.y * inverse_dim * r * r;
+            T *const at = dst + i * side.out.head;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int head = me.first + (j0 + i) * p.split;
-                const bool work = row.mine && head < side.heads, live = work && row.there;
-                float f[kOwn][2], g[kOwn][2], square = 0.0f, dot = 0.0f;
+            for (int n = 0; n < kOwn; ++n) {
+                if (!own.has[n]) continue;
+                float dx[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int n = 0; n < kOwn; ++n) {
-                    f[n][0] = f[n][1] = g[n][0] = g[n][1] = 0.0f;
-                    if (live && own.has[n]) {
-                        const float ya = to_float(y[i][n][0]), yb = to_float(y[i][n][1]);
-                        f[n][0] = to_float(x[i][n][0]);
-                        f[n][1] = to_float(x[i][n][1]);
-                        g[n][0] = fmaf(ya, c[n], yb * s[n]);
-                        g[n][1] = fmaf(yb, c[n], -ya * s[n]);
+                for (int e = 0; e < 2; ++e)
+                    if (row.there) {
+                        dw[n][e] = fmaf(g[n][e], f[n][e] * r, dw[n][e]);
+                        dx[e] = r * fmaf(-f[n][e], pull, g[n][e] * own.w[n][e]);
                     }
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        square = fmaf(f[n][e], f[n][e], square);
-                        dot = fmaf(f[n][e] * own.w[n][e], g[n][e], dot);
-                    }
-                }
-                const float2 both = group_sum(make_float2(square, dot), p.lanes);
-                if (!work) continue;
-                const float r = rsqrtf(fmaf(both.x, inverse_dim, p.eps)), pull = both.y * inverse_dim * r * r;
-                T *const at = dst + head * side.out.head;
-#pragma unroll
-                for (int n = 0; n < kOwn; ++n) {
-                    if (!own.has[n]) continue;
-                    float dx[2] = {0.0f, 0.0f};
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        if (row.there) {
-                            dw[n][e] = fmaf(g[n][e], f[n][e] * r, dw[n][e]);
-                            dx[e] = r * fmaf(-f[n][e], pull, g[n][e] * own.w[n][e]);
-                        }
-                    at[own.at[n].a] = from_float<T>(dx[0]);
-                    at[own.at[n].b] = from_float<T>(dx[1]);
-                }
+                at[own.at[n].a] = from_float<T>(dx[0]);
+                at[own.at[n].b] = from_float<T>(dx[1]);
             }
         }
+        now.next(p, heads, turns);
+        fresh = now.head == 0;
     }
 #pragma unroll
     for (int n = 0; n < kOwn; ++n)
@@ -633,23 +714,28 @@ struct WeightParams {
     unsigned blocks[2];
     int dim, bf16;
 };
-// The blocks' sums of 32 channels of a side: a warp's share of the blocks each, the warps in order.
+// The blocks' sums of eight channels of a side: a thread's share of the blocks each, lanes and warps in order.
+constexpr int kJoin = 8;
 __global__ void __launch_bounds__(1024) rotary_weight_kernel(const WeightParams p)
 {
-    __shared__ float sum[32][33];
-    const int side = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32, ch = blockIdx.x * 32 + lane;
+    __shared__ float sum[32][kJoin];
+    const int side = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32, ch = blockIdx.x * kJoin + threadIdx.x % kJoin;
+    const float *const partial = side ? p.partial[1] : p.partial[0];
+    const unsigned blocks = side ? p.blocks[1] : p.blocks[0];
     wait_for_previous();
     float v = 0.0f;
     if (ch < p.dim)
-        for (unsigned b = warp; b < p.blocks[side]; b += 32) v += p.partial[side][(unsigned long long)b * p.dim + ch];
-    sum[warp][lane] = v;
+        for (unsigned b = threadIdx.x / kJoin; b < blocks; b += 1024 / kJoin) v += partial[(unsigned long long)b * p.dim + ch];
+    for (int o = kJoin; o < 32; o *= 2) v += __shfl_xor_sync(~0u, v, o);
+    if (lane < kJoin) sum[warp][lane] = v;
     __syncthreads();
-    v = sum[lane][warp];                               // channel `warp` of the block's
-    for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(~0u, v, o);
-    const int out = blockIdx.x * 32 + warp;
-    if (lane == 0 && out < p.dim) {
-        if (p.bf16) static_cast<__nv_bfloat16 *>(p.grad[side])[out] = __float2bfloat16_rn(v);
-        else static_cast<float *>(p.grad[side])[out] = v;
+    if (warp > 0) return;
+    v = 0.0f;
+    for (int w = lane / kJoin; w < 32; w += 32 / kJoin) v += sum[w][lane % kJoin];
+    for (int o = kJoin; o < 32; o *= 2) v += __shfl_xor_sync(~0u, v, o);
+    if (lane < kJoin && ch < p.dim) {
+        if (p.bf16) static_cast<__nv_bfloat16 *>(side ? p.grad[1] : p.grad[0])[ch] = __float2bfloat16_rn(v);
+        else static_cast<float *>(side ? p.grad[1] : p.grad[0])[ch] = v;
     }
 }
 
@@ -707,32 +793,48 @@ bool wide_view(const omni_rotary *r, const View &v)
     return aligned(v.data, 16) && v.batch * size % 16 == 0 && v.row * size % 16 == 0 && v.head * size % 16 == 0;
 }
 
-// The launch: lanes of a head vector, groups that share a row's heads, blocks of either side.
+// The launch: lanes of a head vector, how rows and heads are dealt, blocks of either side.
 struct Shape {
     int lanes, split;
-    unsigned blocks[2];
+    unsigned bundles, step, blocks[2];
 };
-
-// A group has all heads of a row, so that every angle is made once; where there are few rows (decoding) groups share a row and make its angles each.
-Shape shape_of(const omni_rotary *r, bool wide, int sms, int resident)
+int lanes_of(const omni_rotary *r, bool wide)
 {
-    Shape s;
     const int units = wide ? r->dim / 16 : r->dim / 2;
-    s.lanes = 1;
-    while (s.lanes < units && s.lanes < 32) s.lanes *= 2;
+    int lanes = 1;
+    while (lanes < units && lanes < 32) lanes *= 2;
+    return lanes;
+}
+
+// Forward: a group has all heads of a row, so that every angle is made once; where there are few rows (decoding) groups share a row and
+// make its angles each.
+Shape forward_shape(const omni_rotary *r, bool wide, int sms)
+{
+    Shape s = {lanes_of(r, wide), 1, 0, 0, {0, 0}};
     const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length);
     const int groups = kThreads / s.lanes, most = r->heads > r->kv_heads ? r->heads : r->kv_heads;
-    s.split = 1;
     while (s.split < groups && s.split < most && rows * s.split < uint64_t(sms) * groups * 2) s.split *= 2;
-    const uint64_t of_block = groups / s.split, blocks = (rows + of_block - 1) / of_block;
-    s.blocks[0] = s.blocks[1] = unsigned(blocks);
-    if (resident) {                                   // blocks that stay: shares by the work of a row, its angles about that of two heads
-        const uint64_t all = uint64_t(sms) * resident, q = r->heads + 2, k = r->kv_heads + 2;
-        uint64_t share = all * q / (q + k);
-        share = share < 1 ? 1 : share > all - 1 ? all - 1 : share;
-        s.blocks[0] = unsigned(blocks < share ? blocks : share);
-        s.blocks[1] = unsigned(blocks < all - share ? blocks : all - share);
-    }
+    const uint64_t of_block = groups / s.split;
+    s.blocks[0] = s.blocks[1] = unsigned((rows + of_block - 1) / of_block);
+    return s;
+}
+
+// Backward: as many blocks as are resident at once, shared between the sides by the work of a row, whose angles are about that of two
+// heads; where there is less work a warp has one turn.
+Shape backward_shape(const omni_rotary *r, bool wide, int sms)
+{
+    Shape s = {lanes_of(r, wide), 1, 0, 0, {0, 0}};
+    const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length), of_bundle = 32 / s.lanes;
+    s.bundles = unsigned((rows + of_bundle - 1) / of_bundle);
+    s.step = s.bundles / 2 + s.bundles / 8 + 1;       // no common divisor with their number: every bundle comes up once
+    while (std::gcd(s.step, s.bundles) != 1) ++s.step;
+    s.step %= s.bundles;
+    const uint64_t all = uint64_t(sms) * kResident, q = r->heads + 2, k = r->kv_heads + 2;
+    uint64_t share = all * q / (q + k);
+    share = share < 1 ? 1 : share > all - 1 ? all - 1 : share;
+    const uint64_t q_most = (s.bundles * uint64_t(r->heads) + kWarps - 1) / kWarps, k_most = (s.bundles * uint64_t(r->kv_heads) + kWarps - 1) / kWarps;
+    s.blocks[0] = unsigned(q_most < share ? q_most : share);
+    s.blocks[1] = unsigned(k_most < all - share ? k_most : all - share);
     return s;
 }
 
@@ -753,6 +855,8 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
     p->axes = r->axes;
     p->lanes = s.lanes;
     p->split = s.split;
+    p->bundles = s.bundles;
+    p->step = s.step;
     p->wide_positions = r->position_type == OMNI_I64;
     p->bf16_weight = r->weight_dtype == OMNI_BF16;
     p->interleaved = r->interleaved != 0;
@@ -810,7 +914,7 @@ int rotate(omni_ctx *ctx, const omni_rotary *r, const omni_attn_view *const (&in
         p.side[i] = {view_of(r, in[i], heads), {}, view_of(r, out[i], heads), nullptr, nullptr, 0, 0};
         wide = wide && wide_view(r, p.side[i].x) && wide_view(r, p.side[i].out);
     }
-    fill(&p, r, shape_of(r, wide, dev.sm_count, 0), backwards);
+    fill(&p, r, forward_shape(r, wide, dev.sm_count), backwards);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool norm = r->q_weight && !backwards;
     if (r->dtype == OMNI_BF16)
@@ -904,7 +1008,7 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
             p.side[i] = {view_of(r, x[i], heads), view_of(r, dy[i], heads), view_of(r, dx[i], heads), nullptr, nullptr, 0, 0};
             wide = wide && wide_view(r, p.side[i].x) && wide_view(r, p.side[i].dy) && wide_view(r, p.side[i].out);
         }
-        const Shape shape = shape_of(r, wide, dev.sm_count < kMostSms ? dev.sm_count : kMostSms, kResident);
+        const Shape shape = backward_shape(r, wide, dev.sm_count < kMostSms ? dev.sm_count : kMostSms);
         fill(&p, r, shape, false);
         p.overlap = dev.overlap;
         p.side[0].partial = static_cast<float *>(workspace);
@@ -916,7 +1020,7 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
         rc = r->dtype == OMNI_BF16 ? enqueue_backward<__nv_bfloat16>(ctx, p, wide, s) : enqueue_backward<float>(ctx, p, wide, s);
         if (rc != OMNI_OK) return rc;
     }
-    Dependent launch(dev, dim3((r->dim + 31) / 32, 2), 1024, 0, s);
+    Dependent launch(dev, dim3((r->dim + kJoin - 1) / kJoin, 2), 1024, 0, s);
     if (empty) launch.cfg.numAttrs = 0;
     return context_launched(ctx, int(cudaLaunchKernelEx(&launch.cfg, rotary_weight_kernel, w)));
 }
