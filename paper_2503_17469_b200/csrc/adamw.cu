@@ -110,28 +110,60 @@ __device__ __forceinline__ void store_codes(unsigned char *p, bool wide, int cou
         if (i < count) p[i] = (unsigned char)((i < 4 ? c.x : c.y) >> (8 * (i % 4)));
 }
 
-// What a code stands for; MOST: 127 for the signed codes of m, 255 for those of v.
-template <int MOST> __device__ __forceinline__ float decode(uint32_t code, int top)
+// What four codes in a word stand for; MOST: 127 for the signed codes of m, 255 for those of v.  A byte is put to bits 16 to 23, and one
+// multiply-add shifts it and adds the block's offset: the units of whole numbers are the busiest part of this kernel.
+template <int MOST> __device__ __forceinline__ void decode4(uint32_t word, uint32_t below, float *f)
 {
-    const int c = int(code & MOST);
-    const uint32_t bits = c ? uint32_t(c + top - MOST) << 20 : 0u;
-    return __uint_as_float(MOST == 127 ? bits | (code & 128u) << 24 : bits);
+    const uint32_t sizes = MOST == 127 ? word & 0x7f7f7f7fu : word;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t c = __byte_perm(sizes, 0u, 0x4044 | i << 8), bits = c ? c * 16u + below : 0u;
+        f[i] = __uint_as_float(MOST == 127 ? bits | (__byte_perm(word, 0u, 0x0444 | i << 12) & 0x80000000u) : bits);
+    }
 }
 template <int MOST> __device__ __forceinline__ void decode8(uint2 c, int top, float *f)
 {
+    const uint32_t below = uint32_t(top - MOST) << 20;
+    decode4<MOST>(c.x, below, f);
+    decode4<MOST>(c.y, below, f + 4);
+}
+// The float's top twelve bits less the sign, rounded by 16 random bits at bit 4.  A NaN may come out one too high.
+__device__ __forceinline__ uint32_t rounded(uint32_t bits, uint32_t random) { return random * 16u + bits >> 20; }
+// The low bytes of four words as one.
+__device__ __forceinline__ uint32_t join4(const uint32_t *c)
+{
+    return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+}
+// Codes of four elements from their rounded tops r <= top, and from the elements themselves (for the signs).
+template <int MOST> __device__ __forceinline__ uint32_t encode4(const uint32_t *r, int top, const float *x)
+{
+    uint32_t c[4];
 #pragma unroll
-    for (int i = 0; i < kGroup; ++i) f[i] = decode<MOST>((i < 4 ? c.x : c.y) >> (8 * (i % 4)) & 255u, top);
+    for (int i = 0; i < 4; ++i) {
+        c[i] = uint32_t(__viaddmax_s32(int(r[i]), MOST - top, MOST == 255 ? 1 : 0));
+        if (MOST == 255) c[i] = top >= 255 ? min(c[i], r[i]) : r[i] ? c[i] : 0u;       // zero stays zero
+        else if (top < 127) c[i] = r[i] ? c[i] : 0u;
+    }
+    const uint32_t word = join4(c);
+    if (MOST == 255) return word;
+    uint32_t s[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = __float_as_uint(x[i]);
+    const uint32_t signs = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410);
+    return word | (word + 0x7f7f7f7fu & 0x80808080u & signs);           // a code of 0 has no sign
 }
-// The float's top twelve bits less the sign, rounded by 16 random bits; a NaN stays one.
-__device__ __forceinline__ uint32_t rounded(float x, uint32_t random)
+// Within 2^-22 of the root and of the inverse.
+__device__ __forceinline__ float root(float x)
 {
-    return min((__float_as_uint(x) & 0x7fffffffu) + (random << 4) >> 20, 0x7ffu);
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
-template <int MOST> __device__ __forceinline__ uint32_t encode(uint32_t r, int top, float x)
+__device__ __forceinline__ float inverse(float x)
 {
-    const int c = int(r) - top + MOST;
-    if (MOST == 255) return r ? uint32_t(max(c, 1)) : 0u;
-    return c > 0 ? uint32_t(c) | (__float_as_uint(x) >> 24 & 128u) : 0u;
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
 // 32 bits of an element's own, by multiplications and shifts of its number, its tensor's and the step's.
@@ -190,11 +222,15 @@ template <typename G, int BITS> __global__ void __launch_bounds__(kThreads) adam
     }
     const float keep = float(1.0 - p.lr * e.decay);
 #pragma unroll
-    for (int i = 0; i < kGroup; ++i) {
-        m[i] = __fmaf_rn(p.b1, m[i], __fmul_rn(p.c1, g[i]));
-        v[i] = __fmaf_rn(__fmul_rn(p.c2, g[i]), g[i], __fmul_rn(p.b2, v[i]));
-        const float below = __fmaf_rn(__fsqrt_rn(v[i]), spread, p.eps);
-        theta[i] = __fmaf_rn(-rate, __fdiv_rn(m[i], below), __fmul_rn(keep, theta[i]));
+    for (int i = 0; i < kGroup; i += 2) {
+        const float2 x = {g[i], g[i + 1]}, t = {theta[i], theta[i + 1]};
+        const float2 m1 = fma2({p.b1, p.b1}, {m[i], m[i + 1]}, mul2({p.c1, p.c1}, x));
+        const float2 v1 = fma2(mul2({p.c2, p.c2}, x), x, mul2({p.b2, p.b2}, {v[i], v[i + 1]}));
+        const float2 below = fma2({root(v1.x), root(v1.y)}, {spread, spread}, {p.eps, p.eps});
+        const float2 t1 = fma2({-rate, -rate}, mul2(m1, {inverse(below.x), inverse(below.y)}), mul2({keep, keep}, t));
+        m[i] = m1.x; m[i + 1] = m1.y;
+        v[i] = v1.x; v[i + 1] = v1.y;
+        theta[i] = t1.x; theta[i + 1] = t1.y;
     }
     store8(e.param + at, wide, count, theta);
     if (e.copy) store8(e.copy + at, wide, count, theta);
@@ -203,25 +239,29 @@ template <typename G, int BITS> __global__ void __launch_bounds__(kThreads) adam
         store8(fv, wide, count, v);
     } else {
         const uint32_t start = step * 0x85EBCA77u + tensor * 0xC2B2AE3Du + uint32_t(at) * kStride;
+        // What stands behind the end was loaded as zeros: it is zero still, and its codes are not stored.
         uint32_t rm[kGroup], rv[kGroup], most_m = 0, most_v = 0;
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) {
             const uint32_t random = scramble(start + i * kStride);
-            rm[i] = i < count ? rounded(m[i], random & 0xffffu) : 0u;
-            rv[i] = i < count ? rounded(v[i], random >> 16) : 0u;
+            rm[i] = rounded(__float_as_uint(m[i]) & 0x7fffffffu, random & 0xffffu);
+            rv[i] = rounded(__float_as_uint(v[i]), random >> 16);        // not negative
             most_m = max(most_m, rm[i]);
             most_v = max(most_v, rv[i]);
         }
         most_m = __reduce_max_sync(~0u, most_m);
         most_v = __reduce_max_sync(~0u, most_v);
-        uint32_t wm[2] = {0, 0}, wv[2] = {0, 0};
+        if (max(most_m, most_v) > 0x7ffu) {
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) {
-            wm[i / 4] |= encode<127>(rm[i], int(most_m), m[i]) << (8 * (i % 4));
-            wv[i / 4] |= encode<255>(rv[i], int(most_v), v[i]) << (8 * (i % 4));
+            for (int i = 0; i < kGroup; ++i) {
+                rm[i] = min(rm[i], 0x7ffu);
+                rv[i] = min(rv[i], 0x7ffu);
+            }
+            most_m = min(most_m, 0x7ffu);
+            most_v = min(most_v, 0x7ffu);
         }
-        store_codes(cm, wide, count, {wm[0], wm[1]});
-        store_codes(cv, wide, count, {wv[0], wv[1]});
+        store_codes(cm, wide, count, {encode4<127>(rm, int(most_m), m), encode4<127>(rm + 4, int(most_m), m + 4)});
+        store_codes(cv, wide, count, {encode4<255>(rv, int(most_v), v), encode4<255>(rv + 4, int(most_v), v + 4)});
         if (threadIdx.x % 32 == 0) e.tops[at / kBlock] = most_m | most_v << 16;
     }
 }

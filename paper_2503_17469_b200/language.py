@@ -26,6 +26,7 @@ from . import binding as B
 _DTYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16}
 _INDEX = {torch.int32: B.I32, torch.int64: B.I64}
 _like, _float, _bf16, _byte = torch.empty_like, torch.float32, torch.bfloat16, torch.uint8
+_size, _contiguous, _where, _address = torch.Tensor.size, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr
 _ref = C.byref
 
 
@@ -606,6 +607,7 @@ class AdamW(_Operator):
         self._record = host
         self._record_dev = host.to(f"cuda:{self._at}")
         self._batches = C.c_int32 * self.K
+        self._shapes, self._pointers = [p.shape for p in params], C.c_void_p * max(1, len(params))
 
     @staticmethod
     def _zeros(p, bits):
@@ -650,16 +652,14 @@ class AdamW(_Operator):
             raise ValueError("out: moments of 32 bits are the state itself")
         if out is None:
             out = [tuple(torch.empty(s[0].shape, dtype=_float, device=s[0].device) for _ in range(2)) for s in self.state]
-        if len(out) != len(self.state):
+        if len(out) != len(self.state) or any(len(pair) != 2 for pair in out):
             raise ValueError("out: a pair for each tensor is wanted")
+        # many short tensors: by functions that run over all of them, not tensor by tensor
         tables = []
-        for j in range(2):
-            table = (C.c_void_p * max(1, len(out)))()
-            for i, pair in enumerate(out):
-                t = pair[j]
-                if t.dtype != _float or t.shape != self.state[i][0].shape or not t.is_contiguous() or t.get_device() != self._at:
-                    raise ValueError(f"out[{i}]: contiguous float32 of shape {tuple(self.state[i][0].shape)} on the current device is wanted")
-                table[i] = t.data_ptr()
-            tables.append(table)
+        for values in zip(*out) if out else ((), ()):
+            if list(map(_size, values)) != self._shapes or not all(map(_contiguous, values)) or any(t.dtype is not _float for t in values) \
+                    or any(map(self._at.__ne__, map(_where, values))):
+                raise ValueError("out: contiguous float32 pairs of the tensors' shapes on the current device are wanted")
+            tables.append(self._pointers(*map(_address, values)))
         self._check(self._lib.omni_adamw_moments(self.ctx._h, self._record.data_ptr(), self._record_dev.data_ptr(), *tables, _raw_stream(self._at)))
         return out
