@@ -145,12 +145,9 @@ template <int MOST> __device__ __forceinline__ uint32_t encode4(const uint32_t *
         else if (top < 127) c[i] = r[i] ? c[i] : 0u;
     }
     const uint32_t word = join4(c);
-    if (MOST == 255) return word;
-    uint32_t s[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = __float_as_uint(x[i]);
-    const uint32_t signs = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410);
-    return word | (word + 0x7f7f7f7fu & 0x80808080u & signs);           // a code of 0 has no sign
+    const uint32_t signs = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0073),
+                                       __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
+    return MOST == 255 ? word : word | (word + 0x7f7f7f7fu & 0x80808080u & signs);           // a code of 0 has no sign
 }
 // Within 2^-22 of the root and of the inverse.
 __device__ __forceinline__ float root(float x)

@@ -12,7 +12,8 @@
 namespace omni {
 namespace {
 
-constexpr int kMostWalkers = 256;
+constexpr int kWalkers = 256, kMostWalkers = 512;     // threads of a row: backward; forward and step
+constexpr int kMostHeld = 112 * 1024;                 // bytes of a row that is held: two rows an SM
 enum Mode { kForward = 0, kBackward = 1, kStep = 2 };
 
 struct PolicyParams {
@@ -62,9 +63,85 @@ __device__ __forceinline__ Value value_of(const PolicyParams &p, float logp)
     return v;
 }
 
-// The gradient of the row, by the whole CTA.  q(z) is -weight times the probability of a token with logit z.
-template <int AHEAD, typename T, bool NEAR>
-__device__ __forceinline__ void put_row(const PolicyParams &p, const Row<T> &w, const Sample &t, const Softmax<NEAR> &q, float weight)
+// A row's groups as its threads fetch them ahead, each thread those that it walks: two groups to a step, 64 to 128 bytes in flight.
+// With HELD every group has a place of its own, and the second walk finds the row in shared memory; otherwise a few places go round.
+template <typename T, bool HELD> struct Fetched {
+    static constexpr int kStep = 2, kAhead = sizeof(T) == 2 ? 4 : 2;
+    const Row<T> &w;
+    char *const at;
+    int own, fetched = 0;                             // groups of this thread, groups asked for
+    __device__ __forceinline__ Fetched(const Row<T> &row, char *shared)
+        : w(row), at(shared), own((row.parts.groups - int(threadIdx.x) + row.walkers - 1) / row.walkers) {}
+    static __host__ __device__ size_t bytes(int vocab, int walkers)
+    {
+        return HELD ? size_t(vocab / kGroup) * kGroup * sizeof(T) : size_t(kStep * kAhead) * walkers * kGroup * sizeof(T);
+    }
+    __device__ __forceinline__ char *place(int i) const
+    {
+        return at + size_t(((HELD ? i : i % (kStep * kAhead)) * w.walkers + threadIdx.x)) * (kGroup * sizeof(T));
+    }
+    __device__ __forceinline__ void ask()
+    {
+#pragma unroll
+        for (int i = 0; i < kStep; ++i, ++fetched) {
+            if (fetched >= own) continue;
+            const char *from = reinterpret_cast<const char *>(w.row + w.parts.head + (long long)(threadIdx.x + fetched * w.walkers) * kGroup);
+            const uint32_t to = uint32_t(__cvta_generic_to_shared(place(fetched)));
+#pragma unroll
+            for (int piece = 0; piece < int(kGroup * sizeof(T)) / 16; ++piece)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + piece * 16), "l"(from + piece * 16) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ Group<T> group(int i) const { return *reinterpret_cast<const Group<T> *>(place(i)); }
+};
+
+// The walkers' maxima and sums into their warps' cells, over groups that are fetched ahead.
+template <typename T, bool HELD> __device__ __forceinline__ void reduce_fetched(Fetched<T, HELD> &f, float unit, Joined *cell)
+{
+    constexpr int kStep = f.kStep, kAhead = f.kAhead;
+    Running<false> run;
+    if (f.w.edge() >= 0) run.take_one(to_float(f.w.row[f.w.edge()]), unit);
+    for (int i = 0; i < f.own; i += kStep) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+        if (i + kStep <= f.own) {
+            Group<T> x[kStep];
+#pragma unroll
+            for (int k = 0; k < kStep; ++k) x[k] = f.group(i + k);
+            run.take(x, unit);
+        } else {
+            for (int k = i; k < f.own; ++k) {
+                Group<T> x[1] = {f.group(k)};
+                run.take(x, unit);
+            }
+        }
+        f.ask();
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncwarp();
+    put_warp(run, unit, cell + threadIdx.x / 32);
+}
+
+// f(first group, groups) over the groups of a thread that are held, as walk() over those in memory.
+template <int AHEAD, typename T, bool HELD, typename F> __device__ __forceinline__ void walk(const Fetched<T, HELD> &held, F f)
+{
+    int i = 0;
+    for (; i + AHEAD <= held.own; i += AHEAD) {
+        Group<T> x[AHEAD];
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) x[a] = held.group(i + a);
+        f(int(threadIdx.x) + i * held.w.walkers, x);
+    }
+    for (; i < held.own; ++i) {
+        Group<T> x[1] = {held.group(i)};
+        f(int(threadIdx.x) + i * held.w.walkers, x);
+    }
+}
+
+// The gradient of the row, by the whole CTA, from the groups of `walked` (the row itself, or what is held of it).  q(z) is -weight times
+// the probability of a token with logit z.
+template <int AHEAD, typename W, typename T, bool NEAR>
+__device__ __forceinline__ void put_row(const PolicyParams &p, const W &walked, const Row<T> &w, const Sample &t, const Softmax<NEAR> &q, float weight)
 {
     T *out = static_cast<T *>(p.grad) + blockIdx.x * p.grad_stride;
     const int tid = threadIdx.x, walkers = w.walkers;
@@ -76,7 +153,7 @@ __device__ __forceinline__ void put_row(const PolicyParams &p, const Row<T> &w, 
         return;
     }
     if (same_phase(out, w.row)) {
-        walk<AHEAD>(w, [&](int g, const auto &x) {
+        walk<AHEAD>(walked, [&](int g, const auto &x) {
 #pragma unroll
             for (int a = 0; a < int(sizeof x / sizeof x[0]); ++a)
                 put_group(out + w.parts.head + (long long)(g + a * walkers) * kGroup, x[a], q);
@@ -114,37 +191,49 @@ template <typename T, int MODE> __device__ __forceinline__ void far_row(const Po
     const float logp = nothing ? -INFINITY : __fsub_rn(__fsub_rn(t.z, all.m) / p.temperature, log_sum);
     const float weight = finish(p, t, __fadd_rn(all.m / p.temperature, log_sum), logp, MODE == kStep);
     if constexpr (MODE == kStep)
-        put_row<1>(p, w, t, Softmax<false>{1.0f, Running<true>::reference(all.m), unit, nothing ? 0.0f : -weight / all.s}, weight);
+        put_row<1>(p, w, w, t, Softmax<false>{1.0f, Running<true>::reference(all.m), unit, nothing ? 0.0f : -weight / all.s}, weight);
 }
 
-template <typename T, typename I, int MODE>
-__global__ void __launch_bounds__(kMostWalkers, 4) policy_kernel(const __grid_constant__ PolicyParams p)
+// From a kept lse: one walk.
+template <typename T, typename I> __global__ void __launch_bounds__(kWalkers, 4) policy_backward_kernel(const __grid_constant__ PolicyParams p)
 {
-    __shared__ Joined cell[kMostWalkers / 32];
     constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;    // groups a thread has in flight
     const Row<T> w(static_cast<const T *>(p.logits) + blockIdx.x * p.row_stride, p.vocab, blockDim.x);
     const Sample t = sample_of<T, I>(p, w.row);
+    const float lse = p.lse_in[blockIdx.x];
+    const float logp = __fsub_rn(t.z / p.temperature, lse);
+    const float slope = t.there() ? value_of(p, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
+    const float weight = __fdiv_rn(__fmul_rn(p.grad_loss[blockIdx.x], slope), p.temperature);
+    __syncthreads();                                  // every thread has the token's logit: the gradient may be written over it
+    put_row<kAhead>(p, w, w, t, Softmax<false>{1.0f / p.temperature, lse == -INFINITY ? 0.0f : -lse, kLog2e, -weight}, weight);
+}
+
+template <typename T, typename I, bool STEP, bool HELD>
+__global__ void __launch_bounds__(kMostWalkers, 2) policy_kernel(const __grid_constant__ PolicyParams p)
+{
+    extern __shared__ __align__(16) char shared[];
+    __shared__ Joined cell[kMostWalkers / 32];
+    const Row<T> w(static_cast<const T *>(p.logits) + blockIdx.x * p.row_stride, p.vocab, blockDim.x);
+    Fetched<T, HELD> fetched(w, shared);
+#pragma unroll
+    for (int i = 0; i < fetched.kAhead; ++i) fetched.ask();
+    const Sample t = sample_of<T, I>(p, w.row);
     const float unit = kLog2e / p.temperature;
-    if constexpr (MODE == kBackward) {
-        const float lse = p.lse_in[blockIdx.x];
-        const float logp = __fsub_rn(t.z / p.temperature, lse);
-        const float slope = t.there() ? value_of(p, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
-        const float weight = __fdiv_rn(__fmul_rn(p.grad_loss[blockIdx.x], slope), p.temperature);
-        __syncthreads();                              // every thread has the token's logit: the gradient may be written over it
-        put_row<kAhead>(p, w, t, Softmax<false>{1.0f / p.temperature, lse == -INFINITY ? 0.0f : -lse, kLog2e, -weight}, weight);
-    } else {
-        reduce_row<false, kAhead>(w, unit, cell);
-        __syncthreads();
-        const Joined all = join_cells<false>(cell, w.walkers / 32, unit);     // every warp finds the same
-        if (!(fabsf(all.m) < kFar)) {
-            far_row<T, MODE>(p, w, t, cell);
-            return;
-        }
-        const float log_sum = log2f(all.s);
-        // the token's exponent less the maximum first: what is added up is all distances
-        const float logp = __fmul_rn(__fsub_rn(__fmaf_rn(t.z, unit, -all.m), log_sum), kLn2);
-        const float weight = finish(p, t, __fmul_rn(__fadd_rn(all.m, log_sum), kLn2), logp, MODE == kStep);
-        if constexpr (MODE == kStep) put_row<kAhead>(p, w, t, Softmax<true>{unit, -all.m, 1.0f, -weight / all.s}, weight);
+    reduce_fetched(fetched, unit, cell);
+    __syncthreads();
+    const Joined all = join_cells<false>(cell, w.walkers / 32, unit);         // every warp finds the same
+    if (!(fabsf(all.m) < kFar)) {
+        far_row<T, STEP ? kStep : kForward>(p, w, t, cell);
+        return;
+    }
+    const float log_sum = log2f(all.s);
+    // the token's exponent less the maximum first: what is added up is all distances
+    const float logp = __fmul_rn(__fsub_rn(__fmaf_rn(t.z, unit, -all.m), log_sum), kLn2);
+    const float weight = finish(p, t, __fmul_rn(__fadd_rn(all.m, log_sum), kLn2), logp, STEP);
+    if constexpr (STEP) {
+        const Softmax<true> q{unit, -all.m, 1.0f, -weight / all.s};
+        if constexpr (HELD) put_row<2>(p, fetched, w, t, q, weight);
+        else put_row<sizeof(T) == 2 ? 4 : 2>(p, w, w, t, q, weight);
     }
 }
 
@@ -173,11 +262,19 @@ int check_policy(const omni_policy *d, bool valued)
 
 template <typename T, typename I> int enqueue(omni_ctx *ctx, int mode, const PolicyParams &p, unsigned rows, cudaStream_t s)
 {
+    const int most = mode == kBackward ? kWalkers : kMostWalkers;
     int walkers = 64;
-    while (walkers < kMostWalkers && walkers * 8 * kGroup < p.vocab) walkers *= 2;
-    if (mode == kForward) policy_kernel<T, I, kForward><<<rows, walkers, 0, s>>>(p);
-    else if (mode == kBackward) policy_kernel<T, I, kBackward><<<rows, walkers, 0, s>>>(p);
-    else policy_kernel<T, I, kStep><<<rows, walkers, 0, s>>>(p);
+    while (walkers < most && walkers * 8 * kGroup < p.vocab) walkers *= 2;
+    if (mode == kBackward) {
+        policy_backward_kernel<T, I><<<rows, walkers, 0, s>>>(p);
+        return context_launched(ctx, int(cudaGetLastError()));
+    }
+    const bool held = mode == kStep && Fetched<T, true>::bytes(p.vocab, walkers) <= size_t(kMostHeld);
+    const size_t bytes = held ? Fetched<T, true>::bytes(p.vocab, walkers) : Fetched<T, false>::bytes(p.vocab, walkers);
+    void (*const kernel)(PolicyParams) = mode == kForward ? policy_kernel<T, I, false, false> : held ? policy_kernel<T, I, true, true> : policy_kernel<T, I, true, false>;
+    const int rc = bytes > 40 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMostHeld) : OMNI_OK;
+    if (rc != OMNI_OK) return rc;
+    kernel<<<rows, walkers, bytes, s>>>(p);
     return context_launched(ctx, int(cudaGetLastError()));
 }
 

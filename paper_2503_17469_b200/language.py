@@ -17,6 +17,7 @@ enqueued; what the library refuses raises ``OmniError``.
 from __future__ import annotations
 
 import ctypes as C
+from array import array
 from typing import Optional
 
 import torch
@@ -26,7 +27,7 @@ from . import binding as B
 _DTYPES = {torch.float32: B.F32, torch.bfloat16: B.BF16}
 _INDEX = {torch.int32: B.I32, torch.int64: B.I64}
 _like, _float, _bf16, _byte = torch.empty_like, torch.float32, torch.bfloat16, torch.uint8
-_size, _contiguous, _where, _address = torch.Tensor.size, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr
+_numel, _contiguous, _where, _address = torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr
 _ref = C.byref
 
 
@@ -338,7 +339,7 @@ class Rotary(_Operator):
     ``frequencies``: radians per position of each rotated pair (``Rotary.geometric`` gives the usual ones), at most dim / 2;
     elements behind the pairs are not rotated.  ``axes``: the position axis of each pair, for positions of
     several axes (time, height, width).  ``interleaved``: pairs are neighbours, otherwise element i and i + pairs.  Any strides with a
-    contiguous last dimension; 16-byte boundaries run faster."""
+    contiguous last dimension; 16-byte boundaries run faster.  Like its context, an object takes one call at a time."""
 
     def __init__(self, ctx: "B.Omni", heads: int, kv_heads: int, dim: int, frequencies, axes=None, interleaved: bool = False,
                  eps: float = 1e-6):
@@ -357,8 +358,12 @@ class Rotary(_Operator):
             raise ValueError("eps is finite and not negative")
         self.heads, self.kv_heads, self.dim, self.interleaved, self.eps = heads, kv_heads, dim, interleaved, eps
         self.frequencies, self.axes = frequencies, max(axes) + 1
-        self._frequency = (C.c_double * len(frequencies))(*frequencies)
-        self._axis = (C.c_int32 * len(axes))(*axes)
+        self._tables = ((C.c_double * len(frequencies))(*frequencies), (C.c_int32 * len(axes))(*axes))
+        # What a call passes, made once and filled at each call: its fields' cost is most of a single token's.
+        self._call = B.omni_rotary(0, 0, heads, kv_heads, dim, len(frequencies), self.axes, interleaved, 0, 0, 0, eps, *self._tables)
+        self._call_ref = _ref(self._call)
+        self._views = [B.omni_attn_view() for _ in range(6)]
+        self._view_refs = [_ref(v) for v in self._views]
 
     @staticmethod
     def geometric(pairs: int, base: float = 10000.0):
@@ -366,7 +371,7 @@ class Rotary(_Operator):
         return [base ** (-i / pairs) for i in range(pairs)]
 
     def _describe(self, q, k, positions, q_weight, k_weight, lengths):
-        """(sizes, shape of the queries, shape of the keys) of a call."""
+        """Fills the call's sizes; (shape of the queries, shape of the keys, dtype, device)."""
         if q.dim() != 4 or k.dim() != 4:
             raise ValueError("q and k: [batch, length, head, dim] is wanted")
         batch, length = q.shape[:2]
@@ -393,20 +398,25 @@ class Rotary(_Operator):
         if lengths is not None and (lengths.dtype != torch.int32 or not lengths.is_contiguous() or lengths.shape != (batch,)
                                     or lengths.get_device() != device):
             raise ValueError("lengths: contiguous int32 [batch] on the tensors' device is wanted")
-        r = B.omni_rotary(batch, length, self.heads, self.kv_heads, self.dim, len(self.frequencies), self.axes, self.interleaved,
-                          _code(q, _DTYPES, "q"), weight, _code(positions, _INDEX, "positions"), self.eps, self._frequency, self._axis,
-                          positions.data_ptr(), axis, *strides, *at, None if lengths is None else lengths.data_ptr())
-        return r, (batch, length, self.heads, self.dim), (batch, length, self.kv_heads, self.dim)
+        r = self._call
+        r.batch, r.length = batch, length
+        r.dtype, r.weight_dtype, r.position_type = _code(q, _DTYPES, "q"), weight, _code(positions, _INDEX, "positions")
+        r.positions, r.position_axis = positions.data_ptr(), axis
+        r.position_batch, r.position_row = strides
+        r.q_weight, r.k_weight = at
+        r.lengths = None if lengths is None else lengths.data_ptr()
+        return (batch, length, self.heads, self.dim), (batch, length, self.kv_heads, self.dim), q.dtype, device
 
-    @staticmethod
-    def _view(t, what: str, shape, q):
-        if t.dtype != q.dtype:
-            raise TypeError(f"{what}: dtype {t.dtype} is not that of q, {q.dtype}")
-        if t.shape != shape or t.stride(3) != 1 or t.get_device() != q.get_device():
+    def _view(self, i: int, t, what: str, shape, dtype, device: int):
+        if t.dtype is not dtype:
+            raise TypeError(f"{what}: dtype {t.dtype} is not that of q, {dtype}")
+        v = self._views[i]
+        if t.shape != shape or t.get_device() != device or t.stride(3) != 1:
             raise ValueError(f"{what}: shape {shape} with a contiguous last dimension on the current device is wanted, "
                              f"got {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
-        batch, row, head, _ = t.stride()
-        return _ref(B.omni_attn_view(t.data_ptr(), batch, row, head))
+        v.data = t.data_ptr()
+        v.batch, v.row, v.head, _ = t.stride()
+        return self._view_refs[i]
 
     def forward(self, q, k, positions, q_weight=None, k_weight=None, lengths=None, out=None, stream=None):
         """Returns normed and rotated (q, k); into ``out``, a tuple of two, if given (q and k themselves, or places in a cache).
@@ -415,12 +425,12 @@ class Rotary(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.forward(q, k, positions, q_weight, k_weight, lengths, out)
-        r, rows, keys = self._describe(q, k, positions, q_weight, k_weight, lengths)
+        rows, keys, dtype, device = self._describe(q, k, positions, q_weight, k_weight, lengths)
         view = self._view
         out_q, out_k = (_like(q), _like(k)) if out is None else out
         self._check(self._lib.omni_rotary_forward(
-            self.ctx._h, _ref(r), view(q, "q", rows, q), view(k, "k", keys, q), view(out_q, "out[0]", rows, q),
-            view(out_k, "out[1]", keys, q), _raw_stream(q.get_device())))
+            self.ctx._h, self._call_ref, view(0, q, "q", rows, dtype, device), view(1, k, "k", keys, dtype, device),
+            view(2, out_q, "out[0]", rows, dtype, device), view(3, out_k, "out[1]", keys, dtype, device), _raw_stream(device)))
         return out_q, out_k
 
     def backward(self, q, k, positions, grad_q, grad_k, q_weight=None, k_weight=None, lengths=None, grads=None, dtype=torch.float32,
@@ -431,7 +441,7 @@ class Rotary(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.backward(q, k, positions, grad_q, grad_k, q_weight, k_weight, lengths, grads, dtype, weight_grads)
-        r, rows, keys = self._describe(q, k, positions, q_weight, k_weight, lengths)
+        rows, keys, kind, device = self._describe(q, k, positions, q_weight, k_weight, lengths)
         view = self._view
         dq, dk = (_like(q), _like(k)) if grads is None else grads
         if q_weight is None:
@@ -441,19 +451,20 @@ class Rotary(_Operator):
             dqw, dkw = (q_weight.new_empty(self.dim, dtype=dtype) for _ in range(2)) if weight_grads is None else weight_grads
             code = _code(dqw, _DTYPES, "weight_grads")
             for w in (dqw, dkw):
-                if w.shape != (self.dim,) or not w.is_contiguous() or w.dtype != dqw.dtype or w.get_device() != q.get_device():
+                if w.shape != (self.dim,) or not w.is_contiguous() or w.dtype != dqw.dtype or w.get_device() != device:
                     raise ValueError("weight_grads: contiguous [dim] of one dtype on the current device is wanted")
             size = self._sizes.get(0)
             if size is None:
                 need = C.c_uint64()
-                self._check(self._lib.omni_rotary_workspace(_ref(r), _ref(need)))
+                self._check(self._lib.omni_rotary_workspace(self._call_ref, _ref(need)))
                 size = self._sizes[0] = need.value
             scratch = q.new_empty(size, dtype=_byte)
             at = (dqw.data_ptr(), dkw.data_ptr(), scratch.data_ptr())
         self._check(self._lib.omni_rotary_backward(
-            self.ctx._h, _ref(r), view(q, "q", rows, q), view(k, "k", keys, q), view(grad_q, "grad_q", rows, q),
-            view(grad_k, "grad_k", keys, q), view(dq, "grads[0]", rows, q), view(dk, "grads[1]", keys, q), at[0], at[1], code, at[2], size,
-            _raw_stream(q.get_device())))
+            self.ctx._h, self._call_ref, view(0, q, "q", rows, kind, device), view(1, k, "k", keys, kind, device),
+            view(2, grad_q, "grad_q", rows, kind, device), view(3, grad_k, "grad_k", keys, kind, device),
+            view(4, dq, "grads[0]", rows, kind, device), view(5, dk, "grads[1]", keys, kind, device), at[0], at[1], code, at[2], size,
+            _raw_stream(device)))
         return dq, dk, dqw, dkw
 
 
@@ -577,7 +588,7 @@ class AdamW(_Operator):
         dtype = grads[0][0].dtype if grads else _float
         code = B.F32 if not grads else _code(grads[0][0], _DTYPES, "grads")
         moments = (_float, _float) if bits == 32 else (_byte, _byte, torch.int16)
-        array = (B.omni_adamw_tensor * max(1, len(params)))()
+        described = (B.omni_adamw_tensor * max(1, len(params)))()
         self._tables = []
         for i, (p, gs, c, s) in enumerate(zip(params, grads, copies, self.state)):
             n, shape = p.numel(), p.shape
@@ -596,18 +607,18 @@ class AdamW(_Operator):
                     raise _elsewhere(**{what: t})
             table = (C.c_void_p * self.K)(*(g.data_ptr() for g in gs))
             self._tables.append(table)
-            array[i] = B.omni_adamw_tensor(p.data_ptr(), None if c is None else c.data_ptr(), table, s[0].data_ptr(), s[1].data_ptr(),
-                                           s[2].data_ptr() if bits == 8 else None, n, decay[i])
+            described[i] = B.omni_adamw_tensor(p.data_ptr(), None if c is None else c.data_ptr(), table, s[0].data_ptr(), s[1].data_ptr(),
+                                               s[2].data_ptr() if bits == 8 else None, n, decay[i])
         self._keep = (params, grads, copies)
         self.betas, self.eps, self.bits, self.steps = (float(betas[0]), float(betas[1])), float(eps), bits, int(steps)
         need = C.c_uint64()
-        self._check(self._lib.omni_adamw_plan_bytes(array, len(params), self.K, code, bits, _ref(need)))
+        self._check(self._lib.omni_adamw_plan_bytes(described, len(params), self.K, code, bits, _ref(need)))
         host = torch.empty(need.value, dtype=_byte)
-        self._check(self._lib.omni_adamw_plan(array, len(params), self.K, code, bits, host.data_ptr(), need.value))
+        self._check(self._lib.omni_adamw_plan(described, len(params), self.K, code, bits, host.data_ptr(), need.value))
         self._record = host
         self._record_dev = host.to(f"cuda:{self._at}")
         self._batches = C.c_int32 * self.K
-        self._shapes, self._pointers = [p.shape for p in params], C.c_void_p * max(1, len(params))
+        self._numels, self._pointers = [p.numel() for p in params], C.c_void_p * max(1, len(params))
 
     @staticmethod
     def _zeros(p, bits):
@@ -652,14 +663,13 @@ class AdamW(_Operator):
             raise ValueError("out: moments of 32 bits are the state itself")
         if out is None:
             out = [tuple(torch.empty(s[0].shape, dtype=_float, device=s[0].device) for _ in range(2)) for s in self.state]
-        if len(out) != len(self.state) or any(len(pair) != 2 for pair in out):
-            raise ValueError("out: a pair for each tensor is wanted")
         # many short tensors: by functions that run over all of them, not tensor by tensor
+        m, v = tuple(zip(*out)) or ((), ())
         tables = []
-        for values in zip(*out) if out else ((), ()):
-            if list(map(_size, values)) != self._shapes or not all(map(_contiguous, values)) or any(t.dtype is not _float for t in values) \
-                    or any(map(self._at.__ne__, map(_where, values))):
-                raise ValueError("out: contiguous float32 pairs of the tensors' shapes on the current device are wanted")
-            tables.append(self._pointers(*map(_address, values)))
+        for t in (m, v):
+            if list(map(_numel, t)) != self._numels or not all(map(_contiguous, t)) or not {x.dtype for x in t} <= {_float} \
+                    or not set(map(_where, t)) <= {self._at}:
+                raise ValueError("out: for each tensor a pair of contiguous float32 tensors of its size on the current device is wanted")
+            tables.append(self._pointers.from_buffer(array("Q", map(_address, t) if t else (0,))))
         self._check(self._lib.omni_adamw_moments(self.ctx._h, self._record.data_ptr(), self._record_dev.data_ptr(), *tables, _raw_stream(self._at)))
         return out
