@@ -12,8 +12,7 @@
 namespace omni {
 namespace {
 
-constexpr int kWalkers = 256, kMostWalkers = 512;     // threads of a row: backward; forward and step
-constexpr int kMostHeld = 112 * 1024;                 // bytes of a row that is held: two rows an SM
+constexpr int kFewestWalkers = 32, kMostWalkers = 512; // threads of a row
 enum Mode { kForward = 0, kBackward = 1, kStep = 2 };
 
 struct PolicyParams {
@@ -28,26 +27,27 @@ struct PolicyParams {
     float low, high, kl, temperature;                 // low, high: borders of the ratio
 };
 
-// A row's scalars, the same in every thread.
+// A row's scalars, the same in every thread; asked for before the walk.
 struct Sample {
     int token;                                        // -1: none
     float z;                                          // its logit
+    float old, advantage, reference, grad_loss;       // what is given of them
     __device__ __forceinline__ bool there() const { return token >= 0; }
 };
-template <typename T, typename I> __device__ __forceinline__ Sample sample_of(const PolicyParams &p, const T *row)
+template <typename T, typename I> __device__ __forceinline__ Sample sample_of(const PolicyParams &p, const T *row, unsigned r, bool weighed)
 {
-    const long long t = load_index<I>(p.tokens, blockIdx.x);
+    const long long t = load_index<I>(p.tokens, r);
     const bool there = t >= 0 && t < p.vocab;
-    return {there ? int(t) : -1, there ? to_float(row[t]) : 0.0f};
+    return {there ? int(t) : -1, there ? to_float(row[t]) : 0.0f, p.old ? p.old[r] : 0.0f, p.old ? p.advantage[r] : 0.0f,
+            p.kl != 0.0f ? p.reference[r] : 0.0f, weighed ? p.grad_loss[r] : 0.0f};
 }
 
 struct Value { float loss, slope; };
 // The loss of a row with a token and its derivative by logp.  On a border of the ratio the surrogate counts as not clipped; an advantage
 // of zero takes no part, whatever the ratio.
-__device__ __forceinline__ Value value_of(const PolicyParams &p, float logp)
+__device__ __forceinline__ Value value_of(const PolicyParams &p, const Sample &t, float logp)
 {
-    const float a = p.advantage[blockIdx.x];
-    const float ratio = expf(__fsub_rn(logp, p.old[blockIdx.x]));
+    const float a = t.advantage, ratio = expf(__fsub_rn(logp, t.old));
     Value v = {0.0f, 0.0f};
     if (a != 0.0f) {
         const float gain = __fmul_rn(ratio, a), clipped = __fmul_rn(fminf(fmaxf(ratio, p.low), p.high), a);
@@ -56,130 +56,145 @@ __device__ __forceinline__ Value value_of(const PolicyParams &p, float logp)
         v.slope = taken ? -gain : other ? 0.0f : gain + clipped;
     }
     if (p.kl != 0.0f) {
-        const float gap = __fsub_rn(p.reference[blockIdx.x], logp), away = expm1f(gap);
+        const float gap = __fsub_rn(t.reference, logp), away = expm1f(gap);
         v.loss = __fmaf_rn(p.kl, __fsub_rn(away, fminf(gap, 3.4e38f)), v.loss);     // infinite for an infinite gap, not inf - inf
         v.slope = __fmaf_rn(-p.kl, away, v.slope);
     }
     return v;
 }
 
-// A row's groups as its threads fetch them ahead, each thread those that it walks: two groups to a step, 64 to 128 bytes in flight.
-// With HELD every group has a place of its own, and the second walk finds the row in shared memory; otherwise a few places go round.
-template <typename T, bool HELD> struct Fetched {
-    static constexpr int kStep = 2, kAhead = sizeof(T) == 2 ? 4 : 2;
-    const Row<T> &w;
-    char *const at;
-    int own, fetched = 0;                             // groups of this thread, groups asked for
-    __device__ __forceinline__ Fetched(const Row<T> &row, char *shared)
-        : w(row), at(shared), own((row.parts.groups - int(threadIdx.x) + row.walkers - 1) / row.walkers) {}
-    static __host__ __device__ size_t bytes(int vocab, int walkers)
-    {
-        return HELD ? size_t(vocab / kGroup) * kGroup * sizeof(T) : size_t(kStep * kAhead) * walkers * kGroup * sizeof(T);
-    }
-    __device__ __forceinline__ char *place(int i) const
-    {
-        return at + size_t(((HELD ? i : i % (kStep * kAhead)) * w.walkers + threadIdx.x)) * (kGroup * sizeof(T));
-    }
-    __device__ __forceinline__ void ask()
+// What a thread walks of a row: groups threadIdx.x, + walkers, ... and at most one element outside them.
+template <typename T> __device__ __forceinline__ int own_groups(const Row<T> &w)
+{
+    return (w.parts.groups - int(threadIdx.x) + w.walkers - 1) / w.walkers;
+}
+
+// Groups as the threads fetch them ahead, each thread its own, kStep of them to a step, into places of 16 or 32 bytes side by side.
+template <typename T> struct Places {
+    static constexpr int kSize = kGroup * int(sizeof(T)), kStep = 2;
+    char *at;
+    __device__ __forceinline__ char *place(int i, int walkers) const { return at + (i * walkers + int(threadIdx.x)) * kSize; }
+    // groups i .. i + kStep - 1 of the thread into the places from `to` on
+    __device__ __forceinline__ void ask(const Row<T> &w, int own, int i, int to) const
     {
 #pragma unroll
-        for (int i = 0; i < kStep; ++i, ++fetched) {
-            if (fetched >= own) continue;
-            const char *from = reinterpret_cast<const char *>(w.row + w.parts.head + (long long)(threadIdx.x + fetched * w.walkers) * kGroup);
-            const uint32_t to = uint32_t(__cvta_generic_to_shared(place(fetched)));
+        for (int k = 0; k < kStep; ++k) {
+            if (i + k >= own) break;
+            const char *from = reinterpret_cast<const char *>(w.row + w.parts.head + (long long)(threadIdx.x + (i + k) * w.walkers) * kGroup);
+            const uint32_t into = uint32_t(__cvta_generic_to_shared(place(to + k, w.walkers)));
 #pragma unroll
-            for (int piece = 0; piece < int(kGroup * sizeof(T)) / 16; ++piece)
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + piece * 16), "l"(from + piece * 16) : "memory");
+            for (int piece = 0; piece < kSize / 16; ++piece)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(into + piece * 16), "l"(from + piece * 16) : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    __device__ __forceinline__ Group<T> group(int i) const { return *reinterpret_cast<const Group<T> *>(place(i)); }
+    __device__ __forceinline__ Group<T> group(int i, int walkers) const { return *reinterpret_cast<const Group<T> *>(place(i, walkers)); }
 };
+template <int LEFT> __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// The walkers' maxima and sums into their warps' cells, over groups that are fetched ahead.
-template <typename T, bool HELD> __device__ __forceinline__ void reduce_fetched(Fetched<T, HELD> &f, float unit, Joined *cell)
+// Takes groups i .. of the thread from their places.
+template <typename T> __device__ __forceinline__ void take_step(Running<false> &run, const Places<T> &at, int i, int own, int from, int walkers, float unit)
 {
-    constexpr int kStep = f.kStep, kAhead = f.kAhead;
-    Running<false> run;
-    if (f.w.edge() >= 0) run.take_one(to_float(f.w.row[f.w.edge()]), unit);
-    for (int i = 0; i < f.own; i += kStep) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-        if (i + kStep <= f.own) {
-            Group<T> x[kStep];
+    constexpr int kStep = Places<T>::kStep;
+    if (i + kStep <= own) {
+        Group<T> x[kStep];
 #pragma unroll
-            for (int k = 0; k < kStep; ++k) x[k] = f.group(i + k);
-            run.take(x, unit);
-        } else {
-            for (int k = i; k < f.own; ++k) {
-                Group<T> x[1] = {f.group(k)};
-                run.take(x, unit);
-            }
-        }
-        f.ask();
+        for (int k = 0; k < kStep; ++k) x[k] = at.group(from + k, walkers);
+        run.take(x, unit);
+    } else if (i < own) {
+        Group<T> x[1] = {at.group(from, walkers)};
+        run.take(x, unit);
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    __syncwarp();
-    put_warp(run, unit, cell + threadIdx.x / 32);
 }
 
-// f(first group, groups) over the groups of a thread that are held, as walk() over those in memory.
-template <int AHEAD, typename T, bool HELD, typename F> __device__ __forceinline__ void walk(const Fetched<T, HELD> &held, F f)
+// The thread that writes a token's element of a gradient that is written in groups, and what it writes there.
+template <typename T> __device__ __forceinline__ int owner_of(const Row<T> &w, int token)
 {
-    int i = 0;
-    for (; i + AHEAD <= held.own; i += AHEAD) {
+    const int in = token - w.parts.head, grouped = w.parts.groups * kGroup;
+    return in >= 0 && in < grouped ? in / kGroup % w.walkers : in < 0 ? token : token - grouped;
+}
+__device__ __forceinline__ float at_token(float weight, float q) { return __fadd_rn(weight, q); }
+
+// A walk over a row that nothing reads again: its lines are the first to leave L2, so that rows that others are in the middle of stay.
+__device__ __forceinline__ void load_last(uint4 &x, const void *p)
+{
+    unsigned long long policy;
+    asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+    asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+                 : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p), "l"(policy) : "memory");
+}
+template <typename T> __device__ __forceinline__ Group<T> last_group(const T *p)
+{
+    union { uint4 u[sizeof(Group<T>) / 16]; Group<T> g; } x;
+#pragma unroll
+    for (int i = 0; i < int(sizeof(Group<T>) / 16); ++i) load_last(x.u[i], reinterpret_cast<const char *>(p) + 16 * i);
+    return x.g;
+}
+template <int AHEAD, typename T, typename F> __device__ __forceinline__ void walk_last(const Row<T> &w, F f)
+{
+    const T *const first = w.row + w.parts.head;
+    int g = threadIdx.x;
+    for (; g + (AHEAD - 1) * w.walkers < w.parts.groups; g += w.walkers * AHEAD) {
         Group<T> x[AHEAD];
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) x[a] = held.group(i + a);
-        f(int(threadIdx.x) + i * held.w.walkers, x);
+        for (int a = 0; a < AHEAD; ++a) x[a] = last_group(first + (long long)(g + a * w.walkers) * kGroup);
+        f(g, x);
     }
-    for (; i < held.own; ++i) {
-        Group<T> x[1] = {held.group(i)};
-        f(int(threadIdx.x) + i * held.w.walkers, x);
+    for (; g < w.parts.groups; g += w.walkers) {
+        Group<T> x[1] = {last_group(first + (long long)g * kGroup)};
+        f(g, x);
     }
 }
 
-// The gradient of the row, by the whole CTA, from the groups of `walked` (the row itself, or what is held of it).  q(z) is -weight times
-// the probability of a token with logit z.
-template <int AHEAD, typename W, typename T, bool NEAR>
-__device__ __forceinline__ void put_row(const PolicyParams &p, const W &walked, const Row<T> &w, const Sample &t, const Softmax<NEAR> &q, float weight)
+// A row of zeros.
+template <typename T> __device__ __forceinline__ void put_zeros(T *out, int vocab, int walkers)
 {
-    T *out = static_cast<T *>(p.grad) + blockIdx.x * p.grad_stride;
+    const Parts<T> parts(out, vocab);
+    const float zeros[kGroup] = {};
+    for (int g = threadIdx.x; g < parts.groups; g += walkers) store_streaming(out + parts.head + (long long)g * kGroup, zeros);
+    if (int(threadIdx.x) < vocab - parts.groups * kGroup) out[parts.edge(threadIdx.x)] = from_float<T>(0.0f);
+}
+
+// The gradient of a row from memory, by the whole CTA.  q(z) is -weight times the probability of a token with logit z.
+template <int AHEAD, typename T, bool NEAR>
+__device__ __forceinline__ void put_row(const PolicyParams &p, T *out, const Row<T> &w, const Sample &t, const Softmax<NEAR> &q, float weight)
+{
     const int tid = threadIdx.x, walkers = w.walkers;
     if (!t.there() || weight == 0.0f) {
-        const Parts<T> parts(out, p.vocab);
-        const float zeros[kGroup] = {};
-        for (int g = tid; g < parts.groups; g += walkers) store_streaming(out + parts.head + (long long)g * kGroup, zeros);
-        if (tid < p.vocab - parts.groups * kGroup) out[parts.edge(tid)] = from_float<T>(0.0f);
+        put_zeros(out, p.vocab, walkers);
         return;
     }
+    int owner = t.token % walkers;
     if (same_phase(out, w.row)) {
-        walk<AHEAD>(walked, [&](int g, const auto &x) {
+        walk_last<AHEAD>(w, [&](int g, const auto &x) {
 #pragma unroll
             for (int a = 0; a < int(sizeof x / sizeof x[0]); ++a)
                 put_group(out + w.parts.head + (long long)(g + a * walkers) * kGroup, x[a], q);
         });
         if (w.edge() >= 0) out[w.edge()] = from_float<T>(q(to_float(w.row[w.edge()])));
+        owner = owner_of(w, t.token);
     } else {
         for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(q(to_float(w.row[v])));
     }
-    __syncthreads();
-    if (tid == 0) out[t.token] = from_float<T>(__fadd_rn(weight, q(t.z)));
+    if (tid == owner) out[t.token] = from_float<T>(at_token(weight, q(t.z)));     // over what the same thread wrote
 }
 
-// What follows from a row's log-sum-exp and its token's log-probability.
-__device__ __forceinline__ float finish(const PolicyParams &p, const Sample &t, float lse, float logp, bool step)
+// What follows from a row's log-sum-exp and its token's log-probability: the results, and the weight of the gradient.
+template <bool STEP> __device__ __forceinline__ float finish(const PolicyParams &p, unsigned r, const Sample &t, float lse, float logp)
 {
-    const Value v = t.there() && (step || p.loss) ? value_of(p, logp) : Value{0.0f, 0.0f};
+    const Value v = t.there() && (STEP || p.loss) ? value_of(p, t, logp) : Value{0.0f, 0.0f};
     if (threadIdx.x == 0) {
-        p.lse_out[blockIdx.x] = lse;
-        p.logp[blockIdx.x] = t.there() ? logp : 0.0f;
-        if (p.loss) p.loss[blockIdx.x] = v.loss;
+        p.lse_out[r] = lse;
+        p.logp[r] = t.there() ? logp : 0.0f;
+        if (p.loss) p.loss[r] = v.loss;
     }
-    return step ? __fdiv_rn(__fmul_rn(p.grad_loss[blockIdx.x], v.slope), p.temperature) : 0.0f;
+    return STEP ? __fdiv_rn(__fmul_rn(t.grad_loss, v.slope), p.temperature) : 0.0f;
 }
+
+template <typename T> __device__ __forceinline__ T *gradient_of(const PolicyParams &p, unsigned r) { return static_cast<T *>(p.grad) + r * p.grad_stride; }
 
 // A row far from zero from its start, by the whole CTA.
-template <typename T, int MODE> __device__ __forceinline__ void far_row(const PolicyParams &p, const Row<T> &w, const Sample &t, Joined *cell)
+template <typename T, bool STEP> __device__ __forceinline__ void far_row(const PolicyParams &p, unsigned r, const Row<T> &w, const Sample &t, Joined *cell)
 {
     const float unit = kLog2e / p.temperature;
     __syncthreads();                                  // the cells have been read
@@ -189,52 +204,69 @@ template <typename T, int MODE> __device__ __forceinline__ void far_row(const Po
     const bool nothing = all.m == -INFINITY && all.s == 0.0f;           // a row of -inf: no token has a probability
     const float log_sum = __fmul_rn(log2f(all.s), kLn2);
     const float logp = nothing ? -INFINITY : __fsub_rn(__fsub_rn(t.z, all.m) / p.temperature, log_sum);
-    const float weight = finish(p, t, __fadd_rn(all.m / p.temperature, log_sum), logp, MODE == kStep);
-    if constexpr (MODE == kStep)
-        put_row<1>(p, w, w, t, Softmax<false>{1.0f, Running<true>::reference(all.m), unit, nothing ? 0.0f : -weight / all.s}, weight);
+    const float weight = finish<STEP>(p, r, t, __fadd_rn(all.m / p.temperature, log_sum), logp);
+    if constexpr (STEP)
+        put_row<1>(p, gradient_of<T>(p, r), w, t, Softmax<false>{1.0f, Running<true>::reference(all.m), unit, nothing ? 0.0f : -weight / all.s}, weight);
 }
 
-// From a kept lse: one walk.
-template <typename T, typename I> __global__ void __launch_bounds__(kWalkers, 4) policy_backward_kernel(const __grid_constant__ PolicyParams p)
+// A row near zero: its results; the gradient's softmax and weight.
+struct Ending { Softmax<true> q; float weight; };
+template <bool STEP> __device__ __forceinline__ Ending near_row(const PolicyParams &p, unsigned r, const Sample &t, const Joined &all, float unit)
 {
-    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;    // groups a thread has in flight
-    const Row<T> w(static_cast<const T *>(p.logits) + blockIdx.x * p.row_stride, p.vocab, blockDim.x);
-    const Sample t = sample_of<T, I>(p, w.row);
-    const float lse = p.lse_in[blockIdx.x];
-    const float logp = __fsub_rn(t.z / p.temperature, lse);
-    const float slope = t.there() ? value_of(p, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
-    const float weight = __fdiv_rn(__fmul_rn(p.grad_loss[blockIdx.x], slope), p.temperature);
-    __syncthreads();                                  // every thread has the token's logit: the gradient may be written over it
-    put_row<kAhead>(p, w, w, t, Softmax<false>{1.0f / p.temperature, lse == -INFINITY ? 0.0f : -lse, kLog2e, -weight}, weight);
-}
-
-template <typename T, typename I, bool STEP, bool HELD>
-__global__ void __launch_bounds__(kMostWalkers, 2) policy_kernel(const __grid_constant__ PolicyParams p)
-{
-    extern __shared__ __align__(16) char shared[];
-    __shared__ Joined cell[kMostWalkers / 32];
-    const Row<T> w(static_cast<const T *>(p.logits) + blockIdx.x * p.row_stride, p.vocab, blockDim.x);
-    Fetched<T, HELD> fetched(w, shared);
-#pragma unroll
-    for (int i = 0; i < fetched.kAhead; ++i) fetched.ask();
-    const Sample t = sample_of<T, I>(p, w.row);
-    const float unit = kLog2e / p.temperature;
-    reduce_fetched(fetched, unit, cell);
-    __syncthreads();
-    const Joined all = join_cells<false>(cell, w.walkers / 32, unit);         // every warp finds the same
-    if (!(fabsf(all.m) < kFar)) {
-        far_row<T, STEP ? kStep : kForward>(p, w, t, cell);
-        return;
-    }
     const float log_sum = log2f(all.s);
     // the token's exponent less the maximum first: what is added up is all distances
     const float logp = __fmul_rn(__fsub_rn(__fmaf_rn(t.z, unit, -all.m), log_sum), kLn2);
-    const float weight = finish(p, t, __fmul_rn(__fadd_rn(all.m, log_sum), kLn2), logp, STEP);
-    if constexpr (STEP) {
-        const Softmax<true> q{unit, -all.m, 1.0f, -weight / all.s};
-        if constexpr (HELD) put_row<2>(p, fetched, w, t, q, weight);
-        else put_row<sizeof(T) == 2 ? 4 : 2>(p, w, w, t, q, weight);
+    const float weight = finish<STEP>(p, r, t, __fmul_rn(__fadd_rn(all.m, log_sum), kLn2), logp);
+    return {{unit, -all.m, 1.0f, -weight / all.s}, weight};
+}
+
+// From a kept lse: one walk.
+template <typename T, typename I> __global__ void __launch_bounds__(kMostWalkers, 2) policy_backward_kernel(const __grid_constant__ PolicyParams p)
+{
+    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;    // groups a thread has in flight
+    const unsigned r = blockIdx.x;
+    const Row<T> w(static_cast<const T *>(p.logits) + r * p.row_stride, p.vocab, blockDim.x);
+    const Sample t = sample_of<T, I>(p, w.row, r, true);
+    const float lse = p.lse_in[r];
+    const float logp = __fsub_rn(t.z / p.temperature, lse);
+    const float slope = t.there() ? value_of(p, t, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
+    const float weight = __fdiv_rn(__fmul_rn(t.grad_loss, slope), p.temperature);
+    __syncthreads();                                  // every thread has the token's logit: the gradient may be written over it
+    put_row<kAhead>(p, gradient_of<T>(p, r), w, t, Softmax<false>{1.0f / p.temperature, lse == -INFINITY ? 0.0f : -lse, kLog2e, -weight}, weight);
+}
+
+// A CTA a row; a few places go round.  The gradient of a step finds the row in L2.
+template <typename T> constexpr int kRound = sizeof(T) == 2 ? 8 : 4;       // places of a thread
+template <typename T, typename I, bool STEP> __global__ void __launch_bounds__(kMostWalkers, 2) policy_kernel(const __grid_constant__ PolicyParams p)
+{
+    extern __shared__ __align__(16) char shared[];
+    __shared__ Joined cell[kMostWalkers / 32];
+    constexpr int kStep = Places<T>::kStep, kSteps = kRound<T> / kStep;
+    const unsigned r = blockIdx.x;
+    const Row<T> w(static_cast<const T *>(p.logits) + r * p.row_stride, p.vocab, blockDim.x);
+    const Places<T> at{shared};
+    const int own = own_groups(w);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) at.ask(w, own, i * kStep, i * kStep);
+    const Sample t = sample_of<T, I>(p, w.row, r, STEP);
+    const float unit = kLog2e / p.temperature;
+    Running<false> run;
+    if (w.edge() >= 0) run.take_one(to_float(w.row[w.edge()]), unit);
+    for (int i = 0; i < own; i += kStep) {
+        arrived<kSteps - 1>();
+        take_step(run, at, i, own, i % kRound<T>, w.walkers, unit);
+        at.ask(w, own, i + kRound<T>, i % kRound<T>);
     }
+    __syncwarp();
+    put_warp(run, unit, cell + threadIdx.x / 32);
+    __syncthreads();
+    const Joined all = join_cells<false>(cell, w.walkers / 32, unit);         // every warp finds the same
+    if (!(fabsf(all.m) < kFar)) {
+        far_row<T, STEP>(p, r, w, t, cell);
+        return;
+    }
+    const Ending end = near_row<STEP>(p, r, t, all, unit);
+    if constexpr (STEP) put_row<sizeof(T) == 2 ? 4 : 2>(p, gradient_of<T>(p, r), w, t, end.q, end.weight);
 }
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -262,17 +294,18 @@ int check_policy(const omni_policy *d, bool valued)
 
 template <typename T, typename I> int enqueue(omni_ctx *ctx, int mode, const PolicyParams &p, unsigned rows, cudaStream_t s)
 {
-    const int most = mode == kBackward ? kWalkers : kMostWalkers;
-    int walkers = 64;
-    while (walkers < most && walkers * 8 * kGroup < p.vocab) walkers *= 2;
+    // About fifteen pieces of 16 bytes for each thread of a row, whatever the direction and the number of rows: sums have the same order, and
+    // the log-probabilities of a step are those of an earlier call bit for bit.
+    int walkers = kFewestWalkers;
+    while (walkers < kMostWalkers && size_t(walkers) * 480 <= size_t(p.vocab) * sizeof(T)) walkers *= 2;
     if (mode == kBackward) {
         policy_backward_kernel<T, I><<<rows, walkers, 0, s>>>(p);
         return context_launched(ctx, int(cudaGetLastError()));
     }
-    const bool held = mode == kStep && Fetched<T, true>::bytes(p.vocab, walkers) <= size_t(kMostHeld);
-    const size_t bytes = held ? Fetched<T, true>::bytes(p.vocab, walkers) : Fetched<T, false>::bytes(p.vocab, walkers);
-    void (*const kernel)(PolicyParams) = mode == kForward ? policy_kernel<T, I, false, false> : held ? policy_kernel<T, I, true, true> : policy_kernel<T, I, true, false>;
-    const int rc = bytes > 40 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMostHeld) : OMNI_OK;
+    const size_t bytes = size_t(kRound<T>) * walkers * Places<T>::kSize;
+    void (*const kernel)(PolicyParams) = mode == kStep ? policy_kernel<T, I, true> : policy_kernel<T, I, false>;
+    constexpr int kMost = kRound<T> * kMostWalkers * Places<T>::kSize;
+    const int rc = bytes > 40 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMost) : OMNI_OK;
     if (rc != OMNI_OK) return rc;
     kernel<<<rows, walkers, bytes, s>>>(p);
     return context_launched(ctx, int(cudaGetLastError()));
@@ -305,7 +338,7 @@ int run(omni_ctx *ctx, int mode, bool valued, const omni_policy *d, const float 
     p.row_stride = d->row_stride;
     p.grad_stride = r.grad_stride;
     p.tokens = d->tokens;
-    p.old = d->old;
+    p.old = valued ? d->old : nullptr;                // the log-probabilities alone look at none of these
     p.advantage = d->advantage;
     p.reference = d->reference;
     p.grad_loss = grad_loss;
@@ -317,7 +350,7 @@ int run(omni_ctx *ctx, int mode, bool valued, const omni_policy *d, const float 
     p.vocab = d->vocab;
     p.low = 1.0f - d->clip_low;
     p.high = 1.0f + d->clip_high;
-    p.kl = d->kl;
+    p.kl = valued ? d->kl : 0.0f;
     p.temperature = d->temperature;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const unsigned rows = unsigned(d->rows);
