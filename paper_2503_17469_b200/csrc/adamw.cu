@@ -22,7 +22,7 @@
 namespace omni {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kBlock = OMNI_ADAMW_BLOCK;              // elements with one offset: a warp's, eight a lane
 constexpr int kUnit = kThreads * kGroup;              // elements a CTA has at a time
 static_assert(kBlock == 32 * kGroup, "a warp holds a block");
@@ -127,33 +127,34 @@ template <int MOST> __device__ __forceinline__ void decode8(uint2 c, int top, fl
     decode4<MOST>(c.x, below, f);
     decode4<MOST>(c.y, below, f + 4);
 }
-// The float's top twelve bits less the sign, rounded by 16 random bits at bit 4.  A NaN may come out one too high.
-__device__ __forceinline__ uint32_t rounded(uint32_t bits, uint32_t random) { return random * 16u + bits >> 20; }
-// The low bytes of four words as one.
+// The float's bits less the sign, with 16 random ones added at bit 4: from bit 20 on its rounded top.  A NaN may come out one too high.
+__device__ __forceinline__ uint32_t rounded(uint32_t bits, uint32_t random) { return random * 16u + bits; }
+// The top bytes of four words as one.
 __device__ __forceinline__ uint32_t join4(const uint32_t *c)
 {
-    return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+    return __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
 }
-// Codes of four elements from their rounded tops r <= top, and from the elements themselves (for the signs).
+// Codes of four elements from their rounded bits r, the largest top of the block, and the elements themselves (for the signs).
 template <int MOST> __device__ __forceinline__ uint32_t encode4(const uint32_t *r, int top, const float *x)
 {
     uint32_t c[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        c[i] = uint32_t(__viaddmax_s32(int(r[i]), MOST - top, MOST == 255 ? 1 : 0));
-        if (MOST == 255) c[i] = top >= 255 ? min(c[i], r[i]) : r[i] ? c[i] : 0u;       // zero stays zero
-        else if (top < 127) c[i] = r[i] ? c[i] : 0u;
+        c[i] = uint32_t(__viaddmax_s32(int(r[i]), (MOST - top) * (1 << 20), MOST == 255 ? 1 << 20 : 0));
+        if (top < MOST) c[i] = r[i] >> 20 ? c[i] : 0u;          // zero stays zero
+        else if (MOST == 255) c[i] = min(c[i], r[i]);           // here as well: r is below one step then
+        c[i] *= 16u;                                            // the code is the top byte
     }
     const uint32_t word = join4(c);
     const uint32_t signs = __byte_perm(__byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0073),
                                        __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
     return MOST == 255 ? word : word | (word + 0x7f7f7f7fu & 0x80808080u & signs);           // a code of 0 has no sign
 }
-// Within 2^-22 of the root and of the inverse.
+// Within 2^-22 of the root and of the inverse; numbers below float's normal range count as 0.
 __device__ __forceinline__ float root(float x)
 {
     float y;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ float inverse(float x)
@@ -171,71 +172,152 @@ __device__ __forceinline__ uint32_t scramble(uint32_t x)
     return x ^ x >> 15;
 }
 
-template <typename G, int BITS> __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamParams p)
+// The step's number and what follows from it; with a clock on the device, by one thread of the CTA.
+struct Scales {
+    float rate, spread;
+    uint32_t step;
+};
+__device__ __forceinline__ Scales scales_of(const AdamParams &p)
 {
-    __shared__ float scales[2];
-    __shared__ unsigned long long step_now;
-    float rate = p.rate, spread = p.spread;
-    uint32_t step = p.step;
-    if (p.clock) {
-        if (threadIdx.x == 0) {
-            const long long t = *p.clock;
-            scales[0] = float(p.lr / (1.0 - pow(p.beta1, double(t))));
-            scales[1] = float(1.0 / sqrt(1.0 - pow(p.beta2, double(t))));
-            step_now = (unsigned long long)t;
+    if (!p.clock) return {p.rate, p.spread, p.step};
+    __shared__ Scales now;
+    if (threadIdx.x == 0) {
+        const long long t = *p.clock;
+        now = {float(p.lr / (1.0 - pow(p.beta1, double(t)))), float(1.0 / sqrt(1.0 - pow(p.beta2, double(t)))), uint32_t(t)};
+    }
+    __syncthreads();
+    return now;
+}
+
+// Eight gradients as loaded: what waits for a load stands behind all of them.
+template <typename G> struct Raw;
+template <> struct Raw<float> {
+    float f[kGroup];
+    __device__ __forceinline__ void load(const float *p) { load_group(p, f); }
+    __device__ __forceinline__ void get(float *x) const
+    {
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) x[i] = f[i];
+    }
+};
+template <> struct Raw<__nv_bfloat16> {
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { u = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ void get(float *x) const { widen(u, x); }
+};
+
+// A lane's place in a tensor.
+struct Place {
+    unsigned tensor;
+    unsigned long long at;
+    int count;                                        // of its eight elements before the tensor's end
+    bool block, whole;                                // the warp's block begins before the end; accesses of eight are allowed
+    __device__ __forceinline__ Place(const AdamParams &p, unsigned unit, const Entry *&e) : tensor(p.owners[unit])
+    {
+        e = p.entries + tensor;
+        at = (unsigned long long)(unit - e->first_unit) * kUnit + threadIdx.x * kGroup;
+        count = at >= e->n ? 0 : e->n - at < kGroup ? int(e->n - at) : kGroup;
+        block = at - threadIdx.x % 32 * kGroup < e->n;
+        whole = e->wide && count == kGroup;
+    }
+};
+
+// The weighted gradient, ascending k, loads of four or two workers at a time.
+template <typename G> constexpr int kWorkers = sizeof(G) == 2 ? 4 : 2;
+template <typename G> __device__ __forceinline__ void aggregate(const AdamParams &p, const Place &x, const Raw<G> &first, float *g)
+{
+    const void *const *const grads = p.grads + (unsigned long long)x.tensor * p.K;
+    float f[kGroup];
+    first.get(f);
+#pragma unroll
+    for (int i = 0; i < kGroup; ++i) g[i] = __fmaf_rn(p.lambda[0], f[i], 0.0f);
+    for (int k = 1; k < p.K; k += kWorkers<G>) {
+        Raw<G> raw[kWorkers<G>];
+#pragma unroll
+        for (int j = 0; j < kWorkers<G>; ++j)
+            if (k + j < p.K) raw[j].load(static_cast<const G *>(grads[k + j]) + x.at);
+#pragma unroll
+        for (int j = 0; j < kWorkers<G>; ++j) {
+            if (k + j >= p.K) break;
+            raw[j].get(f);
+#pragma unroll
+            for (int i = 0; i < kGroup; ++i) g[i] = __fmaf_rn(p.lambda[k + j], f[i], g[i]);
         }
-        __syncthreads();
-        rate = scales[0];
-        spread = scales[1];
-        step = uint32_t(step_now);
     }
-    const unsigned unit = blockIdx.x, tensor = p.owners[unit];
-    const Entry &e = p.entries[tensor];
-    const unsigned long long at = (unsigned long long)(unit - e.first_unit) * kUnit + threadIdx.x * kGroup;
-    if (at - threadIdx.x % 32 * kGroup >= e.n) return;                    // the warp's block is behind the end
-    const bool wide = e.wide;
-    const int count = at >= e.n ? 0 : e.n - at < kGroup ? int(e.n - at) : kGroup;
-    float theta[kGroup], m[kGroup], v[kGroup], g[kGroup];
-    load8(e.param + at, wide, count, theta);
-    unsigned char *const cm = static_cast<unsigned char *>(e.m) + at, *const cv = static_cast<unsigned char *>(e.v) + at;
-    float *const fm = static_cast<float *>(e.m) + at, *const fv = static_cast<float *>(e.v) + at;
-    if constexpr (BITS == 32) {
-        load8(fm, wide, count, m);
-        load8(fv, wide, count, v);
-    } else {
-        const uint32_t tops = e.tops[at / kBlock];
-        decode8<127>(load_codes(cm, wide, count), int(tops & 0xffffu), m);
-        decode8<255>(load_codes(cv, wide, count), int(tops >> 16), v);
-    }
-    const void *const *grads = p.grads + (unsigned long long)tensor * p.K;
-#pragma unroll
-    for (int i = 0; i < kGroup; ++i) g[i] = 0.0f;
+}
+// The same element by element.
+template <typename G> __device__ __forceinline__ void aggregate_some(const AdamParams &p, const Place &x, float *g)
+{
     for (int k = 0; k < p.K; ++k) {
-        float x[kGroup];
-        load8(static_cast<const G *>(grads[k]) + at, wide, count, x);
-        const float lambda = p.lambda[k];
+        float f[kGroup];
+        load8(static_cast<const G *>(p.grads[(unsigned long long)x.tensor * p.K + k]) + x.at, false, x.count, f);
 #pragma unroll
-        for (int i = 0; i < kGroup; ++i) g[i] = __fmaf_rn(lambda, x[i], g[i]);
+        for (int i = 0; i < kGroup; ++i) g[i] = __fmaf_rn(p.lambda[k], f[i], k ? g[i] : 0.0f);
+    }
+}
+
+template <typename G, int BITS> __global__ void __launch_bounds__(kThreads, BITS == 8 ? 9 : 7) adamw_kernel(const __grid_constant__ AdamParams p)
+{
+    const Entry *entry;
+    const Place x(p, blockIdx.x, entry);
+    const Entry &e = *entry;
+    float theta[kGroup], m[kGroup], v[kGroup], g[kGroup];
+    float *const fm = static_cast<float *>(e.m) + x.at, *const fv = static_cast<float *>(e.v) + x.at;
+    unsigned char *const cm = static_cast<unsigned char *>(e.m) + x.at, *const cv = static_cast<unsigned char *>(e.v) + x.at;
+    uint2 codes_m = {0, 0}, codes_v = {0, 0};
+    uint32_t tops = 0;
+    Raw<G> first;
+    if (x.whole) {
+        first.load(static_cast<const G *>(p.grads[(unsigned long long)x.tensor * p.K]) + x.at);
+        load_group(e.param + x.at, theta);
+        if constexpr (BITS == 32) {
+            load_group(fm, m);
+            load_group(fv, v);
+        } else {
+            codes_m = *reinterpret_cast<const uint2 *>(cm);
+            codes_v = *reinterpret_cast<const uint2 *>(cv);
+            tops = e.tops[x.at / kBlock];
+        }
+    }
+    const Scales now = scales_of(p);
+    if (!x.block) return;
+    if (x.whole) {
+        aggregate(p, x, first, g);
+    } else {
+        load8(e.param + x.at, false, x.count, theta);
+        if constexpr (BITS == 32) {
+            load8(fm, false, x.count, m);
+            load8(fv, false, x.count, v);
+        } else {
+            codes_m = load_codes(cm, false, x.count);
+            codes_v = load_codes(cv, false, x.count);
+            tops = e.tops[x.at / kBlock];
+        }
+        aggregate_some<G>(p, x, g);
+    }
+    if constexpr (BITS == 8) {
+        decode8<127>(codes_m, int(tops & 0xffffu), m);
+        decode8<255>(codes_v, int(tops >> 16), v);
     }
     const float keep = float(1.0 - p.lr * e.decay);
 #pragma unroll
     for (int i = 0; i < kGroup; i += 2) {
-        const float2 x = {g[i], g[i + 1]}, t = {theta[i], theta[i + 1]};
-        const float2 m1 = fma2({p.b1, p.b1}, {m[i], m[i + 1]}, mul2({p.c1, p.c1}, x));
-        const float2 v1 = fma2(mul2({p.c2, p.c2}, x), x, mul2({p.b2, p.b2}, {v[i], v[i + 1]}));
-        const float2 below = fma2({root(v1.x), root(v1.y)}, {spread, spread}, {p.eps, p.eps});
-        const float2 t1 = fma2({-rate, -rate}, mul2(m1, {inverse(below.x), inverse(below.y)}), mul2({keep, keep}, t));
+        const float2 d = {g[i], g[i + 1]}, t = {theta[i], theta[i + 1]};
+        const float2 m1 = fma2({p.b1, p.b1}, {m[i], m[i + 1]}, mul2({p.c1, p.c1}, d));
+        const float2 v1 = fma2(mul2({p.c2, p.c2}, d), d, mul2({p.b2, p.b2}, {v[i], v[i + 1]}));
+        const float2 below = fma2({root(v1.x), root(v1.y)}, {now.spread, now.spread}, {p.eps, p.eps});
+        const float2 t1 = fma2({-now.rate, -now.rate}, mul2(m1, {inverse(below.x), inverse(below.y)}), mul2({keep, keep}, t));
         m[i] = m1.x; m[i + 1] = m1.y;
         v[i] = v1.x; v[i + 1] = v1.y;
         theta[i] = t1.x; theta[i + 1] = t1.y;
     }
-    store8(e.param + at, wide, count, theta);
-    if (e.copy) store8(e.copy + at, wide, count, theta);
+    store8(e.param + x.at, x.whole, x.count, theta);
+    if (e.copy) store8(e.copy + x.at, x.whole, x.count, theta);
     if constexpr (BITS == 32) {
-        store8(fm, wide, count, m);
-        store8(fv, wide, count, v);
+        store8(fm, x.whole, x.count, m);
+        store8(fv, x.whole, x.count, v);
     } else {
-        const uint32_t start = step * 0x85EBCA77u + tensor * 0xC2B2AE3Du + uint32_t(at) * kStride;
+        const uint32_t start = now.step * 0x85EBCA77u + x.tensor * 0xC2B2AE3Du + uint32_t(x.at) * kStride;
         // What stands behind the end was loaded as zeros: it is zero still, and its codes are not stored.
         uint32_t rm[kGroup], rv[kGroup], most_m = 0, most_v = 0;
 #pragma unroll
@@ -248,18 +330,20 @@ template <typename G, int BITS> __global__ void __launch_bounds__(kThreads) adam
         }
         most_m = __reduce_max_sync(~0u, most_m);
         most_v = __reduce_max_sync(~0u, most_v);
-        if (max(most_m, most_v) > 0x7ffu) {
+        if (max(most_m, most_v) >> 31) {
 #pragma unroll
             for (int i = 0; i < kGroup; ++i) {
-                rm[i] = min(rm[i], 0x7ffu);
-                rv[i] = min(rv[i], 0x7ffu);
+                rm[i] = min(rm[i], 0x7fffffffu);
+                rv[i] = min(rv[i], 0x7fffffffu);
             }
-            most_m = min(most_m, 0x7ffu);
-            most_v = min(most_v, 0x7ffu);
+            most_m = min(most_m, 0x7fffffffu);
+            most_v = min(most_v, 0x7fffffffu);
         }
-        store_codes(cm, wide, count, {encode4<127>(rm, int(most_m), m), encode4<127>(rm + 4, int(most_m), m + 4)});
-        store_codes(cv, wide, count, {encode4<255>(rv, int(most_v), v), encode4<255>(rv + 4, int(most_v), v + 4)});
-        if (threadIdx.x % 32 == 0) e.tops[at / kBlock] = most_m | most_v << 16;
+        most_m >>= 20;
+        most_v >>= 20;
+        store_codes(cm, x.whole, x.count, {encode4<127>(rm, int(most_m), m), encode4<127>(rm + 4, int(most_m), m + 4)});
+        store_codes(cv, x.whole, x.count, {encode4<255>(rv, int(most_v), v), encode4<255>(rv + 4, int(most_v), v + 4)});
+        if (threadIdx.x % 32 == 0) e.tops[x.at / kBlock] = most_m | most_v << 16;
     }
 }
 

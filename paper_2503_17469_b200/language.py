@@ -510,8 +510,7 @@ class Policy(_Operator):
             with self._on_stream(stream):
                 return self.logprob(logits, tokens)
         d = self._describe(logits, tokens)
-        logp = logits.new_empty(d.rows, dtype=_float)
-        lse = _like(logp)
+        logp, lse = logits.new_empty((2, d.rows), dtype=_float).unbind(0)
         self._check(self._lib.omni_policy_logprob(self.ctx._h, _ref(d), logp.data_ptr(), lse.data_ptr(), _raw_stream(logits.get_device())))
         return logp, lse
 
@@ -522,7 +521,7 @@ class Policy(_Operator):
             with self._on_stream(stream):
                 return self.forward(logits, tokens, old, advantage, reference)
         d = self._describe(logits, tokens, old, advantage, reference)
-        loss, logp, lse = (_like(old) for _ in range(3))
+        loss, logp, lse = old.new_empty((3, d.rows)).unbind(0)
         self._check(self._lib.omni_policy_forward(self.ctx._h, _ref(d), loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
                                                   _raw_stream(logits.get_device())))
         return loss, logp, lse
@@ -547,7 +546,7 @@ class Policy(_Operator):
                 return self.step(logits, tokens, old, advantage, grad_loss, reference, grad)
         d = self._describe(logits, tokens, old, advantage, reference)
         weights = self._row_values(grad_loss, logits, "grad_loss")
-        loss, logp, lse = (_like(grad_loss) for _ in range(3))
+        loss, logp, lse = old.new_empty((3, d.rows)).unbind(0)
         grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_policy_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
                                                grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
