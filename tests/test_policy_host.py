@@ -57,6 +57,7 @@ def test_refuses_outputs(omni):
 def test_tensors_of_another_device_are_refused(omni, monkeypatch):
     monkeypatch.setattr(L, "_raw_stream", lambda d: 0)
     monkeypatch.setattr(L, "_like", lambda t: Elsewhere(t.shape, t.dtype))
+    monkeypatch.setattr(Elsewhere, "unbind", lambda t, dim: [Elsewhere(t.shape[1:], t.dtype) for _ in range(t.shape[0])], raising=False)
     p = L.Policy(omni, kl=0.1)
     p._lib = Library()
     z, t, r = Elsewhere((4, 50), F32), Elsewhere((4,), I64), Elsewhere((4,), F32)
