@@ -11,6 +11,7 @@
 
 #include <cmath>
 #include <numeric>
+#include <type_traits>
 
 namespace omni {
 namespace {
@@ -235,7 +236,15 @@ __device__ __forceinline__ void put_partial(const RotaryParams &p, const float *
     }
 }
 
-// ---- wide accesses: a lane has a unit of eight pairs, fetched ahead by asynchronous copies into slots of its own ----------------
+// ---- wide accesses: a lane has sixteen elements, fetched ahead by asynchronous copies into slots of its own ----------------------
+
+// Which sixteen: eight pairs whose halves are both whole groups of eight; eight pairs of neighbours; or, with halves that do not begin on a
+// group, sixteen elements in a row, whose partners are read one by one from the slots of the lanes that have them.
+enum Layout { kHalves, kNeighbours, kGathered };
+template <Layout L> __device__ __forceinline__ Place wide_place(const RotaryParams &p, int unit)
+{
+    return L == kHalves ? place<8>(p, unit) : Place{16 * unit, 16 * unit + 8};
+}
 
 // Eight elements in shared memory: pieces of 16 bytes, each piece of all threads side by side.
 template <typename T> constexpr int kPieces = int(sizeof(T)) / 2;
@@ -265,6 +274,16 @@ template <typename T, int CHUNKS, int STAGES> struct Ring {
 #pragma unroll
         for (int i = 0; i < CHUNKS * kPieces<T>; ++i) *reinterpret_cast<uint4 *>(base + stage * kStage + i * kThreads * 16) = make_uint4(0, 0, 0, 0);
     }
+    // Where element j of the group's head vector stands in a stage, from the start of the block's slots on; `first`: the group's first thread.
+    static __device__ __forceinline__ int element(int first, int chunk, int j)
+    {
+        const int piece = (chunk + j / 8 % 2) * kPieces<T> + j % 8 * int(sizeof(T)) / 16;
+        return (piece * kThreads + first + j / 16) * 16 + j * int(sizeof(T)) % 16;
+    }
+    __device__ __forceinline__ float at(int stage, int offset) const
+    {
+        return to_float(*reinterpret_cast<const T *>(base - threadIdx.x * 16 + stage * kStage + offset));
+    }
     __device__ __forceinline__ void get(int stage, int chunk, float *f) const
     {
         const char *const at = base + stage * kStage + chunk * kPieces<T> * kThreads * 16;
@@ -279,17 +298,17 @@ template <typename T, int CHUNKS, int STAGES> struct Ring {
 };
 
 // A unit's 16 elements, in the order of its two chunks, as two pairs (of first or of second elements) of consecutive rotations.
-template <bool ADJACENT> __device__ __forceinline__ float2 firsts(const float *f, int i)
+template <Layout L> __device__ __forceinline__ float2 firsts(const float *f, int i)
 {
-    return ADJACENT ? make_float2(f[4 * i], f[4 * i + 2]) : make_float2(f[2 * i], f[2 * i + 1]);
+    return L == kNeighbours ? make_float2(f[4 * i], f[4 * i + 2]) : make_float2(f[2 * i], f[2 * i + 1]);
 }
-template <bool ADJACENT> __device__ __forceinline__ float2 seconds(const float *f, int i)
+template <Layout L> __device__ __forceinline__ float2 seconds(const float *f, int i)
 {
-    return ADJACENT ? make_float2(f[4 * i + 1], f[4 * i + 3]) : make_float2(f[8 + 2 * i], f[8 + 2 * i + 1]);
+    return L == kNeighbours ? make_float2(f[4 * i + 1], f[4 * i + 3]) : make_float2(f[8 + 2 * i], f[8 + 2 * i + 1]);
 }
-template <bool ADJACENT> __device__ __forceinline__ void put_pairs(float *f, int i, float2 a, float2 b)
+template <Layout L> __device__ __forceinline__ void put_pairs(float *f, int i, float2 a, float2 b)
 {
-    if (ADJACENT) {
+    if (L == kNeighbours) {
         f[4 * i] = a.x; f[4 * i + 2] = a.y; f[4 * i + 1] = b.x; f[4 * i + 3] = b.y;
     } else {
         f[2 * i] = a.x; f[2 * i + 1] = a.y; f[8 + 2 * i] = b.x; f[8 + 2 * i + 1] = b.y;
@@ -297,27 +316,63 @@ template <bool ADJACENT> __device__ __forceinline__ void put_pairs(float *f, int
 }
 __device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
 
-// The side's weights in shared memory, those of the pairs' first elements, then of the second.
+// The side's weights in shared memory.
 struct Weights {
-    float first[kMaxPairs], second[kMaxPairs];
+    float w[OMNI_ROTARY_MAX_DIM];
     __device__ __forceinline__ void fill(const RotaryParams &p, const Side &side)
     {
-        for (int i = threadIdx.x; i < p.dim / 2; i += kThreads) {
-            const Place at = place<1>(p, i);
-            first[i] = weight_at(p, side, at.a);
-            second[i] = weight_at(p, side, at.b);
-        }
+        for (int i = threadIdx.x; i < p.dim; i += kThreads) w[i] = weight_at(p, side, i);
     }
 };
 __device__ __forceinline__ float2 two(const float *f, int i) { return *reinterpret_cast<const float2 *>(f + i); }
+// Those of pairs 2 i and 2 i + 1 of a unit, first and second elements.
+template <Layout L> __device__ __forceinline__ void weights_of(const Weights &weights, Place at, int i, float2 *a, float2 *b)
+{
+    if (L == kNeighbours) {
+        const float2 x = two(weights.w, at.a + 4 * i), y = two(weights.w, at.a + 4 * i + 2);
+        *a = make_float2(x.x, y.x);
+        *b = make_float2(x.y, y.y);
+    } else {
+        *a = two(weights.w, at.a + 2 * i);
+        *b = two(weights.w, at.b + 2 * i);
+    }
+}
+
+// What a pair's other element adds to one that is not turned is nothing, whatever it is (a product with a sine of 0 would carry infinities and
+// NaN over): of two consecutive pairs or elements, of which `turned` counts those that are.
+__device__ __forceinline__ float2 still(float2 x, int turned) { return make_float2(turned > 0 ? x.x : 0.0f, turned > 1 ? x.y : 0.0f); }
+
+// Gathered: what turns element i, the element it is turned with, and the sign of that one's sine.
+struct Partner {
+    int pair, with;
+    float sign;
+    __device__ __forceinline__ Partner(const RotaryParams &p, int i, bool back)
+    {
+        pair = i < p.pairs ? i : i < 2 * p.pairs ? i - p.pairs : p.pairs;        // those that are not turned: a frequency of 0
+        with = i < p.pairs ? i + p.pairs : i < 2 * p.pairs ? i - p.pairs : i;
+        sign = (i < p.pairs) == back ? 1.0f : -1.0f;
+    }
+};
+// The offsets of sixteen partners in a stage, two to a word.
+template <typename R> __device__ __forceinline__ void partner_offsets(const RotaryParams &p, int first, int chunk, int from, uint32_t *offset)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        offset[e] = uint32_t(R::element(first, chunk, Partner(p, from + 2 * e, false).with)) |
+                    uint32_t(R::element(first, chunk, Partner(p, from + 2 * e + 1, false).with)) << 16;
+}
+template <typename R> __device__ __forceinline__ float2 partners(const R &ring, int stage, uint32_t offset)
+{
+    return make_float2(ring.at(stage, int(offset & 0xffffu)), ring.at(stage, int(offset >> 16)));
+}
 
 template <typename T> constexpr int kForwardStages = sizeof(T) == 2 ? 6 : 4;
 template <typename T> using ForwardRing = Ring<T, 2, kForwardStages<T>>;
 
 // Forward: a group of lanes has a row of one side.  With weights they are folded into the angles, and a result is
 // y_a = r ((w_a cos) x_a - (w_b sin) x_b), y_b = r ((w_b cos) x_b + (w_a sin) x_a).
-template <typename T, bool ADJACENT, bool NORM>
-__global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const __grid_constant__ RotaryParams p)
+template <typename T, Layout L, bool NORM>
+__global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
     extern __shared__ __align__(16) char shared[];
     __shared__ Pairs pairs;
@@ -330,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const 
     const RowAt row(p, (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * rows_of_block(p) + me.row);
     const bool has = me.lane * 16 < p.dim;
     const int unit = has ? me.lane : 0;
-    const Place at = place<8>(p, unit);
+    const Place at = wide_place<L>(p, unit);
     const int to_b = at.b - at.a;
     const T *src = row.in<T>(side.x) + me.first * side.x.head + at.a;
     T *dst = row.in<T>(side.out) + me.first * side.out.head + at.a;
@@ -352,25 +407,51 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const 
     pairs.fill(p);
     if constexpr (NORM) weights.fill(p, side);
     __syncthreads();
-    float2 ca[4], sa[4], cb[4], sb[4];                // cos and sin, with weights those times w_a and w_b; sb with its sign
-    Angles angles{p, pairs, row, position_at(p, row, pairs.axis[unit * 8]), pairs.axis[unit * 8]};
+    constexpr int kCoefficients = L == kGathered ? 8 : 4;
+    // cos and sin, with weights those times w_a and w_b, sb with its sign; gathered: of an element and of its partner
+    float2 ca[kCoefficients], sa[kCoefficients], cb[4], sb[4];
+    uint32_t offset[8];
+    const int first_pair = L == kGathered ? Partner(p, at.a, false).pair : unit * 8;
+    Angles angles{p, pairs, row, position_at(p, row, pairs.axis[first_pair]), pairs.axis[first_pair]};
+    if constexpr (L == kGathered) {
+        partner_offsets<ForwardRing<T>>(p, int(threadIdx.x) - me.lane, 0, at.a, offset);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float2 c, s;
-        angles.two(unit * 8 + 2 * i, &c, &s);
-        const float2 wa = NORM ? two(weights.first, unit * 8 + 2 * i) : c, wb = NORM ? two(weights.second, unit * 8 + 2 * i) : c;
-        ca[i] = NORM ? mul2(c, wa) : c;
-        cb[i] = NORM ? mul2(c, wb) : c;
-        sa[i] = NORM ? mul2(s, wa) : s;
-        sb[i] = minus(NORM ? mul2(s, wb) : s);
+        for (int e = 0; e < 8; ++e) {
+            const Partner x(p, at.a + 2 * e, false), y(p, at.a + 2 * e + 1, false);
+            angles.at(x.pair, &ca[e].x, &sa[e].x);
+            angles.at(y.pair, &ca[e].y, &sa[e].y);
+            sa[e] = mul2(sa[e], make_float2(x.sign, y.sign));
+            if constexpr (NORM) {
+                ca[e] = mul2(ca[e], two(weights.w, at.a + 2 * e));
+                sa[e] = mul2(sa[e], make_float2(weights.w[x.with], weights.w[y.with]));
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float2 c, s, wa = {1.0f, 1.0f}, wb = {1.0f, 1.0f};
+            angles.two(unit * 8 + 2 * i, &c, &s);
+            if constexpr (NORM) weights_of<L>(weights, at, i, &wa, &wb);
+            ca[i] = NORM ? mul2(c, wa) : c;
+            cb[i] = NORM ? mul2(c, wb) : c;
+            sa[i] = NORM ? mul2(s, wa) : s;
+            sb[i] = minus(NORM ? mul2(s, wb) : s);
+        }
     }
     const float inverse_dim = 1.0f / float(p.dim);
+    // pairs of the lane that are turned, gathered: elements
+    const int turned = L == kGathered ? 2 * p.pairs - at.a : p.pairs - unit * 8;
     int stage = 0, head = row.mine && has ? me.first : side.heads;
     for (int j = 0; j < me.turns; ++j, head += p.split, dst += dst_step) {
         copies_wait<kStages - 2>();
         float f[16];
+        float2 with[8];
+        if constexpr (L == kGathered) __syncwarp();   // other lanes' copies have arrived, and they are done with the turn before
         ring.get(stage, 0, f);
         ring.get(stage, 1, f + 8);
+        if constexpr (L == kGathered)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) with[e] = partners(ring, stage, offset[e]);
         // into the slot that the turn before this one has used up
         fetch(stage == 0 ? kStages - 1 : stage - 1);
         stage = stage == kStages - 1 ? 0 : stage + 1;
@@ -382,16 +463,33 @@ __global__ void __launch_bounds__(kThreads, 3) rotary_forward_wide_kernel(const 
             const float squares = group_sum(sum.x + sum.y, p.lanes);
             r.x = r.y = row.there ? rsqrtf(fmaf(squares, inverse_dim, p.eps)) : 0.0f;
         }
+        const auto turn = [&](auto some) {             // some of them are not
+            constexpr bool kSome = decltype(some)::value;
+            if constexpr (L == kGathered) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-            float2 ya = fma2(a, ca[i], mul2(b, sb[i])), yb = fma2(b, cb[i], mul2(a, sa[i]));
-            if constexpr (NORM) {
-                ya = mul2(ya, r);
-                yb = mul2(yb, r);
+                for (int e = 0; e < 8; ++e) {
+                    const float2 other = kSome ? still(with[e], turned - 2 * e) : with[e];
+                    float2 y = fma2(make_float2(f[2 * e], f[2 * e + 1]), ca[e], mul2(other, sa[e]));
+                    if constexpr (NORM) y = mul2(y, r);
+                    f[2 * e] = y.x;
+                    f[2 * e + 1] = y.y;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 a = firsts<L>(f, i), b = seconds<L>(f, i);
+                    const float2 to_a = kSome ? still(b, turned - 2 * i) : b, to_b = kSome ? still(a, turned - 2 * i) : a;
+                    float2 ya = fma2(a, ca[i], mul2(to_a, sb[i])), yb = fma2(b, cb[i], mul2(to_b, sa[i]));
+                    if constexpr (NORM) {
+                        ya = mul2(ya, r);
+                        yb = mul2(yb, r);
+                    }
+                    put_pairs<L>(f, i, ya, yb);
+                }
             }
-            put_pairs<ADJACENT>(f, i, ya, yb);
-        }
+        };
+        if (turned >= (L == kGathered ? 16 : 8)) turn(std::false_type());
+        else turn(std::true_type());
         if (head < side.heads) {
             store_group(dst, f);
             store_group(dst + to_b, f + 8);
@@ -403,7 +501,7 @@ template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 3;
 template <typename T> using BackwardRing = Ring<T, 4, kBackwardStages<T>>;
 
 // Backward of the norm and the rotation: blocks that stay, each on rows of one side, with the weight's gradient in registers.
-template <typename T, bool ADJACENT>
+template <typename T, Layout L>
 __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
     extern __shared__ __align__(16) char shared[];
@@ -418,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
     const int heads = side.heads, lane = threadIdx.x % p.lanes;
     const bool has = lane * 16 < p.dim;
     const int unit = has ? lane : 0;
-    const Place at = place<8>(p, unit);
+    const Place at = wide_place<L>(p, unit);
     const int to_b = at.b - at.a;
     const float inverse_dim = 1.0f / float(p.dim);
     // what is fetched next: the loads run ahead of the sums, over the bundles' ends
@@ -454,14 +552,17 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
     pairs.fill(p);
     weights.fill(p, side);
     __syncthreads();
+    constexpr int kCoefficients = L == kGathered ? 8 : 4;
     float2 wa[4], wb[4], da[4] = {}, db[4] = {};
+    uint32_t offset[8];
+    if constexpr (L == kGathered) partner_offsets<BackwardRing<T>>(p, int(threadIdx.x) - lane, 2, at.a, offset);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        wa[i] = two(weights.first, unit * 8 + 2 * i);
-        wb[i] = two(weights.second, unit * 8 + 2 * i);
-    }
-    unsigned long long position = position_at(p, RowAt(p, now.row(p)), pairs.axis[unit * 8]);
-    float2 c[4], s[4];
+    for (int i = 0; i < 4; ++i) weights_of<L>(weights, at, i, &wa[i], &wb[i]);
+    const int first_pair = L == kGathered ? Partner(p, at.a, true).pair : unit * 8;
+    unsigned long long position = position_at(p, RowAt(p, now.row(p)), pairs.axis[first_pair]);
+    float2 c[kCoefficients], s[kCoefficients];        // gathered: of an element and of its partner, with its sign
+    // pairs of the lane that are turned, gathered: elements
+    const int turned = L == kGathered ? 2 * p.pairs - at.a : p.pairs - unit * 8;
     T *dst = nullptr;
     bool mine = false, there = false, fresh = true;
     int stage = 0;
@@ -477,33 +578,63 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
             });
             if (now.left == 0) break;
             const RowAt row(p, now.row(p));
-            if (skipped) position = position_at(p, row, pairs.axis[unit * 8]);
+            if (skipped) position = position_at(p, row, pairs.axis[first_pair]);
             mine = row.mine && has;
             there = row.there && has;
             dst = row.in<T>(side.out) + now.head * side.out.head + at.a;
-            Angles angles{p, pairs, row, position, pairs.axis[unit * 8]};
-            position = position_at(p, RowAt(p, now.next_row(p)), pairs.axis[unit * 8]);
+            Angles angles{p, pairs, row, position, pairs.axis[first_pair]};
+            position = position_at(p, RowAt(p, now.next_row(p)), pairs.axis[first_pair]);
+            if constexpr (L == kGathered) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) angles.two(unit * 8 + 2 * i, &c[i], &s[i]);
+                for (int e = 0; e < 8; ++e) {
+                    const Partner x(p, at.a + 2 * e, true), y(p, at.a + 2 * e + 1, true);
+                    angles.at(x.pair, &c[e].x, &s[e].x);
+                    angles.at(y.pair, &c[e].y, &s[e].y);
+                    s[e] = mul2(s[e], make_float2(x.sign, y.sign));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) angles.two(unit * 8 + 2 * i, &c[i], &s[i]);
+            }
         }
         copies_wait<kStages - 2>();
         float f[16], g[16];
+        if constexpr (L == kGathered) __syncwarp();   // other lanes' copies have arrived, and they are done with the turn before
         ring.get(stage, 0, f);
         ring.get(stage, 1, f + 8);
         ring.get(stage, 2, g);
         ring.get(stage, 3, g + 8);
+        const auto turn = [&](auto some) {             // back; some of them are not turned
+            constexpr bool kSome = decltype(some)::value;
+            if constexpr (L == kGathered) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 with = partners(ring, stage, offset[e]);
+                    const float2 n = fma2(make_float2(g[2 * e], g[2 * e + 1]), c[e], mul2(kSome ? still(with, turned - 2 * e) : with, s[e]));
+                    g[2 * e] = n.x;
+                    g[2 * e + 1] = n.y;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 a = firsts<L>(g, i), b = seconds<L>(g, i);
+                    const float2 to_a = kSome ? still(b, turned - 2 * i) : b, to_b = kSome ? still(a, turned - 2 * i) : a;
+                    put_pairs<L>(g, i, fma2(a, c[i], mul2(to_a, s[i])), fma2(b, c[i], mul2(to_b, minus(s[i]))));
+                }
+            }
+        };
+        if (turned >= (L == kGathered ? 16 : 8)) turn(std::false_type());
+        else turn(std::true_type());
         // into the slot that the turn before this one has used up
         fetch(stage == 0 ? kStages - 1 : stage - 1);
         stage = stage == kStages - 1 ? 0 : stage + 1;
         float2 square = {0.0f, 0.0f}, dot = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-            const float2 ya = firsts<ADJACENT>(g, i), yb = seconds<ADJACENT>(g, i);
-            const float2 na = fma2(ya, c[i], mul2(yb, s[i])), nb = fma2(yb, c[i], mul2(ya, minus(s[i])));
+            const float2 a = firsts<L>(f, i), b = seconds<L>(f, i);
+            const float2 na = firsts<L>(g, i), nb = seconds<L>(g, i);
             square = fma2(b, b, fma2(a, a, square));
             dot = fma2(mul2(b, wb[i]), nb, fma2(mul2(a, wa[i]), na, dot));
-            put_pairs<ADJACENT>(g, i, na, nb);
         }
         const float2 sums = group_sum(make_float2(square.x + square.y, dot.x + dot.y), p.lanes);
         // 0 where nothing is there: infinite without eps, it would make a NaN of the zeros
@@ -511,11 +642,11 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
         const float2 r = {scale, scale}, q = {pull, pull};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 a = firsts<ADJACENT>(f, i), b = seconds<ADJACENT>(f, i);
-            const float2 na = firsts<ADJACENT>(g, i), nb = seconds<ADJACENT>(g, i);
+            const float2 a = firsts<L>(f, i), b = seconds<L>(f, i);
+            const float2 na = firsts<L>(g, i), nb = seconds<L>(g, i);
             da[i] = fma2(na, mul2(a, r), da[i]);
             db[i] = fma2(nb, mul2(b, r), db[i]);
-            put_pairs<ADJACENT>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
+            put_pairs<L>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
         }
         if (mine) {
             store_group(dst, f);
@@ -530,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
     float *const sums = reinterpret_cast<float *>(shared);
     float dw[16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) put_pairs<ADJACENT>(dw, i, da[i], db[i]);
+    for (int i = 0; i < 4; ++i) put_pairs<L>(dw, i, da[i], db[i]);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const float v = warp_groups_sum(dw[e], p.lanes);
@@ -545,7 +676,7 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
 constexpr int kOwn = kMaxPairs / 32;                  // pairs of a lane
 struct Own {
     Place at[kOwn];
-    bool has[kOwn];
+    bool has[kOwn], turned[kOwn];
     float w[kOwn][2];
     __device__ __forceinline__ Own(const RotaryParams &p, const Side &side, int lane, bool norm)
     {
@@ -553,6 +684,7 @@ struct Own {
         for (int n = 0; n < kOwn; ++n) {
             const int unit = lane + n * p.lanes;
             has[n] = unit < p.dim / 2;
+            turned[n] = unit < p.pairs;
             at[n] = place<1>(p, has[n] ? unit : 0);
             w[n][0] = norm ? weight_at(p, side, at[n].a) : 1.0f;
             w[n][1] = norm ? weight_at(p, side, at[n].b) : 1.0f;
@@ -612,8 +744,8 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
             for (int n = 0; n < kOwn; ++n) {
                 if (!own.has[n]) continue;
                 const float a = NORM ? f[n][0] * r * own.w[n][0] : f[n][0], b = NORM ? f[n][1] * r * own.w[n][1] : f[n][1];
-                at[own.at[n].a] = from_float<T>(row.there ? fmaf(a, c[n], -b * s[n]) : 0.0f);
-                at[own.at[n].b] = from_float<T>(row.there ? fmaf(b, c[n], a * s[n]) : 0.0f);
+                at[own.at[n].a] = from_float<T>(!row.there ? 0.0f : own.turned[n] ? fmaf(a, c[n], -b * s[n]) : a);
+                at[own.at[n].b] = from_float<T>(!row.there ? 0.0f : own.turned[n] ? fmaf(b, c[n], a * s[n]) : b);
             }
         }
     }
@@ -667,8 +799,8 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
                     const float ya = to_float(y[i][n][0]), yb = to_float(y[i][n][1]);
                     f[n][0] = to_float(x[i][n][0]);
                     f[n][1] = to_float(x[i][n][1]);
-                    g[n][0] = fmaf(ya, c[n], yb * s[n]);
-                    g[n][1] = fmaf(yb, c[n], -ya * s[n]);
+                    g[n][0] = own.turned[n] ? fmaf(ya, c[n], yb * s[n]) : ya;
+                    g[n][1] = own.turned[n] ? fmaf(yb, c[n], -ya * s[n]) : yb;
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -875,8 +1007,8 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
     for (int i = 0; i < 2; ++i) p->side[i].blocks = s.blocks[i];
 }
 
-// Whole units of eight pairs: rotated and unrotated halves of multiples of eight, or any pairs that stand next to one another.
-bool wide_units(const omni_rotary *r) { return r->dim % 16 == 0 && (r->interleaved || r->pairs % 8 == 0); }
+// Sixteen elements a lane, in one of the three layouts.
+bool wide_units(const omni_rotary *r) { return r->dim % 16 == 0; }
 
 constexpr int kMostShared = 112 * 1024;               // dynamic shared memory of a block: two fit an SM
 
@@ -892,15 +1024,15 @@ template <typename T, bool NORM>
 int enqueue_forward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
     if (!wide) return enqueue(ctx, rotary_forward_kernel<T, NORM>, p, 0, s);
-    return enqueue(ctx, p.interleaved ? rotary_forward_wide_kernel<T, true, NORM> : rotary_forward_wide_kernel<T, false, NORM>, p,
-                   ForwardRing<T>::kBytes, s);
+    return enqueue(ctx, p.interleaved ? rotary_forward_wide_kernel<T, kNeighbours, NORM> : p.pairs % 8 == 0 ? rotary_forward_wide_kernel<T, kHalves, NORM>
+                   : rotary_forward_wide_kernel<T, kGathered, NORM>, p, ForwardRing<T>::kBytes, s);
 }
 
 template <typename T> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
     if (!wide) return enqueue(ctx, rotary_backward_kernel<T>, p, 0, s);
-    return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, true> : rotary_backward_wide_kernel<T, false>, p,
-                   BackwardRing<T>::kBytes, s);
+    return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, kNeighbours> : p.pairs % 8 == 0 ? rotary_backward_wide_kernel<T, kHalves>
+                   : rotary_backward_wide_kernel<T, kGathered>, p, BackwardRing<T>::kBytes, s);
 }
 
 // One pass over both sides without sums: the forward call, and the gradient where there are no weights.

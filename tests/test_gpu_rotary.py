@@ -97,7 +97,7 @@ def inputs(b, n, h, hk, d, dtype, seed, weight=None, axes=1, far=1000):
 
 SHAPES = [  # batch, length, heads, kv_heads, dim, pairs
     (1, 1, 1, 1, 2, 1), (3, 1, 16, 4, 128, 64), (2, 5, 3, 1, 64, 32), (1, 77, 7, 7, 80, 40), (2, 33, 12, 4, 96, 24), (1, 19, 2, 1, 256, 128),
-    (1, 700, 40, 8, 128, 64), (5, 301, 4, 2, 48, 8), (1, 3, 33, 5, 250, 125), (2, 130, 3, 1, 34, 11), (1, 5000, 2, 1, 16, 8), (1, 6000, 1, 1, 6, 2),
+    (1, 700, 40, 8, 128, 64), (5, 301, 4, 2, 48, 8), (2, 45, 9, 3, 64, 9), (3, 130, 6, 6, 96, 12), (1, 260, 2, 1, 256, 100), (2, 7, 5, 5, 16, 3), (1, 3, 33, 5, 250, 125), (2, 130, 3, 1, 34, 11), (1, 5000, 2, 1, 16, 8), (1, 6000, 1, 1, 6, 2),
 ]
 
 
@@ -251,6 +251,22 @@ def test_extreme_values(ctx, dtype, d, pairs):
     bad = torch.zeros_like(out, dtype=torch.bool)
     bad[0, 3, 1] = True
     assert torch.equal(out.isnan(), bad) and not bool(out[0, 0].any())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,pairs", [(64, 8), (64, 5), (96, 12), (50, 7), (128, 60)])
+def test_what_is_not_turned_stays_as_it_is(ctx, dtype, interleaved, d, pairs):
+    """Elements behind the pairs pass through, infinities and NaN beside them too."""
+    q, k, positions, _ = inputs(2, 9, 3, 3, d, dtype, 13)
+    r = L.Rotary(ctx, 3, 3, d, L.Rotary.geometric(pairs), interleaved=interleaved)
+    clean = r.forward(q, k, positions)[0]
+    q[0, 1, 2, 2 * pairs + 1], q[1, 3, 0, d - 1], q[1, 4, 1, 2 * pairs] = math.nan, math.inf, -math.inf
+    out, _ = r.forward(q, k, positions)
+    back = r.backward(q, k, positions, q, k)[0]
+    assert torch.equal(out[..., :2 * pairs], clean[..., :2 * pairs])
+    for t in (out, back):
+        assert torch.equal(t[..., 2 * pairs:].nan_to_num(7.0), q[..., 2 * pairs:].nan_to_num(7.0)) and int(t.isnan().sum()) == 1
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
