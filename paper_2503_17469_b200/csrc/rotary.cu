@@ -10,7 +10,6 @@
 #include "vector.cuh"
 
 #include <cmath>
-#include <numeric>
 #include <type_traits>
 
 namespace omni {
@@ -19,6 +18,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxPairs = OMNI_ROTARY_MAX_DIM / 2;
+constexpr int kMostSequences = 1024;                  // of a padded batch whose absent rows are passed over
 constexpr int kResident = 2;                          // backward blocks an SM
 
 struct View {
@@ -41,7 +41,8 @@ struct RotaryParams {
     unsigned magic, shift;                            // row / length = (mulhi(magic, row) + row) >> shift
     int dim, pairs, axes;
     int lanes, split;                                 // lanes of a head vector, groups of lanes that share a row's heads (forward): powers of two
-    unsigned bundles, step;                           // backward: rows in bundles of 32 / lanes; bundle number u of the walk is u * step modulo bundles
+    unsigned bundles;                                 // backward: rows in bundles of 32 / lanes
+    int batch, padded;                                // sequences; backward walks the bundles before their lengths alone
     int wide_positions, bf16_weight, interleaved, overlap;
     int backwards;                                    // the opposite angle
     float eps;
@@ -163,57 +164,89 @@ struct Share {
 };
 __device__ __forceinline__ unsigned rows_of_block(const RotaryParams &p) { return kThreads / (p.lanes * p.split); }
 
-// Backward: a warp's share of a side: a group of lanes has a row, the warp's groups a bundle of rows, and a turn is one head of each.  The turns of all
-// bundles are dealt to the side's warps in equal parts, wherever in a bundle they begin; the bundles are walked by large
-// steps, so that sequences of different lengths are spread over all warps.
-struct Walk {
-    unsigned number, bundle;                          // of the walk, of the rows
-    int head, left;                                   // turns that are left
-    __device__ __forceinline__ Walk(const RotaryParams &p, unsigned block, unsigned blocks, int heads)
+// Backward, of a padded batch: how many bundles (the rows of a warp's groups) lie before each sequence, counting those that begin
+// before its length.
+struct Sequences {
+    int before[kMostSequences + 1];
+    __device__ __forceinline__ void fill(const RotaryParams &p)
     {
-        const unsigned long long all = (unsigned long long)p.bundles * heads, warps = (unsigned long long)blocks * kWarps;
+        if (threadIdx.x >= 32) return;
+        const int lane = threadIdx.x, each = (p.batch + 31) / 32, first = min(lane * each, p.batch), last = min(first + each, p.batch);
+        const int rows = 32 / p.lanes;
+        int sum = 0;
+        for (int b = first; b < last; ++b) {
+            before[b] = sum;                          // of this lane's
+            sum += (min(max(p.lengths[b], 0), int(p.length)) + rows - 1) / rows;
+        }
+        int ahead = sum;
+        for (int o = 1; o < 32; o *= 2) {
+            const int other = __shfl_up_sync(~0u, ahead, o);
+            if (lane >= o) ahead += other;
+        }
+        if (lane == 31) before[p.batch] = ahead;
+        for (int b = first; b < last; ++b) before[b] += ahead - sum;
+    }
+};
+
+// Backward: a warp's share of a side: a group of lanes has a row, the warp's groups a bundle of rows, and a turn is one head of each.  The turns of all
+// bundles are dealt to the side's warps in equal parts, wherever in a bundle they begin.  PADDED: of the bundles before the sequences' lengths alone.
+constexpr unsigned kNoRow = 0x7fffffffu;              // behind all rows
+template <bool PADDED> struct Walk {
+    unsigned number;                                  // of the bundle
+    int sequence, head, left;                         // its sequence; turns that are left
+    __device__ __forceinline__ Walk(const RotaryParams &p, const Sequences *seq, unsigned block, unsigned blocks, int heads) : sequence(0)
+    {
+        const unsigned long long bundles = PADDED ? unsigned(seq->before[p.batch]) : p.bundles;
+        const unsigned long long all = bundles * heads, warps = (unsigned long long)blocks * kWarps;
         const unsigned long long me = (unsigned long long)block * kWarps + threadIdx.x / 32;
         const unsigned long long first = all * me / warps;
         left = int(all * (me + 1) / warps - first);
         number = unsigned(first / heads);
         head = int(first - (unsigned long long)number * heads);
-        bundle = unsigned((unsigned long long)number * p.step % p.bundles);
-    }
-    __device__ __forceinline__ unsigned following(const RotaryParams &p) const
-    {
-        return bundle >= p.bundles - p.step ? bundle - (p.bundles - p.step) : bundle + p.step;
+        if (!PADDED || left == 0) return;
+        int high = p.batch;                           // the last sequence that begins at or before the bundle
+        while (high - sequence > 1) {
+            const int middle = (sequence + high) / 2;
+            if (seq->before[middle] <= int(number)) sequence = middle;
+            else high = middle;
+        }
     }
     // the group's row
-    __device__ __forceinline__ unsigned row(const RotaryParams &p) const { return bundle * unsigned(32 / p.lanes) + threadIdx.x % 32 / p.lanes; }
-    __device__ __forceinline__ unsigned next_row(const RotaryParams &p) const
+    __device__ __forceinline__ unsigned row(const RotaryParams &p, const Sequences *seq) const
     {
-        return number + 1 < p.bundles ? following(p) * unsigned(32 / p.lanes) + threadIdx.x % 32 / p.lanes : 0x7fffffffu;    // behind all rows
+        const unsigned rows = 32 / p.lanes, group = threadIdx.x % 32 / p.lanes;
+        if constexpr (PADDED) {
+            const unsigned i = (number - unsigned(seq->before[sequence])) * rows + group;
+            return i < p.length ? sequence * p.length + i : kNoRow;
+        } else {
+            return number * rows + group;
+        }
     }
-    __device__ __forceinline__ void next(const RotaryParams &p, int heads, int by = 1)
+    __device__ __forceinline__ void next(const RotaryParams &p, const Sequences *seq, int heads, int by = 1)
     {
         left -= by;
         head += by;
-        if (head == heads) {
-            head = 0;
-            ++number;
-            bundle = following(p);
-        }
+        if (head < heads) return;
+        head = 0;
+        ++number;
+        if constexpr (PADDED)
+            while (sequence < p.batch - 1 && seq->before[sequence + 1] <= int(number)) ++sequence;
+    }
+    __device__ __forceinline__ unsigned next_row(const RotaryParams &p, const Sequences *seq, int heads) const
+    {
+        Walk then = *this;
+        then.next(p, seq, heads, heads - head);
+        return left > heads - head ? then.row(p, seq) : kNoRow;
     }
 };
 
-// Over the bundles that lie behind their sequences' lengths altogether: f(the group's row, turns) for each.  Whether there were any.
-template <typename F> __device__ __forceinline__ bool skip_absent(const RotaryParams &p, int heads, Walk &walk, F f)
+// Backward, of a padded batch: f(a row behind its length) by each group, over all rows.
+template <typename F> __device__ __forceinline__ void absent_rows(const RotaryParams &p, const Side &side, unsigned block, F f)
 {
-    bool any = false;
-    while (p.lengths && walk.left > 0) {
-        const RowAt row(p, walk.row(p));
-        if (__any_sync(~0u, row.there)) break;
-        const int turns = min(walk.left, heads - walk.head);
-        f(row, turns);
-        walk.next(p, heads, turns);
-        any = true;
+    for (unsigned n = block * kWarps + threadIdx.x / 32; n < p.bundles; n += side.blocks * kWarps) {
+        const RowAt row(p, n * unsigned(32 / p.lanes) + threadIdx.x % 32 / p.lanes);
+        if (row.mine && !row.there) f(row);
     }
-    return any;
 }
 
 __device__ __forceinline__ float weight_at(const RotaryParams &p, const Side &side, int c)
@@ -501,7 +534,7 @@ template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 3;
 template <typename T> using BackwardRing = Ring<T, 4, kBackwardStages<T>>;
 
 // Backward of the norm and the rotation: blocks that stay, each on rows of one side, with the weight's gradient in registers.
-template <typename T, Layout L>
+template <typename T, Layout L, bool PADDED>
 __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
     extern __shared__ __align__(16) char shared[];
@@ -519,15 +552,20 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
     const Place at = wide_place<L>(p, unit);
     const int to_b = at.b - at.a;
     const float inverse_dim = 1.0f / float(p.dim);
+    __shared__ Sequences sequences[1];
+    const Sequences *const seq = sequences;
+    if constexpr (PADDED) {
+        sequences->fill(p);
+        __syncthreads();
+    }
     // what is fetched next: the loads run ahead of the sums, over the bundles' ends
-    Walk now(p, block, side.blocks, heads), ahead = now;
+    Walk<PADDED> now(p, seq, block, side.blocks, heads), ahead = now;
     const T *src = nullptr, *grad = nullptr;
     bool ahead_there = false, ahead_new = true;
     const auto fetch = [&](int stage) {
-        if (ahead_new) skip_absent(p, heads, ahead, [](const RowAt &, int) {});
         if (ahead.left > 0) {
             if (ahead_new) {
-                const RowAt row(p, ahead.row(p));
+                const RowAt row(p, ahead.row(p, seq));
                 ahead_there = row.there && has;
                 src = row.in<T>(side.x) + ahead.head * side.x.head + at.a;
                 grad = row.in<T>(side.dy) + ahead.head * side.dy.head + at.a;
@@ -542,7 +580,7 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
             }
             src += side.x.head;
             grad += side.dy.head;
-            ahead.next(p, heads);
+            ahead.next(p, seq, heads);
             ahead_new = ahead.head == 0;
         }
         copies_commit();
@@ -559,31 +597,21 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
 #pragma unroll
     for (int i = 0; i < 4; ++i) weights_of<L>(weights, at, i, &wa[i], &wb[i]);
     const int first_pair = L == kGathered ? Partner(p, at.a, true).pair : unit * 8;
-    unsigned long long position = position_at(p, RowAt(p, now.row(p)), pairs.axis[first_pair]);
+    unsigned long long position = position_at(p, RowAt(p, now.row(p, seq)), pairs.axis[first_pair]);
     float2 c[kCoefficients], s[kCoefficients];        // gathered: of an element and of its partner, with its sign
     // pairs of the lane that are turned, gathered: elements
     const int turned = L == kGathered ? 2 * p.pairs - at.a : p.pairs - unit * 8;
     T *dst = nullptr;
     bool mine = false, there = false, fresh = true;
     int stage = 0;
-    while (true) {
+    while (now.left > 0) {
         if (fresh) {
-            const bool skipped = skip_absent(p, heads, now, [&](const RowAt &row, int turns) {
-                T *to = row.in<T>(side.out) + now.head * side.out.head + at.a;
-                const float zeros[8] = {};
-                for (; row.mine && has && turns > 0; --turns, to += side.out.head) {
-                    store_group(to, zeros);
-                    store_group(to + to_b, zeros);
-                }
-            });
-            if (now.left == 0) break;
-            const RowAt row(p, now.row(p));
-            if (skipped) position = position_at(p, row, pairs.axis[first_pair]);
+            const RowAt row(p, now.row(p, seq));
             mine = row.mine && has;
             there = row.there && has;
             dst = row.in<T>(side.out) + now.head * side.out.head + at.a;
             Angles angles{p, pairs, row, position, pairs.axis[first_pair]};
-            position = position_at(p, RowAt(p, now.next_row(p)), pairs.axis[first_pair]);
+            position = position_at(p, RowAt(p, now.next_row(p, seq, heads)), pairs.axis[first_pair]);
             if constexpr (L == kGathered) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -653,9 +681,18 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
             store_group(dst + to_b, f + 8);
         }
         dst += side.out.head;
-        now.next(p, heads);
-        fresh = now.head == 0 || now.left == 0;
+        now.next(p, seq, heads);
+        fresh = now.head == 0;
     }
+    if constexpr (PADDED)
+        absent_rows(p, side, block, [&](const RowAt &row) {
+            T *to = row.in<T>(side.out) + at.a;
+            const float zeros[8] = {};
+            for (int head = 0; has && head < heads; ++head, to += side.out.head) {
+                store_group(to, zeros);
+                store_group(to + to_b, zeros);
+            }
+        });
     copies_wait<0>();
     __syncthreads();
     float *const sums = reinterpret_cast<float *>(shared);
@@ -751,7 +788,7 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
+template <typename T, bool PADDED> __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
 {
     __shared__ Pairs pairs;
     __shared__ float sums[kWarps * OMNI_ROTARY_MAX_DIM];
@@ -763,12 +800,15 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
     const int heads = side.heads, lane = threadIdx.x % p.lanes;
     const Own own(p, side, lane, true);
     const float inverse_dim = 1.0f / float(p.dim);
+    __shared__ Sequences sequences[1];
+    const Sequences *const seq = sequences;
     pairs.fill(p);
+    if constexpr (PADDED) sequences->fill(p);
     __syncthreads();
     float dw[kOwn][2] = {}, c[kOwn], s[kOwn];
     bool fresh = true;
-    for (Walk now(p, block, side.blocks, heads); now.left > 0;) {
-        const RowAt row(p, now.row(p));
+    for (Walk<PADDED> now(p, seq, block, side.blocks, heads); now.left > 0;) {
+        const RowAt row(p, now.row(p, seq));
         const T *const src = row.in<T>(side.x) + now.head * side.x.head, *const grad = row.in<T>(side.dy) + now.head * side.dy.head;
         T *const dst = row.in<T>(side.out) + now.head * side.out.head;
         const int turns = min(min(kAhead, now.left), heads - now.head);
@@ -826,9 +866,17 @@ template <typename T> __global__ void __launch_bounds__(kThreads, kResident) rot
                 at[own.at[n].b] = from_float<T>(dx[1]);
             }
         }
-        now.next(p, heads, turns);
+        now.next(p, seq, heads, turns);
         fresh = now.head == 0;
     }
+    if constexpr (PADDED)
+        absent_rows(p, side, block, [&](const RowAt &row) {
+            T *to = row.in<T>(side.out);
+            for (int head = 0; head < heads; ++head, to += side.out.head)
+#pragma unroll
+                for (int n = 0; n < kOwn; ++n)
+                    if (own.has[n]) to[own.at[n].a] = to[own.at[n].b] = from_float<T>(0.0f);
+        });
 #pragma unroll
     for (int n = 0; n < kOwn; ++n)
 #pragma unroll
@@ -928,7 +976,7 @@ bool wide_view(const omni_rotary *r, const View &v)
 // The launch: lanes of a head vector, how rows and heads are dealt, blocks of either side.
 struct Shape {
     int lanes, split;
-    unsigned bundles, step, blocks[2];
+    unsigned bundles, blocks[2];
 };
 int lanes_of(const omni_rotary *r, bool wide)
 {
@@ -942,7 +990,7 @@ int lanes_of(const omni_rotary *r, bool wide)
 // make its angles each.
 Shape forward_shape(const omni_rotary *r, bool wide, int sms)
 {
-    Shape s = {lanes_of(r, wide), 1, 0, 0, {0, 0}};
+    Shape s = {lanes_of(r, wide), 1, 0, {0, 0}};
     const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length);
     const int groups = kThreads / s.lanes, most = r->heads > r->kv_heads ? r->heads : r->kv_heads;
     while (s.split < groups && s.split < most && rows * s.split < uint64_t(sms) * groups * 2) s.split *= 2;
@@ -955,12 +1003,9 @@ Shape forward_shape(const omni_rotary *r, bool wide, int sms)
 // heads; where there is less work a warp has one turn.
 Shape backward_shape(const omni_rotary *r, bool wide, int sms)
 {
-    Shape s = {lanes_of(r, wide), 1, 0, 0, {0, 0}};
+    Shape s = {lanes_of(r, wide), 1, 0, {0, 0}};
     const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length), of_bundle = 32 / s.lanes;
     s.bundles = unsigned((rows + of_bundle - 1) / of_bundle);
-    s.step = s.bundles / 2 + s.bundles / 8 + 1;       // no common divisor with their number: every bundle comes up once
-    while (std::gcd(s.step, s.bundles) != 1) ++s.step;
-    s.step %= s.bundles;
     const uint64_t all = uint64_t(sms) * kResident, q = r->heads + 2, k = r->kv_heads + 2;
     uint64_t share = all * q / (q + k);
     share = share < 1 ? 1 : share > all - 1 ? all - 1 : share;
@@ -988,7 +1033,8 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
     p->lanes = s.lanes;
     p->split = s.split;
     p->bundles = s.bundles;
-    p->step = s.step;
+    p->batch = r->batch;
+    p->padded = r->lengths && r->batch <= kMostSequences;
     p->wide_positions = r->position_type == OMNI_I64;
     p->bf16_weight = r->weight_dtype == OMNI_BF16;
     p->interleaved = r->interleaved != 0;
@@ -1028,11 +1074,15 @@ int enqueue_forward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_
                    : rotary_forward_wide_kernel<T, kGathered, NORM>, p, ForwardRing<T>::kBytes, s);
 }
 
+template <typename T, bool PADDED> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
+{
+    if (!wide) return enqueue(ctx, rotary_backward_kernel<T, PADDED>, p, 0, s);
+    return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, kNeighbours, PADDED> : p.pairs % 8 == 0 ? rotary_backward_wide_kernel<T, kHalves, PADDED>
+                   : rotary_backward_wide_kernel<T, kGathered, PADDED>, p, BackwardRing<T>::kBytes, s);
+}
 template <typename T> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
 {
-    if (!wide) return enqueue(ctx, rotary_backward_kernel<T>, p, 0, s);
-    return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, kNeighbours> : p.pairs % 8 == 0 ? rotary_backward_wide_kernel<T, kHalves>
-                   : rotary_backward_wide_kernel<T, kGathered>, p, BackwardRing<T>::kBytes, s);
+    return p.padded ? enqueue_backward<T, true>(ctx, p, wide, s) : enqueue_backward<T, false>(ctx, p, wide, s);
 }
 
 // One pass over both sides without sums: the forward call, and the gradient where there are no weights.

@@ -150,6 +150,32 @@ def test_lengths_and_what_stands_behind_them(ctx, dtype, weight, d, pairs):
     assert not bool(dirty[0][0][behind].any()) and not bool(dirty[1][1][behind].any())
     far = torch.tensor([99, -3, 1, 20], device="cuda", dtype=torch.int32)       # clamped
     assert torch.equal(r.forward(q, k, positions, *weights, lengths=far)[1], clean[1])
+    for a, b in zip(clean_grads, r.backward(q, k, positions, gq, gk, *weights, lengths=far)):
+        assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,n,d,pairs,kind", [
+    (1000, 5, 64, 32, "any"), (1024, 3, 48, 5, "any"), (1025, 3, 48, 24, "any"), (70, 40, 42, 9, "any"), (33, 300, 128, 64, "empty but one"),
+    (33, 300, 128, 64, "empty"), (2000, 7, 30, 15, "empty"), (64, 50, 32, 16, "full"), (5, 1500, 16, 8, "any"),
+])
+def test_padded_batches(ctx, dtype, b, n, d, pairs, kind):
+    """Many sequences, most of them short or empty: the backward pass walks the rows that are there alone."""
+    q, k, positions, weights = inputs(b, n, 5, 2, d, dtype, b + n, F32)
+    gen = torch.Generator(device="cuda").manual_seed(b)
+    lengths = torch.randint(-1, n + 2, (b,), device="cuda", generator=gen).int()
+    if kind != "any":
+        lengths.fill_(n if kind == "full" else 0)
+    if kind == "empty but one":
+        lengths[17] = 1
+    r = L.Rotary(ctx, 5, 2, d, L.Rotary.geometric(pairs))
+    check(ctx, q, k, positions, weights, r, lengths=lengths.clamp(0, n))
+    behind = torch.arange(n, device="cuda")[None] >= lengths[:, None]
+    q[behind], k[behind] = math.nan, math.inf
+    grads = [torch.full_like(x, 3.0) for x in (q, k)]
+    out = r.backward(q, k, positions, q, k, *weights, lengths=lengths, grads=grads)
+    assert all(bool(x.isfinite().all()) for x in out)
+    assert not bool(grads[0][behind].any()) and not bool(grads[1][behind].any())
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
