@@ -517,6 +517,7 @@ int omni_distill_step(omni_ctx *ctx, const omni_distill *d, const float *grad_lo
  * positions keep their phase), everything else in float with one rounding where a result is stored.
  * Backward, dn being the results' gradients turned back and g = w dn:
  *   dx = r (g - x r^2 mean_c(g_c x_c)),  r = (mean_c x_c^2 + eps)^(-1/2);  dw_c = sum over rows and heads of dn_c x_c r
+ * A row of zeros is zeros (with eps = 0 not a number).
  * lengths: device int32[batch] or NULL: rows from there on are not read (NaN included), their results are 0 and they are in no sum. */
 typedef struct {
     int32_t batch, length, heads, kv_heads;
@@ -577,6 +578,7 @@ typedef struct {
 /* omni_policy_logprob: logp[rows] and lse[rows] (device float) alone; old, advantage, reference, clip and kl are not looked at.
  * omni_policy_forward: loss, logp, lse.  omni_policy_backward: grad (rows x vocab of the logits' dtype, grad_stride apart) from the
  * kept lse and grad_loss[rows]; omni_policy_step: both in one pass over the logits, for a caller that knows grad_loss beforehand.
+ * logp and lse are the same bits from the three calls that return them: the ratio to an `old` that one of them gave is exactly 1.
  * grad may be the logits' own storage (same pointer and stride).  A gradient whose rows lie to 16-byte boundaries as the logits' do
  * is written in groups of eight, any other element by element.
  * Errors: NULL, BAD_CONFIG (dtype, vocab < 1, temperature, clip or kl negative or not finite, a stride below the row), ALIGN,
@@ -593,7 +595,8 @@ int omni_policy_step(omni_ctx *ctx, const omni_policy *d, const float *grad_loss
  *   g = fma(lambda_{K-1}, g_{K-1}, ... fma(lambda_0, g_0, 0));  m = fma(beta1, m, c1 g);  v = fma(c2 g, g, beta2 v)
  *   theta = fma(-rate, m / fma(sqrt(v), spread, eps), keep theta);  param_lp = bfloat16(theta)
  * c = float(1 - beta), rate = float(lr / (1 - beta1^t)), spread = float((1 - beta2^t)^(-1/2)), keep = float(1 - lr weight_decay), t = 1,
- * 2, ... the step's number.  The quotient and the root may be off by 2^-21 of themselves; m and v are exact.
+ * 2, ... the step's number.  The quotient and the root may be off by 2^-21 of themselves (a v below
+ * float's normal range counts as 0 in the root); m and v are exact.
  * bits = 8: m and v are kept as codes of the float's bits 20 to 30 (exponent and three bits of the fraction), counted from the largest
  * of their block of OMNI_ADAMW_BLOCK consecutive elements.  With top the block's largest, a code c > 0 is the float of bits (c + top - 127) << 20
  * for m, bit 7 of the byte its sign, and (c + top - 255) << 20 for v; c = 0 is 0.  theta is computed from m and v before they are
@@ -618,7 +621,7 @@ typedef struct {
  * omni_adamw_step: one step; b: host int32[K], the batches of the gradients.  The step's number is `step`, or, if clock_dev is not
  * NULL, the int64 that clock_dev (device, 8-byte aligned) holds when the kernel runs, for a step that is captured in a graph; lr is the host's.
  * omni_adamw_moments: what the codes stand for, into m[i], v[i] (HOST arrays of device float pointers, one for each tensor); 8 bits only.
- * Errors: NULL, BAD_K, BAD_CONFIG (dtype, bits, tensors written to that overlap, not a record, lr or weight_decay not finite, beta outside [0, 1), eps, step < 1), BAD_BATCH,
+ * Errors: NULL, BAD_K, BAD_CONFIG (dtype, bits, what is written overlaps other tensors, not a record, lr or weight_decay not finite, beta outside [0, 1), eps, step < 1), BAD_BATCH,
  * ALIGN, TOO_LARGE (a tensor of 2^42 elements, 2^31 pieces of 2048 in all, a record that is too small), NO_MEMORY, CUDA. */
 int omni_adamw_plan_bytes(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, uint64_t *bytes);
 int omni_adamw_plan(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, void *record, uint64_t bytes);

@@ -410,27 +410,38 @@ bool all_wide(const omni_adamw_tensor &t, int K, int bits)
     return wide;
 }
 
-// Whether what a step writes lies apart, all of it: a tensor that stands in the list twice would be updated twice at once.
-int check_apart(const omni_adamw_tensor *t, int32_t count, int32_t bits)
+// Whether what a step writes lies apart from all else that it writes or reads: a tensor that stands in the list twice would be updated
+// twice at once, a gradient that is another tensor's parameter read before or after its update.
+int check_apart(const omni_adamw_tensor *t, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits)
 {
+    struct Range {
+        uintptr_t from, to;
+        bool written;
+        bool operator<(const Range &other) const { return from < other.from; }
+    };
     try {
-        std::vector<std::pair<uintptr_t, uintptr_t>> ranges;
-        ranges.reserve(size_t(count) * 5);
-        const auto add = [&](const void *p, uint64_t bytes) {
-            if (p) ranges.emplace_back(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes);
+        std::vector<Range> ranges;
+        ranges.reserve(size_t(count) * (5 + size_t(K)));
+        const auto add = [&](const void *p, uint64_t bytes, bool written) {
+            if (p) ranges.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, written});
         };
         for (int32_t i = 0; i < count; ++i) {
             if (t[i].n == 0) continue;
             const uint64_t n = t[i].n, state = bits == 8 ? n : 4 * n;
-            add(t[i].param, 4 * n);
-            add(t[i].param_lp, 2 * n);
-            add(t[i].m, state);
-            add(t[i].v, state);
-            if (bits == 8) add(t[i].tops, (n + kBlock - 1) / kBlock * 4);
+            add(t[i].param, 4 * n, true);
+            add(t[i].param_lp, 2 * n, true);
+            add(t[i].m, state, true);
+            add(t[i].v, state, true);
+            if (bits == 8) add(t[i].tops, (n + kBlock - 1) / kBlock * 4, true);
+            for (int k = 0; k < K; ++k) add(t[i].grads[k], (grad_dtype == OMNI_BF16 ? 2 : 4) * n, false);
         }
         std::sort(ranges.begin(), ranges.end());
-        for (size_t i = 1; i < ranges.size(); ++i)
-            if (ranges[i].first < ranges[i - 1].second) return OMNI_ERR_BAD_CONFIG;
+        uintptr_t written = 0, read = 0;              // where those before end
+        for (const Range &r : ranges) {
+            if (r.from < written || (r.written && r.from < read)) return OMNI_ERR_BAD_CONFIG;
+            uintptr_t &last = r.written ? written : read;
+            if (r.to > last) last = r.to;
+        }
         return OMNI_OK;
     } catch (const std::bad_alloc &) {
         return OMNI_ERR_NO_MEMORY;
@@ -472,7 +483,7 @@ int omni_adamw_plan(const omni_adamw_tensor *tensors, int32_t count, int32_t K, 
     if (!aligned(record, 8)) return OMNI_ERR_ALIGN;
     unsigned units = 0;
     int rc = check_tensors(tensors, count, K, grad_dtype, bits, &units);
-    if (rc == OMNI_OK) rc = check_apart(tensors, count, bits);
+    if (rc == OMNI_OK) rc = check_apart(tensors, count, K, grad_dtype, bits);
     if (rc != OMNI_OK) return rc;
     const Layout at(count, K, units);
     if (bytes < at.bytes) return OMNI_ERR_TOO_LARGE;

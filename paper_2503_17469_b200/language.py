@@ -482,7 +482,7 @@ class Policy(_Operator):
             raise ValueError("temperature is positive")
         self.clip, self.clip_high, self.kl, self.temperature = clip, high, kl, temperature
 
-    def _describe(self, logits, tokens, old=None, advantage=None, reference=None):
+    def _describe(self, logits, tokens, valued: bool = False, old=None, advantage=None, reference=None):
         rows, vocab = logits.shape
         if tokens.shape != (rows,) or not tokens.is_contiguous():
             raise ValueError("logits [rows, vocab] and contiguous tokens [rows] are wanted")
@@ -492,9 +492,9 @@ class Policy(_Operator):
         if not logits.is_cuda or not logits.get_device() == device == _device():
             raise _elsewhere(logits=logits, tokens=tokens)
         at = (None, None, None)
-        if old is not None:
-            if self.kl and reference is None:
-                raise ValueError("kl needs the reference's log-probabilities")
+        if valued:
+            if old is None or advantage is None or (self.kl and reference is None):
+                raise ValueError("old, advantage and, with kl, the reference's log-probabilities are wanted")
             at = (self._row_values(old, logits, "old"), self._row_values(advantage, logits, "advantage"),
                   self._row_values(reference, logits, "reference") if self.kl else None)
         return B.omni_policy(logits.data_ptr(), rows, _rows(logits, "logits"), vocab, _code(logits, _DTYPES, "logits"), tokens.data_ptr(),
@@ -520,7 +520,7 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.forward(logits, tokens, old, advantage, reference)
-        d = self._describe(logits, tokens, old, advantage, reference)
+        d = self._describe(logits, tokens, True, old, advantage, reference)
         loss, logp, lse = old.new_empty((3, d.rows)).unbind(0)
         self._check(self._lib.omni_policy_forward(self.ctx._h, _ref(d), loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
                                                   _raw_stream(logits.get_device())))
@@ -531,7 +531,7 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.backward(logits, tokens, lse, old, advantage, grad_loss, reference, grad)
-        d = self._describe(logits, tokens, old, advantage, reference)
+        d = self._describe(logits, tokens, True, old, advantage, reference)
         grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_policy_backward(
             self.ctx._h, _ref(d), self._row_values(lse, logits, "lse"), self._row_values(grad_loss, logits, "grad_loss"), grad.data_ptr(),
@@ -544,7 +544,7 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.step(logits, tokens, old, advantage, grad_loss, reference, grad)
-        d = self._describe(logits, tokens, old, advantage, reference)
+        d = self._describe(logits, tokens, True, old, advantage, reference)
         weights = self._row_values(grad_loss, logits, "grad_loss")
         loss, logp, lse = old.new_empty((3, d.rows)).unbind(0)
         grad = self._grad_like(logits, grad)

@@ -16,7 +16,7 @@ def omni():
     return B.Omni(1, 1, 1, 1)
 
 
-def tensor(at=PTR, grads=(PTR, PTR), **kw):
+def tensor(at=PTR, grads=(1 << 28, 1 << 28), **kw):
     d = dict(param=at, param_lp=at + (1 << 16), grads=(C.c_void_p * 2)(*grads) if grads else None, m=at + (2 << 16), v=at + (3 << 16),
              tops=at + (4 << 16), n=5000, weight_decay=0.1)
     d.update(kw)
@@ -37,9 +37,9 @@ def step(ctx, record, dev=PTR, b=(1, 2), lr=0.1, beta1=0.9, beta2=0.9, eps=1e-8,
 
 
 @pytest.mark.parametrize("change,status", [
-    (dict(param=None), B.ERR_NULL), (dict(grads=None), B.ERR_NULL), (dict(grads=(PTR, 0)), B.ERR_NULL), (dict(m=None), B.ERR_NULL),
+    (dict(param=None), B.ERR_NULL), (dict(grads=None), B.ERR_NULL), (dict(grads=(1 << 28, 0)), B.ERR_NULL), (dict(m=None), B.ERR_NULL),
     (dict(v=None), B.ERR_NULL), (dict(tops=None), B.ERR_NULL), (dict(param=PTR + 2), B.ERR_ALIGN), (dict(param_lp=PTR + 1), B.ERR_ALIGN),
-    (dict(grads=(PTR, PTR + 1)), B.ERR_ALIGN), (dict(tops=PTR + (4 << 16) + 2), B.ERR_ALIGN), (dict(weight_decay=math.nan), B.ERR_BAD_CONFIG),
+    (dict(grads=(1 << 28, (1 << 28) + 1)), B.ERR_ALIGN), (dict(tops=PTR + (4 << 16) + 2), B.ERR_ALIGN), (dict(weight_decay=math.nan), B.ERR_BAD_CONFIG),
     (dict(n=1 << 42), B.ERR_TOO_LARGE), (dict(n=(1 << 42) - 1), B.ERR_TOO_LARGE),
 ])
 def test_refuses_tensors(change, status):
@@ -58,6 +58,16 @@ def test_refuses_results_that_overlap(change):
     assert plan(tensor(), tensor())[1] == B.ERR_BAD_CONFIG
     assert plan(tensor(), tensor(1 << 25))[1] == B.OK
     assert plan(tensor(n=0), tensor(n=0), tensor())[1] == B.OK               # nothing is written there
+
+
+@pytest.mark.parametrize("at,status", [
+    (PTR, B.ERR_BAD_CONFIG), (PTR + 4 * 5000 - 2, B.ERR_BAD_CONFIG), (PTR - 2 * 5000 + 2, B.ERR_BAD_CONFIG), (PTR - 2 * 5000, B.OK),
+    (PTR + (2 << 16) + 4000, B.ERR_BAD_CONFIG), (PTR + 4 * 5000, B.OK),
+])
+def test_refuses_gradients_that_a_step_writes(at, status):
+    elsewhere = 1 << 24
+    assert plan(tensor(grads=(elsewhere, at)))[1] == status
+    assert plan(tensor(1 << 25, grads=(at, elsewhere)), tensor(grads=(elsewhere, elsewhere)))[1] == status
 
 
 def test_record(omni):

@@ -294,7 +294,8 @@ def test_refusals(ctx):
     z, tokens, old, advantage, reference, gl = inputs(4, 300, F32, torch.int64, 10, p)
     for bad in (lambda: L.Policy(ctx, -0.1), lambda: L.Policy(ctx, 0.1, math.inf), lambda: L.Policy(ctx, kl=-1.0),
                 lambda: L.Policy(ctx, kl=math.nan), lambda: L.Policy(ctx, temperature=0.0),
-                lambda: p.forward(z, tokens, old, advantage), lambda: p.forward(z, tokens[:3], old, advantage, reference),
+                lambda: p.forward(z, tokens, old, advantage), lambda: p.forward(z, tokens, None, advantage, reference),
+                lambda: p.step(z, tokens, old, None, gl, reference), lambda: p.forward(z, tokens[:3], old, advantage, reference),
                 lambda: p.forward(z, tokens, old[:3], advantage, reference), lambda: p.forward(z, tokens, old, advantage.double(), reference),
                 lambda: p.forward(z.t(), tokens, old, advantage, reference), lambda: p.logprob(z, tokens.cpu()),
                 lambda: p.logprob(z, torch.stack([tokens, tokens], 1)[:, 0]),

@@ -215,10 +215,10 @@ def test_strides_alignment_and_places_in_a_cache(ctx, dtype, shift, row, head):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("weight", [None, F32])
-@pytest.mark.parametrize("d", [64, 42])
-def test_in_place(ctx, dtype, weight, d):
+@pytest.mark.parametrize("d,pairs", [(64, 32), (42, 21), (64, 13), (128, 20), (256, 100)])
+def test_in_place(ctx, dtype, weight, d, pairs):
     q, k, positions, weights = inputs(2, 50, 4, 2, d, dtype, 5, weight)
-    r = L.Rotary(ctx, 4, 2, d, L.Rotary.geometric(d // 2), interleaved=d == 42)
+    r = L.Rotary(ctx, 4, 2, d, L.Rotary.geometric(pairs), interleaved=d == 42)
     want = r.forward(q, k, positions, *weights)
     gq, gk = torch.randn_like(want[0]), torch.randn_like(want[1])
     want_grads = r.backward(q, k, positions, gq, gk, *weights)
