@@ -389,8 +389,8 @@ uint64_t omni_kernel_launches(const omni_ctx *ctx);
 
 /* ==================================================================================================
  * Operators of a language model's training pass: what a worker computes its gradients with.  The
- * embedding at the bottom (its dense gradient is a slice of a gradient bucket), attention in the
- * blocks, the distillation loss on top.  They take the context of the step for their launches,
+ * embedding at the bottom (its dense gradient is a slice of a gradient bucket), head norms with rotation and attention in the
+ * blocks, the distillation or the policy loss on top; and AdamW on the workers' weighted gradients.  They take the context of the step for their launches,
  * their errors and the status word of bounded waits; scratch memory is the caller's (a query
  * function gives its size), so calls on different streams are independent as long as their
  * buffers are.  Kernels are enqueued on `stream`; nothing synchronises.  Sums, norms and softmax

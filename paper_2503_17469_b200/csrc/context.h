@@ -1,4 +1,4 @@
-// What the operators of a language model (embed.cu, attention.cu, distill.cu) need of a context.
+// What the operators of a language model (embed.cu, attention.cu, distill.cu, rotary.cu, policy.cu, adamw.cu) need of a context.
 // The context itself is omni.cu's; these three calls are the whole seam.
 #pragma once
 #include <cuda_runtime.h>

@@ -4,8 +4,17 @@
 // logp; the gradient is w ([v = t] - exp(z_v / T - lse)) with w = grad_loss c / T.  The floor is one read of the logits and one
 // write of the gradient.
 //
-// A CTA owns a row.  The first walk keeps a running maximum and sum per thread, the second finds the row, which the same CTA
-// read a moment ago, in L2.  A row whose weight is zero (its ratio is clipped) is not walked again: zeros are written.
+// A CTA owns a row.  The first walk keeps a running maximum and sum per thread; its groups come by asynchronous copies, 128 bytes a
+// thread in flight, into places of the thread's own.  The second finds the row, which the same CTA read a moment ago, in L2, and marks its
+// lines as the first to leave.  A row whose weight is zero (its ratio is clipped) is not walked again: zeros are written.
+// What bounds it: the gradient alone the memory (4096 x 32000 float 154 us, 6.8 TB/s); log-probabilities the memory beside one exponential an
+// element, 74 % of the special-function units (3000 x 131072 bfloat16 122-135 us, floor 120); the step two exponentials and two reads of L2 (8192 x
+// 50257 bfloat16, rows on 2-byte boundaries, 287 us, 323 when the 1000 W cap has brought the clock down to 1.6 GHz; floor 252).
+// Rows in flight have to stay in L2 between their walks: four CTAs of 256 an SM (59 MB) 287 us, five 336, six 372, three 309.  So the
+// threads of a row follow its bytes: 32 for 8 KB (16384 x 1000 bfloat16 30 us, with 128 threads 53), 512 for 128 KB and more (3000 x 131072
+// 301 us, with 256 threads 338).
+// Tried for the step: the row held in shared memory, two CTAs of 512 an SM 329 us, the same with the next row's loads behind the gradient 339; a batch
+// of loads in registers instead of the asynchronous ones 327.
 #include "context.h"
 #include "row_softmax.cuh"
 

@@ -5,7 +5,21 @@
 //   y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin.
 // Backward, from x and dy: dn is dy turned back, dw_c = sum of dn_c x_c r over all rows and heads of the side, and with g = w dn
 //   dx = r (g - x r^2 mean_c(g_c x_c)).
-// Without weights the gradient is the rotation by the opposite angle.
+// Without weights the gradient is the rotation by the opposite angle.  Floors: one read and one write of the heads; backward two reads.
+//
+// A group of lanes has a head vector, sixteen elements a lane, fetched ahead into shared memory by asynchronous copies: no registers
+// wait for them, and no barrier stands between rows.  An angle belongs to a row, so a group keeps its row's angles in registers for all
+// heads.  Angles are taken in whole numbers of 2^-64 turns and turned into sines by Taylor's series after the nearest quadrant:
+// about 35 instructions a pair, where products in 64-bit floats and the library's function took about 100.
+// Forward: blocks of rows, more of them than fit at once; blocks that stay, with the turns dealt out evenly, took 66-75 us where these
+// take 58.  Backward: blocks that stay, so that a weight's gradient is summed in registers and 296 partial sums are joined by a second launch;
+// the turns of all rows (of a padded batch those before the lengths alone) are dealt to the warps in equal parts.
+// Measured: 4 x 4096, 32 heads on 8 of 128 bfloat16, forward 58 us (floor 51); backward 2 x 8192, 16 heads on 8 of 128, 61 us (floor 46): the
+// kernel 53, bound by its 320 instructions a turn at 58 % of the issue slots (16 warps an SM at 128 registers), the join 5; 6 x 1777 of 80, float,
+// padded, a quarter of the rows there, 36 us; a single token of 16 sequences 4.6 us.  Rows that no 16-byte access fits, or heads
+// that are no multiple of 16, run element by element: 4751 rows of 16 heads of 84 bfloat16 35 us (floor 4).
+// Tried for the backward kernel: loads by registers 111 us; angles of a tile in shared memory between barriers 68-82; weights and angles read from
+// shared memory at each turn for a third block an SM 84 (spills); groups of five lanes for a head of 80 39 instead of 36.
 #include "context.h"
 #include "vector.cuh"
 
@@ -533,7 +547,8 @@ __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forwa
 template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 3;
 template <typename T> using BackwardRing = Ring<T, 4, kBackwardStages<T>>;
 
-// Backward of the norm and the rotation: blocks that stay, each on rows of one side, with the weight's gradient in registers.
+// Backward of the norm and the rotation: blocks that stay, each on rows of one side, with the weight's gradient in registers.  Two an
+// SM: a turn holds x, dy, angles, weights and sums of sixteen elements each, 120 registers and more.
 template <typename T, Layout L, bool PADDED>
 __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kernel(const __grid_constant__ RotaryParams p)
 {

@@ -1,4 +1,5 @@
-"""Operators of a language model's training pass: embedding, attention, distillation loss.
+"""Operators of a language model's training pass: embedding, head norms with rotation, attention, distillation and policy
+losses; AdamW on the workers' gradients.
 
 What a worker computes its gradients with, on torch tensors of the current CUDA device.  Each class keeps an
 operator's constants and an ``Omni`` context (launch counts, errors, the status word of bounded
