@@ -412,11 +412,14 @@ class Rotary(_Operator):
         if t.dtype is not dtype:
             raise TypeError(f"{what}: dtype {t.dtype} is not that of q, {dtype}")
         v = self._views[i]
-        if t.shape != shape or t.get_device() != device or t.stride(3) != 1:
+        if t.shape != shape or t.get_device() != device:
+            one = 0
+        else:
+            v.batch, v.row, v.head, one = t.stride()
+        if one != 1:
             raise ValueError(f"{what}: shape {shape} with a contiguous last dimension on the current device is wanted, "
                              f"got {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
         v.data = t.data_ptr()
-        v.batch, v.row, v.head, _ = t.stride()
         return self._view_refs[i]
 
     def forward(self, q, k, positions, q_weight=None, k_weight=None, lengths=None, out=None, stream=None):
@@ -472,7 +475,8 @@ class Rotary(_Operator):
 class Policy(_Operator):
     """Clipped policy loss on sampled tokens, with ``kl`` times a divergence from a reference policy, per row of logits.
     The ratio to the sampling policy is clipped to 1 - ``clip`` .. 1 + ``clip_high`` (default ``clip``).  A token of -1 marks a row
-    without one (a prompt's, padding): loss 0, log-probability 0 and no gradient, whatever its other values are."""
+    without one (a prompt's, padding): loss 0, log-probability 0 and no gradient, whatever its other values are.  Like its context, an object
+    takes one call at a time."""
 
     def __init__(self, ctx: "B.Omni", clip: float = 0.2, clip_high: Optional[float] = None, kl: float = 0.0, temperature: float = 1.0):
         super().__init__(ctx)
@@ -482,6 +486,8 @@ class Policy(_Operator):
         if not temperature > 0:
             raise ValueError("temperature is positive")
         self.clip, self.clip_high, self.kl, self.temperature = clip, high, kl, temperature
+        self._call = B.omni_policy()                  # filled at each call
+        self._call_ref = _ref(self._call)
 
     def _describe(self, logits, tokens, valued: bool = False, old=None, advantage=None, reference=None):
         rows, vocab = logits.shape
@@ -492,16 +498,23 @@ class Policy(_Operator):
         device = tokens.get_device()
         if not logits.is_cuda or not logits.get_device() == device == _device():
             raise _elsewhere(logits=logits, tokens=tokens)
-        at = (None, None, None)
+        d, n = self._call, (rows,)
+        d.logits, d.rows, d.row_stride, d.vocab, d.dtype = logits.data_ptr(), rows, _rows(logits, "logits"), vocab, _code(logits, _DTYPES, "logits")
+        d.tokens, d.index_type, d.temperature = tokens.data_ptr(), _code(tokens, _INDEX, "tokens"), self.temperature
         if valued:
+            d.clip_low, d.clip_high, d.kl = self.clip, self.clip_high, self.kl
             if old is None or advantage is None or (self.kl and reference is None):
                 raise ValueError("old, advantage and, with kl, the reference's log-probabilities are wanted")
-            at = (self._row_values(old, logits, "old"), self._row_values(advantage, logits, "advantage"),
-                  self._row_values(reference, logits, "reference") if self.kl else None)
-        return B.omni_policy(logits.data_ptr(), rows, _rows(logits, "logits"), vocab, _code(logits, _DTYPES, "logits"), tokens.data_ptr(),
-                             *at, _code(tokens, _INDEX, "tokens"), self.clip, self.clip_high, self.kl, self.temperature)
+            d.old, d.advantage = self._row_values(old, n, device, "old"), self._row_values(advantage, n, device, "advantage")
+            d.reference = self._row_values(reference, n, device, "reference") if self.kl else None
+        return n, device
 
-    _row_values = staticmethod(Distillation._row_values)
+    @staticmethod
+    def _row_values(t, shape, device: int, what: str) -> int:
+        if t.dtype is not _float or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+            raise ValueError(f"{what}: contiguous float32 [rows] on the logits' device is wanted")
+        return t.data_ptr()
+
     _grad_like = staticmethod(Distillation._grad_like)
 
     def logprob(self, logits, tokens, stream=None):
@@ -510,9 +523,10 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.logprob(logits, tokens)
-        d = self._describe(logits, tokens)
-        logp, lse = logits.new_empty((2, d.rows), dtype=_float).unbind(0)
-        self._check(self._lib.omni_policy_logprob(self.ctx._h, _ref(d), logp.data_ptr(), lse.data_ptr(), _raw_stream(logits.get_device())))
+        n, device = self._describe(logits, tokens)
+        logp = logits.new_empty(n, dtype=_float)
+        lse = _like(logp)
+        self._check(self._lib.omni_policy_logprob(self.ctx._h, self._call_ref, logp.data_ptr(), lse.data_ptr(), _raw_stream(device)))
         return logp, lse
 
     def forward(self, logits, tokens, old, advantage, reference=None, stream=None):
@@ -521,10 +535,10 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.forward(logits, tokens, old, advantage, reference)
-        d = self._describe(logits, tokens, True, old, advantage, reference)
-        loss, logp, lse = old.new_empty((3, d.rows)).unbind(0)
-        self._check(self._lib.omni_policy_forward(self.ctx._h, _ref(d), loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
-                                                  _raw_stream(logits.get_device())))
+        _, device = self._describe(logits, tokens, True, old, advantage, reference)
+        loss, logp, lse = _like(old), _like(old), _like(old)
+        self._check(self._lib.omni_policy_forward(self.ctx._h, self._call_ref, loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
+                                                  _raw_stream(device)))
         return loss, logp, lse
 
     def backward(self, logits, tokens, lse, old, advantage, grad_loss, reference=None, grad=None, stream=None):
@@ -532,11 +546,11 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.backward(logits, tokens, lse, old, advantage, grad_loss, reference, grad)
-        d = self._describe(logits, tokens, True, old, advantage, reference)
+        n, device = self._describe(logits, tokens, True, old, advantage, reference)
         grad = self._grad_like(logits, grad)
         self._check(self._lib.omni_policy_backward(
-            self.ctx._h, _ref(d), self._row_values(lse, logits, "lse"), self._row_values(grad_loss, logits, "grad_loss"), grad.data_ptr(),
-            _rows(grad, "grad"), _raw_stream(logits.get_device())))
+            self.ctx._h, self._call_ref, self._row_values(lse, n, device, "lse"), self._row_values(grad_loss, n, device, "grad_loss"),
+            grad.data_ptr(), _rows(grad, "grad"), _raw_stream(device)))
         return grad
 
     def step(self, logits, tokens, old, advantage, grad_loss, reference=None, grad=None, stream=None):
@@ -545,12 +559,12 @@ class Policy(_Operator):
         if stream is not None:
             with self._on_stream(stream):
                 return self.step(logits, tokens, old, advantage, grad_loss, reference, grad)
-        d = self._describe(logits, tokens, True, old, advantage, reference)
-        weights = self._row_values(grad_loss, logits, "grad_loss")
-        loss, logp, lse = old.new_empty((3, d.rows)).unbind(0)
+        n, device = self._describe(logits, tokens, True, old, advantage, reference)
+        weights = self._row_values(grad_loss, n, device, "grad_loss")
+        loss, logp, lse = _like(old), _like(old), _like(old)
         grad = self._grad_like(logits, grad)
-        self._check(self._lib.omni_policy_step(self.ctx._h, _ref(d), weights, loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
-                                               grad.data_ptr(), _rows(grad, "grad"), _raw_stream(logits.get_device())))
+        self._check(self._lib.omni_policy_step(self.ctx._h, self._call_ref, weights, loss.data_ptr(), logp.data_ptr(), lse.data_ptr(),
+                                               grad.data_ptr(), _rows(grad, "grad"), _raw_stream(device)))
         return loss, logp, lse, grad
 
 
