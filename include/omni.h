@@ -538,7 +538,7 @@ typedef struct {
 #define OMNI_ROTARY_MAX_DIM 256
 #define OMNI_ROTARY_MAX_AXES 4
 /* Operands are omni_attn_views of dtype (element (b, i, h, c) at data[b * batch + i * row + h * head + c]), aligned as their elements;
- * on 16-byte boundaries throughout, with dim a multiple of 16, they run with wide accesses.  A result may be its operand's own storage (same pointer and strides).
+ * on 16-byte boundaries throughout, with dim a multiple of 16, they run with wide accesses, otherwise with those of 8, 4 or 2 bytes.  A result may be its operand's own storage (same pointer and strides).
  * omni_rotary_backward: dq_out, dk_out are the gradients of the forward call's results, dq and dk those of q and k.  With weights it
  * writes their gradients, dim values each of weight_grad_dtype (zeros if there are no rows), and needs a workspace (device,
  * 16-byte aligned, omni_rotary_workspace() bytes); without weights q, k, the weight gradients and the workspace are not looked at.

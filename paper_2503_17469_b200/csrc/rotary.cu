@@ -7,7 +7,7 @@
 //   dx = r (g - x r^2 mean_c(g_c x_c)).
 // Without weights the gradient is the rotation by the opposite angle.  Floors: one read and one write of the heads; backward two reads.
 //
-// A group of lanes has a head vector, sixteen elements a lane, fetched ahead into shared memory by asynchronous copies: no registers
+// A group of lanes has a head vector, up to sixteen elements a lane, fetched ahead into shared memory by asynchronous copies: no registers
 // wait for them, and no barrier stands between rows.  An angle belongs to a row, so a group keeps its row's angles in registers for all
 // heads.  Angles are taken in whole numbers of 2^-64 turns and turned into sines by Taylor's series after the nearest quadrant:
 // about 35 instructions a pair, where products in 64-bit floats and the library's function took about 100.
@@ -16,14 +16,17 @@
 // the turns of all rows (of a padded batch those before the lengths alone) are dealt to the warps in equal parts.
 // Measured: 4 x 4096, 32 heads on 8 of 128 bfloat16, forward 58 us (floor 51); backward 2 x 8192, 16 heads on 8 of 128, 61 us (floor 46): the
 // kernel 53, bound by its 320 instructions a turn at 58 % of the issue slots (16 warps an SM at 128 registers), the join 5; 6 x 1777 of 80, float,
-// padded, a quarter of the rows there, 36 us; a single token of 16 sequences 4.6 us.  Rows that no 16-byte access fits, or heads
-// that are no multiple of 16, run element by element: 4751 rows of 16 heads of 84 bfloat16 35 us (floor 4).
+// padded, a quarter of the rows there, 36 us; a single token of 16 sequences 4.6 us.
+// Heads or halves that no 16-byte access fits take 8 or 4 bytes at a time, the lanes of a head side by side (sixteen elements in a row
+// to a lane: up to twice the time, from the pieces of sectors that are stored): 4751 rows of 16 heads on 4 of 84 bfloat16 18 us (floor 5), backward 29
+// (7), 2 x 4096 of 16 on 8 of 250 float 90 (60) and 143 (90).  Element by element those took 37, 51, 91 and 138.
 // Tried for the backward kernel: loads by registers 111 us; angles of a tile in shared memory between barriers 68-82; weights and angles read from
 // shared memory at each turn for a third block an SM 84 (spills); groups of five lanes for a head of 80 39 instead of 36.
 #include "context.h"
 #include "vector.cuh"
 
 #include <cmath>
+#include <initializer_list>
 #include <type_traits>
 
 namespace omni {
@@ -124,11 +127,12 @@ __device__ __forceinline__ void cos_sin(uint32_t angle, float *c, float *s)
 // A block's copy of the pairs' frequencies (0, which gives cosine 1 and sine 0, for those that are not rotated) and axes: asked of the
 // parameters, every lane another, they are slow.
 struct Pairs {
-    unsigned long long frequency[kMaxPairs];
-    unsigned char axis[kMaxPairs];
+    static constexpr int kCount = kMaxPairs + 1;      // the last is never turned
+    unsigned long long frequency[kCount];
+    unsigned char axis[kCount];
     __device__ __forceinline__ void fill(const RotaryParams &p)
     {
-        for (int i = threadIdx.x; i < kMaxPairs; i += kThreads) {
+        for (int i = threadIdx.x; i < kCount; i += kThreads) {
             frequency[i] = i < p.pairs ? p.frequency[i] : 0;
             axis[i] = i < p.pairs ? p.axis[i] : 0;
         }
@@ -156,11 +160,6 @@ struct Angles {
     {
         if (p.axes > 1 && pairs.axis[pair] != axis) position = position_at(p, row, axis = pairs.axis[pair]);
         cos_sin(uint32_t(position * pairs.frequency[pair] >> 32), c, s);
-    }
-    __device__ __forceinline__ void two(int pair, float2 *c, float2 *s)
-    {
-        at(pair, &c->x, &s->x);
-        at(pair + 1, &c->y, &s->y);
     }
 };
 
@@ -293,16 +292,120 @@ template <Layout L> __device__ __forceinline__ Place wide_place(const RotaryPara
     return L == kHalves ? place<8>(p, unit) : Place{16 * unit, 16 * unit + 8};
 }
 
+// A lane's two chunks of eight, as it reads and writes them.  GRAIN: bytes of an access.  16: a chunk is eight elements in a row.  Below, where
+// operands or halves do not begin on groups of eight, it is runs of a few, the lanes of a head side by side, so that an access of a
+// warp still is a few whole pieces of memory; some runs may not exist, and count as zeros.
+template <typename T, Layout L, int GRAIN> struct Lane {
+    // elements of an access and of a run, runs of a chunk
+    enum : int { kLeast = GRAIN / int(sizeof(T)), kEach = GRAIN == 16 ? kGroup : L == kNeighbours && kLeast < 2 ? 2 : kLeast, kRuns = kGroup / kEach };
+    bool has;
+    int unit, start, to_b;                            // the place of the first element; 16: from there to the other chunk
+    int step, turned_runs, runs[2];                   // from run to run; those of pairs that are turned; those of either chunk that exist
+    int pairs, half;                                  // what is not turned is dealt in two halves, from 2 * pairs on
+    __device__ __forceinline__ Lane(const RotaryParams &p, int lane) : unit(lane), pairs(p.pairs)
+    {
+        if constexpr (GRAIN == 16) {
+            has = lane * 16 < p.dim;
+            if (!has) unit = 0;
+            const Place at = wide_place<L>(p, unit);
+            start = at.a;
+            to_b = at.b - at.a;
+        } else {
+            start = lane * kEach;
+            step = p.lanes * kEach;
+            const auto before = [&](int end) { return max(0, min(int(kRuns), (end - start + step - 1) / step)); };       // runs that begin before `end`
+            if constexpr (L == kNeighbours) {
+                runs[0] = before(p.dim);
+                runs[1] = max(0, min(int(kRuns), (p.dim - start - kRuns * step + step - 1) / step));
+            } else {
+                const int rest = (p.dim - 2 * pairs) / kEach;
+                half = (rest + 1) / 2 * kEach;
+                turned_runs = before(pairs);
+                runs[0] = before(pairs + half);
+                runs[1] = max(turned_runs, before(p.dim - pairs - half));
+            }
+            has = runs[0] > 0;
+        }
+    }
+    // from `start` to run i of a chunk
+    __device__ __forceinline__ int offset(int chunk, int i) const
+    {
+        if constexpr (GRAIN == 16) return chunk ? to_b : 0;
+        else if constexpr (L == kNeighbours) return (chunk * kRuns + i) * step;
+        else return i * step + (i < turned_runs ? chunk ? pairs : 0 : chunk ? pairs + half : pairs);
+    }
+    __device__ __forceinline__ bool there(int chunk, int i) const { return GRAIN == 16 || i < runs[chunk]; }
+    // Of the sixteen elements in the order of the chunks, element x: its place in the head vector, and whether it exists.
+    __device__ __forceinline__ int element(int x) const { return start + offset(x / kGroup, x % kGroup / kEach) + x % kEach; }
+    __device__ __forceinline__ bool exists(int x) const { return there(x / kGroup, x % kGroup / kEach); }
+    // Pair j of the eight.
+    __device__ __forceinline__ int pair(int j) const
+    {
+        if constexpr (GRAIN == 16) return unit * 8 + j;
+        else if constexpr (L == kNeighbours) return min(element(2 * j) / 2, pairs);
+        else return min(start + j / kEach * step + j % kEach, pairs);
+    }
+    // How many of its leading pairs are turned; eight as well if only such exist.
+    __device__ __forceinline__ int turned() const
+    {
+        if constexpr (GRAIN == 16) {
+            return L == kGathered ? 2 * pairs - start : pairs - unit * 8;
+        } else {
+            int n = 0, all = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool is = exists(L == kNeighbours ? 2 * j : j);
+                n += is && pair(j) < pairs;
+                all += is;
+            }
+            return n == all ? 8 : n;
+        }
+    }
+    __device__ __forceinline__ void put(T *to, const float *f) const
+    {
+#pragma unroll
+        for (int chunk = 0; chunk < 2; ++chunk) {
+            if constexpr (GRAIN == 16) {
+                store_group(to + offset(chunk, 0), f + 8 * chunk);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRuns; ++i) {
+                    if (!there(chunk, i)) break;
+                    put_run(to + offset(chunk, i), f + 8 * chunk + i * kEach);
+                }
+            }
+        }
+    }
+    static __device__ __forceinline__ uint32_t word(const float *f)
+    {
+        if constexpr (sizeof(T) == 4) return __float_as_uint(f[0]);
+        const __nv_bfloat162 x = __floats2bfloat162_rn(f[0], f[1]);
+        return *reinterpret_cast<const uint32_t *>(&x);
+    }
+    static __device__ __forceinline__ void put_run(T *to, const float *f)
+    {
+#pragma unroll
+        for (int e = 0; e < kEach; e += kLeast) {
+            if constexpr (GRAIN == 8) *reinterpret_cast<uint2 *>(to + e) = make_uint2(word(f + e), word(f + e + kLeast / 2));
+            else *reinterpret_cast<uint32_t *>(to + e) = word(f + e);
+        }
+    }
+};
+
 // Eight elements in shared memory: pieces of 16 bytes, each piece of all threads side by side.
 template <typename T> constexpr int kPieces = int(sizeof(T)) / 2;
 __device__ __forceinline__ void copy_async(uint32_t to, const void *from)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+template <int GRAIN> __device__ __forceinline__ void copy_async_grain(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(GRAIN) : "memory");
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// CHUNKS chunks of eight elements a stage.
+// CHUNKS chunks of eight elements a stage.  The start is on 128 bytes, so that a warp's 512 are four whole lines: backward 61 us, 65 without.
 template <typename T, int CHUNKS, int STAGES> struct Ring {
     static constexpr int kStage = CHUNKS * kPieces<T> * kThreads * 16;
     static constexpr int kBytes = STAGES * kStage;
@@ -314,6 +417,27 @@ template <typename T, int CHUNKS, int STAGES> struct Ring {
 #pragma unroll
         for (int i = 0; i < kPieces<T>; ++i)
             copy_async(shared + stage * kStage + (chunk * kPieces<T> + i) * kThreads * 16, reinterpret_cast<const char *>(from) + 16 * i);
+    }
+    // A lane's two chunks, from the first one's start on.
+    template <Layout L, int GRAIN> __device__ __forceinline__ void fetch(int stage, int chunk, const T *from, const Lane<T, L, GRAIN> &lane) const
+    {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if constexpr (GRAIN == 16) {
+                fetch(stage, chunk + c, from + lane.offset(c, 0));
+            } else {
+                const uint32_t to = shared + stage * kStage + (chunk + c) * kPieces<T> * kThreads * 16;
+#pragma unroll
+                for (int i = 0; i < lane.kRuns; ++i) {
+                    if (!lane.there(c, i)) break;
+#pragma unroll
+                    for (int e = 0; e < lane.kEach; e += lane.kLeast) {
+                        const int o = (i * lane.kEach + e) * int(sizeof(T));
+                        copy_async_grain<GRAIN>(to + o / 16 * kThreads * 16 + o % 16, from + lane.offset(c, i) + e);
+                    }
+                }
+            }
+        }
     }
     // Zeros in place of what is not there: a turn's sums need no cases then.
     __device__ __forceinline__ void clear(int stage) const
@@ -372,17 +496,11 @@ struct Weights {
     }
 };
 __device__ __forceinline__ float2 two(const float *f, int i) { return *reinterpret_cast<const float2 *>(f + i); }
-// Those of pairs 2 i and 2 i + 1 of a unit, first and second elements.
-template <Layout L> __device__ __forceinline__ void weights_of(const Weights &weights, Place at, int i, float2 *a, float2 *b)
+// Those of a lane's sixteen elements, in the order of the chunks.
+template <typename T, Layout L, int GRAIN> __device__ __forceinline__ void weights_of(const Weights &weights, const Lane<T, L, GRAIN> &lane, float *w)
 {
-    if (L == kNeighbours) {
-        const float2 x = two(weights.w, at.a + 4 * i), y = two(weights.w, at.a + 4 * i + 2);
-        *a = make_float2(x.x, y.x);
-        *b = make_float2(x.y, y.y);
-    } else {
-        *a = two(weights.w, at.a + 2 * i);
-        *b = two(weights.w, at.b + 2 * i);
-    }
+#pragma unroll
+    for (int x = 0; x < 16; ++x) w[x] = lane.exists(x) ? weights.w[lane.element(x)] : 0.0f;
 }
 
 // What a pair's other element adds to one that is not turned is nothing, whatever it is (a product with a sine of 0 would carry infinities and
@@ -418,10 +536,10 @@ template <typename T> using ForwardRing = Ring<T, 2, kForwardStages<T>>;
 
 // Forward: a group of lanes has a row of one side.  With weights they are folded into the angles, and a result is
 // y_a = r ((w_a cos) x_a - (w_b sin) x_b), y_b = r ((w_b cos) x_b + (w_a sin) x_a).
-template <typename T, Layout L, bool NORM>
+template <typename T, Layout L, bool NORM, int GRAIN>
 __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
-    extern __shared__ __align__(16) char shared[];
+    extern __shared__ __align__(128) char shared[];
     __shared__ Pairs pairs;
     __shared__ __align__(16) Weights weights;
     constexpr int kStages = kForwardStages<T>;
@@ -430,18 +548,16 @@ __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forwa
     const Side &side = p.side[keys];
     const Share me(p, side.heads);
     const RowAt row(p, (blockIdx.x - (keys ? p.side[0].blocks : 0u)) * rows_of_block(p) + me.row);
-    const bool has = me.lane * 16 < p.dim;
-    const int unit = has ? me.lane : 0;
-    const Place at = wide_place<L>(p, unit);
-    const int to_b = at.b - at.a;
-    const T *src = row.in<T>(side.x) + me.first * side.x.head + at.a;
-    T *dst = row.in<T>(side.out) + me.first * side.out.head + at.a;
+    const Lane<T, L, GRAIN> mine(p, me.lane);
+    const bool has = mine.has;
+    const int from = mine.start;
+    const T *src = row.in<T>(side.x) + me.first * side.x.head + from;
+    T *dst = row.in<T>(side.out) + me.first * side.out.head + from;
     const unsigned long long src_step = p.split * side.x.head, dst_step = p.split * side.out.head;
     int ahead = row.there && has ? me.first : side.heads;               // the next head to be fetched
     const auto fetch = [&](int stage) {
         if (ahead < side.heads) {
-            ring.fetch(stage, 0, src);
-            ring.fetch(stage, 1, src + to_b);
+            ring.fetch(stage, 0, src, mine);
             src += src_step;
             ahead += p.split;
         } else {
@@ -449,6 +565,8 @@ __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forwa
         }
         copies_commit();
     };
+    if constexpr (GRAIN < 16)
+        for (int j = 0; j < kStages; ++j) ring.clear(j);
 #pragma unroll
     for (int j = 0; j < kStages - 1; ++j) fetch(j);
     pairs.fill(p);
@@ -458,27 +576,30 @@ __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forwa
     // cos and sin, with weights those times w_a and w_b, sb with its sign; gathered: of an element and of its partner
     float2 ca[kCoefficients], sa[kCoefficients], cb[4], sb[4];
     uint32_t offset[8];
-    const int first_pair = L == kGathered ? Partner(p, at.a, false).pair : unit * 8;
+    const int first_pair = L == kGathered ? Partner(p, from, false).pair : mine.pair(0);
     Angles angles{p, pairs, row, position_at(p, row, pairs.axis[first_pair]), pairs.axis[first_pair]};
     if constexpr (L == kGathered) {
-        partner_offsets<ForwardRing<T>>(p, int(threadIdx.x) - me.lane, 0, at.a, offset);
+        partner_offsets<ForwardRing<T>>(p, int(threadIdx.x) - me.lane, 0, from, offset);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const Partner x(p, at.a + 2 * e, false), y(p, at.a + 2 * e + 1, false);
+            const Partner x(p, from + 2 * e, false), y(p, from + 2 * e + 1, false);
             angles.at(x.pair, &ca[e].x, &sa[e].x);
             angles.at(y.pair, &ca[e].y, &sa[e].y);
             sa[e] = mul2(sa[e], make_float2(x.sign, y.sign));
             if constexpr (NORM) {
-                ca[e] = mul2(ca[e], two(weights.w, at.a + 2 * e));
+                ca[e] = mul2(ca[e], two(weights.w, from + 2 * e));
                 sa[e] = mul2(sa[e], make_float2(weights.w[x.with], weights.w[y.with]));
             }
         }
     } else {
+        float w[16];
+        if constexpr (NORM) weights_of(weights, mine, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float2 c, s, wa = {1.0f, 1.0f}, wb = {1.0f, 1.0f};
-            angles.two(unit * 8 + 2 * i, &c, &s);
-            if constexpr (NORM) weights_of<L>(weights, at, i, &wa, &wb);
+            float2 c, s;
+            angles.at(mine.pair(2 * i), &c.x, &s.x);
+            angles.at(mine.pair(2 * i + 1), &c.y, &s.y);
+            const float2 wa = firsts<L>(w, i), wb = seconds<L>(w, i);
             ca[i] = NORM ? mul2(c, wa) : c;
             cb[i] = NORM ? mul2(c, wb) : c;
             sa[i] = NORM ? mul2(s, wa) : s;
@@ -486,8 +607,7 @@ __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forwa
         }
     }
     const float inverse_dim = 1.0f / float(p.dim);
-    // pairs of the lane that are turned, gathered: elements
-    const int turned = L == kGathered ? 2 * p.pairs - at.a : p.pairs - unit * 8;
+    const int turned = mine.turned();                  // gathered: elements
     int stage = 0, head = row.mine && has ? me.first : side.heads;
     for (int j = 0; j < me.turns; ++j, head += p.split, dst += dst_step) {
         copies_wait<kStages - 2>();
@@ -537,10 +657,7 @@ __global__ void __launch_bounds__(kThreads, L == kGathered ? 2 : 3) rotary_forwa
         };
         if (turned >= (L == kGathered ? 16 : 8)) turn(std::false_type());
         else turn(std::true_type());
-        if (head < side.heads) {
-            store_group(dst, f);
-            store_group(dst + to_b, f + 8);
-        }
+        if (head < side.heads) mine.put(dst, f);
     }
 }
 
@@ -549,10 +666,10 @@ template <typename T> using BackwardRing = Ring<T, 4, kBackwardStages<T>>;
 
 // Backward of the norm and the rotation: blocks that stay, each on rows of one side, with the weight's gradient in registers.  Two an
 // SM: a turn holds x, dy, angles, weights and sums of sixteen elements each, 120 registers and more.
-template <typename T, Layout L, bool PADDED>
+template <typename T, Layout L, bool PADDED, int GRAIN>
 __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kernel(const __grid_constant__ RotaryParams p)
 {
-    extern __shared__ __align__(16) char shared[];
+    extern __shared__ __align__(128) char shared[];
     __shared__ Pairs pairs;
     __shared__ __align__(16) Weights weights;
     constexpr int kStages = kBackwardStages<T>;
@@ -562,10 +679,9 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
     const Side &side = p.side[keys];
     const unsigned block = blockIdx.x - (keys ? p.side[0].blocks : 0u);
     const int heads = side.heads, lane = threadIdx.x % p.lanes;
-    const bool has = lane * 16 < p.dim;
-    const int unit = has ? lane : 0;
-    const Place at = wide_place<L>(p, unit);
-    const int to_b = at.b - at.a;
+    const Lane<T, L, GRAIN> own(p, lane);
+    const bool has = own.has;
+    const int from = own.start;
     const float inverse_dim = 1.0f / float(p.dim);
     __shared__ Sequences sequences[1];
     const Sequences *const seq = sequences;
@@ -582,14 +698,12 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
             if (ahead_new) {
                 const RowAt row(p, ahead.row(p, seq));
                 ahead_there = row.there && has;
-                src = row.in<T>(side.x) + ahead.head * side.x.head + at.a;
-                grad = row.in<T>(side.dy) + ahead.head * side.dy.head + at.a;
+                src = row.in<T>(side.x) + ahead.head * side.x.head + from;
+                grad = row.in<T>(side.dy) + ahead.head * side.dy.head + from;
             }
             if (ahead_there) {
-                ring.fetch(stage, 0, src);
-                ring.fetch(stage, 1, src + to_b);
-                ring.fetch(stage, 2, grad);
-                ring.fetch(stage, 3, grad + to_b);
+                ring.fetch(stage, 0, src, own);
+                ring.fetch(stage, 2, grad, own);
             } else {
                 ring.clear(stage);
             }
@@ -600,6 +714,8 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
         }
         copies_commit();
     };
+    if constexpr (GRAIN < 16)
+        for (int j = 0; j < kStages; ++j) ring.clear(j);
 #pragma unroll
     for (int j = 0; j < kStages - 1; ++j) fetch(j);
     pairs.fill(p);
@@ -608,14 +724,20 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
     constexpr int kCoefficients = L == kGathered ? 8 : 4;
     float2 wa[4], wb[4], da[4] = {}, db[4] = {};
     uint32_t offset[8];
-    if constexpr (L == kGathered) partner_offsets<BackwardRing<T>>(p, int(threadIdx.x) - lane, 2, at.a, offset);
+    if constexpr (L == kGathered) partner_offsets<BackwardRing<T>>(p, int(threadIdx.x) - lane, 2, from, offset);
+    {
+        float w[16];
+        weights_of(weights, own, w);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) weights_of<L>(weights, at, i, &wa[i], &wb[i]);
-    const int first_pair = L == kGathered ? Partner(p, at.a, true).pair : unit * 8;
+        for (int i = 0; i < 4; ++i) {
+            wa[i] = firsts<L>(w, i);
+            wb[i] = seconds<L>(w, i);
+        }
+    }
+    const int first_pair = L == kGathered ? Partner(p, from, true).pair : own.pair(0);
     unsigned long long position = position_at(p, RowAt(p, now.row(p, seq)), pairs.axis[first_pair]);
     float2 c[kCoefficients], s[kCoefficients];        // gathered: of an element and of its partner, with its sign
-    // pairs of the lane that are turned, gathered: elements
-    const int turned = L == kGathered ? 2 * p.pairs - at.a : p.pairs - unit * 8;
+    const int turned = own.turned();                   // gathered: elements
     T *dst = nullptr;
     bool mine = false, there = false, fresh = true;
     int stage = 0;
@@ -624,20 +746,23 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
             const RowAt row(p, now.row(p, seq));
             mine = row.mine && has;
             there = row.there && has;
-            dst = row.in<T>(side.out) + now.head * side.out.head + at.a;
+            dst = row.in<T>(side.out) + now.head * side.out.head + from;
             Angles angles{p, pairs, row, position, pairs.axis[first_pair]};
             position = position_at(p, RowAt(p, now.next_row(p, seq, heads)), pairs.axis[first_pair]);
             if constexpr (L == kGathered) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const Partner x(p, at.a + 2 * e, true), y(p, at.a + 2 * e + 1, true);
+                    const Partner x(p, from + 2 * e, true), y(p, from + 2 * e + 1, true);
                     angles.at(x.pair, &c[e].x, &s[e].x);
                     angles.at(y.pair, &c[e].y, &s[e].y);
                     s[e] = mul2(s[e], make_float2(x.sign, y.sign));
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) angles.two(unit * 8 + 2 * i, &c[i], &s[i]);
+                for (int i = 0; i < 4; ++i) {
+                    angles.at(own.pair(2 * i), &c[i].x, &s[i].x);
+                    angles.at(own.pair(2 * i + 1), &c[i].y, &s[i].y);
+                }
             }
         }
         copies_wait<kStages - 2>();
@@ -691,22 +816,16 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
             db[i] = fma2(nb, mul2(b, r), db[i]);
             put_pairs<L>(f, i, mul2(r, fma2(a, q, mul2(na, wa[i]))), mul2(r, fma2(b, q, mul2(nb, wb[i]))));
         }
-        if (mine) {
-            store_group(dst, f);
-            store_group(dst + to_b, f + 8);
-        }
+        if (mine) own.put(dst, f);
         dst += side.out.head;
         now.next(p, seq, heads);
         fresh = now.head == 0;
     }
     if constexpr (PADDED)
         absent_rows(p, side, block, [&](const RowAt &row) {
-            T *to = row.in<T>(side.out) + at.a;
-            const float zeros[8] = {};
-            for (int head = 0; has && head < heads; ++head, to += side.out.head) {
-                store_group(to, zeros);
-                store_group(to + to_b, zeros);
-            }
+            T *to = row.in<T>(side.out) + from;
+            const float zeros[16] = {};
+            for (int head = 0; has && head < heads; ++head, to += side.out.head) own.put(to, zeros);
         });
     copies_wait<0>();
     __syncthreads();
@@ -717,13 +836,13 @@ __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_wide_kern
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         const float v = warp_groups_sum(dw[e], p.lanes);
-        if (int(threadIdx.x % 32) < p.lanes && has) sums[threadIdx.x / 32 * p.dim + (e < 8 ? at.a + e : at.b + e - 8)] = v;
+        if (int(threadIdx.x % 32) < p.lanes && has && own.exists(e)) sums[threadIdx.x / 32 * p.dim + own.element(e)] = v;
     }
     __syncthreads();
     put_partial(p, sums, side.partial + (unsigned long long)block * p.dim);
 }
 
-// ---- any alignment: element by element, up to four pairs a lane in registers ------------------------------------------------------
+// ---- bfloat16 that no access of two elements fits: element by element, up to four pairs a lane in registers ----------------------
 
 constexpr int kOwn = kMaxPairs / 32;                  // pairs of a lane
 struct Own {
@@ -744,9 +863,9 @@ struct Own {
     }
 };
 
-template <typename T, bool NORM>
-__global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
+template <bool NORM> __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_constant__ RotaryParams p)
 {
+    using T = __nv_bfloat16;
     __shared__ Pairs pairs;
     constexpr int kAhead = 4;                         // heads in flight
     const bool keys = blockIdx.x >= p.side[0].blocks;
@@ -803,8 +922,9 @@ __global__ void __launch_bounds__(kThreads) rotary_forward_kernel(const __grid_c
     }
 }
 
-template <typename T, bool PADDED> __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
+template <bool PADDED> __global__ void __launch_bounds__(kThreads, kResident) rotary_backward_kernel(const __grid_constant__ RotaryParams p)
 {
+    using T = __nv_bfloat16;
     __shared__ Pairs pairs;
     __shared__ float sums[kWarps * OMNI_ROTARY_MAX_DIM];
     constexpr int kAhead = 2;
@@ -981,11 +1101,32 @@ View view_of(const omni_rotary *r, const omni_attn_view *v, int heads)
     return {v->data, r->batch > 1 ? v->batch : 0, r->length > 1 ? v->row : 0, heads > 1 ? v->head : 0};
 }
 
-// Whether every chunk of eight elements of an operand lies on a 16-byte boundary.
-bool wide_view(const omni_rotary *r, const View &v)
+// Whether every head vector of an operand begins on a boundary of `to` bytes.
+bool on_boundaries(const omni_rotary *r, const View &v, size_t to)
 {
     const size_t size = r->dtype == OMNI_BF16 ? 2 : 4;
-    return aligned(v.data, 16) && v.batch * size % 16 == 0 && v.row * size % 16 == 0 && v.head * size % 16 == 0;
+    return aligned(v.data, to) && v.batch * size % to == 0 && v.row * size % to == 0 && v.head * size % to == 0;
+}
+
+// The bytes of an access: the most that every head vector, and every half of one, allows; 0: element by element, which floats never need.  Halves that begin on no group of
+// eight run gathered where an access would be one element: forward, 5 x 2630, 32 heads on 8 of 64, float with 9 pairs turned 77 us gathered, 106 by 4
+// bytes; bfloat16 with 9 53, element by element 163, but with 20 56, by 8 bytes 37, and 2 x 4096 of 128 with 62 51, by 4 bytes 37.
+// Backward the float ones are 231 and 157, so there only odd halves of bfloat16 are left to it (107, element by element 225).
+int grain_of(const omni_rotary *r, std::initializer_list<const View *> views, bool backward)
+{
+    const auto all_on = [&](size_t to) {
+        for (const View *v : views)
+            if (!on_boundaries(r, *v, to)) return false;
+        return true;
+    };
+    const bool whole = r->dim % 16 == 0 && all_on(16);
+    if (whole && (r->interleaved || r->pairs % 8 == 0)) return 16;
+    for (int grain = 8; grain >= 4; grain /= 2) {
+        const int each = grain / (r->dtype == OMNI_BF16 ? 2 : 4);
+        if (whole && !backward && each == 1) return 16;
+        if (r->dim % each == 0 && (r->interleaved || r->pairs % each == 0) && all_on(grain)) return grain;
+    }
+    return whole ? 16 : 0;
 }
 
 // The launch: lanes of a head vector, how rows and heads are dealt, blocks of either side.
@@ -993,9 +1134,13 @@ struct Shape {
     int lanes, split;
     unsigned bundles, blocks[2];
 };
-int lanes_of(const omni_rotary *r, bool wide)
+int lanes_of(const omni_rotary *r, int grain)
 {
-    const int units = wide ? r->dim / 16 : r->dim / 2;
+    int units = r->dim / 2;
+    if (grain) {
+        const int each = grain / (r->dtype == OMNI_BF16 ? 2 : 4), rest = (r->dim - 2 * r->pairs) / each;
+        units = grain == 16 || r->interleaved ? (r->dim + 15) / 16 : (r->pairs + (rest + 1) / 2 * each + 7) / 8;
+    }
     int lanes = 1;
     while (lanes < units && lanes < 32) lanes *= 2;
     return lanes;
@@ -1003,9 +1148,9 @@ int lanes_of(const omni_rotary *r, bool wide)
 
 // Forward: a group has all heads of a row, so that every angle is made once; where there are few rows (decoding) groups share a row and
 // make its angles each.
-Shape forward_shape(const omni_rotary *r, bool wide, int sms)
+Shape forward_shape(const omni_rotary *r, int grain, int sms)
 {
-    Shape s = {lanes_of(r, wide), 1, 0, {0, 0}};
+    Shape s = {lanes_of(r, grain), 1, 0, {0, 0}};
     const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length);
     const int groups = kThreads / s.lanes, most = r->heads > r->kv_heads ? r->heads : r->kv_heads;
     while (s.split < groups && s.split < most && rows * s.split < uint64_t(sms) * groups * 2) s.split *= 2;
@@ -1016,9 +1161,9 @@ Shape forward_shape(const omni_rotary *r, bool wide, int sms)
 
 // Backward: as many blocks as are resident at once, shared between the sides by the work of a row, whose angles are about that of two
 // heads; where there is less work a warp has one turn.
-Shape backward_shape(const omni_rotary *r, bool wide, int sms)
+Shape backward_shape(const omni_rotary *r, int grain, int sms)
 {
-    Shape s = {lanes_of(r, wide), 1, 0, {0, 0}};
+    Shape s = {lanes_of(r, grain), 1, 0, {0, 0}};
     const uint64_t rows = uint64_t(r->batch) * uint64_t(r->length), of_bundle = 32 / s.lanes;
     s.bundles = unsigned((rows + of_bundle - 1) / of_bundle);
     const uint64_t all = uint64_t(sms) * kResident, q = r->heads + 2, k = r->kv_heads + 2;
@@ -1068,9 +1213,6 @@ void fill(RotaryParams *p, const omni_rotary *r, const Shape &s, bool backwards)
     for (int i = 0; i < 2; ++i) p->side[i].blocks = s.blocks[i];
 }
 
-// Sixteen elements a lane, in one of the three layouts.
-bool wide_units(const omni_rotary *r) { return r->dim % 16 == 0; }
-
 constexpr int kMostShared = 112 * 1024;               // dynamic shared memory of a block: two fit an SM
 
 int enqueue(omni_ctx *ctx, void (*kernel)(RotaryParams), const RotaryParams &p, size_t smem, cudaStream_t s)
@@ -1081,23 +1223,38 @@ int enqueue(omni_ctx *ctx, void (*kernel)(RotaryParams), const RotaryParams &p, 
     return context_launched(ctx, int(cudaGetLastError()));
 }
 
-template <typename T, bool NORM>
-int enqueue_forward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
+template <typename T, bool NORM, int GRAIN> void (*forward_kernel(const RotaryParams &p))(RotaryParams)
 {
-    if (!wide) return enqueue(ctx, rotary_forward_kernel<T, NORM>, p, 0, s);
-    return enqueue(ctx, p.interleaved ? rotary_forward_wide_kernel<T, kNeighbours, NORM> : p.pairs % 8 == 0 ? rotary_forward_wide_kernel<T, kHalves, NORM>
-                   : rotary_forward_wide_kernel<T, kGathered, NORM>, p, ForwardRing<T>::kBytes, s);
+    if (p.interleaved) return rotary_forward_wide_kernel<T, kNeighbours, NORM, GRAIN>;
+    if constexpr (GRAIN == 16)
+        if (p.pairs % 8) return rotary_forward_wide_kernel<T, kGathered, NORM, GRAIN>;
+    return rotary_forward_wide_kernel<T, kHalves, NORM, GRAIN>;
+}
+template <typename T, bool NORM> int enqueue_forward(omni_ctx *ctx, const RotaryParams &p, int grain, cudaStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (!grain) return enqueue(ctx, rotary_forward_kernel<NORM>, p, 0, s);
+    return enqueue(ctx, grain == 16 ? forward_kernel<T, NORM, 16>(p) : grain == 8 ? forward_kernel<T, NORM, 8>(p) : forward_kernel<T, NORM, 4>(p), p,
+                   ForwardRing<T>::kBytes, s);
 }
 
-template <typename T, bool PADDED> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
+template <typename T, bool PADDED, int GRAIN> void (*backward_kernel(const RotaryParams &p))(RotaryParams)
 {
-    if (!wide) return enqueue(ctx, rotary_backward_kernel<T, PADDED>, p, 0, s);
-    return enqueue(ctx, p.interleaved ? rotary_backward_wide_kernel<T, kNeighbours, PADDED> : p.pairs % 8 == 0 ? rotary_backward_wide_kernel<T, kHalves, PADDED>
-                   : rotary_backward_wide_kernel<T, kGathered, PADDED>, p, BackwardRing<T>::kBytes, s);
+    if (p.interleaved) return rotary_backward_wide_kernel<T, kNeighbours, PADDED, GRAIN>;
+    if constexpr (GRAIN == 16 && sizeof(T) == 2)
+        if (p.pairs % 8) return rotary_backward_wide_kernel<T, kGathered, PADDED, GRAIN>;
+    return rotary_backward_wide_kernel<T, kHalves, PADDED, GRAIN>;
 }
-template <typename T> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, bool wide, cudaStream_t s)
+template <typename T, bool PADDED> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, int grain, cudaStream_t s)
 {
-    return p.padded ? enqueue_backward<T, true>(ctx, p, wide, s) : enqueue_backward<T, false>(ctx, p, wide, s);
+    if constexpr (sizeof(T) == 2)
+        if (!grain) return enqueue(ctx, rotary_backward_kernel<PADDED>, p, 0, s);
+    return enqueue(ctx, grain == 16 ? backward_kernel<T, PADDED, 16>(p) : grain == 8 ? backward_kernel<T, PADDED, 8>(p) : backward_kernel<T, PADDED, 4>(p), p,
+                   BackwardRing<T>::kBytes, s);
+}
+template <typename T> int enqueue_backward(omni_ctx *ctx, const RotaryParams &p, int grain, cudaStream_t s)
+{
+    return p.padded ? enqueue_backward<T, true>(ctx, p, grain, s) : enqueue_backward<T, false>(ctx, p, grain, s);
 }
 
 // One pass over both sides without sums: the forward call, and the gradient where there are no weights.
@@ -1105,18 +1262,17 @@ int rotate(omni_ctx *ctx, const omni_rotary *r, const omni_attn_view *const (&in
            const ContextDevice &dev, void *stream)
 {
     RotaryParams p;
-    bool wide = wide_units(r);
     for (int i = 0; i < 2; ++i) {
         const int heads = i ? r->kv_heads : r->heads;
         p.side[i] = {view_of(r, in[i], heads), {}, view_of(r, out[i], heads), nullptr, nullptr, 0, 0};
-        wide = wide && wide_view(r, p.side[i].x) && wide_view(r, p.side[i].out);
     }
-    fill(&p, r, forward_shape(r, wide, dev.sm_count), backwards);
+    const int grain = grain_of(r, {&p.side[0].x, &p.side[0].out, &p.side[1].x, &p.side[1].out}, false);
+    fill(&p, r, forward_shape(r, grain, dev.sm_count), backwards);
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const bool norm = r->q_weight && !backwards;
     if (r->dtype == OMNI_BF16)
-        return norm ? enqueue_forward<__nv_bfloat16, true>(ctx, p, wide, s) : enqueue_forward<__nv_bfloat16, false>(ctx, p, wide, s);
-    return norm ? enqueue_forward<float, true>(ctx, p, wide, s) : enqueue_forward<float, false>(ctx, p, wide, s);
+        return norm ? enqueue_forward<__nv_bfloat16, true>(ctx, p, grain, s) : enqueue_forward<__nv_bfloat16, false>(ctx, p, grain, s);
+    return norm ? enqueue_forward<float, true>(ctx, p, grain, s) : enqueue_forward<float, false>(ctx, p, grain, s);
 }
 
 
@@ -1199,13 +1355,12 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
     if (!empty) {
         RotaryParams p;
         const omni_attn_view *const x[2] = {q, k}, *const dy[2] = {dq_out, dk_out}, *const dx[2] = {dq, dk};
-        bool wide = wide_units(r);
         for (int i = 0; i < 2; ++i) {
             const int heads = i ? r->kv_heads : r->heads;
             p.side[i] = {view_of(r, x[i], heads), view_of(r, dy[i], heads), view_of(r, dx[i], heads), nullptr, nullptr, 0, 0};
-            wide = wide && wide_view(r, p.side[i].x) && wide_view(r, p.side[i].dy) && wide_view(r, p.side[i].out);
         }
-        const Shape shape = backward_shape(r, wide, dev.sm_count < kMostSms ? dev.sm_count : kMostSms);
+        const int grain = grain_of(r, {&p.side[0].x, &p.side[0].dy, &p.side[0].out, &p.side[1].x, &p.side[1].dy, &p.side[1].out}, true);
+        const Shape shape = backward_shape(r, grain, dev.sm_count < kMostSms ? dev.sm_count : kMostSms);
         fill(&p, r, shape, false);
         p.overlap = dev.overlap;
         p.side[0].partial = static_cast<float *>(workspace);
@@ -1214,7 +1369,7 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
             w.partial[i] = p.side[i].partial;
             w.blocks[i] = shape.blocks[i];
         }
-        rc = r->dtype == OMNI_BF16 ? enqueue_backward<__nv_bfloat16>(ctx, p, wide, s) : enqueue_backward<float>(ctx, p, wide, s);
+        rc = r->dtype == OMNI_BF16 ? enqueue_backward<__nv_bfloat16>(ctx, p, grain, s) : enqueue_backward<float>(ctx, p, grain, s);
         if (rc != OMNI_OK) return rc;
     }
     Dependent launch(dev, dim3((r->dim + kJoin - 1) / kJoin, 2), 1024, 0, s);

@@ -295,6 +295,39 @@ def test_what_is_not_turned_stays_as_it_is(ctx, dtype, interleaved, d, pairs):
         assert torch.equal(t[..., 2 * pairs:].nan_to_num(7.0), q[..., 2 * pairs:].nan_to_num(7.0)) and int(t.isnan().sum()) == 1
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("shift", [0, 1, 2, 4])
+@pytest.mark.parametrize("d,pairs", [(84, 42), (82, 41), (82, 40), (128, 20), (20, 10), (36, 18), (36, 4), (250, 123), (252, 126), (256, 126), (256, 127), (4, 1),
+                                     (8, 4), (66, 1)])
+def test_accesses_of_every_width(ctx, dtype, interleaved, shift, d, pairs):
+    """Heads whose size, halves and boundaries allow 16, 8, 4 or 2 bytes at a time, among storage that stays as it is."""
+    b, n, h, hk = 3, 41, 3, 2
+    axes = [i % 2 for i in range(pairs)]
+    r = L.Rotary(ctx, h, hk, d, L.Rotary.geometric(pairs), axes=axes, interleaved=interleaved)
+    q, k, positions, weights = inputs(b, n, h, hk, d, dtype, d + pairs, dtype, axes=r.axes)
+    lengths = torch.tensor([n, 0, 17], device="cuda", dtype=torch.int32)
+
+    def place(heads):
+        strides = (n * heads * d + shift, heads * d, d, 1)
+        store = torch.full((shift + b * strides[0] + 16,), 5.0, device="cuda", dtype=dtype)
+        return store, store.as_strided((b, n, heads, d), strides, shift)
+
+    stores, places = zip(*(place(x) for x in (h, hk, h, hk)))
+    inputs_at = tuple(p.copy_(x) for p, x in zip(places[2:], (q, k)))
+    for w in (weights, (None, None)):
+        check(ctx, *inputs_at, positions, w, r, axes, lengths)
+        out = r.forward(*inputs_at, positions, *w, lengths=lengths, out=places[:2])
+        back = r.backward(*inputs_at, positions, q, k, *w, lengths=lengths)
+        assert all(torch.equal(x, y) for x, y in zip(out, r.forward(*inputs_at, positions, *w, lengths=lengths)))
+        same = r.backward(*inputs_at, positions, q, k, *w, lengths=lengths, grads=places[:2])
+        assert all(torch.equal(x, y) for x, y in zip(back[:2], same))
+    for store, at in zip(stores, places):
+        untouched = torch.ones_like(store, dtype=torch.bool)
+        untouched.as_strided(at.shape, at.stride(), shift).fill_(False)
+        assert bool((store[untouched] == 5.0).all())
+
+
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_gradient_against_differences(ctx, interleaved):
     q, k, positions, weights = inputs(1, 4, 3, 1, 32, F32, 10, F32)
