@@ -14,7 +14,8 @@
 // threads of a row follow its bytes: 32 for 8 KB (16384 x 1000 bfloat16 30 us, with 128 threads 53), 512 for 128 KB and more (3000 x 131072
 // 301 us, with 256 threads 338).
 // Tried for the step: the row held in shared memory, two CTAs of 512 an SM 329 us, the same with the next row's loads behind the gradient 339; a batch
-// of loads in registers instead of the asynchronous ones 327.
+// of loads in registers instead of the asynchronous ones 327.  A cluster of CTAs for each row above 128 KB, whatever their number: 68 x 168451 float
+// 30 instead of 44 us, but 3000 x 131072 bfloat16 331 instead of 298 and its log-probabilities 180 instead of 129.
 #include "context.h"
 #include "row_softmax.cuh"
 

@@ -61,7 +61,9 @@ template <> struct Group<__nv_bfloat16> {
 constexpr float kFar = 16777216.0f;                  // of a row's m: from here on its rounding is a factor of two and more
 
 template <bool FAR> struct Running {
-    float m = -INFINITY;
+    // Near zero it begins where far begins: a thread that sees nothing but a mask of -1e30 would have the power of two of that product's rounding,
+    // an overflow, and infinity times the ratio of 0 to the row's maximum is no number.
+    float m = FAR ? -INFINITY : -kFar;
     float2 a = {0.0f, 0.0f}, b = {0.0f, 0.0f};
     template <typename T, int K> __device__ __forceinline__ void take(const Group<T> (&g)[K], float unit)
     {
@@ -97,7 +99,7 @@ template <bool FAR> struct Running {
     }
     __device__ __forceinline__ float sum() const { return __fadd_rn(__fadd_rn(a.x, a.y), __fadd_rn(b.x, b.y)); }
     // what is added to an exponent; -inf - -inf would be no number
-    __device__ __forceinline__ static float reference(float m) { return m == -INFINITY ? 0.0f : -m; }
+    __device__ __forceinline__ static float reference(float m) { return FAR && m == -INFINITY ? 0.0f : -m; }
     // of a sum over `from` to one over `to`
     __device__ __forceinline__ static float ratio(float from, float to, float unit) { return exp2_fast(FAR ? __fmul_rn(from - to, unit) : from - to); }
 };
@@ -117,7 +119,7 @@ __device__ __forceinline__ float warp_sum(float x)
 template <bool FAR> __device__ __forceinline__ Joined join_warp(float own, float s, float unit)
 {
     const float m = warp_max(own);
-    return {m, warp_sum(m == -INFINITY || own == m ? s : __fmul_rn(s, Running<FAR>::ratio(own, m, unit)))};
+    return {m, warp_sum((FAR && m == -INFINITY) || own == m ? s : __fmul_rn(s, Running<FAR>::ratio(own, m, unit)))};
 }
 // A warp's maximum and sum into its cell.
 template <bool FAR> __device__ __forceinline__ void put_warp(const Running<FAR> &run, float unit, Joined *cell)
