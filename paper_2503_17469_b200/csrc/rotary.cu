@@ -20,6 +20,8 @@
 // Heads or halves that no 16-byte access fits take 8 or 4 bytes at a time, the lanes of a head side by side (sixteen elements in a row
 // to a lane: up to twice the time, from the pieces of sectors that are stored): 4751 rows of 16 heads on 4 of 84 bfloat16 18 us (floor 5), backward 29
 // (7), 2 x 4096 of 16 on 8 of 250 float 90 (60) and 143 (90).  Element by element those took 37, 51, 91 and 138.
+// Tried forward: a group that has a row's queries and keys with one set of angles 61 us where two groups take 58 (1 + 1 heads of 128, 27990 rows, 16
+// instead of 20).
 // Tried for the backward kernel: loads by registers 111 us; angles of a tile in shared memory between barriers 68-82; weights and angles read from
 // shared memory at each turn for a third block an SM 84 (spills); groups of five lanes for a head of 80 39 instead of 36.
 #include "context.h"
