@@ -7,7 +7,8 @@
 // A CTA owns a row.  The first walk keeps a running maximum and sum per thread; its groups come by asynchronous copies, 128 bytes a
 // thread in flight, into places of the thread's own.  The second finds the row, which the same CTA read a moment ago, in L2, and marks its
 // lines as the first to leave.  A row whose weight is zero (its ratio is clipped) is not walked again: zeros are written.
-// What bounds it: the gradient alone the memory (4096 x 32000 float 154 us, 6.8 TB/s); log-probabilities the memory beside one exponential an
+// What bounds it: the gradient alone the memory (4096 x 32000 float 154 us, 6.8 TB/s; rows that are walked for their sum first 181, 8192 x 50257
+// bfloat16 349 for 263); log-probabilities the memory beside one exponential an
 // element, 74 % of the special-function units (3000 x 131072 bfloat16 122-135 us, floor 120); the step two exponentials and two reads of L2 (8192 x
 // 50257 bfloat16, rows on 2-byte boundaries, 287 us, 323 when the 1000 W cap has brought the clock down to 1.6 GHz; floor 252).
 // Rows in flight have to stay in L2 between their walks: four CTAs of 256 an SM (59 MB) 287 us, five 336, six 372, three 309.  So the
@@ -102,17 +103,17 @@ template <typename T> struct Places {
 };
 template <int LEFT> __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// Takes groups i .. of the thread from their places.
-template <typename T> __device__ __forceinline__ void take_step(Running<false> &run, const Places<T> &at, int i, int own, int from, int walkers, float unit)
+// Takes groups i .. of the thread's `own`, group(k) being i + k: the order of a row's sum, in every call.
+template <typename T, typename F> __device__ __forceinline__ void take_step(Running<false> &run, int i, int own, float unit, F group)
 {
     constexpr int kStep = Places<T>::kStep;
     if (i + kStep <= own) {
         Group<T> x[kStep];
 #pragma unroll
-        for (int k = 0; k < kStep; ++k) x[k] = at.group(from + k, walkers);
+        for (int k = 0; k < kStep; ++k) x[k] = group(k);
         run.take(x, unit);
     } else if (i < own) {
-        Group<T> x[1] = {at.group(from, walkers)};
+        Group<T> x[1] = {group(0)};
         run.take(x, unit);
     }
 }
@@ -189,22 +190,22 @@ __device__ __forceinline__ void put_row(const PolicyParams &p, T *out, const Row
     if (tid == owner) out[t.token] = from_float<T>(at_token(weight, q(t.z)));     // over what the same thread wrote
 }
 
-// What follows from a row's log-sum-exp and its token's log-probability: the results, and the weight of the gradient.
-template <bool STEP> __device__ __forceinline__ float finish(const PolicyParams &p, unsigned r, const Sample &t, float lse, float logp)
+// What follows from a row's log-sum-exp and its token's log-probability: the results (backward has none), and the weight of the gradient.
+template <int MODE> __device__ __forceinline__ float finish(const PolicyParams &p, unsigned r, const Sample &t, float lse, float logp)
 {
-    const Value v = t.there() && (STEP || p.loss) ? value_of(p, t, logp) : Value{0.0f, 0.0f};
-    if (threadIdx.x == 0) {
+    const Value v = t.there() && (MODE != kForward || p.loss) ? value_of(p, t, logp) : Value{0.0f, 0.0f};
+    if (MODE != kBackward && threadIdx.x == 0) {
         p.lse_out[r] = lse;
         p.logp[r] = t.there() ? logp : 0.0f;
         if (p.loss) p.loss[r] = v.loss;
     }
-    return STEP ? __fdiv_rn(__fmul_rn(t.grad_loss, v.slope), p.temperature) : 0.0f;
+    return MODE != kForward ? __fdiv_rn(__fmul_rn(t.grad_loss, v.slope), p.temperature) : 0.0f;
 }
 
 template <typename T> __device__ __forceinline__ T *gradient_of(const PolicyParams &p, unsigned r) { return static_cast<T *>(p.grad) + r * p.grad_stride; }
 
 // A row far from zero from its start, by the whole CTA.
-template <typename T, bool STEP> __device__ __forceinline__ void far_row(const PolicyParams &p, unsigned r, const Row<T> &w, const Sample &t, Joined *cell)
+template <typename T, int MODE> __device__ __forceinline__ void far_row(const PolicyParams &p, unsigned r, const Row<T> &w, const Sample &t, Joined *cell)
 {
     const float unit = kLog2e / p.temperature;
     __syncthreads();                                  // the cells have been read
@@ -214,40 +215,42 @@ template <typename T, bool STEP> __device__ __forceinline__ void far_row(const P
     const bool nothing = all.m == -INFINITY && all.s == 0.0f;           // a row of -inf: no token has a probability
     const float log_sum = __fmul_rn(log2f(all.s), kLn2);
     const float logp = nothing ? -INFINITY : __fsub_rn(__fsub_rn(t.z, all.m) / p.temperature, log_sum);
-    const float weight = finish<STEP>(p, r, t, __fadd_rn(all.m / p.temperature, log_sum), logp);
-    if constexpr (STEP)
+    const float weight = finish<MODE>(p, r, t, __fadd_rn(all.m / p.temperature, log_sum), logp);
+    if constexpr (MODE != kForward)
         put_row<1>(p, gradient_of<T>(p, r), w, t, Softmax<false>{1.0f, Running<true>::reference(all.m), unit, nothing ? 0.0f : -weight / all.s}, weight);
 }
 
 // A row near zero: its results; the gradient's softmax and weight.
 struct Ending { Softmax<true> q; float weight; };
-template <bool STEP> __device__ __forceinline__ Ending near_row(const PolicyParams &p, unsigned r, const Sample &t, const Joined &all, float unit)
+template <int MODE> __device__ __forceinline__ Ending near_row(const PolicyParams &p, unsigned r, const Sample &t, const Joined &all, float unit)
 {
     const float log_sum = log2f(all.s);
     // the token's exponent less the maximum first: what is added up is all distances
     const float logp = __fmul_rn(__fsub_rn(__fmaf_rn(t.z, unit, -all.m), log_sum), kLn2);
-    const float weight = finish<STEP>(p, r, t, __fmul_rn(__fadd_rn(all.m, log_sum), kLn2), logp);
+    const float weight = finish<MODE>(p, r, t, __fmul_rn(__fadd_rn(all.m, log_sum), kLn2), logp);
     return {{unit, -all.m, 1.0f, -weight / all.s}, weight};
 }
 
-// From a kept lse: one walk.
-template <typename T, typename I> __global__ void __launch_bounds__(kMostWalkers, 2) policy_backward_kernel(const __grid_constant__ PolicyParams p)
+// From the threads' maxima and sums of a row to its results and its gradient.
+template <typename T> constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;       // groups a thread has in flight in the second walk
+template <typename T, int MODE>
+__device__ __forceinline__ void end_row(const PolicyParams &p, unsigned r, const Row<T> &w, const Sample &t, const Running<false> &run, float unit, Joined *cell)
 {
-    constexpr int kAhead = sizeof(T) == 2 ? 4 : 2;    // groups a thread has in flight
-    const unsigned r = blockIdx.x;
-    const Row<T> w(static_cast<const T *>(p.logits) + r * p.row_stride, p.vocab, blockDim.x);
-    const Sample t = sample_of<T, I>(p, w.row, r, true);
-    const float lse = p.lse_in[r];
-    const float logp = __fsub_rn(t.z / p.temperature, lse);
-    const float slope = t.there() ? value_of(p, t, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
-    const float weight = __fdiv_rn(__fmul_rn(t.grad_loss, slope), p.temperature);
-    __syncthreads();                                  // every thread has the token's logit: the gradient may be written over it
-    put_row<kAhead>(p, gradient_of<T>(p, r), w, t, Softmax<false>{1.0f / p.temperature, lse == -INFINITY ? 0.0f : -lse, kLog2e, -weight}, weight);
+    __syncwarp();
+    put_warp(run, unit, cell + threadIdx.x / 32);
+    __syncthreads();
+    const Joined all = join_cells<false>(cell, w.walkers / 32, unit);         // every warp finds the same
+    if (!(fabsf(all.m) < kFar)) {
+        far_row<T, MODE>(p, r, w, t, cell);
+        return;
+    }
+    const Ending end = near_row<MODE>(p, r, t, all, unit);
+    if constexpr (MODE != kForward) put_row<kAhead<T>>(p, gradient_of<T>(p, r), w, t, end.q, end.weight);
 }
 
 // A CTA a row; a few places go round.  The gradient of a step finds the row in L2.
 template <typename T> constexpr int kRound = sizeof(T) == 2 ? 8 : 4;       // places of a thread
-template <typename T, typename I, bool STEP> __global__ void __launch_bounds__(kMostWalkers, 2) policy_kernel(const __grid_constant__ PolicyParams p)
+template <typename T, typename I, int MODE> __global__ void __launch_bounds__(kMostWalkers, 2) policy_kernel(const __grid_constant__ PolicyParams p)
 {
     extern __shared__ __align__(16) char shared[];
     __shared__ Joined cell[kMostWalkers / 32];
@@ -258,25 +261,48 @@ template <typename T, typename I, bool STEP> __global__ void __launch_bounds__(k
     const int own = own_groups(w);
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) at.ask(w, own, i * kStep, i * kStep);
-    const Sample t = sample_of<T, I>(p, w.row, r, STEP);
+    const Sample t = sample_of<T, I>(p, w.row, r, MODE == kStep);
     const float unit = kLog2e / p.temperature;
     Running<false> run;
     if (w.edge() >= 0) run.take_one(to_float(w.row[w.edge()]), unit);
     for (int i = 0; i < own; i += kStep) {
         arrived<kSteps - 1>();
-        take_step(run, at, i, own, i % kRound<T>, w.walkers, unit);
+        take_step<T>(run, i, own, unit, [&](int k) { return at.group(i % kRound<T> + k, w.walkers); });
         at.ask(w, own, i + kRound<T>, i % kRound<T>);
     }
-    __syncwarp();
-    put_warp(run, unit, cell + threadIdx.x / 32);
-    __syncthreads();
-    const Joined all = join_cells<false>(cell, w.walkers / 32, unit);         // every warp finds the same
-    if (!(fabsf(all.m) < kFar)) {
-        far_row<T, STEP>(p, r, w, t, cell);
+    end_row<T, MODE>(p, r, w, t, run, unit, cell);
+}
+
+// From a kept lse: one walk.  Its rounding is a factor of 1 + 2^-24 |lse| of every probability, and far from zero the row's sum is lost
+// in it altogether; so from kKept on (the logits of a model in use are well below), the row is walked once more for its sum, in the order of the
+// other calls.
+constexpr float kKept = 128.0f;
+template <typename T, typename I> __global__ void __launch_bounds__(kMostWalkers, 2) policy_backward_kernel(const __grid_constant__ PolicyParams p)
+{
+    __shared__ Joined cell[kMostWalkers / 32];
+    const unsigned r = blockIdx.x;
+    const Row<T> w(static_cast<const T *>(p.logits) + r * p.row_stride, p.vocab, blockDim.x);
+    const Sample t = sample_of<T, I>(p, w.row, r, true);
+    const float lse = p.lse_in[r];
+    if (t.there() && !(fabsf(lse) < kKept)) {
+        const float unit = kLog2e / p.temperature;
+        Running<false> run;
+        if (w.edge() >= 0) run.take_one(to_float(w.row[w.edge()]), unit);
+        const int own = own_groups(w);
+        for (int i = 0; i < own; i += Places<T>::kStep)
+            take_step<T>(run, i, own, unit, [&](int k) {
+                Group<T> x;
+                x.load(w.row + w.parts.head + (long long)(threadIdx.x + (i + k) * w.walkers) * kGroup);
+                return x;
+            });
+        end_row<T, kBackward>(p, r, w, t, run, unit, cell);
         return;
     }
-    const Ending end = near_row<STEP>(p, r, t, all, unit);
-    if constexpr (STEP) put_row<sizeof(T) == 2 ? 4 : 2>(p, gradient_of<T>(p, r), w, t, end.q, end.weight);
+    const float logp = __fsub_rn(t.z / p.temperature, lse);
+    const float slope = t.there() ? value_of(p, t, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
+    const float weight = __fdiv_rn(__fmul_rn(t.grad_loss, slope), p.temperature);
+    __syncthreads();                                  // every thread has the token's logit: the gradient may be written over it
+    put_row<kAhead<T>>(p, gradient_of<T>(p, r), w, t, Softmax<false>{1.0f / p.temperature, -lse, kLog2e, -weight}, weight);
 }
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -313,7 +339,7 @@ template <typename T, typename I> int enqueue(omni_ctx *ctx, int mode, const Pol
         return context_launched(ctx, int(cudaGetLastError()));
     }
     const size_t bytes = size_t(kRound<T>) * walkers * Places<T>::kSize;
-    void (*const kernel)(PolicyParams) = mode == kStep ? policy_kernel<T, I, true> : policy_kernel<T, I, false>;
+    void (*const kernel)(PolicyParams) = mode == kStep ? policy_kernel<T, I, kStep> : policy_kernel<T, I, kForward>;
     constexpr int kMost = kRound<T> * kMostWalkers * Places<T>::kSize;
     const int rc = bytes > 40 * 1024 ? context_shared(ctx, reinterpret_cast<const void *>(kernel), kMost) : OMNI_OK;
     if (rc != OMNI_OK) return rc;

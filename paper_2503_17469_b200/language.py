@@ -542,7 +542,8 @@ class Policy(_Operator):
         return loss, logp, lse
 
     def backward(self, logits, tokens, lse, old, advantage, grad_loss, reference=None, grad=None, stream=None):
-        """Gradient of the logits from ``lse`` of the forward call and ``grad_loss`` [rows]; ``grad`` may be ``logits``."""
+        """Gradient of the logits from ``lse`` of the forward call and ``grad_loss`` [rows]; ``grad`` may be ``logits``.  Rows that are far from
+        zero (an ``lse`` of 128 and more) take their own sum instead, in one more walk."""
         if stream is not None:
             with self._on_stream(stream):
                 return self.backward(logits, tokens, lse, old, advantage, grad_loss, reference, grad)
