@@ -1,5 +1,5 @@
-"""The policy loss's gradient from a kept log-sum-exp where that float says little: rows far from zero.  Against the definition in 64 bits, as
-the step's gradient of the same rows.
+"""The policy loss's gradient from a kept log-sum-exp where that float says little: rows far from zero, and ratios next to a border.
+Against the definition in 64 bits, and against the step's gradient of the same rows.
 
 Tolerances, as in the distillation loss's test of far logits.  A probability depends on distances from the row's largest logit M only, D_v =
 (M - z_v) / T in powers of two: three roundings of 2^-24 D and 2^-21 for the hardware's 2^x; the sum S over the row is off by the mean
@@ -13,6 +13,8 @@ import torch
 
 from paper_2503_17469_b200 import binding as B
 from paper_2503_17469_b200 import language as L
+
+from test_gpu_policy import inputs as near_inputs
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
@@ -84,3 +86,29 @@ def test_rows_far_from_zero(ctx, dtype, temp, vocab):
         # the last row is near zero, where the kept lse is what the gradient is taken from
         err = (got.double() - want).abs()[:10]
         assert bool((err <= room[:10]).all()), (err - room[:10]).amax(1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("temp", TEMPERATURES)
+@pytest.mark.parametrize("clip,high", [(0.0, None), (0.0, 0.5), (0.2, 0.28), (1.0, 0.0)])
+def test_ratios_next_to_a_border(ctx, dtype, temp, clip, high):
+    """What forward counts as not clipped has its gradient from either call, a few steps of the float around a border."""
+    p = L.Policy(ctx, clip, high, 0.0, temp)
+    z, tokens, _, advantage, _, gl = near_inputs(4000, 100, dtype, torch.int64, 11, p)
+    logp, lse = p.logprob(z, tokens)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for border in (1.0, 1 - p.clip, 1 + p.clip_high):
+        if border <= 0:
+            continue
+        old = logp - math.log(border)
+        for steps in (0, 4):
+            shift = torch.randint(-steps, steps + 1, old.shape, device="cuda", generator=gen)
+            close = old + shift * (old.abs() + 1) * 2.0 ** -24
+            grad = p.step(z, tokens, close, advantage, gl)[3].double()
+            kept = p.backward(z, tokens, lse, close, advantage, gl).double()
+            assert torch.equal(kept.abs().amax(1) > 0, grad.abs().amax(1) > 0)
+            # twice `e` of test_gpu_policy.py, which is below 2^-16 for logits of this size
+            room = 1.5 * (gl * advantage / temp).double().abs()[:, None] * 2.0 ** -15 + 2 * ROUND[dtype] * grad.abs()
+            assert bool(((kept - grad).abs() <= room).all())
+        if border == 1.0:
+            assert torch.equal(p.backward(z, tokens, lse, old, advantage, gl).abs().amax(1) > 0, tokens >= 0)
