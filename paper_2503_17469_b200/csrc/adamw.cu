@@ -13,7 +13,7 @@
 //
 // A table of the tensors in device memory names the owner of each 1024 elements: one launch, whatever their number; a warp has a block, a lane
 // eight elements.  Every load of a lane stands before whatever waits for one (a widening between them cost a quarter of the time).
-// What bounds it: with float moments the memory (140 million elements, bfloat16 gradients and copy, 571 us, 6.8 TB/s; floor 597 at the copy
+// What bounds it: with float moments the memory (140 million elements, bfloat16 gradients and copy, 574 us, 6.8 TB/s; floor 597 at the copy
 // rate); with 8 bits the whole-number units, at 70 % (73 million elements 213 us, floor 180; four workers' gradients 270, floor 248), which is
 // why codes are packed four at a time and shifts are written as products.  Their values as floats take 113 us more (floor 112).
 // Tried for 8 bits: CTAs that stay with a ring of asynchronous copies 274-480 us; two units a CTA 272; eight or ten CTAs an SM 223 and 220
@@ -158,9 +158,15 @@ template <int MOST> __device__ __forceinline__ uint32_t encode4(const uint32_t *
                                        __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
     return MOST == 255 ? word : word | (word + 0x7f7f7f7fu & 0x80808080u & signs);           // a code of 0 has no sign
 }
-// Within 2^-22 of the root and of the inverse; numbers below float's normal range count as 0.
-__device__ __forceinline__ float root(float x)
+// Root and quotient of m / fma(sqrt(v), spread, eps).  Rounded correctly they hide behind the memory with float moments (140 million 574 us, with the
+// short forms 571), but make the 8-bit step 228 us instead of 205 (73 million): there short forms stand in, within 2^-22 each.  Those count numbers
+// below float's normal range as 0, which changes the divisor by less than 2^-63 spread; with an eps between 2^-41 spread and 2^100 that is
+// below 2^-22 of it, and no inverse leaves float's range.  Spread is largest in the first step, so an eps of 1e-8 has the short forms up to
+// a beta2 of 1 - 2^-28.
+bool short_forms(double eps, double beta2) { return eps >= 0x1p-41 / std::sqrt(1.0 - beta2) && eps <= 0x1p100; }
+template <bool SHORT> __device__ __forceinline__ float root(float x)
 {
+    if (!SHORT) return __fsqrt_rn(x);
     float y;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
@@ -170,6 +176,11 @@ __device__ __forceinline__ float inverse(float x)
     float y;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+template <bool SHORT> __device__ __forceinline__ float2 quotient(float2 x, float2 y)
+{
+    if (!SHORT) return make_float2(__fdiv_rn(x.x, y.x), __fdiv_rn(x.y, y.y));
+    return mul2(x, {inverse(y.x), inverse(y.y)});
 }
 
 // 32 bits of an element's own, by multiplications and shifts of its number, its tensor's and the step's.
@@ -264,7 +275,7 @@ template <typename G> __device__ __forceinline__ void aggregate_some(const AdamP
     }
 }
 
-template <typename G, int BITS> __global__ void __launch_bounds__(kThreads, BITS == 8 ? 9 : 7) adamw_kernel(const __grid_constant__ AdamParams p)
+template <typename G, int BITS, bool SHORT> __global__ void __launch_bounds__(kThreads, BITS == 8 ? 9 : 7) adamw_kernel(const __grid_constant__ AdamParams p)
 {
     const Entry *entry;
     const Place x(p, blockIdx.x, entry);
@@ -313,8 +324,8 @@ template <typename G, int BITS> __global__ void __launch_bounds__(kThreads, BITS
         const float2 d = {g[i], g[i + 1]}, t = {theta[i], theta[i + 1]};
         const float2 m1 = fma2({p.b1, p.b1}, {m[i], m[i + 1]}, mul2({p.c1, p.c1}, d));
         const float2 v1 = fma2(mul2({p.c2, p.c2}, d), d, mul2({p.b2, p.b2}, {v[i], v[i + 1]}));
-        const float2 below = fma2({root(v1.x), root(v1.y)}, {now.spread, now.spread}, {p.eps, p.eps});
-        const float2 t1 = fma2({-now.rate, -now.rate}, mul2(m1, {inverse(below.x), inverse(below.y)}), mul2({keep, keep}, t));
+        const float2 below = fma2({root<SHORT>(v1.x), root<SHORT>(v1.y)}, {now.spread, now.spread}, {p.eps, p.eps});
+        const float2 t1 = fma2({-now.rate, -now.rate}, quotient<SHORT>(m1, below), mul2({keep, keep}, t));
         m[i] = m1.x; m[i + 1] = m1.y;
         v[i] = v1.x; v[i + 1] = v1.y;
         theta[i] = t1.x; theta[i + 1] = t1.y;
@@ -465,8 +476,9 @@ const Header *header_of(const void *record)
 
 template <typename G> void launch(const AdamParams &p, int bits, unsigned units, cudaStream_t s)
 {
-    if (bits == 8) adamw_kernel<G, 8><<<units, kThreads, 0, s>>>(p);
-    else adamw_kernel<G, 32><<<units, kThreads, 0, s>>>(p);
+    if (bits == 32) adamw_kernel<G, 32, false><<<units, kThreads, 0, s>>>(p);
+    else if (short_forms(p.eps, p.beta2)) adamw_kernel<G, 8, true><<<units, kThreads, 0, s>>>(p);
+    else adamw_kernel<G, 8, false><<<units, kThreads, 0, s>>>(p);
 }
 
 }  // namespace
