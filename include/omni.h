@@ -543,8 +543,8 @@ typedef struct {
  * writes their gradients, dim values each of weight_grad_dtype (zeros if there are no rows), and needs a workspace (device,
  * 16-byte aligned, omni_rotary_workspace() bytes); without weights q, k, the weight gradients and the workspace are not looked at.
  * Sums over rows are added in an order that the sizes alone decide.
- * Errors: NULL, BAD_CONFIG (sizes, dim odd, pairs, axes, dtype, eps, a frequency that is not finite, a result's stride below dim), ALIGN,
- * TOO_LARGE (dim, batch * length >= 2^31, heads > 65535, strides >= 2^40, a workspace below the size asked for), CUDA. */
+ * Errors: NULL, BAD_CONFIG (sizes, dim odd, pairs, axes, dtype, eps, a frequency that is not finite, a result's stride below dim, results
+ * that write an element twice or share one with each other), ALIGN, TOO_LARGE (dim, batch * length >= 2^31, heads > 65535, strides >= 2^40, a workspace below the size asked for), CUDA. */
 int omni_rotary_forward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_view *q, const omni_attn_view *k,
                         const omni_attn_view *q_out, const omni_attn_view *k_out, void *stream);
 int omni_rotary_workspace(const omni_rotary *r, uint64_t *bytes);

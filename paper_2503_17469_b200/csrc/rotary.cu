@@ -30,6 +30,7 @@
 #include <cmath>
 #include <initializer_list>
 #include <type_traits>
+#include <utility>
 
 namespace omni {
 namespace {
@@ -1092,10 +1093,79 @@ int check_view(const omni_rotary *r, const omni_attn_view *v, int heads, bool wr
     const struct { int extent; uint64_t stride; } axis[3] = {{r->batch, v->batch}, {r->length, v->row}, {heads, v->head}};
     for (const auto &a : axis) {
         if (a.extent <= 1) continue;
-        if (a.stride >= (1ull << 40)) return OMNI_ERR_TOO_LARGE;
+        if (a.stride >= (1ull << 40) || (written && a.stride > (1ull << 57) / unsigned(a.extent))) return OMNI_ERR_TOO_LARGE;
         if (written && a.stride < uint64_t(r->dim)) return OMNI_ERR_BAD_CONFIG;      // rows that a result would write twice
     }
     return OMNI_OK;
+}
+
+// Whether what a call writes is written once.  Two head vectors of dim elements share one if their distance, a sum of one multiple of each stride, is below dim
+// either way.  The strides are tried from the largest on, and of each the multiples that the smaller ones can still bring back: where the smaller
+// ones' extents fit into a stride, as in any slice of a larger tensor, that is three multiples at most.
+class Distances {
+    struct Axis { int64_t stride, low, high; } axis[6];      // multiples from low to high
+    int64_t low[7], high[7], dim;                     // what the axes from i on add at least and at most
+    int count = 0, steps = 1 << 16;                   // layouts that take more are refused
+
+    bool meet(int i, int64_t from, bool apart)
+    {
+        if (from + low[i] >= dim || from + high[i] <= -dim) return false;
+        if (i == count) return apart;
+        if (--steps < 0) return true;
+        const Axis &a = axis[i];
+        if (from == 0 && a.stride + low[i + 1] >= dim && high[i + 1] - a.stride <= -dim) return meet(i + 1, 0, apart);       // only 0 of them
+        // below (dim - from - low) / stride and above (-dim - from - high) / stride: by division towards 0, one too many at either end
+        const int64_t first = (-dim - from - high[i + 1]) / a.stride - 1, last = (dim - from - low[i + 1]) / a.stride + 1;
+        for (int64_t m = first > a.low ? first : a.low; m <= a.high && m <= last; ++m)
+            if (meet(i + 1, from + m * a.stride, apart || m != 0)) return true;
+        return false;
+    }
+
+public:
+    explicit Distances(const omni_rotary *r) : dim(r->dim) {}
+    // Multiples of a stride from low to high; those of one stride in two results are one axis, of two axes of one result they are not.
+    void add(uint64_t stride, int64_t from, int64_t to, bool join)
+    {
+        if (from == to) return;
+        int i = 0;
+        while (i < count && axis[i].stride > int64_t(stride)) ++i;
+        if (!join || i == count || axis[i].stride != int64_t(stride)) {
+            for (int j = count++; j > i; --j) axis[j] = axis[j - 1];
+            axis[i] = {int64_t(stride), 0, 0};
+        }
+        axis[i].low += from;
+        axis[i].high += to;
+    }
+    // What a result's indices add to a distance that begins (away) or ends (back) at one of its vectors.
+    void add(const omni_rotary *r, const omni_attn_view *v, int heads, int away, int back, bool join)
+    {
+        const std::pair<int, uint64_t> all[3] = {{r->batch, v->batch}, {r->length, v->row}, {heads, v->head}};
+        for (const auto &[extent, stride] : all) add(stride, -int64_t(extent - 1) * away, int64_t(extent - 1) * back, join);
+    }
+    // apart: the vectors are of two results, `from` apart at first.
+    bool meet(int64_t from, bool apart)
+    {
+        low[count] = high[count] = 0;
+        for (int i = count - 1; i >= 0; --i) {
+            low[i] = low[i + 1] + axis[i].low * axis[i].stride;
+            high[i] = high[i + 1] + axis[i].high * axis[i].stride;
+        }
+        return meet(0, from, apart);
+    }
+};
+int check_written_once(const omni_rotary *r, const omni_attn_view *q, const omni_attn_view *k)
+{
+    if (uint64_t(r->batch) * uint64_t(r->length) == 0) return OMNI_OK;
+    for (const auto &[v, heads] : {std::pair(q, r->heads), std::pair(k, r->kv_heads)}) {
+        Distances own(r);
+        own.add(r, v, heads, 1, 1, false);
+        if (own.meet(0, false)) return OMNI_ERR_BAD_CONFIG;
+    }
+    Distances both(r);
+    both.add(r, q, r->heads, 1, 0, true);
+    both.add(r, k, r->kv_heads, 0, 1, true);
+    const int64_t bytes = int64_t(reinterpret_cast<uintptr_t>(k->data) - reinterpret_cast<uintptr_t>(q->data));
+    return both.meet(bytes / (r->dtype == OMNI_BF16 ? 2 : 4), true) ? OMNI_ERR_BAD_CONFIG : OMNI_OK;
 }
 
 View view_of(const omni_rotary *r, const omni_attn_view *v, int heads)
@@ -1301,6 +1371,7 @@ int omni_rotary_forward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vie
     if (rc == OMNI_OK) rc = check_view(r, k, r->kv_heads, false);
     if (rc == OMNI_OK) rc = check_view(r, q_out, r->heads, true);
     if (rc == OMNI_OK) rc = check_view(r, k_out, r->kv_heads, true);
+    if (rc == OMNI_OK) rc = check_written_once(r, q_out, k_out);
     if (rc != OMNI_OK) return rc;
     ContextDevice dev;
     rc = context_bind(ctx, &dev);
@@ -1340,6 +1411,8 @@ int omni_rotary_backward(omni_ctx *ctx, const omni_rotary *r, const omni_attn_vi
         if (!aligned(dq_weight, size) || !aligned(dk_weight, size) || !aligned(workspace, 16)) return OMNI_ERR_ALIGN;
         if (bytes < workspace_bytes(r)) return OMNI_ERR_TOO_LARGE;
     }
+    rc = check_written_once(r, dq, dk);
+    if (rc != OMNI_OK) return rc;
     ContextDevice dev;
     rc = context_bind(ctx, &dev);
     if (rc != OMNI_OK) return rc;
