@@ -41,7 +41,7 @@ struct omni_ctx {
     omni::LaunchShape overwrite_shape[2][2];            // [dtype][wide]
     omni::LaunchShape bulk_overwrite_shape[2];          // [dtype], ring kernel as push with overwrite
     omni::LaunchShape seq_shape[2][2][OMNI_MAX_ASP_BATCH + 1];  // [dtype][wide][M]
-    const void *opted[32] = {};                         // kernels opted into their dynamic shared memory (context_shared)
+    const void *opted[128] = {};                        // kernels opted into their dynamic shared memory (context_shared): all of the library, 71
     int n_opted = 0;
 };
 
