@@ -119,8 +119,8 @@ class Student:
         gen = torch.Generator(device=device).manual_seed(seed)
         n = self.layout.total
         self.theta = torch.zeros(n, device=device)
-        for part, shape in zip(self.views(self.theta), cfg.shapes):
-            if shape[0] == 2 and cfg.rotary:
+        for i, (part, shape) in enumerate(zip(self.views(self.theta), cfg.shapes)):
+            if i == 3:                                                                  # the norms' weights
                 part.fill_(1.0)
                 continue
             part.normal_(0.0, cfg.dim ** -0.5 if shape[0] == cfg.vocab else shape[0] ** -0.5, generator=gen)
