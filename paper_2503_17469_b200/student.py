@@ -217,12 +217,14 @@ class Student:
         mean = reward.sum() / there.sum()
         return Samples(batch.tokens, batch.lengths, actions, old, ref, (reward - mean) * there, mean)
 
-    def step(self, batches, throughputs: Sequence[float], lr: float, momentum: float = 0.9) -> torch.Tensor:
-        """One iteration of Algorithm 1: every worker's gradient, then aggregation, update and re-batch."""
+    def step(self, batches, throughputs: Sequence[float], lr: float, momentum: Optional[float] = None) -> torch.Tensor:
+        """One iteration of Algorithm 1: every worker's gradient, then aggregation, update and re-batch.  ``momentum`` is SGD's, 0.9 by default."""
+        if momentum is not None and self.adamw is not None:
+            raise ValueError("momentum: AdamW has none")
         used = self.omni.batches
         losses = torch.stack([self.gradient(k, b) for k, b in enumerate(batches)])
         if self.adamw is None:
-            self.omni.step_bsp(self.buckets, throughputs, lr, momentum)
+            self.omni.step_bsp(self.buckets, throughputs, lr, 0.9 if momentum is None else momentum)
         else:
             self.adamw.step(lr, used)
             self.omni.rebatch(throughputs)
