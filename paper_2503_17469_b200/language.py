@@ -652,6 +652,8 @@ class AdamW(_Operator):
             batches = (1,)
         if len(batches) != self.K:
             raise ValueError(f"batches: {self.K} of them are wanted")
+        if sum(batches) >> 31 and any(b >> 31 not in (0, -1) for b in batches):       # the sum first: a fifth of the time
+            raise _too_large()
         if self._at != _device():
             raise _elsewhere(params=self._record_dev)
         at = None
