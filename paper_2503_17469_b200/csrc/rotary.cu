@@ -188,11 +188,11 @@ struct Sequences {
     {
         if (threadIdx.x >= 32) return;
         const int lane = threadIdx.x, each = (p.batch + 31) / 32, first = min(lane * each, p.batch), last = min(first + each, p.batch);
-        const int rows = 32 / p.lanes;
+        const unsigned rows = 32 / p.lanes;
         int sum = 0;
         for (int b = first; b < last; ++b) {
             before[b] = sum;                          // of this lane's
-            sum += (min(max(p.lengths[b], 0), int(p.length)) + rows - 1) / rows;
+            sum += (min(unsigned(max(p.lengths[b], 0)), p.length) + rows - 1) / rows;        // unsigned: may pass 31 bits
         }
         int ahead = sum;
         for (int o = 1; o < 32; o *= 2) {
