@@ -143,7 +143,7 @@ __device__ __forceinline__ void put_row(const DistillParams &p, const Row<T> &w,
     const bool target = te.target;
     if (tid < walkers) {
         if (!target) {
-            for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(0.0f);
+            for (unsigned v = tid; v < unsigned(p.vocab); v += walkers) out[v] = from_float<T>(0.0f);
         } else if (same_phase(out, w.row)) {
             walk<AHEAD>(w, [&](int g, const auto &x) {
 #pragma unroll
@@ -152,7 +152,7 @@ __device__ __forceinline__ void put_row(const DistillParams &p, const Row<T> &w,
             });
             if (w.edge() >= 0) out[w.edge()] = from_float<T>(q(to_float(w.row[w.edge()])));
         } else {
-            for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(q(to_float(w.row[v])));
+            for (unsigned v = tid; v < unsigned(p.vocab); v += walkers) out[v] = from_float<T>(q(to_float(w.row[v])));
         }
     }
     __syncthreads();

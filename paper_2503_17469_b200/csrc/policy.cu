@@ -185,7 +185,7 @@ __device__ __forceinline__ void put_row(const PolicyParams &p, T *out, const Row
         if (w.edge() >= 0) out[w.edge()] = from_float<T>(q(to_float(w.row[w.edge()])));
         owner = owner_of(w, t.token);
     } else {
-        for (int v = tid; v < p.vocab; v += walkers) out[v] = from_float<T>(q(to_float(w.row[v])));
+        for (unsigned v = tid; v < unsigned(p.vocab); v += walkers) out[v] = from_float<T>(q(to_float(w.row[v])));
     }
     if (tid == owner) out[t.token] = from_float<T>(at_token(weight, q(t.z)));     // over what the same thread wrote
 }
