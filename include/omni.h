@@ -623,7 +623,7 @@ typedef struct {
  * NULL, the int64 that clock_dev (device, 8-byte aligned) holds when the kernel runs, for a step that is captured in a graph; lr is the host's.
  * omni_adamw_moments: what the codes stand for, into m[i], v[i] (HOST arrays of device float pointers, one for each tensor); 8 bits only.
  * Errors: NULL, BAD_K, BAD_CONFIG (dtype, bits, what is written overlaps other tensors, not a record, lr or weight_decay not finite, beta outside [0, 1), eps, step < 1), BAD_BATCH,
- * ALIGN, TOO_LARGE (a tensor of 2^42 elements, 2^31 pieces of 2048 in all, a record that is too small), NO_MEMORY, CUDA. */
+ * ALIGN, TOO_LARGE (a tensor of 2^42 elements, 2^31 pieces of 1024 in all, a record that is too small), NO_MEMORY, CUDA. */
 int omni_adamw_plan_bytes(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, uint64_t *bytes);
 int omni_adamw_plan(const omni_adamw_tensor *tensors, int32_t count, int32_t K, int32_t grad_dtype, int32_t bits, void *record, uint64_t bytes);
 int omni_adamw_step(omni_ctx *ctx, const void *record, const void *record_dev, const int32_t *b, double lr, double beta1, double beta2,

@@ -78,16 +78,13 @@ struct AdamParams {
     float lambda[OMNI_MAX_K];
 };
 
-// Eight elements, or those of them before the end one by one.
-template <typename T> __device__ __forceinline__ void load8(const T *p, bool wide, int count, float *f)
+// Eight elements, those before the end, one by one.
+template <typename T> __device__ __forceinline__ void load8(const T *p, int count, float *f)
 {
-    if (wide && count == kGroup) {
-        load_group(p, f);
-        return;
-    }
 #pragma unroll
     for (int i = 0; i < kGroup; ++i) f[i] = i < count ? to_float(p[i]) : 0.0f;
 }
+// Eight elements, or those of them before the end one by one.
 template <typename T> __device__ __forceinline__ void store8(T *p, bool wide, int count, const float *f)
 {
     if (wide && count == kGroup) {
@@ -183,7 +180,9 @@ template <bool SHORT> __device__ __forceinline__ float2 quotient(float2 x, float
     return mul2(x, {inverse(y.x), inverse(y.y)});
 }
 
-// 32 bits of an element's own, by multiplications and shifts of its number, its tensor's and the step's.
+// 32 bits of an element's own, by multiplications and shifts of its number, its tensor's and the step's.  The multipliers are published constants of
+// integer hashing: 2^32 over the golden ratio and two primes of its kind for the start, and the first of the two rounds (16, 0x7FEB352D, 15) of C. Wellons'
+// search for mixers with little bias; one round is enough for bits that round.
 constexpr uint32_t kStride = 0x9E3779B1u;
 __device__ __forceinline__ uint32_t scramble(uint32_t x)
 {
@@ -269,7 +268,7 @@ template <typename G> __device__ __forceinline__ void aggregate_some(const AdamP
 {
     for (int k = 0; k < p.K; ++k) {
         float f[kGroup];
-        load8(static_cast<const G *>(p.grads[(unsigned long long)x.tensor * p.K + k]) + x.at, false, x.count, f);
+        load8(static_cast<const G *>(p.grads[(unsigned long long)x.tensor * p.K + k]) + x.at, x.count, f);
 #pragma unroll
         for (int i = 0; i < kGroup; ++i) g[i] = __fmaf_rn(p.lambda[k], f[i], k ? g[i] : 0.0f);
     }
@@ -303,10 +302,10 @@ template <typename G, int BITS, bool SHORT> __global__ void __launch_bounds__(kT
     if (x.whole) {
         aggregate(p, x, first, g);
     } else {
-        load8(e.param + x.at, false, x.count, theta);
+        load8(e.param + x.at, x.count, theta);
         if constexpr (BITS == 32) {
-            load8(fm, false, x.count, m);
-            load8(fv, false, x.count, v);
+            load8(fm, x.count, m);
+            load8(fv, x.count, v);
         } else {
             codes_m = load_codes(cm, false, x.count);
             codes_v = load_codes(cv, false, x.count);

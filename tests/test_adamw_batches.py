@@ -1,4 +1,4 @@
-"""Batch sizes that the library takes as 32 bits are refused, not cut: without a GPU."""
+"""Batch sizes that the library takes as 32 bits are refused, not cut, and where its limit on elements lies: without a GPU."""
 import ctypes as C
 
 import pytest
@@ -40,3 +40,12 @@ def test_sizes_of_32_bits(op):
     for batches in ((1, 2), ((1 << 31) - 1, 7), [3, 4]):
         op.step(1e-3, batches)
     assert op.steps == 3 and op._lib.batches == [[1, 2], [(1 << 31) - 1, 7], [3, 4]]
+
+
+def test_pieces_of_all_tensors():
+    """Fewer than 2^31 of 1024 elements."""
+    at, need, grads = 1 << 20, C.c_uint64(), (C.c_void_p * 1)(1 << 20)
+    for sizes, status in (([(1 << 41) - 1024], B.OK), ([(1 << 41) - 1023], B.ERR_TOO_LARGE), ([1 << 40, (1 << 40) - 1024], B.OK),
+                          ([1 << 40, (1 << 40) - 1024, 1], B.ERR_TOO_LARGE)):
+        tensors = (B.omni_adamw_tensor * len(sizes))(*(B.omni_adamw_tensor(at, None, grads, at, at, at, n, 0.0) for n in sizes))
+        assert B.lib().omni_adamw_plan_bytes(tensors, len(sizes), 1, B.F32, 8, C.byref(need)) == status
