@@ -596,8 +596,8 @@ int omni_policy_step(omni_ctx *ctx, const omni_policy *d, const float *grad_loss
  *   g = fma(lambda_{K-1}, g_{K-1}, ... fma(lambda_0, g_0, 0));  m = fma(beta1, m, c1 g);  v = fma(c2 g, g, beta2 v)
  *   theta = fma(-rate, m / fma(sqrt(v), spread, eps), keep theta);  param_lp = bfloat16(theta)
  * c = float(1 - beta), rate = float(lr / (1 - beta1^t)), spread = float((1 - beta2^t)^(-1/2)), keep = float(1 - lr weight_decay), t = 1,
- * 2, ... the step's number.  m and v are exact, with float moments theta is as well.  With 8 bits and an eps between 2^-41 (1 - beta2)^(-1/2) and
- * 2^100 the quotient, its root included, is off by up to 2^-20.5 of itself.  An eps of 0 is allowed: the quotient of a v of 0 is not finite then.
+ * 2, ... the step's number.  m and v are exact.  With an eps between 2^-41 (1 - beta2)^(-1/2) and 2^100 the quotient, its root
+ * included, is off by up to 2^-20.5 of itself, with any other theta is exact too.  An eps of 0 is allowed: the quotient of a v of 0 is not finite then.
  * bits = 8: m and v are kept as codes of the float's bits 20 to 30 (exponent and three bits of the fraction), counted from the largest
  * of their block of OMNI_ADAMW_BLOCK consecutive elements.  With top the block's largest, a code c > 0 is the float of bits (c + top - 127) << 20
  * for m, bit 7 of the byte its sign, and (c + top - 255) << 20 for v; c = 0 is 0.  theta is computed from m and v before they are

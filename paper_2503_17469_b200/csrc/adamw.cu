@@ -13,7 +13,7 @@
 //
 // A table of the tensors in device memory names the owner of each 1024 elements: one launch, whatever their number; a warp has a block, a lane
 // eight elements.  Every load of a lane stands before whatever waits for one (a widening between them cost a quarter of the time).
-// What bounds it: with float moments the memory (140 million elements, bfloat16 gradients and copy, 574 us, 6.8 TB/s; floor 597 at the copy
+// What bounds it: with float moments the memory (140 million elements, bfloat16 gradients and copy, 570 us, 6.8 TB/s; floor 597 at the copy
 // rate); with 8 bits the whole-number units, at 70 % (73 million elements 213 us, floor 180; four workers' gradients 270, floor 248), which is
 // why codes are packed four at a time and shifts are written as products.  Their values as floats take 113 us more (floor 112).
 // Tried for 8 bits: CTAs that stay with a ring of asynchronous copies 274-480 us; two units a CTA 272; eight or ten CTAs an SM 223 and 220
@@ -155,11 +155,11 @@ template <int MOST> __device__ __forceinline__ uint32_t encode4(const uint32_t *
                                        __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
     return MOST == 255 ? word : word | (word + 0x7f7f7f7fu & 0x80808080u & signs);           // a code of 0 has no sign
 }
-// Root and quotient of m / fma(sqrt(v), spread, eps).  Rounded correctly they hide behind the memory with float moments (140 million 574 us, with the
-// short forms 571), but make the 8-bit step 228 us instead of 205 (73 million): there short forms stand in, within 2^-22 each.  Those count numbers
-// below float's normal range as 0, which changes the divisor by less than 2^-63 spread; with an eps between 2^-41 spread and 2^100 that is
-// below 2^-22 of it, and no inverse leaves float's range.  Spread is largest in the first step, so an eps of 1e-8 has the short forms up to
-// a beta2 of 1 - 2^-28.
+// Root and quotient of m / fma(sqrt(v), spread, eps): short forms, within 2^-22 each, which a step of the usual size loses in theta's own rounding.
+// Rounded correctly they take a small model's step from 6.0 to 6.5 us, 140 million with float moments from 570 to 574 and 73 million with 8
+// bits from 205 to 228.  The short forms count numbers below float's normal range as 0, which changes the divisor by less than
+// 2^-63 spread; with an eps between 2^-41 spread and 2^100 that is below 2^-22 of it, and no inverse leaves float's range.  Spread is largest in the
+// first step, so an eps of 1e-8 has the short forms up to a beta2 of 1 - 2^-28.  Any other eps has the correct ones.
 bool short_forms(double eps, double beta2) { return eps >= 0x1p-41 / std::sqrt(1.0 - beta2) && eps <= 0x1p100; }
 template <bool SHORT> __device__ __forceinline__ float root(float x)
 {
@@ -473,11 +473,15 @@ const Header *header_of(const void *record)
     return h->magic == kMagic && h->bytes == Layout(h->tensors, h->K, h->units).bytes ? h : nullptr;
 }
 
+template <typename G, int BITS> void launch(const AdamParams &p, unsigned units, cudaStream_t s)
+{
+    if (short_forms(p.eps, p.beta2)) adamw_kernel<G, BITS, true><<<units, kThreads, 0, s>>>(p);
+    else adamw_kernel<G, BITS, false><<<units, kThreads, 0, s>>>(p);
+}
 template <typename G> void launch(const AdamParams &p, int bits, unsigned units, cudaStream_t s)
 {
-    if (bits == 32) adamw_kernel<G, 32, false><<<units, kThreads, 0, s>>>(p);
-    else if (short_forms(p.eps, p.beta2)) adamw_kernel<G, 8, true><<<units, kThreads, 0, s>>>(p);
-    else adamw_kernel<G, 8, false><<<units, kThreads, 0, s>>>(p);
+    if (bits == 8) launch<G, 8>(p, units, s);
+    else launch<G, 32>(p, units, s);
 }
 
 }  // namespace

@@ -1,6 +1,6 @@
 """AdamW with any eps: moments below float's normal range keep their root, and no quotient overflows that float can hold.  Bounds:
-those of test_gpu_adamw.py; with float moments every operation is rounded once, which 64 bits and one more rounding show (but for a
-probability of 2^-29 a value)."""
+those of test_gpu_adamw.py; where eps is not between 2^-41 (1 - beta2)^(-1/2) and 2^100 every operation is rounded once, which 64 bits and
+one more rounding show (but for a probability of 2^-29 a value)."""
 import math
 
 import pytest
@@ -59,8 +59,8 @@ def test_no_gradient_moves_nothing(ctx, bits, eps):
 
 
 @pytest.mark.parametrize("shift", [0, 1])
-@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-20, 1e-8, 1.0])
-def test_parameters_with_float_moments_bit_by_bit(ctx, shift, eps):
+@pytest.mark.parametrize("eps", [0.0, 1e-40, 1e-20, 1e-13, 1e31])
+def test_parameters_bit_by_bit(ctx, shift, eps):
     c = Case(ctx, [3000, 257, 5], 1, F32, 32, shift=shift, eps=eps)
     for t in (1, 2):
         sizes_of_all_kinds(c)
