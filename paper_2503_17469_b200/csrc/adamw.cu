@@ -181,7 +181,7 @@ template <bool SHORT> __device__ __forceinline__ float2 quotient(float2 x, float
 }
 
 // 32 bits of an element's own, by multiplications and shifts of its number, its tensor's and the step's.  The multipliers are published constants of
-// integer hashing: 2^32 over the golden ratio and two primes of its kind for the start, and the first of the two rounds (16, 0x7FEB352D, 15) of C. Wellons'
+// integer hashing: the prime next to 2^32 over the golden ratio and two others for the start, and the first of the two rounds (16, 0x7FEB352D, 15) of C. Wellons'
 // search for mixers with little bias; one round is enough for bits that round.
 constexpr uint32_t kStride = 0x9E3779B1u;
 __device__ __forceinline__ uint32_t scramble(uint32_t x)

@@ -15,7 +15,7 @@
 // take 58.  Backward: blocks that stay, so that a weight's gradient is summed in registers and 296 partial sums are joined by a second launch;
 // the turns of all rows (of a padded batch those before the lengths alone) are dealt to the warps in equal parts.
 // Measured: 4 x 4096, 32 heads on 8 of 128 bfloat16, forward 58 us (floor 51); backward 2 x 8192, 16 heads on 8 of 128, 61 us (floor 46): the
-// kernel 53, bound by its 320 instructions a turn at 58 % of the issue slots (16 warps an SM at 128 registers), the join 5; 6 x 1777 of 80, float,
+// kernel 53, bound by latency that 16 warps an SM, at 128 registers, do not cover (issue 58 %, DRAM 61 %), the join 5; 6 x 1777 of 80, float,
 // padded, a quarter of the rows there, 36 us; a single token of 16 sequences 4.6 us.
 // Heads or halves that no 16-byte access fits take 8 or 4 bytes at a time, the lanes of a head side by side (sixteen elements in a row
 // to a lane: up to twice the time, from the pieces of sectors that are stored): 4751 rows of 16 heads on 4 of 84 bfloat16 18 us (floor 5), backward 29

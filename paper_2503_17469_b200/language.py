@@ -574,7 +574,8 @@ class AdamW(_Operator):
 
     ``params``: float32 tensors; ``grads[i][k]``: worker k's gradient of tensor i, float32 or bfloat16; ``copies``: bfloat16 tensors
     that receive the rounded parameters, or None.  All contiguous, of the current device, and kept alive by this object, which
-    notes where they lie: they are updated in place and are not to be replaced.  ``weight_decay``: one for all or one for each.
+    notes where they lie: they are updated in place and are not to be replaced, and a graph that a step was captured into needs the object
+    for as long as it is replayed.  ``weight_decay``: one for all or one for each.
     ``bits``: 32, or 8 for moments in one byte each with stochastic rounding (formats and formulas in ``include/omni.h``).
     ``state``: (m, v) float32 tensors, or (m, v, tops) uint8, uint8 and int16 [blocks, 2], for each tensor, to go on from; zeros
     by default.  ``state`` and ``steps`` (how many have been made) are what a checkpoint holds."""
