@@ -577,8 +577,9 @@ typedef struct {
 } omni_policy;
 /* omni_policy_logprob: logp[rows] and lse[rows] (device float) alone; old, advantage, reference, clip and kl are not looked at.
  * omni_policy_forward: loss, logp, lse.  omni_policy_backward: grad (rows x vocab of the logits' dtype, grad_stride apart) from the
- * kept lse and grad_loss[rows] (a row whose |lse| is 128 or more, or whose ratio is within that float's rounding of a border, is walked once more
- * for its own sum: its gradient is the step's, with the side of the border that forward found); omni_policy_step: both in one pass over the logits, for a caller that knows grad_loss beforehand.
+ * kept lse and grad_loss[rows]; a row whose |lse| or token's |z_t / T| is 128 or more, or whose ratio is within that float's rounding of a border, is
+ * walked once more for its own sum: its gradient is the step's, on the side of the border that forward found.
+ * omni_policy_step: both in one pass over the logits, for a caller that knows grad_loss beforehand.
  * logp and lse are the same bits from the three calls that return them: the ratio to an `old` that one of them gave is exactly 1.
  * grad may be the logits' own storage (same pointer and stride).  A gradient whose rows lie to 16-byte boundaries as the logits' do
  * is written in groups of eight, any other element by element.

@@ -274,15 +274,16 @@ template <typename T, typename I, int MODE> __global__ void __launch_bounds__(kM
 }
 
 // From a kept lse: one walk.  Its rounding is a factor of 1 + 2^-24 |lse| of every probability, and far from zero the row's sum is lost
-// in it altogether; so from kKept on (the logits of a model in use are well below), the row is walked once more for its sum, in the order of the
-// other calls.
+// in it altogether, as a token's log-probability is in its difference from a logit that is far off.  So from kKept on (the logits of a model
+// in use are well below) the row is walked once more for its sum, in the order of the other calls.
 constexpr float kKept = 128.0f;
 // Nor does the kept lse say on which side of a border a ratio stands that is within its rounding: 1 itself with a clip of 0, where forward's ratio is exact
-// and half of such rows would lose their gradient.  The two log-probabilities are within 10 x 2^-24 (|z / T| + |lse|) of each other, and either's
-// ratio is off by 4 x 2^-24 and half a rounding of the exponent.
-__device__ __forceinline__ bool next_to_border(const PolicyParams &p, const Sample &t, float lse, float logp)
+// and half of such rows would lose their gradient.  The two log-probabilities are within 10 x 2^-24 (|z / T| + |lse|) of each other, which
+// kKept keeps below 2^-12, and either's ratio is off by 4 x 2^-24 and half a rounding of the exponent.
+__device__ __forceinline__ bool says_too_little(const PolicyParams &p, const Sample &t, float lse, float z, float logp)
 {
-    const float x = __fsub_rn(logp, t.old), ratio = expf(x), room = ratio * 0x1p-20f * (fabsf(t.z / p.temperature) + fabsf(lse) + fabsf(x) + 1.0f);
+    if (!(fabsf(lse) < kKept && fabsf(z) < kKept)) return true;
+    const float x = __fsub_rn(logp, t.old), ratio = expf(x), room = ratio * 0x1p-20f * (fabsf(z) + fabsf(lse) + fabsf(x) + 1.0f);
     return t.advantage != 0.0f && (fabsf(ratio - p.low) <= room || fabsf(ratio - p.high) <= room);
 }
 template <typename T, typename I> __global__ void __launch_bounds__(kMostWalkers, 2) policy_backward_kernel(const __grid_constant__ PolicyParams p)
@@ -292,8 +293,8 @@ template <typename T, typename I> __global__ void __launch_bounds__(kMostWalkers
     const Row<T> w(static_cast<const T *>(p.logits) + r * p.row_stride, p.vocab, blockDim.x);
     const Sample t = sample_of<T, I>(p, w.row, r, true);
     const float lse = p.lse_in[r];
-    const float logp = __fsub_rn(t.z / p.temperature, lse);
-    if (t.there() && (!(fabsf(lse) < kKept) || next_to_border(p, t, lse, logp))) {
+    const float z = t.z / p.temperature, logp = __fsub_rn(z, lse);
+    if (t.there() && says_too_little(p, t, lse, z, logp)) {
         const float unit = kLog2e / p.temperature;
         Running<false> run;
         if (w.edge() >= 0) run.take_one(to_float(w.row[w.edge()]), unit);
@@ -307,7 +308,7 @@ template <typename T, typename I> __global__ void __launch_bounds__(kMostWalkers
         end_row<T, kBackward>(p, r, w, t, run, unit, cell);
         return;
     }
-    const float slope = t.there() ? value_of(p, t, t.z == -INFINITY ? -INFINITY : logp).slope : 0.0f;
+    const float slope = t.there() ? value_of(p, t, logp).slope : 0.0f;
     const float weight = __fdiv_rn(__fmul_rn(t.grad_loss, slope), p.temperature);
     __syncthreads();                                  // every thread has the token's logit: the gradient may be written over it
     put_row<kAhead<T>>(p, gradient_of<T>(p, r), w, t, Softmax<false>{1.0f / p.temperature, -lse, kLog2e, -weight}, weight);

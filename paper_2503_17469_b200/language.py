@@ -543,7 +543,7 @@ class Policy(_Operator):
 
     def backward(self, logits, tokens, lse, old, advantage, grad_loss, reference=None, grad=None, stream=None):
         """Gradient of the logits from ``lse`` of the forward call and ``grad_loss`` [rows]; ``grad`` may be ``logits``.  Rows that are far from
-        zero (an ``lse`` of 128 and more), or whose ratio stands within rounding of a border, take their own sum instead, in one more walk."""
+        zero (an ``lse`` or a token's logit of 128 and more), or whose ratio stands within rounding of a border, take their own sum instead, in one more walk."""
         if stream is not None:
             with self._on_stream(stream):
                 return self.backward(logits, tokens, lse, old, advantage, grad_loss, reference, grad)

@@ -112,3 +112,23 @@ def test_ratios_next_to_a_border(ctx, dtype, temp, clip, high):
             assert bool(((kept - grad).abs() <= room).all())
         if border == 1.0:
             assert torch.equal(p.backward(z, tokens, lse, old, advantage, gl).abs().amax(1) > 0, tokens >= 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("temp", TEMPERATURES)
+def test_tokens_far_below_their_row(ctx, dtype, temp):
+    """The row is near zero, the sampled token masked by a large number: its log-probability is lost in a difference of floats as well.  The ratio to an
+    `old` of the same call is that call's, so the gradient is the step's to the bit."""
+    p = L.Policy(ctx, 0.2, 0.28, 0.05, temp)
+    masks = [-300.0, -3e3, -1e5, -3e7, -1e9, -1e30, torch.finfo(dtype).min, -math.inf]
+    rows = 20 * len(masks)
+    z, tokens, _, advantage, _, gl = near_inputs(rows, 1000, dtype, torch.int64, 12, p)
+    tokens = tokens.clamp(min=0)
+    z[torch.arange(rows), tokens] = torch.tensor(masks, device="cuda").repeat_interleave(20).to(dtype)
+    logp, lse = p.logprob(z, tokens)
+    assert float(lse.abs().max()) < 64
+    old, reference = logp - 0.1, logp.clamp(min=-1e38) + 0.3
+    grad = p.step(z, tokens, old, advantage, gl, reference)[3]
+    kept = p.backward(z, tokens, lse, old, advantage, gl, reference)
+    same = (kept == grad) | (kept.isnan() & grad.isnan())
+    assert bool(same.all()), (~same).any(1).nonzero()[:, 0]
